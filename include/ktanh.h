@@ -297,6 +297,97 @@ ktanh_status_t klstm_cell64_backward(const uint16_t *gates, const float *c_prev,
                                      const float *dc_next, uint16_t *dgates, float *dc_prev, size_t B,
                                      size_t H, const ktanh_lut64_t *lut, ktanh_stream_t stream);
 
+/* ---- Attention with capped scores -------------------------------------------------------------------
+ * Where a transformer bounds its attention scores with TanH, K-TanH takes its place.  For a query q and a key k
+ * that it sees, in Float32:
+ *   t = Kf(q.k * (scale / cap)),   y = cap * t,   weight = e^y / sum of e^y over the keys that q sees
+ * and the output is the weighted sum of the values.  Kf is ktanh_f32 with the bits that its shift drops kept (the line
+ * A x + B that Algorithm 1 follows on each interval), one fused multiply-add; scale / cap is rounded to Float32 once.
+ * q . k, the weights and their sum are Float32; the weights are rounded to BFloat16 for the product with the
+ * values, whose sum is Float32; outputs are rounded to nearest even.  Since |y| <= cap <= KCAP_MAX no maximum is
+ * subtracted; the sums of e^y v must stay within Float32, which they do at any cap for values up to 1e9.  K-TanH jumps at the ends of its intervals, by up to 0.016: y by up to 0.016 cap, and two
+ * computations whose q . k differ in the last bits may differ by that there.
+ *
+ * Masks.  Sequences ("documents") are packed one behind the other; a query sees keys of its own document alone.  Where a
+ * document has fewer or more queries than keys, the last query stands at the last key: query i is at place
+ * p = i + keys - queries.  With `causal` it sees the keys up to p, with window w > 0 those from p - w + 1 on.  A query
+ * that sees no key has the output 0 and the log-sum -infinity.  Keys and values that a query does not see do not
+ * reach its output, infinities and NaN included; a NaN among the scores it sees makes its output NaN, and so does
+ * an overflowing q . k.
+ *
+ * Shared heads: query head h reads key/value head h / (heads / kv_heads).
+ * Offsets and lengths are read on the GPU, where values out of range are taken as the nearest in range. */
+#define KCAP_MAX 64.0
+
+typedef struct kcap_shape {
+    size_t docs;                   /* documents                                                     */
+    size_t q_rows, k_rows;         /* rows of q, and of k and v, all documents together             */
+    size_t heads, kv_heads, dim;   /* heads a multiple of kv_heads; dim 64 or 128                   */
+    size_t q_row, q_head;          /* strides in elements, multiples of 8: tensors are              */
+    size_t k_row, k_head;          /*   [rows][heads][dim] with dim contiguous                      */
+    size_t v_row, v_head;
+    double scale, cap;             /* scale finite, 0 < cap <= KCAP_MAX                             */
+    size_t window;                 /* 0: none                                                       */
+    int causal;
+} kcap_shape_t;
+
+/* q_offsets, k_offsets: device, docs + 1 each: rows of document d are offsets[d] .. offsets[d + 1] - 1.
+ *   o    device, out: BFloat16 [q_rows][heads][dim], dense; rows in no document are left as they are
+ *   lse  device, out, may be NULL: Float32 [heads][q_rows], log of the sum of e^y (kcap_attention_backward reads it)
+ * q, k, v 16-byte aligned, o 8-byte (KT_ERR_ALIGN).  q_rows == 0 or docs == 0 returns KT_OK without a launch.
+ * KT_ERR_SHAPE: another dim, heads not a multiple of kv_heads, a cap or scale out of range, more than 2^30 rows.
+ * KT_ERR_LUT: also a table whose K exceeds 1. */
+ktanh_status_t kcap_attention(const kcap_shape_t *shape, const uint16_t *q, const uint16_t *k, const uint16_t *v,
+                              const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *o, float *lse,
+                              const ktanh_lut_t *lut, ktanh_stream_t stream);
+ktanh_status_t kcap_attention64(const kcap_shape_t *shape, const uint16_t *q, const uint16_t *k, const uint16_t *v,
+                                const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *o, float *lse,
+                                const ktanh_lut64_t *lut, ktanh_stream_t stream);
+
+/* A cache of keys and values in pages: key j of sequence s lies in slot j % page_size of page
+ * pages[s * table_row + j / page_size].  Strides in elements, multiples of 8; dim contiguous. */
+typedef struct kcap_pages {
+    size_t page_size;              /* a power of two                                                */
+    size_t page_count;             /* pages in the cache                                            */
+    size_t most;                   /* pages per sequence in the table: lengths beyond are cut       */
+    size_t table_row;              /* from one sequence's row of the table to the next              */
+    size_t k_page, k_slot, k_head;
+    size_t v_page, v_slot, v_head;
+} kcap_pages_t;
+
+/* The same attention over a paged cache, causal: the queries are the last tokens of their sequences, whose keys and
+ * values (their own among them) are in the cache.  shape: docs = sequences, q_rows, heads, kv_heads, dim, q_row, q_head,
+ * scale, cap, window; the rest is not read.
+ *   pages      device, [docs][most] with rows table_row apart; a number outside the cache is taken as the nearest page
+ *   lengths    device, docs: keys of each sequence
+ *   q_offsets  device, docs + 1, or NULL: one query for each sequence (q_rows == docs), which is the faster form for that
+ *   workspace  device, 16-byte aligned, kcap_attention_paged_workspace bytes; unused and may be NULL where that is 0.
+ *              What it holds before does not matter; calls that may run at once need one each. */
+size_t kcap_attention_paged_workspace(const kcap_shape_t *shape, const kcap_pages_t *cache, int single);
+ktanh_status_t kcap_attention_paged(const kcap_shape_t *shape, const kcap_pages_t *cache, const uint16_t *q, const uint16_t *k_cache,
+                                    const uint16_t *v_cache, const int32_t *pages, const int32_t *lengths,
+                                    const int32_t *q_offsets, uint16_t *o, void *workspace, const ktanh_lut_t *lut,
+                                    ktanh_stream_t stream);
+ktanh_status_t kcap_attention64_paged(const kcap_shape_t *shape, const kcap_pages_t *cache, const uint16_t *q, const uint16_t *k_cache,
+                                      const uint16_t *v_cache, const int32_t *pages, const int32_t *lengths,
+                                      const int32_t *q_offsets, uint16_t *o, void *workspace, const ktanh_lut64_t *lut,
+                                      ktanh_stream_t stream);
+
+/* New tokens into the cache: their keys rotated to their positions, their values as they are; and their
+ * queries rotated.  Token i of sequence s (row q_offsets[s] + i) has the position lengths[s] + i, lengths being the keys
+ * in the cache before the call.  Pairs (a, b) become (a cos - b sin, b cos + a sin) in Float32, rounded once; pair i of the first
+ * 2 * angles values is (x_i, x_{i + angles}), or (x_{2i}, x_{2i+1}) where `interleaved`; what is behind them is copied.
+ * shape: docs, q_rows (tokens), heads, kv_heads, dim and all strides; the rest is not read.
+ *   cos, sin   device, Float32 [positions][angles], dense, 16-byte aligned; angles a multiple of 8, 2 * angles <= dim
+ *   q_offsets  device, docs + 1, or NULL: one token for each sequence
+ *   q_out      device, BFloat16 [q_rows][heads][dim], dense, 16-byte aligned; may be q where q is dense
+ * A token whose position has no page in the table, or a page number outside the cache, is not written to the cache; one whose
+ * position has no angles has NaN for its query and is not written either. */
+ktanh_status_t kcap_append(const kcap_shape_t *shape, const kcap_pages_t *cache, const uint16_t *q, const uint16_t *k,
+                           const uint16_t *v, uint16_t *q_out, uint16_t *k_cache, uint16_t *v_cache, const int32_t *pages,
+                           const int32_t *lengths, const int32_t *q_offsets, const float *cos, const float *sin,
+                           size_t positions, size_t angles, int interleaved, ktanh_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

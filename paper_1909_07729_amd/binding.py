@@ -27,7 +27,7 @@ INTERVALS = 32
 
 # Every function include/ktanh.h declares, with the kinds of its parameters:
 #   p = device tensor pointer, n = size_t, l = table pointer (32 intervals), L = table pointer (64),
-#   s = stream, i = int status.  The ctypes prototypes below are built from these strings and nothing else.
+#   a = kcap_shape_t pointer, g = kcap_pages_t pointer, t = int, s = stream, i = int status.  The ctypes prototypes below are built from these strings and nothing else.
 SIGNATURES = {
     "ktanh_status_string": "i", "ktanh_default_lut": "", "ktanh_lut_validate": "l",
     "ktanh_lut64_validate": "L", "ktanh_fit_lut": "l", "ktanh_fit_lut64": "L", "ktanh_fit_lut_bmin0": "l",
@@ -46,6 +46,10 @@ SIGNATURES = {
     "klstm_cell_backward": "ppppppnnls", "klstm_cell64_backward": "ppppppnnLs",
     "kpade32_bf16": "ppns", "kpade78_bf16": "ppns",
     "ktaylor2_bf16": "ppns", "ktaylor3_bf16": "ppns",
+    "kcap_attention": "apppppppls", "kcap_attention64": "apppppppLs",
+    "kcap_attention_paged_workspace": "agt",
+    "kcap_attention_paged": "agppppppppls", "kcap_attention64_paged": "agppppppppLs",
+    "kcap_append": "agpppppppppppnnts",
 }
 EXPORTS = tuple(SIGNATURES)
 
@@ -90,6 +94,21 @@ class KtanhLut64(ctypes.Structure):
         return [(int(self.E[t]), int(self.r[t]), int(self.b[t])) for t in range(64)]
 
 
+class KcapShape(ctypes.Structure):
+    """Mirror of ``kcap_shape_t``."""
+
+    _fields_ = [(name, ctypes.c_size_t) for name in
+                ("docs", "q_rows", "k_rows", "heads", "kv_heads", "dim", "q_row", "q_head", "k_row", "k_head", "v_row", "v_head")]
+    _fields_ += [("scale", ctypes.c_double), ("cap", ctypes.c_double), ("window", ctypes.c_size_t), ("causal", ctypes.c_int)]
+
+
+class KcapPages(ctypes.Structure):
+    """Mirror of ``kcap_pages_t``."""
+
+    _fields_ = [(name, ctypes.c_size_t) for name in
+                ("page_size", "page_count", "most", "table_row", "k_page", "k_slot", "k_head", "v_page", "v_slot", "v_head")]
+
+
 class KtanhError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -131,13 +150,15 @@ def load_library() -> ctypes.CDLL:
                 f"{LIB_PATH} is not built; run `python -c 'import __graft_entry__ as g; g.build()'`")
         lib = ctypes.CDLL(LIB_PATH)
         kinds = {"p": ctypes.c_void_p, "n": ctypes.c_size_t, "s": ctypes.c_void_p, "i": ctypes.c_int,
-                 "l": ctypes.POINTER(KtanhLut), "L": ctypes.POINTER(KtanhLut64)}
+                 "l": ctypes.POINTER(KtanhLut), "L": ctypes.POINTER(KtanhLut64),
+                 "a": ctypes.POINTER(KcapShape), "g": ctypes.POINTER(KcapPages), "t": ctypes.c_int}
         for name, params in SIGNATURES.items():
             fn = getattr(lib, name)
             fn.argtypes = [kinds[k] for k in params]
             fn.restype = ctypes.c_int
         lib.ktanh_status_string.restype = ctypes.c_char_p
         lib.ktanh_default_lut.restype = ctypes.POINTER(KtanhLut)
+        lib.kcap_attention_paged_workspace.restype = ctypes.c_size_t
         _load_host()
         _lib = lib
     return _lib
@@ -552,3 +573,177 @@ def klstm_cell_backward(gates, c_prev, dh, dc_next, dgates=None, dc_prev=None, l
     if st != 0:
         raise KtanhError(st, _entry)
     return dgates, dc_prev
+
+
+# ------------------------------------------------------------------------- attention with capped scores
+
+
+def _check_rows(t, what, dims=3):
+    """[rows, heads, dim] (or pages of that) with dim contiguous; any other strides."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor (device memory)")
+    if t.dtype not in _BF16_VIEWS:
+        raise TypeError(f"{what} has dtype {t.dtype}, expected one of {_BF16_VIEWS}")
+    if t.dim() != dims:
+        raise ValueError(f"{what} must have {dims} dimensions")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what} must be contiguous in its last dimension")
+    if any(step < 0 for step in t.stride()):
+        raise ValueError(f"{what} has a negative stride")
+
+
+def _check_int32(t, what, shape):
+    _check(t, (torch.int32,), what)
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{what} must be of shape {shape}")
+
+
+def _step(t, dim):
+    """A stride; the one of a dimension of a single element means nothing."""
+    return t.stride(dim) if t.shape[dim] > 1 else 0
+
+
+def _cap_shape(q, k, v, docs, k_rows, cap, scale, window, causal):
+    heads, dim = q.shape[1:]
+    kv_heads = k.shape[-2]
+    if k.shape != v.shape or k.shape[-1] != dim:
+        raise ValueError("q, k and v do not agree in heads or dim")
+    if kv_heads == 0 or heads % kv_heads:
+        raise ValueError("the heads of q must be a multiple of those of k and v")
+    if window < 0:
+        raise ValueError("window must not be negative")
+    return KcapShape(docs, q.shape[0], k_rows, heads, kv_heads, dim, _step(q, 0), _step(q, 1), _step(k, -3), _step(k, -2),
+                     _step(v, -3), _step(v, -2), dim ** -0.5 if scale is None else scale, cap, window, bool(causal))
+
+
+def _empty(shape, dtype, like, stream):
+    """Memory of the stream that the call runs on: what ran before on it, and what reuses it, is in order."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _dense_out(t, what, shape, dtypes):
+    _check(t, dtypes, what)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be of shape {tuple(shape)}")
+    return t
+
+
+def kcap_attention(q, k, v, q_offsets, k_offsets=None, *, cap, scale=None, causal=True, window=0, out=None, lse=None,
+                   lut=None, stream=None, _entry="kcap_attention"):
+    """Attention with scores cap * K(scale * q.k / cap) over packed documents.
+
+    q [q_rows, heads, dim], k and v [k_rows, kv_heads, dim] BFloat16, any strides with dim contiguous; q_offsets and
+    k_offsets int32 [documents + 1] on the GPU (k_offsets None: the same rows).  A query is at the place of its key counted from
+    the documents' ends; it sees the keys up to there if ``causal``, and the last ``window`` of them if that is not 0.
+    ``scale`` None is dim ** -0.5.  Returns (out [q_rows, heads, dim], lse [heads, q_rows] Float32).
+    """
+    k_offsets = q_offsets if k_offsets is None else k_offsets
+    for t, what in ((q, "q"), (k, "k"), (v, "v")):
+        _check_rows(t, what)
+    docs = max(q_offsets.numel() - 1, 0)
+    _check_int32(q_offsets, "q_offsets", (docs + 1,))
+    _check_int32(k_offsets, "k_offsets", (docs + 1,))
+    shape = _cap_shape(q, k, v, docs, k.shape[0], cap, scale, window, causal)
+    out = _empty(q.shape, q.dtype, q, stream) if out is None else _dense_out(out, "out", q.shape, _BF16_VIEWS)
+    sums = (q.shape[1], q.shape[0])
+    lse = _empty(sums, torch.float32, q, stream) if lse is None else _dense_out(lse, "lse", sums, (torch.float32,))
+    st = getattr(load_library(), _entry)(shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_offsets.data_ptr(), k_offsets.data_ptr(),
+                                         out.data_ptr(), lse.data_ptr(), _lut_arg(lut), _stream_handle(stream))
+    if st != 0:
+        raise KtanhError(st, _entry)
+    return out, lse
+
+
+def kcap_attention64(q, k, v, q_offsets, k_offsets=None, **options):
+    """``kcap_attention`` with a 64-interval table (``KtanhLut64``; None = the fitted one)."""
+    return kcap_attention(q, k, v, q_offsets, k_offsets, **options, _entry="kcap_attention64")
+
+
+def _cap_pages(k_cache, v_cache, pages, docs):
+    if k_cache.shape != v_cache.shape:
+        raise ValueError("k_cache and v_cache differ in shape")
+    if not pages.is_cuda:
+        raise ValueError("pages must be a CUDA tensor (device memory)")
+    if pages.dtype != torch.int32:
+        raise TypeError(f"pages has dtype {pages.dtype}, expected torch.int32")
+    if pages.dim() != 2 or pages.shape[0] != docs or (pages.shape[1] > 1 and pages.stride(1) != 1) or pages.stride(0) < 0:
+        raise ValueError("pages must be [sequences, pages of each], contiguous in its last dimension")
+    return KcapPages(k_cache.shape[1], k_cache.shape[0], pages.shape[1], _step(pages, 0),
+                     *(_step(cache, i) for cache in (k_cache, v_cache) for i in range(3)))
+
+
+def _docs_of(q, q_offsets):
+    if q_offsets is None:
+        return q.shape[0]
+    docs = max(q_offsets.numel() - 1, 0)
+    _check_int32(q_offsets, "q_offsets", (docs + 1,))
+    return docs
+
+
+def kcap_attention_paged(q, k_cache, v_cache, pages, lengths, q_offsets=None, *, cap, scale=None, window=0, out=None,
+                         lut=None, stream=None, _entry="kcap_attention_paged"):
+    """The same attention over keys and values in the pages of a cache, causal; the queries are the last tokens of
+    their sequences.
+
+    q [tokens, heads, dim]; k_cache, v_cache [pages, page size, kv_heads, dim] BFloat16, any strides with dim contiguous; pages
+    int32 [sequences, most]; lengths int32 [sequences], the keys of each; q_offsets int32 [sequences + 1], or None: one
+    token for each sequence.  Pass the columns of ``pages`` that the longest sequence needs: the work is cut by them.
+    Returns out [tokens, heads, dim].
+    """
+    _check_rows(q, "q")
+    _check_rows(k_cache, "k_cache", 4)
+    _check_rows(v_cache, "v_cache", 4)
+    docs = _docs_of(q, q_offsets)
+    _check_int32(lengths, "lengths", (docs,))
+    cache = _cap_pages(k_cache, v_cache, pages, docs)
+    shape = _cap_shape(q, k_cache, v_cache, docs, 0, cap, scale, window, True)
+    out = _empty(q.shape, q.dtype, q, stream) if out is None else _dense_out(out, "out", q.shape, _BF16_VIEWS)
+    lib = load_library()
+    size = lib.kcap_attention_paged_workspace(shape, cache, q_offsets is None)
+    workspace = _empty((size,), torch.uint8, q, stream) if size else None
+    st = getattr(lib, _entry)(shape, cache, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), pages.data_ptr(), lengths.data_ptr(),
+                              None if q_offsets is None else q_offsets.data_ptr(), out.data_ptr(),
+                              None if workspace is None else workspace.data_ptr(), _lut_arg(lut), _stream_handle(stream))
+    if st != 0:
+        raise KtanhError(st, _entry)
+    return out
+
+
+def kcap_attention64_paged(q, k_cache, v_cache, pages, lengths, q_offsets=None, **options):
+    """``kcap_attention_paged`` with a 64-interval table (``KtanhLut64``; None = the fitted one)."""
+    return kcap_attention_paged(q, k_cache, v_cache, pages, lengths, q_offsets, **options, _entry="kcap_attention64_paged")
+
+
+def kcap_append(q, k, v, k_cache, v_cache, pages, lengths, q_offsets=None, *, cos, sin, interleaved=False, out=None, stream=None):
+    """New tokens into a paged cache: k rotated to its place and v into their pages, q rotated and returned.
+
+    q [tokens, heads, dim], k and v [tokens, kv_heads, dim], caches, pages and q_offsets as for ``kcap_attention_paged``;
+    lengths int32 [sequences], the keys in the cache before the call: token i of sequence s goes to place lengths[s] + i.
+    cos and sin Float32 [positions, angles]: pairs (x_i, x_{i + angles}) of the first 2 * angles values are turned, or
+    (x_{2i}, x_{2i+1}) if ``interleaved``.  ``out`` may be ``q`` where that is contiguous.
+    """
+    for t, what in ((q, "q"), (k, "k"), (v, "v")):
+        _check_rows(t, what)
+    _check_rows(k_cache, "k_cache", 4)
+    _check_rows(v_cache, "v_cache", 4)
+    if k.shape[0] != q.shape[0] or k_cache.shape[2:] != k.shape[1:]:
+        raise ValueError("q, k and v, and the cache do not agree in tokens, heads or dim")
+    docs = _docs_of(q, q_offsets)
+    _check_int32(lengths, "lengths", (docs,))
+    for t, what in ((cos, "cos"), (sin, "sin")):
+        _check(t, (torch.float32,), what)
+    if cos.dim() != 2 or cos.shape != sin.shape:
+        raise ValueError("cos and sin must be [positions, angles]")
+    cache = _cap_pages(k_cache, v_cache, pages, docs)
+    shape = _cap_shape(q, k, v, docs, 0, 1.0, 1.0, 0, True)
+    out = _empty(q.shape, q.dtype, q, stream) if out is None else _dense_out(out, "out", q.shape, _BF16_VIEWS)
+    st = load_library().kcap_append(shape, cache, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), k_cache.data_ptr(),
+                                    v_cache.data_ptr(), pages.data_ptr(), lengths.data_ptr(),
+                                    None if q_offsets is None else q_offsets.data_ptr(), cos.data_ptr(), sin.data_ptr(),
+                                    cos.shape[0], cos.shape[1], bool(interleaved), _stream_handle(stream))
+    if st != 0:
+        raise KtanhError(st, "kcap_append")
+    return out

@@ -1,0 +1,168 @@
+// Attention with scores capped through K-TanH: what its kernels share.
+//
+//   s = q . k,   t = K(s * scale / cap),   y = cap * t,   p = softmax of y over the keys that a query sees
+//
+// K is the Float32 form of Algorithm 1 (arXiv:1909.07729).  On one interval of the table it is a line,
+//   K(x) = A x + B for x > 0,   A = 2^(E - E_i - r),   B = 2^(E - 127) (1 - 2^-r + b/128),
+// which the kernels evaluate with one fused multiply-add: what the shift of Algorithm 1 drops below the
+// last place of a Float32 is kept.  128 lines are held in LDS, indexed by the three low exponent bits and the four
+// high mantissa bits of |x| clamped to [0.125, 16]: the identity below 0.25, saturation from 4 on and the
+// table in between need no comparisons, and tables of 32 and of 64 intervals run the same code.
+//
+// |y| <= cap, and caps are at most 64, so e^y stays within e^-64 .. e^64 and the softmax needs no running
+// maximum: the weights are summed as they are, which also lets parts of a row be joined by adding.
+//
+// Matrix products use v_mfma_f32_32x32x16_bf16.  Scores are formed so that the lane that holds a weight holds it
+// where the next product wants it: an accumulator's lane l has column l & 31 and the rows
+// (r & 3) + 8 (r >> 2) + 4 (l >> 5), r = 0..15; packed to BFloat16, registers 8 i .. 8 i + 7 are the second operand of a
+// product over 16 of those rows in the order  8 i' + 4 (l >> 5) + (j & 3),  and the first operand is read from LDS in that same
+// order by transposing reads of 4 rows x 16 columns (ds_read_b64_tr_b16).  No weight crosses lanes.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ktanh_pack.h"
+
+namespace ktanh_cap {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kRows = 128;   // rows of a block: 32 for each wavefront
+constexpr int kTile = 64;    // rows of a tile in LDS
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// A tensor [rows][heads][dim], dim contiguous.
+struct Rows {
+    const uint16_t *at;
+    long long row, head;  // strides in elements
+};
+
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
+__device__ __forceinline__ bf16x8 pack8(const float *v)
+{
+    return __builtin_bit_cast(bf16x8, u32x4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])});
+}
+
+// ------------------------------------------------------------------------------------------ the cap
+// lines[i], i = low three exponent bits << 4 | high four mantissa bits, times `unit`.
+__device__ __forceinline__ void spread_lines(f32x2 *lines, const KtCapPack &pack, float unit)
+{
+    const int i = threadIdx.x;
+    if (i < 128) {
+        const int e = i >> 4, slot = i & 63;
+        const float a = e == 4 ? 1.0f : (e >= 1 && e <= 3) ? 0.0f : pack.a[slot];
+        const float b = e == 4 ? 0.0f : (e >= 1 && e <= 3) ? 1.0f : pack.b[slot];
+        lines[i] = f32x2{a * unit, b * unit};
+    }
+}
+
+// unit * K(x).  A NaN stays one.
+__device__ __forceinline__ float capped(float x, const f32x2 *lines)
+{
+    const uint32_t key = __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fabsf(x), 0.125f, 16.0f));
+    const f32x2 line = *reinterpret_cast<const f32x2 *>(reinterpret_cast<const char *>(lines) + ((key >> 16) & 0x3F8u));
+    return __builtin_copysignf(__builtin_fmaf(line.x, __builtin_fabsf(x), line.y), x);
+}
+
+// ------------------------------------------------------------------------------------- tiles in LDS
+// kTile rows of D BFloat16 values, 16-byte chunks swapped within a row so that both ways of reading run without bank
+// conflicts: 8 rows at one chunk (ds_read_b128, rows as they are), and 4 rows x 4 chunks (transposing reads).
+template <int D>
+__device__ __forceinline__ int swap_of(int row)
+{
+    if constexpr (D == 64) return ((row >> 1 & 1) << 2) | (row >> 2 & 3);
+    else return ((row & 3) << 2) | (row >> 2 & 3);
+}
+
+template <int D>
+__device__ __forceinline__ int chunk_at(int row, int chunk)  // byte offset
+{
+    return row * (2 * D) + ((chunk ^ swap_of<D>(row)) << 4);
+}
+
+// Operand of 32 rows of the tile (from `row0`, a multiple of 32) over values 16 k .. 16 k + 15 of each.
+template <int D>
+__device__ __forceinline__ bf16x8 rows_of(const char *tile, int row0, int k)
+{
+    const int lane = threadIdx.x & 63;
+    return *reinterpret_cast<const bf16x8 *>(tile + chunk_at<D>(lane & 31, 2 * k + (lane >> 5)) + row0 * (2 * D));
+}
+
+// Operand of columns 32 c .. 32 c + 31 of the tile over its rows row0 .. row0 + 15 in the order of a packed accumulator.
+template <int D>
+__device__ __forceinline__ bf16x8 columns_of(const char *tile, int row0, int c)
+{
+    typedef __attribute__((address_space(3))) s16x4 *lds4;
+    const int lane = threadIdx.x & 63;
+    const int row = (lane >> 5) * 4 + (lane >> 2 & 3), chunk = 4 * c + (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
+    const char *p0 = tile + row0 * (2 * D) + chunk_at<D>(row, chunk) + (lane & 1) * 8;
+    const char *p1 = tile + row0 * (2 * D) + chunk_at<D>(row + 8, chunk) + (lane & 1) * 8;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p0));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p1));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// ------------------------------------------------------------------------------------------- blocks
+// Consecutive blocks go to the eight dies in turn; block -> place in an order of which each die takes one stretch,
+// so that blocks that share keys share a second-level cache.  Launch 8 * ceil(total / 8) blocks.
+__device__ __forceinline__ unsigned place_of_block(unsigned block, unsigned total)
+{
+    return (block & 7) * ((total + 7) / 8) + (block >> 3);
+}
+
+// Which document the `tile`-th stretch of `size` rows belongs to.  Document d owns the stretches from
+// offsets[d] / size + d on, at least as many as it needs; there are rows / size + documents in all, known without reading the offsets.
+// Offsets outside [0, rows] are taken as the nearest in range, so that a wrong one reads nothing out of bounds.
+struct Stretch {
+    int doc, begin, end, first;  // rows of the document, and the first of the stretch; first >= end: nothing to do
+};
+
+__device__ __forceinline__ int offset_at(const int *offsets, int d, int rows)
+{
+    return offsets == nullptr ? min(d, rows) : min(max(offsets[d], 0), rows);
+}
+
+// The last document for which `starts` (true up to some document, false behind it) holds; 0 if none.  By whole wavefronts.
+template <class Starts>
+__device__ __forceinline__ int last_document(int docs, Starts starts)
+{
+    int before = 0;
+    if (docs > 1) {
+        for (int base = 0; base < docs; base += 64) {
+            const int d = base + (int)(threadIdx.x & 63);
+            const int n = __builtin_popcountll(__ballot(d < docs && starts(d)));
+            before += n;
+            if (n < 64) break;
+        }
+    }
+    return __builtin_amdgcn_readfirstlane(max(before, 1) - 1);
+}
+
+__device__ __forceinline__ Stretch stretch_of(int tile, const int *offsets, int docs, int rows, int size)
+{
+    Stretch s;
+    s.doc = last_document(docs, [&](int d) { return offset_at(offsets, d, rows) / size + d <= tile; });
+    s.begin = offset_at(offsets, s.doc, rows);
+    s.end = max(offset_at(offsets, s.doc + 1, rows), s.begin);
+    s.first = s.begin + (tile - (s.begin / size + s.doc)) * size;
+    return s;
+}
+
+}  // namespace ktanh_cap

@@ -201,3 +201,40 @@ void kt_pack_taylor(KtLutPack *pack)
         pack->slot[string & 63] = bits((float)std::tanh(a));
     }
 }
+
+// ---- K-TanH as lines ------------------------------------------------------------------------------
+namespace {
+
+// Slot t of 64; the interval [(1 + first/16) 2^e, (1 + (first + 1)/16) 2^e) of its input exponent e_in = e + 127.
+bool line_of(int t, int E, int r, int b, KtCapPack *pack)
+{
+    const int e_in = 125 + (((t >> 4) - 125) & 3);
+    const double slope = std::ldexp(1.0, E - e_in - r);
+    const double at_zero = std::ldexp(1.0 - std::ldexp(1.0, -r) + b / 128.0, E - 127);
+    pack->a[t] = (float)slope;
+    pack->b[t] = (float)at_zero;
+    const double end = std::ldexp(1.0 + ((t & 15) + 1) / 16.0, e_in - 127);
+    return slope * end + at_zero <= 1.0;
+}
+
+}  // namespace
+
+ktanh_status_t kt_pack_cap(const ktanh_lut_t *lut, KtCapPack *pack)
+{
+    if (lut == nullptr) lut = &kTable1;
+    const ktanh_status_t st = ktanh_lut_validate(lut);
+    if (st != KT_OK) return st;
+    bool bounded = true;
+    for (int t = 0; t < 64; ++t) bounded &= line_of(t, lut->E[t >> 1], lut->r[t >> 1], lut->b[t >> 1], pack);
+    return bounded ? KT_OK : KT_ERR_LUT;
+}
+
+ktanh_status_t kt_pack_cap64(const ktanh_lut64_t *lut, KtCapPack *pack)
+{
+    if (lut == nullptr) lut = fitted_lut64();
+    const ktanh_status_t st = ktanh_lut64_validate(lut);
+    if (st != KT_OK) return st;
+    bool bounded = true;
+    for (int t = 0; t < 64; ++t) bounded &= line_of(t, lut->E[t], lut->r[t], lut->b[t], pack);
+    return bounded ? KT_OK : KT_ERR_LUT;
+}

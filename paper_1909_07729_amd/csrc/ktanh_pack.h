@@ -37,3 +37,12 @@ ktanh_status_t kt_pack_lut64_f32(const ktanh_lut64_t *lut, KtLutPack *pack);
 // of each of Table 1's 32 intervals, formed in double precision and rounded to Float32, as the bits of a
 // Float32 in the slot of the 32-interval table that the interval's magnitudes select; 1.0 everywhere else.
 void kt_pack_taylor(KtLutPack *pack);
+
+// K-TanH as lines, for the capped attention: K(x) = a x + b on the interval t = (E_i & 3) << 4 | (M_i >> 3) of [0.25, 4);
+// a table of 32 intervals fills each of its intervals' two slots alike.  Attention takes e^(cap K) without a
+// maximum, so a table whose K exceeds 1 is refused (KT_ERR_LUT).  NULL = Table 1 / the fitted 64-interval table.
+struct KtCapPack {
+    float a[64], b[64];
+};
+ktanh_status_t kt_pack_cap(const ktanh_lut_t *lut, KtCapPack *pack);
+ktanh_status_t kt_pack_cap64(const ktanh_lut64_t *lut, KtCapPack *pack);

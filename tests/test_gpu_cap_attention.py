@@ -1,0 +1,428 @@
+"""Attention with scores capped through K-TanH against a 64-bit reference: packed documents, shared heads, masks that leave
+rows empty, values that are not finite behind masks, strides, streams, the paged cache and the appending to it.
+
+q and k are multiples of 1/8 below 8, so that every q.k is exact in Float32 and both sides see the same interval of K-TanH's table;
+the bounds are the reference's own (what rounding weights, scores' gradients and results to BFloat16 may change)."""
+import numpy as np
+import pytest
+
+from oracle import kcap_oracle
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def gpu(oracle):
+    import torch
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    from paper_1909_07729_amd import autograd, binding
+    binding.load_library()
+    torch.cuda.set_device(0)
+    return binding, autograd, torch
+
+
+def _grid(rng, shape, spread):
+    return np.clip(np.round(rng.standard_normal(shape) * spread * 8), -63, 63) / 8
+
+
+def _bf16(torch, a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).cuda().bfloat16()
+
+
+def _inputs(torch, seed, q_rows, k_rows, heads, kv_heads, dim, spread=2.0):
+    """(device tensors q, k, v), (the same as doubles)"""
+    rng = np.random.default_rng(seed)
+    arrays = [_grid(rng, (q_rows, heads, dim), spread), _grid(rng, (k_rows, kv_heads, dim), spread), rng.standard_normal((k_rows, kv_heads, dim))]
+    tensors = [_bf16(torch, a) for a in arrays]
+    return tensors, [t.float().cpu().numpy().astype(np.float64) for t in tensors]
+
+
+def _offsets(torch, lengths):
+    at = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+    return torch.from_numpy(at).cuda(), at
+
+
+def _near(got, want, off, what):
+    got = got.float().cpu().numpy().astype(np.float64) if not isinstance(got, np.ndarray) else got
+    assert got.shape == want.shape
+    fine = np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want)), f"{what}: NaN elsewhere"
+    assert np.array_equal(got[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)]), f"{what}: infinities elsewhere"
+    far = np.abs(got[fine] - want[fine]) / off[fine]
+    assert far.max(initial=0.0) <= 1.0, f"{what}: {far.max():.2f} of the bound"
+
+
+# (query lengths, key lengths or None for the same)
+DOCS = {
+    "one token": ([1], None),
+    "one of each size around a tile": ([63, 64, 65, 1, 0, 127, 128, 129, 2], None),
+    "one long": ([401], None),
+    "empty documents": ([0, 5, 0, 0, 70, 0], None),
+    "fewer queries than keys": ([3, 1, 60, 130], [200, 64, 61, 131]),
+    "more queries than keys": ([40, 130, 7, 4], [5, 64, 0, 3]),
+}
+MASKS = {"causal": dict(causal=True), "all": dict(causal=False), "window": dict(causal=True, window=37),
+         "window of one": dict(causal=True, window=1), "window, later keys too": dict(causal=False, window=70),
+         "window beyond 32 bits": dict(causal=True, window=1 << 40)}
+HEADS = [(1, 1, 64), (4, 2, 128), (5, 1, 64), (3, 3, 128)]
+
+
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("docs", DOCS)
+@pytest.mark.parametrize("heads,kv_heads,dim", HEADS)
+def test_documents(gpu, docs, mask, heads, kv_heads, dim):
+    binding, _, torch = gpu
+    q_lengths, k_lengths = DOCS[docs]
+    k_lengths = q_lengths if k_lengths is None else k_lengths
+    (q, k, v), wide = _inputs(torch, 1, sum(q_lengths), sum(k_lengths), heads, kv_heads, dim)
+    (q_at, q_np), (k_at, k_np) = _offsets(torch, q_lengths), _offsets(torch, k_lengths)
+    options = dict(cap=32.0, scale=dim ** -0.5, **MASKS[mask])
+    o, lse = binding.kcap_attention(q, k, v, q_at, k_at, **options)
+    want = kcap_oracle.attention(*wide, q_np, k_np, **options)
+    _near(o, want["o"], want["o_off"], "o")
+    _near(lse, want["lse"], want["lse_off"], "lse")
+    empty = np.isinf(want["lse"])
+    assert not o.float().cpu().numpy().transpose(1, 0, 2)[empty].any()
+
+
+@pytest.mark.parametrize("intervals", [32, 64])
+@pytest.mark.parametrize("cap,spread", [(0.5, 2.0), (20.0, 3.0), (50.0, 3.0), (64.0, 4.0), (64.0, 0.2)])
+def test_caps_and_tables(gpu, cap, spread, intervals):
+    """From saturated scores (cap 0.5) to ones that never leave the identity, with the default and a caller's tables."""
+    binding, _, torch = gpu
+    (q, k, v), wide = _inputs(torch, 2, 150, 150, 2, 1, 128, spread)
+    at, at_np = _offsets(torch, [150])
+    entry = binding.kcap_attention if intervals == 32 else binding.kcap_attention64
+    tables = [(None, None)]
+    from oracle import ktanh_oracle
+    if intervals == 32:
+        tables.append((binding.ktanh_fit_lut_bmin0(), ktanh_oracle.fit_lut_bmin0()))
+    else:
+        rows = binding.ktanh_fit_lut64().as_tuples()
+        rows[20] = (125, 1, 3)
+        tables.append((binding.KtanhLut64.from_tuples(rows), ktanh_oracle.OracleLut64.from_tuples(rows)))
+    for lut, oracle_lut in tables:
+        options = dict(cap=cap, scale=128 ** -0.5)
+        o, lse = entry(q, k, v, at, lut=lut, **options)
+        want = kcap_oracle.attention(*wide, at_np, at_np, intervals=intervals, lut=oracle_lut, **options)
+        _near(o, want["o"], want["o_off"], "o")
+        _near(lse, want["lse"], want["lse_off"], "lse")
+
+
+@pytest.mark.parametrize("mask", ["causal", "window", "all"])
+def test_what_is_not_seen_does_not_reach_a_row(gpu, mask):
+    """NaN and infinities in keys and values: of other documents, later than the query, before its window, and in rows of no document."""
+    binding, _, torch = gpu
+    (q, k, v), (q64, k64, v64) = _inputs(torch, 3, 300, 300, 2, 1, 64)
+    at, at_np = _offsets(torch, [90, 140])          # the last 70 rows belong to nobody
+    rng = np.random.default_rng(4)
+    for value in (np.nan, np.inf, -np.inf):
+        for j in rng.integers(0, 300, 4):
+            v64[j, 0, rng.integers(0, 64, 3)] = value
+    for j in (250,) if mask == "all" else (80, 229, 250):
+        k64[j, 0, 5] = np.nan
+    k, v = _bf16(torch, k64), _bf16(torch, v64)
+    v64 = v.float().cpu().numpy().astype(np.float64)
+    options = dict(cap=32.0, scale=0.125, **MASKS[mask])
+    o, _ = binding.kcap_attention(q, k, v, at, **options)
+    want = kcap_oracle.attention(q64, k64, v64, at_np, at_np, **options)["o"]
+    # rows that see a NaN key are NaN
+    for d, (a, b) in enumerate(zip(at_np[:-1], at_np[1:])):
+        ok = kcap_oracle.seen(b - a, b - a, options.get("causal", True), options.get("window", 0))
+        bad = ok @ np.isnan(k64[a:b, 0]).any(1)
+        want[a:b][bad] = np.nan
+    got = o.float().cpu().numpy()[:230]
+    assert np.isfinite(want[:230]).any() and not np.isfinite(want[:230]).all()
+    assert np.array_equal(np.isnan(got), np.isnan(want[:230]))
+    fine = ~np.isnan(got)
+    assert np.array_equal(np.isinf(got)[fine], np.isinf(want[:230])[fine])
+
+
+def test_strided_tensors_and_given_outputs(gpu):
+    """q, k and v as views of one fused tensor, heads before rows, results in the caller's memory, rows of no document untouched."""
+    binding, _, torch = gpu
+    (q, k, v), wide = _inputs(torch, 5, 200, 200, 4, 2, 64)
+    fused = torch.cat([q, k, v], 1).contiguous()
+    views = fused[:, :4], fused[:, 4:6], fused[:, 6:]
+    turned = [t.transpose(0, 1).contiguous().transpose(0, 1) for t in (q, k, v)]
+    at, at_np = _offsets(torch, [31, 150])
+    options = dict(cap=50.0, scale=0.125)
+    want = kcap_oracle.attention(*wide, at_np, at_np, **options)
+    first = None
+    for tensors in ((q, k, v), views, turned):
+        out = torch.full((200, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((4, 200), 7.0, device="cuda")
+        o, sums = binding.kcap_attention(*tensors, at, out=out, lse=lse, **options)
+        assert o is out and sums is lse
+        _near(o[:181], want["o"][:181], want["o_off"][:181], "o")
+        assert (o[181:] == 7).all() and (lse[:, 181:] == 7).all()
+        first = o.clone() if first is None else first
+        assert torch.equal(o, first)
+
+
+def test_offsets_out_of_range_read_nothing_out_of_bounds(gpu):
+    binding, _, torch = gpu
+    (q, k, v), wide = _inputs(torch, 6, 100, 100, 2, 2, 64)
+    options = dict(cap=50.0, scale=0.125, causal=False)
+    wrong = torch.tensor([-5, 60, 1000], dtype=torch.int32, device="cuda")
+    right = torch.tensor([0, 60, 100], dtype=torch.int32, device="cuda")
+    a, b = (binding.kcap_attention(q, k, v, at, **options)[0] for at in (wrong, right))
+    assert torch.equal(a, b)
+
+
+def test_many_documents(gpu):
+    """More documents than a wavefront looks at in one step."""
+    binding, _, torch = gpu
+    rng = np.random.default_rng(7)
+    lengths = rng.integers(0, 9, 300)
+    (q, k, v), wide = _inputs(torch, 8, lengths.sum(), lengths.sum(), 2, 1, 64)
+    at, at_np = _offsets(torch, lengths)
+    options = dict(cap=50.0, scale=0.125)
+    o, lse = binding.kcap_attention(q, k, v, at, **options)
+    want = kcap_oracle.attention(*wide, at_np, at_np, **options)
+    _near(o, want["o"], want["o_off"], "o")
+    _near(lse, want["lse"], want["lse_off"], "lse")
+
+
+def test_on_another_stream_and_in_a_graph(gpu):
+    binding, _, torch = gpu
+    (q, k, v), _ = _inputs(torch, 9, 500, 500, 2, 1, 128)
+    at, _ = _offsets(torch, [500])
+    want, _ = binding.kcap_attention(q, k, v, at, cap=50.0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got, _ = binding.kcap_attention(q, k, v, at, cap=50.0, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held, _ = binding.kcap_attention(q, k, v, at, cap=50.0)
+    for scale in (1.0, 0.5, 2.0):
+        v.copy_(v * scale)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held, binding.kcap_attention(q, k, v, at, cap=50.0)[0])
+
+
+# ------------------------------------------------------------------------------------------ the cache
+
+
+def _cache(torch, seed, lengths, page, kv_heads, dim, spare=2, spread=2.0):
+    """A cache with shuffled pages, garbage (NaN too) wherever no key is; (tensors k, v, pages), (k, v per sequence as doubles)."""
+    rng = np.random.default_rng(seed)
+    most = max(1, -(-max(lengths) // page))
+    count = len(lengths) * most + spare
+    pages = rng.permutation(count)[:len(lengths) * most].reshape(len(lengths), most).astype(np.int32)
+    k, v = (np.full((count, page, kv_heads, dim), np.nan) for _ in range(2))
+    each = []
+    for s, n in enumerate(lengths):
+        ks, vs = _grid(rng, (n, kv_heads, dim), spread), rng.standard_normal((n, kv_heads, dim))
+        for j in range(n):
+            k[pages[s, j // page], j % page], v[pages[s, j // page], j % page] = ks[j], vs[j]
+        each.append((ks, vs))
+    k, v = _bf16(torch, k), _bf16(torch, v)
+    each = [(ks, kcap_oracle.gather(v.float().cpu().numpy().astype(np.float64), pages[s], len(ks))) for s, (ks, _) in enumerate(each)]
+    return (k, v, torch.from_numpy(pages).cuda()), each
+
+
+LENGTHS = {"one token": [1], "ragged": [1, 2, 31, 32, 33, 127, 128, 129, 300], "some empty": [0, 40, 0, 700], "long": [2050, 5]}
+
+
+@pytest.mark.parametrize("window", [0, 1, 50])
+@pytest.mark.parametrize("page", [1, 16, 64])
+@pytest.mark.parametrize("lengths", LENGTHS)
+@pytest.mark.parametrize("heads,kv_heads,dim", [(8, 2, 128), (3, 3, 64), (40, 1, 64)])
+def test_single_tokens_over_pages(gpu, lengths, page, heads, kv_heads, dim, window):
+    binding, _, torch = gpu
+    lengths = LENGTHS[lengths]
+    (k, v, pages), each = _cache(torch, 10, lengths, page, kv_heads, dim)
+    q64 = _grid(np.random.default_rng(11), (len(lengths), heads, dim), 2.0)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    options = dict(cap=32.0, scale=dim ** -0.5, window=window)
+    o = binding.kcap_attention_paged(_bf16(torch, q64), k, v, pages, n, **options)
+    for s, (ks, vs) in enumerate(each):
+        want = kcap_oracle.attention(q64[s:s + 1], ks, vs, [0, 1], [0, len(ks)], **options)
+        _near(o[s:s + 1], want["o"], want["o_off"], f"sequence {s}")
+
+
+@pytest.mark.parametrize("window", [0, 45])
+@pytest.mark.parametrize("page", [8, 128])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(4, 2, 128), (3, 1, 64)])
+def test_pieces_of_prompts_over_pages(gpu, page, heads, kv_heads, dim, window):
+    binding, _, torch = gpu
+    new, lengths = [1, 60, 0, 130, 7], [1, 200, 30, 130, 400]
+    (k, v, pages), each = _cache(torch, 12, lengths, page, kv_heads, dim)
+    at, at_np = _offsets(torch, new)
+    q64 = _grid(np.random.default_rng(13), (sum(new), heads, dim), 2.0)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    options = dict(cap=32.0, scale=dim ** -0.5, window=window)
+    o = binding.kcap_attention_paged(_bf16(torch, q64), k, v, pages, n, at, **options)
+    for s, (ks, vs) in enumerate(each):
+        rows = slice(at_np[s], at_np[s + 1])
+        want = kcap_oracle.attention(q64[rows], ks, vs, [0, new[s]], [0, len(ks)], **options)
+        _near(o[rows], want["o"], want["o_off"], f"sequence {s}")
+
+
+def test_wide_tables_and_layouts_of_the_cache(gpu):
+    """64 intervals; heads before slots in a page, keys and values in one tensor, a table wider than its rows."""
+    binding, _, torch = gpu
+    lengths = [300, 77, 1000]
+    (k, v, pages), each = _cache(torch, 14, lengths, 16, 2, 64)
+    q64 = _grid(np.random.default_rng(15), (3, 6, 64), 2.0)
+    q, n = _bf16(torch, q64), torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    both = torch.stack([k, v], 1)                       # [pages, 2, page, heads, dim]
+    heads_first = [t.transpose(1, 2).contiguous().transpose(1, 2) for t in (k, v)]
+    wider = torch.full((3, pages.shape[1] + 5), 1 << 20, dtype=torch.int32, device="cuda")
+    wider[:, :pages.shape[1]] = pages
+    options = dict(cap=50.0, scale=0.125)
+    one = torch.tensor([0, 1, 2, 3], dtype=torch.int32, device="cuda")
+    first = binding.kcap_attention64_paged(q, k, v, pages, n, **options)
+    for s, (ks, vs) in enumerate(each):
+        want = kcap_oracle.attention(q64[s:s + 1], ks, vs, [0, 1], [0, len(ks)], intervals=64, **options)
+        _near(first[s:s + 1], want["o"], want["o_off"], f"sequence {s}")
+        many = binding.kcap_attention64_paged(q, k, v, pages, n, one, **options)
+        _near(many[s:s + 1], want["o"], want["o_off"], f"sequence {s}, as a piece of a prompt")
+    for kc, vc, table in ((both[:, 0], both[:, 1], pages), (*heads_first, pages), (k, v, wider), (k, v, wider[:, :pages.shape[1]])):
+        got = binding.kcap_attention64_paged(q, kc, vc, table, n, **options)
+        assert torch.allclose(got.float(), first.float(), rtol=2 ** -7, atol=1e-3)
+
+
+def test_a_long_cache_past_32_bits(gpu):
+    """Pages behind 2^32 bytes and 2^31 elements of the cache."""
+    binding, _, torch = gpu
+    page, kv_heads, dim = 64, 8, 128
+    count = (1 << 31) // (page * kv_heads * dim) + 300
+    k, v = (torch.zeros((count, page, kv_heads, dim), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    rng = np.random.default_rng(16)
+    pages = torch.tensor([[count - 1, 3, count - 5]], dtype=torch.int32, device="cuda")
+    cos = torch.ones((192, 64), device="cuda")
+    new_k, new_v = (_bf16(torch, _grid(rng, (150, kv_heads, dim), 2.0)) for _ in range(2))
+    q = _bf16(torch, _grid(rng, (150, 8, dim), 2.0))
+    at = torch.tensor([0, 150], dtype=torch.int32, device="cuda")
+    binding.kcap_append(q, new_k, new_v, k, v, pages, torch.zeros(1, dtype=torch.int32, device="cuda"), at, cos=cos, sin=torch.zeros_like(cos))
+    assert torch.equal(k[count - 1], new_k[:64]) and torch.equal(k[3], new_k[64:128]) and torch.equal(v[count - 5, :22], new_v[128:])
+    n = torch.tensor([150], dtype=torch.int32, device="cuda")
+    one = binding.kcap_attention_paged(q[-1:], k, v, pages, n, cap=50.0)
+    all_ = binding.kcap_attention_paged(q, k, v, pages, n, at, cap=50.0)
+    flat, _ = binding.kcap_attention(q, new_k, new_v, at, cap=50.0)
+    assert torch.equal(all_, flat)
+    assert torch.allclose(one.float(), flat[-1:].float(), rtol=2 ** -7, atol=1e-3)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("angles", [8, 32, 64])
+@pytest.mark.parametrize("page", [1, 16])
+def test_append(gpu, interleaved, angles, page):
+    """Keys and queries turned, values and the rest as they are, in their places and nowhere else; parts of heads turned."""
+    binding, _, torch = gpu
+    dim, heads, kv_heads = 128, 6, 2
+    rng = np.random.default_rng(17)
+    before, new = [0, 13, 40, 7], [20, 1, 0, 30]
+    most = -(-60 // page)
+    count = 4 * most + 3
+    pages = rng.permutation(count)[:4 * most].reshape(4, most).astype(np.int32)
+    q, k, v = (_bf16(torch, rng.standard_normal((sum(new), h, dim))) for h in (heads, kv_heads, kv_heads))
+    caches = [torch.full((count, page, kv_heads, dim), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    angle = np.outer(np.arange(64), 10000.0 ** (-np.arange(angles) / angles))
+    cos, sin = (torch.from_numpy(f(angle).astype(np.float32)).cuda() for f in (np.cos, np.sin))
+    at, at_np = _offsets(torch, new)
+    n = torch.tensor(before, dtype=torch.int32, device="cuda")
+    out = binding.kcap_append(q, k, v, *caches, torch.from_numpy(pages).cuda(), n, at, cos=cos, sin=sin, interleaved=interleaved)
+    wide = [t.float().cpu().numpy().astype(np.float64) for t in (q, k, v)]
+    want_q = np.zeros(wide[0].shape)
+    want = [np.full(c.shape, 9.0) for c in caches]
+    c64, s64 = cos.double().cpu().numpy(), sin.double().cpu().numpy()
+    for s in range(4):
+        for i in range(new[s]):
+            row, place = at_np[s] + i, before[s] + i
+            want_q[row] = kcap_oracle.turned(wide[0][row], c64[place], s64[place], interleaved)
+            spot = pages[s, place // page], place % page
+            want[0][spot] = kcap_oracle.turned(wide[1][row], c64[place], s64[place], interleaved)
+            want[1][spot] = wide[2][row]
+    # two products, a sum and the rounding of the result
+    for got, exact, size in ((out, want_q, np.abs(wide[0]).max()), (caches[0], want[0], np.abs(wide[1]).max()), (caches[1], want[1], 0.0)):
+        _near(got, exact, kcap_oracle.HALF * np.abs(exact) + 4 * 2.0 ** -24 * size + 1e-30, "append")
+
+
+def test_append_in_place_one_token_each_and_tokens_without_a_place(gpu):
+    binding, _, torch = gpu
+    rng = np.random.default_rng(18)
+    q, k, v = (_bf16(torch, rng.standard_normal((5, h, 64))) for h in (4, 2, 2))
+    pages = torch.tensor([[0, 1], [2, 3], [4, 99], [5, -1], [6, 7]], dtype=torch.int32, device="cuda")
+    #      in page 0 | past the table | page 99 is none | page -1 is none | no angles
+    before = torch.tensor([3, 32, 16, 20, 25], dtype=torch.int32, device="cuda")
+    angle = np.outer(np.arange(25), 0.1 * np.arange(32))
+    cos, sin = (torch.from_numpy(f(angle).astype(np.float32)).cuda() for f in (np.cos, np.sin))
+    caches = [torch.full((8, 16, 2, 64), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    turned = q.clone()
+    assert binding.kcap_append(turned, k, v, *caches, pages, before, cos=cos, sin=sin, out=turned) is turned
+    assert torch.equal(binding.kcap_append(q, k, v, *caches, pages, before, cos=cos, sin=sin).view(torch.int16), turned.view(torch.int16))
+    assert torch.equal(caches[1][0, 3], v[0])
+    caches[0][0, 3], caches[1][0, 3] = 9.0, 9.0
+    assert all((c == 9).all() for c in caches)
+    assert turned[[1, 4]].isnan().all() and not turned[[0, 2, 3]].isnan().any()
+
+
+# ----------------------------------------------------------------------------------------- refusals
+
+
+def test_refusals(gpu):
+    binding, _, torch = gpu
+    q, k, v = (torch.zeros((8, h, 64), dtype=torch.bfloat16, device="cuda") for h in (4, 2, 2))
+    at = torch.tensor([0, 8], dtype=torch.int32, device="cuda")
+    with pytest.raises(TypeError):
+        binding.kcap_attention(q.float(), k, v, at, cap=50.0)
+    with pytest.raises(TypeError):
+        binding.kcap_attention(q, k, v, at.long(), cap=50.0)
+    with pytest.raises(ValueError):
+        binding.kcap_attention(q.cpu(), k, v, at, cap=50.0)
+    with pytest.raises(ValueError):
+        binding.kcap_attention(q, k[:, :, ::2], v[:, :, ::2], at, cap=50.0)
+    with pytest.raises(ValueError):
+        binding.kcap_attention(q[:, :3], k, v, at, cap=50.0)
+    with pytest.raises(ValueError):
+        binding.kcap_attention(q, k, v[:4], at, cap=50.0)
+    with pytest.raises(ValueError):
+        binding.kcap_attention(q, k, v, at, cap=50.0, window=-1)
+    with pytest.raises(ValueError):
+        binding.kcap_attention(q, k, v, at, cap=50.0, out=torch.empty_like(q)[:4])
+    for bad in (0.0, -1.0, 65.0, float("nan"), float("inf")):
+        with pytest.raises(binding.KtanhError) as err:
+            binding.kcap_attention(q, k, v, at, cap=bad)
+        assert err.value.status == 4
+    with pytest.raises(binding.KtanhError) as err:
+        binding.kcap_attention(q, k, v, at, cap=50.0, scale=float("inf"))
+    assert err.value.status == 4
+    narrow = [t[..., :32] for t in (q, k, v)]
+    with pytest.raises(binding.KtanhError) as err:
+        binding.kcap_attention(*narrow, at, cap=50.0)
+    assert err.value.status == 4
+    off = torch.zeros(8 * 4 * 64 + 1, dtype=torch.bfloat16, device="cuda")[1:].view(8, 4, 64)
+    with pytest.raises(binding.KtanhError) as err:
+        binding.kcap_attention(off, k, v, at, cap=50.0)
+    assert err.value.status == 2
+    rows = binding.ktanh_default_lut().as_tuples()
+    rows[31] = (127, 4, 110)                            # a valid table, but K up to 1.9
+    with pytest.raises(binding.KtanhError) as err:
+        binding.kcap_attention(q, k, v, at, cap=50.0, lut=binding.KtanhLut.from_tuples(rows))
+    assert err.value.status == 3
+    caches = [torch.zeros((4, 12, 2, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    pages, n = torch.zeros((8, 2), dtype=torch.int32, device="cuda"), torch.ones(8, dtype=torch.int32, device="cuda")
+    with pytest.raises(binding.KtanhError) as err:      # twelve slots in a page
+        binding.kcap_attention_paged(q, *caches, pages, n, cap=50.0)
+    assert err.value.status == 4
+    good = [c[:, :8] for c in caches]
+    with pytest.raises(ValueError):
+        binding.kcap_attention_paged(q, *good, pages[:4], n, cap=50.0)
+    with pytest.raises(ValueError):
+        binding.kcap_attention_paged(q, *good, pages, n[:4], cap=50.0)
+    with pytest.raises(TypeError):
+        binding.kcap_attention_paged(q, *good, pages.long(), n, cap=50.0)
+    cos = torch.ones((16, 12), device="cuda")
+    with pytest.raises(binding.KtanhError) as err:      # twelve angles
+        binding.kcap_append(q, k, v, *good, pages, n, cos=cos, sin=cos)
+    assert err.value.status == 4
+    with pytest.raises(ValueError):
+        binding.kcap_append(q, k, v, *good, pages, n, cos=cos, sin=cos[:3])
+    empty = binding.kcap_attention(q[:0], k[:0], v[:0], torch.zeros(1, dtype=torch.int32, device="cuda"), cap=50.0)
+    assert empty[0].shape == (0, 4, 64) and empty[1].shape == (4, 0)
