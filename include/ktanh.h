@@ -332,7 +332,7 @@ typedef struct kcap_shape {
 } kcap_shape_t;
 
 /* q_offsets, k_offsets: device, docs + 1 each: rows of document d are offsets[d] .. offsets[d + 1] - 1.
- *   o    device, out: BFloat16 [q_rows][heads][dim], dense; rows in no document are left as they are
+ *   o    device, out: BFloat16 [q_rows][heads][dim], dense; rows in no document become 0
  *   lse  device, out, may be NULL: Float32 [heads][q_rows], log of the sum of e^y (kcap_attention_backward reads it)
  * q, k, v 16-byte aligned, o 8-byte (KT_ERR_ALIGN).  q_rows == 0 or docs == 0 returns KT_OK without a launch.
  * KT_ERR_SHAPE: another dim, heads not a multiple of kv_heads, a cap or scale out of range, more than 2^30 rows.
@@ -343,6 +343,25 @@ ktanh_status_t kcap_attention(const kcap_shape_t *shape, const uint16_t *q, cons
 ktanh_status_t kcap_attention64(const kcap_shape_t *shape, const uint16_t *q, const uint16_t *k, const uint16_t *v,
                                 const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *o, float *lse,
                                 const ktanh_lut64_t *lut, ktanh_stream_t stream);
+
+/* Gradients of kcap_attention from its inputs and its o and lse, with the library's derivative identity of TanH:
+ *   P = e^(y - lse),  dS = P (dO.V - sum over dim of dO * O) (1 - t^2),  dq = scale dS K,  dk = scale dS^T Q,  dv = P^T dO
+ * Products take BFloat16 roundings of P and dS and sum in Float32; gradients of shared heads are summed in Float32 before they are
+ * rounded, in a fixed order.  Rows in no document, and queries that see no key, have the gradient 0.  A NaN or
+ * infinity in a document may reach all of that document's gradients.
+ *   d_o        device, BFloat16 [q_rows][heads][dim] with strides do_row, do_head (multiples of 8), 16-byte aligned
+ *   o, lse     as kcap_attention gave them
+ *   dq, dk, dv device, out: BFloat16, dense [rows][heads][dim], 16-byte aligned
+ *   workspace  device, 16-byte aligned, kcap_attention_backward_workspace bytes, whatever is in it */
+size_t kcap_attention_backward_workspace(const kcap_shape_t *shape);
+ktanh_status_t kcap_attention_backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t do_row, size_t do_head, const uint16_t *q,
+                                       const uint16_t *k, const uint16_t *v, const uint16_t *o, const float *lse,
+                                       const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *dq, uint16_t *dk, uint16_t *dv,
+                                       void *workspace, const ktanh_lut_t *lut, ktanh_stream_t stream);
+ktanh_status_t kcap_attention64_backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t do_row, size_t do_head, const uint16_t *q,
+                                         const uint16_t *k, const uint16_t *v, const uint16_t *o, const float *lse,
+                                         const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *dq, uint16_t *dk, uint16_t *dv,
+                                         void *workspace, const ktanh_lut64_t *lut, ktanh_stream_t stream);
 
 /* A cache of keys and values in pages: key j of sequence s lies in slot j % page_size of page
  * pages[s * table_row + j / page_size].  Strides in elements, multiples of 8; dim contiguous. */

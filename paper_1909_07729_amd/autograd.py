@@ -107,6 +107,24 @@ class _KLstmCell(torch.autograd.Function):
         return dgates, dc_prev, None, None
 
 
+class _KCapAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, q_offsets, k_offsets, options, wide):
+        attend = binding.kcap_attention64 if wide else binding.kcap_attention
+        out, lse = attend(q, k, v, q_offsets, k_offsets, **options)
+        ctx.save_for_backward(q, k, v, out, lse, q_offsets, k_offsets)
+        ctx.options, ctx.wide = options, wide
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        attend = binding.kcap_attention64_backward if ctx.wide else binding.kcap_attention_backward
+        *tensors, q_offsets, k_offsets = ctx.saved_tensors
+        if dout.stride(-1) != 1 or any(step % 8 for step in dout.stride()[:2]) or dout.data_ptr() % 16:
+            dout = dout.contiguous()        # also the expanded gradient of a sum
+        return (*attend(dout, *tensors, q_offsets, k_offsets, **ctx.options), None, None, None, None)
+
+
 def _activation(code, function, names, x, lut, intervals):
     """The activation as a C++ autograd function over the same two entry points where ``x`` is an ordinary
     tensor and nothing watches or transforms operations, else as the Python function given.  ``code`` is
@@ -148,3 +166,12 @@ def klstm_cell(gates: torch.Tensor, c_prev: torch.Tensor, lut=None, intervals: i
         if out is not None:
             return out
     return _KLstmCell.apply(gates, c_prev, lut, wide)
+
+
+def kcap_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor, k_offsets=None, *, cap: float,
+                   scale=None, causal: bool = True, window: int = 0, lut=None, intervals: int = 32) -> torch.Tensor:
+    """Attention with scores cap * K(scale * q.k / cap) over packed documents (``binding.kcap_attention``):
+    q [rows, heads, dim], k and v [rows, kv_heads, dim] BFloat16, differentiable with respect to q, k and v."""
+    wide = _is_wide(lut, intervals)
+    options = {"cap": cap, "scale": scale, "causal": causal, "window": window, "lut": lut}
+    return _KCapAttention.apply(q, k, v, q_offsets, q_offsets if k_offsets is None else k_offsets, options, wide)

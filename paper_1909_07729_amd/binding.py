@@ -47,6 +47,8 @@ SIGNATURES = {
     "kpade32_bf16": "ppns", "kpade78_bf16": "ppns",
     "ktaylor2_bf16": "ppns", "ktaylor3_bf16": "ppns",
     "kcap_attention": "apppppppls", "kcap_attention64": "apppppppLs",
+    "kcap_attention_backward_workspace": "a",
+    "kcap_attention_backward": "apnnpppppppppppls", "kcap_attention64_backward": "apnnpppppppppppLs",
     "kcap_attention_paged_workspace": "agt",
     "kcap_attention_paged": "agppppppppls", "kcap_attention64_paged": "agppppppppLs",
     "kcap_append": "agpppppppppppnnts",
@@ -158,7 +160,7 @@ def load_library() -> ctypes.CDLL:
             fn.restype = ctypes.c_int
         lib.ktanh_status_string.restype = ctypes.c_char_p
         lib.ktanh_default_lut.restype = ctypes.POINTER(KtanhLut)
-        lib.kcap_attention_paged_workspace.restype = ctypes.c_size_t
+        lib.kcap_attention_paged_workspace.restype = lib.kcap_attention_backward_workspace.restype = ctypes.c_size_t
         _load_host()
         _lib = lib
     return _lib
@@ -660,6 +662,37 @@ def kcap_attention(q, k, v, q_offsets, k_offsets=None, *, cap, scale=None, causa
 def kcap_attention64(q, k, v, q_offsets, k_offsets=None, **options):
     """``kcap_attention`` with a 64-interval table (``KtanhLut64``; None = the fitted one)."""
     return kcap_attention(q, k, v, q_offsets, k_offsets, **options, _entry="kcap_attention64")
+
+
+def kcap_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets=None, *, cap, scale=None, causal=True, window=0,
+                            dq=None, dk=None, dv=None, lut=None, stream=None, _entry="kcap_attention_backward"):
+    """Gradients of ``kcap_attention`` from its inputs, its results and the gradient of ``out``.  Returns (dq, dk, dv), contiguous."""
+    k_offsets = q_offsets if k_offsets is None else k_offsets
+    for t, what in ((q, "q"), (k, "k"), (v, "v"), (dout, "dout")):
+        _check_rows(t, what)
+    docs = max(q_offsets.numel() - 1, 0)
+    _check_int32(q_offsets, "q_offsets", (docs + 1,))
+    _check_int32(k_offsets, "k_offsets", (docs + 1,))
+    shape = _cap_shape(q, k, v, docs, k.shape[0], cap, scale, window, causal)
+    if dout.shape != q.shape:
+        raise ValueError("dout and q differ in shape")
+    _dense_out(out, "out", q.shape, _BF16_VIEWS)
+    _dense_out(lse, "lse", (q.shape[1], q.shape[0]), (torch.float32,))
+    dq, dk, dv = (_empty(like.shape, like.dtype, like, stream) if t is None else _dense_out(t, what, like.shape, _BF16_VIEWS)
+                  for t, what, like in ((dq, "dq", q), (dk, "dk", k), (dv, "dv", v)))
+    lib = load_library()
+    workspace = _empty((lib.kcap_attention_backward_workspace(shape),), torch.uint8, q, stream)
+    st = getattr(lib, _entry)(shape, dout.data_ptr(), _step(dout, 0), _step(dout, 1), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                              out.data_ptr(), lse.data_ptr(), q_offsets.data_ptr(), k_offsets.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+                              dv.data_ptr(), workspace.data_ptr(), _lut_arg(lut), _stream_handle(stream))
+    if st != 0:
+        raise KtanhError(st, _entry)
+    return dq, dk, dv
+
+
+def kcap_attention64_backward(dout, q, k, v, out, lse, q_offsets, k_offsets=None, **options):
+    """``kcap_attention_backward`` with a 64-interval table (``KtanhLut64``; None = the fitted one)."""
+    return kcap_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets, **options, _entry="kcap_attention64_backward")
 
 
 def _cap_pages(k_cache, v_cache, pages, docs):

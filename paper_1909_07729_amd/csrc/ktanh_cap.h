@@ -120,6 +120,9 @@ __device__ __forceinline__ bf16x8 columns_of(const char *tile, int row0, int c)
 }
 
 // ------------------------------------------------------------------------------------------- blocks
+// Blocks that compute, and behind them `heads` blocks that clear.
+__device__ __forceinline__ unsigned padded(unsigned total) { return (total + 7) / 8 * 8; }
+
 // Consecutive blocks go to the eight dies in turn; block -> place in an order of which each die takes one stretch,
 // so that blocks that share keys share a second-level cache.  Launch 8 * ceil(total / 8) blocks.
 __device__ __forceinline__ unsigned place_of_block(unsigned block, unsigned total)
@@ -163,6 +166,20 @@ __device__ __forceinline__ Stretch stretch_of(int tile, const int *offsets, int 
     s.end = max(offset_at(offsets, s.doc + 1, rows), s.begin);
     s.first = s.begin + (tile - (s.begin / size + s.doc)) * size;
     return s;
+}
+
+// Rows of one head that no document covers (documents follow each other, so they lie before the first and behind the last)
+// of a dense tensor [rows][heads][D] become zero; by one block.
+template <int D, class Also>
+__device__ __forceinline__ void clear_rows(uint16_t *tensor, const int *offsets, int docs, int rows, int heads, int head, Also also)
+{
+    const int first = offset_at(offsets, 0, rows), last = max(offset_at(offsets, docs, rows), first);
+    const int count = first + rows - last;
+    for (long long i = threadIdx.x; i < (long long)count * (D / 4); i += kThreads) {
+        const int n = (int)(i / (D / 4)), row = n < first ? n : n - first + last;
+        *reinterpret_cast<u32x2 *>(tensor + ((long long)row * heads + head) * D + 4 * (i % (D / 4))) = u32x2{0, 0};
+        if (i % (D / 4) == 0) also(row);
+    }
 }
 
 }  // namespace ktanh_cap

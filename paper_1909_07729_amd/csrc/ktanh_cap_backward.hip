@@ -1,0 +1,428 @@
+// libktanh: gradients of the capped attention.
+//
+//   P = e^(y - lse),  dP = dO V^T,  delta = rowsum(dO * O),  dS = P (dP - delta) (1 - t^2),
+//   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
+//
+// 1 - t^2 is the library's derivative identity of TanH at K-TanH's value.  Scores are formed again in two kernels, each
+// summing what it owns in registers, so that no gradient is added to by two blocks and results do not depend on their order:
+//   cap_dq_kernel    128 queries of a head, over their keys; also forms delta
+//   cap_dkdv_kernel  128 keys of a key/value head, over the queries of the heads that share them
+#include "ktanh_cap_args.h"
+
+using namespace ktanh_cap;
+
+namespace {
+
+struct BackwardArgs {
+    CapShape s;
+    const int *q_offsets, *k_offsets;
+    Rows o, d_o;                // dense o, d_o with any strides
+    const float *lse;           // [heads][q_rows]
+    float *delta;               // [heads][q_rows]
+    uint16_t *dq, *dk, *dv;     // dense
+    float *dk_parts, *dv_parts; // [parts][k_rows][kv_heads][dim], NULL where one block sums all heads of a group
+    unsigned tiles;
+    int parts;
+};
+
+// 64 rows of two tensors on their way to LDS: rows from `end` on are zero.
+template <int D>
+struct Pair {
+    static constexpr int kChunks = D / 8, kStep = kThreads / kChunks, kCount = kTile / kStep;
+    u32x4 a[kCount], b[kCount];
+
+    __device__ __forceinline__ void load(const Rows &from_a, const Rows &from_b, int row0, int end)
+    {
+        const int chunk = threadIdx.x % kChunks;
+#pragma unroll
+        for (int n = 0; n < kCount; ++n) {
+            const int row = min(row0 + (int)threadIdx.x / kChunks + n * kStep, end - 1);
+            a[n] = *reinterpret_cast<const u32x4 *>(from_a.at + row * from_a.row + 8 * chunk);
+            b[n] = *reinterpret_cast<const u32x4 *>(from_b.at + row * from_b.row + 8 * chunk);
+        }
+    }
+    __device__ __forceinline__ void store(char *to_a, char *to_b, int row0, int end) const
+    {
+        const int chunk = threadIdx.x % kChunks;
+#pragma unroll
+        for (int n = 0; n < kCount; ++n) {
+            const int row = threadIdx.x / kChunks + n * kStep;
+            const bool there = row0 + row < end;
+            *reinterpret_cast<u32x4 *>(to_a + chunk_at<D>(row, chunk)) = there ? a[n] : u32x4{0, 0, 0, 0};
+            *reinterpret_cast<u32x4 *>(to_b + chunk_at<D>(row, chunk)) = there ? b[n] : u32x4{0, 0, 0, 0};
+        }
+    }
+};
+
+__device__ __forceinline__ Rows of_head(const Rows &t, int head) { return Rows{t.at + head * t.head, t.row, t.head}; }
+
+// A lane's share of one row as second operands: values 16 k + 8 (lane / 32) .. + 7.
+template <int D>
+__device__ __forceinline__ void load_row(bf16x8 (&to)[D / 16], const Rows &from, int row)
+{
+    const uint16_t *at = from.at + row * from.row + 8 * ((threadIdx.x & 63) >> 5);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) to[k] = *reinterpret_cast<const bf16x8 *>(at + 16 * k);
+}
+
+// An accumulator [dim][32 rows] as a lane's row of a dense tensor, times `by`.
+template <int D>
+__device__ __forceinline__ void store_row(uint16_t *row, const f32x16 (&acc)[D / 32], float by)
+{
+    row += 4 * ((threadIdx.x & 63) >> 5);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<u32x2 *>(row + 32 * c + 8 * i) =
+                u32x2{pack2(acc[c][4 * i] * by, acc[c][4 * i + 1] * by), pack2(acc[c][4 * i + 2] * by, acc[c][4 * i + 3] * by)};
+}
+
+template <int D>
+__device__ __forceinline__ void store_row(float *row, const f32x16 (&acc)[D / 32], float by)
+{
+    row += 4 * ((threadIdx.x & 63) >> 5);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<f32x4 *>(row + 32 * c + 8 * i) =
+                f32x4{acc[c][4 * i] * by, acc[c][4 * i + 1] * by, acc[c][4 * i + 2] * by, acc[c][4 * i + 3] * by};
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 1) void cap_dq_kernel(BackwardArgs a, KtCapPack pack)
+{
+    constexpr int kBytes = kTile * D * 2, kSteps = D / 16, kBlocks = D / 32;
+    __shared__ __align__(16) char k_tiles[2][kBytes];
+    __shared__ __align__(16) char v_tiles[2][kBytes];
+    __shared__ f32x2 lines[128];
+
+    const unsigned total = a.tiles * (unsigned)a.s.heads;
+    if (blockIdx.x >= padded(total)) {
+        clear_rows<D>(a.dq, a.q_offsets, a.s.docs, a.s.q_rows, a.s.heads, (int)(blockIdx.x - padded(total)), [](int) {});
+        return;
+    }
+    const unsigned place = place_of_block(blockIdx.x, total);
+    if (place >= total) return;
+    const int in_group = place % a.s.group;
+    const int tile = (int)(a.tiles - 1 - place / a.s.group % a.tiles);
+    const int kv_head = place / a.s.group / a.tiles, head = kv_head * a.s.group + in_group;
+    const Stretch at = stretch_of(tile, a.q_offsets, a.s.docs, a.s.q_rows, kRows);
+    if (at.first >= at.end) return;
+    const int k_begin = offset_at(a.k_offsets, at.doc, a.s.k_rows);
+    const int n_keys = max(offset_at(a.k_offsets, at.doc + 1, a.s.k_rows) - k_begin, 0);
+    Rows keys = of_head(a.s.k, kv_head), values = of_head(a.s.v, kv_head);
+    keys.at += k_begin * keys.row;
+    values.at += k_begin * values.row;
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int shift = n_keys - (at.end - at.begin);
+    const int row0 = at.first + 32 * wave, row = row0 + (lane & 31), row_there = min(row, at.end - 1);
+    const int place0 = row0 - at.begin + shift, my_place = row - at.begin + shift;
+    const int block_first = at.first - at.begin + shift;
+    const int block_last = min(at.first + kRows, at.end) - 1 - at.begin + shift;
+    const int key_end = a.s.causal ? min(n_keys, block_last + 1) : n_keys;
+    const int key_begin = a.s.window > 0 ? max(0, block_first - a.s.window + 1) & ~(kTile - 1) : 0;
+    spread_lines(lines, pack, 1.0f);
+
+    bf16x8 q[kSteps], d_o[kSteps];
+    load_row<D>(q, of_head(a.s.q, head), row_there);
+    load_row<D>(d_o, of_head(a.d_o, head), row_there);
+    float delta = 0.0f;
+    {
+        bf16x8 o[kSteps];
+        load_row<D>(o, of_head(a.o, head), row_there);
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) delta = __builtin_fmaf((float)d_o[k][i], (float)o[k][i], delta);
+        delta += __shfl_xor(delta, 32);
+    }
+    const long long sum_at = (long long)head * a.s.q_rows + row;
+    if (row < at.end && lane < 32) a.delta[sum_at] = delta;
+    const float lse2 = a.lse[(long long)head * a.s.q_rows + row_there] * kLog2e;
+    const float unit = a.s.cap * kLog2e;
+
+    f32x16 dq[kBlocks];
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c) dq[c] = f32x16{0};
+    Pair<D> share;
+    if (key_begin < key_end) share.load(keys, values, key_begin, n_keys);
+    int buffer = 0;
+    for (int j0 = key_begin; j0 < key_end; j0 += kTile, buffer ^= 1) {
+        char *k_tile = k_tiles[buffer], *v_tile = v_tiles[buffer];
+        share.store(k_tile, v_tile, j0, n_keys);
+        __syncthreads();
+        if (j0 + kTile < key_end) share.load(keys, values, j0 + kTile, n_keys);
+        const bool none = (a.s.causal && j0 > place0 + 31) || (a.s.window > 0 && j0 + kTile - 1 <= place0 - a.s.window) || row0 >= at.end;
+        if (none) continue;
+        const bool partial = j0 + kTile > n_keys || (a.s.causal && j0 + kTile - 1 > place0) ||
+                             (a.s.window > 0 && j0 <= place0 + 31 - a.s.window);
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+            f32x16 s = f32x16{0}, dp = f32x16{0};
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) s = mfma(rows_of<D>(k_tile, 32 * sub, k), q[k], s);
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) dp = mfma(rows_of<D>(v_tile, 32 * sub, k), d_o[k], dp);
+            float ds[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float t = capped(s[r] * a.s.to_x, lines);
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(t, unit, -lse2));
+                ds[r] = p * (dp[r] - delta) * __builtin_fmaf(-t, t, 1.0f);
+            }
+            if (partial) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int j = j0 + 32 * sub + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
+                    const bool seen = j < n_keys && (!a.s.causal || j <= my_place) && (a.s.window == 0 || j > my_place - a.s.window);
+                    ds[r] = seen ? ds[r] : 0.0f;
+                }
+            }
+            const bf16x8 shares[2] = {pack8(ds), pack8(ds + 8)};
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int c = 0; c < kBlocks; ++c) dq[c] = mfma(columns_of<D>(k_tile, 32 * sub + 16 * i, c), shares[i], dq[c]);
+        }
+    }
+    if (row < at.end) store_row<D>(a.dq + ((long long)row * a.s.heads + head) * D, dq, a.s.scale);
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, KtCapPack pack)
+{
+    constexpr int kBytes = kTile * D * 2, kSteps = D / 16, kBlocks = D / 32;
+    __shared__ __align__(16) char q_tiles[2][kBytes];
+    __shared__ __align__(16) char do_tiles[2][kBytes];
+    __shared__ __align__(16) float sums[2][2][kTile];  // lse * log2 e | delta of a tile's rows
+    __shared__ f32x2 lines[128];
+
+    const unsigned total = a.tiles * (unsigned)(a.s.kv_heads * a.parts);
+    if (blockIdx.x >= padded(total)) {  // where there are parts, the kernel that joins them clears
+        const int head = (int)(blockIdx.x - padded(total));
+        clear_rows<D>(a.dk, a.k_offsets, a.s.docs, a.s.k_rows, a.s.kv_heads, head, [](int) {});
+        clear_rows<D>(a.dv, a.k_offsets, a.s.docs, a.s.k_rows, a.s.kv_heads, head, [](int) {});
+        return;
+    }
+    const unsigned place = place_of_block(blockIdx.x, total);
+    if (place >= total) return;
+    const int part = place % a.parts, tile = (int)(place / a.parts % a.tiles), kv_head = place / a.parts / a.tiles;
+    const Stretch at = stretch_of(tile, a.k_offsets, a.s.docs, a.s.k_rows, kRows);
+    if (at.first >= at.end) return;
+    const int q_begin = offset_at(a.q_offsets, at.doc, a.s.q_rows);
+    const int n_queries = max(offset_at(a.q_offsets, at.doc + 1, a.s.q_rows) - q_begin, 0);
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int shift = (at.end - at.begin) - n_queries;  // query i is key i + shift
+    const int row0 = at.first + 32 * wave, row = row0 + (lane & 31), row_there = min(row, at.end - 1);
+    const int key0 = row0 - at.begin, key = row - at.begin;
+    const int block_first = at.first - at.begin, block_last = min(at.first + kRows, at.end) - 1 - at.begin;
+    // queries that see some key of the block
+    const int from = a.s.causal ? max(0, block_first - shift) & ~(kTile - 1) : 0;
+    const int to = a.s.window > 0 ? min((long long)n_queries, max(0ll, (long long)block_last - shift + a.s.window)) : n_queries;
+    spread_lines(lines, pack, 1.0f);
+    const float unit = a.s.cap * kLog2e;
+
+    bf16x8 k[kSteps], v[kSteps];
+    load_row<D>(k, of_head(a.s.k, kv_head), row_there);
+    load_row<D>(v, of_head(a.s.v, kv_head), row_there);
+    f32x16 dk[kBlocks], dv[kBlocks];
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c) dk[c] = dv[c] = f32x16{0};
+
+    const int heads = a.s.group / a.parts, head0 = kv_head * a.s.group + part * heads;
+    const int rounds = from < to ? (to - from + kTile - 1) / kTile : 0;
+    Pair<D> share;
+    float share_sum = 0.0f;
+    auto load = [&](int n) {  // the n-th tile: heads one behind the other
+        const int head = head0 + n / rounds, i0 = from + n % rounds * kTile;
+        Rows q = of_head(a.s.q, head), d_o = of_head(a.d_o, head);
+        q.at += q_begin * q.row;
+        d_o.at += q_begin * d_o.row;
+        share.load(q, d_o, i0, n_queries);
+        const int i = min(i0 + lane, n_queries - 1);
+        if (wave < 2) share_sum = (wave == 0 ? a.lse : a.delta)[(long long)head * a.s.q_rows + q_begin + i];
+    };
+    if (rounds > 0) load(0);
+    int buffer = 0;
+    for (int n = 0; n < heads * rounds; ++n, buffer ^= 1) {
+        const int i0 = from + n % rounds * kTile;
+        char *q_tile = q_tiles[buffer], *do_tile = do_tiles[buffer];
+        share.store(q_tile, do_tile, i0, n_queries);
+        if (wave < 2) sums[buffer][wave][lane] = wave == 0 ? share_sum * kLog2e : share_sum;
+        __syncthreads();
+        if (n + 1 < heads * rounds) load(n + 1);
+        const int first = i0 + shift;  // the tile's first query's place
+        const bool none = (a.s.causal && first + kTile - 1 < key0) || (a.s.window > 0 && first > key0 + 31 + a.s.window - 1) || row0 >= at.end;
+        if (none) continue;
+        const bool partial = i0 + kTile > n_queries || (a.s.causal && first < key0 + 31) || (a.s.window > 0 && first + kTile - 1 >= key0 + a.s.window);
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+            f32x16 s = f32x16{0}, dp = f32x16{0};
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) s = mfma(rows_of<D>(q_tile, 32 * sub, i), k[i], s);
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) dp = mfma(rows_of<D>(do_tile, 32 * sub, i), v[i], dp);
+            float p[16], ds[16];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int at_row = 32 * sub + 8 * g + 4 * (lane >> 5);
+                const f32x4 lse2 = *reinterpret_cast<const f32x4 *>(&sums[buffer][0][at_row]);
+                const f32x4 delta = *reinterpret_cast<const f32x4 *>(&sums[buffer][1][at_row]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 4 * g + e;
+                    const float t = capped(s[r] * a.s.to_x, lines);
+                    p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(t, unit, -lse2[e]));
+                    ds[r] = p[r] * (dp[r] - delta[e]) * __builtin_fmaf(-t, t, 1.0f);
+                }
+            }
+            if (partial) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int i = i0 + 32 * sub + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
+                    const bool seen = i < n_queries && (!a.s.causal || key <= i + shift) && (a.s.window == 0 || key > i + shift - a.s.window);
+                    p[r] = seen ? p[r] : 0.0f;
+                    ds[r] = seen ? ds[r] : 0.0f;
+                }
+            }
+            const bf16x8 weights[2] = {pack8(p), pack8(p + 8)}, shares[2] = {pack8(ds), pack8(ds + 8)};
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int c = 0; c < kBlocks; ++c) {
+                    dv[c] = mfma(columns_of<D>(do_tile, 32 * sub + 16 * i, c), weights[i], dv[c]);
+                    dk[c] = mfma(columns_of<D>(q_tile, 32 * sub + 16 * i, c), shares[i], dk[c]);
+                }
+        }
+    }
+    if (row >= at.end) return;
+    const long long to_row = ((long long)row * a.s.kv_heads + kv_head) * D;
+    if (a.dk_parts == nullptr) {
+        store_row<D>(a.dk + to_row, dk, a.s.scale);
+        store_row<D>(a.dv + to_row, dv, 1.0f);
+    } else {
+        const long long part_at = (long long)part * a.s.k_rows * a.s.kv_heads * D + to_row;
+        store_row<D>(a.dk_parts + part_at, dk, a.s.scale);
+        store_row<D>(a.dv_parts + part_at, dv, 1.0f);
+    }
+}
+
+// The parts of shared heads added up in their order, zero for rows of no document: 8 values of dk or dv for each thread.
+__global__ __launch_bounds__(kThreads) void cap_join_grads_kernel(BackwardArgs a, long long width)
+{
+    const long long i = ((long long)blockIdx.x * kThreads + threadIdx.x) * 8, each = a.s.k_rows * width;
+    if (i >= each) return;
+    const int first = offset_at(a.k_offsets, 0, a.s.k_rows), row = (int)(i / width);
+    const float *from = blockIdx.y == 0 ? a.dk_parts : a.dv_parts;
+    float v[8] = {};
+    if (row >= first && row < offset_at(a.k_offsets, a.s.docs, a.s.k_rows))
+        for (int p = 0; p < a.parts; ++p)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x4 w = *reinterpret_cast<const f32x4 *>(from + p * each + i + 4 * h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[4 * h + e] += w[e];
+            }
+    *reinterpret_cast<bf16x8 *>((blockIdx.y == 0 ? a.dk : a.dv) + i) = pack8(v);
+}
+
+// Blocks over 128 keys of a key/value head, all heads of its group one behind the other, where those blocks are many; else one head each.
+int parts_of(const kcap_shape_t &s)
+{
+    const size_t group = s.heads / s.kv_heads;
+    return (s.k_rows / kRows + s.docs) * s.kv_heads >= 2048 ? 1 : (int)group;
+}
+
+size_t delta_bytes(const kcap_shape_t &s) { return (s.heads * s.q_rows * 4 + 127) / 128 * 128; }
+
+template <class Lut>
+ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t do_row, size_t do_head, const uint16_t *q, const uint16_t *k,
+                        const uint16_t *v, const uint16_t *o, const float *lse, const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *dq,
+                        uint16_t *dk, uint16_t *dv, void *workspace, const Lut *lut, ktanh_stream_t stream)
+{
+    if (shape == nullptr) return KT_ERR_NULL;
+    if (shape->docs == 0 || (shape->q_rows == 0 && shape->k_rows == 0)) return KT_OK;
+    const bool queries = shape->q_rows != 0, keys = shape->k_rows != 0;
+    if (q_offsets == nullptr || k_offsets == nullptr || workspace == nullptr) return KT_ERR_NULL;
+    if (queries && (d_o == nullptr || q == nullptr || o == nullptr || lse == nullptr || dq == nullptr)) return KT_ERR_NULL;
+    if (keys && (k == nullptr || v == nullptr || dk == nullptr || dv == nullptr)) return KT_ERR_NULL;
+    BackwardArgs a{};
+    ktanh_status_t st = read_shape(shape, q, k, v, &a.s);
+    if (st != KT_OK) return st;
+    if (do_row % 8 != 0 || do_head % 8 != 0 || !aligned16(d_o) || !aligned16(o) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(workspace) ||
+        reinterpret_cast<uintptr_t>(lse) % 4 != 0 || reinterpret_cast<uintptr_t>(q_offsets) % 4 != 0 || reinterpret_cast<uintptr_t>(k_offsets) % 4 != 0)
+        return KT_ERR_ALIGN;
+    if (do_row > (size_t)1 << 40 || do_head > (size_t)1 << 40) return KT_ERR_SHAPE;
+    KtCapPack pack;
+    if ((st = pack_lines(lut, &pack)) != KT_OK) return st;
+    const long long dim = (long long)shape->dim;
+    a.q_offsets = q_offsets;
+    a.k_offsets = k_offsets;
+    a.o = Rows{o, a.s.heads * dim, dim};
+    a.d_o = Rows{d_o, (long long)do_row, (long long)do_head};
+    a.lse = lse;
+    a.delta = static_cast<float *>(workspace);
+    a.dq = dq;
+    a.dk = dk;
+    a.dv = dv;
+    a.parts = parts_of(*shape);
+    const long long each = (long long)a.s.k_rows * a.s.kv_heads * dim;
+    if (a.parts > 1) {
+        a.dk_parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + delta_bytes(*shape));
+        a.dv_parts = a.dk_parts + a.parts * each;
+    }
+    const unsigned long long q_tiles = shape->q_rows / kRows + shape->docs, k_tiles = shape->k_rows / kRows + shape->docs;
+    const unsigned long long q_blocks = (q_tiles * a.s.heads + 7) / 8 * 8 + a.s.heads;
+    const unsigned long long k_blocks = (k_tiles * a.s.kv_heads * a.parts + 7) / 8 * 8 + (a.parts == 1 ? a.s.kv_heads : 0);
+    const unsigned long long joins = (unsigned long long)(each + kThreads * 8 - 1) / (kThreads * 8);
+    if (q_blocks > kMaxBlocks || k_blocks > kMaxBlocks || joins > kMaxBlocks) return KT_ERR_SHAPE;
+
+    const auto on = static_cast<hipStream_t>(stream);
+    if (queries) {
+        a.tiles = (unsigned)q_tiles;
+        auto *kernel = dim == 64 ? &cap_dq_kernel<64> : &cap_dq_kernel<128>;
+        kernel<<<dim3((unsigned)q_blocks), dim3(kThreads), 0, on>>>(a, pack);
+        if ((st = launched()) != KT_OK) return st;
+    }
+    if (!keys) return KT_OK;
+    a.tiles = (unsigned)k_tiles;
+    auto *kernel = dim == 64 ? &cap_dkdv_kernel<64> : &cap_dkdv_kernel<128>;
+    kernel<<<dim3((unsigned)k_blocks), dim3(kThreads), 0, on>>>(a, pack);
+    if ((st = launched()) != KT_OK) return st;
+    if (a.parts > 1) {
+        cap_join_grads_kernel<<<dim3((unsigned)joins, 2), dim3(kThreads), 0, on>>>(a, a.s.kv_heads * dim);
+        st = launched();
+    }
+    return st;
+}
+
+}  // namespace
+
+extern "C" size_t kcap_attention_backward_workspace(const kcap_shape_t *shape)
+{
+    if (shape == nullptr || shape->kv_heads == 0 || shape->heads < shape->kv_heads || shape->heads > 65536 || shape->dim > 128 ||
+        shape->q_rows > 1u << 30 || shape->k_rows > 1u << 30 || shape->docs > 1u << 30)
+        return 0;
+    const size_t parts = (size_t)parts_of(*shape);
+    return delta_bytes(*shape) + 128 + (parts > 1 ? 2 * parts * shape->k_rows * shape->kv_heads * shape->dim * 4 : 0);
+}
+
+extern "C" ktanh_status_t kcap_attention_backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t do_row, size_t do_head, const uint16_t *q,
+                                                  const uint16_t *k, const uint16_t *v, const uint16_t *o, const float *lse, const int32_t *q_offsets,
+                                                  const int32_t *k_offsets, uint16_t *dq, uint16_t *dk, uint16_t *dv, void *workspace,
+                                                  const ktanh_lut_t *lut, ktanh_stream_t stream)
+{
+    return backward(shape, d_o, do_row, do_head, q, k, v, o, lse, q_offsets, k_offsets, dq, dk, dv, workspace, lut, stream);
+}
+
+extern "C" ktanh_status_t kcap_attention64_backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t do_row, size_t do_head, const uint16_t *q,
+                                                    const uint16_t *k, const uint16_t *v, const uint16_t *o, const float *lse, const int32_t *q_offsets,
+                                                    const int32_t *k_offsets, uint16_t *dq, uint16_t *dk, uint16_t *dv, void *workspace,
+                                                    const ktanh_lut64_t *lut, ktanh_stream_t stream)
+{
+    return backward(shape, d_o, do_row, do_head, q, k, v, o, lse, q_offsets, k_offsets, dq, dk, dv, workspace, lut, stream);
+}

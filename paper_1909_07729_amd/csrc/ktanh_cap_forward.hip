@@ -112,6 +112,13 @@ __global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a,
     __shared__ int special;  // whether a value was taken out of a tile
 
     const unsigned total = a.tiles * (unsigned)a.s.heads;
+    if (blockIdx.x >= padded(total)) {
+        const int head = (int)(blockIdx.x - padded(total));
+        clear_rows<D>(a.o, a.q_offsets, a.s.docs, a.s.q_rows, a.s.heads, head, [&](int row) {
+            if (a.lse != nullptr) a.lse[(long long)head * a.s.q_rows + row] = -__builtin_inff();
+        });
+        return;
+    }
     const unsigned place = place_of_block(blockIdx.x, total);
     if (place >= total) return;
     // heads that share keys side by side, then the stretches from the last (the longest, if causal) to the first
@@ -260,7 +267,7 @@ __global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a,
 template <bool PAGED>
 ktanh_status_t launch_forward(const ForwardArgs &a, size_t dim, const KtCapPack &pack, ktanh_stream_t stream)
 {
-    const unsigned long long blocks = ((unsigned long long)a.tiles * a.s.heads + 7) / 8 * 8;
+    const unsigned long long blocks = ((unsigned long long)a.tiles * a.s.heads + 7) / 8 * 8 + a.s.heads;
     if (blocks > kMaxBlocks) return KT_ERR_SHAPE;
     auto *kernel = dim == 64 ? &cap_forward_kernel<64, PAGED> : &cap_forward_kernel<128, PAGED>;
     kernel<<<dim3((unsigned)blocks), dim3(kThreads), 0, static_cast<hipStream_t>(stream)>>>(a, pack);
