@@ -303,8 +303,9 @@ ktanh_status_t klstm_cell64_backward(const uint16_t *gates, const float *c_prev,
  *   t = Kf(q.k * (scale / cap)),   y = cap * t,   weight = e^y / sum of e^y over the keys that q sees
  * and the output is the weighted sum of the values.  Kf is ktanh_f32 with the bits that its shift drops kept (the line
  * A x + B that Algorithm 1 follows on each interval), one fused multiply-add; scale / cap is rounded to Float32 once.
- * q . k, the weights and their sum are Float32; the weights are rounded to BFloat16 for the product with the
- * values, whose sum is Float32; outputs are rounded to nearest even.  Since |y| <= cap <= KCAP_MAX no maximum is
+ * q . k and the weights are Float32; the weights are rounded to BFloat16 for the product with the values, whose
+ * sum is Float32 and is divided by the sum of the rounded weights (the log-sum is that of the weights before); outputs are rounded to
+ * nearest even.  Since |y| <= cap <= KCAP_MAX no maximum is
  * subtracted; the sums of e^y v must stay within Float32, which they do at any cap for values up to 1e9.  K-TanH jumps at the ends of its intervals, by up to 0.016: y by up to 0.016 cap, and two
  * computations whose q . k differ in the last bits may differ by that there.
  *
@@ -333,15 +334,16 @@ typedef struct kcap_shape {
 
 /* q_offsets, k_offsets: device, docs + 1 each: rows of document d are offsets[d] .. offsets[d + 1] - 1.
  *   o    device, out: BFloat16 [q_rows][heads][dim], dense; rows in no document become 0
+ *   rest device, out, may be NULL: like o, what its rounding dropped, rounded: training keeps it for the gradients
  *   lse  device, out, may be NULL: Float32 [heads][q_rows], log of the sum of e^y (kcap_attention_backward reads it)
- * q, k, v 16-byte aligned, o 8-byte (KT_ERR_ALIGN).  q_rows == 0 or docs == 0 returns KT_OK without a launch.
+ * q, k, v 16-byte aligned, o and rest 8-byte (KT_ERR_ALIGN).  q_rows == 0 or docs == 0 returns KT_OK without a launch.
  * KT_ERR_SHAPE: another dim, heads not a multiple of kv_heads, a cap or scale out of range, more than 2^30 rows.
  * KT_ERR_LUT: also a table whose K exceeds 1. */
 ktanh_status_t kcap_attention(const kcap_shape_t *shape, const uint16_t *q, const uint16_t *k, const uint16_t *v,
-                              const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *o, float *lse,
+                              const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *o, uint16_t *rest, float *lse,
                               const ktanh_lut_t *lut, ktanh_stream_t stream);
 ktanh_status_t kcap_attention64(const kcap_shape_t *shape, const uint16_t *q, const uint16_t *k, const uint16_t *v,
-                                const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *o, float *lse,
+                                const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *o, uint16_t *rest, float *lse,
                                 const ktanh_lut64_t *lut, ktanh_stream_t stream);
 
 /* Gradients of kcap_attention from its inputs and its o and lse, with the library's derivative identity of TanH:
@@ -350,16 +352,17 @@ ktanh_status_t kcap_attention64(const kcap_shape_t *shape, const uint16_t *q, co
  * rounded, in a fixed order.  Rows in no document, and queries that see no key, have the gradient 0.  A NaN or
  * infinity in a document may reach all of that document's gradients.
  *   d_o        device, BFloat16 [q_rows][heads][dim] with strides do_row, do_head (multiples of 8), 16-byte aligned
- *   o, lse     as kcap_attention gave them
+ *   o, rest, lse  as kcap_attention gave them.  rest may be NULL: dq and dk of peaked rows are then less exact (for scores of
+ *              standard deviation 6 they are 0.005 off in norm instead of 0.0027, of which 0.0017 is their own rounding)
  *   dq, dk, dv device, out: BFloat16, dense [rows][heads][dim], 16-byte aligned
  *   workspace  device, 16-byte aligned, kcap_attention_backward_workspace bytes, whatever is in it */
 size_t kcap_attention_backward_workspace(const kcap_shape_t *shape);
 ktanh_status_t kcap_attention_backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t do_row, size_t do_head, const uint16_t *q,
-                                       const uint16_t *k, const uint16_t *v, const uint16_t *o, const float *lse,
+                                       const uint16_t *k, const uint16_t *v, const uint16_t *o, const uint16_t *rest, const float *lse,
                                        const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *dq, uint16_t *dk, uint16_t *dv,
                                        void *workspace, const ktanh_lut_t *lut, ktanh_stream_t stream);
 ktanh_status_t kcap_attention64_backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t do_row, size_t do_head, const uint16_t *q,
-                                         const uint16_t *k, const uint16_t *v, const uint16_t *o, const float *lse,
+                                         const uint16_t *k, const uint16_t *v, const uint16_t *o, const uint16_t *rest, const float *lse,
                                          const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *dq, uint16_t *dk, uint16_t *dv,
                                          void *workspace, const ktanh_lut64_t *lut, ktanh_stream_t stream);
 

@@ -111,18 +111,20 @@ class _KCapAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, q_offsets, k_offsets, options, wide):
         attend = binding.kcap_attention64 if wide else binding.kcap_attention
-        out, lse = attend(q, k, v, q_offsets, k_offsets, **options)
-        ctx.save_for_backward(q, k, v, out, lse, q_offsets, k_offsets)
+        # what the rounding of the output drops is kept where gradients will be asked for
+        rest = torch.empty(q.shape, dtype=q.dtype, device=q.device) if any(ctx.needs_input_grad[:3]) else None
+        out, lse = attend(q, k, v, q_offsets, k_offsets, rest=rest, **options)
+        ctx.save_for_backward(q, k, v, out, lse, q_offsets, k_offsets, rest)
         ctx.options, ctx.wide = options, wide
         return out
 
     @staticmethod
     def backward(ctx, dout):
         attend = binding.kcap_attention64_backward if ctx.wide else binding.kcap_attention_backward
-        *tensors, q_offsets, k_offsets = ctx.saved_tensors
+        *tensors, q_offsets, k_offsets, rest = ctx.saved_tensors
         if dout.stride(-1) != 1 or any(step % 8 for step in dout.stride()[:2]) or dout.data_ptr() % 16:
             dout = dout.contiguous()        # also the expanded gradient of a sum
-        return (*attend(dout, *tensors, q_offsets, k_offsets, **ctx.options), None, None, None, None)
+        return (*attend(dout, *tensors, q_offsets, k_offsets, rest=rest, **ctx.options), None, None, None, None)
 
 
 def _activation(code, function, names, x, lut, intervals):

@@ -46,9 +46,9 @@ SIGNATURES = {
     "klstm_cell_backward": "ppppppnnls", "klstm_cell64_backward": "ppppppnnLs",
     "kpade32_bf16": "ppns", "kpade78_bf16": "ppns",
     "ktaylor2_bf16": "ppns", "ktaylor3_bf16": "ppns",
-    "kcap_attention": "apppppppls", "kcap_attention64": "apppppppLs",
+    "kcap_attention": "appppppppls", "kcap_attention64": "appppppppLs",
     "kcap_attention_backward_workspace": "a",
-    "kcap_attention_backward": "apnnpppppppppppls", "kcap_attention64_backward": "apnnpppppppppppLs",
+    "kcap_attention_backward": "apnnppppppppppppls", "kcap_attention64_backward": "apnnppppppppppppLs",
     "kcap_attention_paged_workspace": "agt",
     "kcap_attention_paged": "agppppppppls", "kcap_attention64_paged": "agppppppppLs",
     "kcap_append": "agpppppppppppnnts",
@@ -634,13 +634,14 @@ def _dense_out(t, what, shape, dtypes):
 
 
 def kcap_attention(q, k, v, q_offsets, k_offsets=None, *, cap, scale=None, causal=True, window=0, out=None, lse=None,
-                   lut=None, stream=None, _entry="kcap_attention"):
+                   rest=None, lut=None, stream=None, _entry="kcap_attention"):
     """Attention with scores cap * K(scale * q.k / cap) over packed documents.
 
     q [q_rows, heads, dim], k and v [k_rows, kv_heads, dim] BFloat16, any strides with dim contiguous; q_offsets and
     k_offsets int32 [documents + 1] on the GPU (k_offsets None: the same rows).  A query is at the place of its key counted from
     the documents' ends; it sees the keys up to there if ``causal``, and the last ``window`` of them if that is not 0.
-    ``scale`` None is dim ** -0.5.  Returns (out [q_rows, heads, dim], lse [heads, q_rows] Float32).
+    ``scale`` None is dim ** -0.5.  ``rest``, a tensor like ``out``, takes what the rounding of ``out`` dropped, for the
+    gradients.  Returns (out [q_rows, heads, dim], lse [heads, q_rows] Float32).
     """
     k_offsets = q_offsets if k_offsets is None else k_offsets
     for t, what in ((q, "q"), (k, "k"), (v, "v")):
@@ -652,8 +653,10 @@ def kcap_attention(q, k, v, q_offsets, k_offsets=None, *, cap, scale=None, causa
     out = _empty(q.shape, q.dtype, q, stream) if out is None else _dense_out(out, "out", q.shape, _BF16_VIEWS)
     sums = (q.shape[1], q.shape[0])
     lse = _empty(sums, torch.float32, q, stream) if lse is None else _dense_out(lse, "lse", sums, (torch.float32,))
+    if rest is not None:
+        _dense_out(rest, "rest", q.shape, _BF16_VIEWS)
     st = getattr(load_library(), _entry)(shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_offsets.data_ptr(), k_offsets.data_ptr(),
-                                         out.data_ptr(), lse.data_ptr(), _lut_arg(lut), _stream_handle(stream))
+                                         out.data_ptr(), None if rest is None else rest.data_ptr(), lse.data_ptr(), _lut_arg(lut), _stream_handle(stream))
     if st != 0:
         raise KtanhError(st, _entry)
     return out, lse
@@ -665,8 +668,9 @@ def kcap_attention64(q, k, v, q_offsets, k_offsets=None, **options):
 
 
 def kcap_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets=None, *, cap, scale=None, causal=True, window=0,
-                            dq=None, dk=None, dv=None, lut=None, stream=None, _entry="kcap_attention_backward"):
-    """Gradients of ``kcap_attention`` from its inputs, its results and the gradient of ``out``.  Returns (dq, dk, dv), contiguous."""
+                            rest=None, dq=None, dk=None, dv=None, lut=None, stream=None, _entry="kcap_attention_backward"):
+    """Gradients of ``kcap_attention`` from its inputs, its results and the gradient of ``out``, more
+    exact with its ``rest``.  Returns (dq, dk, dv), contiguous."""
     k_offsets = q_offsets if k_offsets is None else k_offsets
     for t, what in ((q, "q"), (k, "k"), (v, "v"), (dout, "dout")):
         _check_rows(t, what)
@@ -680,10 +684,12 @@ def kcap_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets=None, 
     _dense_out(lse, "lse", (q.shape[1], q.shape[0]), (torch.float32,))
     dq, dk, dv = (_empty(like.shape, like.dtype, like, stream) if t is None else _dense_out(t, what, like.shape, _BF16_VIEWS)
                   for t, what, like in ((dq, "dq", q), (dk, "dk", k), (dv, "dv", v)))
+    if rest is not None:
+        _dense_out(rest, "rest", q.shape, _BF16_VIEWS)
     lib = load_library()
     workspace = _empty((lib.kcap_attention_backward_workspace(shape),), torch.uint8, q, stream)
     st = getattr(lib, _entry)(shape, dout.data_ptr(), _step(dout, 0), _step(dout, 1), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                              out.data_ptr(), lse.data_ptr(), q_offsets.data_ptr(), k_offsets.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+                              out.data_ptr(), None if rest is None else rest.data_ptr(), lse.data_ptr(), q_offsets.data_ptr(), k_offsets.data_ptr(), dq.data_ptr(), dk.data_ptr(),
                               dv.data_ptr(), workspace.data_ptr(), _lut_arg(lut), _stream_handle(stream))
     if st != 0:
         raise KtanhError(st, _entry)

@@ -60,6 +60,21 @@ __device__ __forceinline__ bf16x8 pack8(const float *v)
     return __builtin_bit_cast(bf16x8, u32x4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])});
 }
 
+// The same, with the sum of the rounded values.  Outputs are divided by the sum of the weights as the product has them: the
+// roundings of one weight in numerator and denominator cancel (o is off by 0.0018 of its norm instead of 0.0023, 0.0017 of it the
+// rounding of o itself).
+__device__ __forceinline__ bf16x8 pack8(const float *v, float *sum)
+{
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bf16x2 pair = __builtin_convertvector(f32x2{v[2 * i], v[2 * i + 1]}, bf16x2);
+        *sum = __builtin_amdgcn_fdot2_f32_bf16(pair, __builtin_bit_cast(bf16x2, 0x3F803F80u), *sum, false);
+        w[i] = __builtin_bit_cast(uint32_t, pair);
+    }
+    return __builtin_bit_cast(bf16x8, w);
+}
+
 // ------------------------------------------------------------------------------------------ the cap
 // lines[i], i = low three exponent bits << 4 | high four mantissa bits, times `unit`.
 __device__ __forceinline__ void spread_lines(f32x2 *lines, const KtCapPack &pack, float unit)
@@ -79,6 +94,16 @@ __device__ __forceinline__ float capped(float x, const f32x2 *lines)
     const uint32_t key = __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fabsf(x), 0.125f, 16.0f));
     const f32x2 line = *reinterpret_cast<const f32x2 *>(reinterpret_cast<const char *>(lines) + ((key >> 16) & 0x3F8u));
     return __builtin_copysignf(__builtin_fmaf(line.x, __builtin_fabsf(x), line.y), x);
+}
+
+// Whether some |s * to_x| of the wavefront leaves the identity; a NaN does not.  (K is only worth its eleven instructions
+// where one does: heads whose scores stay below cap / 4 take the exponential of the score itself, with the same roundings.)
+__device__ __forceinline__ bool any_capped(const f32x16 &s, float to_x)
+{
+    float m = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) m = __builtin_fmaxf(__builtin_fmaxf(m, __builtin_fabsf(s[r])), __builtin_fabsf(s[r + 1]));
+    return __any(__builtin_fabsf(m * to_x) >= 0.25f);
 }
 
 // ------------------------------------------------------------------------------------- tiles in LDS

@@ -16,7 +16,7 @@ namespace {
 struct BackwardArgs {
     CapShape s;
     const int *q_offsets, *k_offsets;
-    Rows o, d_o;                // dense o, d_o with any strides
+    Rows o, rest, d_o;          // dense o and rest, d_o with any strides
     const float *lse;           // [heads][q_rows]
     float *delta;               // [heads][q_rows]
     uint16_t *dq, *dk, *dv;     // dense
@@ -131,12 +131,18 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dq_kernel(BackwardArgs a, KtC
     load_row<D>(d_o, of_head(a.d_o, head), row_there);
     float delta = 0.0f;
     {
-        bf16x8 o[kSteps];
+        bf16x8 o[kSteps], rest[kSteps];
         load_row<D>(o, of_head(a.o, head), row_there);
+        if (a.rest.at != nullptr) {
+            load_row<D>(rest, of_head(a.rest, head), row_there);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) rest[k] = bf16x8{};
+        }
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) delta = __builtin_fmaf((float)d_o[k][i], (float)o[k][i], delta);
+            for (int i = 0; i < 8; ++i) delta = __builtin_fmaf((float)d_o[k][i], (float)o[k][i] + (float)rest[k][i], delta);
         delta += __shfl_xor(delta, 32);
     }
     const long long sum_at = (long long)head * a.s.q_rows + row;
@@ -167,9 +173,16 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dq_kernel(BackwardArgs a, KtC
 #pragma unroll
             for (int k = 0; k < kSteps; ++k) dp = mfma(rows_of<D>(v_tile, 32 * sub, k), d_o[k], dp);
             float ds[16];
+            if (any_capped(s, a.s.to_x)) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = capped(s[r] * a.s.to_x, lines);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] *= a.s.to_x;
+            }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float t = capped(s[r] * a.s.to_x, lines);
+                const float t = s[r];
                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(t, unit, -lse2));
                 ds[r] = p * (dp[r] - delta) * __builtin_fmaf(-t, t, 1.0f);
             }
@@ -177,7 +190,7 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dq_kernel(BackwardArgs a, KtC
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int j = j0 + 32 * sub + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
-                    const bool seen = j < n_keys && (!a.s.causal || j <= my_place) && (a.s.window == 0 || j > my_place - a.s.window);
+                    const bool seen = (j < n_keys) & (!a.s.causal | (j <= my_place)) & ((a.s.window == 0) | (j > my_place - a.s.window));
                     ds[r] = seen ? ds[r] : 0.0f;
                 }
             }
@@ -267,6 +280,13 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, K
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) dp = mfma(rows_of<D>(do_tile, 32 * sub, i), v[i], dp);
             float p[16], ds[16];
+            if (any_capped(s, a.s.to_x)) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = capped(s[r] * a.s.to_x, lines);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] *= a.s.to_x;
+            }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int at_row = 32 * sub + 8 * g + 4 * (lane >> 5);
@@ -275,7 +295,7 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, K
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int r = 4 * g + e;
-                    const float t = capped(s[r] * a.s.to_x, lines);
+                    const float t = s[r];
                     p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(t, unit, -lse2[e]));
                     ds[r] = p[r] * (dp[r] - delta[e]) * __builtin_fmaf(-t, t, 1.0f);
                 }
@@ -284,7 +304,7 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, K
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int i = i0 + 32 * sub + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
-                    const bool seen = i < n_queries && (!a.s.causal || key <= i + shift) && (a.s.window == 0 || key > i + shift - a.s.window);
+                    const bool seen = (i < n_queries) & (!a.s.causal | (key <= i + shift)) & ((a.s.window == 0) | (key > i + shift - a.s.window));
                     p[r] = seen ? p[r] : 0.0f;
                     ds[r] = seen ? ds[r] : 0.0f;
                 }
@@ -341,7 +361,7 @@ size_t delta_bytes(const kcap_shape_t &s) { return (s.heads * s.q_rows * 4 + 127
 
 template <class Lut>
 ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t do_row, size_t do_head, const uint16_t *q, const uint16_t *k,
-                        const uint16_t *v, const uint16_t *o, const float *lse, const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *dq,
+                        const uint16_t *v, const uint16_t *o, const uint16_t *rest, const float *lse, const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *dq,
                         uint16_t *dk, uint16_t *dv, void *workspace, const Lut *lut, ktanh_stream_t stream)
 {
     if (shape == nullptr) return KT_ERR_NULL;
@@ -353,7 +373,7 @@ ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t d
     BackwardArgs a{};
     ktanh_status_t st = read_shape(shape, q, k, v, &a.s);
     if (st != KT_OK) return st;
-    if (do_row % 8 != 0 || do_head % 8 != 0 || !aligned16(d_o) || !aligned16(o) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(workspace) ||
+    if (do_row % 8 != 0 || do_head % 8 != 0 || !aligned16(d_o) || !aligned16(o) || !aligned16(rest) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(workspace) ||
         reinterpret_cast<uintptr_t>(lse) % 4 != 0 || reinterpret_cast<uintptr_t>(q_offsets) % 4 != 0 || reinterpret_cast<uintptr_t>(k_offsets) % 4 != 0)
         return KT_ERR_ALIGN;
     if (do_row > (size_t)1 << 40 || do_head > (size_t)1 << 40) return KT_ERR_SHAPE;
@@ -363,6 +383,7 @@ ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t d
     a.q_offsets = q_offsets;
     a.k_offsets = k_offsets;
     a.o = Rows{o, a.s.heads * dim, dim};
+    a.rest = Rows{rest, a.s.heads * dim, dim};
     a.d_o = Rows{d_o, (long long)do_row, (long long)do_head};
     a.lse = lse;
     a.delta = static_cast<float *>(workspace);
@@ -412,17 +433,17 @@ extern "C" size_t kcap_attention_backward_workspace(const kcap_shape_t *shape)
 }
 
 extern "C" ktanh_status_t kcap_attention_backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t do_row, size_t do_head, const uint16_t *q,
-                                                  const uint16_t *k, const uint16_t *v, const uint16_t *o, const float *lse, const int32_t *q_offsets,
+                                                  const uint16_t *k, const uint16_t *v, const uint16_t *o, const uint16_t *rest, const float *lse, const int32_t *q_offsets,
                                                   const int32_t *k_offsets, uint16_t *dq, uint16_t *dk, uint16_t *dv, void *workspace,
                                                   const ktanh_lut_t *lut, ktanh_stream_t stream)
 {
-    return backward(shape, d_o, do_row, do_head, q, k, v, o, lse, q_offsets, k_offsets, dq, dk, dv, workspace, lut, stream);
+    return backward(shape, d_o, do_row, do_head, q, k, v, o, rest, lse, q_offsets, k_offsets, dq, dk, dv, workspace, lut, stream);
 }
 
 extern "C" ktanh_status_t kcap_attention64_backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t do_row, size_t do_head, const uint16_t *q,
-                                                    const uint16_t *k, const uint16_t *v, const uint16_t *o, const float *lse, const int32_t *q_offsets,
+                                                    const uint16_t *k, const uint16_t *v, const uint16_t *o, const uint16_t *rest, const float *lse, const int32_t *q_offsets,
                                                     const int32_t *k_offsets, uint16_t *dq, uint16_t *dk, uint16_t *dv, void *workspace,
                                                     const ktanh_lut64_t *lut, ktanh_stream_t stream)
 {
-    return backward(shape, d_o, do_row, do_head, q, k, v, o, lse, q_offsets, k_offsets, dq, dk, dv, workspace, lut, stream);
+    return backward(shape, d_o, do_row, do_head, q, k, v, o, rest, lse, q_offsets, k_offsets, dq, dk, dv, workspace, lut, stream);
 }

@@ -104,11 +104,19 @@ __global__ __launch_bounds__(kThreads, 2) void cap_decode_kernel(DecodeArgs a, K
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) sum += p[r];
+        // The matrix units wait for memory here: weights go in as two BFloat16 values each, 16 bits of them.
         const bf16x8 weights[2] = {pack8(p), pack8(p + 8)};
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] -= (float)weights[r / 8][r % 8];
+        const bf16x8 rests[2] = {pack8(p), pack8(p + 8)};
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int c = 0; c < kBlocks; ++c) o[c] = mfma(columns_of<D>(v_tile, 16 * i, c), weights[i], o[c]);
+            for (int c = 0; c < kBlocks; ++c) {
+                const bf16x8 columns = columns_of<D>(v_tile, 16 * i, c);
+                o[c] = mfma(columns, weights[i], o[c]);
+                o[c] = mfma(columns, rests[i], o[c]);
+            }
         __builtin_amdgcn_wave_barrier();
     }
 

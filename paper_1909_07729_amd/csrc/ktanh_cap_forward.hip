@@ -96,7 +96,7 @@ __device__ __forceinline__ void store_share(const Share<D> &share, char *k_tile,
 struct ForwardArgs {
     CapShape s;
     const int *q_offsets, *k_offsets;
-    uint16_t *o;
+    uint16_t *o, *rest;
     float *lse;
     CapPages p;
     unsigned tiles;
@@ -160,7 +160,8 @@ __global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a,
     const int key_begin = a.s.window > 0 ? max(0, block_first - a.s.window + 1) & ~(kTile - 1) : 0;
 
     if (threadIdx.x == 0) special = 0;
-    spread_lines(lines, pack, a.s.cap * kLog2e);
+    const float unit = a.s.cap * kLog2e;
+    spread_lines(lines, pack, unit);
     __syncthreads();
 
     bf16x8 q[kSteps];
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a,
     f32x16 o[kBlocks];
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c) o[c] = f32x16{0};
-    float sum = 0.0f;
+    float sum = 0.0f, rounded_sum = 0.0f;  // of the weights, and of the weights as the product has them
 
     Share<D> share;
     int pages[Share<D>::kCount];
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a,
     auto mixed = [&](int j0) {
         return j0 + kTile > n_keys || (a.s.causal && j0 + kTile - 1 > block_first) || (a.s.window > 0 && j0 <= block_last - a.s.window);
     };
-    auto seen = [&](int j) { return j < n_keys && (!a.s.causal || j <= my_place) && (a.s.window == 0 || j > my_place - a.s.window); };
+    auto seen = [&](int j) { return (j < n_keys) & (!a.s.causal | (j <= my_place)) & ((a.s.window == 0) | (j > my_place - a.s.window)); };
     int buffer = 0;
     for (int j0 = key_begin; j0 < key_end; j0 += kTile, buffer ^= 1) {
         char *k_tile = k_tiles[buffer], *v_tile = v_tiles[buffer];
@@ -213,8 +214,13 @@ __global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a,
 #pragma unroll
             for (int k = 0; k < kSteps; ++k) s = mfma(rows_of<D>(k_tile, 32 * sub, k), q[k], s);
             float p[16];
+            if (any_capped(s, a.s.to_x)) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(capped(s[r] * a.s.to_x, lines));
+                for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(capped(s[r] * a.s.to_x, lines));
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(s[r] * a.s.to_x * unit);
+            }
             if (partial) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
@@ -222,9 +228,11 @@ __global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a,
                     p[r] = seen(j) ? p[r] : 0.0f;
                 }
             }
+            if (a.lse != nullptr) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sum += p[r];
-            const bf16x8 weights[2] = {pack8(p), pack8(p + 8)};
+                for (int r = 0; r < 16; ++r) sum += p[r];
+            }
+            const bf16x8 weights[2] = {pack8(p, &rounded_sum), pack8(p + 8, &rounded_sum)};
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -251,17 +259,27 @@ __global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a,
     }
 
     sum += __shfl_xor(sum, 32);
+    rounded_sum += __shfl_xor(rounded_sum, 32);
     if (row >= at.end) return;
     if (a.lse != nullptr && lane < 32)
         a.lse[(long long)head * a.s.q_rows + row] = sum > 0.0f ? __builtin_logf(sum) : sum == 0.0f ? -__builtin_inff() : sum;
-    const float to_mean = sum == 0.0f ? 0.0f : 1.0f / sum;
-    uint16_t *to = a.o + ((long long)row * a.s.heads + head) * D + 4 * (lane >> 5);
+    const float to_mean = rounded_sum == 0.0f ? 0.0f : 1.0f / rounded_sum;
+    const long long to = ((long long)row * a.s.heads + head) * D + 4 * (lane >> 5);
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<u32x2 *>(to + 32 * c + 8 * i) =
-                u32x2{pack2(o[c][4 * i] * to_mean, o[c][4 * i + 1] * to_mean), pack2(o[c][4 * i + 2] * to_mean, o[c][4 * i + 3] * to_mean)};
+        for (int i = 0; i < 4; ++i) {
+            float w[4], rest[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = o[c][4 * i + e] * to_mean;
+            const u32x2 rounded = {pack2(w[0], w[1]), pack2(w[2], w[3])};
+            *reinterpret_cast<u32x2 *>(a.o + to + 32 * c + 8 * i) = rounded;
+            if (a.rest != nullptr) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) rest[e] = w[e] - __uint_as_float(e & 1 ? rounded[e / 2] & 0xFFFF0000u : rounded[e / 2] << 16);
+                *reinterpret_cast<u32x2 *>(a.rest + to + 32 * c + 8 * i) = u32x2{pack2(rest[0], rest[1]), pack2(rest[2], rest[3])};
+            }
+        }
 }
 
 template <bool PAGED>
@@ -276,7 +294,7 @@ ktanh_status_t launch_forward(const ForwardArgs &a, size_t dim, const KtCapPack 
 
 template <class Lut>
 ktanh_status_t attention(const kcap_shape_t *shape, const uint16_t *q, const uint16_t *k, const uint16_t *v, const int32_t *q_offsets,
-                         const int32_t *k_offsets, uint16_t *o, float *lse, const Lut *lut, ktanh_stream_t stream)
+                         const int32_t *k_offsets, uint16_t *o, uint16_t *rest, float *lse, const Lut *lut, ktanh_stream_t stream)
 {
     if (shape == nullptr) return KT_ERR_NULL;
     if (shape->q_rows == 0 || shape->docs == 0) return KT_OK;
@@ -284,13 +302,14 @@ ktanh_status_t attention(const kcap_shape_t *shape, const uint16_t *q, const uin
     ForwardArgs a{};
     ktanh_status_t st = read_shape(shape, q, k, v, &a.s);
     if (st != KT_OK) return st;
-    if (reinterpret_cast<uintptr_t>(o) % 8 != 0 || reinterpret_cast<uintptr_t>(lse) % 4 != 0 ||
+    if (reinterpret_cast<uintptr_t>(o) % 8 != 0 || reinterpret_cast<uintptr_t>(rest) % 8 != 0 || reinterpret_cast<uintptr_t>(lse) % 4 != 0 ||
         reinterpret_cast<uintptr_t>(q_offsets) % 4 != 0 || reinterpret_cast<uintptr_t>(k_offsets) % 4 != 0) return KT_ERR_ALIGN;
     KtCapPack pack;
     if ((st = pack_lines(lut, &pack)) != KT_OK) return st;
     a.q_offsets = q_offsets;
     a.k_offsets = k_offsets;
     a.o = o;
+    a.rest = rest;
     a.lse = lse;
     a.tiles = (unsigned)(shape->q_rows / kRows + shape->docs);
     return launch_forward<false>(a, shape->dim, pack, stream);
@@ -311,15 +330,15 @@ ktanh_status_t ktanh_cap::launch_forward_paged(const CapShape &s, const CapPages
 }
 
 extern "C" ktanh_status_t kcap_attention(const kcap_shape_t *shape, const uint16_t *q, const uint16_t *k, const uint16_t *v,
-                                         const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *o, float *lse,
+                                         const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *o, uint16_t *rest, float *lse,
                                          const ktanh_lut_t *lut, ktanh_stream_t stream)
 {
-    return attention(shape, q, k, v, q_offsets, k_offsets, o, lse, lut, stream);
+    return attention(shape, q, k, v, q_offsets, k_offsets, o, rest, lse, lut, stream);
 }
 
 extern "C" ktanh_status_t kcap_attention64(const kcap_shape_t *shape, const uint16_t *q, const uint16_t *k, const uint16_t *v,
-                                           const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *o, float *lse,
+                                           const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *o, uint16_t *rest, float *lse,
                                            const ktanh_lut64_t *lut, ktanh_stream_t stream)
 {
-    return attention(shape, q, k, v, q_offsets, k_offsets, o, lse, lut, stream);
+    return attention(shape, q, k, v, q_offsets, k_offsets, o, rest, lse, lut, stream);
 }

@@ -284,9 +284,31 @@ def test_gradient_of_a_sum_and_of_shared_inputs(gpu):
     k.requires_grad_()
     o = autograd.kcap_attention(q, k, k, at, cap=50.0)
     dq, dk = torch.autograd.grad(o.sum(), (q, k))
-    o, lse = binding.kcap_attention(q.detach(), k.detach(), k.detach(), at, cap=50.0)
-    want = binding.kcap_attention_backward(torch.ones_like(q), q.detach(), k.detach(), k.detach(), o, lse, at, cap=50.0)
+    rest = torch.empty_like(q)
+    o, lse = binding.kcap_attention(q.detach(), k.detach(), k.detach(), at, cap=50.0, rest=rest)
+    want = binding.kcap_attention_backward(torch.ones_like(q), q.detach(), k.detach(), k.detach(), o, lse, at, cap=50.0, rest=rest)
     assert torch.equal(dq, want[0]) and torch.equal(dk, want[1] + want[2])
+
+
+def test_what_rounding_dropped(gpu):
+    """o and its rest together are the output to sixteen bits; with it the gradients of a peaked head are at least as near."""
+    binding, _, torch = gpu
+    (q, k, v), wide = _inputs(torch, 29, 200, 200, 2, 1, 128, 2.4)
+    do = _bf16(torch, np.random.default_rng(30).standard_normal((200, 2, 128)))
+    at, at_np = _offsets(torch, [200])
+    options = dict(cap=50.0, scale=128 ** -0.5)
+    rest = torch.empty_like(q)
+    o, lse = binding.kcap_attention(q, k, v, at, rest=rest, **options)
+    plain = binding.kcap_attention(q, k, v, at, **options)
+    assert torch.equal(o, plain[0]) and torch.equal(lse, plain[1])
+    assert (rest.float().abs() <= 2 ** -8 * o.float().abs()).all() and rest.any()       # half a step of o, itself rounded
+    want = kcap_oracle.attention(*wide, at_np, at_np, do=do.float().cpu().numpy().astype(np.float64), **options)
+
+    def off(**more):
+        got = binding.kcap_attention_backward(do, q, k, v, o, lse, at, **more, **options)
+        return [np.linalg.norm(t.double().cpu().numpy() - want[n]) / np.linalg.norm(want[n]) for n, t in zip(("dq", "dk", "dv"), got)]
+    with_rest, without = off(rest=rest), off()
+    assert all(a <= b for a, b in zip(with_rest, without)) and max(with_rest) < 4e-3, (with_rest, without)
 
 
 def test_gradients_against_differences(gpu):
@@ -414,7 +436,9 @@ def test_a_long_cache_past_32_bits(gpu):
     all_ = binding.kcap_attention_paged(q, k, v, pages, n, at, cap=50.0)
     flat, _ = binding.kcap_attention(q, new_k, new_v, at, cap=50.0)
     assert torch.equal(all_, flat)
-    assert torch.allclose(one.float(), flat[-1:].float(), rtol=2 ** -7, atol=1e-3)
+    q64, k64, v64 = (t.double().cpu().numpy() for t in (q[-1:], new_k, new_v))
+    want = kcap_oracle.attention(q64, k64, v64, [0, 1], [0, 150], cap=50.0, scale=dim ** -0.5)
+    _near(one, want["o"], want["o_off"], "one token")
 
 
 @pytest.mark.parametrize("interleaved", [False, True])
