@@ -6,7 +6,7 @@
 //   K(x) = A x + B for x > 0,   A = 2^(E - E_i - r),   B = 2^(E - 127) (1 - 2^-r + b/128),
 // which the kernels evaluate with one fused multiply-add: what the shift of Algorithm 1 drops below the
 // last place of a Float32 is kept.  128 lines are held in LDS, indexed by the three low exponent bits and the four
-// high mantissa bits of |x| clamped to [0.125, 16]: the identity below 0.25, saturation from 4 on and the
+// high mantissa bits of |x| clamped to [0.25 - 2^-26, 16]: the identity below 0.25, saturation from 4 on and the
 // table in between need no comparisons, and tables of 32 and of 64 intervals run the same code.
 //
 // |y| <= cap, and caps are at most 64, so e^y stays within e^-64 .. e^64 and the softmax needs no running
@@ -88,38 +88,42 @@ __device__ __forceinline__ void spread_lines(f32x2 *lines, const KtCapPack &pack
     }
 }
 
-// unit * K(x).  A NaN stays one.
+// unit * K(x).  A NaN stays one.  Everything below 0.25 reads one line, so that lanes of small scores share an address: table reads
+// at many are what the LDS unit has least time for.
 __device__ __forceinline__ float capped(float x, const f32x2 *lines)
 {
-    const uint32_t key = __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fabsf(x), 0.125f, 16.0f));
+    const uint32_t key = __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fabsf(x), 0x1.fffffep-3f, 16.0f));
     const f32x2 line = *reinterpret_cast<const f32x2 *>(reinterpret_cast<const char *>(lines) + ((key >> 16) & 0x3F8u));
     return __builtin_copysignf(__builtin_fmaf(line.x, __builtin_fabsf(x), line.y), x);
 }
 
-// Whether some |s * to_x| of the wavefront leaves the identity; a NaN does not.  (K is only worth its eleven instructions
-// where one does: heads whose scores stay below cap / 4 take the exponential of the score itself, with the same roundings.)
-__device__ __forceinline__ bool any_capped(const f32x16 &s, float to_x)
+// Which accumulator rows of a lane, numbered from 0 at `at`, lie in [first, last): others become zero.  In a branch of its
+// own (the statement keeps the compiler from testing every tile).
+struct Span {
+    uint32_t from, count;
+    __device__ __forceinline__ Span(int first, int last, int at) : from((uint32_t)(at + 4 * (int)((threadIdx.x & 63) >> 5) - first)), count((uint32_t)max(last - first, 0))
+    {
+    }
+    __device__ __forceinline__ bool has(int r) const { return from + (uint32_t)((r & 3) + 8 * (r >> 2)) < count; }
+};
+
+__device__ __forceinline__ void keep(float *p, Span span)
 {
-    float m = 0.0f;
+    asm volatile("" : "+v"(span.count));
 #pragma unroll
-    for (int r = 0; r < 16; r += 2) m = __builtin_fmaxf(__builtin_fmaxf(m, __builtin_fabsf(s[r])), __builtin_fabsf(s[r + 1]));
-    return __any(__builtin_fabsf(m * to_x) >= 0.25f);
+    for (int r = 0; r < 16; ++r) p[r] = span.has(r) ? p[r] : 0.0f;
 }
 
 // ------------------------------------------------------------------------------------- tiles in LDS
-// kTile rows of D BFloat16 values, 16-byte chunks swapped within a row so that both ways of reading run without bank
-// conflicts: 8 rows at one chunk (ds_read_b128, rows as they are), and 4 rows x 4 chunks (transposing reads).
-template <int D>
-__device__ __forceinline__ int swap_of(int row)
-{
-    if constexpr (D == 64) return ((row >> 1 & 1) << 2) | (row >> 2 & 3);
-    else return ((row & 3) << 2) | (row >> 2 & 3);
-}
+// Rows of D BFloat16 values, 16 bytes apart, in an order in which the two low bits of a row's number change places with the two
+// above them.  Both ways of reading then run without bank conflicts, eight rows at one 16-byte chunk (ds_read_b128) and 64 bytes of
+// four consecutive rows (transposing reads), and all reads of a lane are one address and constant offsets.
+template <int D> constexpr int kPitch = 2 * D + 16;
 
 template <int D>
 __device__ __forceinline__ int chunk_at(int row, int chunk)  // byte offset
 {
-    return row * (2 * D) + ((chunk ^ swap_of<D>(row)) << 4);
+    return ((row & ~15) | (row & 3) << 2 | (row >> 2 & 3)) * kPitch<D> + 16 * chunk;
 }
 
 // Operand of 32 rows of the tile (from `row0`, a multiple of 32) over values 16 k .. 16 k + 15 of each.
@@ -127,7 +131,7 @@ template <int D>
 __device__ __forceinline__ bf16x8 rows_of(const char *tile, int row0, int k)
 {
     const int lane = threadIdx.x & 63;
-    return *reinterpret_cast<const bf16x8 *>(tile + chunk_at<D>(lane & 31, 2 * k + (lane >> 5)) + row0 * (2 * D));
+    return *reinterpret_cast<const bf16x8 *>(tile + chunk_at<D>(lane & 31, lane >> 5) + row0 * kPitch<D> + 32 * k);
 }
 
 // Operand of columns 32 c .. 32 c + 31 of the tile over its rows row0 .. row0 + 15 in the order of a packed accumulator.
@@ -136,13 +140,54 @@ __device__ __forceinline__ bf16x8 columns_of(const char *tile, int row0, int c)
 {
     typedef __attribute__((address_space(3))) s16x4 *lds4;
     const int lane = threadIdx.x & 63;
-    const int row = (lane >> 5) * 4 + (lane >> 2 & 3), chunk = 4 * c + (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
-    const char *p0 = tile + row0 * (2 * D) + chunk_at<D>(row, chunk) + (lane & 1) * 8;
-    const char *p1 = tile + row0 * (2 * D) + chunk_at<D>(row + 8, chunk) + (lane & 1) * 8;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p0));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p1));
+    const char *at = tile + chunk_at<D>((lane >> 5) * 4 + (lane >> 2 & 3), 0) + (lane >> 4 & 1) * 32 + (lane & 3) * 8 + row0 * kPitch<D> + 64 * c;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 2 * kPitch<D>));  // eight rows on
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
+
+// 32 rows of D BFloat16 values as direct loads bring them (each instruction of a wavefront writes 1 KiB in the order of its lanes):
+// row m lies in stretch m % kStretches, m / kStretches rows into it.  The stretches start such that, again, eight rows at one
+// 16-byte chunk and 64 bytes of four consecutive rows lie in different banks, and all reads of a lane are one address and constants.
+template <int D>
+struct Keys32 {
+    static constexpr int kStretches = D / 16, kDeep = 32 / kStretches, kChunks = D / 8;
+    static constexpr int kBytes = D == 128 ? 8 * 1088 + 32 : 4 * 1104;
+
+    __device__ __forceinline__ static int stretch_at(int g) { return D == 128 ? g * 1088 + (g >> 2) * 16 : g * 1104; }
+    __device__ __forceinline__ static int row_at(int m) { return stretch_at(m % kStretches) + m / kStretches * (2 * D); }
+    // The row and the chunk of it that a lane loads into stretch g.
+    __device__ __forceinline__ static int row_of_lane(int g) { return g + (int)(threadIdx.x & 63) / kChunks * kStretches; }
+    __device__ __forceinline__ static int chunk_of_lane() { return threadIdx.x % kChunks; }
+
+    // Operand of the 32 rows over values 16 k .. 16 k + 15 of each.
+    __device__ __forceinline__ static bf16x8 rows(const char *tile, int k)
+    {
+        const int lane = threadIdx.x & 63;
+        return *reinterpret_cast<const bf16x8 *>(tile + row_at(lane & 31) + 16 * (lane >> 5) + 32 * k);
+    }
+    // Operand of columns 32 c .. 32 c + 31 over rows 16 i .. 16 i + 15 in the order of a packed accumulator.
+    __device__ __forceinline__ static bf16x8 columns(const char *tile, int i, int c)
+    {
+        typedef __attribute__((address_space(3))) s16x4 *lds4;
+        const int lane = threadIdx.x & 63;
+        const char *at = tile + row_at((lane >> 5) * 4 + (lane >> 2 & 3)) + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 16 / kStretches * i * (2 * D) + 64 * c));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + (16 * i + 8) / kStretches * (2 * D) + 64 * c));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+// 16 bytes of each lane from memory to LDS, at `to` + 16 * lane, with no register between.
+__device__ __forceinline__ void load_direct(const void *from, char *to)
+{
+    typedef const __attribute__((address_space(1))) void *global;
+    typedef __attribute__((address_space(3))) void *local;
+    __builtin_amdgcn_global_load_lds((global)from, (local)to, 16, 0, 0);
+}
+
+// This wavefront's loads, direct ones among them, have arrived.
+__device__ __forceinline__ void wait_for_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 
 // ------------------------------------------------------------------------------------------- blocks
 // Blocks that compute, and behind them `heads` blocks that clear.

@@ -93,10 +93,13 @@ __device__ __forceinline__ void store_row(float *row, const f32x16 (&acc)[D / 32
 template <int D>
 __global__ __launch_bounds__(kThreads, 1) void cap_dq_kernel(BackwardArgs a, KtCapPack pack)
 {
-    constexpr int kBytes = kTile * D * 2, kSteps = D / 16, kBlocks = D / 32;
-    __shared__ __align__(16) char k_tiles[2][kBytes];
-    __shared__ __align__(16) char v_tiles[2][kBytes];
-    __shared__ f32x2 lines[128];
+    constexpr int kBytes = kTile * kPitch<D>, kSteps = D / 16, kBlocks = D / 32;
+    struct Shared {
+        f32x2 lines[128];  // first: the offset of a line is its address
+        char k[2][kBytes], v[2][kBytes];
+    };
+    __shared__ __align__(16) Shared shared;
+    f32x2 *lines = shared.lines;
 
     const unsigned total = a.tiles * (unsigned)a.s.heads;
     if (blockIdx.x >= padded(total)) {
@@ -116,7 +119,7 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dq_kernel(BackwardArgs a, KtC
     keys.at += k_begin * keys.row;
     values.at += k_begin * values.row;
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int shift = n_keys - (at.end - at.begin);
     const int row0 = at.first + 32 * wave, row = row0 + (lane & 31), row_there = min(row, at.end - 1);
     const int place0 = row0 - at.begin + shift, my_place = row - at.begin + shift;
@@ -124,6 +127,7 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dq_kernel(BackwardArgs a, KtC
     const int block_last = min(at.first + kRows, at.end) - 1 - at.begin + shift;
     const int key_end = a.s.causal ? min(n_keys, block_last + 1) : n_keys;
     const int key_begin = a.s.window > 0 ? max(0, block_first - a.s.window + 1) & ~(kTile - 1) : 0;
+    const int first_seen = a.s.window > 0 ? max(0, my_place - a.s.window + 1) : 0, last_seen = a.s.causal ? min(n_keys, my_place + 1) : n_keys;
     spread_lines(lines, pack, 1.0f);
 
     bf16x8 q[kSteps], d_o[kSteps];
@@ -157,7 +161,7 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dq_kernel(BackwardArgs a, KtC
     if (key_begin < key_end) share.load(keys, values, key_begin, n_keys);
     int buffer = 0;
     for (int j0 = key_begin; j0 < key_end; j0 += kTile, buffer ^= 1) {
-        char *k_tile = k_tiles[buffer], *v_tile = v_tiles[buffer];
+        char *k_tile = shared.k[buffer], *v_tile = shared.v[buffer];
         share.store(k_tile, v_tile, j0, n_keys);
         __syncthreads();
         if (j0 + kTile < key_end) share.load(keys, values, j0 + kTile, n_keys);
@@ -173,27 +177,13 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dq_kernel(BackwardArgs a, KtC
 #pragma unroll
             for (int k = 0; k < kSteps; ++k) dp = mfma(rows_of<D>(v_tile, 32 * sub, k), d_o[k], dp);
             float ds[16];
-            if (any_capped(s, a.s.to_x)) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = capped(s[r] * a.s.to_x, lines);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] *= a.s.to_x;
-            }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float t = s[r];
+                const float t = capped(s[r] * a.s.to_x, lines);
                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(t, unit, -lse2));
                 ds[r] = p * (dp[r] - delta) * __builtin_fmaf(-t, t, 1.0f);
             }
-            if (partial) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int j = j0 + 32 * sub + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
-                    const bool seen = (j < n_keys) & (!a.s.causal | (j <= my_place)) & ((a.s.window == 0) | (j > my_place - a.s.window));
-                    ds[r] = seen ? ds[r] : 0.0f;
-                }
-            }
+            if (partial) keep(ds, Span(first_seen, last_seen, j0 + 32 * sub));
             const bf16x8 shares[2] = {pack8(ds), pack8(ds + 8)};
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -207,11 +197,14 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dq_kernel(BackwardArgs a, KtC
 template <int D>
 __global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, KtCapPack pack)
 {
-    constexpr int kBytes = kTile * D * 2, kSteps = D / 16, kBlocks = D / 32;
-    __shared__ __align__(16) char q_tiles[2][kBytes];
-    __shared__ __align__(16) char do_tiles[2][kBytes];
-    __shared__ __align__(16) float sums[2][2][kTile];  // lse * log2 e | delta of a tile's rows
-    __shared__ f32x2 lines[128];
+    constexpr int kBytes = kTile * kPitch<D>, kSteps = D / 16, kBlocks = D / 32;
+    struct Shared {
+        f32x2 lines[128];  // first: the offset of a line is its address
+        char q[2][kBytes], d_o[2][kBytes];
+        float sums[2][2][kTile];  // lse * log2 e | delta of a tile's rows
+    };
+    __shared__ __align__(16) Shared shared;
+    f32x2 *lines = shared.lines;
 
     const unsigned total = a.tiles * (unsigned)(a.s.kv_heads * a.parts);
     if (blockIdx.x >= padded(total)) {  // where there are parts, the kernel that joins them clears
@@ -228,14 +221,17 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, K
     const int q_begin = offset_at(a.q_offsets, at.doc, a.s.q_rows);
     const int n_queries = max(offset_at(a.q_offsets, at.doc + 1, a.s.q_rows) - q_begin, 0);
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int shift = (at.end - at.begin) - n_queries;  // query i is key i + shift
     const int row0 = at.first + 32 * wave, row = row0 + (lane & 31), row_there = min(row, at.end - 1);
-    const int key0 = row0 - at.begin, key = row - at.begin;
+    const int key0 = row0 - at.begin, key = row_there - at.begin;
     const int block_first = at.first - at.begin, block_last = min(at.first + kRows, at.end) - 1 - at.begin;
     // queries that see some key of the block
     const int from = a.s.causal ? max(0, block_first - shift) & ~(kTile - 1) : 0;
     const int to = a.s.window > 0 ? min((long long)n_queries, max(0ll, (long long)block_last - shift + a.s.window)) : n_queries;
+    // queries that see this lane's key
+    const int first_seen = a.s.causal ? max(0, key - shift) : 0;
+    const int last_seen = a.s.window > 0 ? (int)min((long long)n_queries, max(0ll, (long long)key - shift + a.s.window)) : n_queries;
     spread_lines(lines, pack, 1.0f);
     const float unit = a.s.cap * kLog2e;
 
@@ -263,9 +259,9 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, K
     int buffer = 0;
     for (int n = 0; n < heads * rounds; ++n, buffer ^= 1) {
         const int i0 = from + n % rounds * kTile;
-        char *q_tile = q_tiles[buffer], *do_tile = do_tiles[buffer];
+        char *q_tile = shared.q[buffer], *do_tile = shared.d_o[buffer];
         share.store(q_tile, do_tile, i0, n_queries);
-        if (wave < 2) sums[buffer][wave][lane] = wave == 0 ? share_sum * kLog2e : share_sum;
+        if (wave < 2) shared.sums[buffer][wave][lane] = wave == 0 ? share_sum * kLog2e : share_sum;
         __syncthreads();
         if (n + 1 < heads * rounds) load(n + 1);
         const int first = i0 + shift;  // the tile's first query's place
@@ -280,34 +276,23 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, K
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) dp = mfma(rows_of<D>(do_tile, 32 * sub, i), v[i], dp);
             float p[16], ds[16];
-            if (any_capped(s, a.s.to_x)) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = capped(s[r] * a.s.to_x, lines);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] *= a.s.to_x;
-            }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int at_row = 32 * sub + 8 * g + 4 * (lane >> 5);
-                const f32x4 lse2 = *reinterpret_cast<const f32x4 *>(&sums[buffer][0][at_row]);
-                const f32x4 delta = *reinterpret_cast<const f32x4 *>(&sums[buffer][1][at_row]);
+                const f32x4 lse2 = *reinterpret_cast<const f32x4 *>(&shared.sums[buffer][0][at_row]);
+                const f32x4 delta = *reinterpret_cast<const f32x4 *>(&shared.sums[buffer][1][at_row]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int r = 4 * g + e;
-                    const float t = s[r];
+                    const float t = capped(s[r] * a.s.to_x, lines);
                     p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(t, unit, -lse2[e]));
                     ds[r] = p[r] * (dp[r] - delta[e]) * __builtin_fmaf(-t, t, 1.0f);
                 }
             }
             if (partial) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int i = i0 + 32 * sub + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
-                    const bool seen = (i < n_queries) & (!a.s.causal | (key <= i + shift)) & ((a.s.window == 0) | (key > i + shift - a.s.window));
-                    p[r] = seen ? p[r] : 0.0f;
-                    ds[r] = seen ? ds[r] : 0.0f;
-                }
+                const Span seen(first_seen, last_seen, i0 + 32 * sub);
+                keep(p, seen);
+                keep(ds, seen);
             }
             const bf16x8 weights[2] = {pack8(p), pack8(p + 8)}, shares[2] = {pack8(ds), pack8(ds + 8)};
 #pragma unroll

@@ -25,11 +25,15 @@ __device__ __forceinline__ int first_key(const CapShape &s, int n_keys) { return
 template <int D>
 __global__ __launch_bounds__(kThreads, 2) void cap_decode_kernel(DecodeArgs a, KtCapPack pack)
 {
-    constexpr int kBytes = kKeys * D * 2, kSteps = D / 16, kBlocks = D / 32;
+    constexpr int kBytes = kKeys * kPitch<D>, kSteps = D / 16, kBlocks = D / 32;
     constexpr int kChunks = D / 8, kLoads = kKeys * kChunks / 64;  // 16-byte loads of a lane for each of K and V
-    __shared__ __align__(16) char tiles[kWaves][2 * kBytes];       // keys | values; at the end 32 x D numerators
-    __shared__ f32x2 lines[128];
-    __shared__ float wave_sums[kWaves][32];
+    struct Shared {
+        f32x2 lines[128];                 // first: the offset of a line is its address
+        char tiles[kWaves][2 * kBytes];   // keys | values; at the end 32 x D numerators
+        float sums[kWaves][32];
+    };
+    __shared__ __align__(16) Shared shared;
+    f32x2 *lines = shared.lines;
 
     // heads and sequences first: the empty spans behind short sequences come last
     const int row_block = (int)(blockIdx.x % a.row_blocks), kv_head = (int)(blockIdx.x / a.row_blocks % a.s.kv_heads);
@@ -37,11 +41,11 @@ __global__ __launch_bounds__(kThreads, 2) void cap_decode_kernel(DecodeArgs a, K
     const int n_keys = keys_in_pages(a.p, seq), begin = max(first_key(a.s, n_keys), span * a.span), end = min(n_keys, (span + 1) * a.span);
     if (begin >= end && a.parts != nullptr) return;
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head0 = kv_head * a.s.group + 32 * row_block, heads = min(32, a.s.group - 32 * row_block);
     const int *pages = a.p.pages + seq * a.p.row;
     const uint16_t *k = a.s.k.at + kv_head * a.s.k.head, *v = a.s.v.at + kv_head * a.s.v.head;
-    char *k_tile = tiles[wave], *v_tile = tiles[wave] + kBytes;
+    char *k_tile = shared.tiles[wave], *v_tile = shared.tiles[wave] + kBytes;
     spread_lines(lines, pack, a.s.cap * kLog2e);
 
     bf16x8 q[kSteps];
@@ -123,9 +127,9 @@ __global__ __launch_bounds__(kThreads, 2) void cap_decode_kernel(DecodeArgs a, K
     // numerators [32][D] of each wavefront where its tile was, and their sums over the wavefronts
     __syncthreads();
     sum += __shfl_xor(sum, 32);
-    if (lane < 32) wave_sums[wave][lane] = sum;
+    if (lane < 32) shared.sums[wave][lane] = sum;
     if ((lane & 31) < heads) {
-        float *mine = reinterpret_cast<float *>(tiles[wave]) + (lane & 31) * D + 4 * (lane >> 5);
+        float *mine = reinterpret_cast<float *>(shared.tiles[wave]) + (lane & 31) * D + 4 * (lane >> 5);
 #pragma unroll
         for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
@@ -139,8 +143,8 @@ __global__ __launch_bounds__(kThreads, 2) void cap_decode_kernel(DecodeArgs a, K
         float total = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            n += *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(tiles[w]) + h * D + d);
-            total += wave_sums[w][h];
+            n += *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(shared.tiles[w]) + h * D + d);
+            total += shared.sums[w][h];
         }
         if (a.parts == nullptr) {
             const float to_mean = total == 0.0f ? 0.0f : 1.0f / total;

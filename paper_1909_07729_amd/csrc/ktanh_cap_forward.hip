@@ -2,8 +2,15 @@
 // prompts over a paged cache.
 //
 // A block holds 128 queries of one head and one document, 32 in each wavefront's registers, and goes once over the
-// keys that they see in tiles of 64, double-buffered in LDS (the next tile travels through registers while this one is used).
+// keys that they see in tiles of 32, double-buffered in LDS by direct loads.
 //   S^T = K Q^T (keys x queries), p = e^(cap K(x)) in the accumulator, O^T += V^T P^T with P^T as it lies.
+//
+// What bounds it: a wavefront's 16 matrix and about 150 vector instructions of a tile take some 340 ns side by side with two
+// others' (269 the matrix instructions alone), and three wavefronts share a SIMD because the tile's 32 keys and the direct loads leave
+// 160 registers enough.  16384 tokens, 32 heads of 128, causal: 2331 us, 943 TFLOP/s; with 64 keys to a tile, through registers, and
+// two wavefronts 2736; with 32 keys through registers 2620.
+#include <type_traits>
+
 #include "ktanh_cap_args.h"
 
 using namespace ktanh_cap;
@@ -41,29 +48,36 @@ struct Keys {
     }
 };
 
-// One thread's share of a tile: chunk threadIdx % (D / 8) of the rows threadIdx / (D / 8) + n * kStep.
+constexpr int kKeys = 32;  // of a tile
+
+// The wavefront's stretches of a tile.
 template <int D>
-struct Share {
-    static constexpr int kChunks = D / 8, kStep = kThreads / kChunks, kCount = kTile / kStep;
-    u32x4 k[kCount], v[kCount];
-};
+constexpr int kShare = Keys32<D>::kStretches / kWaves;
 
 template <int D, bool PAGED>
-__device__ __forceinline__ void pages_of(const Keys<PAGED> &keys, int j0, int (&pages)[Share<D>::kCount])
+__device__ __forceinline__ void pages_of(const Keys<PAGED> &keys, int j0, int wave, int (&pages)[kShare<D>])
 {
 #pragma unroll
-    for (int n = 0; n < Share<D>::kCount; ++n) pages[n] = keys.page(j0 + (int)threadIdx.x / Share<D>::kChunks + n * Share<D>::kStep);
+    for (int n = 0; n < kShare<D>; ++n) pages[n] = keys.page(j0 + Keys32<D>::row_of_lane(wave * kShare<D> + n));
 }
 
+// Rows j0 .. j0 + 31 on their way to LDS; a row that is not there is read as the last one.
 template <int D, bool PAGED>
-__device__ __forceinline__ void load_share(Share<D> &share, const Keys<PAGED> &keys, int j0, const int (&pages)[Share<D>::kCount])
+__device__ __forceinline__ void load_tile(const Keys<PAGED> &keys, int j0, int wave, const int (&pages)[kShare<D>], char *k_tile, char *v_tile)
 {
-    const int chunk = threadIdx.x % Share<D>::kChunks;
+    const int chunk = Keys32<D>::chunk_of_lane();
 #pragma unroll
-    for (int n = 0; n < Share<D>::kCount; ++n) {
-        const int j = j0 + (int)threadIdx.x / Share<D>::kChunks + n * Share<D>::kStep;
-        share.k[n] = *reinterpret_cast<const u32x4 *>(keys.k_at(j, pages[n]) + 8 * chunk);
-        share.v[n] = *reinterpret_cast<const u32x4 *>(keys.v_at(j, pages[n]) + 8 * chunk);
+    for (int n = 0; n < kShare<D>; ++n) {
+        const int g = wave * kShare<D> + n, row = Keys32<D>::row_of_lane(g);
+        if constexpr (PAGED) {
+            load_direct(keys.k_at(j0 + row, pages[n]) + 8 * chunk, k_tile + Keys32<D>::stretch_at(g));
+            load_direct(keys.v_at(j0 + row, pages[n]) + 8 * chunk, v_tile + Keys32<D>::stretch_at(g));
+        } else {
+            // one address for all lanes and 32 bits of offset for each (strides are below 2^24)
+            const uint32_t there = min(row, keys.last - j0);
+            load_direct(reinterpret_cast<const char *>(keys.k + j0 * keys.k_row) + (there * 2 * (uint32_t)keys.k_row + 16 * chunk), k_tile + Keys32<D>::stretch_at(g));
+            load_direct(reinterpret_cast<const char *>(keys.v + j0 * keys.v_row) + (there * 2 * (uint32_t)keys.v_row + 16 * chunk), v_tile + Keys32<D>::stretch_at(g));
+        }
     }
 }
 
@@ -80,17 +94,22 @@ __device__ __forceinline__ bool take_special(u32x4 *v)
     return found;
 }
 
-// Values of rows from `end` on are zero: their weights are, and zero times an infinity would not be.
+// Of the rows that this wavefront loaded: values behind the last key become zero, as infinities and NaN do.  Their weights are zero,
+// and the product would not be.
 template <int D>
-__device__ __forceinline__ void store_share(const Share<D> &share, char *k_tile, char *v_tile, int j0, int end)
+__device__ __forceinline__ bool clean_values(char *v_tile, int wave, int there)
 {
-    const int chunk = threadIdx.x % Share<D>::kChunks;
+    bool found = false;
 #pragma unroll
-    for (int n = 0; n < Share<D>::kCount; ++n) {
-        const int row = threadIdx.x / Share<D>::kChunks + n * Share<D>::kStep;
-        *reinterpret_cast<u32x4 *>(k_tile + chunk_at<D>(row, chunk)) = share.k[n];
-        *reinterpret_cast<u32x4 *>(v_tile + chunk_at<D>(row, chunk)) = j0 + row < end ? share.v[n] : u32x4{0, 0, 0, 0};
+    for (int n = 0; n < kShare<D>; ++n) {
+        const int g = wave * kShare<D> + n;
+        u32x4 *at = reinterpret_cast<u32x4 *>(v_tile + Keys32<D>::stretch_at(g) + 16 * (threadIdx.x & 63));
+        u32x4 w = *at;
+        if (Keys32<D>::row_of_lane(g) >= there) w = u32x4{0, 0, 0, 0};
+        else found |= take_special(&w);
+        *at = w;
     }
+    return found;
 }
 
 struct ForwardArgs {
@@ -102,20 +121,24 @@ struct ForwardArgs {
     unsigned tiles;
 };
 
-template <int D, bool PAGED>
-__global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a, KtCapPack pack)
+// SUMS: with log-sums.
+template <int D, bool PAGED, bool SUMS>
+__global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a, KtCapPack pack)
 {
-    constexpr int kBytes = kTile * D * 2, kSteps = D / 16, kBlocks = D / 32;
-    __shared__ __align__(16) char k_tiles[2][kBytes];
-    __shared__ __align__(16) char v_tiles[2][kBytes];
-    __shared__ f32x2 lines[128];
-    __shared__ int special;  // whether a value was taken out of a tile
+    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32;
+    struct Shared {
+        f32x2 lines[128];  // first: the offset of a line is its address
+        char k[2][kBytes], v[2][kBytes];
+        int special;       // whether a value was taken out of a tile
+    };
+    __shared__ __align__(16) Shared shared;
+    f32x2 *lines = shared.lines;
 
     const unsigned total = a.tiles * (unsigned)a.s.heads;
     if (blockIdx.x >= padded(total)) {
         const int head = (int)(blockIdx.x - padded(total));
         clear_rows<D>(a.o, a.q_offsets, a.s.docs, a.s.q_rows, a.s.heads, head, [&](int row) {
-            if (a.lse != nullptr) a.lse[(long long)head * a.s.q_rows + row] = -__builtin_inff();
+            if (SUMS) a.lse[(long long)head * a.s.q_rows + row] = -__builtin_inff();
         });
         return;
     }
@@ -149,7 +172,7 @@ __global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a,
     keys.v_row = a.s.v.row;
     keys.last = n_keys - 1;
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int shift = n_keys - (at.end - at.begin);            // query i is key i + shift
     const int row0 = at.first + 32 * wave;                     // this wavefront's first query
     const int row = row0 + (lane & 31);                        // this lane's
@@ -157,9 +180,9 @@ __global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a,
     const int block_first = at.first - at.begin + shift;
     const int block_last = min(at.first + kRows, at.end) - 1 - at.begin + shift;
     const int key_end = a.s.causal ? min(n_keys, block_last + 1) : n_keys;
-    const int key_begin = a.s.window > 0 ? max(0, block_first - a.s.window + 1) & ~(kTile - 1) : 0;
+    const int key_begin = a.s.window > 0 ? max(0, block_first - a.s.window + 1) & ~(kKeys - 1) : 0;
 
-    if (threadIdx.x == 0) special = 0;
+    if (threadIdx.x == 0) shared.special = 0;
     const float unit = a.s.cap * kLog2e;
     spread_lines(lines, pack, unit);
     __syncthreads();
@@ -175,77 +198,59 @@ __global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a,
     for (int c = 0; c < kBlocks; ++c) o[c] = f32x16{0};
     float sum = 0.0f, rounded_sum = 0.0f;  // of the weights, and of the weights as the product has them
 
-    Share<D> share;
-    int pages[Share<D>::kCount];
+    int pages[kShare<D>];
     if (key_begin < key_end) {
-        pages_of<D>(keys, key_begin, pages);
-        load_share<D>(share, keys, key_begin, pages);
-        if constexpr (PAGED) pages_of<D>(keys, key_begin + kTile, pages);
+        pages_of<D>(keys, key_begin, wave, pages);
+        load_tile<D>(keys, key_begin, wave, pages, shared.k[0], shared.v[0]);
+        if constexpr (PAGED) pages_of<D>(keys, key_begin + kKeys, wave, pages);
     }
     // Whether some query of the block does not see all of the tile.  There a weight may be zero because its key is hidden, and
     // the product with an infinite or NaN value would not be: such values are taken out, and added behind the loop where they are seen.
     auto mixed = [&](int j0) {
-        return j0 + kTile > n_keys || (a.s.causal && j0 + kTile - 1 > block_first) || (a.s.window > 0 && j0 <= block_last - a.s.window);
+        return j0 + kKeys > n_keys || (a.s.causal && j0 + kKeys - 1 > block_first) || (a.s.window > 0 && j0 <= block_last - a.s.window);
     };
-    auto seen = [&](int j) { return (j < n_keys) & (!a.s.causal | (j <= my_place)) & ((a.s.window == 0) | (j > my_place - a.s.window)); };
-    int buffer = 0;
-    for (int j0 = key_begin; j0 < key_end; j0 += kTile, buffer ^= 1) {
-        char *k_tile = k_tiles[buffer], *v_tile = v_tiles[buffer];
-        if (mixed(j0)) {
-            bool found = false;
-#pragma unroll
-            for (int n = 0; n < Share<D>::kCount; ++n) found |= take_special(&share.v[n]);
-            if (found) special = 1;
-        }
-        store_share<D>(share, k_tile, v_tile, j0, n_keys);
-        // Another wavefront may still read the other buffer, which is next written behind this barrier's successor.
+    const int first_seen = a.s.window > 0 ? max(0, my_place - a.s.window + 1) : 0, last_seen = a.s.causal ? min(n_keys, my_place + 1) : n_keys;
+    auto step = [&](int j0, char *__restrict__ k_tile, char *__restrict__ v_tile, char *__restrict__ next_k, char *__restrict__ next_v) {
+        wait_for_loads();
+        if (mixed(j0) && clean_values<D>(v_tile, wave, n_keys - j0)) shared.special = 1;
+        // Behind this barrier the tile is complete and all are done with the one before, whose place the next one takes.
         __syncthreads();
-        if (j0 + kTile < key_end) {
-            load_share<D>(share, keys, j0 + kTile, pages);
-            if constexpr (PAGED) pages_of<D>(keys, j0 + 2 * kTile, pages);
+        if (j0 + kKeys < key_end) {
+            load_tile<D>(keys, j0 + kKeys, wave, pages, next_k, next_v);
+            if constexpr (PAGED) pages_of<D>(keys, j0 + 2 * kKeys, wave, pages);
         }
-        const bool none = (a.s.causal && j0 > place0 + 31) || (a.s.window > 0 && j0 + kTile - 1 <= place0 - a.s.window) || row0 >= at.end;
-        if (none) continue;
-        const bool partial = j0 + kTile > n_keys || (a.s.causal && j0 + kTile - 1 > place0) ||
+        const bool none = (a.s.causal && j0 > place0 + 31) || (a.s.window > 0 && j0 + kKeys - 1 <= place0 - a.s.window) || row0 >= at.end;
+        if (none) return;
+        const bool partial = j0 + kKeys > n_keys || (a.s.causal && j0 + kKeys - 1 > place0) ||
                              (a.s.window > 0 && j0 <= place0 + 31 - a.s.window);
+        f32x16 s = f32x16{0};
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            f32x16 s = f32x16{0};
+        for (int k = 0; k < kSteps; ++k) s = mfma(Keys32<D>::rows(k_tile, k), q[k], s);
+        float p[16];
 #pragma unroll
-            for (int k = 0; k < kSteps; ++k) s = mfma(rows_of<D>(k_tile, 32 * sub, k), q[k], s);
-            float p[16];
-            if (any_capped(s, a.s.to_x)) {
+        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(capped(s[r] * a.s.to_x, lines));
+        if (partial) keep(p, Span(first_seen, last_seen, j0));
+        if constexpr (SUMS) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(capped(s[r] * a.s.to_x, lines));
-            } else {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(s[r] * a.s.to_x * unit);
-            }
-            if (partial) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int j = j0 + 32 * sub + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
-                    p[r] = seen(j) ? p[r] : 0.0f;
-                }
-            }
-            if (a.lse != nullptr) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) sum += p[r];
-            }
-            const bf16x8 weights[2] = {pack8(p, &rounded_sum), pack8(p + 8, &rounded_sum)};
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int c = 0; c < kBlocks; ++c) o[c] = mfma(columns_of<D>(v_tile, 32 * sub + 16 * i, c), weights[i], o[c]);
+            for (int r = 0; r < 16; ++r) sum += p[r];
         }
+        const bf16x8 weights[2] = {pack8(p, &rounded_sum), pack8(p + 8, &rounded_sum)};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int c = 0; c < kBlocks; ++c) o[c] = mfma(Keys32<D>::columns(v_tile, i, c), weights[i], o[c]);
+    };
+    for (int j0 = key_begin; j0 < key_end; j0 += 2 * kKeys) {
+        step(j0, shared.k[0], shared.v[0], shared.k[1], shared.v[1]);
+        if (j0 + kKeys < key_end) step(j0 + kKeys, shared.k[1], shared.v[1], shared.k[0], shared.v[0]);
     }
 
     __syncthreads();
-    if (special) {
-        for (int j0 = key_begin; j0 < key_end; j0 += kTile) {
+    if (shared.special) {
+        for (int j0 = key_begin; j0 < key_end; j0 += kKeys) {
             if (!mixed(j0)) continue;
-            for (int j = j0; j < min(j0 + kTile, n_keys); ++j) {
-                if (row >= at.end || !seen(j)) continue;
+            for (int j = j0; j < min(j0 + kKeys, n_keys); ++j) {
+                if (row >= at.end || j < first_seen || j >= last_seen) continue;
                 const uint16_t *value = keys.v_at(j, keys.page(j)) + 4 * (lane >> 5);
 #pragma unroll
                 for (int c = 0; c < kBlocks; ++c)
@@ -261,7 +266,7 @@ __global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a,
     sum += __shfl_xor(sum, 32);
     rounded_sum += __shfl_xor(rounded_sum, 32);
     if (row >= at.end) return;
-    if (a.lse != nullptr && lane < 32)
+    if (SUMS && lane < 32)
         a.lse[(long long)head * a.s.q_rows + row] = sum > 0.0f ? __builtin_logf(sum) : sum == 0.0f ? -__builtin_inff() : sum;
     const float to_mean = rounded_sum == 0.0f ? 0.0f : 1.0f / rounded_sum;
     const long long to = ((long long)row * a.s.heads + head) * D + 4 * (lane >> 5);
@@ -282,12 +287,12 @@ __global__ __launch_bounds__(kThreads, 2) void cap_forward_kernel(ForwardArgs a,
         }
 }
 
-template <bool PAGED>
+template <bool PAGED, bool SUMS>
 ktanh_status_t launch_forward(const ForwardArgs &a, size_t dim, const KtCapPack &pack, ktanh_stream_t stream)
 {
     const unsigned long long blocks = ((unsigned long long)a.tiles * a.s.heads + 7) / 8 * 8 + a.s.heads;
     if (blocks > kMaxBlocks) return KT_ERR_SHAPE;
-    auto *kernel = dim == 64 ? &cap_forward_kernel<64, PAGED> : &cap_forward_kernel<128, PAGED>;
+    auto *kernel = dim == 64 ? &cap_forward_kernel<64, PAGED, SUMS> : &cap_forward_kernel<128, PAGED, SUMS>;
     kernel<<<dim3((unsigned)blocks), dim3(kThreads), 0, static_cast<hipStream_t>(stream)>>>(a, pack);
     return launched();
 }
@@ -312,7 +317,7 @@ ktanh_status_t attention(const kcap_shape_t *shape, const uint16_t *q, const uin
     a.rest = rest;
     a.lse = lse;
     a.tiles = (unsigned)(shape->q_rows / kRows + shape->docs);
-    return launch_forward<false>(a, shape->dim, pack, stream);
+    return lse != nullptr ? launch_forward<false, true>(a, shape->dim, pack, stream) : launch_forward<false, false>(a, shape->dim, pack, stream);
 }
 
 }  // namespace
@@ -326,7 +331,7 @@ ktanh_status_t ktanh_cap::launch_forward_paged(const CapShape &s, const CapPages
     a.q_offsets = q_offsets;
     a.o = o;
     a.tiles = (unsigned)(s.q_rows / kRows + s.docs);
-    return launch_forward<true>(a, (size_t)dim, pack, stream);
+    return launch_forward<true, false>(a, (size_t)dim, pack, stream);
 }
 
 extern "C" ktanh_status_t kcap_attention(const kcap_shape_t *shape, const uint16_t *q, const uint16_t *k, const uint16_t *v,
