@@ -61,25 +61,61 @@ __device__ __forceinline__ void pages_of(const Keys<PAGED> &keys, int j0, int wa
     for (int n = 0; n < kShare<D>; ++n) pages[n] = keys.page(j0 + Keys32<D>::row_of_lane(wave * kShare<D> + n));
 }
 
-// Rows j0 .. j0 + 31 on their way to LDS; a row that is not there is read as the last one.
+// Tiles on their way to LDS, one behind the other; a row that is not there is read as the last one.
 template <int D, bool PAGED>
-__device__ __forceinline__ void load_tile(const Keys<PAGED> &keys, int j0, int wave, const int (&pages)[kShare<D>], char *k_tile, char *v_tile)
-{
-    const int chunk = Keys32<D>::chunk_of_lane();
-#pragma unroll
-    for (int n = 0; n < kShare<D>; ++n) {
-        const int g = wave * kShare<D> + n, row = Keys32<D>::row_of_lane(g);
+struct Stream {
+    const Keys<PAGED> &keys;
+    const int wave;
+    // the tile's first row (one address for all lanes), and a lane's offsets from it (32 bits: strides are below 2^24)
+    const char *k, *v;
+    uint32_t k_off, v_off;
+    int pages[kShare<D>];
+
+    __device__ __forceinline__ Stream(const Keys<PAGED> &keys, int wave, int j0) : keys(keys), wave(wave)
+    {
         if constexpr (PAGED) {
-            load_direct(keys.k_at(j0 + row, pages[n]) + 8 * chunk, k_tile + Keys32<D>::stretch_at(g));
-            load_direct(keys.v_at(j0 + row, pages[n]) + 8 * chunk, v_tile + Keys32<D>::stretch_at(g));
+            pages_of<D>(keys, j0, wave, pages);
         } else {
-            // one address for all lanes and 32 bits of offset for each (strides are below 2^24)
-            const uint32_t there = min(row, keys.last - j0);
-            load_direct(reinterpret_cast<const char *>(keys.k + j0 * keys.k_row) + (there * 2 * (uint32_t)keys.k_row + 16 * chunk), k_tile + Keys32<D>::stretch_at(g));
-            load_direct(reinterpret_cast<const char *>(keys.v + j0 * keys.v_row) + (there * 2 * (uint32_t)keys.v_row + 16 * chunk), v_tile + Keys32<D>::stretch_at(g));
+            const int g = wave * kShare<D>;
+            k = reinterpret_cast<const char *>(keys.k + (j0 + g) * keys.k_row);
+            v = reinterpret_cast<const char *>(keys.v + (j0 + g) * keys.v_row);
+            const uint32_t row = Keys32<D>::row_of_lane(0), chunk = 16 * Keys32<D>::chunk_of_lane();
+            k_off = row * 2 * (uint32_t)keys.k_row + chunk;
+            v_off = row * 2 * (uint32_t)keys.v_row + chunk;
         }
     }
-}
+    // Loads rows j0 .. j0 + 31, which are next.
+    __device__ __forceinline__ void next(int j0, char *k_tile, char *v_tile)
+    {
+        const int chunk = Keys32<D>::chunk_of_lane();
+#pragma unroll
+        for (int n = 0; n < kShare<D>; ++n) {
+            const int g = wave * kShare<D> + n, row = Keys32<D>::row_of_lane(g);
+            if constexpr (PAGED) {
+                load_direct(keys.k_at(j0 + row, pages[n]) + 8 * chunk, k_tile + Keys32<D>::stretch_at(g));
+                load_direct(keys.v_at(j0 + row, pages[n]) + 8 * chunk, v_tile + Keys32<D>::stretch_at(g));
+            } else {
+                uint32_t k_at = k_off, v_at = v_off;
+                const char *k_row = k + n * 2 * keys.k_row, *v_row = v + n * 2 * keys.v_row;
+                if (j0 + kKeys > keys.last + 1) {
+                    const uint32_t there = min(row, keys.last - j0);
+                    k_row = reinterpret_cast<const char *>(keys.k + j0 * keys.k_row);
+                    v_row = reinterpret_cast<const char *>(keys.v + j0 * keys.v_row);
+                    k_at = there * 2 * (uint32_t)keys.k_row + 16 * chunk;
+                    v_at = there * 2 * (uint32_t)keys.v_row + 16 * chunk;
+                }
+                load_direct(k_row + k_at, k_tile + Keys32<D>::stretch_at(g));
+                load_direct(v_row + v_at, v_tile + Keys32<D>::stretch_at(g));
+            }
+        }
+        if constexpr (PAGED) {
+            pages_of<D>(keys, j0 + kKeys, wave, pages);
+        } else {
+            k += kKeys * 2 * keys.k_row;
+            v += kKeys * 2 * keys.v_row;
+        }
+    }
+};
 
 // Infinities and NaN become zero.  Returns whether there was one.
 __device__ __forceinline__ bool take_special(u32x4 *v)
@@ -198,38 +234,20 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     for (int c = 0; c < kBlocks; ++c) o[c] = f32x16{0};
     float sum = 0.0f, rounded_sum = 0.0f;  // of the weights, and of the weights as the product has them
 
-    int pages[kShare<D>];
-    if (key_begin < key_end) {
-        pages_of<D>(keys, key_begin, wave, pages);
-        load_tile<D>(keys, key_begin, wave, pages, shared.k[0], shared.v[0]);
-        if constexpr (PAGED) pages_of<D>(keys, key_begin + kKeys, wave, pages);
-    }
-    // Whether some query of the block does not see all of the tile.  There a weight may be zero because its key is hidden, and
-    // the product with an infinite or NaN value would not be: such values are taken out, and added behind the loop where they are seen.
-    auto mixed = [&](int j0) {
-        return j0 + kKeys > n_keys || (a.s.causal && j0 + kKeys - 1 > block_first) || (a.s.window > 0 && j0 <= block_last - a.s.window);
-    };
+    // Tiles that every query of the block sees whole.  In the others a weight may be zero because its key is hidden, and the product
+    // with an infinite or NaN value would not be: such values are taken out, and added behind the loop where they are seen.
+    const int whole_from = a.s.window > 0 ? block_last - a.s.window + 1 : 0, whole_to = a.s.causal ? min(n_keys, block_first + 1) : n_keys;
+    auto whole = [&](int j0) { return j0 >= whole_from && j0 + kKeys <= whole_to; };
     const int first_seen = a.s.window > 0 ? max(0, my_place - a.s.window + 1) : 0, last_seen = a.s.causal ? min(n_keys, my_place + 1) : n_keys;
-    auto step = [&](int j0, char *__restrict__ k_tile, char *__restrict__ v_tile, char *__restrict__ next_k, char *__restrict__ next_v) {
-        wait_for_loads();
-        if (mixed(j0) && clean_values<D>(v_tile, wave, n_keys - j0)) shared.special = 1;
-        // Behind this barrier the tile is complete and all are done with the one before, whose place the next one takes.
-        __syncthreads();
-        if (j0 + kKeys < key_end) {
-            load_tile<D>(keys, j0 + kKeys, wave, pages, next_k, next_v);
-            if constexpr (PAGED) pages_of<D>(keys, j0 + 2 * kKeys, wave, pages);
-        }
-        const bool none = (a.s.causal && j0 > place0 + 31) || (a.s.window > 0 && j0 + kKeys - 1 <= place0 - a.s.window) || row0 >= at.end;
-        if (none) return;
-        const bool partial = j0 + kKeys > n_keys || (a.s.causal && j0 + kKeys - 1 > place0) ||
-                             (a.s.window > 0 && j0 <= place0 + 31 - a.s.window);
+    const bool idle = row0 >= at.end;
+    auto add_tile = [&](int j0, const char *__restrict__ k_tile, const char *__restrict__ v_tile, bool masked) {
         f32x16 s = f32x16{0};
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) s = mfma(Keys32<D>::rows(k_tile, k), q[k], s);
         float p[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(capped(s[r] * a.s.to_x, lines));
-        if (partial) keep(p, Span(first_seen, last_seen, j0));
+        if (masked) keep(p, Span(first_seen, last_seen, j0));
         if constexpr (SUMS) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) sum += p[r];
@@ -240,6 +258,18 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
 #pragma unroll
             for (int c = 0; c < kBlocks; ++c) o[c] = mfma(Keys32<D>::columns(v_tile, i, c), weights[i], o[c]);
     };
+    Stream<D, PAGED> stream(keys, wave, key_begin);
+    auto step = [&](int j0, char *__restrict__ k_tile, char *__restrict__ v_tile, char *__restrict__ next_k, char *__restrict__ next_v) {
+        wait_for_loads();
+        const bool is_whole = whole(j0);
+        if (!is_whole && clean_values<D>(v_tile, wave, n_keys - j0)) shared.special = 1;
+        // Behind this barrier the tile is complete and all are done with the one before, whose place the next one takes.
+        __syncthreads();
+        if (j0 + kKeys < key_end) stream.next(j0 + kKeys, next_k, next_v);
+        if (is_whole ? !idle : !idle && !(a.s.causal && j0 > place0 + 31) && !(a.s.window > 0 && j0 + kKeys - 1 <= place0 - a.s.window))
+            add_tile(j0, k_tile, v_tile, !is_whole);
+    };
+    if (key_begin < key_end) stream.next(key_begin, shared.k[0], shared.v[0]);
     for (int j0 = key_begin; j0 < key_end; j0 += 2 * kKeys) {
         step(j0, shared.k[0], shared.v[0], shared.k[1], shared.v[1]);
         if (j0 + kKeys < key_end) step(j0 + kKeys, shared.k[1], shared.v[1], shared.k[0], shared.v[0]);
@@ -248,7 +278,7 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     __syncthreads();
     if (shared.special) {
         for (int j0 = key_begin; j0 < key_end; j0 += kKeys) {
-            if (!mixed(j0)) continue;
+            if (whole(j0)) continue;
             for (int j = j0; j < min(j0 + kKeys, n_keys); ++j) {
                 if (row >= at.end || j < first_seen || j >= last_seen) continue;
                 const uint16_t *value = keys.v_at(j, keys.page(j)) + 4 * (lane >> 5);
