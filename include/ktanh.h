@@ -324,7 +324,7 @@ typedef struct kcap_shape {
     size_t docs;                   /* documents                                                     */
     size_t q_rows, k_rows;         /* rows of q, and of k and v, all documents together             */
     size_t heads, kv_heads, dim;   /* heads a multiple of kv_heads; dim 64 or 128                   */
-    size_t q_row, q_head;          /* strides in elements, multiples of 8: tensors are              */
+    size_t q_row, q_head;          /* strides in elements, multiples of 8 below 2^24: tensors are   */
     size_t k_row, k_head;          /*   [rows][heads][dim] with dim contiguous                      */
     size_t v_row, v_head;
     double scale, cap;             /* scale finite, 0 < cap <= KCAP_MAX                             */
@@ -384,7 +384,8 @@ typedef struct kcap_pages {
  *   lengths    device, docs: keys of each sequence
  *   q_offsets  device, docs + 1, or NULL: one query for each sequence (q_rows == docs), which is the faster form for that
  *   workspace  device, 16-byte aligned, kcap_attention_paged_workspace bytes; unused and may be NULL where that is 0.
- *              What it holds before does not matter; calls that may run at once need one each. */
+ *              What it holds before does not matter; calls that may run at once need one each.
+ * kcap_attention_paged_workspace: `single` is whether q_offsets will be NULL. */
 size_t kcap_attention_paged_workspace(const kcap_shape_t *shape, const kcap_pages_t *cache, int single);
 ktanh_status_t kcap_attention_paged(const kcap_shape_t *shape, const kcap_pages_t *cache, const uint16_t *q, const uint16_t *k_cache,
                                     const uint16_t *v_cache, const int32_t *pages, const int32_t *lengths,

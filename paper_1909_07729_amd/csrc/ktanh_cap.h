@@ -36,7 +36,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kRows = 128;   // rows of a block: 32 for each wavefront
-constexpr int kTile = 64;    // rows of a tile in LDS
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // A tensor [rows][heads][dim], dim contiguous.
@@ -188,6 +187,54 @@ __device__ __forceinline__ void load_direct(const void *from, char *to)
 
 // This wavefront's loads, direct ones among them, have arrived.
 __device__ __forceinline__ void wait_for_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
+// Tiles of 32 rows of two tensors on their way to LDS, one behind the other, a wavefront's stretches of each; a row behind the last one is
+// read as the last.  One address for all lanes and 32 bits of offset for each (strides are below 2^24).
+template <int D>
+struct Stream {
+    typedef Keys32<D> Tile;
+    static constexpr int kShare = Tile::kStretches / kWaves;
+    const uint16_t *a_rows, *b_rows;
+    long long a_row, b_row;
+    int last, wave;
+    const char *a, *b;  // the next tile's first row of this wavefront
+    uint32_t a_off, b_off;
+
+    __device__ __forceinline__ Stream(const uint16_t *a_rows, long long a_row, const uint16_t *b_rows, long long b_row, int last, int wave, int at)
+        : a_rows(a_rows), b_rows(b_rows), a_row(a_row), b_row(b_row), last(last), wave(wave)
+    {
+        const uint32_t row = Tile::row_of_lane(0), chunk = 16 * Tile::chunk_of_lane();
+        a_off = row * 2 * (uint32_t)a_row + chunk;
+        b_off = row * 2 * (uint32_t)b_row + chunk;
+        start(at);
+    }
+    __device__ __forceinline__ void start(int at)
+    {
+        a = reinterpret_cast<const char *>(a_rows + (at + wave * kShare) * a_row);
+        b = reinterpret_cast<const char *>(b_rows + (at + wave * kShare) * b_row);
+    }
+    // Loads rows at .. at + 31, which are next.
+    __device__ __forceinline__ void next(int at, char *a_tile, char *b_tile)
+    {
+#pragma unroll
+        for (int n = 0; n < kShare; ++n) {
+            const int g = wave * kShare + n;
+            uint32_t a_at = a_off, b_at = b_off;
+            const char *a_from = a + n * 2 * a_row, *b_from = b + n * 2 * b_row;
+            if (at + 32 > last + 1) {
+                const uint32_t there = min(Tile::row_of_lane(g), last - at), chunk = 16 * Tile::chunk_of_lane();
+                a_from = reinterpret_cast<const char *>(a_rows + at * a_row);
+                b_from = reinterpret_cast<const char *>(b_rows + at * b_row);
+                a_at = there * 2 * (uint32_t)a_row + chunk;
+                b_at = there * 2 * (uint32_t)b_row + chunk;
+            }
+            load_direct(a_from + a_at, a_tile + Tile::stretch_at(g));
+            load_direct(b_from + b_at, b_tile + Tile::stretch_at(g));
+        }
+        a += 32 * 2 * a_row;
+        b += 32 * 2 * b_row;
+    }
+};
 
 // ------------------------------------------------------------------------------------------- blocks
 // Blocks that compute, and behind them `heads` blocks that clear.

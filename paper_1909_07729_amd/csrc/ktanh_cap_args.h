@@ -28,7 +28,7 @@ inline ktanh_status_t read_shape(const kcap_shape_t *s, const uint16_t *q, const
     if (!(s->cap > 0.0 && s->cap <= KCAP_MAX) || !std::isfinite(s->scale)) return KT_ERR_SHAPE;
     for (size_t stride : {s->q_row, s->q_head, s->k_row, s->k_head, s->v_row, s->v_head}) {
         if (stride % 8 != 0) return KT_ERR_ALIGN;
-        if (stride > (size_t)1 << 40) return KT_ERR_SHAPE;
+        if (stride >= (size_t)1 << 24) return KT_ERR_SHAPE;
     }
     if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return KT_ERR_ALIGN;
     out->docs = (int)s->docs;
@@ -76,7 +76,7 @@ inline ktanh_status_t read_pages(const kcap_pages_t *p, const int32_t *pages, co
     if (p->page_count == 0 || p->page_count > 0x7FFFFFFF || p->most == 0 || p->most > (1u << 30) / p->page_size || p->table_row > (size_t)1 << 40) return KT_ERR_SHAPE;
     for (size_t stride : {p->k_page, p->k_slot, p->k_head, p->v_page, p->v_slot, p->v_head}) {
         if (stride % 8 != 0) return KT_ERR_ALIGN;
-        if (stride > (size_t)1 << 31) return KT_ERR_SHAPE;
+        if (stride > (size_t)1 << 40) return KT_ERR_SHAPE;
     }
     if (!aligned16(k) || !aligned16(v)) return KT_ERR_ALIGN;
     if (reinterpret_cast<uintptr_t>(pages) % 4 != 0 || reinterpret_cast<uintptr_t>(lengths) % 4 != 0) return KT_ERR_ALIGN;
@@ -91,8 +91,11 @@ inline ktanh_status_t read_pages(const kcap_pages_t *p, const int32_t *pages, co
     return KT_OK;
 }
 
-// Many queries of each sequence over the cache (ktanh_cap_forward.hip).
-ktanh_status_t launch_forward_paged(const CapShape &s, const CapPages &p, const int *q_offsets, uint16_t *o, int dim, const KtCapPack &pack,
-                                    ktanh_stream_t stream);
+// Many queries of each sequence over the cache (ktanh_cap_forward.hip).  Where forward_parts is above 1 the workspace holds
+// forward_sums Float32 sums and as many times dim numerators.
+int forward_parts(const kcap_shape_t &s, const kcap_pages_t &p);
+inline size_t forward_sums(size_t parts, size_t rows, size_t heads) { return (parts * rows * heads + 31) / 32 * 32; }
+ktanh_status_t launch_forward_paged(const CapShape &s, const CapPages &p, const int *q_offsets, uint16_t *o, int dim, int parts, float *workspace,
+                                    const KtCapPack &pack, ktanh_stream_t stream);
 
 }  // namespace ktanh_cap

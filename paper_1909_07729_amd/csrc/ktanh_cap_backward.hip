@@ -25,34 +25,19 @@ struct BackwardArgs {
     int parts;
 };
 
-// 64 rows of two tensors on their way to LDS: rows from `end` on are zero.
-template <int D>
-struct Pair {
-    static constexpr int kChunks = D / 8, kStep = kThreads / kChunks, kCount = kTile / kStep;
-    u32x4 a[kCount], b[kCount];
+constexpr int kTile = 32;  // rows of a tile in LDS
 
-    __device__ __forceinline__ void load(const Rows &from_a, const Rows &from_b, int row0, int end)
-    {
-        const int chunk = threadIdx.x % kChunks;
+// Of the rows that this wavefront loaded, those behind the last become zero in both tiles: what they hold is not the document's.
+template <int D>
+__device__ __forceinline__ void clear_behind(char *a_tile, char *b_tile, int wave, int there)
+{
 #pragma unroll
-        for (int n = 0; n < kCount; ++n) {
-            const int row = min(row0 + (int)threadIdx.x / kChunks + n * kStep, end - 1);
-            a[n] = *reinterpret_cast<const u32x4 *>(from_a.at + row * from_a.row + 8 * chunk);
-            b[n] = *reinterpret_cast<const u32x4 *>(from_b.at + row * from_b.row + 8 * chunk);
-        }
+    for (int n = 0; n < Stream<D>::kShare; ++n) {
+        const int g = wave * Stream<D>::kShare + n, at = Keys32<D>::stretch_at(g) + 16 * (threadIdx.x & 63);
+        if (Keys32<D>::row_of_lane(g) >= there)
+            *reinterpret_cast<u32x4 *>(a_tile + at) = *reinterpret_cast<u32x4 *>(b_tile + at) = u32x4{0, 0, 0, 0};
     }
-    __device__ __forceinline__ void store(char *to_a, char *to_b, int row0, int end) const
-    {
-        const int chunk = threadIdx.x % kChunks;
-#pragma unroll
-        for (int n = 0; n < kCount; ++n) {
-            const int row = threadIdx.x / kChunks + n * kStep;
-            const bool there = row0 + row < end;
-            *reinterpret_cast<u32x4 *>(to_a + chunk_at<D>(row, chunk)) = there ? a[n] : u32x4{0, 0, 0, 0};
-            *reinterpret_cast<u32x4 *>(to_b + chunk_at<D>(row, chunk)) = there ? b[n] : u32x4{0, 0, 0, 0};
-        }
-    }
-};
+}
 
 __device__ __forceinline__ Rows of_head(const Rows &t, int head) { return Rows{t.at + head * t.head, t.row, t.head}; }
 
@@ -91,9 +76,9 @@ __device__ __forceinline__ void store_row(float *row, const f32x16 (&acc)[D / 32
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, 1) void cap_dq_kernel(BackwardArgs a, KtCapPack pack)
+__global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtCapPack pack)
 {
-    constexpr int kBytes = kTile * kPitch<D>, kSteps = D / 16, kBlocks = D / 32;
+    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32;
     struct Shared {
         f32x2 lines[128];  // first: the offset of a line is its address
         char k[2][kBytes], v[2][kBytes];
@@ -157,39 +142,42 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dq_kernel(BackwardArgs a, KtC
     f32x16 dq[kBlocks];
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c) dq[c] = f32x16{0};
-    Pair<D> share;
-    if (key_begin < key_end) share.load(keys, values, key_begin, n_keys);
-    int buffer = 0;
-    for (int j0 = key_begin; j0 < key_end; j0 += kTile, buffer ^= 1) {
-        char *k_tile = shared.k[buffer], *v_tile = shared.v[buffer];
-        share.store(k_tile, v_tile, j0, n_keys);
+    // tiles that every query of the block sees whole
+    const int whole_from = a.s.window > 0 ? block_last - a.s.window + 1 : 0, whole_to = a.s.causal ? min(n_keys, block_first + 1) : n_keys;
+    const bool idle = row0 >= at.end;
+    Stream<D> stream(keys.at, keys.row, values.at, values.row, n_keys - 1, wave, key_begin);
+    auto step = [&](int j0, char *__restrict__ k_tile, char *__restrict__ v_tile, char *__restrict__ next_k, char *__restrict__ next_v) {
+        wait_for_loads();
+        const bool whole = j0 >= whole_from && j0 + kTile <= whole_to;
+        if (j0 + kTile > n_keys) clear_behind<D>(k_tile, v_tile, wave, n_keys - j0);
+        // Behind this barrier the tile is complete and all are done with the one before, whose place the next one takes.
         __syncthreads();
-        if (j0 + kTile < key_end) share.load(keys, values, j0 + kTile, n_keys);
-        const bool none = (a.s.causal && j0 > place0 + 31) || (a.s.window > 0 && j0 + kTile - 1 <= place0 - a.s.window) || row0 >= at.end;
-        if (none) continue;
-        const bool partial = j0 + kTile > n_keys || (a.s.causal && j0 + kTile - 1 > place0) ||
-                             (a.s.window > 0 && j0 <= place0 + 31 - a.s.window);
+        if (j0 + kTile < key_end) stream.next(j0 + kTile, next_k, next_v);
+        if (idle || (!whole && ((a.s.causal && j0 > place0 + 31) || (a.s.window > 0 && j0 + kTile - 1 <= place0 - a.s.window)))) return;
+        f32x16 s = f32x16{0}, dp = f32x16{0};
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            f32x16 s = f32x16{0}, dp = f32x16{0};
+        for (int k = 0; k < kSteps; ++k) s = mfma(Keys32<D>::rows(k_tile, k), q[k], s);
 #pragma unroll
-            for (int k = 0; k < kSteps; ++k) s = mfma(rows_of<D>(k_tile, 32 * sub, k), q[k], s);
+        for (int k = 0; k < kSteps; ++k) dp = mfma(Keys32<D>::rows(v_tile, k), d_o[k], dp);
+        float ds[16];
 #pragma unroll
-            for (int k = 0; k < kSteps; ++k) dp = mfma(rows_of<D>(v_tile, 32 * sub, k), d_o[k], dp);
-            float ds[16];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float t = capped(s[r] * a.s.to_x, lines);
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(t, unit, -lse2));
-                ds[r] = p * (dp[r] - delta) * __builtin_fmaf(-t, t, 1.0f);
-            }
-            if (partial) keep(ds, Span(first_seen, last_seen, j0 + 32 * sub));
-            const bf16x8 shares[2] = {pack8(ds), pack8(ds + 8)};
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int c = 0; c < kBlocks; ++c) dq[c] = mfma(columns_of<D>(k_tile, 32 * sub + 16 * i, c), shares[i], dq[c]);
+        for (int r = 0; r < 16; ++r) {
+            const float t = capped(s[r] * a.s.to_x, lines);
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(t, unit, -lse2));
+            ds[r] = p * (dp[r] - delta) * __builtin_fmaf(-t, t, 1.0f);
         }
+        if (!whole) keep(ds, Span(first_seen, last_seen, j0));
+        const bf16x8 shares[2] = {pack8(ds), pack8(ds + 8)};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int c = 0; c < kBlocks; ++c) dq[c] = mfma(Keys32<D>::columns(k_tile, i, c), shares[i], dq[c]);
+    };
+    if (key_begin < key_end) stream.next(key_begin, shared.k[0], shared.v[0]);
+    __syncthreads();  // lines
+    for (int j0 = key_begin; j0 < key_end; j0 += 2 * kTile) {
+        step(j0, shared.k[0], shared.v[0], shared.k[1], shared.v[1]);
+        if (j0 + kTile < key_end) step(j0 + kTile, shared.k[1], shared.v[1], shared.k[0], shared.v[0]);
     }
     if (row < at.end) store_row<D>(a.dq + ((long long)row * a.s.heads + head) * D, dq, a.s.scale);
 }
@@ -197,11 +185,11 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dq_kernel(BackwardArgs a, KtC
 template <int D>
 __global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, KtCapPack pack)
 {
-    constexpr int kBytes = kTile * kPitch<D>, kSteps = D / 16, kBlocks = D / 32;
+    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32;
     struct Shared {
         f32x2 lines[128];  // first: the offset of a line is its address
         char q[2][kBytes], d_o[2][kBytes];
-        float sums[2][2][kTile];  // lse * log2 e | delta of a tile's rows
+        float sums[2][2 * kTile];  // lse * log2 e | delta of a tile's rows
     };
     __shared__ __align__(16) Shared shared;
     f32x2 *lines = shared.lines;
@@ -243,67 +231,82 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, K
     for (int c = 0; c < kBlocks; ++c) dk[c] = dv[c] = f32x16{0};
 
     const int heads = a.s.group / a.parts, head0 = kv_head * a.s.group + part * heads;
-    const int rounds = from < to ? (to - from + kTile - 1) / kTile : 0;
-    Pair<D> share;
-    float share_sum = 0.0f;
-    auto load = [&](int n) {  // the n-th tile: heads one behind the other
-        const int head = head0 + n / rounds, i0 = from + n % rounds * kTile;
-        Rows q = of_head(a.s.q, head), d_o = of_head(a.d_o, head);
-        q.at += q_begin * q.row;
-        d_o.at += q_begin * d_o.row;
-        share.load(q, d_o, i0, n_queries);
-        const int i = min(i0 + lane, n_queries - 1);
-        if (wave < 2) share_sum = (wave == 0 ? a.lse : a.delta)[(long long)head * a.s.q_rows + q_begin + i];
-    };
-    if (rounds > 0) load(0);
-    int buffer = 0;
-    for (int n = 0; n < heads * rounds; ++n, buffer ^= 1) {
-        const int i0 = from + n % rounds * kTile;
-        char *q_tile = shared.q[buffer], *do_tile = shared.d_o[buffer];
-        share.store(q_tile, do_tile, i0, n_queries);
-        if (wave < 2) shared.sums[buffer][wave][lane] = wave == 0 ? share_sum * kLog2e : share_sum;
-        __syncthreads();
-        if (n + 1 < heads * rounds) load(n + 1);
-        const int first = i0 + shift;  // the tile's first query's place
-        const bool none = (a.s.causal && first + kTile - 1 < key0) || (a.s.window > 0 && first > key0 + 31 + a.s.window - 1) || row0 >= at.end;
-        if (none) continue;
-        const bool partial = i0 + kTile > n_queries || (a.s.causal && first < key0 + 31) || (a.s.window > 0 && first + kTile - 1 >= key0 + a.s.window);
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            f32x16 s = f32x16{0}, dp = f32x16{0};
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) s = mfma(rows_of<D>(q_tile, 32 * sub, i), k[i], s);
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) dp = mfma(rows_of<D>(do_tile, 32 * sub, i), v[i], dp);
-            float p[16], ds[16];
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int at_row = 32 * sub + 8 * g + 4 * (lane >> 5);
-                const f32x4 lse2 = *reinterpret_cast<const f32x4 *>(&shared.sums[buffer][0][at_row]);
-                const f32x4 delta = *reinterpret_cast<const f32x4 *>(&shared.sums[buffer][1][at_row]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 4 * g + e;
-                    const float t = capped(s[r] * a.s.to_x, lines);
-                    p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(t, unit, -lse2[e]));
-                    ds[r] = p[r] * (dp[r] - delta[e]) * __builtin_fmaf(-t, t, 1.0f);
-                }
-            }
-            if (partial) {
-                const Span seen(first_seen, last_seen, i0 + 32 * sub);
-                keep(p, seen);
-                keep(ds, seen);
-            }
-            const bf16x8 weights[2] = {pack8(p), pack8(p + 8)}, shares[2] = {pack8(ds), pack8(ds + 8)};
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int c = 0; c < kBlocks; ++c) {
-                    dv[c] = mfma(columns_of<D>(do_tile, 32 * sub + 16 * i, c), weights[i], dv[c]);
-                    dk[c] = mfma(columns_of<D>(q_tile, 32 * sub + 16 * i, c), shares[i], dk[c]);
-                }
+    // tiles of queries that all see every key of the block
+    const int whole_from = a.s.causal ? block_last - shift : 0;
+    const int whole_to = a.s.window > 0 ? (int)min((long long)n_queries, (long long)block_first - shift + a.s.window) : n_queries;
+    const bool idle = row0 >= at.end;
+    const long long first_query = q_begin;
+    const Rows q = of_head(a.s.q, head0), d_o = of_head(a.d_o, head0);
+    Stream<D> stream(q.at + first_query * q.row, q.row, d_o.at + first_query * d_o.row, d_o.row, n_queries - 1, wave, from);
+    // a wavefront brings 16 of a tile's 64 sums
+    const float *sum_from = ((wave & 1) == 0 ? a.lse : a.delta) + (long long)head0 * a.s.q_rows + q_begin;
+    float next_sum = 0.0f;
+    int left = from < to ? heads : 0, next_query = from;  // heads not loaded to their end, and where
+    auto load = [&](char *q_tile, char *do_tile) {  // the next tile: heads one behind the other
+        stream.next(next_query, q_tile, do_tile);
+        next_sum = sum_from[min(next_query + 16 * (wave >> 1) + (lane & 15), n_queries - 1)];
+        next_query += kTile;
+        if (next_query >= to) {
+            next_query = from;
+            --left;
+            stream.a_rows += q.head;
+            stream.b_rows += d_o.head;
+            stream.start(from);
+            sum_from += a.s.q_rows;
         }
-    }
+    };
+    auto step = [&](int i0, char *__restrict__ q_tile, char *__restrict__ do_tile, float *__restrict__ sums, char *__restrict__ next_q,
+                    char *__restrict__ next_do) {
+        wait_for_loads();
+        if (i0 + kTile > n_queries) clear_behind<D>(q_tile, do_tile, wave, n_queries - i0);
+        if (lane < 16) sums[(wave & 1) * kTile + 16 * (wave >> 1) + lane] = (wave & 1) == 0 ? next_sum * kLog2e : next_sum;
+        __syncthreads();
+        if (left > 0) load(next_q, next_do);
+        const int first = i0 + shift;  // the place of the tile's first query
+        const bool whole = i0 >= whole_from && i0 + kTile <= whole_to;
+        if (idle || (!whole && ((a.s.causal && first + kTile - 1 < key0) || (a.s.window > 0 && first > key0 + 31 + a.s.window - 1)))) return;
+        f32x16 s = f32x16{0}, dp = f32x16{0};
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) s = mfma(Keys32<D>::rows(q_tile, i), k[i], s);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) dp = mfma(Keys32<D>::rows(do_tile, i), v[i], dp);
+        float p[16], ds[16];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int at_row = 8 * g + 4 * (lane >> 5);
+            const f32x4 lse2 = *reinterpret_cast<const f32x4 *>(sums + at_row);
+            const f32x4 delta = *reinterpret_cast<const f32x4 *>(sums + kTile + at_row);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = 4 * g + e;
+                const float t = capped(s[r] * a.s.to_x, lines);
+                p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(t, unit, -lse2[e]));
+                ds[r] = p[r] * (dp[r] - delta[e]) * __builtin_fmaf(-t, t, 1.0f);
+            }
+        }
+        if (!whole) {
+            const Span seen(first_seen, last_seen, i0);
+            keep(p, seen);
+            keep(ds, seen);
+        }
+        const bf16x8 weights[2] = {pack8(p), pack8(p + 8)}, shares[2] = {pack8(ds), pack8(ds + 8)};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int c = 0; c < kBlocks; ++c) {
+                dv[c] = mfma(Keys32<D>::columns(do_tile, i, c), weights[i], dv[c]);
+                dk[c] = mfma(Keys32<D>::columns(q_tile, i, c), shares[i], dk[c]);
+            }
+    };
+    const int heads_of_tiles = left;
+    if (left > 0) load(shared.q[0], shared.d_o[0]);
+    __syncthreads();  // lines
+    bool odd = false;
+    for (int h = 0; h < heads_of_tiles; ++h)
+        for (int i0 = from; i0 < to; i0 += kTile, odd = !odd) {
+            if (odd) step(i0, shared.q[1], shared.d_o[1], shared.sums[1], shared.q[0], shared.d_o[0]);
+            else step(i0, shared.q[0], shared.d_o[0], shared.sums[0], shared.q[1], shared.d_o[1]);
+        }
     if (row >= at.end) return;
     const long long to_row = ((long long)row * a.s.kv_heads + kv_head) * D;
     if (a.dk_parts == nullptr) {

@@ -228,7 +228,12 @@ ktanh_status_t attention_paged(const kcap_shape_t *shape, const kcap_pages_t *ca
     if (reinterpret_cast<uintptr_t>(o) % 8 != 0 || reinterpret_cast<uintptr_t>(q_offsets) % 4 != 0) return KT_ERR_ALIGN;
     KtCapPack pack;
     if ((st = pack_lines(lut, &pack)) != KT_OK) return st;
-    if (q_offsets != nullptr) return launch_forward_paged(a.s, p, q_offsets, o, (int)shape->dim, pack, stream);
+    if (q_offsets != nullptr) {
+        const int parts = forward_parts(*shape, *cache);
+        if (parts > 1 && workspace == nullptr) return KT_ERR_NULL;
+        if (parts > 1 && !aligned16(workspace)) return KT_ERR_ALIGN;
+        return launch_forward_paged(a.s, p, q_offsets, o, (int)shape->dim, parts, static_cast<float *>(workspace), pack, stream);
+    }
 
     if (shape->q_rows != shape->docs) return KT_ERR_SHAPE;
     a.p = p;
@@ -258,9 +263,13 @@ ktanh_status_t attention_paged(const kcap_shape_t *shape, const kcap_pages_t *ca
 
 extern "C" size_t kcap_attention_paged_workspace(const kcap_shape_t *shape, const kcap_pages_t *cache, int single)
 {
-    if (shape == nullptr || cache == nullptr || !single || shape->docs == 0 || cache->page_size == 0 || cache->page_size > 1u << 20 ||
-        cache->most == 0 || cache->most > 1u << 30 || shape->docs > 1u << 30 || shape->heads > 65536 || shape->kv_heads > 65536 || shape->dim > 128)
+    if (shape == nullptr || cache == nullptr || shape->docs == 0 || cache->page_size == 0 || cache->page_size > 1u << 20 ||
+        cache->most == 0 || cache->most > 1u << 30 || shape->docs > 1u << 30 || shape->heads > 65536 || shape->kv_heads > 65536 || shape->dim > 128 || shape->q_rows > 1u << 30)
         return 0;
+    if (!single) {
+        const size_t parts = (size_t)forward_parts(*shape, *cache);
+        return parts > 1 ? (forward_sums(parts, shape->q_rows, shape->heads) + parts * shape->q_rows * shape->heads * shape->dim) * 4 : 0;
+    }
     const unsigned long long spans = spans_of(*cache, span_of(*shape, *cache));
     if (spans <= 1) return 0;
     return (size_t)(sums_bytes(*shape, spans) + shape->docs * spans * shape->heads * shape->dim * 4);

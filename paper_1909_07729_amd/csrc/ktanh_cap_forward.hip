@@ -50,72 +50,41 @@ struct Keys {
 
 constexpr int kKeys = 32;  // of a tile
 
-// The wavefront's stretches of a tile.
+// The same for keys and values in pages: the pages of a tile's rows are looked up one tile ahead.
 template <int D>
-constexpr int kShare = Keys32<D>::kStretches / kWaves;
-
-template <int D, bool PAGED>
-__device__ __forceinline__ void pages_of(const Keys<PAGED> &keys, int j0, int wave, int (&pages)[kShare<D>])
-{
-#pragma unroll
-    for (int n = 0; n < kShare<D>; ++n) pages[n] = keys.page(j0 + Keys32<D>::row_of_lane(wave * kShare<D> + n));
-}
-
-// Tiles on their way to LDS, one behind the other; a row that is not there is read as the last one.
-template <int D, bool PAGED>
-struct Stream {
-    const Keys<PAGED> &keys;
+struct PagedStream {
+    typedef Keys32<D> Tile;
+    static constexpr int kShare = Tile::kStretches / kWaves;
+    const Keys<true> &keys;
     const int wave;
-    // the tile's first row (one address for all lanes), and a lane's offsets from it (32 bits: strides are below 2^24)
-    const char *k, *v;
-    uint32_t k_off, v_off;
-    int pages[kShare<D>];
+    int pages[kShare];
 
-    __device__ __forceinline__ Stream(const Keys<PAGED> &keys, int wave, int j0) : keys(keys), wave(wave)
+    __device__ __forceinline__ PagedStream(const Keys<true> &keys, int wave, int at) : keys(keys), wave(wave) { look_up(at); }
+    __device__ __forceinline__ void look_up(int at)
     {
-        if constexpr (PAGED) {
-            pages_of<D>(keys, j0, wave, pages);
-        } else {
-            const int g = wave * kShare<D>;
-            k = reinterpret_cast<const char *>(keys.k + (j0 + g) * keys.k_row);
-            v = reinterpret_cast<const char *>(keys.v + (j0 + g) * keys.v_row);
-            const uint32_t row = Keys32<D>::row_of_lane(0), chunk = 16 * Keys32<D>::chunk_of_lane();
-            k_off = row * 2 * (uint32_t)keys.k_row + chunk;
-            v_off = row * 2 * (uint32_t)keys.v_row + chunk;
-        }
-    }
-    // Loads rows j0 .. j0 + 31, which are next.
-    __device__ __forceinline__ void next(int j0, char *k_tile, char *v_tile)
-    {
-        const int chunk = Keys32<D>::chunk_of_lane();
 #pragma unroll
-        for (int n = 0; n < kShare<D>; ++n) {
-            const int g = wave * kShare<D> + n, row = Keys32<D>::row_of_lane(g);
-            if constexpr (PAGED) {
-                load_direct(keys.k_at(j0 + row, pages[n]) + 8 * chunk, k_tile + Keys32<D>::stretch_at(g));
-                load_direct(keys.v_at(j0 + row, pages[n]) + 8 * chunk, v_tile + Keys32<D>::stretch_at(g));
-            } else {
-                uint32_t k_at = k_off, v_at = v_off;
-                const char *k_row = k + n * 2 * keys.k_row, *v_row = v + n * 2 * keys.v_row;
-                if (j0 + kKeys > keys.last + 1) {
-                    const uint32_t there = min(row, keys.last - j0);
-                    k_row = reinterpret_cast<const char *>(keys.k + j0 * keys.k_row);
-                    v_row = reinterpret_cast<const char *>(keys.v + j0 * keys.v_row);
-                    k_at = there * 2 * (uint32_t)keys.k_row + 16 * chunk;
-                    v_at = there * 2 * (uint32_t)keys.v_row + 16 * chunk;
-                }
-                load_direct(k_row + k_at, k_tile + Keys32<D>::stretch_at(g));
-                load_direct(v_row + v_at, v_tile + Keys32<D>::stretch_at(g));
-            }
+        for (int n = 0; n < kShare; ++n) pages[n] = keys.page(at + Tile::row_of_lane(wave * kShare + n));
+    }
+    __device__ __forceinline__ void next(int at, char *k_tile, char *v_tile)
+    {
+        const int chunk = Tile::chunk_of_lane();
+#pragma unroll
+        for (int n = 0; n < kShare; ++n) {
+            const int g = wave * kShare + n, row = Tile::row_of_lane(g);
+            load_direct(keys.k_at(at + row, pages[n]) + 8 * chunk, k_tile + Tile::stretch_at(g));
+            load_direct(keys.v_at(at + row, pages[n]) + 8 * chunk, v_tile + Tile::stretch_at(g));
         }
-        if constexpr (PAGED) {
-            pages_of<D>(keys, j0 + kKeys, wave, pages);
-        } else {
-            k += kKeys * 2 * keys.k_row;
-            v += kKeys * 2 * keys.v_row;
-        }
+        look_up(at + kKeys);
     }
 };
+
+template <int D>
+__device__ __forceinline__ Stream<D> stream_of(const Keys<false> &keys, int wave, int at)
+{
+    return Stream<D>(keys.k, keys.k_row, keys.v, keys.v_row, keys.last, wave, at);
+}
+template <int D>
+__device__ __forceinline__ PagedStream<D> stream_of(const Keys<true> &keys, int wave, int at) { return PagedStream<D>(keys, wave, at); }
 
 // Infinities and NaN become zero.  Returns whether there was one.
 __device__ __forceinline__ bool take_special(u32x4 *v)
@@ -137,8 +106,8 @@ __device__ __forceinline__ bool clean_values(char *v_tile, int wave, int there)
 {
     bool found = false;
 #pragma unroll
-    for (int n = 0; n < kShare<D>; ++n) {
-        const int g = wave * kShare<D> + n;
+    for (int n = 0; n < Stream<D>::kShare; ++n) {
+        const int g = wave * Stream<D>::kShare + n;
         u32x4 *at = reinterpret_cast<u32x4 *>(v_tile + Keys32<D>::stretch_at(g) + 16 * (threadIdx.x & 63));
         u32x4 w = *at;
         if (Keys32<D>::row_of_lane(g) >= there) w = u32x4{0, 0, 0, 0};
@@ -155,6 +124,9 @@ struct ForwardArgs {
     float *lse;
     CapPages p;
     unsigned tiles;
+    // PAGED: blocks of a stretch that share its keys, with sums [parts][q_rows][heads] and numerators [parts][q_rows][heads][dim] in Float32
+    int parts;
+    float *part_sums, *part_values;
 };
 
 // SUMS: with log-sums.
@@ -170,7 +142,7 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     __shared__ __align__(16) Shared shared;
     f32x2 *lines = shared.lines;
 
-    const unsigned total = a.tiles * (unsigned)a.s.heads;
+    const unsigned total = a.tiles * (unsigned)(a.s.heads * a.parts);
     if (blockIdx.x >= padded(total)) {
         const int head = (int)(blockIdx.x - padded(total));
         clear_rows<D>(a.o, a.q_offsets, a.s.docs, a.s.q_rows, a.s.heads, head, [&](int row) {
@@ -181,9 +153,10 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     const unsigned place = place_of_block(blockIdx.x, total);
     if (place >= total) return;
     // heads that share keys side by side, then the stretches from the last (the longest, if causal) to the first
-    const int in_group = place % a.s.group;
-    const int tile = (int)(a.tiles - 1 - place / a.s.group % a.tiles);
-    const int kv_head = place / a.s.group / a.tiles, head = kv_head * a.s.group + in_group;
+    const int in_group = place % a.s.group, part = PAGED ? place / a.s.group % a.parts : 0;
+    const unsigned stretch = place / a.s.group / a.parts;
+    const int tile = (int)(a.tiles - 1 - stretch % a.tiles);
+    const int kv_head = stretch / a.tiles, head = kv_head * a.s.group + in_group;
     const Stretch at = stretch_of(tile, a.q_offsets, a.s.docs, a.s.q_rows, kRows);
     if (at.first >= at.end) return;
 
@@ -215,8 +188,13 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     const int place0 = row0 - at.begin + shift, my_place = row - at.begin + shift;
     const int block_first = at.first - at.begin + shift;
     const int block_last = min(at.first + kRows, at.end) - 1 - at.begin + shift;
-    const int key_end = a.s.causal ? min(n_keys, block_last + 1) : n_keys;
-    const int key_begin = a.s.window > 0 ? max(0, block_first - a.s.window + 1) & ~(kKeys - 1) : 0;
+    int key_end = a.s.causal ? min(n_keys, block_last + 1) : n_keys;
+    int key_begin = a.s.window > 0 ? max(0, block_first - a.s.window + 1) & ~(kKeys - 1) : 0;
+    if (PAGED && a.parts > 1) {  // this block's share of them, in whole tiles
+        const int share = (max(key_end - key_begin, 0) + a.parts * kKeys - 1) / (a.parts * kKeys) * kKeys;
+        key_begin = min(key_begin + part * share, max(key_end, key_begin));
+        key_end = min(key_end, key_begin + share);
+    }
 
     if (threadIdx.x == 0) shared.special = 0;
     const float unit = a.s.cap * kLog2e;
@@ -258,7 +236,7 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
 #pragma unroll
             for (int c = 0; c < kBlocks; ++c) o[c] = mfma(Keys32<D>::columns(v_tile, i, c), weights[i], o[c]);
     };
-    Stream<D, PAGED> stream(keys, wave, key_begin);
+    auto stream = stream_of<D>(keys, wave, key_begin);
     auto step = [&](int j0, char *__restrict__ k_tile, char *__restrict__ v_tile, char *__restrict__ next_k, char *__restrict__ next_v) {
         wait_for_loads();
         const bool is_whole = whole(j0);
@@ -298,6 +276,17 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     if (row >= at.end) return;
     if (SUMS && lane < 32)
         a.lse[(long long)head * a.s.q_rows + row] = sum > 0.0f ? __builtin_logf(sum) : sum == 0.0f ? -__builtin_inff() : sum;
+    if (PAGED && a.parts > 1) {
+        const long long at_row = ((long long)part * a.s.q_rows + row) * a.s.heads + head;
+        if (lane < 32) a.part_sums[at_row] = rounded_sum;
+        float *values = a.part_values + at_row * D + 4 * (lane >> 5);
+#pragma unroll
+        for (int c = 0; c < kBlocks; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<f32x4 *>(values + 32 * c + 8 * i) = f32x4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
+        return;
+    }
     const float to_mean = rounded_sum == 0.0f ? 0.0f : 1.0f / rounded_sum;
     const long long to = ((long long)row * a.s.heads + head) * D + 4 * (lane >> 5);
 #pragma unroll
@@ -317,14 +306,41 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
         }
 }
 
+// The parts of a row added up in their order: four values of one row and head for each thread.
+template <int D>
+__global__ __launch_bounds__(kThreads) void cap_join_parts_kernel(ForwardArgs a)
+{
+    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x, rows = (long long)a.s.q_rows * a.s.heads, at = i / (D / 4);
+    if (at >= rows) return;
+    const int first = offset_at(a.q_offsets, 0, a.s.q_rows), row = (int)(at / a.s.heads);
+    f32x4 n = f32x4{0, 0, 0, 0};
+    float total = 0.0f;
+    if (row >= first && row < offset_at(a.q_offsets, a.s.docs, a.s.q_rows))
+        for (int part = 0; part < a.parts; ++part) {
+            n += *reinterpret_cast<const f32x4 *>(a.part_values + (part * rows + at) * D + 4 * (i % (D / 4)));
+            total += a.part_sums[part * rows + at];
+        }
+    const float to_mean = total == 0.0f ? 0.0f : 1.0f / total;
+    *reinterpret_cast<u32x2 *>(a.o + 4 * i) = u32x2{pack2(n[0] * to_mean, n[1] * to_mean), pack2(n[2] * to_mean, n[3] * to_mean)};
+}
+
 template <bool PAGED, bool SUMS>
 ktanh_status_t launch_forward(const ForwardArgs &a, size_t dim, const KtCapPack &pack, ktanh_stream_t stream)
 {
-    const unsigned long long blocks = ((unsigned long long)a.tiles * a.s.heads + 7) / 8 * 8 + a.s.heads;
-    if (blocks > kMaxBlocks) return KT_ERR_SHAPE;
+    const unsigned long long blocks = ((unsigned long long)a.tiles * a.s.heads * a.parts + 7) / 8 * 8 + (a.parts == 1 ? a.s.heads : 0);
+    const unsigned long long joins = ((unsigned long long)a.s.q_rows * a.s.heads * dim / 4 + kThreads - 1) / kThreads;
+    if (blocks > kMaxBlocks || (a.parts > 1 && joins > kMaxBlocks)) return KT_ERR_SHAPE;
     auto *kernel = dim == 64 ? &cap_forward_kernel<64, PAGED, SUMS> : &cap_forward_kernel<128, PAGED, SUMS>;
     kernel<<<dim3((unsigned)blocks), dim3(kThreads), 0, static_cast<hipStream_t>(stream)>>>(a, pack);
-    return launched();
+    ktanh_status_t st = launched();
+    if constexpr (PAGED) {
+        if (st == KT_OK && a.parts > 1) {
+            auto *join = dim == 64 ? &cap_join_parts_kernel<64> : &cap_join_parts_kernel<128>;
+            join<<<dim3((unsigned)joins), dim3(kThreads), 0, static_cast<hipStream_t>(stream)>>>(a);
+            st = launched();
+        }
+    }
+    return st;
 }
 
 template <class Lut>
@@ -346,20 +362,33 @@ ktanh_status_t attention(const kcap_shape_t *shape, const uint16_t *q, const uin
     a.o = o;
     a.rest = rest;
     a.lse = lse;
+    a.parts = 1;
     a.tiles = (unsigned)(shape->q_rows / kRows + shape->docs);
     return lse != nullptr ? launch_forward<false, true>(a, shape->dim, pack, stream) : launch_forward<false, false>(a, shape->dim, pack, stream);
 }
 
 }  // namespace
 
-ktanh_status_t ktanh_cap::launch_forward_paged(const CapShape &s, const CapPages &p, const int *q_offsets, uint16_t *o, int dim,
-                                               const KtCapPack &pack, ktanh_stream_t stream)
+// Three blocks fit a compute unit: where a call has fewer than fill the chip, each shares its keys (256 or more for each) with others.
+int ktanh_cap::forward_parts(const kcap_shape_t &s, const kcap_pages_t &p)
+{
+    const unsigned long long blocks = (s.q_rows / kRows + s.docs) * s.heads, keys = (unsigned long long)p.most * p.page_size;
+    const unsigned long long fill = 768 / (blocks > 0 ? blocks : 1), most = keys / 256;
+    const unsigned long long parts = fill < most ? fill : most;
+    return parts < 1 ? 1 : parts > 64 ? 64 : (int)parts;
+}
+
+ktanh_status_t ktanh_cap::launch_forward_paged(const CapShape &s, const CapPages &p, const int *q_offsets, uint16_t *o, int dim, int parts,
+                                               float *workspace, const KtCapPack &pack, ktanh_stream_t stream)
 {
     ForwardArgs a{};
     a.s = s;
     a.p = p;
     a.q_offsets = q_offsets;
     a.o = o;
+    a.parts = parts;
+    a.part_sums = workspace;
+    a.part_values = workspace + forward_sums(parts, s.q_rows, s.heads);
     a.tiles = (unsigned)(s.q_rows / kRows + s.docs);
     return launch_forward<true, false>(a, (size_t)dim, pack, stream);
 }
