@@ -298,15 +298,17 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, K
                 dk[c] = mfma(Keys32<D>::columns(q_tile, i, c), shares[i], dk[c]);
             }
     };
-    const int heads_of_tiles = left;
+    const int tiles = left * ((to - from + kTile - 1) / kTile);
     if (left > 0) load(shared.q[0], shared.d_o[0]);
     __syncthreads();  // lines
-    bool odd = false;
-    for (int h = 0; h < heads_of_tiles; ++h)
-        for (int i0 = from; i0 < to; i0 += kTile, odd = !odd) {
-            if (odd) step(i0, shared.q[1], shared.d_o[1], shared.sums[1], shared.q[0], shared.d_o[0]);
-            else step(i0, shared.q[0], shared.d_o[0], shared.sums[0], shared.q[1], shared.d_o[1]);
-        }
+    int i0 = from;
+    for (int n = 0; n < tiles; n += 2) {
+        step(i0, shared.q[0], shared.d_o[0], shared.sums[0], shared.q[1], shared.d_o[1]);
+        i0 = i0 + kTile < to ? i0 + kTile : from;
+        if (n + 1 == tiles) break;
+        step(i0, shared.q[1], shared.d_o[1], shared.sums[1], shared.q[0], shared.d_o[0]);
+        i0 = i0 + kTile < to ? i0 + kTile : from;
+    }
     if (row >= at.end) return;
     const long long to_row = ((long long)row * a.s.kv_heads + kv_head) * D;
     if (a.dk_parts == nullptr) {
