@@ -183,12 +183,13 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, KtCapPack pack)
+__global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, KtCapPack pack)
 {
     constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32;
     struct Shared {
         f32x2 lines[128];  // first: the offset of a line is its address
         char q[2][kBytes], d_o[2][kBytes];
+        char v[kWaves][kBytes];   // each wavefront's 32 rows of values: registers for them would leave one wavefront to a SIMD
         float sums[2][2 * kTile];  // lse * log2 e | delta of a tile's rows
     };
     __shared__ __align__(16) Shared shared;
@@ -223,9 +224,14 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, K
     spread_lines(lines, pack, 1.0f);
     const float unit = a.s.cap * kLog2e;
 
-    bf16x8 k[kSteps], v[kSteps];
+    bf16x8 k[kSteps];
     load_row<D>(k, of_head(a.s.k, kv_head), row_there);
-    load_row<D>(v, of_head(a.s.v, kv_head), row_there);
+    {
+        const Rows v = of_head(a.s.v, kv_head);
+#pragma unroll
+        for (int g = 0; g < Keys32<D>::kStretches; ++g)
+            load_direct(v.at + min(row0 + Keys32<D>::row_of_lane(g), at.end - 1) * v.row + 8 * Keys32<D>::chunk_of_lane(), shared.v[wave] + Keys32<D>::stretch_at(g));
+    }
     f32x16 dk[kBlocks], dv[kBlocks];
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c) dk[c] = dv[c] = f32x16{0};
@@ -255,7 +261,7 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, K
             sum_from += a.s.q_rows;
         }
     };
-    auto step = [&](int i0, char *__restrict__ q_tile, char *__restrict__ do_tile, float *__restrict__ sums, char *__restrict__ next_q,
+    auto step = [&](int i0, const char *__restrict__ v_tile, char *__restrict__ q_tile, char *__restrict__ do_tile, float *__restrict__ sums, char *__restrict__ next_q,
                     char *__restrict__ next_do) {
         wait_for_loads();
         if (i0 + kTile > n_queries) clear_behind<D>(q_tile, do_tile, wave, n_queries - i0);
@@ -265,48 +271,57 @@ __global__ __launch_bounds__(kThreads, 1) void cap_dkdv_kernel(BackwardArgs a, K
         const int first = i0 + shift;  // the place of the tile's first query
         const bool whole = i0 >= whole_from && i0 + kTile <= whole_to;
         if (idle || (!whole && ((a.s.causal && first + kTile - 1 < key0) || (a.s.window > 0 && first > key0 + 31 + a.s.window - 1)))) return;
-        f32x16 s = f32x16{0}, dp = f32x16{0};
+        // the scores' weights, their product, and only then dP: fewer registers at once
+        f32x16 s = f32x16{0};
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) s = mfma(Keys32<D>::rows(q_tile, i), k[i], s);
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) dp = mfma(Keys32<D>::rows(do_tile, i), v[i], dp);
-        float p[16], ds[16];
+        float p[16], slope[16];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const int at_row = 8 * g + 4 * (lane >> 5);
-            const f32x4 lse2 = *reinterpret_cast<const f32x4 *>(sums + at_row);
-            const f32x4 delta = *reinterpret_cast<const f32x4 *>(sums + kTile + at_row);
+            const f32x4 lse2 = *reinterpret_cast<const f32x4 *>(sums + 8 * g + 4 * (lane >> 5));
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int r = 4 * g + e;
                 const float t = capped(s[r] * a.s.to_x, lines);
                 p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(t, unit, -lse2[e]));
-                ds[r] = p[r] * (dp[r] - delta[e]) * __builtin_fmaf(-t, t, 1.0f);
+                slope[r] = p[r] * __builtin_fmaf(-t, t, 1.0f);
             }
         }
         if (!whole) {
             const Span seen(first_seen, last_seen, i0);
             keep(p, seen);
-            keep(ds, seen);
+            keep(slope, seen);
         }
-        const bf16x8 weights[2] = {pack8(p), pack8(p + 8)}, shares[2] = {pack8(ds), pack8(ds + 8)};
+        const bf16x8 weights[2] = {pack8(p), pack8(p + 8)};
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int c = 0; c < kBlocks; ++c) {
-                dv[c] = mfma(Keys32<D>::columns(do_tile, i, c), weights[i], dv[c]);
-                dk[c] = mfma(Keys32<D>::columns(q_tile, i, c), shares[i], dk[c]);
-            }
+            for (int c = 0; c < kBlocks; ++c) dv[c] = mfma(Keys32<D>::columns(do_tile, i, c), weights[i], dv[c]);
+        f32x16 dp = f32x16{0};
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) dp = mfma(Keys32<D>::rows(do_tile, i), Keys32<D>::rows(v_tile, i), dp);
+        float ds[16];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 delta = *reinterpret_cast<const f32x4 *>(sums + kTile + 8 * g + 4 * (lane >> 5));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ds[4 * g + e] = slope[4 * g + e] * (dp[4 * g + e] - delta[e]);
+        }
+        const bf16x8 shares[2] = {pack8(ds), pack8(ds + 8)};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int c = 0; c < kBlocks; ++c) dk[c] = mfma(Keys32<D>::columns(q_tile, i, c), shares[i], dk[c]);
     };
     const int tiles = left * ((to - from + kTile - 1) / kTile);
     if (left > 0) load(shared.q[0], shared.d_o[0]);
     __syncthreads();  // lines
     int i0 = from;
     for (int n = 0; n < tiles; n += 2) {
-        step(i0, shared.q[0], shared.d_o[0], shared.sums[0], shared.q[1], shared.d_o[1]);
+        step(i0, shared.v[wave], shared.q[0], shared.d_o[0], shared.sums[0], shared.q[1], shared.d_o[1]);
         i0 = i0 + kTile < to ? i0 + kTile : from;
         if (n + 1 == tiles) break;
-        step(i0, shared.q[1], shared.d_o[1], shared.sums[1], shared.q[0], shared.d_o[0]);
+        step(i0, shared.v[wave], shared.q[1], shared.d_o[1], shared.sums[1], shared.q[0], shared.d_o[0]);
         i0 = i0 + kTile < to ? i0 + kTile : from;
     }
     if (row >= at.end) return;
