@@ -94,12 +94,11 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
     const unsigned place = place_of_block(blockIdx.x, total);
     if (place >= total) return;
     const int in_group = place % a.s.group;
-    const int tile = (int)(a.tiles - 1 - place / a.s.group % a.tiles);
     const int kv_head = place / a.s.group / a.tiles, head = kv_head * a.s.group + in_group;
-    const Stretch at = stretch_of(tile, a.q_offsets, a.s.docs, a.s.q_rows, kRows);
+    auto keys_of = [&](int doc) { return max(offset_at(a.k_offsets, doc + 1, a.s.k_rows) - offset_at(a.k_offsets, doc, a.s.k_rows), 0); };
+    const Stretch at = stretch_of((int)(place / a.s.group % a.tiles), a.q_offsets, a.s.docs, a.s.q_rows, a.s.causal, true, keys_of);
     if (at.first >= at.end) return;
-    const int k_begin = offset_at(a.k_offsets, at.doc, a.s.k_rows);
-    const int n_keys = max(offset_at(a.k_offsets, at.doc + 1, a.s.k_rows) - k_begin, 0);
+    const int k_begin = offset_at(a.k_offsets, at.doc, a.s.k_rows), n_keys = keys_of(at.doc);
     Rows keys = of_head(a.s.k, kv_head), values = of_head(a.s.v, kv_head);
     keys.at += k_begin * keys.row;
     values.at += k_begin * values.row;
@@ -204,11 +203,11 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
     }
     const unsigned place = place_of_block(blockIdx.x, total);
     if (place >= total) return;
-    const int part = place % a.parts, tile = (int)(place / a.parts % a.tiles), kv_head = place / a.parts / a.tiles;
-    const Stretch at = stretch_of(tile, a.k_offsets, a.s.docs, a.s.k_rows, kRows);
+    const int part = place % a.parts, kv_head = place / a.parts / a.tiles;
+    auto queries_of = [&](int doc) { return max(offset_at(a.q_offsets, doc + 1, a.s.q_rows) - offset_at(a.q_offsets, doc, a.s.q_rows), 0); };
+    const Stretch at = stretch_of((int)(place / a.parts % a.tiles), a.k_offsets, a.s.docs, a.s.k_rows, a.s.causal, false, queries_of);
     if (at.first >= at.end) return;
-    const int q_begin = offset_at(a.q_offsets, at.doc, a.s.q_rows);
-    const int n_queries = max(offset_at(a.q_offsets, at.doc + 1, a.s.q_rows) - q_begin, 0);
+    const int q_begin = offset_at(a.q_offsets, at.doc, a.s.q_rows), n_queries = queries_of(at.doc);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int shift = (at.end - at.begin) - n_queries;  // query i is key i + shift

@@ -152,18 +152,20 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     }
     const unsigned place = place_of_block(blockIdx.x, total);
     if (place >= total) return;
-    // heads that share keys side by side, then the stretches from the last (the longest, if causal) to the first
+    // heads that share keys side by side, then the stretches by their work
     const int in_group = place % a.s.group, part = PAGED ? place / a.s.group % a.parts : 0;
     const unsigned stretch = place / a.s.group / a.parts;
-    const int tile = (int)(a.tiles - 1 - stretch % a.tiles);
     const int kv_head = stretch / a.tiles, head = kv_head * a.s.group + in_group;
-    const Stretch at = stretch_of(tile, a.q_offsets, a.s.docs, a.s.q_rows, kRows);
+    auto keys_of = [&](int doc) {
+        if constexpr (PAGED) return keys_in_pages(a.p, doc);
+        else return max(offset_at(a.k_offsets, doc + 1, a.s.k_rows) - offset_at(a.k_offsets, doc, a.s.k_rows), 0);
+    };
+    const Stretch at = stretch_of((int)(stretch % a.tiles), a.q_offsets, a.s.docs, a.s.q_rows, a.s.causal, true, keys_of);
     if (at.first >= at.end) return;
 
     Keys<PAGED> keys;
-    int n_keys;
+    const int n_keys = keys_of(at.doc);
     if constexpr (PAGED) {
-        n_keys = keys_in_pages(a.p, at.doc);
         keys.k = a.s.k.at + kv_head * a.s.k.head;
         keys.v = a.s.v.at + kv_head * a.s.v.head;
         keys.pages = a.p.pages + at.doc * a.p.row;
@@ -173,7 +175,6 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
         keys.v_page = a.p.v_page;
     } else {
         const int begin = offset_at(a.k_offsets, at.doc, a.s.k_rows);
-        n_keys = max(offset_at(a.k_offsets, at.doc + 1, a.s.k_rows) - begin, 0);
         keys.k = a.s.k.at + begin * a.s.k.row + kv_head * a.s.k.head;
         keys.v = a.s.v.at + begin * a.s.v.row + kv_head * a.s.v.head;
     }
