@@ -175,5 +175,9 @@ def kcap_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets:
     """Attention with scores cap * K(scale * q.k / cap) over packed documents (``binding.kcap_attention``):
     q [rows, heads, dim], k and v [rows, kv_heads, dim] BFloat16, differentiable with respect to q, k and v."""
     wide = _is_wide(lut, intervals)
+    if lut is None and binding._host is not None:
+        out = binding._host.train_cap_attention(q, k, v, q_offsets, q_offsets if k_offsets is None else k_offsets, cap, scale, causal, window, wide)
+        if out is not None:
+            return out
     options = {"cap": cap, "scale": scale, "causal": causal, "window": window, "lut": lut}
     return _KCapAttention.apply(q, k, v, q_offsets, q_offsets if k_offsets is None else k_offsets, options, wide)

@@ -644,6 +644,11 @@ def kcap_attention(q, k, v, q_offsets, k_offsets=None, *, cap, scale=None, causa
     gradients.  Returns (out [q_rows, heads, dim], lse [heads, q_rows] Float32).
     """
     k_offsets = q_offsets if k_offsets is None else k_offsets
+    if stream is None and _host is not None:
+        done = _host.cap_attention(q, k, v, q_offsets, k_offsets, cap, scale, causal, window, out, lse, rest, lut,
+                                   _entry == "kcap_attention64")
+        if done is not None:
+            return done
     for t, what in ((q, "q"), (k, "k"), (v, "v")):
         _check_rows(t, what)
     docs = max(q_offsets.numel() - 1, 0)
@@ -732,6 +737,11 @@ def kcap_attention_paged(q, k_cache, v_cache, pages, lengths, q_offsets=None, *,
     token for each sequence.  Pass the columns of ``pages`` that the longest sequence needs: the work is cut by them.
     Returns out [tokens, heads, dim].
     """
+    if stream is None and _host is not None:
+        done = _host.cap_attention_paged(q, k_cache, v_cache, pages, lengths, q_offsets, cap, scale, window, out, lut,
+                                         _entry == "kcap_attention64_paged")
+        if done is not None:
+            return done
     _check_rows(q, "q")
     _check_rows(k_cache, "k_cache", 4)
     _check_rows(v_cache, "v_cache", 4)
@@ -764,6 +774,10 @@ def kcap_append(q, k, v, k_cache, v_cache, pages, lengths, q_offsets=None, *, co
     cos and sin Float32 [positions, angles]: pairs (x_i, x_{i + angles}) of the first 2 * angles values are turned, or
     (x_{2i}, x_{2i+1}) if ``interleaved``.  ``out`` may be ``q`` where that is contiguous.
     """
+    if stream is None and _host is not None:
+        done = _host.cap_append(q, k, v, k_cache, v_cache, pages, lengths, q_offsets, cos, sin, interleaved, out)
+        if done is not None:
+            return done
     for t, what in ((q, "q"), (k, "k"), (v, "v")):
         _check_rows(t, what)
     _check_rows(k_cache, "k_cache", 4)

@@ -25,6 +25,7 @@
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPFunctions.h>
 
+#include <cmath>
 #include <iterator>
 
 #include "ktanh.h"
@@ -126,17 +127,18 @@ bool ordinary_thread()
            !torch::jit::tracer::isTracing();
 }
 
-// A dense tensor on the current GPU with none of the keys of a wrapper, a conjugate or negative view, a
+// A strided tensor on the current GPU with none of the keys of a wrapper, a conjugate or negative view, a
 // quantised or sparse layout.
-bool ordinary(const Tensor &t, at::ScalarType type)
+bool ordinary_strided(const Tensor &t, at::ScalarType type)
 {
     static const uint64_t known =
         (c10::DispatchKeySet(c10::DispatchKey::CUDA) | c10::DispatchKeySet(c10::DispatchKey::ADInplaceOrView) |
          c10::getAutogradRelatedKeySetFromBackend(c10::BackendComponent::CUDABit) |
          c10::getAutocastRelatedKeySetFromBackend(c10::BackendComponent::CUDABit)).raw_repr();
-    return t.is_cuda() && (t.key_set().raw_repr() & ~known) == 0 && t.scalar_type() == type && t.is_contiguous() &&
+    return t.is_cuda() && (t.key_set().raw_repr() & ~known) == 0 && t.scalar_type() == type &&
            t.get_device() == c10::hip::current_device();
 }
+bool ordinary(const Tensor &t, at::ScalarType type) { return ordinary_strided(t, type) && t.is_contiguous(); }
 
 // The tensor behind a Python object, if it is exactly a torch.Tensor or a Parameter and ordinary().
 const Tensor *tensor_of(PyObject *o, at::ScalarType type)
@@ -511,6 +513,295 @@ PyObject *train_cell_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
+// ------------------------------------------------------------------------- attention with capped scores
+// A tensor behind a Python object with its last dimension contiguous, as the rows of attention are taken.
+const Tensor *rows_of(PyObject *o, int64_t dims)
+{
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const Tensor &t = THPVariable_Unpack(o);
+    if (!t.defined() || !ordinary_strided(t, kBf16) || t.dim() != dims || (t.size(-1) > 1 && t.stride(-1) != 1)) return nullptr;
+    for (const int64_t step : t.strides())
+        if (step < 0) return nullptr;
+    return &t;
+}
+
+const Tensor *int32_of(PyObject *o, int64_t count)
+{
+    const Tensor *t = tensor_of(o, at::kInt);
+    return t != nullptr && t->dim() == 1 && t->numel() == count ? t : nullptr;
+}
+
+// A given output, or null in *t for None; false if it is not one.
+bool output_of(PyObject *o, at::ScalarType type, at::IntArrayRef sizes, const Tensor **t)
+{
+    *t = nullptr;
+    if (o == Py_None) return true;
+    *t = tensor_of(o, type);
+    return *t != nullptr && (*t)->sizes() == sizes;
+}
+
+bool number_of(PyObject *o, double *v)
+{
+    if (!PyFloat_CheckExact(o) && !PyLong_CheckExact(o)) return false;
+    *v = PyFloat_AsDouble(o);
+    if (*v == -1.0 && PyErr_Occurred() != nullptr) {
+        PyErr_Clear();
+        return false;
+    }
+    return true;
+}
+
+// The stride of a dimension of a single element means nothing.
+size_t step(const Tensor &t, int64_t dim) { return t.size(dim) > 1 ? (size_t)t.stride(dim) : 0; }
+
+struct CapOptions {
+    double cap = 0.0, scale = 0.0;
+    bool causal = true;
+    size_t window = 0;
+};
+
+// cap, scale (None: dim ** -0.5), window
+bool options_of(PyObject *cap, PyObject *scale, PyObject *window, int64_t dim, CapOptions *out)
+{
+    if (dim <= 0 || !number_of(cap, &out->cap) || !PyLong_CheckExact(window)) return false;
+    if (scale == Py_None) out->scale = std::pow((double)dim, -0.5);
+    else if (!number_of(scale, &out->scale)) return false;
+    int overflow = 0;
+    const long long w = PyLong_AsLongLongAndOverflow(window, &overflow);
+    out->window = (size_t)w;
+    return overflow == 0 && w >= 0;
+}
+
+bool cap_shape(const Tensor &q, const Tensor &k, const Tensor &v, int64_t docs, int64_t k_rows, const CapOptions &options, kcap_shape_t *s)
+{
+    const int64_t heads = q.size(1), kv_heads = k.size(-2);
+    if (k.sizes() != v.sizes() || k.size(-1) != q.size(2) || kv_heads == 0 || heads % kv_heads != 0) return false;
+    *s = kcap_shape_t{(size_t)docs, (size_t)q.size(0), (size_t)k_rows, (size_t)heads, (size_t)kv_heads, (size_t)q.size(2), step(q, 0), step(q, 1),
+                      step(k, -3), step(k, -2), step(v, -3), step(v, -2), options.scale, options.cap, options.window, options.causal};
+    return true;
+}
+
+const uint16_t *in(const Tensor &t) { return static_cast<const uint16_t *>(t.const_data_ptr()); }
+uint16_t *out(const Tensor &t) { return static_cast<uint16_t *>(t.mutable_data_ptr()); }
+const int32_t *ints(const Tensor &t) { return static_cast<const int32_t *>(t.const_data_ptr()); }
+
+const char *cap_name(bool wide) { return wide ? "kcap_attention64" : "kcap_attention"; }
+const char *cap_backward_name(bool wide) { return wide ? "kcap_attention64_backward" : "kcap_attention_backward"; }
+const char *cap_paged_name(bool wide) { return wide ? "kcap_attention64_paged" : "kcap_attention_paged"; }
+
+ktanh_status_t cap_entry(bool wide, const kcap_shape_t &s, const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &q_offsets,
+                         const Tensor &k_offsets, const Tensor &o, const Tensor &rest, const Tensor &lse, const void *lut)
+{
+    uint16_t *r = rest.defined() ? out(rest) : nullptr;
+    auto *sums = static_cast<float *>(lse.mutable_data_ptr());
+    return wide ? kcap_attention64(&s, in(q), in(k), in(v), ints(q_offsets), ints(k_offsets), out(o), r, sums, static_cast<const ktanh_lut64_t *>(lut), current_stream())
+                : kcap_attention(&s, in(q), in(k), in(v), ints(q_offsets), ints(k_offsets), out(o), r, sums, static_cast<const ktanh_lut_t *>(lut), current_stream());
+}
+
+// cap_attention(q, k, v, q_offsets, k_offsets, cap, scale, causal, window, out, lse, rest, lut, wide) -> (out, lse), or None
+PyObject *cap_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (nargs != 14 || !ordinary_thread()) Py_RETURN_NONE;
+    const bool wide = args[13] == Py_True;
+    const Tensor *q = rows_of(args[0], 3), *k = rows_of(args[1], 3), *v = rows_of(args[2], 3), *q_offsets = tensor_of(args[3], at::kInt);
+    if (q == nullptr || k == nullptr || v == nullptr || q_offsets == nullptr || q_offsets->dim() != 1 || q_offsets->numel() < 1) Py_RETURN_NONE;
+    const int64_t docs = q_offsets->numel() - 1;
+    const Tensor *k_offsets = int32_of(args[4], docs + 1);
+    CapOptions options;
+    options.causal = args[7] == Py_True;
+    kcap_shape_t shape;
+    if (k_offsets == nullptr || (args[7] != Py_True && args[7] != Py_False) || !options_of(args[5], args[6], args[8], q->size(2), &options) ||
+        !cap_shape(*q, *k, *v, docs, k->size(0), options, &shape))
+        Py_RETURN_NONE;
+    const Tensor *o_given, *lse_given, *rest_given;
+    if (!output_of(args[9], kBf16, q->sizes(), &o_given) || !output_of(args[10], kF32, {q->size(1), q->size(0)}, &lse_given) ||
+        !output_of(args[11], kBf16, q->sizes(), &rest_given))
+        Py_RETURN_NONE;
+    const TableArgument lut(args[12], wide ? TABLE64 : TABLE32);
+    if (!lut.good()) Py_RETURN_NONE;
+    Tensor o, lse;
+    {
+        pybind11::gil_scoped_release no_gil;
+        o = o_given != nullptr ? *o_given : at::empty(q->sizes(), q->options());
+        lse = lse_given != nullptr ? *lse_given : at::empty({q->size(1), q->size(0)}, q->options().dtype(kF32));
+        check_status(cap_entry(wide, shape, *q, *k, *v, *q_offsets, *k_offsets, o, rest_given != nullptr ? *rest_given : Tensor(), lse, lut.pointer()), cap_name(wide));
+    }
+    return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(o)), THPVariable_Wrap(std::move(lse)));
+    END_HANDLE_TH_ERRORS
+}
+
+bool cap_pages(const Tensor &k_cache, const Tensor &v_cache, const Tensor &pages, int64_t docs, kcap_pages_t *p)
+{
+    if (k_cache.sizes() != v_cache.sizes() || pages.dim() != 2 || pages.size(0) != docs || (pages.size(1) > 1 && pages.stride(1) != 1) || pages.stride(0) < 0)
+        return false;
+    *p = kcap_pages_t{(size_t)k_cache.size(1), (size_t)k_cache.size(0), (size_t)pages.size(1), step(pages, 0), step(k_cache, 0), step(k_cache, 1),
+                      step(k_cache, 2), step(v_cache, 0), step(v_cache, 1), step(v_cache, 2)};
+    return true;
+}
+
+const Tensor *pages_of(PyObject *o)
+{
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const Tensor &t = THPVariable_Unpack(o);
+    return t.defined() && ordinary_strided(t, at::kInt) ? &t : nullptr;
+}
+
+// q_offsets [docs + 1], or None in *t: one row for each
+bool offsets_of(PyObject *o, const Tensor &q, const Tensor **t, int64_t *docs)
+{
+    *t = nullptr;
+    *docs = q.size(0);
+    if (o == Py_None) return true;
+    *t = tensor_of(o, at::kInt);
+    if (*t == nullptr || (*t)->dim() != 1 || (*t)->numel() < 1) return false;
+    *docs = (*t)->numel() - 1;
+    return true;
+}
+
+// cap_attention_paged(q, k_cache, v_cache, pages, lengths, q_offsets, cap, scale, window, out, lut, wide) -> out, or None
+PyObject *cap_paged_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (nargs != 12 || !ordinary_thread()) Py_RETURN_NONE;
+    const bool wide = args[11] == Py_True;
+    const Tensor *q = rows_of(args[0], 3), *k = rows_of(args[1], 4), *v = rows_of(args[2], 4), *pages = pages_of(args[3]), *q_offsets;
+    int64_t docs;
+    if (q == nullptr || k == nullptr || v == nullptr || pages == nullptr || !offsets_of(args[5], *q, &q_offsets, &docs)) Py_RETURN_NONE;
+    const Tensor *lengths = int32_of(args[4], docs), *given;
+    CapOptions options;
+    kcap_shape_t shape;
+    kcap_pages_t cache;
+    if (lengths == nullptr || !options_of(args[6], args[7], args[8], q->size(2), &options) || !cap_shape(*q, *k, *v, docs, 0, options, &shape) ||
+        !cap_pages(*k, *v, *pages, docs, &cache) || !output_of(args[9], kBf16, q->sizes(), &given))
+        Py_RETURN_NONE;
+    const TableArgument lut(args[10], wide ? TABLE64 : TABLE32);
+    if (!lut.good()) Py_RETURN_NONE;
+    Tensor o;
+    {
+        pybind11::gil_scoped_release no_gil;
+        o = given != nullptr ? *given : at::empty(q->sizes(), q->options());
+        const size_t size = kcap_attention_paged_workspace(&shape, &cache, q_offsets == nullptr);
+        const Tensor workspace = size != 0 ? at::empty({(int64_t)size}, q->options().dtype(at::kByte)) : Tensor();
+        void *work = size != 0 ? workspace.mutable_data_ptr() : nullptr;
+        const int32_t *offsets = q_offsets != nullptr ? ints(*q_offsets) : nullptr;
+        check_status(wide ? kcap_attention64_paged(&shape, &cache, in(*q), in(*k), in(*v), ints(*pages), ints(*lengths), offsets, out(o), work,
+                                                   static_cast<const ktanh_lut64_t *>(lut.pointer()), current_stream())
+                          : kcap_attention_paged(&shape, &cache, in(*q), in(*k), in(*v), ints(*pages), ints(*lengths), offsets, out(o), work,
+                                                 static_cast<const ktanh_lut_t *>(lut.pointer()), current_stream()),
+                     cap_paged_name(wide));
+    }
+    return THPVariable_Wrap(std::move(o));
+    END_HANDLE_TH_ERRORS
+}
+
+// cap_append(q, k, v, k_cache, v_cache, pages, lengths, q_offsets, cos, sin, interleaved, out) -> out, or None
+PyObject *cap_append_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (nargs != 12 || !ordinary_thread()) Py_RETURN_NONE;
+    const Tensor *q = rows_of(args[0], 3), *k = rows_of(args[1], 3), *v = rows_of(args[2], 3), *k_cache = rows_of(args[3], 4),
+                 *v_cache = rows_of(args[4], 4), *pages = pages_of(args[5]), *cos = tensor_of(args[8], kF32), *sin = tensor_of(args[9], kF32), *q_offsets;
+    int64_t docs;
+    if (q == nullptr || k == nullptr || v == nullptr || k_cache == nullptr || v_cache == nullptr || pages == nullptr || cos == nullptr || sin == nullptr ||
+        !offsets_of(args[7], *q, &q_offsets, &docs))
+        Py_RETURN_NONE;
+    const Tensor *lengths = int32_of(args[6], docs), *given;
+    kcap_shape_t shape;
+    kcap_pages_t cache;
+    CapOptions options;
+    options.cap = options.scale = 1.0;
+    if (lengths == nullptr || k->size(0) != q->size(0) || k_cache->size(2) != k->size(1) || k_cache->size(3) != k->size(2) || cos->dim() != 2 ||
+        cos->sizes() != sin->sizes() || (args[10] != Py_True && args[10] != Py_False) || !cap_shape(*q, *k, *v, docs, 0, options, &shape) ||
+        !cap_pages(*k_cache, *v_cache, *pages, docs, &cache) || !output_of(args[11], kBf16, q->sizes(), &given))
+        Py_RETURN_NONE;
+    Tensor turned;
+    {
+        pybind11::gil_scoped_release no_gil;
+        turned = given != nullptr ? *given : at::empty(q->sizes(), q->options());
+        check_status(kcap_append(&shape, &cache, in(*q), in(*k), in(*v), out(turned), out(*k_cache), out(*v_cache), ints(*pages), ints(*lengths),
+                                 q_offsets != nullptr ? ints(*q_offsets) : nullptr, static_cast<const float *>(cos->const_data_ptr()),
+                                 static_cast<const float *>(sin->const_data_ptr()), (size_t)cos->size(0), (size_t)cos->size(1), args[10] == Py_True,
+                                 current_stream()),
+                     "kcap_append");
+    }
+    return THPVariable_Wrap(std::move(turned));
+    END_HANDLE_TH_ERRORS
+}
+
+struct CapAttention : public torch::autograd::Function<CapAttention> {
+    static Tensor forward(AutogradContext *ctx, const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &q_offsets, const Tensor &k_offsets,
+                          double cap, double scale, bool causal, int64_t window, bool wide)
+    {
+        kcap_shape_t shape;
+        CapOptions options{cap, scale, causal, (size_t)window};
+        TORCH_CHECK_VALUE(cap_shape(q, k, v, q_offsets.numel() - 1, k.size(0), options, &shape), "q, k and v do not agree in heads or dim");
+        const Tensor o = at::empty(q.sizes(), q.options()), rest = at::empty(q.sizes(), q.options());
+        const Tensor lse = at::empty({q.size(1), q.size(0)}, q.options().dtype(kF32));
+        check_status(cap_entry(wide, shape, q, k, v, q_offsets, k_offsets, o, rest, lse, nullptr), cap_name(wide));
+        ctx->save_for_backward({q, k, v, q_offsets, k_offsets, o, rest, lse});
+        ctx->saved_data["cap"] = cap;
+        ctx->saved_data["scale"] = scale;
+        ctx->saved_data["causal"] = causal;
+        ctx->saved_data["window"] = window;
+        ctx->saved_data["wide"] = wide;
+        return o;
+    }
+    static variable_list backward(AutogradContext *ctx, const variable_list &grads)
+    {
+        const variable_list saved = ctx->get_saved_variables();
+        const Tensor &q = saved[0], &k = saved[1], &v = saved[2];
+        const bool wide = ctx->saved_data["wide"].toBool();
+        for (const Tensor *t : {&q, &k, &v, &grads[0]}) {
+            TORCH_CHECK(t->defined() && ordinary_strided(*t, kBf16) && t->dim() == 3, "a saved tensor or the gradient is not an ordinary BFloat16 tensor of rows");
+        }
+        for (const size_t i : {(size_t)3, (size_t)4}) checked(saved[i], at::kInt, "offsets");
+        for (const size_t i : {(size_t)5, (size_t)6}) checked(saved[i], kBf16, "the saved output");
+        checked(saved[7], kF32, "the saved sums");
+        Tensor d_o = grads[0];
+        if (d_o.stride(2) != 1 || d_o.stride(0) % 8 != 0 || d_o.stride(1) % 8 != 0 || reinterpret_cast<uintptr_t>(d_o.const_data_ptr()) % 16 != 0)
+            d_o = d_o.contiguous();  // also the expanded gradient of a sum
+        kcap_shape_t shape;
+        const CapOptions options{ctx->saved_data["cap"].toDouble(), ctx->saved_data["scale"].toDouble(), ctx->saved_data["causal"].toBool(),
+                                 (size_t)ctx->saved_data["window"].toInt()};
+        TORCH_CHECK_VALUE(cap_shape(q, k, v, saved[3].numel() - 1, k.size(0), options, &shape) && d_o.sizes() == q.sizes() && saved[5].sizes() == q.sizes() &&
+                          saved[6].sizes() == q.sizes() && saved[3].numel() == saved[4].numel() && saved[7].numel() == q.size(0) * q.size(1),
+                          "the saved tensors and the gradient do not agree");
+        const Tensor dq = at::empty(q.sizes(), q.options()), dk = at::empty(k.sizes(), k.options()), dv = at::empty(v.sizes(), v.options());
+        const Tensor workspace = at::empty({(int64_t)kcap_attention_backward_workspace(&shape)}, q.options().dtype(at::kByte));
+        const auto *sums = static_cast<const float *>(saved[7].const_data_ptr());
+        check_status(wide ? kcap_attention64_backward(&shape, in(d_o), step(d_o, 0), step(d_o, 1), in(q), in(k), in(v), in(saved[5]), in(saved[6]), sums,
+                                                      ints(saved[3]), ints(saved[4]), out(dq), out(dk), out(dv), workspace.mutable_data_ptr(), nullptr, current_stream())
+                          : kcap_attention_backward(&shape, in(d_o), step(d_o, 0), step(d_o, 1), in(q), in(k), in(v), in(saved[5]), in(saved[6]), sums,
+                                                    ints(saved[3]), ints(saved[4]), out(dq), out(dk), out(dv), workspace.mutable_data_ptr(), nullptr, current_stream()),
+                     cap_backward_name(wide));
+        return {dq, dk, dv, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+    }
+};
+
+// train_cap_attention(q, k, v, q_offsets, k_offsets, cap, scale, causal, window, wide) -> out, or None
+PyObject *train_cap_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (nargs != 10 || !ordinary_thread()) Py_RETURN_NONE;
+    const Tensor *q = rows_of(args[0], 3), *k = rows_of(args[1], 3), *v = rows_of(args[2], 3), *q_offsets = tensor_of(args[3], at::kInt);
+    if (q == nullptr || k == nullptr || v == nullptr || q_offsets == nullptr || q_offsets->dim() != 1 || q_offsets->numel() < 1) Py_RETURN_NONE;
+    const Tensor *k_offsets = int32_of(args[4], q_offsets->numel());
+    CapOptions options;
+    kcap_shape_t shape;
+    if (k_offsets == nullptr || (args[7] != Py_True && args[7] != Py_False) || !options_of(args[5], args[6], args[8], q->size(2), &options) ||
+        !cap_shape(*q, *k, *v, q_offsets->numel() - 1, k->size(0), options, &shape) || !differentiable(*q) || !differentiable(*k) || !differentiable(*v))
+        Py_RETURN_NONE;
+    if (!at::GradMode::is_enabled() || !(q->requires_grad() || k->requires_grad() || v->requires_grad())) Py_RETURN_NONE;
+    Tensor o;
+    {
+        pybind11::gil_scoped_release no_gil;
+        o = CapAttention::apply(*q, *k, *v, *q_offsets, *k_offsets, options.cap, options.scale, args[7] == Py_True, (int64_t)options.window, args[9] == Py_True);
+    }
+    return THPVariable_Wrap(std::move(o));
+    END_HANDLE_TH_ERRORS
+}
+
 // ------------------------------------------------------------------------------------------ module
 // setup(KtanhLut, KtanhLut64, KtanhError): the classes of binding.py
 PyObject *setup_call(PyObject *, PyObject *args)
@@ -534,6 +825,10 @@ PyMethodDef kMethods[] = {
     {"cell_backward", as_method(cell_backward_call), METH_FASTCALL, nullptr},
     {"train", as_method(train_call), METH_FASTCALL, nullptr},
     {"train_cell", as_method(train_cell_call), METH_FASTCALL, nullptr},
+    {"cap_attention", as_method(cap_call), METH_FASTCALL, nullptr},
+    {"cap_attention_paged", as_method(cap_paged_call), METH_FASTCALL, nullptr},
+    {"cap_append", as_method(cap_append_call), METH_FASTCALL, nullptr},
+    {"train_cap_attention", as_method(train_cap_call), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyMethodDef g_unary_defs[std::size(kUnary)], g_binary_defs[std::size(kBinary)];

@@ -495,6 +495,73 @@ def test_append_in_place_one_token_each_and_tokens_without_a_place(gpu):
     assert turned[[1, 4]].isnan().all() and not turned[[0, 2, 3]].isnan().any()
 
 
+# ------------------------------------------------------------------------------------- the host path
+
+
+def _both_paths(binding, call):
+    """What a call gives through the C++ host path and through the Python code."""
+    assert binding._host is not None
+    patch = pytest.MonkeyPatch()
+    taken = call()
+    patch.setattr(binding, "_host", None)
+    patch.setattr(binding, "_calls", {})
+    try:
+        return taken, call()
+    finally:
+        patch.undo()
+
+
+def test_host_path_and_python_code_give_the_same(gpu):
+    binding, autograd, torch = gpu
+    (q, k, v), _ = _inputs(torch, 31, 90, 90, 4, 2, 64)
+    do = _bf16(torch, np.random.default_rng(32).standard_normal((90, 4, 64)))
+    at, _ = _offsets(torch, [30, 60])
+    (kc, vc, pages), _ = _cache(torch, 33, [300, 40], 16, 2, 64)
+    n = torch.tensor([300, 40], dtype=torch.int32, device="cuda")
+    two = torch.tensor([0, 5, 6], dtype=torch.int32, device="cuda")
+    cos, sin = torch.rand((400, 32), device="cuda"), torch.rand((400, 32), device="cuda")
+    fused = torch.cat([q, k, v], 1)
+    rest = torch.empty_like(q)
+
+    def train(**options):
+        leaves = [t.detach().clone().requires_grad_() for t in (q, k, v)]
+        o = autograd.kcap_attention(*leaves, at, **options)
+        return (o, *torch.autograd.grad(o, leaves, do))
+    lut32, lut64 = binding.ktanh_fit_lut_bmin0(), binding.ktanh_fit_lut64()
+    calls = [
+        lambda: binding.kcap_attention(q, k, v, at, cap=50.0),
+        lambda: binding.kcap_attention(q, k, v, at, at, cap=30, scale=0.25, causal=False, window=9, lut=lut32),
+        lambda: (*binding.kcap_attention64(q, k, v, at, cap=50.0, lut=lut64, out=torch.empty_like(q), rest=rest), rest.clone()),
+        lambda: binding.kcap_attention(fused[:, :4], fused[:, 4:6], fused[:, 6:], at, cap=50.0),
+        lambda: (binding.kcap_attention_paged(q[:2], kc, vc, pages, n, cap=50.0),),
+        lambda: (binding.kcap_attention64_paged(q[:6], kc, vc, pages, n, two, cap=50.0, scale=0.1, window=33),),
+        lambda: (binding.kcap_append(q[:2], k[:2], v[:2], kc, vc, pages, n - 1, cos=cos, sin=sin), kc.clone(), vc.clone()),
+        lambda: (binding.kcap_append(q[:6], k[:6], v[:6], kc, vc, pages, n - 9, two, cos=cos, sin=sin, interleaved=True), kc.clone(), vc.clone()),
+        lambda: train(cap=50.0), lambda: train(cap=30.0, scale=0.3, causal=False, window=20, intervals=64),
+    ]
+    for i, call in enumerate(calls):
+        fast, slow = _both_paths(binding, call)
+        assert len(fast) == len(slow)
+        for a, b in zip(fast, slow):
+            assert a.dtype == b.dtype and a.shape == b.shape and a.stride() == b.stride() and a.requires_grad == b.requires_grad, i
+            assert torch.equal(a.detach().view(torch.int16), b.detach().view(torch.int16)), i
+    host = binding._host
+    assert host.cap_attention(q, k, v, at, at, 50.0, None, True, 0, None, None, None, None, False) is not None
+    assert host.cap_attention_paged(q[:2], kc, vc, pages, n, None, 50.0, None, 0, None, None, True) is not None
+    assert host.cap_append(q[:2], k[:2], v[:2], kc, vc, pages, n - 1, None, cos, sin, False, None) is not None
+    leaf = q.clone().requires_grad_()
+    assert host.train_cap_attention(leaf, k, v, at, at, 50.0, None, True, 0, False) is not None
+    # and what is not ordinary is left to the Python code
+    assert host.cap_attention(q.float(), k, v, at, at, 50.0, None, True, 0, None, None, None, None, False) is None
+    assert host.cap_attention(q, k, v, at, at, "50", None, True, 0, None, None, None, None, False) is None
+    assert host.cap_attention(q, k, v, at, at[:1], 50.0, None, True, 0, None, None, None, None, False) is None
+    assert host.cap_attention(q[:, :3], k, v, at, at, 50.0, None, True, 0, None, None, None, None, False) is None
+    assert host.train_cap_attention(q, k, v, at, at, 50.0, None, True, 0, False) is None
+    with pytest.raises(binding.KtanhError) as err:
+        binding.kcap_attention(q, k, v, at, cap=80.0)
+    assert err.value.status == 4
+
+
 # ----------------------------------------------------------------------------------------- refusals
 
 
