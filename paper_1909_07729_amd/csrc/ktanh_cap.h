@@ -76,10 +76,10 @@ __device__ __forceinline__ bf16x8 pack8(const float *v, float *sum)
 
 // ------------------------------------------------------------------------------------------ the cap
 // lines[i], i = low three exponent bits << 4 | high four mantissa bits, times `unit`.
+template <int THREADS = kThreads>
 __device__ __forceinline__ void spread_lines(f32x2 *lines, const KtCapPack &pack, float unit)
 {
-    const int i = threadIdx.x;
-    if (i < 128) {
+    for (int i = threadIdx.x; i < 128; i += THREADS) {
         const int e = i >> 4, slot = i & 63;
         const float a = e == 4 ? 1.0f : (e >= 1 && e <= 3) ? 0.0f : pack.a[slot];
         const float b = e == 4 ? 0.0f : (e >= 1 && e <= 3) ? 1.0f : pack.b[slot];

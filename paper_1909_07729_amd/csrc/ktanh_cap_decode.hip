@@ -1,112 +1,188 @@
 // libktanh: capped attention over a paged cache, one query for each sequence.
 //
-// What it costs is reading the keys and values once.  The keys of a sequence and key/value head are cut into spans, a block
-// for each; a wavefront takes every fourth tile of 32 keys for up to 32 query heads that share them, with the tile in LDS of its own
-// (no barrier in the loop) and the next one on its way in registers.  Weights need no maximum (|y| <= cap),
-// so wavefronts and spans are joined by adding numerators and denominators.
+// What it costs is reading the keys and values once.  All tiles of 32 keys of all sequences and key/value heads form one row, which is
+// cut into equal shares, one for each wavefront that the chip holds: however the lengths differ, all are done at the same time,
+// and none waits for a first load but at its start.  A wavefront works for up to 32 query heads that share keys, with the tile in LDS of its
+// own (no barriers), the next one on its way in registers and the pages of the one behind it looked up.  Weights need no
+// maximum (|y| <= cap), so what several wavefronts have of a sequence is joined by adding numerators and denominators; a
+// sequence within one share is finished there.
 #include "ktanh_cap_args.h"
 
 using namespace ktanh_cap;
 
 namespace {
 
-constexpr int kKeys = 32;  // of a wavefront's tile
+constexpr int kKeys = 32;  // of a tile
 
 struct DecodeArgs {
     CapShape s;
     CapPages p;
     uint16_t *o;
-    float *sums, *parts;  // [docs][spans][heads], [docs][spans][heads][dim]: NULL where one span holds all keys
-    int span, spans, row_blocks;
+    // what a wavefront has of the first and of the last sequence of its share, if others have the rest: [shares][2][rows] and [..][rows][dim]
+    float *sums, *parts;
+    int shares, rows, row_blocks, slices;
 };
 
 __device__ __forceinline__ int first_key(const CapShape &s, int n_keys) { return s.window > 0 ? max(0, n_keys - s.window) : 0; }
 
+__device__ __forceinline__ int tiles_of(const DecodeArgs &a, int seq)
+{
+    const int n_keys = keys_in_pages(a.p, seq);
+    return (n_keys + kKeys - 1) / kKeys - first_key(a.s, n_keys) / kKeys;
+}
+
+// The row of tiles: sequence by sequence, in each head by head (or 32 heads by 32).
+struct Row {
+    int total, share;  // tiles in all, and of a wavefront
+    int seq, before;   // the sequence that holds the first tile of share `at_share` (or, from 0 on, `given`), and the tiles before it
+    __device__ __forceinline__ Row(const DecodeArgs &a, int at_share, int given) : total(0), share(1), seq(max(given, 0)), before(0)
+    {
+        const int heads = a.s.kv_heads * a.row_blocks, lane = (int)(threadIdx.x & 63);
+        int count = 0, bits = 0;  // tiles of the sequences that the lanes look at, for one head
+        auto look_at = [&](int base) {
+            count = base + lane < a.s.docs ? tiles_of(a, base + lane) : 0;
+            for (bits = 0; bits < 31 && __ballot(count >> bits) != 0;) ++bits;
+        };
+        for (int base = 0; base < a.s.docs; base += 64) {
+            look_at(base);
+            total += lanes_sum(count, bits) * heads;
+        }
+        share = max((total + a.shares - 1) / a.shares, 1);
+        const int at = at_share * share;
+        for (int base = 0, sum = 0; base < a.s.docs; base += 64) {
+            if (a.s.docs > 64) look_at(base);
+            const int mine = sum + lanes_before(count, bits) * heads;
+            const unsigned long long here = __ballot(given >= 0 ? base + lane == given : mine <= at && at < mine + count * heads);
+            if (here != 0) {
+                const int at_lane = __builtin_ctzll(here);
+                seq = base + at_lane;
+                before = __builtin_amdgcn_readlane(mine, at_lane);
+                break;
+            }
+            sum += lanes_sum(count, bits) * heads;
+        }
+    }
+};
+
+// A tile's place: scalars.
+struct Place {
+    int seq, head, j0, n_keys, first;  // head counts key/value heads by blocks of 32 query heads
+
+    __device__ __forceinline__ void enter(const DecodeArgs &a)
+    {
+        n_keys = __builtin_amdgcn_readfirstlane(keys_in_pages(a.p, seq));
+        first = first_key(a.s, n_keys);
+        j0 = first & ~(kKeys - 1);
+    }
+    __device__ __forceinline__ void advance(const DecodeArgs &a)
+    {
+        j0 += kKeys;
+        if (j0 < n_keys) return;
+        j0 = first & ~(kKeys - 1);
+        if (++head < a.s.kv_heads * a.row_blocks) return;
+        head = 0;
+        do {
+            ++seq;
+            enter(a);
+        } while (n_keys == 0 && seq + 1 < a.s.docs);
+    }
+};
+
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void cap_decode_kernel(DecodeArgs a, KtCapPack pack)
+__global__ __launch_bounds__(64, 2) void cap_decode_kernel(DecodeArgs a, KtCapPack pack)
 {
     constexpr int kBytes = kKeys * kPitch<D>, kSteps = D / 16, kBlocks = D / 32;
     constexpr int kChunks = D / 8, kLoads = kKeys * kChunks / 64;  // 16-byte loads of a lane for each of K and V
     struct Shared {
-        f32x2 lines[128];                 // first: the offset of a line is its address
-        char tiles[kWaves][2 * kBytes];   // keys | values; at the end 32 x D numerators
-        float sums[kWaves][32];
+        f32x2 lines[128];  // first: the offset of a line is its address
+        char k[kBytes], v[kBytes];
     };
     __shared__ __align__(16) Shared shared;
     f32x2 *lines = shared.lines;
 
-    // heads and sequences first: the empty spans behind short sequences come last
-    const int row_block = (int)(blockIdx.x % a.row_blocks), kv_head = (int)(blockIdx.x / a.row_blocks % a.s.kv_heads);
-    const int seq = (int)(blockIdx.x / a.row_blocks / a.s.kv_heads % a.s.docs), span = (int)(blockIdx.x / a.row_blocks / a.s.kv_heads / a.s.docs);
-    const int n_keys = keys_in_pages(a.p, seq), begin = max(first_key(a.s, n_keys), span * a.span), end = min(n_keys, (span + 1) * a.span);
-    if (begin >= end && a.parts != nullptr) return;
-
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int head0 = kv_head * a.s.group + 32 * row_block, heads = min(32, a.s.group - 32 * row_block);
-    const int *pages = a.p.pages + seq * a.p.row;
-    const uint16_t *k = a.s.k.at + kv_head * a.s.k.head, *v = a.s.v.at + kv_head * a.s.v.head;
-    char *k_tile = shared.tiles[wave], *v_tile = shared.tiles[wave] + kBytes;
-    spread_lines(lines, pack, a.s.cap * kLog2e);
-
-    bf16x8 q[kSteps];
+    const int lane = threadIdx.x;
+    const Row all(a, (int)blockIdx.x, -1);
+    const int start = (int)blockIdx.x * all.share, end = min(all.total, start + all.share);
+    if (start >= end) return;
+    Place now;
+    now.seq = __builtin_amdgcn_readfirstlane(all.seq);
+    now.enter(a);
     {
-        const uint16_t *from = a.s.q.at + seq * a.s.q.row + (head0 + min(lane & 31, heads - 1)) * a.s.q.head + 8 * (lane >> 5);
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) q[i] = *reinterpret_cast<const bf16x8 *>(from + 16 * i);
+        const int tiles = (now.n_keys + kKeys - 1) / kKeys - now.first / kKeys, in_seq = start - __builtin_amdgcn_readfirstlane(all.before);
+        now.head = in_seq / tiles;
+        now.j0 += in_seq % tiles * kKeys;
     }
-    f32x16 o[kBlocks];
-#pragma unroll
-    for (int c = 0; c < kBlocks; ++c) o[c] = f32x16{0};
-    float sum = 0.0f;
+    spread_lines<64>(lines, pack, a.s.cap * kLog2e);
 
-    // The page of key j0 + (lane & 31): loaded two tiles ahead, handed to the lanes that load the row one tile ahead.
-    auto page_for = [&](int j0) { return min(max(pages[min(j0 + (lane & 31), n_keys - 1) >> a.p.shift], 0), a.p.count - 1); };
+    // The page of key j0 + (lane & 31), handed to the lanes that load the row one tile later.
+    auto page_for = [&](const Place &at) {
+        return min(max(a.p.pages[at.seq * a.p.row + (min(at.j0 + (lane & 31), at.n_keys - 1) >> a.p.shift)], 0), a.p.count - 1);
+    };
     u32x4 next_k[kLoads], next_v[kLoads];
-    auto load = [&](int j0, int page) {
+    auto load = [&](const Place &at, int page) {
+        const int kv_head = at.head / a.row_blocks;
+        const uint16_t *k = a.s.k.at + kv_head * a.s.k.head, *v = a.s.v.at + kv_head * a.s.v.head;
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
-            const int row = lane / kChunks + n * (64 / kChunks), j = min(j0 + row, n_keys - 1);
+            const int row = lane / kChunks + n * (64 / kChunks), j = min(at.j0 + row, at.n_keys - 1);
             const long long in_page = j & ((1 << a.p.shift) - 1), p = __shfl(page, row);
             // read once: with the hint a batch takes 200 us instead of 222
             next_k[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(k + p * a.p.k_page + in_page * a.s.k.row + 8 * (lane % kChunks)));
             next_v[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(v + p * a.p.v_page + in_page * a.s.v.row + 8 * (lane % kChunks)));
         }
     };
-    constexpr int kStride = kWaves * kKeys;
-    int j0 = (begin & ~(kKeys - 1)) + wave * kKeys;
-    int page = 0;
-    if (j0 < end) {
-        load(j0, page_for(j0));
-        page = page_for(j0 + kStride);
-    }
-    __syncthreads();  // lines
-    for (; j0 < end; j0 += kStride) {
+    bf16x8 q[kSteps];
+    f32x16 o[kBlocks];
+    float sum = 0.0f;
+    int head0 = 0, heads = 0;  // query heads of the present sequence and key/value head
+    auto begin = [&](const Place &at) {
+        const int kv_head = at.head / a.row_blocks, row_block = at.head % a.row_blocks;
+        head0 = kv_head * a.s.group + 32 * row_block;
+        heads = min(32, a.s.group - 32 * row_block);
+        const uint16_t *from = a.s.q.at + at.seq * a.s.q.row + (head0 + min(lane & 31, heads - 1)) * a.s.q.head + 8 * (lane >> 5);
 #pragma unroll
-        for (int n = 0; n < kLoads; ++n) {
-            const int row = lane / kChunks + n * (64 / kChunks), chunk = lane % kChunks;
-            const bool seen = j0 + row >= begin && j0 + row < end;  // a value that is not seen may be an infinity
-            *reinterpret_cast<u32x4 *>(k_tile + chunk_at<D>(row, chunk)) = next_k[n];
-            *reinterpret_cast<u32x4 *>(v_tile + chunk_at<D>(row, chunk)) = seen ? next_v[n] : u32x4{0, 0, 0, 0};
+        for (int i = 0; i < kSteps; ++i) q[i] = *reinterpret_cast<const bf16x8 *>(from + 16 * i);
+#pragma unroll
+        for (int c = 0; c < kBlocks; ++c) o[c] = f32x16{0};
+        sum = 0.0f;
+    };
+
+    Place next = now, pages = now;
+    int page = page_for(now);
+    load(now, page);
+    if (start + 1 < end) {
+        next.advance(a);
+        page = page_for(next);
+        pages = next;
+    }
+    begin(now);
+    int segment = start;  // the first tile of the present sequence and head in this share
+    __syncthreads();      // lines
+    for (int n = start; n < end; ++n) {
+        const int j0 = now.j0;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = lane / kChunks + i * (64 / kChunks), chunk = lane % kChunks;
+            const bool seen = j0 + row >= now.first && j0 + row < now.n_keys;  // a value that is not seen may be an infinity
+            *reinterpret_cast<u32x4 *>(shared.k + chunk_at<D>(row, chunk)) = next_k[i];
+            *reinterpret_cast<u32x4 *>(shared.v + chunk_at<D>(row, chunk)) = seen ? next_v[i] : u32x4{0, 0, 0, 0};
         }
-        if (j0 + kStride < end) {
-            load(j0 + kStride, page);
-            page = page_for(j0 + 2 * kStride);
+        if (n + 1 < end) {
+            load(next, page);
+            if (n + 2 < end) {
+                pages.advance(a);
+                page = page_for(pages);
+            }
         }
         // the tile is this wavefront's own: its LDS accesses are served in order
         __builtin_amdgcn_wave_barrier();
         f32x16 s = f32x16{0};
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) s = mfma(rows_of<D>(k_tile, 0, i), q[i], s);
+        for (int i = 0; i < kSteps; ++i) s = mfma(rows_of<D>(shared.k, 0, i), q[i], s);
         float p[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(capped(s[r] * a.s.to_x, lines));
-        if (j0 < begin || j0 + kKeys > end) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int j = j0 + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5);
-                p[r] = j >= begin && j < end ? p[r] : 0.0f;
-            }
-        }
+        if (j0 < now.first || j0 + kKeys > now.n_keys) keep(p, Span(now.first, now.n_keys, j0));
 #pragma unroll
         for (int r = 0; r < 16; ++r) sum += p[r];
         // The matrix units wait for memory here: weights go in as two BFloat16 values each, 16 bits of them.
@@ -118,95 +194,104 @@ __global__ __launch_bounds__(kThreads, 2) void cap_decode_kernel(DecodeArgs a, K
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int c = 0; c < kBlocks; ++c) {
-                const bf16x8 columns = columns_of<D>(v_tile, 16 * i, c);
+                const bf16x8 columns = columns_of<D>(shared.v, 16 * i, c);
                 o[c] = mfma(columns, weights[i], o[c]);
                 o[c] = mfma(columns, rests[i], o[c]);
             }
         __builtin_amdgcn_wave_barrier();
-    }
 
-    // numerators [32][D] of each wavefront where its tile was, and their sums over the wavefronts
-    __syncthreads();
-    sum += __shfl_xor(sum, 32);
-    if (lane < 32) shared.sums[wave][lane] = sum;
-    if ((lane & 31) < heads) {
-        float *mine = reinterpret_cast<float *>(shared.tiles[wave]) + (lane & 31) * D + 4 * (lane >> 5);
+        const bool last = j0 + kKeys >= now.n_keys;  // of this sequence and head
+        if (last || n + 1 == end) {
+            const float all_keys = sum + __shfl_xor(sum, 32);
+            const int tiles = (now.n_keys + kKeys - 1) / kKeys - now.first / kKeys;
+            const bool whole = last && n + 1 - segment == tiles;
+            const int row = lane & 31;
+            if (row < heads) {
+                if (whole) {
+                    const float to_mean = all_keys == 0.0f ? 0.0f : 1.0f / all_keys;
+                    uint16_t *to = a.o + ((long long)now.seq * a.s.heads + head0 + row) * D + 4 * (lane >> 5);
 #pragma unroll
-        for (int c = 0; c < kBlocks; ++c)
+                    for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<f32x4 *>(mine + 32 * c + 8 * i) = f32x4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < heads * (D / 4); i += kThreads) {
-        const int h = i / (D / 4), d = i % (D / 4) * 4;
-        f32x4 n = f32x4{0, 0, 0, 0};
-        float total = 0.0f;
+                        for (int i = 0; i < 4; ++i)
+                            *reinterpret_cast<u32x2 *>(to + 32 * c + 8 * i) =
+                                u32x2{pack2(o[c][4 * i] * to_mean, o[c][4 * i + 1] * to_mean), pack2(o[c][4 * i + 2] * to_mean, o[c][4 * i + 3] * to_mean)};
+                } else {
+                    const long long at = ((long long)blockIdx.x * 2 + (segment == start ? 0 : 1)) * a.rows + row;
+                    if (lane < 32) a.sums[at] = all_keys;
+                    float *to = a.parts + at * D + 4 * (lane >> 5);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            n += *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(shared.tiles[w]) + h * D + d);
-            total += shared.sums[w][h];
+                    for (int c = 0; c < kBlocks; ++c)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            *reinterpret_cast<f32x4 *>(to + 32 * c + 8 * i) = f32x4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
+                }
+            }
+            if (n + 1 < end) {
+                begin(next);
+                segment = n + 1;
+            }
         }
-        if (a.parts == nullptr) {
-            const float to_mean = total == 0.0f ? 0.0f : 1.0f / total;
-            *reinterpret_cast<u32x2 *>(a.o + ((long long)seq * a.s.heads + head0 + h) * D + d) =
-                u32x2{pack2(n[0] * to_mean, n[1] * to_mean), pack2(n[2] * to_mean, n[3] * to_mean)};
-        } else {
-            const long long at = ((long long)seq * a.spans + span) * a.s.heads + head0 + h;
-            *reinterpret_cast<f32x4 *>(a.parts + at * D + d) = n;
-            if (d == 0) a.sums[at] = total;
-        }
+        now = next;
+        next = pages;
     }
 }
 
-// The spans of a sequence and head added up: four values of one head for each thread, spans dealt to 16 or 32 threads in turn and
-// those joined in their order.
-constexpr int kJoinThreads = 1024;
+// The parts of a sequence and key/value head added up: four values of a row for each thread, the shares dealt to as many threads
+// as there are for them in turn, and what those have joined in their order.  Where sequences are few a block takes a slice of the values.
+constexpr int kJoinThreads = 256;
 
 template <int D>
 __global__ __launch_bounds__(kJoinThreads) void cap_join_kernel(DecodeArgs a)
 {
-    constexpr int kAcross = D / 4, kDeep = kJoinThreads / kAcross;
-    __shared__ f32x4 parts[kDeep][kAcross];
-    __shared__ float sums[kDeep];
-    const int seq = blockIdx.x / a.s.heads, head = blockIdx.x % a.s.heads;
-    const int n_keys = keys_in_pages(a.p, seq), begin = first_key(a.s, n_keys);
-    const int across = threadIdx.x % kAcross, deep = threadIdx.x / kAcross;
+    __shared__ f32x4 parts[kJoinThreads];
+    __shared__ float sums[kJoinThreads];
+    const int pairs = a.s.kv_heads * a.row_blocks, slice = blockIdx.x % a.slices, seq = blockIdx.x / a.slices / pairs, pair = blockIdx.x / a.slices % pairs;
+    const int head0 = pair / a.row_blocks * a.s.group + 32 * (pair % a.row_blocks), heads = min(32, a.s.group - 32 * (pair % a.row_blocks));
+    const Row all(a, 0, seq);
+    const int tiles = tiles_of(a, seq), from = all.before + pair * tiles;
+    const int first = from / all.share, last = tiles > 0 ? (from + tiles - 1) / all.share : first;
+    if (tiles > 0 && first == last) return;  // finished by that wavefront
+    const int across = heads * (D / 4) / a.slices, deep = kJoinThreads / across, at_deep = threadIdx.x / across;
+    const int item = slice * across + threadIdx.x % across, row = item / (D / 4), d = item % (D / 4) * 4;
     f32x4 n = f32x4{0, 0, 0, 0};
     float total = 0.0f;
-    for (int span = begin / a.span + deep; span * a.span < n_keys; span += kDeep) {
-        const long long at = ((long long)seq * a.spans + span) * a.s.heads + head;
-        n += *reinterpret_cast<const f32x4 *>(a.parts + at * D + 4 * across);
-        total += a.sums[at];
+    if (tiles > 0 && at_deep < deep) {
+#pragma unroll 4
+        for (int share = first + at_deep; share <= last; share += deep) {
+            const long long at = ((long long)share * 2 + (from <= share * all.share ? 0 : 1)) * a.rows + row;
+            n += *reinterpret_cast<const f32x4 *>(a.parts + at * D + d);
+            total += a.sums[at];
+        }
     }
-    parts[deep][across] = n;
-    if (across == 0) sums[deep] = total;
+    parts[threadIdx.x] = n;
+    sums[threadIdx.x] = total;
     __syncthreads();
-    if (deep != 0) return;
-#pragma unroll
-    for (int i = 1; i < kDeep; ++i) {
-        n += parts[i][across];
-        total += sums[i];
+    if (at_deep != 0) return;
+    for (int i = 1; i < deep; ++i) {
+        n += parts[threadIdx.x + i * across];
+        total += sums[threadIdx.x + i * across];
     }
     const float to_mean = total == 0.0f ? 0.0f : 1.0f / total;
-    *reinterpret_cast<u32x2 *>(a.o + ((long long)seq * a.s.heads + head) * D + 4 * across) =
+    *reinterpret_cast<u32x2 *>(a.o + ((long long)seq * a.s.heads + head0 + row) * D + d) =
         u32x2{pack2(n[0] * to_mean, n[1] * to_mean), pack2(n[2] * to_mean, n[3] * to_mean)};
 }
 
-// Keys of a span: a power of two between one round of the four wavefronts and 1024 keys, such that all sequences' spans
-// fill the chip several times over if they are as long as the table allows.
-int span_of(const kcap_shape_t &s, const kcap_pages_t &p)
-{
-    const unsigned long long keys = (unsigned long long)p.most * p.page_size, across = (unsigned long long)s.docs * s.kv_heads;
-    int span = 1024;
-    while (span > kWaves * kKeys && across * ((keys + span - 1) / span) < 2048) span /= 2;
-    return span;
-}
-
-unsigned long long spans_of(const kcap_pages_t &p, int span) { return ((unsigned long long)p.most * p.page_size + span - 1) / span; }
-
-// Bytes of the sums in front of the numerators, which start on a cache line.
-unsigned long long sums_bytes(const kcap_shape_t &s, unsigned long long spans) { return (s.docs * spans * s.heads * 4 + 127) / 128 * 128; }
+// Wavefronts: as many as the chip holds (eight to a compute unit at dim 128, twelve at 64), at most one for each tile that the table has room for.
+struct Shares {
+    unsigned long long tiles, shares, rows, row_blocks;
+    Shares(const kcap_shape_t &s, const kcap_pages_t &p)
+    {
+        const unsigned long long group = s.kv_heads > 0 ? s.heads / s.kv_heads : 0;
+        row_blocks = (group + 31) / 32;
+        rows = group < 32 ? group : 32;
+        tiles = ((unsigned long long)p.most * p.page_size + kKeys - 1) / kKeys * s.docs * s.kv_heads * row_blocks;
+        const unsigned long long most = s.dim == 64 ? 3072 : 2048;
+        shares = tiles < most ? tiles : most;
+    }
+    // Bytes of the sums in front of the numerators, which start on a cache line.
+    unsigned long long sums_bytes() const { return (shares * 2 * rows * 4 + 127) / 128 * 128; }
+};
 
 template <class Lut>
 ktanh_status_t attention_paged(const kcap_shape_t *shape, const kcap_pages_t *cache, const uint16_t *q, const uint16_t *k_cache,
@@ -239,26 +324,25 @@ ktanh_status_t attention_paged(const kcap_shape_t *shape, const kcap_pages_t *ca
     }
 
     if (shape->q_rows != shape->docs) return KT_ERR_SHAPE;
+    const Shares cut(*shape, *cache);
+    const unsigned long long joins = shape->docs * shape->kv_heads * cut.row_blocks;
+    if (cut.tiles > 0x7FFFFFFF - 65536 || joins > kMaxBlocks / 8) return KT_ERR_SHAPE;
+    if (workspace == nullptr) return KT_ERR_NULL;
+    if (!aligned16(workspace)) return KT_ERR_ALIGN;
     a.p = p;
     a.o = o;
-    a.span = span_of(*shape, *cache);
-    const unsigned long long spans = spans_of(*cache, a.span);
-    a.row_blocks = (a.s.group + 31) / 32;
-    const unsigned long long blocks = spans * shape->docs * shape->kv_heads * a.row_blocks, joins = shape->docs * shape->heads;
-    if (blocks > kMaxBlocks || joins > kMaxBlocks / (kJoinThreads / kThreads)) return KT_ERR_SHAPE;
-    a.spans = (int)spans;
-    if (spans > 1) {
-        if (workspace == nullptr) return KT_ERR_NULL;
-        if (!aligned16(workspace)) return KT_ERR_ALIGN;
-        a.sums = static_cast<float *>(workspace);
-        a.parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + sums_bytes(*shape, spans));
-    }
+    a.shares = (int)cut.shares;
+    a.rows = (int)cut.rows;
+    a.row_blocks = (int)cut.row_blocks;
+    a.sums = static_cast<float *>(workspace);
+    a.parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + cut.sums_bytes());
     const auto on = static_cast<hipStream_t>(stream);
     auto *kernel = shape->dim == 64 ? &cap_decode_kernel<64> : &cap_decode_kernel<128>;
-    kernel<<<dim3((unsigned)blocks), dim3(kThreads), 0, on>>>(a, pack);
-    if ((st = launched()) != KT_OK || spans == 1) return st;
+    kernel<<<dim3((unsigned)cut.shares), dim3(64), 0, on>>>(a, pack);
+    if ((st = launched()) != KT_OK) return st;
     auto *join = shape->dim == 64 ? &cap_join_kernel<64> : &cap_join_kernel<128>;
-    join<<<dim3((unsigned)joins), dim3(kJoinThreads), 0, on>>>(a);
+    a.slices = joins >= 256 && a.rows * (int)shape->dim / 4 <= kJoinThreads ? 1 : 8;  // a slice is no more than a block's threads
+    join<<<dim3((unsigned)(joins * a.slices)), dim3(kJoinThreads), 0, on>>>(a);
     return launched();
 }
 
@@ -273,9 +357,8 @@ extern "C" size_t kcap_attention_paged_workspace(const kcap_shape_t *shape, cons
         const size_t parts = (size_t)forward_parts(*shape, *cache);
         return parts > 1 ? (forward_sums(parts, shape->q_rows, shape->heads) + parts * shape->q_rows * shape->heads * shape->dim) * 4 : 0;
     }
-    const unsigned long long spans = spans_of(*cache, span_of(*shape, *cache));
-    if (spans <= 1) return 0;
-    return (size_t)(sums_bytes(*shape, spans) + shape->docs * spans * shape->heads * shape->dim * 4);
+    const Shares cut(*shape, *cache);
+    return (size_t)(cut.sums_bytes() + cut.shares * 2 * cut.rows * shape->dim * 4);
 }
 
 extern "C" ktanh_status_t kcap_attention_paged(const kcap_shape_t *shape, const kcap_pages_t *cache, const uint16_t *q, const uint16_t *k_cache,
