@@ -367,7 +367,8 @@ ktanh_status_t kcap_attention64_backward(const kcap_shape_t *shape, const uint16
                                          void *workspace, const ktanh_lut64_t *lut, ktanh_stream_t stream);
 
 /* A cache of keys and values in pages: key j of sequence s lies in slot j % page_size of page
- * pages[s * table_row + j / page_size].  Strides in elements, multiples of 8; dim contiguous. */
+ * pages[s * table_row + j / page_size].  Strides in elements, multiples of 8 below 2^31 (slots and heads 2^24
+ * for attention); dim contiguous. */
 typedef struct kcap_pages {
     size_t page_size;              /* a power of two                                                */
     size_t page_count;             /* pages in the cache                                            */
@@ -404,7 +405,7 @@ ktanh_status_t kcap_attention64_paged(const kcap_shape_t *shape, const kcap_page
  *   cos, sin   device, Float32 [positions][angles], dense, 16-byte aligned; angles a multiple of 8, 2 * angles <= dim
  *   q_offsets  device, docs + 1, or NULL: one token for each sequence
  *   q_out      device, BFloat16 [q_rows][heads][dim], dense, 16-byte aligned; may be q where q is dense
- * A token whose position has no page in the table, or a page number outside the cache, is not written to the cache; one whose
+ * Rows in no sequence are left as they are.  A token whose position has no page in the table, or a page number outside the cache, is not written to the cache; one whose
  * position has no angles has NaN for its query and is not written either. */
 ktanh_status_t kcap_append(const kcap_shape_t *shape, const kcap_pages_t *cache, const uint16_t *q, const uint16_t *k,
                            const uint16_t *v, uint16_t *q_out, uint16_t *k_cache, uint16_t *v_cache, const int32_t *pages,

@@ -1,7 +1,8 @@
 // libktanh: new tokens into a paged cache, keys rotated on the way, values as they are, and the queries rotated.
 //
-// Moves each value once.  A lane takes 16 values of one head, two 16-byte pieces: both halves of eight rotated pairs, or
-// what is behind the rotated part.  A wavefront works for one token, so that its place is looked up once.
+// Moves each value once.  A lane takes units of 16 values of one head, two 16-byte pieces: both halves of eight rotated pairs, or
+// what is behind the rotated part.  A wavefront works for one token, so that its place (document, length, page: three loads one behind
+// the other) is looked up once, while the values are on their way.
 #include "ktanh_cap_args.h"
 
 using namespace ktanh_cap;
@@ -29,65 +30,77 @@ __device__ __forceinline__ void unpack8(u32x4 w, float *v)
 
 __device__ __forceinline__ u32x4 packed8(const float *v) { return __builtin_bit_cast(u32x4, pack8(v)); }
 
+constexpr int kUnits = 2;  // of a lane
+
 __global__ __launch_bounds__(kThreads) void cap_append_kernel(AppendArgs a)
 {
-    const long long wave = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    const unsigned wave = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
     const int token = (int)(wave / a.waves_per_token), lane = threadIdx.x & 63;
     if (token >= a.tokens) return;
+
+    // The values are asked for first: nothing of their address depends on where they go.
+    const int pieces = a.dim / 16;  // of a head, 16 values each
+    const int rows = a.heads + 2 * a.kv_heads;
+    int row[kUnits], piece[kUnits], lo[kUnits], hi[kUnits];
+    u32x4 out_lo[kUnits], out_hi[kUnits];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const int unit = ((int)(wave % a.waves_per_token) * kUnits + u) * 64 + lane;
+        row[u] = unit / pieces;
+        piece[u] = unit % pieces;
+        const int at = min(row[u], rows - 1);
+        const bool is_q = at < a.heads, is_v = at >= a.heads + a.kv_heads;
+        const Rows &in = is_q ? a.q : is_v ? a.v : a.k;
+        const uint16_t *from = in.at + token * in.row + (is_q ? at : (at - a.heads) % a.kv_heads) * in.head;
+        const bool halves = !is_v && 8 * piece[u] < a.angles && !a.interleaved;
+        lo[u] = halves ? 8 * piece[u] : 16 * piece[u];
+        hi[u] = halves ? lo[u] + a.angles : lo[u] + 8;
+        out_lo[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from + lo[u]));
+        out_hi[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from + hi[u]));
+    }
+
     const int doc = a.q_offsets == nullptr ? token : last_document(a.docs, [&](int d) { return offset_at(a.q_offsets, d, a.tokens) <= token; });
     const int first = offset_at(a.q_offsets, doc, a.tokens);
     if (token < first || token >= offset_at(a.q_offsets, doc + 1, a.tokens)) return;  // in no sequence
     const int position = (int)min((long long)max(a.p.lengths[doc], 0) + (token - first), 0x7FFFFFFFll);
-
-    const int pieces = a.dim / 16;  // of a head, 16 values each
-    const int unit = (int)(wave % a.waves_per_token) * 64 + lane, row = unit / pieces, piece = unit % pieces;
-    if (row >= a.heads + 2 * a.kv_heads) return;
-    const bool is_q = row < a.heads, is_v = row >= a.heads + a.kv_heads;
-    const int head = is_q ? row : (row - a.heads) % a.kv_heads;
     const bool has_angles = position < a.positions;
+    const int slot = position >> a.p.shift;
+    const int page = has_angles && slot < a.p.most ? a.p.pages[doc * a.p.row + slot] : -1;
+    const long long in_page = position & ((1 << a.p.shift) - 1);
 
-    uint16_t *to;
-    if (is_q) {
-        to = a.q_out + ((long long)token * a.heads + head) * a.dim;
-    } else {
-        const int slot = position >> a.p.shift;
-        if (!has_angles || slot >= a.p.most) return;
-        const int page = a.p.pages[doc * a.p.row + slot];
-        if (page < 0 || page >= a.p.count) return;
-        const long long in_page = position & ((1 << a.p.shift) - 1);
-        to = is_v ? a.v_cache + page * a.p.v_page + in_page * a.v_slot + head * a.v_head
-                  : a.k_cache + page * a.p.k_page + in_page * a.k_slot + head * a.k_head;
-    }
-    const Rows &in = is_q ? a.q : is_v ? a.v : a.k;
-    const uint16_t *from = in.at + token * in.row + head * in.head;
-
-    const bool turned = !is_v && 8 * piece < a.angles;
-    const bool halves = turned && !a.interleaved;
-    const int lo = halves ? 8 * piece : 16 * piece, hi = halves ? lo + a.angles : lo + 8;
-    u32x4 out_lo = *reinterpret_cast<const u32x4 *>(from + lo), out_hi = *reinterpret_cast<const u32x4 *>(from + hi);
-    if (turned) {
-        float x[16], cos[8], sin[8];
-        unpack8(out_lo, x);
-        unpack8(out_hi, x + 8);
-        const long long angle = (long long)min(position, a.positions - 1) * a.angles + 8 * piece;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            *reinterpret_cast<f32x4 *>(cos + 4 * i) = *reinterpret_cast<const f32x4 *>(a.cos + angle + 4 * i);
-            *reinterpret_cast<f32x4 *>(sin + 4 * i) = *reinterpret_cast<const f32x4 *>(a.sin + angle + 4 * i);
-        }
+    for (int u = 0; u < kUnits; ++u) {
+        if (row[u] >= rows) continue;
+        const bool is_q = row[u] < a.heads, is_v = row[u] >= a.heads + a.kv_heads;
+        const int head = is_q ? row[u] : (row[u] - a.heads) % a.kv_heads;
+        if (!is_q && (page < 0 || page >= a.p.count)) continue;
+        uint16_t *to = is_q   ? a.q_out + ((long long)token * a.heads + head) * a.dim
+                       : is_v ? a.v_cache + wide(page, a.p.v_page) + in_page * a.v_slot + head * a.v_head
+                              : a.k_cache + wide(page, a.p.k_page) + in_page * a.k_slot + head * a.k_head;
+        if (!is_v && 8 * piece[u] < a.angles) {
+            float x[16], cos[8], sin[8];
+            unpack8(out_lo[u], x);
+            unpack8(out_hi[u], x + 8);
+            const long long angle = (long long)min(position, a.positions - 1) * a.angles + 8 * piece[u];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int at_a = a.interleaved ? 2 * i : i, at_b = a.interleaved ? 2 * i + 1 : i + 8;
-            const float u = x[at_a], w = x[at_b];
-            x[at_a] = u * cos[i] - w * sin[i];
-            x[at_b] = w * cos[i] + u * sin[i];
+            for (int i = 0; i < 2; ++i) {
+                *reinterpret_cast<f32x4 *>(cos + 4 * i) = *reinterpret_cast<const f32x4 *>(a.cos + angle + 4 * i);
+                *reinterpret_cast<f32x4 *>(sin + 4 * i) = *reinterpret_cast<const f32x4 *>(a.sin + angle + 4 * i);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at_a = a.interleaved ? 2 * i : i, at_b = a.interleaved ? 2 * i + 1 : i + 8;
+                const float v = x[at_a], w = x[at_b];
+                x[at_a] = v * cos[i] - w * sin[i];
+                x[at_b] = w * cos[i] + v * sin[i];
+            }
+            out_lo[u] = packed8(x);
+            out_hi[u] = packed8(x + 8);
         }
-        out_lo = packed8(x);
-        out_hi = packed8(x + 8);
+        if (is_q && !has_angles) out_lo[u] = out_hi[u] = u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
+        *reinterpret_cast<u32x4 *>(to + lo[u]) = out_lo[u];
+        *reinterpret_cast<u32x4 *>(to + hi[u]) = out_hi[u];
     }
-    if (is_q && !has_angles) out_lo = out_hi = u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
-    *reinterpret_cast<u32x4 *>(to + lo) = out_lo;
-    *reinterpret_cast<u32x4 *>(to + hi) = out_hi;
 }
 
 }  // namespace
@@ -132,9 +145,9 @@ extern "C" ktanh_status_t kcap_append(const kcap_shape_t *shape, const kcap_page
     a.positions = (int)positions;
     a.angles = (int)angles;
     a.interleaved = interleaved != 0;
-    a.waves_per_token = ((s.heads + 2 * s.kv_heads) * (a.dim / 16) + 63) / 64;
+    a.waves_per_token = ((s.heads + 2 * s.kv_heads) * (a.dim / 16) + 64 * kUnits - 1) / (64 * kUnits);
     const unsigned long long blocks = ((unsigned long long)a.tokens * a.waves_per_token + kWaves - 1) / kWaves;
-    if (blocks > kMaxBlocks) return KT_ERR_SHAPE;
+    if (blocks > kMaxBlocks) return KT_ERR_SHAPE;  // wavefronts are numbered in 32 bits
     cap_append_kernel<<<dim3((unsigned)blocks), dim3(kThreads), 0, static_cast<hipStream_t>(stream)>>>(a);
     return launched();
 }

@@ -59,8 +59,11 @@ struct CapPages {
     const int *lengths;  // keys of each sequence
     long long row;
     int most, shift, count;
-    long long k_page, v_page;  // strides in elements
+    uint32_t k_page, v_page;  // strides in elements
 };
+
+// Products of two 32-bit numbers in 64 bits: one instruction, where strides of 64 bits take five.
+__device__ __forceinline__ unsigned long long wide(int a, uint32_t b) { return (unsigned long long)(uint32_t)a * b; }
 
 __device__ __forceinline__ int keys_in_pages(const CapPages &p, int sequence)
 {
@@ -76,7 +79,7 @@ inline ktanh_status_t read_pages(const kcap_pages_t *p, const int32_t *pages, co
     if (p->page_count == 0 || p->page_count > 0x7FFFFFFF || p->most == 0 || p->most > (1u << 30) / p->page_size || p->table_row > (size_t)1 << 40) return KT_ERR_SHAPE;
     for (size_t stride : {p->k_page, p->k_slot, p->k_head, p->v_page, p->v_slot, p->v_head}) {
         if (stride % 8 != 0) return KT_ERR_ALIGN;
-        if (stride > (size_t)1 << 40) return KT_ERR_SHAPE;
+        if (stride >= (size_t)1 << 31) return KT_ERR_SHAPE;
     }
     if (!aligned16(k) || !aligned16(v)) return KT_ERR_ALIGN;
     if (reinterpret_cast<uintptr_t>(pages) % 4 != 0 || reinterpret_cast<uintptr_t>(lengths) % 4 != 0) return KT_ERR_ALIGN;
@@ -86,8 +89,8 @@ inline ktanh_status_t read_pages(const kcap_pages_t *p, const int32_t *pages, co
     out->most = (int)p->most;
     out->shift = __builtin_ctzll(p->page_size);
     out->count = (int)p->page_count;
-    out->k_page = (long long)p->k_page;
-    out->v_page = (long long)p->v_page;
+    out->k_page = (uint32_t)p->k_page;
+    out->v_page = (uint32_t)p->v_page;
     return KT_OK;
 }
 

@@ -125,10 +125,10 @@ __global__ __launch_bounds__(64, 2) void cap_decode_kernel(DecodeArgs a, KtCapPa
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
             const int row = lane / kChunks + n * (64 / kChunks), j = min(at.j0 + row, at.n_keys - 1);
-            const long long in_page = j & ((1 << a.p.shift) - 1), p = __shfl(page, row);
+            const int in_page = j & ((1 << a.p.shift) - 1), p = __shfl(page, row);
             // read once: with the hint a batch takes 200 us instead of 222
-            next_k[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(k + p * a.p.k_page + in_page * a.s.k.row + 8 * (lane % kChunks)));
-            next_v[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(v + p * a.p.v_page + in_page * a.s.v.row + 8 * (lane % kChunks)));
+            next_k[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(k + wide(p, a.p.k_page) + wide(in_page, (uint32_t)a.s.k.row) + 8 * (lane % kChunks)));
+            next_v[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(v + wide(p, a.p.v_page) + wide(in_page, (uint32_t)a.s.v.row) + 8 * (lane % kChunks)));
         }
     };
     bf16x8 q[kSteps];

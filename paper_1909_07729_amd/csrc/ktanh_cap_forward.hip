@@ -26,7 +26,7 @@ struct Keys {
     // PAGED
     const int *pages;
     int shift, count;
-    long long k_page, v_page;
+    uint32_t k_page, v_page;
 
     __device__ __forceinline__ int page(int j) const
     {
@@ -38,13 +38,13 @@ struct Keys {
     {
         j = min(j, last);
         if constexpr (!PAGED) return k + j * k_row;
-        return k + page * k_page + (j & ((1 << shift) - 1)) * k_row;
+        return k + wide(page, k_page) + wide(j & ((1 << shift) - 1), (uint32_t)k_row);
     }
     __device__ __forceinline__ const uint16_t *v_at(int j, int page) const
     {
         j = min(j, last);
         if constexpr (!PAGED) return v + j * v_row;
-        return v + page * v_page + (j & ((1 << shift) - 1)) * v_row;
+        return v + wide(page, v_page) + wide(j & ((1 << shift) - 1), (uint32_t)v_row);
     }
 };
 
@@ -370,13 +370,26 @@ ktanh_status_t attention(const kcap_shape_t *shape, const uint16_t *q, const uin
 
 }  // namespace
 
-// Three blocks fit a compute unit: where a call has fewer than fill the chip, each shares its keys (256 or more for each) with others.
+// How many blocks share the keys of a stretch.  768 blocks run at once (three to a compute unit); one takes about 1.2 us for a tile of 32
+// keys and 4 us around them, and joining costs a launch and the parts written and read at 4 TB/s.  By that the least of
+// all rounds: four pieces of 512 tokens in 32 heads are 512 blocks, which take 253 us by themselves, 261 in two parts (two rounds of
+// half the keys) and 228 in three; one piece of a long text needs many.
 int ktanh_cap::forward_parts(const kcap_shape_t &s, const kcap_pages_t &p)
 {
-    const unsigned long long blocks = (s.q_rows / kRows + s.docs) * s.heads, keys = (unsigned long long)p.most * p.page_size;
-    const unsigned long long fill = 768 / (blocks > 0 ? blocks : 1), most = keys / 256;
-    const unsigned long long parts = fill < most ? fill : most;
-    return parts < 1 ? 1 : parts > 64 ? 64 : (int)parts;
+    if (s.docs == 0 || s.q_rows == 0) return 1;
+    const double stretches = (double)s.docs * (double)(((s.q_rows + s.docs - 1) / s.docs + kRows - 1) / kRows);  // of sequences alike
+    const double blocks = stretches * (double)s.heads, keys = (double)p.most * (double)p.page_size;
+    const double part_us = (double)s.q_rows * (double)s.heads * (double)s.dim * 8.0 / 4e6;
+    int best = 1;
+    double least = 0.0;
+    for (int parts = 1; parts <= 64 && (parts == 1 || keys >= 256.0 * parts); ++parts) {
+        const double us = std::ceil(blocks * parts / 768.0) * (keys / 32.0 * 1.2 / parts + 4.0) + (parts > 1 ? 5.0 + part_us * parts : 0.0);
+        if (parts == 1 || us < least) {
+            least = us;
+            best = parts;
+        }
+    }
+    return best;
 }
 
 ktanh_status_t ktanh_cap::launch_forward_paged(const CapShape &s, const CapPages &p, const int *q_offsets, uint16_t *o, int dim, int parts,
