@@ -351,7 +351,7 @@ ktanh_status_t kcap_attention64(const kcap_shape_t *shape, const uint16_t *q, co
  * Products take BFloat16 roundings of P and dS and sum in Float32; gradients of shared heads are summed in Float32 before they are
  * rounded, in a fixed order.  Rows in no document, and queries that see no key, have the gradient 0.  A NaN or
  * infinity in a document may reach all of that document's gradients.
- *   d_o        device, BFloat16 [q_rows][heads][dim] with strides do_row, do_head (multiples of 8), 16-byte aligned
+ *   d_o        device, BFloat16 [q_rows][heads][dim] with strides do_row, do_head (multiples of 8 below 2^24), 16-byte aligned
  *   o, rest, lse  as kcap_attention gave them.  rest may be NULL: dq and dk of peaked rows are then less exact (for scores of
  *              standard deviation 6 they are 0.005 off in norm instead of 0.0027, of which 0.0017 is their own rounding)
  *   dq, dk, dv device, out: BFloat16, dense [rows][heads][dim], 16-byte aligned

@@ -306,7 +306,8 @@ __device__ __forceinline__ Stretch stretch_of(int rank, const int *offsets, int 
         s.doc = last_document(docs, [&](int d) { return offset_at(offsets, d, rows) / kRows + d <= tile; });
         s.begin = offset_at(offsets, s.doc, rows);
         s.end = max(offset_at(offsets, s.doc + 1, rows), s.begin);
-        s.first = s.begin + (tile - (s.begin / kRows + s.doc)) * kRows;
+        const int number = tile - (s.begin / kRows + s.doc);  // below 0: rows before the first document
+        s.first = number >= 0 ? s.begin + number * kRows : s.end;
         return s;
     }
     const int d = (int)(threadIdx.x & 63), my_doc = min(d, docs - 1);

@@ -380,7 +380,7 @@ ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t d
     if (do_row % 8 != 0 || do_head % 8 != 0 || !aligned16(d_o) || !aligned16(o) || !aligned16(rest) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(workspace) ||
         reinterpret_cast<uintptr_t>(lse) % 4 != 0 || reinterpret_cast<uintptr_t>(q_offsets) % 4 != 0 || reinterpret_cast<uintptr_t>(k_offsets) % 4 != 0)
         return KT_ERR_ALIGN;
-    if (do_row > (size_t)1 << 40 || do_head > (size_t)1 << 40) return KT_ERR_SHAPE;
+    if (do_row >= (size_t)1 << 24 || do_head >= (size_t)1 << 24) return KT_ERR_SHAPE;
     KtCapPack pack;
     if ((st = pack_lines(lut, &pack)) != KT_OK) return st;
     const long long dim = (long long)shape->dim;

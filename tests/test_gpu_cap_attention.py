@@ -184,6 +184,18 @@ def test_many_documents(gpu):
     _near(lse, want["lse"], want["lse_off"], "lse")
 
 
+@pytest.mark.parametrize("mask", ["causal", "all", "window"])
+@pytest.mark.parametrize("docs", [2, 64, 65, 200])
+def test_numbers_of_documents_behind_rows_of_none(gpu, docs, mask):
+    """Up to 64 documents blocks go by work, beyond by rows; 300 rows of no document before the first and behind the last."""
+    rng = np.random.default_rng(40)
+    lengths = rng.integers(0, 20, docs)
+    lengths[docs // 2] = 290
+    got, want = _grads(gpu, 41, lengths.tolist(), lengths.tolist(), 2, 1, 64, lead=300, cap=50.0, scale=0.125, **MASKS[mask])
+    for name, t in got.items():
+        _near(t, want[name], want[name + "_off"], name)
+
+
 def test_on_another_stream_and_in_a_graph(gpu):
     binding, _, torch = gpu
     (q, k, v), _ = _inputs(torch, 9, 500, 500, 2, 1, 128)
@@ -217,7 +229,7 @@ def _grads(gpu, seed, q_lengths, k_lengths, heads, kv_heads, dim, spread=2.0, in
     (q_at, q_np), (k_at, k_np) = (q_at[1:], q_np[1:]), (k_at[1:], k_np[1:])
     leaves = [t.clone().requires_grad_() for t in tensors]
     o = autograd.kcap_attention(*leaves, q_at, k_at, intervals=intervals, **options)
-    got = dict(zip(("dq", "dk", "dv"), torch.autograd.grad(o, leaves, do)))
+    got = {"o": o.detach(), **dict(zip(("dq", "dk", "dv"), torch.autograd.grad(o, leaves, do)))}
     want = kcap_oracle.attention(*wide, q_np, k_np, do=do.float().cpu().numpy().astype(np.float64), intervals=intervals, **options)
     return got, want
 
