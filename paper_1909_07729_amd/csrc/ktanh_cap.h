@@ -251,6 +251,11 @@ __device__ __forceinline__ unsigned place_of_block(unsigned block, unsigned tota
 // Offsets outside [0, rows] are taken as the nearest in range, so that a wrong one reads nothing out of bounds.
 struct Stretch {
     int doc, begin, end, first;  // rows of the document, and the first of the stretch; first >= end: nothing to do
+    int other_begin, others;     // rows of the other tensor that belong to the document
+};
+
+struct Others {
+    int begin, count;
 };
 
 __device__ __forceinline__ int offset_at(const int *offsets, int d, int rows)
@@ -294,11 +299,11 @@ __device__ __forceinline__ int lanes_before(int v, int bits)
 
 // The stretch of kRows rows that is the rank-th in work, the most first: blocks start in this order, and the last ones to start are
 // short (in the order of the rows sixteen documents of 8192 tokens keep the chip 79 % busy, like this 94).  By whole wavefronts.
-// `others(d)`: rows of the other tensor that document d has.  Work, in units of kRows: those rows if all are seen; if causal, the
+// `others_of(d)`: rows of the other tensor that document d has; asked for together with the document's own.  Work, in units of kRows: those rows if all are seen; if causal, the
 // number of the stretch and the rows before the document's first (`rising`: queries, over keys), or its number from the end (keys, over
 // queries).  More than 64 documents stay in the order of their rows.
-template <class Others>
-__device__ __forceinline__ Stretch stretch_of(int rank, const int *offsets, int docs, int rows, bool causal, bool rising, Others others)
+template <class OthersOf>
+__device__ __forceinline__ Stretch stretch_of(int rank, const int *offsets, int docs, int rows, bool causal, bool rising, OthersOf others_of)
 {
     Stretch s;
     if (docs > 64) {
@@ -308,9 +313,13 @@ __device__ __forceinline__ Stretch stretch_of(int rank, const int *offsets, int 
         s.end = max(offset_at(offsets, s.doc + 1, rows), s.begin);
         const int number = tile - (s.begin / kRows + s.doc);  // below 0: rows before the first document
         s.first = number >= 0 ? s.begin + number * kRows : s.end;
+        const Others others = others_of(s.doc);
+        s.other_begin = others.begin;
+        s.others = others.count;
         return s;
     }
     const int d = (int)(threadIdx.x & 63), my_doc = min(d, docs - 1);
+    const Others others = others_of(my_doc);
     const int begin = offset_at(offsets, my_doc, rows), end = d < docs ? max(offset_at(offsets, my_doc + 1, rows), begin) : begin;
     const int count = (end - begin + kRows - 1) / kRows;
     int number;  // of the stretch in its document
@@ -319,7 +328,7 @@ __device__ __forceinline__ Stretch stretch_of(int rank, const int *offsets, int 
         number = causal && rising ? count - 1 - rank : rank;
         if (rank >= count) number = count;
     } else {
-        const int least = !causal ? (others(my_doc) + kRows - 1) / kRows : rising ? max(others(my_doc) - (end - begin), 0) / kRows : 0;
+        const int least = !causal ? (others.count + kRows - 1) / kRows : rising ? max(others.count - (end - begin), 0) / kRows : 0;
         // stretches of this document with more work than w
         auto above = [&](int w) { return causal ? min(max(least + count - 1 - w, 0), count) : least > w ? count : 0; };
         int bits = 0, top = 0;
@@ -327,7 +336,7 @@ __device__ __forceinline__ Stretch stretch_of(int rank, const int *offsets, int 
         while (__ballot((causal ? least + count : least) >> top) != 0) ++top;
         int low = -1, high = 1 << top;  // fewer than or as many as `rank` have more work than `high`, more have more than `low`
         if (lanes_sum(count, bits) <= rank) {
-            s.doc = 0, s.begin = s.end = s.first = 0;
+            s.doc = s.begin = s.end = s.first = s.other_begin = s.others = 0;
             return s;
         }
         while (high - low > 1) {
@@ -343,7 +352,16 @@ __device__ __forceinline__ Stretch stretch_of(int rank, const int *offsets, int 
     s.begin = __builtin_amdgcn_readlane(begin, s.doc);
     s.end = __builtin_amdgcn_readlane(end, s.doc);
     s.first = s.begin + __builtin_amdgcn_readlane(number, s.doc) * kRows;
+    s.other_begin = __builtin_amdgcn_readlane(others.begin, s.doc);
+    s.others = __builtin_amdgcn_readlane(others.count, s.doc);
     return s;
+}
+
+// Rows [begin, end) of a document in the other tensor.
+__device__ __forceinline__ Others rows_in(const int *offsets, int doc, int rows)
+{
+    const int begin = offset_at(offsets, doc, rows);
+    return Others{begin, max(offset_at(offsets, doc + 1, rows) - begin, 0)};
 }
 
 // Rows of one head that no document covers (documents follow each other, so they lie before the first and behind the last)

@@ -95,10 +95,10 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
     if (place >= total) return;
     const int in_group = place % a.s.group;
     const int kv_head = place / a.s.group / a.tiles, head = kv_head * a.s.group + in_group;
-    auto keys_of = [&](int doc) { return max(offset_at(a.k_offsets, doc + 1, a.s.k_rows) - offset_at(a.k_offsets, doc, a.s.k_rows), 0); };
+    auto keys_of = [&](int doc) { return rows_in(a.k_offsets, doc, a.s.k_rows); };
     const Stretch at = stretch_of((int)(place / a.s.group % a.tiles), a.q_offsets, a.s.docs, a.s.q_rows, a.s.causal, true, keys_of);
     if (at.first >= at.end) return;
-    const int k_begin = offset_at(a.k_offsets, at.doc, a.s.k_rows), n_keys = keys_of(at.doc);
+    const int k_begin = at.other_begin, n_keys = at.others;
     Rows keys = of_head(a.s.k, kv_head), values = of_head(a.s.v, kv_head);
     keys.at += k_begin * keys.row;
     values.at += k_begin * values.row;
@@ -112,8 +112,9 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
     const int key_end = a.s.causal ? min(n_keys, block_last + 1) : n_keys;
     const int key_begin = a.s.window > 0 ? max(0, block_first - a.s.window + 1) & ~(kTile - 1) : 0;
     const int first_seen = a.s.window > 0 ? max(0, my_place - a.s.window + 1) : 0, last_seen = a.s.causal ? min(n_keys, my_place + 1) : n_keys;
-    spread_lines(lines, pack, 1.0f);
-
+    // What is loaded first is what takes longest; the lines are there behind the first tile's barrier.
+    Stream<D> stream(keys.at, keys.row, values.at, values.row, n_keys - 1, wave, key_begin);
+    if (key_begin < key_end) stream.next(key_begin, shared.k[0], shared.v[0]);
     bf16x8 q[kSteps], d_o[kSteps];
     load_row<D>(q, of_head(a.s.q, head), row_there);
     load_row<D>(d_o, of_head(a.d_o, head), row_there);
@@ -133,6 +134,7 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
             for (int i = 0; i < 8; ++i) delta = __builtin_fmaf((float)d_o[k][i], (float)o[k][i] + (float)rest[k][i], delta);
         delta += __shfl_xor(delta, 32);
     }
+    spread_lines(lines, pack, 1.0f);
     const long long sum_at = (long long)head * a.s.q_rows + row;
     if (row < at.end && lane < 32) a.delta[sum_at] = delta;
     const float lse2 = a.lse[(long long)head * a.s.q_rows + row_there] * kLog2e;
@@ -144,7 +146,6 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
     // tiles that every query of the block sees whole
     const int whole_from = a.s.window > 0 ? block_last - a.s.window + 1 : 0, whole_to = a.s.causal ? min(n_keys, block_first + 1) : n_keys;
     const bool idle = row0 >= at.end;
-    Stream<D> stream(keys.at, keys.row, values.at, values.row, n_keys - 1, wave, key_begin);
     auto step = [&](int j0, char *__restrict__ k_tile, char *__restrict__ v_tile, char *__restrict__ next_k, char *__restrict__ next_v) {
         wait_for_loads();
         const bool whole = j0 >= whole_from && j0 + kTile <= whole_to;
@@ -172,8 +173,6 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
 #pragma unroll
             for (int c = 0; c < kBlocks; ++c) dq[c] = mfma(Keys32<D>::columns(k_tile, i, c), shares[i], dq[c]);
     };
-    if (key_begin < key_end) stream.next(key_begin, shared.k[0], shared.v[0]);
-    __syncthreads();  // lines
     for (int j0 = key_begin; j0 < key_end; j0 += 2 * kTile) {
         step(j0, shared.k[0], shared.v[0], shared.k[1], shared.v[1]);
         if (j0 + kTile < key_end) step(j0 + kTile, shared.k[1], shared.v[1], shared.k[0], shared.v[0]);
@@ -204,10 +203,10 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
     const unsigned place = place_of_block(blockIdx.x, total);
     if (place >= total) return;
     const int part = place % a.parts, kv_head = place / a.parts / a.tiles;
-    auto queries_of = [&](int doc) { return max(offset_at(a.q_offsets, doc + 1, a.s.q_rows) - offset_at(a.q_offsets, doc, a.s.q_rows), 0); };
+    auto queries_of = [&](int doc) { return rows_in(a.q_offsets, doc, a.s.q_rows); };
     const Stretch at = stretch_of((int)(place / a.parts % a.tiles), a.k_offsets, a.s.docs, a.s.k_rows, a.s.causal, false, queries_of);
     if (at.first >= at.end) return;
-    const int q_begin = offset_at(a.q_offsets, at.doc, a.s.q_rows), n_queries = queries_of(at.doc);
+    const int q_begin = at.other_begin, n_queries = at.others;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int shift = (at.end - at.begin) - n_queries;  // query i is key i + shift
@@ -220,7 +219,6 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
     // queries that see this lane's key
     const int first_seen = a.s.causal ? max(0, key - shift) : 0;
     const int last_seen = a.s.window > 0 ? (int)min((long long)n_queries, max(0ll, (long long)key - shift + a.s.window)) : n_queries;
-    spread_lines(lines, pack, 1.0f);
     const float unit = a.s.cap * kLog2e;
 
     bf16x8 k[kSteps];
@@ -314,7 +312,7 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
     };
     const int tiles = left * ((to - from + kTile - 1) / kTile);
     if (left > 0) load(shared.q[0], shared.d_o[0]);
-    __syncthreads();  // lines
+    spread_lines(lines, pack, 1.0f);  // there behind the first tile's barrier
     int i0 = from;
     for (int n = 0; n < tiles; n += 2) {
         step(i0, shared.v[wave], shared.q[0], shared.d_o[0], shared.sums[0], shared.q[1], shared.d_o[1]);

@@ -112,8 +112,6 @@ __global__ __launch_bounds__(64, 2) void cap_decode_kernel(DecodeArgs a, KtCapPa
         now.head = in_seq / tiles;
         now.j0 += in_seq % tiles * kKeys;
     }
-    spread_lines<64>(lines, pack, a.s.cap * kLog2e);
-
     // The page of key j0 + (lane & 31), handed to the lanes that load the row one tile later.
     auto page_for = [&](const Place &at) {
         return min(max(a.p.pages[at.seq * a.p.row + (min(at.j0 + (lane & 31), at.n_keys - 1) >> a.p.shift)], 0), a.p.count - 1);
@@ -156,6 +154,7 @@ __global__ __launch_bounds__(64, 2) void cap_decode_kernel(DecodeArgs a, KtCapPa
         pages = next;
     }
     begin(now);
+    spread_lines<64>(lines, pack, a.s.cap * kLog2e);
     int segment = start;  // the first tile of the present sequence and head in this share
     __syncthreads();      // lines
     for (int n = start; n < end; ++n) {

@@ -137,7 +137,7 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     struct Shared {
         f32x2 lines[128];  // first: the offset of a line is its address
         char k[2][kBytes], v[2][kBytes];
-        int special;       // whether a value was taken out of a tile
+        int special[kWaves];  // whether the wavefront took a value out of a tile
     };
     __shared__ __align__(16) Shared shared;
     f32x2 *lines = shared.lines;
@@ -157,14 +157,14 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     const unsigned stretch = place / a.s.group / a.parts;
     const int kv_head = stretch / a.tiles, head = kv_head * a.s.group + in_group;
     auto keys_of = [&](int doc) {
-        if constexpr (PAGED) return keys_in_pages(a.p, doc);
-        else return max(offset_at(a.k_offsets, doc + 1, a.s.k_rows) - offset_at(a.k_offsets, doc, a.s.k_rows), 0);
+        if constexpr (PAGED) return Others{0, keys_in_pages(a.p, doc)};
+        else return rows_in(a.k_offsets, doc, a.s.k_rows);
     };
     const Stretch at = stretch_of((int)(stretch % a.tiles), a.q_offsets, a.s.docs, a.s.q_rows, a.s.causal, true, keys_of);
     if (at.first >= at.end) return;
 
     Keys<PAGED> keys;
-    const int n_keys = keys_of(at.doc);
+    const int n_keys = at.others;
     if constexpr (PAGED) {
         keys.k = a.s.k.at + kv_head * a.s.k.head;
         keys.v = a.s.v.at + kv_head * a.s.v.head;
@@ -174,9 +174,8 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
         keys.k_page = a.p.k_page;
         keys.v_page = a.p.v_page;
     } else {
-        const int begin = offset_at(a.k_offsets, at.doc, a.s.k_rows);
-        keys.k = a.s.k.at + begin * a.s.k.row + kv_head * a.s.k.head;
-        keys.v = a.s.v.at + begin * a.s.v.row + kv_head * a.s.v.head;
+        keys.k = a.s.k.at + at.other_begin * a.s.k.row + kv_head * a.s.k.head;
+        keys.v = a.s.v.at + at.other_begin * a.s.v.row + kv_head * a.s.v.head;
     }
     keys.k_row = a.s.k.row;
     keys.v_row = a.s.v.row;
@@ -197,11 +196,9 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
         key_end = min(key_end, key_begin + share);
     }
 
-    if (threadIdx.x == 0) shared.special = 0;
-    const float unit = a.s.cap * kLog2e;
-    spread_lines(lines, pack, unit);
-    __syncthreads();
-
+    // What is loaded first is what takes longest; the lines are there behind the first tile's barrier.
+    auto stream = stream_of<D>(keys, wave, key_begin);
+    if (key_begin < key_end) stream.next(key_begin, shared.k[0], shared.v[0]);
     bf16x8 q[kSteps];
     {
         const uint16_t *from = a.s.q.at + min(row, at.end - 1) * a.s.q.row + head * a.s.q.head + 8 * (lane >> 5);
@@ -211,6 +208,8 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     f32x16 o[kBlocks];
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c) o[c] = f32x16{0};
+    spread_lines(lines, pack, a.s.cap * kLog2e);
+    shared.special[wave] = 0;
     float sum = 0.0f, rounded_sum = 0.0f;  // of the weights, and of the weights as the product has them
 
     // Tiles that every query of the block sees whole.  In the others a weight may be zero because its key is hidden, and the product
@@ -237,25 +236,23 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
 #pragma unroll
             for (int c = 0; c < kBlocks; ++c) o[c] = mfma(Keys32<D>::columns(v_tile, i, c), weights[i], o[c]);
     };
-    auto stream = stream_of<D>(keys, wave, key_begin);
     auto step = [&](int j0, char *__restrict__ k_tile, char *__restrict__ v_tile, char *__restrict__ next_k, char *__restrict__ next_v) {
         wait_for_loads();
         const bool is_whole = whole(j0);
-        if (!is_whole && clean_values<D>(v_tile, wave, n_keys - j0)) shared.special = 1;
+        if (!is_whole && clean_values<D>(v_tile, wave, n_keys - j0)) shared.special[wave] = 1;
         // Behind this barrier the tile is complete and all are done with the one before, whose place the next one takes.
         __syncthreads();
         if (j0 + kKeys < key_end) stream.next(j0 + kKeys, next_k, next_v);
         if (is_whole ? !idle : !idle && !(a.s.causal && j0 > place0 + 31) && !(a.s.window > 0 && j0 + kKeys - 1 <= place0 - a.s.window))
             add_tile(j0, k_tile, v_tile, !is_whole);
     };
-    if (key_begin < key_end) stream.next(key_begin, shared.k[0], shared.v[0]);
     for (int j0 = key_begin; j0 < key_end; j0 += 2 * kKeys) {
         step(j0, shared.k[0], shared.v[0], shared.k[1], shared.v[1]);
         if (j0 + kKeys < key_end) step(j0 + kKeys, shared.k[1], shared.v[1], shared.k[0], shared.v[0]);
     }
 
     __syncthreads();
-    if (shared.special) {
+    if (shared.special[0] | shared.special[1] | shared.special[2] | shared.special[3]) {
         for (int j0 = key_begin; j0 < key_end; j0 += kKeys) {
             if (whole(j0)) continue;
             for (int j = j0; j < min(j0 + kKeys, n_keys); ++j) {
