@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     }
     keys.k_row = a.s.k.row;
     keys.v_row = a.s.v.row;
-    keys.last = n_keys - 1;
+    keys.last = max(n_keys - 1, 0);  // a sequence without keys looks up its first page, and reads none
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int shift = n_keys - (at.end - at.begin);            // query i is key i + shift
