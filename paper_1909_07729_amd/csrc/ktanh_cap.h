@@ -35,7 +35,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kRows = 128;   // rows of a block: 32 for each wavefront
+// Rows of a block: 32 for each wavefront, which go over the tiles of the other tensor together, or (SPLIT) 32 for all, each wavefront on its own
+// over every fourth tile, and their sums joined at the end.
+template <bool SPLIT> constexpr int kRows = SPLIT ? 32 : 128;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // A tensor [rows][heads][dim], dim contiguous.
@@ -188,12 +190,21 @@ __device__ __forceinline__ void load_direct(const void *from, char *to)
 // This wavefront's loads, direct ones among them, have arrived.
 __device__ __forceinline__ void wait_for_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 
-// Tiles of 32 rows of two tensors on their way to LDS, one behind the other, a wavefront's stretches of each; a row behind the last one is
-// read as the last.  One address for all lanes and 32 bits of offset for each (strides are below 2^24).
-template <int D>
+// A tile in LDS is complete, and what was in the place of the next one has been read: behind the block's barrier where its wavefronts
+// share it, else behind this wavefront's own reads and writes.
+template <bool SPLIT>
+__device__ __forceinline__ void tile_complete()
+{
+    if constexpr (SPLIT) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    else __syncthreads();
+}
+
+// Tiles of 32 rows of two tensors on their way to LDS, one behind the other, and of each the stretches that wavefront `wave` of LOADERS brings;
+// a row behind the last one is read as the last.  One address for all lanes and 32 bits of offset for each (strides are below 2^24).
+template <int D, int LOADERS, int STEP = 32>
 struct Stream {
     typedef Keys32<D> Tile;
-    static constexpr int kShare = Tile::kStretches / kWaves;
+    static constexpr int kShare = Tile::kStretches / LOADERS;
     const uint16_t *a_rows, *b_rows;
     long long a_row, b_row;
     int last, wave;
@@ -213,7 +224,7 @@ struct Stream {
         a = reinterpret_cast<const char *>(a_rows + (at + wave * kShare) * a_row);
         b = reinterpret_cast<const char *>(b_rows + (at + wave * kShare) * b_row);
     }
-    // Loads rows at .. at + 31, which are next.
+    // Loads rows at .. at + 31, which are next; the ones after begin STEP on.
     __device__ __forceinline__ void next(int at, char *a_tile, char *b_tile)
     {
 #pragma unroll
@@ -231,23 +242,40 @@ struct Stream {
             load_direct(a_from + a_at, a_tile + Tile::stretch_at(g));
             load_direct(b_from + b_at, b_tile + Tile::stretch_at(g));
         }
-        a += 32 * 2 * a_row;
-        b += 32 * 2 * b_row;
+        a += STEP * 2 * a_row;
+        b += STEP * 2 * b_row;
     }
 };
 
 // ------------------------------------------------------------------------------------------- blocks
-// Blocks that compute, and behind them `heads` blocks that clear.
-__device__ __forceinline__ unsigned padded(unsigned total) { return (total + 7) / 8 * 8; }
+// What a block has to do: a stretch of rows, by its rank in work, for one key/value head, one of the parts that it is cut into, and
+// one of the `members` that share its keys (query heads of the group).
+struct Unit {
+    int kv_head, rank, part, member;
+};
 
-// Consecutive blocks go to the eight dies in turn; block -> place in an order of which each die takes one stretch,
-// so that blocks that share keys share a second-level cache.  Launch 8 * ceil(total / 8) blocks.
-__device__ __forceinline__ unsigned place_of_block(unsigned block, unsigned total)
+// Blocks for all units; behind them come the blocks that clear.
+__host__ __device__ __forceinline__ unsigned long long unit_blocks(unsigned long long tiles, int kv_heads, int parts, int members)
 {
-    return (block & 7) * ((total + 7) / 8) + (block >> 3);
+    return (tiles * kv_heads * parts + 7) / 8 * 8 * members;
 }
 
-// A stretch of kRows rows of a document.  There are at most rows / kRows + documents, known without reading the offsets.
+// Consecutive blocks go to the eight dies in turn.  The members of a unit come to one die, and share its second-level cache; where the
+// key/value heads are a multiple of eight, all units of a head do, eight heads after the other; else the heads take turns, so that in either case
+// each die has as much of the long stretches as of the short ones and of those that are empty (pieces of 500 tokens of eight sequences, 12 heads on 4:
+// 268 us; with half of a head's ranks to each die 392).  False: nothing to do.
+__device__ __forceinline__ bool unit_of_block(unsigned block, unsigned tiles, int kv_heads, int parts, int members, Unit *unit)
+{
+    const unsigned i = block >> 3, n = i / members * 8 + (block & 7), turns = kv_heads % 8 == 0 ? 8 : kv_heads, of_head = n / turns;
+    if (n >= tiles * kv_heads * parts) return false;
+    unit->member = (int)(i % members);
+    unit->part = (int)(of_head % parts);
+    unit->rank = (int)(of_head / parts % tiles);
+    unit->kv_head = (int)(of_head / parts / tiles * turns + n % turns);
+    return true;
+}
+
+// A stretch of ROWS rows of a document.  There are at most rows / ROWS + documents, known without reading the offsets.
 // Offsets outside [0, rows] are taken as the nearest in range, so that a wrong one reads nothing out of bounds.
 struct Stretch {
     int doc, begin, end, first;  // rows of the document, and the first of the stretch; first >= end: nothing to do
@@ -297,22 +325,22 @@ __device__ __forceinline__ int lanes_before(int v, int bits)
     return sum;
 }
 
-// The stretch of kRows rows that is the rank-th in work, the most first: blocks start in this order, and the last ones to start are
+// The stretch of ROWS rows that is the rank-th in work, the most first: blocks start in this order, and the last ones to start are
 // short (in the order of the rows sixteen documents of 8192 tokens keep the chip 79 % busy, like this 94).  By whole wavefronts.
-// `others_of(d)`: rows of the other tensor that document d has; asked for together with the document's own.  Work, in units of kRows: those rows if all are seen; if causal, the
+// `others_of(d)`: rows of the other tensor that document d has; asked for together with the document's own.  Work, in units of ROWS: those rows if all are seen; if causal, the
 // number of the stretch and the rows before the document's first (`rising`: queries, over keys), or its number from the end (keys, over
 // queries).  More than 64 documents stay in the order of their rows.
-template <class OthersOf>
+template <int ROWS, class OthersOf>
 __device__ __forceinline__ Stretch stretch_of(int rank, const int *offsets, int docs, int rows, bool causal, bool rising, OthersOf others_of)
 {
     Stretch s;
     if (docs > 64) {
-        const int tile = causal && rising ? rows / kRows + docs - 1 - rank : rank;
-        s.doc = last_document(docs, [&](int d) { return offset_at(offsets, d, rows) / kRows + d <= tile; });
+        const int tile = causal && rising ? rows / ROWS + docs - 1 - rank : rank;
+        s.doc = last_document(docs, [&](int d) { return offset_at(offsets, d, rows) / ROWS + d <= tile; });
         s.begin = offset_at(offsets, s.doc, rows);
         s.end = max(offset_at(offsets, s.doc + 1, rows), s.begin);
-        const int number = tile - (s.begin / kRows + s.doc);  // below 0: rows before the first document
-        s.first = number >= 0 ? s.begin + number * kRows : s.end;
+        const int number = tile - (s.begin / ROWS + s.doc);  // below 0: rows before the first document
+        s.first = number >= 0 ? s.begin + number * ROWS : s.end;
         const Others others = others_of(s.doc);
         s.other_begin = others.begin;
         s.others = others.count;
@@ -321,14 +349,14 @@ __device__ __forceinline__ Stretch stretch_of(int rank, const int *offsets, int 
     const int d = (int)(threadIdx.x & 63), my_doc = min(d, docs - 1);
     const Others others = others_of(my_doc);
     const int begin = offset_at(offsets, my_doc, rows), end = d < docs ? max(offset_at(offsets, my_doc + 1, rows), begin) : begin;
-    const int count = (end - begin + kRows - 1) / kRows;
+    const int count = (end - begin + ROWS - 1) / ROWS;
     int number;  // of the stretch in its document
     if (docs == 1) {
         s.doc = 0;
         number = causal && rising ? count - 1 - rank : rank;
         if (rank >= count) number = count;
     } else {
-        const int least = !causal ? (others.count + kRows - 1) / kRows : rising ? max(others.count - (end - begin), 0) / kRows : 0;
+        const int least = !causal ? (others.count + ROWS - 1) / ROWS : rising ? max(others.count - (end - begin), 0) / ROWS : 0;
         // stretches of this document with more work than w
         auto above = [&](int w) { return causal ? min(max(least + count - 1 - w, 0), count) : least > w ? count : 0; };
         int bits = 0, top = 0;
@@ -351,7 +379,7 @@ __device__ __forceinline__ Stretch stretch_of(int rank, const int *offsets, int 
     s.doc = __builtin_amdgcn_readfirstlane(s.doc);
     s.begin = __builtin_amdgcn_readlane(begin, s.doc);
     s.end = __builtin_amdgcn_readlane(end, s.doc);
-    s.first = s.begin + __builtin_amdgcn_readlane(number, s.doc) * kRows;
+    s.first = s.begin + __builtin_amdgcn_readlane(number, s.doc) * ROWS;
     s.other_begin = __builtin_amdgcn_readlane(others.begin, s.doc);
     s.others = __builtin_amdgcn_readlane(others.count, s.doc);
     return s;

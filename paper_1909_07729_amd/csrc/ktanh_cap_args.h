@@ -94,11 +94,28 @@ inline ktanh_status_t read_pages(const kcap_pages_t *p, const int32_t *pages, co
     return KT_OK;
 }
 
-// Many queries of each sequence over the cache (ktanh_cap_forward.hip).  Where forward_parts is above 1 the workspace holds
+// Whether blocks hold 32 rows, their wavefronts sharing the other tensor's tiles, rather than 128: where blocks of 128 leave compute units idle and
+// there is more than one tile to share.  Output, then gradients, causal, in us, blocks of 128 | of 32:
+//    1024 rows,  8 heads of 128, 8 key/value heads (64 blocks of 128)   38.4 103 | 16.8 40
+//    4096 rows,  8 heads of 128, 8 key/value heads (256)                 130 366 | 66 180
+//    2048 rows, 32 heads of 128, 8 key/value heads (512)                  72 222 | 76 218
+//    32 documents of 64 rows, 32 heads of 128 (1024)                      19 67 | 37 103
+//    a document of 32 rows, 8 heads of 64                                4.7 10.0 | 5.5 11.7
+inline bool split_tiles(size_t rows, size_t others, size_t docs, size_t heads)
+{
+    return (rows / kRows<false> + docs) * heads < 512 && others > 32 * docs;
+}
+inline unsigned long long stretches(size_t rows, size_t docs, bool split) { return rows / (split ? kRows<true> : kRows<false>) + docs; }
+
+// Many queries of each sequence over the cache (ktanh_cap_forward.hip).  Where parts are above 1 the workspace holds
 // forward_sums Float32 sums and as many times dim numerators.
-int forward_parts(const kcap_shape_t &s, const kcap_pages_t &p);
+struct ForwardPlan {
+    bool split;
+    int parts;
+};
+ForwardPlan forward_plan(const kcap_shape_t &s, const kcap_pages_t &p);
 inline size_t forward_sums(size_t parts, size_t rows, size_t heads) { return (parts * rows * heads + 31) / 32 * 32; }
-ktanh_status_t launch_forward_paged(const CapShape &s, const CapPages &p, const int *q_offsets, uint16_t *o, int dim, int parts, float *workspace,
+ktanh_status_t launch_forward_paged(const CapShape &s, const CapPages &p, const int *q_offsets, uint16_t *o, int dim, ForwardPlan plan, float *workspace,
                                     const KtCapPack &pack, ktanh_stream_t stream);
 
 }  // namespace ktanh_cap

@@ -5,8 +5,8 @@
 //
 // 1 - t^2 is the library's derivative identity of TanH at K-TanH's value.  Scores are formed again in two kernels, each
 // summing what it owns in registers, so that no gradient is added to by two blocks and results do not depend on their order:
-//   cap_dq_kernel    128 queries of a head, over their keys; also forms delta
-//   cap_dkdv_kernel  128 keys of a key/value head, over the queries of the heads that share them
+//   cap_dq_kernel    128 (or 32) queries of a head, over their keys; also forms delta
+//   cap_dkdv_kernel  128 (or 32) keys of a key/value head, over the queries of the heads that share them
 #include "ktanh_cap_args.h"
 
 using namespace ktanh_cap;
@@ -28,12 +28,13 @@ struct BackwardArgs {
 constexpr int kTile = 32;  // rows of a tile in LDS
 
 // Of the rows that this wavefront loaded, those behind the last become zero in both tiles: what they hold is not the document's.
-template <int D>
+template <int D, int LOADERS>
 __device__ __forceinline__ void clear_behind(char *a_tile, char *b_tile, int wave, int there)
 {
+    constexpr int kShare = Keys32<D>::kStretches / LOADERS;
 #pragma unroll
-    for (int n = 0; n < Stream<D>::kShare; ++n) {
-        const int g = wave * Stream<D>::kShare + n, at = Keys32<D>::stretch_at(g) + 16 * (threadIdx.x & 63);
+    for (int n = 0; n < kShare; ++n) {
+        const int g = wave * kShare + n, at = Keys32<D>::stretch_at(g) + 16 * (threadIdx.x & 63);
         if (Keys32<D>::row_of_lane(g) >= there)
             *reinterpret_cast<u32x4 *>(a_tile + at) = *reinterpret_cast<u32x4 *>(b_tile + at) = u32x4{0, 0, 0, 0};
     }
@@ -50,53 +51,71 @@ __device__ __forceinline__ void load_row(bf16x8 (&to)[D / 16], const Rows &from,
     for (int k = 0; k < D / 16; ++k) to[k] = *reinterpret_cast<const bf16x8 *>(at + 16 * k);
 }
 
-// An accumulator [dim][32 rows] as a lane's row of a dense tensor, times `by`.
-template <int D>
-__device__ __forceinline__ void store_row(uint16_t *row, const f32x16 (&acc)[D / 32], float by)
+// Values 4 i .. 4 i + 3 of every 32 of an accumulator [dim][32 rows], a lane's row.
+__device__ __forceinline__ f32x4 quad(const f32x16 *acc, int i)
 {
-    row += 4 * ((threadIdx.x & 63) >> 5);
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<u32x2 *>(row + 32 * c + 8 * i) =
-                u32x2{pack2(acc[c][4 * i] * by, acc[c][4 * i + 1] * by), pack2(acc[c][4 * i + 2] * by, acc[c][4 * i + 3] * by)};
+    const f32x16 &c = acc[i / 4];
+    return f32x4{c[4 * (i % 4)], c[4 * (i % 4) + 1], c[4 * (i % 4) + 2], c[4 * (i % 4) + 3]};
 }
 
-template <int D>
-__device__ __forceinline__ void store_row(float *row, const f32x16 (&acc)[D / 32], float by)
+__device__ __forceinline__ void store4(uint16_t *to, f32x4 v) { *reinterpret_cast<u32x2 *>(to) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])}; }
+__device__ __forceinline__ void store4(float *to, f32x4 v) { *reinterpret_cast<f32x4 *>(to) = v; }
+
+// An accumulator as a lane's row of a dense tensor, times `by`.  SPLIT: the sum of all wavefronts' in their order, a fourth written by each;
+// by all threads, and `sums` is free once more behind the next barrier.
+template <int D, bool SPLIT, class T, class Sums>
+__device__ __forceinline__ void store_row(T *row, bool there, const f32x16 (&acc)[D / 32], float by, Sums &sums)
 {
-    row += 4 * ((threadIdx.x & 63) >> 5);
+    constexpr int kQuads = D / 8, kMine = SPLIT ? kQuads / kWaves : kQuads;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = SPLIT ? wave * kMine : 0;
+    if constexpr (SPLIT) {
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c)
+        for (int i = 0; i < kQuads; ++i) sums[wave][i][lane] = quad(acc, i);
+        __syncthreads();
+    }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<f32x4 *>(row + 32 * c + 8 * i) =
-                f32x4{acc[c][4 * i] * by, acc[c][4 * i + 1] * by, acc[c][4 * i + 2] * by, acc[c][4 * i + 3] * by};
+    for (int i = 0; i < kMine; ++i) {
+        f32x4 v;
+        if constexpr (SPLIT) {
+            v = sums[0][first + i][lane];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) v += sums[w][first + i][lane];
+        } else {
+            v = quad(acc, i);
+        }
+        if (there) store4(row + 8 * (first + i) + 4 * (lane >> 5), v * by);
+    }
 }
 
-template <int D>
+template <int D, bool SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtCapPack pack)
 {
-    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32;
+    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32, kRows = ktanh_cap::kRows<SPLIT>;
+    constexpr int kLoaders = SPLIT ? 1 : kWaves, kTiles = SPLIT ? kWaves : 1, kStep = kTile * kTiles;  // a tile's wavefronts; tiles at once
+    constexpr int kBuffers = SPLIT ? 1 : 2;  // two blocks to a compute unit hide each other's loads
+    struct Tiles {
+        char k[kBuffers][kBytes], v[kBuffers][kBytes];
+    };
     struct Shared {
         f32x2 lines[128];  // first: the offset of a line is its address
-        char k[2][kBytes], v[2][kBytes];
+        union {
+            Tiles tiles[kTiles];
+            f32x4 sums[SPLIT ? kWaves : 1][SPLIT ? D / 8 : 1][64];  // of each wavefront, at the end
+        };
     };
     __shared__ __align__(16) Shared shared;
     f32x2 *lines = shared.lines;
 
-    const unsigned total = a.tiles * (unsigned)a.s.heads;
-    if (blockIdx.x >= padded(total)) {
-        clear_rows<D>(a.dq, a.q_offsets, a.s.docs, a.s.q_rows, a.s.heads, (int)(blockIdx.x - padded(total)), [](int) {});
+    const unsigned blocks = (unsigned)unit_blocks(a.tiles, a.s.kv_heads, 1, a.s.group);
+    if (blockIdx.x >= blocks) {
+        clear_rows<D>(a.dq, a.q_offsets, a.s.docs, a.s.q_rows, a.s.heads, (int)(blockIdx.x - blocks), [](int) {});
         return;
     }
-    const unsigned place = place_of_block(blockIdx.x, total);
-    if (place >= total) return;
-    const int in_group = place % a.s.group;
-    const int kv_head = place / a.s.group / a.tiles, head = kv_head * a.s.group + in_group;
+    Unit work;
+    if (!unit_of_block(blockIdx.x, a.tiles, a.s.kv_heads, 1, a.s.group, &work)) return;
+    const int kv_head = work.kv_head, head = kv_head * a.s.group + work.member;
     auto keys_of = [&](int doc) { return rows_in(a.k_offsets, doc, a.s.k_rows); };
-    const Stretch at = stretch_of((int)(place / a.s.group % a.tiles), a.q_offsets, a.s.docs, a.s.q_rows, a.s.causal, true, keys_of);
+    const Stretch at = stretch_of<kRows>(work.rank, a.q_offsets, a.s.docs, a.s.q_rows, a.s.causal, true, keys_of);
     if (at.first >= at.end) return;
     const int k_begin = at.other_begin, n_keys = at.others;
     Rows keys = of_head(a.s.k, kv_head), values = of_head(a.s.v, kv_head);
@@ -105,7 +124,7 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int shift = n_keys - (at.end - at.begin);
-    const int row0 = at.first + 32 * wave, row = row0 + (lane & 31), row_there = min(row, at.end - 1);
+    const int row0 = at.first + (SPLIT ? 0 : 32 * wave), row = row0 + (lane & 31), row_there = min(row, at.end - 1);
     const int place0 = row0 - at.begin + shift, my_place = row - at.begin + shift;
     const int block_first = at.first - at.begin + shift;
     const int block_last = min(at.first + kRows, at.end) - 1 - at.begin + shift;
@@ -113,8 +132,10 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
     const int key_begin = a.s.window > 0 ? max(0, block_first - a.s.window + 1) & ~(kTile - 1) : 0;
     const int first_seen = a.s.window > 0 ? max(0, my_place - a.s.window + 1) : 0, last_seen = a.s.causal ? min(n_keys, my_place + 1) : n_keys;
     // What is loaded first is what takes longest; the lines are there behind the first tile's barrier.
-    Stream<D> stream(keys.at, keys.row, values.at, values.row, n_keys - 1, wave, key_begin);
-    if (key_begin < key_end) stream.next(key_begin, shared.k[0], shared.v[0]);
+    const int loader = SPLIT ? 0 : wave, j_begin = key_begin + (SPLIT ? kTile * wave : 0);  // this wavefront's first tile
+    Tiles &tiles = shared.tiles[SPLIT ? wave : 0];
+    Stream<D, kLoaders, kStep> stream(keys.at, keys.row, values.at, values.row, n_keys - 1, loader, j_begin);
+    if (j_begin < key_end) stream.next(j_begin, tiles.k[0], tiles.v[0]);
     bf16x8 q[kSteps], d_o[kSteps];
     load_row<D>(q, of_head(a.s.q, head), row_there);
     load_row<D>(d_o, of_head(a.d_o, head), row_there);
@@ -135,8 +156,9 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
         delta += __shfl_xor(delta, 32);
     }
     spread_lines(lines, pack, 1.0f);
+    if constexpr (SPLIT) __syncthreads();
     const long long sum_at = (long long)head * a.s.q_rows + row;
-    if (row < at.end && lane < 32) a.delta[sum_at] = delta;
+    if (row < at.end && lane < 32 && (!SPLIT || wave == 0)) a.delta[sum_at] = delta;
     const float lse2 = a.lse[(long long)head * a.s.q_rows + row_there] * kLog2e;
     const float unit = a.s.cap * kLog2e;
 
@@ -149,10 +171,10 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
     auto step = [&](int j0, char *__restrict__ k_tile, char *__restrict__ v_tile, char *__restrict__ next_k, char *__restrict__ next_v) {
         wait_for_loads();
         const bool whole = j0 >= whole_from && j0 + kTile <= whole_to;
-        if (j0 + kTile > n_keys) clear_behind<D>(k_tile, v_tile, wave, n_keys - j0);
+        if (j0 + kTile > n_keys) clear_behind<D, kLoaders>(k_tile, v_tile, loader, n_keys - j0);
         // Behind this barrier the tile is complete and all are done with the one before, whose place the next one takes.
-        __syncthreads();
-        if (j0 + kTile < key_end) stream.next(j0 + kTile, next_k, next_v);
+        tile_complete<SPLIT>();
+        if (!SPLIT && j0 + kStep < key_end) stream.next(j0 + kStep, next_k, next_v);
         if (idle || (!whole && ((a.s.causal && j0 > place0 + 31) || (a.s.window > 0 && j0 + kTile - 1 <= place0 - a.s.window)))) return;
         f32x16 s = f32x16{0}, dp = f32x16{0};
 #pragma unroll
@@ -173,44 +195,61 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
 #pragma unroll
             for (int c = 0; c < kBlocks; ++c) dq[c] = mfma(Keys32<D>::columns(k_tile, i, c), shares[i], dq[c]);
     };
-    for (int j0 = key_begin; j0 < key_end; j0 += 2 * kTile) {
-        step(j0, shared.k[0], shared.v[0], shared.k[1], shared.v[1]);
-        if (j0 + kTile < key_end) step(j0 + kTile, shared.k[1], shared.v[1], shared.k[0], shared.v[0]);
+    if constexpr (SPLIT) {
+        for (int j0 = j_begin; j0 < key_end; j0 += kStep) {
+            step(j0, tiles.k[0], tiles.v[0], nullptr, nullptr);
+            tile_complete<SPLIT>();
+            if (j0 + kStep < key_end) stream.next(j0 + kStep, tiles.k[0], tiles.v[0]);
+        }
+    } else {
+        for (int j0 = j_begin; j0 < key_end; j0 += 2 * kStep) {
+            step(j0, tiles.k[0], tiles.v[0], tiles.k[1], tiles.v[1]);
+            if (j0 + kStep < key_end) step(j0 + kStep, tiles.k[1], tiles.v[1], tiles.k[0], tiles.v[0]);
+        }
     }
-    if (row < at.end) store_row<D>(a.dq + ((long long)row * a.s.heads + head) * D, dq, a.s.scale);
+    if constexpr (SPLIT) __syncthreads();
+    store_row<D, SPLIT>(a.dq + ((long long)row * a.s.heads + head) * D, row < at.end, dq, a.s.scale, shared.sums);
 }
 
-template <int D>
+template <int D, bool SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, KtCapPack pack)
 {
-    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32;
+    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32, kRows = ktanh_cap::kRows<SPLIT>;
+    constexpr int kLoaders = SPLIT ? 1 : kWaves, kTiles = SPLIT ? kWaves : 1;  // a tile's wavefronts; tiles at once
+    constexpr int kBuffers = SPLIT ? 1 : 2;  // two blocks to a compute unit hide each other's loads
+    struct Tiles {
+        char q[kBuffers][kBytes], d_o[kBuffers][kBytes];
+        float sums[kBuffers][2 * kTile];  // lse * log2 e | delta of a tile's rows
+    };
     struct Shared {
         f32x2 lines[128];  // first: the offset of a line is its address
-        char q[2][kBytes], d_o[2][kBytes];
-        char v[kWaves][kBytes];   // each wavefront's 32 rows of values: registers for them would leave one wavefront to a SIMD
-        float sums[2][2 * kTile];  // lse * log2 e | delta of a tile's rows
+        char v[SPLIT ? 1 : kWaves][kBytes];  // the wavefronts' 32 rows of values: registers for them would leave one wavefront to a SIMD
+        union {
+            Tiles tiles[kTiles];
+            f32x4 sums[SPLIT ? kWaves : 1][SPLIT ? D / 8 : 1][64];  // of each wavefront, at the end
+        };
     };
     __shared__ __align__(16) Shared shared;
     f32x2 *lines = shared.lines;
 
-    const unsigned total = a.tiles * (unsigned)(a.s.kv_heads * a.parts);
-    if (blockIdx.x >= padded(total)) {  // where there are parts, the kernel that joins them clears
-        const int head = (int)(blockIdx.x - padded(total));
+    const unsigned blocks = (unsigned)unit_blocks(a.tiles, a.s.kv_heads, a.parts, 1);
+    if (blockIdx.x >= blocks) {  // where there are parts, the kernel that joins them clears
+        const int head = (int)(blockIdx.x - blocks);
         clear_rows<D>(a.dk, a.k_offsets, a.s.docs, a.s.k_rows, a.s.kv_heads, head, [](int) {});
         clear_rows<D>(a.dv, a.k_offsets, a.s.docs, a.s.k_rows, a.s.kv_heads, head, [](int) {});
         return;
     }
-    const unsigned place = place_of_block(blockIdx.x, total);
-    if (place >= total) return;
-    const int part = place % a.parts, kv_head = place / a.parts / a.tiles;
+    Unit work;
+    if (!unit_of_block(blockIdx.x, a.tiles, a.s.kv_heads, a.parts, 1, &work)) return;
+    const int part = work.part, kv_head = work.kv_head;
     auto queries_of = [&](int doc) { return rows_in(a.q_offsets, doc, a.s.q_rows); };
-    const Stretch at = stretch_of((int)(place / a.parts % a.tiles), a.k_offsets, a.s.docs, a.s.k_rows, a.s.causal, false, queries_of);
+    const Stretch at = stretch_of<kRows>(work.rank, a.k_offsets, a.s.docs, a.s.k_rows, a.s.causal, false, queries_of);
     if (at.first >= at.end) return;
     const int q_begin = at.other_begin, n_queries = at.others;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int shift = (at.end - at.begin) - n_queries;  // query i is key i + shift
-    const int row0 = at.first + 32 * wave, row = row0 + (lane & 31), row_there = min(row, at.end - 1);
+    const int row0 = at.first + (SPLIT ? 0 : 32 * wave), row = row0 + (lane & 31), row_there = min(row, at.end - 1);
     const int key0 = row0 - at.begin, key = row_there - at.begin;
     const int block_first = at.first - at.begin, block_last = min(at.first + kRows, at.end) - 1 - at.begin;
     // queries that see some key of the block
@@ -223,11 +262,15 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
 
     bf16x8 k[kSteps];
     load_row<D>(k, of_head(a.s.k, kv_head), row_there);
+    char *values = shared.v[SPLIT ? 0 : wave];
     {
         const Rows v = of_head(a.s.v, kv_head);
+        constexpr int kShare = Keys32<D>::kStretches / kTiles;
 #pragma unroll
-        for (int g = 0; g < Keys32<D>::kStretches; ++g)
-            load_direct(v.at + min(row0 + Keys32<D>::row_of_lane(g), at.end - 1) * v.row + 8 * Keys32<D>::chunk_of_lane(), shared.v[wave] + Keys32<D>::stretch_at(g));
+        for (int n = 0; n < kShare; ++n) {
+            const int g = SPLIT ? wave * kShare + n : n;
+            load_direct(v.at + min(row0 + Keys32<D>::row_of_lane(g), at.end - 1) * v.row + 8 * Keys32<D>::chunk_of_lane(), values + Keys32<D>::stretch_at(g));
+        }
     }
     f32x16 dk[kBlocks], dv[kBlocks];
 #pragma unroll
@@ -240,31 +283,48 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
     const bool idle = row0 >= at.end;
     const long long first_query = q_begin;
     const Rows q = of_head(a.s.q, head0), d_o = of_head(a.d_o, head0);
-    Stream<D> stream(q.at + first_query * q.row, q.row, d_o.at + first_query * d_o.row, d_o.row, n_queries - 1, wave, from);
-    // a wavefront brings 16 of a tile's 64 sums
-    const float *sum_from = ((wave & 1) == 0 ? a.lse : a.delta) + (long long)head0 * a.s.q_rows + q_begin;
+    // Tiles of queries, heads one behind the other: this wavefront's first one and the one that it loads next.
+    const int loader = SPLIT ? 0 : wave, each = max((to - from + kTile - 1) / kTile, 0), tiles = each * heads;  // of a head; of all
+    struct Where {
+        int tile, head, query;
+    };
+    auto advance = [&](Where &w) {
+        w.tile += kTiles;
+        w.query += kTiles * kTile;
+        while (w.query >= to && w.tile < tiles) {
+            w.query -= each * kTile;
+            ++w.head;
+        }
+    };
+    Where now{SPLIT ? wave : 0, 0, from + (SPLIT ? wave * kTile : 0)};
+    now.tile -= kTiles;
+    now.query -= kTiles * kTile;
+    advance(now);
+    Where next = now;
+    Stream<D, kLoaders, kTiles * kTile> stream(q.at + first_query * q.row + next.head * q.head, q.row, d_o.at + first_query * d_o.row + next.head * d_o.head, d_o.row, n_queries - 1, loader, next.query);
+    // Where wavefronts share a tile, one brings 16 of its 64 sums.
+    const int sum_lanes = SPLIT ? 64 : 16, sum_row = SPLIT ? lane & 31 : 16 * (wave >> 1) + (lane & 15);
+    const bool is_delta = SPLIT ? lane >= 32 : (wave & 1) != 0;
+    const float *sum_from = (is_delta ? a.delta : a.lse) + (long long)head0 * a.s.q_rows + q_begin;
     float next_sum = 0.0f;
-    int left = from < to ? heads : 0, next_query = from;  // heads not loaded to their end, and where
-    auto load = [&](char *q_tile, char *do_tile) {  // the next tile: heads one behind the other
-        stream.next(next_query, q_tile, do_tile);
-        next_sum = sum_from[min(next_query + 16 * (wave >> 1) + (lane & 15), n_queries - 1)];
-        next_query += kTile;
-        if (next_query >= to) {
-            next_query = from;
-            --left;
-            stream.a_rows += q.head;
-            stream.b_rows += d_o.head;
-            stream.start(from);
-            sum_from += a.s.q_rows;
+    auto load = [&](char *q_tile, char *do_tile) {
+        stream.next(next.query, q_tile, do_tile);
+        next_sum = sum_from[(long long)next.head * a.s.q_rows + min(next.query + sum_row, n_queries - 1)];
+        const int head = next.head;
+        advance(next);
+        if (next.head != head) {
+            stream.a_rows = q.at + first_query * q.row + next.head * q.head;
+            stream.b_rows = d_o.at + first_query * d_o.row + next.head * d_o.head;
+            stream.start(next.query);
         }
     };
     auto step = [&](int i0, const char *__restrict__ v_tile, char *__restrict__ q_tile, char *__restrict__ do_tile, float *__restrict__ sums, char *__restrict__ next_q,
                     char *__restrict__ next_do) {
         wait_for_loads();
-        if (i0 + kTile > n_queries) clear_behind<D>(q_tile, do_tile, wave, n_queries - i0);
-        if (lane < 16) sums[(wave & 1) * kTile + 16 * (wave >> 1) + lane] = (wave & 1) == 0 ? next_sum * kLog2e : next_sum;
-        __syncthreads();
-        if (left > 0) load(next_q, next_do);
+        if (i0 + kTile > n_queries) clear_behind<D, kLoaders>(q_tile, do_tile, loader, n_queries - i0);
+        if (lane < sum_lanes) sums[(is_delta ? kTile : 0) + sum_row] = is_delta ? next_sum : next_sum * kLog2e;
+        tile_complete<SPLIT>();
+        if (!SPLIT && next.tile < tiles) load(next_q, next_do);
         const int first = i0 + shift;  // the place of the tile's first query
         const bool whole = i0 >= whole_from && i0 + kTile <= whole_to;
         if (idle || (!whole && ((a.s.causal && first + kTile - 1 < key0) || (a.s.window > 0 && first > key0 + 31 + a.s.window - 1)))) return;
@@ -310,26 +370,38 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
 #pragma unroll
             for (int c = 0; c < kBlocks; ++c) dk[c] = mfma(Keys32<D>::columns(q_tile, i, c), shares[i], dk[c]);
     };
-    const int tiles = left * ((to - from + kTile - 1) / kTile);
-    if (left > 0) load(shared.q[0], shared.d_o[0]);
+    Tiles &mine = shared.tiles[SPLIT ? wave : 0];
+    if (next.tile < tiles) load(mine.q[0], mine.d_o[0]);
     spread_lines(lines, pack, 1.0f);  // there behind the first tile's barrier
-    int i0 = from;
-    for (int n = 0; n < tiles; n += 2) {
-        step(i0, shared.v[wave], shared.q[0], shared.d_o[0], shared.sums[0], shared.q[1], shared.d_o[1]);
-        i0 = i0 + kTile < to ? i0 + kTile : from;
-        if (n + 1 == tiles) break;
-        step(i0, shared.v[wave], shared.q[1], shared.d_o[1], shared.sums[1], shared.q[0], shared.d_o[0]);
-        i0 = i0 + kTile < to ? i0 + kTile : from;
+    if constexpr (SPLIT) {
+        wait_for_loads();
+        __syncthreads();
     }
-    if (row >= at.end) return;
+    while (now.tile < tiles) {
+        if constexpr (SPLIT) {
+            step(now.query, values, mine.q[0], mine.d_o[0], mine.sums[0], nullptr, nullptr);
+            tile_complete<SPLIT>();
+            if (next.tile < tiles) load(mine.q[0], mine.d_o[0]);
+        } else {
+            step(now.query, values, mine.q[0], mine.d_o[0], mine.sums[0], mine.q[1], mine.d_o[1]);
+            advance(now);
+            if (now.tile >= tiles) break;
+            step(now.query, values, mine.q[1], mine.d_o[1], mine.sums[1], mine.q[0], mine.d_o[0]);
+        }
+        advance(now);
+    }
+    const bool there = row < at.end;
     const long long to_row = ((long long)row * a.s.kv_heads + kv_head) * D;
+    if constexpr (SPLIT) __syncthreads();
     if (a.dk_parts == nullptr) {
-        store_row<D>(a.dk + to_row, dk, a.s.scale);
-        store_row<D>(a.dv + to_row, dv, 1.0f);
+        store_row<D, SPLIT>(a.dk + to_row, there, dk, a.s.scale, shared.sums);
+        if constexpr (SPLIT) __syncthreads();
+        store_row<D, SPLIT>(a.dv + to_row, there, dv, 1.0f, shared.sums);
     } else {
         const long long part_at = (long long)part * a.s.k_rows * a.s.kv_heads * D + to_row;
-        store_row<D>(a.dk_parts + part_at, dk, a.s.scale);
-        store_row<D>(a.dv_parts + part_at, dv, 1.0f);
+        store_row<D, SPLIT>(a.dk_parts + part_at, there, dk, a.s.scale, shared.sums);
+        if constexpr (SPLIT) __syncthreads();
+        store_row<D, SPLIT>(a.dv_parts + part_at, there, dv, 1.0f, shared.sums);
     }
 }
 
@@ -352,11 +424,11 @@ __global__ __launch_bounds__(kThreads) void cap_join_grads_kernel(BackwardArgs a
     *reinterpret_cast<bf16x8 *>((blockIdx.y == 0 ? a.dk : a.dv) + i) = pack8(v);
 }
 
-// Blocks over 128 keys of a key/value head, all heads of its group one behind the other, where those blocks are many; else one head each.
+// Blocks over the keys of a key/value head, all heads of its group one behind the other, where those blocks are many; else one head each.
 int parts_of(const kcap_shape_t &s)
 {
     const size_t group = s.heads / s.kv_heads;
-    return (s.k_rows / kRows + s.docs) * s.kv_heads >= 2048 ? 1 : (int)group;
+    return (s.k_rows / kRows<false> + s.docs) * s.kv_heads >= 2048 ? 1 : (int)group;
 }
 
 size_t delta_bytes(const kcap_shape_t &s) { return (s.heads * s.q_rows * 4 + 127) / 128 * 128; }
@@ -398,22 +470,26 @@ ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t d
         a.dk_parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + delta_bytes(*shape));
         a.dv_parts = a.dk_parts + a.parts * each;
     }
-    const unsigned long long q_tiles = shape->q_rows / kRows + shape->docs, k_tiles = shape->k_rows / kRows + shape->docs;
-    const unsigned long long q_blocks = (q_tiles * a.s.heads + 7) / 8 * 8 + a.s.heads;
-    const unsigned long long k_blocks = (k_tiles * a.s.kv_heads * a.parts + 7) / 8 * 8 + (a.parts == 1 ? a.s.kv_heads : 0);
+    const bool split_keys = split_tiles(shape->q_rows, shape->k_rows, shape->docs, shape->heads);
+    const bool split_queries = split_tiles(shape->k_rows, shape->q_rows, shape->docs, shape->kv_heads * a.parts);
+    const unsigned long long q_tiles = stretches(shape->q_rows, shape->docs, split_keys), k_tiles = stretches(shape->k_rows, shape->docs, split_queries);
+    const unsigned long long q_blocks = unit_blocks(q_tiles, a.s.kv_heads, 1, a.s.group) + a.s.heads;
+    const unsigned long long k_blocks = unit_blocks(k_tiles, a.s.kv_heads, a.parts, 1) + (a.parts == 1 ? a.s.kv_heads : 0);
     const unsigned long long joins = (unsigned long long)(each + kThreads * 8 - 1) / (kThreads * 8);
     if (q_blocks > kMaxBlocks || k_blocks > kMaxBlocks || joins > kMaxBlocks) return KT_ERR_SHAPE;
 
     const auto on = static_cast<hipStream_t>(stream);
     if (queries) {
         a.tiles = (unsigned)q_tiles;
-        auto *kernel = dim == 64 ? &cap_dq_kernel<64> : &cap_dq_kernel<128>;
+        auto *kernel = split_keys ? dim == 64 ? &cap_dq_kernel<64, true> : &cap_dq_kernel<128, true>
+                                   : dim == 64 ? &cap_dq_kernel<64, false> : &cap_dq_kernel<128, false>;
         kernel<<<dim3((unsigned)q_blocks), dim3(kThreads), 0, on>>>(a, pack);
         if ((st = launched()) != KT_OK) return st;
     }
     if (!keys) return KT_OK;
     a.tiles = (unsigned)k_tiles;
-    auto *kernel = dim == 64 ? &cap_dkdv_kernel<64> : &cap_dkdv_kernel<128>;
+    auto *kernel = split_queries ? dim == 64 ? &cap_dkdv_kernel<64, true> : &cap_dkdv_kernel<128, true>
+                            : dim == 64 ? &cap_dkdv_kernel<64, false> : &cap_dkdv_kernel<128, false>;
     kernel<<<dim3((unsigned)k_blocks), dim3(kThreads), 0, on>>>(a, pack);
     if ((st = launched()) != KT_OK) return st;
     if (a.parts > 1) {

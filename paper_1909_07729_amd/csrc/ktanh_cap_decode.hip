@@ -316,10 +316,10 @@ ktanh_status_t attention_paged(const kcap_shape_t *shape, const kcap_pages_t *ca
     KtCapPack pack;
     if ((st = pack_lines(lut, &pack)) != KT_OK) return st;
     if (q_offsets != nullptr) {
-        const int parts = forward_parts(*shape, *cache);
-        if (parts > 1 && workspace == nullptr) return KT_ERR_NULL;
-        if (parts > 1 && !aligned16(workspace)) return KT_ERR_ALIGN;
-        return launch_forward_paged(a.s, p, q_offsets, o, (int)shape->dim, parts, static_cast<float *>(workspace), pack, stream);
+        const ForwardPlan plan = forward_plan(*shape, *cache);
+        if (plan.parts > 1 && workspace == nullptr) return KT_ERR_NULL;
+        if (plan.parts > 1 && !aligned16(workspace)) return KT_ERR_ALIGN;
+        return launch_forward_paged(a.s, p, q_offsets, o, (int)shape->dim, plan, static_cast<float *>(workspace), pack, stream);
     }
 
     if (shape->q_rows != shape->docs) return KT_ERR_SHAPE;
@@ -353,7 +353,7 @@ extern "C" size_t kcap_attention_paged_workspace(const kcap_shape_t *shape, cons
         cache->most == 0 || cache->most > 1u << 30 || shape->docs > 1u << 30 || shape->heads > 65536 || shape->kv_heads > 65536 || shape->dim > 128 || shape->q_rows > 1u << 30)
         return 0;
     if (!single) {
-        const size_t parts = (size_t)forward_parts(*shape, *cache);
+        const size_t parts = (size_t)forward_plan(*shape, *cache).parts;
         return parts > 1 ? (forward_sums(parts, shape->q_rows, shape->heads) + parts * shape->q_rows * shape->heads * shape->dim) * 4 : 0;
     }
     const Shares cut(*shape, *cache);

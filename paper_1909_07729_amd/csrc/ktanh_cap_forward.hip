@@ -9,8 +9,6 @@
 // others' (269 the matrix instructions alone), and three wavefronts share a SIMD because the tile's 32 keys and the direct loads leave
 // 160 registers enough.  16384 tokens, 32 heads of 128, causal: 2331 us, 943 TFLOP/s; with 64 keys to a tile, through registers, and
 // two wavefronts 2736; with 32 keys through registers 2620.
-#include <type_traits>
-
 #include "ktanh_cap_args.h"
 
 using namespace ktanh_cap;
@@ -51,10 +49,10 @@ struct Keys {
 constexpr int kKeys = 32;  // of a tile
 
 // The same for keys and values in pages: the pages of a tile's rows are looked up one tile ahead.
-template <int D>
+template <int D, int LOADERS, int STEP>
 struct PagedStream {
     typedef Keys32<D> Tile;
-    static constexpr int kShare = Tile::kStretches / kWaves;
+    static constexpr int kShare = Tile::kStretches / LOADERS;
     const Keys<true> &keys;
     const int wave;
     int pages[kShare];
@@ -74,17 +72,20 @@ struct PagedStream {
             load_direct(keys.k_at(at + row, pages[n]) + 8 * chunk, k_tile + Tile::stretch_at(g));
             load_direct(keys.v_at(at + row, pages[n]) + 8 * chunk, v_tile + Tile::stretch_at(g));
         }
-        look_up(at + kKeys);
+        look_up(at + STEP);
     }
 };
 
-template <int D>
-__device__ __forceinline__ Stream<D> stream_of(const Keys<false> &keys, int wave, int at)
+template <int D, int LOADERS, int STEP>
+__device__ __forceinline__ Stream<D, LOADERS, STEP> stream_of(const Keys<false> &keys, int wave, int at)
 {
-    return Stream<D>(keys.k, keys.k_row, keys.v, keys.v_row, keys.last, wave, at);
+    return Stream<D, LOADERS, STEP>(keys.k, keys.k_row, keys.v, keys.v_row, keys.last, wave, at);
 }
-template <int D>
-__device__ __forceinline__ PagedStream<D> stream_of(const Keys<true> &keys, int wave, int at) { return PagedStream<D>(keys, wave, at); }
+template <int D, int LOADERS, int STEP>
+__device__ __forceinline__ PagedStream<D, LOADERS, STEP> stream_of(const Keys<true> &keys, int wave, int at)
+{
+    return PagedStream<D, LOADERS, STEP>(keys, wave, at);
+}
 
 // Infinities and NaN become zero.  Returns whether there was one.
 __device__ __forceinline__ bool take_special(u32x4 *v)
@@ -101,13 +102,14 @@ __device__ __forceinline__ bool take_special(u32x4 *v)
 
 // Of the rows that this wavefront loaded: values behind the last key become zero, as infinities and NaN do.  Their weights are zero,
 // and the product would not be.
-template <int D>
+template <int D, int LOADERS>
 __device__ __forceinline__ bool clean_values(char *v_tile, int wave, int there)
 {
+    constexpr int kShare = Keys32<D>::kStretches / LOADERS;
     bool found = false;
 #pragma unroll
-    for (int n = 0; n < Stream<D>::kShare; ++n) {
-        const int g = wave * Stream<D>::kShare + n;
+    for (int n = 0; n < kShare; ++n) {
+        const int g = wave * kShare + n;
         u32x4 *at = reinterpret_cast<u32x4 *>(v_tile + Keys32<D>::stretch_at(g) + 16 * (threadIdx.x & 63));
         u32x4 w = *at;
         if (Keys32<D>::row_of_lane(g) >= there) w = u32x4{0, 0, 0, 0};
@@ -130,37 +132,43 @@ struct ForwardArgs {
 };
 
 // SUMS: with log-sums.
-template <int D, bool PAGED, bool SUMS>
-__global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a, KtCapPack pack)
+template <int D, bool PAGED, bool SUMS, bool SPLIT>
+__global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(ForwardArgs a, KtCapPack pack)
 {
-    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32;
+    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32, kRows = ktanh_cap::kRows<SPLIT>;
+    constexpr int kLoaders = SPLIT ? 1 : kWaves, kTiles = SPLIT ? kWaves : 1, kStep = kKeys * kTiles;  // a tile's wavefronts; tiles at once
+    constexpr int kBuffers = SPLIT ? 1 : 2;  // two blocks to a compute unit hide each other's loads
+    struct Tiles {
+        char k[kBuffers][kBytes], v[kBuffers][kBytes];
+    };
     struct Shared {
         f32x2 lines[128];  // first: the offset of a line is its address
-        char k[2][kBytes], v[2][kBytes];
+        union {
+            Tiles tiles[kTiles];
+            f32x4 sums[SPLIT ? kWaves : 1][SPLIT ? D / 8 : 1][64];  // of each wavefront, at the end
+        };
+        float weights[SPLIT ? kWaves : 1][SPLIT ? 64 : 1];
         int special[kWaves];  // whether the wavefront took a value out of a tile
     };
     __shared__ __align__(16) Shared shared;
     f32x2 *lines = shared.lines;
 
-    const unsigned total = a.tiles * (unsigned)(a.s.heads * a.parts);
-    if (blockIdx.x >= padded(total)) {
-        const int head = (int)(blockIdx.x - padded(total));
+    const unsigned blocks = (unsigned)unit_blocks(a.tiles, a.s.kv_heads, a.parts, a.s.group);
+    if (blockIdx.x >= blocks) {
+        const int head = (int)(blockIdx.x - blocks);
         clear_rows<D>(a.o, a.q_offsets, a.s.docs, a.s.q_rows, a.s.heads, head, [&](int row) {
             if (SUMS) a.lse[(long long)head * a.s.q_rows + row] = -__builtin_inff();
         });
         return;
     }
-    const unsigned place = place_of_block(blockIdx.x, total);
-    if (place >= total) return;
-    // heads that share keys side by side, then the stretches by their work
-    const int in_group = place % a.s.group, part = PAGED ? place / a.s.group % a.parts : 0;
-    const unsigned stretch = place / a.s.group / a.parts;
-    const int kv_head = stretch / a.tiles, head = kv_head * a.s.group + in_group;
+    Unit work;
+    if (!unit_of_block(blockIdx.x, a.tiles, a.s.kv_heads, PAGED ? a.parts : 1, a.s.group, &work)) return;
+    const int kv_head = work.kv_head, part = work.part, head = kv_head * a.s.group + work.member;
     auto keys_of = [&](int doc) {
         if constexpr (PAGED) return Others{0, keys_in_pages(a.p, doc)};
         else return rows_in(a.k_offsets, doc, a.s.k_rows);
     };
-    const Stretch at = stretch_of((int)(stretch % a.tiles), a.q_offsets, a.s.docs, a.s.q_rows, a.s.causal, true, keys_of);
+    const Stretch at = stretch_of<kRows>(work.rank, a.q_offsets, a.s.docs, a.s.q_rows, a.s.causal, true, keys_of);
     if (at.first >= at.end) return;
 
     Keys<PAGED> keys;
@@ -183,7 +191,7 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int shift = n_keys - (at.end - at.begin);            // query i is key i + shift
-    const int row0 = at.first + 32 * wave;                     // this wavefront's first query
+    const int row0 = at.first + (SPLIT ? 0 : 32 * wave);       // this wavefront's first query
     const int row = row0 + (lane & 31);                        // this lane's
     const int place0 = row0 - at.begin + shift, my_place = row - at.begin + shift;
     const int block_first = at.first - at.begin + shift;
@@ -197,8 +205,10 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     }
 
     // What is loaded first is what takes longest; the lines are there behind the first tile's barrier.
-    auto stream = stream_of<D>(keys, wave, key_begin);
-    if (key_begin < key_end) stream.next(key_begin, shared.k[0], shared.v[0]);
+    const int loader = SPLIT ? 0 : wave, j_begin = key_begin + (SPLIT ? kKeys * wave : 0);  // this wavefront's first tile
+    Tiles &tiles = shared.tiles[SPLIT ? wave : 0];
+    auto stream = stream_of<D, kLoaders, kStep>(keys, loader, j_begin);
+    if (j_begin < key_end) stream.next(j_begin, tiles.k[0], tiles.v[0]);
     bf16x8 q[kSteps];
     {
         const uint16_t *from = a.s.q.at + min(row, at.end - 1) * a.s.q.row + head * a.s.q.head + 8 * (lane >> 5);
@@ -210,6 +220,7 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     for (int c = 0; c < kBlocks; ++c) o[c] = f32x16{0};
     spread_lines(lines, pack, a.s.cap * kLog2e);
     shared.special[wave] = 0;
+    if constexpr (SPLIT) __syncthreads();
     float sum = 0.0f, rounded_sum = 0.0f;  // of the weights, and of the weights as the product has them
 
     // Tiles that every query of the block sees whole.  In the others a weight may be zero because its key is hidden, and the product
@@ -239,21 +250,29 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
     auto step = [&](int j0, char *__restrict__ k_tile, char *__restrict__ v_tile, char *__restrict__ next_k, char *__restrict__ next_v) {
         wait_for_loads();
         const bool is_whole = whole(j0);
-        if (!is_whole && clean_values<D>(v_tile, wave, n_keys - j0)) shared.special[wave] = 1;
+        if (!is_whole && clean_values<D, kLoaders>(v_tile, loader, n_keys - j0)) shared.special[wave] = 1;
         // Behind this barrier the tile is complete and all are done with the one before, whose place the next one takes.
-        __syncthreads();
-        if (j0 + kKeys < key_end) stream.next(j0 + kKeys, next_k, next_v);
+        tile_complete<SPLIT>();
+        if (!SPLIT && j0 + kStep < key_end) stream.next(j0 + kStep, next_k, next_v);
         if (is_whole ? !idle : !idle && !(a.s.causal && j0 > place0 + 31) && !(a.s.window > 0 && j0 + kKeys - 1 <= place0 - a.s.window))
             add_tile(j0, k_tile, v_tile, !is_whole);
     };
-    for (int j0 = key_begin; j0 < key_end; j0 += 2 * kKeys) {
-        step(j0, shared.k[0], shared.v[0], shared.k[1], shared.v[1]);
-        if (j0 + kKeys < key_end) step(j0 + kKeys, shared.k[1], shared.v[1], shared.k[0], shared.v[0]);
+    if constexpr (SPLIT) {
+        for (int j0 = j_begin; j0 < key_end; j0 += kStep) {
+            step(j0, tiles.k[0], tiles.v[0], nullptr, nullptr);
+            tile_complete<SPLIT>();
+            if (j0 + kStep < key_end) stream.next(j0 + kStep, tiles.k[0], tiles.v[0]);
+        }
+    } else {
+        for (int j0 = j_begin; j0 < key_end; j0 += 2 * kStep) {
+            step(j0, tiles.k[0], tiles.v[0], tiles.k[1], tiles.v[1]);
+            if (j0 + kStep < key_end) step(j0 + kStep, tiles.k[1], tiles.v[1], tiles.k[0], tiles.v[0]);
+        }
     }
 
     __syncthreads();
     if (shared.special[0] | shared.special[1] | shared.special[2] | shared.special[3]) {
-        for (int j0 = key_begin; j0 < key_end; j0 += kKeys) {
+        for (int j0 = j_begin; j0 < key_end; j0 += kStep) {
             if (whole(j0)) continue;
             for (int j = j0; j < min(j0 + kKeys, n_keys); ++j) {
                 if (row >= at.end || j < first_seen || j >= last_seen) continue;
@@ -271,37 +290,56 @@ __global__ __launch_bounds__(kThreads, 3) void cap_forward_kernel(ForwardArgs a,
 
     sum += __shfl_xor(sum, 32);
     rounded_sum += __shfl_xor(rounded_sum, 32);
+    // Numerators 4 i .. 4 i + 3 of every 32: a wavefront's own, or (SPLIT) a fourth of all, joined in the order of the wavefronts.
+    constexpr int kQuads = D / 8, kMine = SPLIT ? kQuads / kWaves : kQuads;
+    const int quad0 = SPLIT ? wave * kMine : 0;
+    f32x4 n[kMine];
+    if constexpr (SPLIT) {
+#pragma unroll
+        for (int i = 0; i < kQuads; ++i) shared.sums[wave][i][lane] = f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+        shared.weights[wave][lane] = lane < 32 ? rounded_sum : sum;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) n[i] = f32x4{0, 0, 0, 0};
+        sum = rounded_sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) n[i] += shared.sums[w][quad0 + i][lane];
+            rounded_sum += shared.weights[w][lane & 31];
+            sum += shared.weights[w][32 + (lane & 31)];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kQuads; ++i) n[i] = f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+    }
     if (row >= at.end) return;
-    if (SUMS && lane < 32)
+    const bool writes_sums = lane < 32 && (!SPLIT || wave == 0);
+    if (SUMS && writes_sums)
         a.lse[(long long)head * a.s.q_rows + row] = sum > 0.0f ? __builtin_logf(sum) : sum == 0.0f ? -__builtin_inff() : sum;
+    const int first_value = 8 * quad0 + 4 * (lane >> 5);
     if (PAGED && a.parts > 1) {
         const long long at_row = ((long long)part * a.s.q_rows + row) * a.s.heads + head;
-        if (lane < 32) a.part_sums[at_row] = rounded_sum;
-        float *values = a.part_values + at_row * D + 4 * (lane >> 5);
+        if (writes_sums) a.part_sums[at_row] = rounded_sum;
+        float *values = a.part_values + at_row * D + first_value;
 #pragma unroll
-        for (int c = 0; c < kBlocks; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<f32x4 *>(values + 32 * c + 8 * i) = f32x4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
+        for (int i = 0; i < kMine; ++i) *reinterpret_cast<f32x4 *>(values + 8 * i) = n[i];
         return;
     }
     const float to_mean = rounded_sum == 0.0f ? 0.0f : 1.0f / rounded_sum;
-    const long long to = ((long long)row * a.s.heads + head) * D + 4 * (lane >> 5);
+    const long long to = ((long long)row * a.s.heads + head) * D + first_value;
 #pragma unroll
-    for (int c = 0; c < kBlocks; ++c)
+    for (int i = 0; i < kMine; ++i) {
+        const f32x4 w = n[i] * to_mean;
+        const u32x2 rounded = {pack2(w[0], w[1]), pack2(w[2], w[3])};
+        *reinterpret_cast<u32x2 *>(a.o + to + 8 * i) = rounded;
+        if (a.rest != nullptr) {
+            float rest[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float w[4], rest[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = o[c][4 * i + e] * to_mean;
-            const u32x2 rounded = {pack2(w[0], w[1]), pack2(w[2], w[3])};
-            *reinterpret_cast<u32x2 *>(a.o + to + 32 * c + 8 * i) = rounded;
-            if (a.rest != nullptr) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) rest[e] = w[e] - __uint_as_float(e & 1 ? rounded[e / 2] & 0xFFFF0000u : rounded[e / 2] << 16);
-                *reinterpret_cast<u32x2 *>(a.rest + to + 32 * c + 8 * i) = u32x2{pack2(rest[0], rest[1]), pack2(rest[2], rest[3])};
-            }
+            for (int e = 0; e < 4; ++e) rest[e] = w[e] - __uint_as_float(e & 1 ? rounded[e / 2] & 0xFFFF0000u : rounded[e / 2] << 16);
+            *reinterpret_cast<u32x2 *>(a.rest + to + 8 * i) = u32x2{pack2(rest[0], rest[1]), pack2(rest[2], rest[3])};
         }
+    }
 }
 
 // The parts of a row added up in their order: four values of one row and head for each thread.
@@ -323,12 +361,13 @@ __global__ __launch_bounds__(kThreads) void cap_join_parts_kernel(ForwardArgs a)
 }
 
 template <bool PAGED, bool SUMS>
-ktanh_status_t launch_forward(const ForwardArgs &a, size_t dim, const KtCapPack &pack, ktanh_stream_t stream)
+ktanh_status_t launch_forward(const ForwardArgs &a, size_t dim, bool split, const KtCapPack &pack, ktanh_stream_t stream)
 {
-    const unsigned long long blocks = ((unsigned long long)a.tiles * a.s.heads * a.parts + 7) / 8 * 8 + (a.parts == 1 ? a.s.heads : 0);
+    const unsigned long long blocks = unit_blocks(a.tiles, a.s.kv_heads, a.parts, a.s.group) + (a.parts == 1 ? a.s.heads : 0);
     const unsigned long long joins = ((unsigned long long)a.s.q_rows * a.s.heads * dim / 4 + kThreads - 1) / kThreads;
     if (blocks > kMaxBlocks || (a.parts > 1 && joins > kMaxBlocks)) return KT_ERR_SHAPE;
-    auto *kernel = dim == 64 ? &cap_forward_kernel<64, PAGED, SUMS> : &cap_forward_kernel<128, PAGED, SUMS>;
+    auto *kernel = split ? dim == 64 ? &cap_forward_kernel<64, PAGED, SUMS, true> : &cap_forward_kernel<128, PAGED, SUMS, true>
+                         : dim == 64 ? &cap_forward_kernel<64, PAGED, SUMS, false> : &cap_forward_kernel<128, PAGED, SUMS, false>;
     kernel<<<dim3((unsigned)blocks), dim3(kThreads), 0, static_cast<hipStream_t>(stream)>>>(a, pack);
     ktanh_status_t st = launched();
     if constexpr (PAGED) {
@@ -361,35 +400,44 @@ ktanh_status_t attention(const kcap_shape_t *shape, const uint16_t *q, const uin
     a.rest = rest;
     a.lse = lse;
     a.parts = 1;
-    a.tiles = (unsigned)(shape->q_rows / kRows + shape->docs);
-    return lse != nullptr ? launch_forward<false, true>(a, shape->dim, pack, stream) : launch_forward<false, false>(a, shape->dim, pack, stream);
+    const bool split = split_tiles(shape->q_rows, shape->k_rows, shape->docs, shape->heads);
+    a.tiles = (unsigned)stretches(shape->q_rows, shape->docs, split);
+    return lse != nullptr ? launch_forward<false, true>(a, shape->dim, split, pack, stream) : launch_forward<false, false>(a, shape->dim, split, pack, stream);
 }
 
 }  // namespace
 
-// How many blocks share the keys of a stretch.  768 blocks run at once (three to a compute unit); one takes about 1.2 us for a tile of 32
-// keys and 4 us around them, and joining costs a launch and the parts written and read at 4 TB/s.  By that the least of
-// all rounds: four pieces of 512 tokens in 32 heads are 512 blocks, which take 253 us by themselves, 261 in two parts (two rounds of
-// half the keys) and 228 in three; one piece of a long text needs many.
-int ktanh_cap::forward_parts(const kcap_shape_t &s, const kcap_pages_t &p)
+// How many blocks share the keys of a stretch, and of which kind they are: the least of all rounds, by what a block takes for a tile and
+// around its tiles, the blocks that run at once, and the launch that joins parts written and read at 4 TB/s.
+ktanh_cap::ForwardPlan ktanh_cap::forward_plan(const kcap_shape_t &s, const kcap_pages_t &p)
 {
-    if (s.docs == 0 || s.q_rows == 0) return 1;
-    const double stretches = (double)s.docs * (double)(((s.q_rows + s.docs - 1) / s.docs + kRows - 1) / kRows);  // of sequences alike
-    const double blocks = stretches * (double)s.heads, keys = (double)p.most * (double)p.page_size;
-    const double part_us = (double)s.q_rows * (double)s.heads * (double)s.dim * 8.0 / 4e6;
-    int best = 1;
+    ForwardPlan best{false, 1};
+    if (s.docs == 0 || s.q_rows == 0) return best;
+    const double each = std::ceil((double)s.q_rows / (double)s.docs);  // of sequences alike
+    const double cached = (double)p.most * (double)p.page_size, part_us = (double)s.q_rows * (double)s.heads * (double)s.dim * 8.0 / 4e6;
     double least = 0.0;
-    for (int parts = 1; parts <= 64 && (parts == 1 || keys >= 256.0 * parts); ++parts) {
-        const double us = std::ceil(blocks * parts / 768.0) * (keys / 32.0 * 1.2 / parts + 4.0) + (parts > 1 ? 5.0 + part_us * parts : 0.0);
-        if (parts == 1 || us < least) {
-            least = us;
-            best = parts;
+    for (const bool split : {false, true}) {
+        const double rows = split ? kRows<true> : kRows<false>, blocks = std::ceil(each / rows) * (double)s.docs * (double)s.heads;
+        const double keys = s.window > 0 ? std::min(cached, (double)s.window + std::min(rows, each)) : cached;
+        // Microseconds of 32 keys with 128 rows, or 128 with 32, by how many blocks a compute unit holds, up to as many as it can.
+        const double full_us[4] = {0.0, 1.2, 1.45, 1.85}, split_us[3] = {0.0, 1.75, 2.6};
+        const double tiles = keys / (split ? 128.0 : 32.0);
+        const int most = split ? 2 : 3;
+        for (int parts = 1; parts <= 64 && (parts == 1 || keys >= 256.0 * parts); ++parts) {
+            const double held = std::ceil(blocks * parts / 256.0), rounds = std::floor(held / most);
+            const int rest = (int)(held - rounds * most);
+            const double tile_us = split ? rounds * split_us[2] + split_us[rest] : rounds * full_us[3] + full_us[rest];
+            const double t = tiles / parts * tile_us + 4.0 * std::ceil(held / most) + (parts > 1 ? 5.0 + part_us * parts : 0.0);
+            if (least == 0.0 || t < least) {
+                least = t;
+                best = ForwardPlan{split, parts};
+            }
         }
     }
     return best;
 }
 
-ktanh_status_t ktanh_cap::launch_forward_paged(const CapShape &s, const CapPages &p, const int *q_offsets, uint16_t *o, int dim, int parts,
+ktanh_status_t ktanh_cap::launch_forward_paged(const CapShape &s, const CapPages &p, const int *q_offsets, uint16_t *o, int dim, ForwardPlan plan,
                                                float *workspace, const KtCapPack &pack, ktanh_stream_t stream)
 {
     ForwardArgs a{};
@@ -397,11 +445,11 @@ ktanh_status_t ktanh_cap::launch_forward_paged(const CapShape &s, const CapPages
     a.p = p;
     a.q_offsets = q_offsets;
     a.o = o;
-    a.parts = parts;
+    a.parts = plan.parts;
     a.part_sums = workspace;
-    a.part_values = workspace + forward_sums(parts, s.q_rows, s.heads);
-    a.tiles = (unsigned)(s.q_rows / kRows + s.docs);
-    return launch_forward<true, false>(a, (size_t)dim, pack, stream);
+    a.part_values = workspace + forward_sums(plan.parts, s.q_rows, s.heads);
+    a.tiles = (unsigned)stretches(s.q_rows, s.docs, plan.split);
+    return launch_forward<true, false>(a, (size_t)dim, plan.split, pack, stream);
 }
 
 extern "C" ktanh_status_t kcap_attention(const kcap_shape_t *shape, const uint16_t *q, const uint16_t *k, const uint16_t *v,

@@ -254,7 +254,8 @@ def test_gradients_of_caps_and_tables(gpu, cap, spread, intervals):
 
 
 def test_gradients_with_many_blocks_and_with_few_are_the_same(gpu):
-    """Enough keys that one block sums all heads of a group, against the same documents in calls of their own."""
+    """Enough keys that one block sums all heads of a group, against the same documents in calls of their own, where four wavefronts
+    share the tiles of 32 rows."""
     binding, _, torch = gpu
     docs, n = 520, 130
     (q, k, v), _ = _inputs(torch, 22, docs * n, docs * n, 4, 2, 64)
@@ -266,8 +267,7 @@ def test_gradients_with_many_blocks_and_with_few_are_the_same(gpu):
     for d in (0, 7, docs - 1):
         rows = slice(d * n, (d + 1) * n)
         parts = binding.kcap_attention_backward(do[rows], q[rows], k[rows], v[rows], o[rows], lse[:, rows].contiguous(), one, cap=50.0)
-        assert torch.equal(whole[0][rows], parts[0])
-        for a, b in zip(whole[1:], parts[1:]):          # sums of Float32 in another order, rounded
+        for a, b in zip(whole, parts):                  # sums of Float32 in another order, rounded
             assert torch.allclose(a[rows].float(), b.float(), rtol=2 ** -7, atol=2 ** -12)
 
 
