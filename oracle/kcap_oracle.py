@@ -57,7 +57,12 @@ def head(q, k, v, *, cap, scale, causal=True, window=0, intervals=32, lut=None, 
     lse = np.where(some, np.log(np.where(some, total, 1.0)), -np.inf)
     # y is off by a few roundings of products up to cap * log2 e: the same share of each weight, and again through the sum
     weight = 2 * 8 * F32 * cap + keys * F32
-    o_off = (HALF + weight) * (p @ np.abs(vs)) + HALF * np.abs(o) + 1e-30
+    # Weights p (1 + d), |d| <= HALF, stand in the numerators and in the sum that divides them: o is off by
+    # sum p d (v - o) / sum p (1 + d), and sum p |v - o| is no more than the root of sum p (v - o)^2.
+    mean = p @ vs
+    spread = np.sqrt(np.maximum(p @ (vs * vs) - mean * mean, 0.0) + 1e-15 * (p @ (vs * vs)))
+    o_off = HALF / (1 - HALF) * spread + weight * (p @ np.abs(vs))
+    o_off = o_off + HALF * (np.abs(o) + o_off) + 1e-30
     out = {"o": o, "lse": lse, "o_off": o_off, "lse_off": weight + 4 * F32 * np.abs(np.where(some, lse, 0.0))}
     if do is None:
         return out

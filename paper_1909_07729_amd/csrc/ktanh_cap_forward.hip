@@ -407,27 +407,29 @@ ktanh_status_t attention(const kcap_shape_t *shape, const uint16_t *q, const uin
 
 }  // namespace
 
-// How many blocks share the keys of a stretch, and of which kind they are: the least of all rounds, by what a block takes for a tile and
-// around its tiles, the blocks that run at once, and the launch that joins parts written and read at 4 TB/s.
+// How many blocks share the keys of a stretch, and of which kind they are: the least time of all, by what a block takes for a tile and around its
+// tiles, how many a compute unit holds, and the launch that joins parts written and read at 4 TB/s.  Only the longest text is known here; texts
+// are taken to be spread evenly up to it, so that the time is that of the longest or that of all on average.
+// Four pieces of 512 tokens behind texts of up to 6000, 32 heads of 128: 253 us in one part, 261 in two, 228 in three (of 6000 each: 260, 304, 277).
+// 8 tokens behind 16384 of four sequences: 143 us in blocks of 128 rows, 96 in blocks of 32; 512 behind 512 of eight: 58 and 107.
 ktanh_cap::ForwardPlan ktanh_cap::forward_plan(const kcap_shape_t &s, const kcap_pages_t &p)
 {
     ForwardPlan best{false, 1};
     if (s.docs == 0 || s.q_rows == 0) return best;
-    const double each = std::ceil((double)s.q_rows / (double)s.docs);  // of sequences alike
+    const double docs = (double)s.docs, each = std::ceil((double)s.q_rows / docs), spread = (docs + 1.0) / (2.0 * docs);
     const double cached = (double)p.most * (double)p.page_size, part_us = (double)s.q_rows * (double)s.heads * (double)s.dim * 8.0 / 4e6;
     double least = 0.0;
     for (const bool split : {false, true}) {
-        const double rows = split ? kRows<true> : kRows<false>, blocks = std::ceil(each / rows) * (double)s.docs * (double)s.heads;
+        const double rows = split ? kRows<true> : kRows<false>, blocks = std::ceil(each / rows) * docs * (double)s.heads;
         const double keys = s.window > 0 ? std::min(cached, (double)s.window + std::min(rows, each)) : cached;
         // Microseconds of 32 keys with 128 rows, or 128 with 32, by how many blocks a compute unit holds, up to as many as it can.
         const double full_us[4] = {0.0, 1.2, 1.45, 1.85}, split_us[3] = {0.0, 1.75, 2.6};
-        const double tiles = keys / (split ? 128.0 : 32.0);
+        const double *tile_us = split ? split_us : full_us;
         const int most = split ? 2 : 3;
         for (int parts = 1; parts <= 64 && (parts == 1 || keys >= 256.0 * parts); ++parts) {
-            const double held = std::ceil(blocks * parts / 256.0), rounds = std::floor(held / most);
-            const int rest = (int)(held - rounds * most);
-            const double tile_us = split ? rounds * split_us[2] + split_us[rest] : rounds * full_us[3] + full_us[rest];
-            const double t = tiles / parts * tile_us + 4.0 * std::ceil(held / most) + (parts > 1 ? 5.0 + part_us * parts : 0.0);
+            const double tiles = keys / (split ? 128.0 : 32.0) / parts, held = std::ceil(blocks * parts / 256.0), rounds = std::floor(held / most);
+            const double all_us = rounds * tile_us[most] + tile_us[(int)(held - rounds * most)];
+            const double t = tiles * std::max(tile_us[1], spread * all_us) + 4.0 * std::ceil(held / most) + (parts > 1 ? 5.0 + part_us * parts : 0.0);
             if (least == 0.0 || t < least) {
                 least = t;
                 best = ForwardPlan{split, parts};

@@ -253,6 +253,40 @@ def test_gradients_of_caps_and_tables(gpu, cap, spread, intervals):
         _near(t, want[name], want[name + "_off"], name)
 
 
+def _many_heads(docs, kv_heads):
+    """Query heads, a multiple of kv_heads, that make 512 blocks of 128 rows or more of the documents."""
+    lengths = DOCS[docs][0]
+    return -(-512 // (kv_heads * (min(sum(lengths), sum(DOCS[docs][1] or lengths)) // 128 + len(lengths)))) * kv_heads
+
+
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("docs", DOCS)
+@pytest.mark.parametrize("kv_heads,dim", [(8, 64), (3, 128)])
+def test_blocks_of_128_rows(gpu, docs, mask, kv_heads, dim):
+    """Many heads: a wavefront goes over all tiles of its 32 rows, where few heads let four share them."""
+    heads = _many_heads(docs, kv_heads)
+    test_documents(gpu, docs, mask, heads, kv_heads, dim)
+    test_gradients(gpu, docs, mask, heads, kv_heads, dim)
+
+
+@pytest.mark.parametrize("mask", ["causal", "window"])
+def test_what_is_not_seen_does_not_reach_a_row_of_many_heads(gpu, mask):
+    binding, _, torch = gpu
+    (q, k, v), (q64, k64, v64) = _inputs(torch, 3, 300, 300, 2, 1, 64)
+    at, at_np = _offsets(torch, [90, 140])
+    for j, value in ((20, np.nan), (85, np.inf), (100, -np.inf), (228, np.nan), (250, np.inf)):
+        v64[j, 0, 3:70:20] = value
+    k64[229, 0, 5] = k64[250, 0, 5] = np.nan
+    options = dict(cap=32.0, scale=0.125, **MASKS[mask])
+    o, _ = binding.kcap_attention(q.repeat(1, 128, 1), _bf16(torch, k64), _bf16(torch, v64), at, **options)
+    want = kcap_oracle.attention(q64, np.nan_to_num(k64), v64, at_np, at_np, **options)["o"]
+    want[229] = np.nan      # the only row that sees the NaN key
+    off = kcap_oracle.attention(q64, np.nan_to_num(k64), np.where(np.isfinite(v64), v64, 0.0), at_np, at_np, **options)["o_off"]
+    got = o.float().cpu().numpy()
+    for head in range(0, 256, 51):
+        _near(got[:230, head], want[:230, head % 2], off[:230, head % 2], f"head {head}")
+
+
 def test_gradients_with_many_blocks_and_with_few_are_the_same(gpu):
     """Enough keys that one block sums all heads of a group, against the same documents in calls of their own, where four wavefronts
     share the tiles of 32 rows."""
@@ -403,6 +437,11 @@ def test_pieces_of_prompts_over_pages(gpu, page, heads, kv_heads, dim, window):
         rows = slice(at_np[s], at_np[s + 1])
         want = kcap_oracle.attention(q64[rows], ks, vs, [0, new[s]], [0, len(ks)], **options)
         _near(o[rows], want["o"], want["o_off"], f"sequence {s}")
+
+
+def test_pieces_of_prompts_in_blocks_of_128_rows(gpu):
+    test_pieces_of_prompts_over_pages(gpu, 16, 384, 2, 64, 0)
+    test_pieces_of_prompts_over_pages(gpu, 8, 384, 3, 128, 33)
 
 
 def test_wide_tables_and_layouts_of_the_cache(gpu):
