@@ -227,20 +227,23 @@ struct Stream {
     // Loads rows at .. at + 31, which are next; the ones after begin STEP on.
     __device__ __forceinline__ void next(int at, char *a_tile, char *b_tile)
     {
+        if (at + 32 <= last + 1) {
 #pragma unroll
-        for (int n = 0; n < kShare; ++n) {
-            const int g = wave * kShare + n;
-            uint32_t a_at = a_off, b_at = b_off;
-            const char *a_from = a + n * 2 * a_row, *b_from = b + n * 2 * b_row;
-            if (at + 32 > last + 1) {
-                const uint32_t there = min(Tile::row_of_lane(g), last - at), chunk = 16 * Tile::chunk_of_lane();
-                a_from = reinterpret_cast<const char *>(a_rows + at * a_row);
-                b_from = reinterpret_cast<const char *>(b_rows + at * b_row);
-                a_at = there * 2 * (uint32_t)a_row + chunk;
-                b_at = there * 2 * (uint32_t)b_row + chunk;
+            for (int n = 0; n < kShare; ++n) {
+                const int g = wave * kShare + n;
+                load_direct(a + n * 2 * a_row + a_off, a_tile + Tile::stretch_at(g));
+                load_direct(b + n * 2 * b_row + b_off, b_tile + Tile::stretch_at(g));
             }
-            load_direct(a_from + a_at, a_tile + Tile::stretch_at(g));
-            load_direct(b_from + b_at, b_tile + Tile::stretch_at(g));
+        } else {
+            const char *a_from = reinterpret_cast<const char *>(a_rows + at * a_row), *b_from = reinterpret_cast<const char *>(b_rows + at * b_row);
+            const uint32_t chunk = 16 * Tile::chunk_of_lane();
+#pragma unroll
+            for (int n = 0; n < kShare; ++n) {
+                const int g = wave * kShare + n;
+                const uint32_t there = min(Tile::row_of_lane(g), last - at);
+                load_direct(a_from + (there * 2 * (uint32_t)a_row + chunk), a_tile + Tile::stretch_at(g));
+                load_direct(b_from + (there * 2 * (uint32_t)b_row + chunk), b_tile + Tile::stretch_at(g));
+            }
         }
         a += STEP * 2 * a_row;
         b += STEP * 2 * b_row;

@@ -9,6 +9,8 @@
 // others' (269 the matrix instructions alone), and three wavefronts share a SIMD because the tile's 32 keys and the direct loads leave
 // 160 registers enough.  16384 tokens, 32 heads of 128, causal: 2331 us, 943 TFLOP/s; with 64 keys to a tile, through registers, and
 // two wavefronts 2736; with 32 keys through registers 2620.
+#include <type_traits>
+
 #include "ktanh_cap_args.h"
 
 using namespace ktanh_cap;
@@ -57,8 +59,8 @@ struct PagedStream {
     const int wave;
     int pages[kShare];
 
-    __device__ __forceinline__ PagedStream(const Keys<true> &keys, int wave, int at) : keys(keys), wave(wave) { look_up(at); }
-    __device__ __forceinline__ void look_up(int at)
+    __device__ __forceinline__ PagedStream(const Keys<true> &keys, int wave, int at) : keys(keys), wave(wave) { start(at); }
+    __device__ __forceinline__ void start(int at)
     {
 #pragma unroll
         for (int n = 0; n < kShare; ++n) pages[n] = keys.page(at + Tile::row_of_lane(wave * kShare + n));
@@ -72,7 +74,7 @@ struct PagedStream {
             load_direct(keys.k_at(at + row, pages[n]) + 8 * chunk, k_tile + Tile::stretch_at(g));
             load_direct(keys.v_at(at + row, pages[n]) + 8 * chunk, v_tile + Tile::stretch_at(g));
         }
-        look_up(at + STEP);
+        start(at + STEP);
     }
 };
 
@@ -87,36 +89,31 @@ __device__ __forceinline__ PagedStream<D, LOADERS, STEP> stream_of(const Keys<tr
     return PagedStream<D, LOADERS, STEP>(keys, wave, at);
 }
 
-// Infinities and NaN become zero.  Returns whether there was one.
-__device__ __forceinline__ bool take_special(u32x4 *v)
+// Infinities and NaN become zero.
+__device__ __forceinline__ void take_special(u32x4 *v)
 {
-    bool found = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const bool lo = ((*v)[i] & 0x7F80u) == 0x7F80u, hi = ((*v)[i] & 0x7F800000u) == 0x7F800000u;
         (*v)[i] &= (lo ? 0xFFFF0000u : ~0u) & (hi ? 0xFFFFu : ~0u);
-        found |= lo || hi;
     }
-    return found;
 }
 
 // Of the rows that this wavefront loaded: values behind the last key become zero, as infinities and NaN do.  Their weights are zero,
 // and the product would not be.
 template <int D, int LOADERS>
-__device__ __forceinline__ bool clean_values(char *v_tile, int wave, int there)
+__device__ __forceinline__ void clean_values(char *v_tile, int wave, int there)
 {
     constexpr int kShare = Keys32<D>::kStretches / LOADERS;
-    bool found = false;
 #pragma unroll
     for (int n = 0; n < kShare; ++n) {
         const int g = wave * kShare + n;
         u32x4 *at = reinterpret_cast<u32x4 *>(v_tile + Keys32<D>::stretch_at(g) + 16 * (threadIdx.x & 63));
         u32x4 w = *at;
         if (Keys32<D>::row_of_lane(g) >= there) w = u32x4{0, 0, 0, 0};
-        else found |= take_special(&w);
+        else take_special(&w);
         *at = w;
     }
-    return found;
 }
 
 struct ForwardArgs {
@@ -148,7 +145,7 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
             f32x4 sums[SPLIT ? kWaves : 1][SPLIT ? D / 8 : 1][64];  // of each wavefront, at the end
         };
         float weights[SPLIT ? kWaves : 1][SPLIT ? 64 : 1];
-        int special[kWaves];  // whether the wavefront took a value out of a tile
+        int special[kWaves];  // whether the wavefront has numerators that are not finite
     };
     __shared__ __align__(16) Shared shared;
     f32x2 *lines = shared.lines;
@@ -216,15 +213,14 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
         for (int k = 0; k < kSteps; ++k) q[k] = *reinterpret_cast<const bf16x8 *>(from + 16 * k);
     }
     f32x16 o[kBlocks];
-#pragma unroll
-    for (int c = 0; c < kBlocks; ++c) o[c] = f32x16{0};
     spread_lines(lines, pack, a.s.cap * kLog2e);
-    shared.special[wave] = 0;
     if constexpr (SPLIT) __syncthreads();
-    float sum = 0.0f, rounded_sum = 0.0f;  // of the weights, and of the weights as the product has them
+    float sum, rounded_sum;  // of the weights, and of the weights as the product has them
 
     // Tiles that every query of the block sees whole.  In the others a weight may be zero because its key is hidden, and the product
-    // with an infinite or NaN value would not be: such values are taken out, and added behind the loop where they are seen.
+    // with an infinite or NaN value would not be: a block whose numerators are not all finite goes over its keys once more, and
+    // then takes such values out of these tiles and adds them behind the loop where they are seen.  (Looking for them in every such tile took 4 to 7 %
+    // of the time over documents of some hundred tokens and windows.)
     const int whole_from = a.s.window > 0 ? block_last - a.s.window + 1 : 0, whole_to = a.s.causal ? min(n_keys, block_first + 1) : n_keys;
     auto whole = [&](int j0) { return j0 >= whole_from && j0 + kKeys <= whole_to; };
     const int first_seen = a.s.window > 0 ? max(0, my_place - a.s.window + 1) : 0, last_seen = a.s.causal ? min(n_keys, my_place + 1) : n_keys;
@@ -247,31 +243,46 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
 #pragma unroll
             for (int c = 0; c < kBlocks; ++c) o[c] = mfma(Keys32<D>::columns(v_tile, i, c), weights[i], o[c]);
     };
-    auto step = [&](int j0, char *__restrict__ k_tile, char *__restrict__ v_tile, char *__restrict__ next_k, char *__restrict__ next_v) {
+    auto step = [&](auto careful, int j0, char *__restrict__ k_tile, char *__restrict__ v_tile, char *__restrict__ next_k, char *__restrict__ next_v) {
         wait_for_loads();
         const bool is_whole = whole(j0);
-        if (!is_whole && clean_values<D, kLoaders>(v_tile, loader, n_keys - j0)) shared.special[wave] = 1;
+        if (careful.value && !is_whole) clean_values<D, kLoaders>(v_tile, loader, n_keys - j0);
         // Behind this barrier the tile is complete and all are done with the one before, whose place the next one takes.
         tile_complete<SPLIT>();
         if (!SPLIT && j0 + kStep < key_end) stream.next(j0 + kStep, next_k, next_v);
         if (is_whole ? !idle : !idle && !(a.s.causal && j0 > place0 + 31) && !(a.s.window > 0 && j0 + kKeys - 1 <= place0 - a.s.window))
             add_tile(j0, k_tile, v_tile, !is_whole);
     };
-    if constexpr (SPLIT) {
-        for (int j0 = j_begin; j0 < key_end; j0 += kStep) {
-            step(j0, tiles.k[0], tiles.v[0], nullptr, nullptr);
-            tile_complete<SPLIT>();
-            if (j0 + kStep < key_end) stream.next(j0 + kStep, tiles.k[0], tiles.v[0]);
+    auto add_all = [&](auto careful) {
+#pragma unroll
+        for (int c = 0; c < kBlocks; ++c) o[c] = f32x16{0};
+        sum = rounded_sum = 0.0f;
+        if constexpr (SPLIT) {
+            for (int j0 = j_begin; j0 < key_end; j0 += kStep) {
+                step(careful, j0, tiles.k[0], tiles.v[0], nullptr, nullptr);
+                tile_complete<SPLIT>();
+                if (j0 + kStep < key_end) stream.next(j0 + kStep, tiles.k[0], tiles.v[0]);
+            }
+        } else {
+            for (int j0 = j_begin; j0 < key_end; j0 += 2 * kStep) {
+                step(careful, j0, tiles.k[0], tiles.v[0], tiles.k[1], tiles.v[1]);
+                if (j0 + kStep < key_end) step(careful, j0 + kStep, tiles.k[1], tiles.v[1], tiles.k[0], tiles.v[0]);
+            }
         }
-    } else {
-        for (int j0 = j_begin; j0 < key_end; j0 += 2 * kStep) {
-            step(j0, tiles.k[0], tiles.v[0], tiles.k[1], tiles.v[1]);
-            if (j0 + kStep < key_end) step(j0 + kStep, tiles.k[1], tiles.v[1], tiles.k[0], tiles.v[0]);
-        }
-    }
-
+    };
+    add_all(std::false_type{});
+    float probe = 0.0f;  // NaN if a numerator is not finite
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) probe = __builtin_fmaf(o[c][r], 0.0f, probe);
+    shared.special[wave] = __ballot(probe != probe) != 0;
     __syncthreads();
     if (shared.special[0] | shared.special[1] | shared.special[2] | shared.special[3]) {
+        stream.start(j_begin);
+        if (j_begin < key_end) stream.next(j_begin, tiles.k[0], tiles.v[0]);
+        add_all(std::true_type{});
+        __syncthreads();
         for (int j0 = j_begin; j0 < key_end; j0 += kStep) {
             if (whole(j0)) continue;
             for (int j = j0; j < min(j0 + kKeys, n_keys); ++j) {
