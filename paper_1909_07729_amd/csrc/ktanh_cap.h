@@ -91,12 +91,15 @@ __device__ __forceinline__ void spread_lines(f32x2 *lines, const KtCapPack &pack
 
 // unit * K(x).  A NaN stays one.  Everything below 0.25 reads one line, so that lanes of small scores share an address: table reads
 // at many are what the LDS unit has least time for.
-__device__ __forceinline__ float capped(float x, const f32x2 *lines)
+__device__ __forceinline__ f32x2 line_of(float x, const f32x2 *lines)
 {
     const uint32_t key = __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fabsf(x), 0x1.fffffep-3f, 16.0f));
-    const f32x2 line = *reinterpret_cast<const f32x2 *>(reinterpret_cast<const char *>(lines) + ((key >> 16) & 0x3F8u));
-    return __builtin_copysignf(__builtin_fmaf(line.x, __builtin_fabsf(x), line.y), x);
+    return *reinterpret_cast<const f32x2 *>(reinterpret_cast<const char *>(lines) + ((key >> 16) & 0x3F8u));
 }
+
+__device__ __forceinline__ float on_line(float x, f32x2 line) { return __builtin_copysignf(__builtin_fmaf(line.x, __builtin_fabsf(x), line.y), x); }
+
+__device__ __forceinline__ float capped(float x, const f32x2 *lines) { return on_line(x, line_of(x, lines)); }
 
 // Which accumulator rows of a lane, numbered from 0 at `at`, lie in [first, last): others become zero.  In a branch of its
 // own (the statement keeps the compiler from testing every tile).

@@ -179,15 +179,31 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
         f32x16 s = f32x16{0}, dp = f32x16{0};
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) s = mfma(Keys32<D>::rows(k_tile, k), q[k], s);
+        // the products of dP between the weights' instructions
+        constexpr int kEach = 16 / kSteps;
+        float x[16], ds[16];
+        f32x2 line[16];
+        bf16x8 v_rows = Keys32<D>::rows(v_tile, 0);
+        auto weigh = [&](int r) {
+            const float t = on_line(x[r], line[r]);
+            ds[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(t, unit, -lse2)) * __builtin_fmaf(-t, t, 1.0f);
+        };
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) dp = mfma(Keys32<D>::rows(v_tile, k), d_o[k], dp);
-        float ds[16];
+        for (int k = 0; k < kSteps; ++k) {
+            dp = mfma(v_rows, d_o[k], dp);
+            if (k + 1 < kSteps) v_rows = Keys32<D>::rows(v_tile, k + 1);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const float t = capped(s[r] * a.s.to_x, lines);
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(t, unit, -lse2));
-            ds[r] = p * (dp[r] - delta) * __builtin_fmaf(-t, t, 1.0f);
+            for (int r = k * kEach; r < (k + 1) * kEach; ++r) {
+                x[r] = s[r] * a.s.to_x;
+                line[r] = line_of(x[r], lines);
+                if (r >= kEach) weigh(r - kEach);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int r = 16 - kEach; r < 16; ++r) weigh(r);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ds[r] *= dp[r] - delta;
         if (!whole) keep(ds, Span(first_seen, last_seen, j0));
         const bf16x8 shares[2] = {pack8(ds), pack8(ds + 8)};
 #pragma unroll
