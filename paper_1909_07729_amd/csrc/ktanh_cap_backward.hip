@@ -440,11 +440,46 @@ __global__ __launch_bounds__(kThreads) void cap_join_grads_kernel(BackwardArgs a
     *reinterpret_cast<bf16x8 *>((blockIdx.y == 0 ? a.dk : a.dv) + i) = pack8(v);
 }
 
-// Blocks over the keys of a key/value head, all heads of its group one behind the other, where those blocks are many; else one head each.
-int parts_of(const kcap_shape_t &s)
+// How the blocks over keys are cut: their rows, and into how many parts the query heads that share a key/value head are dealt, each with a
+// block and sums in Float32 of its own that another kernel adds up.
+struct KeysPlan {
+    bool split;
+    int parts;
+};
+
+// The least time of all, of the block that takes longest or of all blocks with some of that one's at their end, by what a block takes for a tile alone, a compute
+// unit with all that it holds, and around its tiles, and of the parts written and read at 4.5 TB/s.  Documents may be twice as long as the average.
+// Gradients causal, 32 heads of 128 on 8, in us with four | two | one part:
+//    six documents, 8192 rows in all    723 |  716 |  963
+//    64 documents of 256                563 |  440 |  339
+//    eight documents of 2048           1451 | 1318 | 1239
+//    one of 8192                       2232 | 2251 | 2801
+//    16 of 256 (one: blocks of 32)      141 |  114 |  103
+KeysPlan keys_plan(const kcap_shape_t &s)
 {
-    const size_t group = s.heads / s.kv_heads;
-    return (s.k_rows / kRows<false> + s.docs) * s.kv_heads >= 2048 ? 1 : (int)group;
+    KeysPlan best{false, 1};
+    if (s.docs == 0 || s.kv_heads == 0 || s.heads < s.kv_heads) return best;
+    const int group = (int)(s.heads / s.kv_heads);
+    const double docs = (double)s.docs, queries = (double)s.q_rows / docs, keys = (double)s.k_rows / docs;
+    double least = 0.0;
+    for (const bool split : {false, true}) {
+        if (split && s.q_rows <= 32 * s.docs) break;  // one tile cannot be shared
+        const double rows = split ? 32.0 : 128.0, at_once = split ? 4.0 : 1.0, alone_us = split ? 2.2 : 1.6, all_us = split ? 1.6 : 1.0, around_us = split ? 12.0 : 4.0;
+        const bool narrow = s.window > 0 && (double)s.window + rows < queries;
+        const double tiles = (narrow ? (double)s.window + rows : queries) / 32.0 / at_once, mean = s.causal && !narrow ? tiles / 2.0 : tiles;
+        for (int parts = 1; parts <= group; ++parts) {
+            if (group % parts != 0) continue;
+            const double heads = group / parts, blocks = std::ceil(keys / rows) * docs * (double)s.kv_heads * parts;
+            const double longest = heads * tiles * (s.docs > 1 && !narrow ? 2.0 : 1.0) * alone_us, all = blocks * heads * mean * all_us / 256.0 + around_us * blocks / 512.0;
+            const double join = parts > 1 ? 5.0 + parts * (double)s.k_rows * (double)s.kv_heads * (double)s.dim * 16.0 / 4.5e6 : 0.0;
+            const double t = std::max(longest, all + longest / 4.0) + join;
+            if (least == 0.0 || t < least) {
+                least = t;
+                best = KeysPlan{split, parts};
+            }
+        }
+    }
+    return best;
 }
 
 size_t delta_bytes(const kcap_shape_t &s) { return (s.heads * s.q_rows * 4 + 127) / 128 * 128; }
@@ -480,15 +515,15 @@ ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t d
     a.dq = dq;
     a.dk = dk;
     a.dv = dv;
-    a.parts = parts_of(*shape);
+    const KeysPlan plan = keys_plan(*shape);
+    a.parts = plan.parts;
     const long long each = (long long)a.s.k_rows * a.s.kv_heads * dim;
     if (a.parts > 1) {
         a.dk_parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + delta_bytes(*shape));
         a.dv_parts = a.dk_parts + a.parts * each;
     }
     const bool split_keys = split_tiles(shape->q_rows, shape->k_rows, shape->docs, shape->heads);
-    const bool split_queries = split_tiles(shape->k_rows, shape->q_rows, shape->docs, shape->kv_heads * a.parts);
-    const unsigned long long q_tiles = stretches(shape->q_rows, shape->docs, split_keys), k_tiles = stretches(shape->k_rows, shape->docs, split_queries);
+    const unsigned long long q_tiles = stretches(shape->q_rows, shape->docs, split_keys), k_tiles = stretches(shape->k_rows, shape->docs, plan.split);
     const unsigned long long q_blocks = unit_blocks(q_tiles, a.s.kv_heads, 1, a.s.group) + a.s.heads;
     const unsigned long long k_blocks = unit_blocks(k_tiles, a.s.kv_heads, a.parts, 1) + (a.parts == 1 ? a.s.kv_heads : 0);
     const unsigned long long joins = (unsigned long long)(each + kThreads * 8 - 1) / (kThreads * 8);
@@ -504,7 +539,7 @@ ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t d
     }
     if (!keys) return KT_OK;
     a.tiles = (unsigned)k_tiles;
-    auto *kernel = split_queries ? dim == 64 ? &cap_dkdv_kernel<64, true> : &cap_dkdv_kernel<128, true>
+    auto *kernel = plan.split ? dim == 64 ? &cap_dkdv_kernel<64, true> : &cap_dkdv_kernel<128, true>
                             : dim == 64 ? &cap_dkdv_kernel<64, false> : &cap_dkdv_kernel<128, false>;
     kernel<<<dim3((unsigned)k_blocks), dim3(kThreads), 0, on>>>(a, pack);
     if ((st = launched()) != KT_OK) return st;
@@ -522,7 +557,7 @@ extern "C" size_t kcap_attention_backward_workspace(const kcap_shape_t *shape)
     if (shape == nullptr || shape->kv_heads == 0 || shape->heads < shape->kv_heads || shape->heads > 65536 || shape->dim > 128 ||
         shape->q_rows > 1u << 30 || shape->k_rows > 1u << 30 || shape->docs > 1u << 30)
         return 0;
-    const size_t parts = (size_t)parts_of(*shape);
+    const size_t parts = (size_t)keys_plan(*shape).parts;
     return delta_bytes(*shape) + 128 + (parts > 1 ? 2 * parts * shape->k_rows * shape->kv_heads * shape->dim * 4 : 0);
 }
 
