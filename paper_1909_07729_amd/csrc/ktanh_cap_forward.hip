@@ -2,13 +2,15 @@
 // prompts over a paged cache.
 //
 // A block holds 128 queries of one head and one document, 32 in each wavefront's registers, and goes once over the
-// keys that they see in tiles of 32, double-buffered in LDS by direct loads.
+// keys that they see in tiles of 32, double-buffered in LDS by direct loads.  Where blocks are few (SPLIT) it holds 32 queries, and each
+// wavefront goes over every fourth tile with a place in LDS of its own; the four sums are joined at the end.
 //   S^T = K Q^T (keys x queries), p = e^(cap K(x)) in the accumulator, O^T += V^T P^T with P^T as it lies.
 //
-// What bounds it: a wavefront's 16 matrix and about 150 vector instructions of a tile take some 340 ns side by side with two
-// others' (269 the matrix instructions alone), and three wavefronts share a SIMD because the tile's 32 keys and the direct loads leave
-// 160 registers enough.  16384 tokens, 32 heads of 128, causal: 2331 us, 943 TFLOP/s; with 64 keys to a tile, through registers, and
-// two wavefronts 2736; with 32 keys through registers 2620.
+// What bounds it: 16384 tokens, 32 heads of 128, causal, take 2300 us, 956 TFLOP/s.  The matrix instructions alone take 1430 (1.54 PFLOP/s, what
+// the card's clock allows a large product too), reading their operands from LDS 160 more, bringing the tiles 310, the cap, the
+// exponentials and the sums, about 130 vector instructions for 16 matrix instructions, 430.  Three wavefronts share a SIMD because the tile's 32 keys
+// and the direct loads leave 160 registers enough: with 64 keys to a tile, through registers, and two wavefronts 2736; with 32 keys through
+// registers 2620.
 #include <type_traits>
 
 #include "ktanh_cap_args.h"
