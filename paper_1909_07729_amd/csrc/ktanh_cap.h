@@ -230,7 +230,26 @@ struct Stream {
     // Loads rows at .. at + 31, which are next; the ones after begin STEP on.
     __device__ __forceinline__ void next(int at, char *a_tile, char *b_tile)
     {
-        if (at + 32 <= last + 1) {
+        const bool there = at + 32 <= last + 1;
+        // Of two stretches each chooses its addresses, eight are in the code twice: with the second form for two 16384 tokens in 32 heads of 128 take
+        // 2360 us instead of 2310, with the first for eight 2048 in 8 heads 29.7 instead of 25.9.
+        if constexpr (kShare <= 2) {
+#pragma unroll
+            for (int n = 0; n < kShare; ++n) {
+                const int g = wave * kShare + n;
+                uint32_t a_at = a_off, b_at = b_off;
+                const char *a_from = a + n * 2 * a_row, *b_from = b + n * 2 * b_row;
+                if (!there) {
+                    const uint32_t row = min(Tile::row_of_lane(g), last - at), chunk = 16 * Tile::chunk_of_lane();
+                    a_from = reinterpret_cast<const char *>(a_rows + at * a_row);
+                    b_from = reinterpret_cast<const char *>(b_rows + at * b_row);
+                    a_at = row * 2 * (uint32_t)a_row + chunk;
+                    b_at = row * 2 * (uint32_t)b_row + chunk;
+                }
+                load_direct(a_from + a_at, a_tile + Tile::stretch_at(g));
+                load_direct(b_from + b_at, b_tile + Tile::stretch_at(g));
+            }
+        } else if (there) {
 #pragma unroll
             for (int n = 0; n < kShare; ++n) {
                 const int g = wave * kShare + n;
@@ -243,9 +262,9 @@ struct Stream {
 #pragma unroll
             for (int n = 0; n < kShare; ++n) {
                 const int g = wave * kShare + n;
-                const uint32_t there = min(Tile::row_of_lane(g), last - at);
-                load_direct(a_from + (there * 2 * (uint32_t)a_row + chunk), a_tile + Tile::stretch_at(g));
-                load_direct(b_from + (there * 2 * (uint32_t)b_row + chunk), b_tile + Tile::stretch_at(g));
+                const uint32_t row = min(Tile::row_of_lane(g), last - at);
+                load_direct(a_from + (row * 2 * (uint32_t)a_row + chunk), a_tile + Tile::stretch_at(g));
+                load_direct(b_from + (row * 2 * (uint32_t)b_row + chunk), b_tile + Tile::stretch_at(g));
             }
         }
         a += STEP * 2 * a_row;
