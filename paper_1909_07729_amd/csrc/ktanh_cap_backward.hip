@@ -11,10 +11,10 @@
 // P and dS are rounded to BFloat16 where they become operands: dq and dk are then off by 0.0025 of their norm, of which 0.0017 is the
 // rounding of the results themselves.  A second term would double the instructions of three of the seven products.
 //
-// What bounds it: six documents of 8192 tokens in all, 32 heads of 128 on 8, causal: dq 301 us, dk and dv 380, their parts joined 46; 48 % of the
-// rate of the forward's products.  A tile of 32 x 32 takes 24 (32) matrix and 220 (235) vector instructions, in 198 (245) registers, so that two
-// wavefronts share a SIMD: its matrix unit is busy 33 (37) % of the time and its vector unit 40 %, and the rest is waiting for one another and for LDS, which is
-// busy 30 (42) %.  Two tiles behind one barrier, or all operands of a tile read ahead, changed less than 2 %.
+// What bounds it: six documents of 8192 tokens in all, 32 heads of 128 on 8, causal: dq 301 us, dk and dv 418 in blocks of 32
+// rows (380 in blocks of 128, and 46 to join four parts).  A tile of 32 x 32 takes 24 (32) matrix and 220 (235) vector instructions, in 198 (245) registers, so that two
+// wavefronts share a SIMD: its matrix unit is busy 30 % of the time and its vector unit 41 (31) %, and the rest is waiting for one another and for LDS, which is
+// busy 30 (37) %.  Two tiles behind one barrier, or all operands of a tile read ahead, changed less than 2 %.
 #include "ktanh_cap_args.h"
 
 using namespace ktanh_cap;

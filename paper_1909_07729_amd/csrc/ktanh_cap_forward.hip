@@ -6,7 +6,7 @@
 // wavefront goes over every fourth tile with a place in LDS of its own; the four sums are joined at the end.
 //   S^T = K Q^T (keys x queries), p = e^(cap K(x)) in the accumulator, O^T += V^T P^T with P^T as it lies.
 //
-// What bounds it: 16384 tokens, 32 heads of 128, causal, take 2300 us, 956 TFLOP/s.  The matrix instructions alone take 1430 (1.54 PFLOP/s, what
+// What bounds it: 16384 tokens, 32 heads of 128, causal, take 2310 us, 952 TFLOP/s.  The matrix instructions alone take 1430 (1.54 PFLOP/s, what
 // the card's clock allows a large product too), reading their operands from LDS 160 more, bringing the tiles 310, the cap, the
 // exponentials and the sums, about 130 vector instructions for 16 matrix instructions, 430.  Three wavefronts share a SIMD because the tile's 32 keys
 // and the direct loads leave 160 registers enough: with 64 keys to a tile, through registers, and two wavefronts 2736; with 32 keys through
