@@ -35,9 +35,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256, kWaves = 4;
-// Rows of a block: 32 for each wavefront, which go over the tiles of the other tensor together, or (SPLIT) 32 for all, each wavefront on its own
-// over every fourth tile, and their sums joined at the end.
-template <bool SPLIT> constexpr int kRows = SPLIT ? 32 : 128;
+// A wavefront has 32 rows.  The four of a block go over the tiles of the other tensor together, with 128 rows, or the same 64 or 32 rows of two or four
+// heads that share that tensor; or (SPLIT) all four have the same 32 rows, each goes over every fourth tile on its own, and their sums are joined at the end.
+constexpr int kRows = 128;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // A tensor [rows][heads][dim], dim contiguous.
@@ -300,7 +300,7 @@ __device__ __forceinline__ bool unit_of_block(unsigned block, unsigned tiles, in
     return true;
 }
 
-// A stretch of ROWS rows of a document.  There are at most rows / ROWS + documents, known without reading the offsets.
+// A stretch of 2^shift rows of a document.  There are at most rows >> shift and documents in sum, known without reading the offsets.
 // Offsets outside [0, rows] are taken as the nearest in range, so that a wrong one reads nothing out of bounds.
 struct Stretch {
     int doc, begin, end, first;  // rows of the document, and the first of the stretch; first >= end: nothing to do
@@ -350,22 +350,22 @@ __device__ __forceinline__ int lanes_before(int v, int bits)
     return sum;
 }
 
-// The stretch of ROWS rows that is the rank-th in work, the most first: blocks start in this order, and the last ones to start are
+// The stretch of 2^shift rows that is the rank-th in work, the most first: blocks start in this order, and the last ones to start are
 // short (in the order of the rows sixteen documents of 8192 tokens keep the chip 79 % busy, like this 94).  By whole wavefronts.
-// `others_of(d)`: rows of the other tensor that document d has; asked for together with the document's own.  Work, in units of ROWS: those rows if all are seen; if causal, the
+// `others_of(d)`: rows of the other tensor that document d has; asked for together with the document's own.  Work, in units of as many rows: those rows if all are seen; if causal, the
 // number of the stretch and the rows before the document's first (`rising`: queries, over keys), or its number from the end (keys, over
 // queries).  More than 64 documents stay in the order of their rows.
-template <int ROWS, class OthersOf>
-__device__ __forceinline__ Stretch stretch_of(int rank, const int *offsets, int docs, int rows, bool causal, bool rising, OthersOf others_of)
+template <class OthersOf>
+__device__ __forceinline__ Stretch stretch_of(int shift, int rank, const int *offsets, int docs, int rows, bool causal, bool rising, OthersOf others_of)
 {
     Stretch s;
     if (docs > 64) {
-        const int tile = causal && rising ? rows / ROWS + docs - 1 - rank : rank;
-        s.doc = last_document(docs, [&](int d) { return offset_at(offsets, d, rows) / ROWS + d <= tile; });
+        const int tile = causal && rising ? (rows >> shift) + docs - 1 - rank : rank;
+        s.doc = last_document(docs, [&](int d) { return (offset_at(offsets, d, rows) >> shift) + d <= tile; });
         s.begin = offset_at(offsets, s.doc, rows);
         s.end = max(offset_at(offsets, s.doc + 1, rows), s.begin);
-        const int number = tile - (s.begin / ROWS + s.doc);  // below 0: rows before the first document
-        s.first = number >= 0 ? s.begin + number * ROWS : s.end;
+        const int number = tile - ((s.begin >> shift) + s.doc);  // below 0: rows before the first document
+        s.first = number >= 0 ? s.begin + (number << shift) : s.end;
         const Others others = others_of(s.doc);
         s.other_begin = others.begin;
         s.others = others.count;
@@ -374,14 +374,14 @@ __device__ __forceinline__ Stretch stretch_of(int rank, const int *offsets, int 
     const int d = (int)(threadIdx.x & 63), my_doc = min(d, docs - 1);
     const Others others = others_of(my_doc);
     const int begin = offset_at(offsets, my_doc, rows), end = d < docs ? max(offset_at(offsets, my_doc + 1, rows), begin) : begin;
-    const int count = (end - begin + ROWS - 1) / ROWS;
+    const int up = (1 << shift) - 1, count = (end - begin + up) >> shift;
     int number;  // of the stretch in its document
     if (docs == 1) {
         s.doc = 0;
         number = causal && rising ? count - 1 - rank : rank;
         if (rank >= count) number = count;
     } else {
-        const int least = !causal ? (others.count + ROWS - 1) / ROWS : rising ? max(others.count - (end - begin), 0) / ROWS : 0;
+        const int least = !causal ? (others.count + up) >> shift : rising ? max(others.count - (end - begin), 0) >> shift : 0;
         // stretches of this document with more work than w
         auto above = [&](int w) { return causal ? min(max(least + count - 1 - w, 0), count) : least > w ? count : 0; };
         int bits = 0, top = 0;
@@ -404,7 +404,7 @@ __device__ __forceinline__ Stretch stretch_of(int rank, const int *offsets, int 
     s.doc = __builtin_amdgcn_readfirstlane(s.doc);
     s.begin = __builtin_amdgcn_readlane(begin, s.doc);
     s.end = __builtin_amdgcn_readlane(end, s.doc);
-    s.first = s.begin + __builtin_amdgcn_readlane(number, s.doc) * ROWS;
+    s.first = s.begin + (__builtin_amdgcn_readlane(number, s.doc) << shift);
     s.other_begin = __builtin_amdgcn_readlane(others.begin, s.doc);
     s.others = __builtin_amdgcn_readlane(others.count, s.doc);
     return s;

@@ -103,9 +103,13 @@ inline ktanh_status_t read_pages(const kcap_pages_t *p, const int32_t *pages, co
 //    a document of 32 rows, 8 heads of 64                                4.7 10.0 | 5.5 11.7
 inline bool split_tiles(size_t rows, size_t others, size_t docs, size_t heads)
 {
-    return (rows / kRows<false> + docs) * heads < 512 && others > 32 * docs;
+    return (rows / kRows + docs) * heads < 512 && others > 32 * docs;
 }
-inline unsigned long long stretches(size_t rows, size_t docs, bool split) { return rows / (split ? kRows<true> : kRows<false>) + docs; }
+
+// Rows of a stretch, as a power of two: of a block whose wavefronts share tiles, or of one with as many query heads of a group together as its four
+// wavefronts can have.  16 documents of 8192 tokens, 32 heads of 128 on 8: 101 us with one head, NNN with four.
+inline int rows_shift(const CapShape &s, bool split) { return split || s.group % 4 == 0 ? 5 : s.group % 2 == 0 ? 6 : 7; }
+inline unsigned long long stretches(size_t rows, size_t docs, int shift) { return (rows >> shift) + docs; }
 
 // Many queries of each sequence over the cache (ktanh_cap_forward.hip).  Where parts are above 1 the workspace holds
 // forward_sums Float32 sums and as many times dim numerators.

@@ -30,6 +30,7 @@ struct BackwardArgs {
     uint16_t *dq, *dk, *dv;     // dense
     float *dk_parts, *dv_parts; // [parts][k_rows][kv_heads][dim], NULL where one block sums all heads of a group
     unsigned tiles;
+    int shift;  // of the rows of a stretch
     int parts;
 };
 
@@ -98,7 +99,7 @@ __device__ __forceinline__ void store_row(T *row, bool there, const f32x16 (&acc
 template <int D, bool SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtCapPack pack)
 {
-    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32, kRows = ktanh_cap::kRows<SPLIT>;
+    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32;
     constexpr int kLoaders = SPLIT ? 1 : kWaves, kTiles = SPLIT ? kWaves : 1, kStep = kTile * kTiles;  // a tile's wavefronts; tiles at once
     constexpr int kBuffers = SPLIT ? 1 : 2;  // two blocks to a compute unit hide each other's loads
     struct Tiles {
@@ -114,28 +115,29 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
     __shared__ __align__(16) Shared shared;
     f32x2 *lines = shared.lines;
 
-    const unsigned blocks = (unsigned)unit_blocks(a.tiles, a.s.kv_heads, 1, a.s.group);
+    const int together = SPLIT ? 0 : 7 - a.shift, members = a.s.group >> together;  // heads of a block, as a power of two; blocks that share keys
+    const unsigned blocks = (unsigned)unit_blocks(a.tiles, a.s.kv_heads, 1, members);
     if (blockIdx.x >= blocks) {
         clear_rows<D>(a.dq, a.q_offsets, a.s.docs, a.s.q_rows, a.s.heads, (int)(blockIdx.x - blocks), [](int) {});
         return;
     }
     Unit work;
-    if (!unit_of_block(blockIdx.x, a.tiles, a.s.kv_heads, 1, a.s.group, &work)) return;
-    const int kv_head = work.kv_head, head = kv_head * a.s.group + work.member;
+    if (!unit_of_block(blockIdx.x, a.tiles, a.s.kv_heads, 1, members, &work)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kv_head = work.kv_head, head = kv_head * a.s.group + (work.member << together) + (wave & ((1 << together) - 1));
     auto keys_of = [&](int doc) { return rows_in(a.k_offsets, doc, a.s.k_rows); };
-    const Stretch at = stretch_of<kRows>(work.rank, a.q_offsets, a.s.docs, a.s.q_rows, a.s.causal, true, keys_of);
+    const Stretch at = stretch_of(a.shift, work.rank, a.q_offsets, a.s.docs, a.s.q_rows, a.s.causal, true, keys_of);
     if (at.first >= at.end) return;
     const int k_begin = at.other_begin, n_keys = at.others;
     Rows keys = of_head(a.s.k, kv_head), values = of_head(a.s.v, kv_head);
     keys.at += k_begin * keys.row;
     values.at += k_begin * values.row;
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int shift = n_keys - (at.end - at.begin);
-    const int row0 = at.first + (SPLIT ? 0 : 32 * wave), row = row0 + (lane & 31), row_there = min(row, at.end - 1);
+    const int row0 = at.first + (SPLIT ? 0 : 32 * (wave >> together)), row = row0 + (lane & 31), row_there = min(row, at.end - 1);
     const int place0 = row0 - at.begin + shift, my_place = row - at.begin + shift;
     const int block_first = at.first - at.begin + shift;
-    const int block_last = min(at.first + kRows, at.end) - 1 - at.begin + shift;
+    const int block_last = min(at.first + (1 << a.shift), at.end) - 1 - at.begin + shift;
     const int key_end = a.s.causal ? min(n_keys, block_last + 1) : n_keys;
     const int key_begin = a.s.window > 0 ? max(0, block_first - a.s.window + 1) & ~(kTile - 1) : 0;
     const int first_seen = a.s.window > 0 ? max(0, my_place - a.s.window + 1) : 0, last_seen = a.s.causal ? min(n_keys, my_place + 1) : n_keys;
@@ -238,7 +240,7 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
 template <int D, bool SPLIT>
 __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, KtCapPack pack)
 {
-    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32, kRows = ktanh_cap::kRows<SPLIT>;
+    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32;
     constexpr int kLoaders = SPLIT ? 1 : kWaves, kTiles = SPLIT ? kWaves : 1;  // a tile's wavefronts; tiles at once
     constexpr int kBuffers = SPLIT ? 1 : 2;  // two blocks to a compute unit hide each other's loads
     struct Tiles {
@@ -267,7 +269,7 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
     if (!unit_of_block(blockIdx.x, a.tiles, a.s.kv_heads, a.parts, 1, &work)) return;
     const int part = work.part, kv_head = work.kv_head;
     auto queries_of = [&](int doc) { return rows_in(a.q_offsets, doc, a.s.q_rows); };
-    const Stretch at = stretch_of<kRows>(work.rank, a.k_offsets, a.s.docs, a.s.k_rows, a.s.causal, false, queries_of);
+    const Stretch at = stretch_of(a.shift, work.rank, a.k_offsets, a.s.docs, a.s.k_rows, a.s.causal, false, queries_of);
     if (at.first >= at.end) return;
     const int q_begin = at.other_begin, n_queries = at.others;
 
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
     const int shift = (at.end - at.begin) - n_queries;  // query i is key i + shift
     const int row0 = at.first + (SPLIT ? 0 : 32 * wave), row = row0 + (lane & 31), row_there = min(row, at.end - 1);
     const int key0 = row0 - at.begin, key = row_there - at.begin;
-    const int block_first = at.first - at.begin, block_last = min(at.first + kRows, at.end) - 1 - at.begin;
+    const int block_first = at.first - at.begin, block_last = min(at.first + (1 << a.shift), at.end) - 1 - at.begin;
     // queries that see some key of the block
     const int from = a.s.causal ? max(0, block_first - shift) & ~(kTile - 1) : 0;
     const int to = a.s.window > 0 ? min((long long)n_queries, max(0ll, (long long)block_last - shift + a.s.window)) : n_queries;
@@ -531,8 +533,9 @@ ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t d
         a.dv_parts = a.dk_parts + a.parts * each;
     }
     const bool split_keys = split_tiles(shape->q_rows, shape->k_rows, shape->docs, shape->heads);
-    const unsigned long long q_tiles = stretches(shape->q_rows, shape->docs, split_keys), k_tiles = stretches(shape->k_rows, shape->docs, plan.split);
-    const unsigned long long q_blocks = unit_blocks(q_tiles, a.s.kv_heads, 1, a.s.group) + a.s.heads;
+    const int q_shift = rows_shift(a.s, split_keys), k_shift = plan.split ? 5 : 7;
+    const unsigned long long q_tiles = stretches(shape->q_rows, shape->docs, q_shift), k_tiles = stretches(shape->k_rows, shape->docs, k_shift);
+    const unsigned long long q_blocks = unit_blocks(q_tiles, a.s.kv_heads, 1, split_keys ? a.s.group : a.s.group >> (7 - q_shift)) + a.s.heads;
     const unsigned long long k_blocks = unit_blocks(k_tiles, a.s.kv_heads, a.parts, 1) + (a.parts == 1 ? a.s.kv_heads : 0);
     const unsigned long long joins = (unsigned long long)(each + kThreads * 8 - 1) / (kThreads * 8);
     if (q_blocks > kMaxBlocks || k_blocks > kMaxBlocks || joins > kMaxBlocks) return KT_ERR_SHAPE;
@@ -540,6 +543,7 @@ ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t d
     const auto on = static_cast<hipStream_t>(stream);
     if (queries) {
         a.tiles = (unsigned)q_tiles;
+        a.shift = q_shift;
         auto *kernel = split_keys ? dim == 64 ? &cap_dq_kernel<64, true> : &cap_dq_kernel<128, true>
                                    : dim == 64 ? &cap_dq_kernel<64, false> : &cap_dq_kernel<128, false>;
         kernel<<<dim3((unsigned)q_blocks), dim3(kThreads), 0, on>>>(a, pack);
@@ -547,6 +551,7 @@ ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t d
     }
     if (!keys) return KT_OK;
     a.tiles = (unsigned)k_tiles;
+    a.shift = k_shift;
     auto *kernel = plan.split ? dim == 64 ? &cap_dkdv_kernel<64, true> : &cap_dkdv_kernel<128, true>
                             : dim == 64 ? &cap_dkdv_kernel<64, false> : &cap_dkdv_kernel<128, false>;
     kernel<<<dim3((unsigned)k_blocks), dim3(kThreads), 0, on>>>(a, pack);

@@ -125,6 +125,7 @@ struct ForwardArgs {
     float *lse;
     CapPages p;
     unsigned tiles;
+    int shift;  // of the rows of a stretch
     // PAGED: blocks of a stretch that share its keys, with sums [parts][q_rows][heads] and numerators [parts][q_rows][heads][dim] in Float32
     int parts;
     float *part_sums, *part_values;
@@ -134,7 +135,7 @@ struct ForwardArgs {
 template <int D, bool PAGED, bool SUMS, bool SPLIT>
 __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(ForwardArgs a, KtCapPack pack)
 {
-    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32, kRows = ktanh_cap::kRows<SPLIT>;
+    constexpr int kBytes = Keys32<D>::kBytes, kSteps = D / 16, kBlocks = D / 32;
     constexpr int kLoaders = SPLIT ? 1 : kWaves, kTiles = SPLIT ? kWaves : 1, kStep = kKeys * kTiles;  // a tile's wavefronts; tiles at once
     constexpr int kBuffers = SPLIT ? 1 : 2;  // two blocks to a compute unit hide each other's loads
     struct Tiles {
@@ -152,7 +153,8 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
     __shared__ __align__(16) Shared shared;
     f32x2 *lines = shared.lines;
 
-    const unsigned blocks = (unsigned)unit_blocks(a.tiles, a.s.kv_heads, a.parts, a.s.group);
+    const int together = SPLIT ? 0 : 7 - a.shift, members = a.s.group >> together;  // heads of a block, as a power of two; blocks that share keys
+    const unsigned blocks = (unsigned)unit_blocks(a.tiles, a.s.kv_heads, a.parts, members);
     if (blockIdx.x >= blocks) {
         const int head = (int)(blockIdx.x - blocks);
         clear_rows<D>(a.o, a.q_offsets, a.s.docs, a.s.q_rows, a.s.heads, head, [&](int row) {
@@ -161,13 +163,15 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
         return;
     }
     Unit work;
-    if (!unit_of_block(blockIdx.x, a.tiles, a.s.kv_heads, PAGED ? a.parts : 1, a.s.group, &work)) return;
-    const int kv_head = work.kv_head, part = work.part, head = kv_head * a.s.group + work.member;
+    if (!unit_of_block(blockIdx.x, a.tiles, a.s.kv_heads, PAGED ? a.parts : 1, members, &work)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kv_head = work.kv_head, part = work.part;
+    const int head = kv_head * a.s.group + (work.member << together) + (wave & ((1 << together) - 1));
     auto keys_of = [&](int doc) {
         if constexpr (PAGED) return Others{0, keys_in_pages(a.p, doc)};
         else return rows_in(a.k_offsets, doc, a.s.k_rows);
     };
-    const Stretch at = stretch_of<kRows>(work.rank, a.q_offsets, a.s.docs, a.s.q_rows, a.s.causal, true, keys_of);
+    const Stretch at = stretch_of(a.shift, work.rank, a.q_offsets, a.s.docs, a.s.q_rows, a.s.causal, true, keys_of);
     if (at.first >= at.end) return;
 
     Keys<PAGED> keys;
@@ -188,13 +192,12 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
     keys.v_row = a.s.v.row;
     keys.last = max(n_keys - 1, 0);  // a sequence without keys looks up its first page, and reads none
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int shift = n_keys - (at.end - at.begin);            // query i is key i + shift
-    const int row0 = at.first + (SPLIT ? 0 : 32 * wave);       // this wavefront's first query
+    const int row0 = at.first + (SPLIT ? 0 : 32 * (wave >> together));       // this wavefront's first query
     const int row = row0 + (lane & 31);                        // this lane's
     const int place0 = row0 - at.begin + shift, my_place = row - at.begin + shift;
     const int block_first = at.first - at.begin + shift;
-    const int block_last = min(at.first + kRows, at.end) - 1 - at.begin + shift;
+    const int block_last = min(at.first + (1 << a.shift), at.end) - 1 - at.begin + shift;
     int key_end = a.s.causal ? min(n_keys, block_last + 1) : n_keys;
     int key_begin = a.s.window > 0 ? max(0, block_first - a.s.window + 1) & ~(kKeys - 1) : 0;
     if (PAGED && a.parts > 1) {  // this block's share of them, in whole tiles
@@ -376,7 +379,7 @@ __global__ __launch_bounds__(kThreads) void cap_join_parts_kernel(ForwardArgs a)
 template <bool PAGED, bool SUMS>
 ktanh_status_t launch_forward(const ForwardArgs &a, size_t dim, bool split, const KtCapPack &pack, ktanh_stream_t stream)
 {
-    const unsigned long long blocks = unit_blocks(a.tiles, a.s.kv_heads, a.parts, a.s.group) + (a.parts == 1 ? a.s.heads : 0);
+    const unsigned long long blocks = unit_blocks(a.tiles, a.s.kv_heads, a.parts, split ? a.s.group : a.s.group >> (7 - a.shift)) + (a.parts == 1 ? a.s.heads : 0);
     const unsigned long long joins = ((unsigned long long)a.s.q_rows * a.s.heads * dim / 4 + kThreads - 1) / kThreads;
     if (blocks > kMaxBlocks || (a.parts > 1 && joins > kMaxBlocks)) return KT_ERR_SHAPE;
     auto *kernel = split ? dim == 64 ? &cap_forward_kernel<64, PAGED, SUMS, true> : &cap_forward_kernel<128, PAGED, SUMS, true>
@@ -414,7 +417,8 @@ ktanh_status_t attention(const kcap_shape_t *shape, const uint16_t *q, const uin
     a.lse = lse;
     a.parts = 1;
     const bool split = split_tiles(shape->q_rows, shape->k_rows, shape->docs, shape->heads);
-    a.tiles = (unsigned)stretches(shape->q_rows, shape->docs, split);
+    a.shift = rows_shift(a.s, split);
+    a.tiles = (unsigned)stretches(shape->q_rows, shape->docs, a.shift);
     return lse != nullptr ? launch_forward<false, true>(a, shape->dim, split, pack, stream) : launch_forward<false, false>(a, shape->dim, split, pack, stream);
 }
 
@@ -428,12 +432,13 @@ ktanh_status_t attention(const kcap_shape_t *shape, const uint16_t *q, const uin
 ktanh_cap::ForwardPlan ktanh_cap::forward_plan(const kcap_shape_t &s, const kcap_pages_t &p)
 {
     ForwardPlan best{false, 1};
-    if (s.docs == 0 || s.q_rows == 0) return best;
+    if (s.docs == 0 || s.q_rows == 0 || s.kv_heads == 0 || s.heads < s.kv_heads) return best;
     const double docs = (double)s.docs, each = std::ceil((double)s.q_rows / docs), spread = (docs + 1.0) / (2.0 * docs);
     const double cached = (double)p.most * (double)p.page_size, part_us = (double)s.q_rows * (double)s.heads * (double)s.dim * 8.0 / 4e6;
     double least = 0.0;
     for (const bool split : {false, true}) {
-        const double rows = split ? kRows<true> : kRows<false>, blocks = std::ceil(each / rows) * docs * (double)s.heads;
+        const size_t group = s.heads / s.kv_heads, together = split ? 1 : group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
+        const double rows = split ? 32.0 : (double)(kRows / together), blocks = std::ceil(each / rows) * docs * (double)(s.heads / together);
         const double keys = s.window > 0 ? std::min(cached, (double)s.window + std::min(rows, each)) : cached;
         // Microseconds of 32 keys with 128 rows, or 128 with 32, by how many blocks a compute unit holds, up to as many as it can.
         const double full_us[4] = {0.0, 1.2, 1.45, 1.85}, split_us[3] = {0.0, 1.75, 2.6};
@@ -463,7 +468,8 @@ ktanh_status_t ktanh_cap::launch_forward_paged(const CapShape &s, const CapPages
     a.parts = plan.parts;
     a.part_sums = workspace;
     a.part_values = workspace + forward_sums(plan.parts, s.q_rows, s.heads);
-    a.tiles = (unsigned)stretches(s.q_rows, s.docs, plan.split);
+    a.shift = rows_shift(s, plan.split);
+    a.tiles = (unsigned)stretches(s.q_rows, s.docs, a.shift);
     return launch_forward<true, false>(a, (size_t)dim, plan.split, pack, stream);
 }
 
