@@ -1,5 +1,6 @@
 // Internal to libktanh: arguments of the capped-attention kernels and the checks that their entry points share.
 #pragma once
+#include <algorithm>
 #include <cmath>
 
 #include "ktanh_cap.h"
@@ -94,21 +95,36 @@ inline ktanh_status_t read_pages(const kcap_pages_t *p, const int32_t *pages, co
     return KT_OK;
 }
 
-// Whether blocks hold 32 rows, their wavefronts sharing the other tensor's tiles, rather than 128: where blocks of 128 leave compute units idle and
-// there is more than one tile to share.  Output, then gradients, causal, in us, blocks of 128 | of 32:
-//    1024 rows,  8 heads of 128, 8 key/value heads (64 blocks of 128)   38.4 103 | 16.8 40
-//    4096 rows,  8 heads of 128, 8 key/value heads (256)                 130 366 | 66 180
-//    2048 rows, 32 heads of 128, 8 key/value heads (512)                  72 222 | 76 218
-//    32 documents of 64 rows, 32 heads of 128 (1024)                      19 67 | 37 103
-//    a document of 32 rows, 8 heads of 64                                4.7 10.0 | 5.5 11.7
-inline bool split_tiles(size_t rows, size_t others, size_t docs, size_t heads)
+// Query heads of a group that a block has together.
+inline int heads_together(size_t group) { return group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1; }
+
+// Whether blocks hold 32 queries, their wavefronts sharing the tiles of keys, rather than 32 in each: the shorter time of the block that takes
+// longest, or of all blocks, by what they take for a tile alone, a compute unit with all that it holds, and around their tiles.  Documents may be twice as
+// long as the average.  Output, then gradients, causal, in us, wavefronts of their own rows | sharing the tiles:
+//    1024 rows,  8 heads of 128 on 8        36  63 |  15  39
+//    4096 rows,  8 heads of 128 on 8       128 245 |  65 179
+//    1500 rows, 32 heads of 128 on 8        51 130 |  45 128
+//    2048 rows, 32 heads of 128 on 8        68 218 |  72 229
+//    eight documents of 256, 32 heads on 8  17  50 |  39  82
+//    8192 rows,  5 heads of 128 on 1       249 561 | 144 459
+//    a document of 32 rows, 8 heads of 64  4.7 10.3 | 5.0 11.3
+inline bool split_tiles(const kcap_shape_t &s)
 {
-    return (rows / kRows + docs) * heads < 512 && others > 32 * docs;
+    if (s.k_rows <= 32 * s.docs) return false;  // one tile cannot be shared
+    const double docs = (double)s.docs, queries = (double)s.q_rows / docs, keys = (double)s.k_rows / docs;
+    const bool narrow = s.window > 0 && (double)s.window + 128.0 < keys;
+    const double seen = narrow ? (double)s.window + 128.0 : keys, mean = s.causal && !narrow ? 0.5 : 1.0, longest = docs > 1.0 && !narrow ? 2.0 : 1.0;
+    const double together = heads_together(s.heads / s.kv_heads);
+    const double own_blocks = std::ceil(queries * together / 128.0) * docs * (double)s.heads / together, own_tiles = seen / 32.0;
+    const double sharing_blocks = std::ceil(queries / 32.0) * docs * (double)s.heads, sharing_tiles = seen / 128.0;
+    return std::max(5.0 + 1.35 * longest * sharing_tiles, sharing_blocks / 256.0 * (0.85 * mean * sharing_tiles + 3.2)) <
+           std::max(3.0 + 1.03 * longest * own_tiles, own_blocks / 256.0 * (0.57 * mean * own_tiles + 3.5));
 }
 
 // Rows of a stretch, as a power of two: of a block whose wavefronts share tiles, or of one with as many query heads of a group together as its four
-// wavefronts can have.  16 documents of 8192 tokens, 32 heads of 128 on 8: 101 us with one head, NNN with four.
-inline int rows_shift(const CapShape &s, bool split) { return split || s.group % 4 == 0 ? 5 : s.group % 2 == 0 ? 6 : 7; }
+// wavefronts can have.  16 documents of 8192 tokens, 32 heads of 128 on 8: 108.7 us with one head, 102.4 with four; 4 tokens each behind up to
+// 2000 of 64 sequences 109 and 70.
+inline int rows_shift(const CapShape &s, bool split) { return split ? 5 : 7 - __builtin_ctz((unsigned)heads_together((size_t)s.group)); }
 inline unsigned long long stretches(size_t rows, size_t docs, int shift) { return (rows >> shift) + docs; }
 
 // Many queries of each sequence over the cache (ktanh_cap_forward.hip).  Where parts are above 1 the workspace holds

@@ -329,13 +329,13 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
 #pragma unroll
         for (int i = 0; i < kQuads; ++i) n[i] = f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
     }
-    if (row >= at.end) return;
-    const bool writes_sums = lane < 32 && (!SPLIT || wave == 0);
+    const bool writes_sums = lane < 32 && (!SPLIT || wave == 0) && row < at.end;
     if (SUMS && writes_sums)
         a.lse[(long long)head * a.s.q_rows + row] = sum > 0.0f ? __builtin_logf(sum) : sum == 0.0f ? -__builtin_inff() : sum;
     const int first_value = 8 * quad0 + 4 * (lane >> 5);
     if (PAGED && a.parts > 1) {
         const long long at_row = ((long long)part * a.s.q_rows + row) * a.s.heads + head;
+        if (row >= at.end) return;
         if (writes_sums) a.part_sums[at_row] = rounded_sum;
         float *values = a.part_values + at_row * D + first_value;
 #pragma unroll
@@ -343,18 +343,27 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
         return;
     }
     const float to_mean = rounded_sum == 0.0f ? 0.0f : 1.0f / rounded_sum;
-    const long long to = ((long long)row * a.s.heads + head) * D + first_value;
+    auto rounded = [&](int i) { return u32x2{pack2(n[i][0] * to_mean, n[i][1] * to_mean), pack2(n[i][2] * to_mean, n[i][3] * to_mean)}; };
+    auto dropped = [&](int i) {  // by rounding
+        const u32x2 kept = rounded(i);
+        float rest[4];
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const f32x4 w = n[i] * to_mean;
-        const u32x2 rounded = {pack2(w[0], w[1]), pack2(w[2], w[3])};
-        *reinterpret_cast<u32x2 *>(a.o + to + 8 * i) = rounded;
-        if (a.rest != nullptr) {
-            float rest[4];
+        for (int e = 0; e < 4; ++e) rest[e] = n[i][e] * to_mean - __uint_as_float(e & 1 ? kept[e / 2] & 0xFFFF0000u : kept[e / 2] << 16);
+        return u32x2{pack2(rest[0], rest[1]), pack2(rest[2], rest[3])};
+    };
+    if constexpr (SPLIT || PAGED) {  // over pages registers would spill
+        if (row >= at.end) return;
+        const long long to = ((long long)row * a.s.heads + head) * D + first_value;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) rest[e] = w[e] - __uint_as_float(e & 1 ? rounded[e / 2] & 0xFFFF0000u : rounded[e / 2] << 16);
-            *reinterpret_cast<u32x2 *>(a.rest + to + 8 * i) = u32x2{pack2(rest[0], rest[1]), pack2(rest[2], rest[3])};
+        for (int i = 0; i < kMine; ++i) {
+            *reinterpret_cast<u32x2 *>(a.o + to + 8 * i) = rounded(i);
+            if (a.rest != nullptr) *reinterpret_cast<u32x2 *>(a.rest + to + 8 * i) = dropped(i);
         }
+    } else {
+        char *tile = tiles.k[0] + wave * kBytes;  // all tiles are free since the barrier behind them
+        const long long to = ((long long)row0 * a.s.heads + head) * D, to_next = (long long)a.s.heads * D;
+        store_rows<D>(tile, a.o + to, to_next, at.end - row0, rounded);
+        if (a.rest != nullptr) store_rows<D>(tile, a.rest + to, to_next, at.end - row0, dropped);
     }
 }
 
@@ -416,7 +425,7 @@ ktanh_status_t attention(const kcap_shape_t *shape, const uint16_t *q, const uin
     a.rest = rest;
     a.lse = lse;
     a.parts = 1;
-    const bool split = split_tiles(shape->q_rows, shape->k_rows, shape->docs, shape->heads);
+    const bool split = split_tiles(*shape);
     a.shift = rows_shift(a.s, split);
     a.tiles = (unsigned)stretches(shape->q_rows, shape->docs, a.shift);
     return lse != nullptr ? launch_forward<false, true>(a, shape->dim, split, pack, stream) : launch_forward<false, false>(a, shape->dim, split, pack, stream);
@@ -437,7 +446,7 @@ ktanh_cap::ForwardPlan ktanh_cap::forward_plan(const kcap_shape_t &s, const kcap
     const double cached = (double)p.most * (double)p.page_size, part_us = (double)s.q_rows * (double)s.heads * (double)s.dim * 8.0 / 4e6;
     double least = 0.0;
     for (const bool split : {false, true}) {
-        const size_t group = s.heads / s.kv_heads, together = split ? 1 : group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
+        const size_t together = split ? 1 : (size_t)heads_together(s.heads / s.kv_heads);
         const double rows = split ? 32.0 : (double)(kRows / together), blocks = std::ceil(each / rows) * docs * (double)(s.heads / together);
         const double keys = s.window > 0 ? std::min(cached, (double)s.window + std::min(rows, each)) : cached;
         // Microseconds of 32 keys with 128 rows, or 128 with 32, by how many blocks a compute unit holds, up to as many as it can.
