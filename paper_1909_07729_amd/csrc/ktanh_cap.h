@@ -202,26 +202,30 @@ __device__ __forceinline__ void tile_complete()
     else __syncthreads();
 }
 
-// A wavefront's 32 rows of D BFloat16 values to memory by whole rows, through its `tile` of LDS: quad(i) are values 8 i + 4 (lane / 32) .. + 3 of row
-// lane & 31.  Straight from the accumulator each store touches 32 rows, 16 bytes of
-// each: 16 documents of 256 tokens, 32 heads of 128, take 46 us so, and 30 this way.
+// 32 rows of D BFloat16 values to memory by whole rows, through `tile` of LDS: a wavefront's own, or (SPLIT) the block's, of which each wavefront has a
+// fourth of the columns.  quad(i) are values 8 i + 4 (lane / 32) .. + 3 of row lane & 31, from the wavefront's first column on.  Straight from the
+// accumulator each store touches 32 rows, 16 bytes of each: 16 documents of 256 tokens, 32 heads of 128, take 46 us so, and 30 this way.
 // Chunks of 16 bytes change places with the low bits of their row's number against bank conflicts.
-template <int D, class Quad>
+template <int D, bool SPLIT, class Quad>
 __device__ __forceinline__ void store_rows(char *tile, uint16_t *to, long long row, int there, Quad quad)
 {
-    constexpr int kChunks = D / 8;
-    const int lane = threadIdx.x & 63, chunk = lane % kChunks;
+    constexpr int kChunks = D / 8, kMine = SPLIT ? kChunks / kWaves : kChunks, kLanes = SPLIT ? kThreads : 64;
+    const int lane = threadIdx.x & 63, first = SPLIT ? (int)(threadIdx.x >> 6) * kMine : 0, member = SPLIT ? (int)threadIdx.x : lane, chunk = member % kChunks;
+    auto complete = [] {
+        if constexpr (SPLIT) __syncthreads();
+        else tile_complete<true>();
+    };
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i)
-        *reinterpret_cast<u32x2 *>(tile + (lane & 31) * 2 * D + 16 * ((i ^ lane) % kChunks) + 8 * (lane >> 5)) = quad(i);
-    tile_complete<true>();
+    for (int i = 0; i < kMine; ++i)
+        *reinterpret_cast<u32x2 *>(tile + (lane & 31) * 2 * D + 16 * (((first + i) ^ lane) % kChunks) + 8 * (lane >> 5)) = quad(i);
+    complete();
 #pragma unroll
-    for (int n = 0; n < kChunks / 2; ++n) {
-        const int at = lane / kChunks + n * (64 / kChunks);
+    for (int n = 0; n < 32 * kChunks / kLanes; ++n) {
+        const int at = member / kChunks + n * (kLanes / kChunks);
         const u32x4 v = *reinterpret_cast<const u32x4 *>(tile + at * 2 * D + 16 * ((chunk ^ at) % kChunks));
         if (at < there) *reinterpret_cast<u32x4 *>(to + at * row + 8 * chunk) = v;
     }
-    tile_complete<true>();
+    complete();
 }
 
 // Tiles of 32 rows of two tensors on their way to LDS, one behind the other, and of each the stretches that wavefront `wave` of LOADERS brings;

@@ -71,37 +71,40 @@ __device__ __forceinline__ void store4(uint16_t *to, f32x4 v) { *reinterpret_cas
 __device__ __forceinline__ void store4(float *to, f32x4 v) { *reinterpret_cast<f32x4 *>(to) = v; }
 
 // An accumulator as the wavefront's rows (first `to`, `next` apart, `there` of them) of a dense tensor, times `by`.  SPLIT: the sum of all
-// wavefronts' in their order, a fourth written by each; by all threads, and `sums` is free once more behind the next barrier.  BY_ROWS: BFloat16 by way of
-// `tile`, LDS of the wavefront's own.
+// wavefronts' in their order, a fourth of the columns by each; by all threads, and `sums` is free once more behind the next barrier.  BY_ROWS: BFloat16 by
+// way of `tile`, LDS that nobody reads any more but the sums' readers.
 template <int D, bool SPLIT, bool BY_ROWS, class T, class Sums>
 __device__ __forceinline__ void store_acc(T *to, long long next, int there, const f32x16 (&acc)[D / 32], float by, Sums &sums, char *tile)
 {
     constexpr int kQuads = D / 8, kMine = SPLIT ? kQuads / kWaves : kQuads;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = SPLIT ? wave * kMine : 0;
+    if constexpr (SPLIT) {
+#pragma unroll
+        for (int i = 0; i < kQuads; ++i) sums[wave][i][lane] = quad(acc, i);
+        __syncthreads();
+    }
+    f32x4 v[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        if constexpr (SPLIT) {
+            v[i] = sums[0][first + i][lane];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) v[i] += sums[w][first + i][lane];
+        } else {
+            v[i] = quad(acc, i);
+        }
+    }
     if constexpr (BY_ROWS && sizeof(T) == 2) {
-        store_rows<D>(tile, to, next, there, [&](int i) {
-            const f32x4 v = quad(acc, i) * by;
-            return u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+        if constexpr (SPLIT) __syncthreads();
+        store_rows<D, SPLIT>(tile, to, next, there, [&](int i) {
+            const f32x4 w = v[i] * by;
+            return u32x2{pack2(w[0], w[1]), pack2(w[2], w[3])};
         });
     } else {
-        if constexpr (SPLIT) {
-#pragma unroll
-            for (int i = 0; i < kQuads; ++i) sums[wave][i][lane] = quad(acc, i);
-            __syncthreads();
-        }
         to += (lane & 31) * next + 4 * (lane >> 5);
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            f32x4 v;
-            if constexpr (SPLIT) {
-                v = sums[0][first + i][lane];
-#pragma unroll
-                for (int w = 1; w < kWaves; ++w) v += sums[w][first + i][lane];
-            } else {
-                v = quad(acc, i);
-            }
-            if ((lane & 31) < there) store4(to + 8 * (first + i), v * by);
-        }
+        for (int i = 0; i < kMine; ++i)
+            if ((lane & 31) < there) store4(to + 8 * (first + i), v[i] * by);
     }
 }
 
@@ -243,8 +246,8 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
         }
     }
     __syncthreads();
-    constexpr bool kByRows = !SPLIT && D == 128;  // at 64 its registers would leave room for three wavefronts instead of four: 8192 tokens 748 us, 730 without
-    store_acc<D, SPLIT, kByRows>(a.dq + ((long long)row0 * a.s.heads + head) * D, (long long)a.s.heads * D, at.end - row0, dq, a.s.scale, shared.sums, tiles.k[0] + wave * kBytes);
+    constexpr bool kByRows = SPLIT || D == 128;  // at 64 its registers would leave room for three wavefronts instead of four: 8192 tokens 748 us, 730 without
+    store_acc<D, SPLIT, kByRows>(a.dq + ((long long)row0 * a.s.heads + head) * D, (long long)a.s.heads * D, at.end - row0, dq, a.s.scale, shared.sums, shared.tiles[0].k[0] + (SPLIT ? 0 : wave * kBytes));
 }
 
 template <int D, bool SPLIT>
@@ -430,9 +433,9 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
     if constexpr (SPLIT) __syncthreads();
     // the wavefront's rows of values are free behind its last tile
     auto store = [&](auto *dk_to, auto *dv_to) {
-        store_acc<D, SPLIT, !SPLIT>(dk_to + first_at, to_next, at.end - row0, dk, a.s.scale, shared.sums, values);
+        store_acc<D, SPLIT, true>(dk_to + first_at, to_next, at.end - row0, dk, a.s.scale, shared.sums, values);
         if constexpr (SPLIT) __syncthreads();
-        store_acc<D, SPLIT, !SPLIT>(dv_to + first_at, to_next, at.end - row0, dv, 1.0f, shared.sums, values);
+        store_acc<D, SPLIT, true>(dv_to + first_at, to_next, at.end - row0, dv, 1.0f, shared.sums, values);
     };
     if (a.dk_parts == nullptr) {
         store(a.dk, a.dv);

@@ -351,19 +351,18 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
         for (int e = 0; e < 4; ++e) rest[e] = n[i][e] * to_mean - __uint_as_float(e & 1 ? kept[e / 2] & 0xFFFF0000u : kept[e / 2] << 16);
         return u32x2{pack2(rest[0], rest[1]), pack2(rest[2], rest[3])};
     };
-    if constexpr (SPLIT || PAGED) {  // over pages registers would spill
+    if constexpr (PAGED && !SPLIT) {  // registers would spill
         if (row >= at.end) return;
         const long long to = ((long long)row * a.s.heads + head) * D + first_value;
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            *reinterpret_cast<u32x2 *>(a.o + to + 8 * i) = rounded(i);
-            if (a.rest != nullptr) *reinterpret_cast<u32x2 *>(a.rest + to + 8 * i) = dropped(i);
-        }
+        for (int i = 0; i < kMine; ++i) *reinterpret_cast<u32x2 *>(a.o + to + 8 * i) = rounded(i);
     } else {
-        char *tile = tiles.k[0] + wave * kBytes;  // all tiles are free since the barrier behind them
+        // all tiles are free since the barrier behind them, and the sums behind this one
+        if constexpr (SPLIT) __syncthreads();
+        char *tile = shared.tiles[0].k[0] + (SPLIT ? 0 : wave * kBytes);
         const long long to = ((long long)row0 * a.s.heads + head) * D, to_next = (long long)a.s.heads * D;
-        store_rows<D>(tile, a.o + to, to_next, at.end - row0, rounded);
-        if (a.rest != nullptr) store_rows<D>(tile, a.rest + to, to_next, at.end - row0, dropped);
+        store_rows<D, SPLIT>(tile, a.o + to, to_next, at.end - row0, rounded);
+        if (a.rest != nullptr) store_rows<D, SPLIT>(tile, a.rest + to, to_next, at.end - row0, dropped);
     }
 }
 
