@@ -5,16 +5,16 @@
 //
 // 1 - t^2 is the library's derivative identity of TanH at K-TanH's value.  Scores are formed again in two kernels, each
 // summing what it owns in registers, so that no gradient is added to by two blocks and results do not depend on their order:
-//   cap_dq_kernel    128 (or 32) queries of a head, over their keys; also forms delta
-//   cap_dkdv_kernel  128 (or 32) keys of a key/value head, over the queries of the heads that share them
+//   cap_dq_kernel    32 queries for each wavefront (or for all), over their keys; also forms delta
+//   cap_dkdv_kernel  32 keys for each wavefront (or for all) of a key/value head, over the queries of the heads that share them
 //
 // P and dS are rounded to BFloat16 where they become operands: dq and dk are then off by 0.0025 of their norm, of which 0.0017 is the
 // rounding of the results themselves.  A second term would double the instructions of three of the seven products.
 //
-// What bounds it: six documents of 8192 tokens in all, 32 heads of 128 on 8, causal: dq 301 us, dk and dv 418 in blocks of 32
-// rows (380 in blocks of 128, and 46 to join four parts).  A tile of 32 x 32 takes 24 (32) matrix and 220 (235) vector instructions, in 198 (245) registers, so that two
-// wavefronts share a SIMD: its matrix unit is busy 30 % of the time and its vector unit 41 (31) %, and the rest is waiting for one another and for LDS, which is
-// busy 30 (37) %.  Two tiles behind one barrier, or all operands of a tile read ahead, changed less than 2 %.
+// What bounds it: six documents of 8192 tokens in all, 32 heads of 128 on 8, causal: dq 291 us, dk and dv 413 in blocks of 32
+// rows (380 in blocks of 128, and 46 to join four parts).  A tile of 32 x 32 takes 24 (32) matrix and 220 (235) vector instructions, in 197 (247) registers, so that two
+// wavefronts share a SIMD: its matrix unit is busy 34 (33) % of the time and its vector unit 46 (38) %, and the rest is waiting for one another and for LDS, which is
+// busy 35 (43) %.  Two tiles behind one barrier, or all operands of a tile read ahead, changed less than 2 %.
 #include "ktanh_cap_args.h"
 
 using namespace ktanh_cap;

@@ -282,7 +282,7 @@ __global__ __launch_bounds__(kJoinThreads) void cap_join_kernel(DecodeArgs a)
 }
 
 // Wavefronts: as many as the chip holds (eight to a compute unit at dim 128, twelve at 64), at most one for each tile that the table has room for.
-// 64 texts of up to 8192 tokens, with half as many, as many and more: 223, 177, 185 us with 1024, 2048, 4096 at dim 128, 112, 101, 103 with 1536, 3072, 4608 at 64.
+// 64 texts of up to 8192 tokens, with four, eight and sixteen to a compute unit 223, 177 and 185 us at dim 128, with six, twelve and eighteen 112, 101 and 103 at 64.
 struct Shares {
     unsigned long long tiles, shares, rows, row_blocks;
     Shares(const kcap_shape_t &s, const kcap_pages_t &p)
@@ -291,7 +291,7 @@ struct Shares {
         row_blocks = (group + 31) / 32;
         rows = group < 32 ? group : 32;
         tiles = ((unsigned long long)p.most * p.page_size + kKeys - 1) / kKeys * s.docs * s.kv_heads * row_blocks;
-        const unsigned long long most = s.dim == 64 ? 3072 : 2048;
+        const unsigned long long most = 256 * (s.dim == 64 ? 12 : 8);
         shares = tiles < most ? tiles : most;
     }
     // Bytes of the sums in front of the numerators, which start on a cache line.

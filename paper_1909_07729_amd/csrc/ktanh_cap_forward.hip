@@ -1,12 +1,12 @@
 // libktanh: attention with scores capped through K-TanH over many queries: packed documents, and pieces of
 // prompts over a paged cache.
 //
-// A block holds 128 queries of one head and one document, 32 in each wavefront's registers, and goes once over the
-// keys that they see in tiles of 32, double-buffered in LDS by direct loads.  Where blocks are few (SPLIT) it holds 32 queries, and each
-// wavefront goes over every fourth tile with a place in LDS of its own; the four sums are joined at the end.
+// A wavefront holds 32 queries in its registers, a block 128 of one document, or the same 64 or 32 of two or four heads that share keys, and
+// goes once over the keys that they see in tiles of 32, double-buffered in LDS by direct loads.  Where blocks are few (SPLIT) all
+// four wavefronts hold the same 32 queries of one head, each goes over every fourth tile with a place in LDS of its own, and the four sums are joined at the end.
 //   S^T = K Q^T (keys x queries), p = e^(cap K(x)) in the accumulator, O^T += V^T P^T with P^T as it lies.
 //
-// What bounds it: 16384 tokens, 32 heads of 128, causal, take 2310 us, 952 TFLOP/s.  The matrix instructions alone take 1430 (1.54 PFLOP/s, what
+// What bounds it: 16384 tokens, 32 heads of 128, causal, take 2290 us, 960 TFLOP/s.  The matrix instructions alone take 1430 (1.54 PFLOP/s, what
 // the card's clock allows a large product too), reading their operands from LDS 160 more, bringing the tiles 310, the cap, the
 // exponentials and the sums, about 130 vector instructions for 16 matrix instructions, 430.  Three wavefronts share a SIMD because the tile's 32 keys
 // and the direct loads leave 160 registers enough: with 64 keys to a tile, through registers, and two wavefronts 2736; with 32 keys through
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
         for (int e = 0; e < 4; ++e) rest[e] = n[i][e] * to_mean - __uint_as_float(e & 1 ? kept[e / 2] & 0xFFFF0000u : kept[e / 2] << 16);
         return u32x2{pack2(rest[0], rest[1]), pack2(rest[2], rest[3])};
     };
-    if constexpr (PAGED && !SPLIT) {  // registers would spill
+    if constexpr (PAGED && !SPLIT) {  // by whole rows 33 registers would spill
         if (row >= at.end) return;
         const long long to = ((long long)row * a.s.heads + head) * D + first_value;
 #pragma unroll
