@@ -228,6 +228,28 @@ __device__ __forceinline__ void store_rows(char *tile, uint16_t *to, long long r
     complete();
 }
 
+// The same of a wavefront's D Float32 values, in two halves: `tile` has 64 D bytes, as for the other.
+template <int D, class Quad>
+__device__ __forceinline__ void store_rows_wide(char *tile, float *to, long long row, int there, Quad quad)
+{
+    constexpr int kChunks = D / 8, kQuads = D / 16;  // of half a row
+    const int lane = threadIdx.x & 63, chunk = lane % kChunks;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int i = 0; i < kQuads; ++i)
+            *reinterpret_cast<f32x4 *>(tile + (lane & 31) * 2 * D + 16 * (((2 * i + (lane >> 5)) ^ lane) % kChunks)) = quad(kQuads * half + i);
+        tile_complete<true>();
+#pragma unroll
+        for (int n = 0; n < kChunks / 2; ++n) {
+            const int at = lane / kChunks + n * (64 / kChunks);
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(tile + at * 2 * D + 16 * ((chunk ^ at) % kChunks));
+            if (at < there) *reinterpret_cast<f32x4 *>(to + at * row + D / 2 * half + 4 * chunk) = v;
+        }
+        tile_complete<true>();
+    }
+}
+
 // Tiles of 32 rows of two tensors on their way to LDS, one behind the other, and of each the stretches that wavefront `wave` of LOADERS brings;
 // a row behind the last one is read as the last.  One address for all lanes and 32 bits of offset for each (strides are below 2^24).
 template <int D, int LOADERS, int STEP = 32>

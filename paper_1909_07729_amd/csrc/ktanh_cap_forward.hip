@@ -334,12 +334,16 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
         a.lse[(long long)head * a.s.q_rows + row] = sum > 0.0f ? __builtin_logf(sum) : sum == 0.0f ? -__builtin_inff() : sum;
     const int first_value = 8 * quad0 + 4 * (lane >> 5);
     if (PAGED && a.parts > 1) {
-        const long long at_row = ((long long)part * a.s.q_rows + row) * a.s.heads + head;
-        if (row >= at.end) return;
-        if (writes_sums) a.part_sums[at_row] = rounded_sum;
-        float *values = a.part_values + at_row * D + first_value;
+        const long long at_row = ((long long)part * a.s.q_rows + row0) * a.s.heads + head;
+        if (writes_sums) a.part_sums[at_row + (long long)(lane & 31) * a.s.heads] = rounded_sum;
+        if constexpr (SPLIT) {
+            if (row >= at.end) return;
+            float *values = a.part_values + (at_row + (long long)(lane & 31) * a.s.heads) * D + first_value;
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) *reinterpret_cast<f32x4 *>(values + 8 * i) = n[i];
+            for (int i = 0; i < kMine; ++i) *reinterpret_cast<f32x4 *>(values + 8 * i) = n[i];
+        } else {
+            store_rows_wide<D>(shared.tiles[0].k[0] + wave * kBytes, a.part_values + at_row * D, (long long)a.s.heads * D, at.end - row0, [&](int i) { return n[i]; });
+        }
         return;
     }
     const float to_mean = rounded_sum == 0.0f ? 0.0f : 1.0f / rounded_sum;
