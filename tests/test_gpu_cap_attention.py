@@ -444,6 +444,22 @@ def test_pieces_of_prompts_in_blocks_of_128_rows(gpu):
     test_pieces_of_prompts_over_pages(gpu, 8, 384, 3, 128, 33)
 
 
+@pytest.mark.parametrize("heads,kv_heads,dim,lengths", [(96, 4, 64, [1400, 600]), (96, 4, 128, [1400, 100]), (63, 7, 128, [2400, 131])])
+def test_pieces_of_prompts_whose_keys_are_shared_out(gpu, heads, kv_heads, dim, lengths):
+    """Few stretches of many rows behind long texts: blocks of 128 rows take parts of the keys, some of them empty in the shorter text."""
+    binding, _, torch = gpu
+    new = [130, 132]
+    (k, v, pages), each = _cache(torch, 43, lengths, 16, kv_heads, dim)
+    at, at_np = _offsets(torch, new)
+    q64 = _grid(np.random.default_rng(44), (sum(new), heads, dim), 2.0)
+    options = dict(cap=32.0, scale=dim ** -0.5)
+    o = binding.kcap_attention_paged(_bf16(torch, q64), k, v, pages, torch.tensor(lengths, dtype=torch.int32, device="cuda"), at, **options)
+    for s, (ks, vs) in enumerate(each):
+        rows = slice(at_np[s], at_np[s + 1])
+        want = kcap_oracle.attention(q64[rows], ks, vs, [0, new[s]], [0, len(ks)], **options)
+        _near(o[rows], want["o"], want["o_off"], f"sequence {s}")
+
+
 def test_wide_tables_and_layouts_of_the_cache(gpu):
     """64 intervals; heads before slots in a page, keys and values in one tensor, a table wider than its rows."""
     binding, _, torch = gpu
