@@ -71,8 +71,8 @@ __device__ __forceinline__ void store4(uint16_t *to, f32x4 v) { *reinterpret_cas
 __device__ __forceinline__ void store4(float *to, f32x4 v) { *reinterpret_cast<f32x4 *>(to) = v; }
 
 // An accumulator as the wavefront's rows (first `to`, `next` apart, `there` of them) of a dense tensor, times `by`.  SPLIT: the sum of all
-// wavefronts' in their order, a fourth of the columns by each; by all threads, and `sums` is free once more behind the next barrier.  BY_ROWS: BFloat16 by
-// way of `tile`, LDS that nobody reads any more but the sums' readers.
+// wavefronts' in their order, a fourth of the columns by each; by all threads, and `sums` is free once more behind the next barrier.  BY_ROWS: by way of `tile`, LDS
+// that nobody reads any more but the sums' readers.
 template <int D, bool SPLIT, bool BY_ROWS, class T, class Sums>
 __device__ __forceinline__ void store_acc(T *to, long long next, int there, const f32x16 (&acc)[D / 32], float by, Sums &sums, char *tile)
 {
@@ -100,6 +100,8 @@ __device__ __forceinline__ void store_acc(T *to, long long next, int there, cons
             const f32x4 w = v[i] * by;
             return u32x2{pack2(w[0], w[1]), pack2(w[2], w[3])};
         });
+    } else if constexpr (BY_ROWS && !SPLIT) {
+        store_rows_wide<D>(tile, to, next, there, [&](int i) { return v[i] * by; });
     } else {
         to += (lane & 31) * next + 4 * (lane >> 5);
 #pragma unroll
