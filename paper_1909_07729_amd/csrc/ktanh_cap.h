@@ -33,6 +33,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_at8 __attribute__((ext_vector_type(4), aligned(8)));  // 16 bytes anywhere that eight may be
 
 constexpr int kThreads = 256, kWaves = 4;
 // A wavefront has 32 rows.  The four of a block go over the tiles of the other tensor together, with 128 rows, or the same 64 or 32 rows of two or four
@@ -223,7 +224,7 @@ __device__ __forceinline__ void store_rows(char *tile, uint16_t *to, long long r
     for (int n = 0; n < 32 * kChunks / kLanes; ++n) {
         const int at = member / kChunks + n * (kLanes / kChunks);
         const u32x4 v = *reinterpret_cast<const u32x4 *>(tile + at * 2 * D + 16 * ((chunk ^ at) % kChunks));
-        if (at < there) *reinterpret_cast<u32x4 *>(to + at * row + 8 * chunk) = v;
+        if (at < there) *reinterpret_cast<u32x4_at8 *>(to + at * row + 8 * chunk) = v;
     }
     complete();
 }

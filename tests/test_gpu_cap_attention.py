@@ -444,6 +444,22 @@ def test_pieces_of_prompts_in_blocks_of_128_rows(gpu):
     test_pieces_of_prompts_over_pages(gpu, 8, 384, 3, 128, 33)
 
 
+@pytest.mark.parametrize("heads", [4, 512])
+def test_outputs_that_start_off_a_16_byte_line(gpu, heads):
+    """Outputs need eight bytes only, with few heads and with many, and nothing next to them is written."""
+    binding, _, torch = gpu
+    (q, k, v), _ = _inputs(torch, 45, 133, 133, heads, 2, 64)
+    at, _ = _offsets(torch, [100, 33])
+    want_rest = torch.empty_like(q)
+    want, _ = binding.kcap_attention(q, k, v, at, cap=50.0, rest=want_rest)
+    rooms = [torch.full((q.numel() + 16,), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    out, rest = (room[4:4 + q.numel()].view(q.shape) for room in rooms)
+    assert out.data_ptr() % 16 == 8
+    binding.kcap_attention(q, k, v, at, cap=50.0, out=out, rest=rest)
+    assert torch.equal(out, want) and torch.equal(rest, want_rest)
+    assert all((room[:4] == 7).all() and (room[4 + q.numel():] == 7).all() for room in rooms)
+
+
 @pytest.mark.parametrize("heads,kv_heads,dim,lengths", [(96, 4, 64, [1400, 600]), (96, 4, 128, [1400, 100]), (63, 7, 128, [2400, 131])])
 def test_pieces_of_prompts_whose_keys_are_shared_out(gpu, heads, kv_heads, dim, lengths):
     """Few stretches of many rows behind long texts: blocks of 128 rows take parts of the keys, some of them empty in the shorter text."""
