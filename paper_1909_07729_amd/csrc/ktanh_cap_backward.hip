@@ -432,8 +432,13 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
         advance(now);
     }
     const long long first_at = ((long long)row0 * a.s.kv_heads + kv_head) * D, to_next = (long long)a.s.kv_heads * D;
-    if constexpr (SPLIT) __syncthreads();
-    // the wavefront's rows of values are free behind its last tile
+    // The wavefront's rows of values are free behind its last tile.  A block that no query sees has had none, and has not waited for those rows yet.
+    if constexpr (SPLIT) {
+        __syncthreads();
+    } else {
+        wait_for_loads();
+        tile_complete<true>();
+    }
     auto store = [&](auto *dk_to, auto *dv_to) {
         store_acc<D, SPLIT, true>(dk_to + first_at, to_next, at.end - row0, dk, a.s.scale, shared.sums, values);
         if constexpr (SPLIT) __syncthreads();

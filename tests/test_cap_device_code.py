@@ -77,3 +77,66 @@ def test_what_is_read_once_is_read_with_the_streaming_hint(kernels):
     for name in ("cap_decode_kernel", "cap_append_kernel"):
         for n, (code, _, _) in _of(kernels, name).items():
             assert re.search(r"global_load_dwordx4 .* nt", code), n
+
+
+def _writes_before_loads_arrive(code):
+    """Blocks of the code with four or more wide LDS writes (tensors that leave through LDS) that some path enters with a direct load on its way."""
+    blocks, starts = [], {}
+    for line in code.splitlines():
+        text = line.split(";")[0].strip()
+        label = re.match(r"(\.LBB\d+_\d+):", text)
+        if label or not blocks:
+            blocks.append([])
+        if label:
+            starts[label.group(1)] = len(blocks) - 1
+        elif text:
+            blocks[-1].append(text)
+            if re.match(r"s_c?branch", text):
+                blocks.append([])
+    follows = []
+    for i, block in enumerate(blocks):
+        last = block[-1] if block else ""
+        to = [i + 1] if i + 1 < len(blocks) and not re.match(r"s_(branch|endpgm)", last) else []
+        jump = re.match(r"s_c?branch\w*\s+(\S+)", last)
+        follows.append(to + ([starts[jump.group(1)]] if jump else []))
+
+    def run(block, coming):
+        """(whether a load may be on its way behind the block, whether it is at a tensor's write)"""
+        writes = [i for i, text in enumerate(block) if re.match(r"ds_write\w*_b(64|128)", text)]
+        early = False
+        for i, text in enumerate(block):
+            if text.startswith("global_load_lds"):
+                coming = True
+            elif re.match(r"s_waitcnt.*vmcnt\(0\)", text):
+                coming = False
+            elif i in writes and len(writes) >= 4 and coming:
+                early = True
+        return coming, early
+    entered, work, found = {0: False}, [0], set()
+    while work:
+        i = work.pop()
+        coming, early = run(blocks[i], entered[i])
+        if early:
+            found.add(i)
+        for to in follows[i]:
+            if to not in entered or coming and not entered[to]:
+                entered[to] = coming
+                work.append(to)
+    return found
+
+
+def test_values_have_arrived_before_their_place_is_written(kernels):
+    """Blocks of 128 keys keep their values in LDS, and write their gradients through that place.  Where no query sees the block there is no tile
+    whose wait would cover the values' loads; a load that lands behind the writes would be stored as a gradient."""
+    found = _of(kernels, "cap_dkdv_kernel")
+    plain = {n: code for n, (code, _, _) in found.items() if "Lb0EE" in n}
+    assert len(plain) == 2
+    for n, code in plain.items():
+        assert not _writes_before_loads_arrive(code), n
+
+
+def test_the_reading_of_late_loads_finds_them():
+    """The check above on code that has the fault on one of two paths, and on code that waits on both."""
+    writes = "\n".join(["  ds_write_b64 v1, v[2:3]"] * 4)
+    code = "  global_load_lds_dwordx4 v[0:1], off\n  s_cbranch_scc1 .LBB0_2\n  s_waitcnt vmcnt(0)\n.LBB0_2:\n{}" + writes + "\n  s_endpgm\n"
+    assert _writes_before_loads_arrive(code.format("")) and not _writes_before_loads_arrive(code.format("  s_waitcnt vmcnt(0) lgkmcnt(0)\n"))
