@@ -62,6 +62,8 @@ __device__ __forceinline__ bf16x8 pack8(const float *v)
     return __builtin_bit_cast(bf16x8, u32x4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])});
 }
 
+__device__ __forceinline__ float sum_of(bf16x2 pair, float sum) { return __builtin_amdgcn_fdot2_f32_bf16(pair, __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false); }
+
 // The same, with the sum of the rounded values.  Outputs are divided by the sum of the weights as the product has them: the
 // roundings of one weight in numerator and denominator cancel (o is off by 0.0018 of its norm instead of 0.0023, 0.0017 of it the
 // rounding of o itself).
@@ -71,7 +73,7 @@ __device__ __forceinline__ bf16x8 pack8(const float *v, float *sum)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const bf16x2 pair = __builtin_convertvector(f32x2{v[2 * i], v[2 * i + 1]}, bf16x2);
-        *sum = __builtin_amdgcn_fdot2_f32_bf16(pair, __builtin_bit_cast(bf16x2, 0x3F803F80u), *sum, false);
+        *sum = sum_of(pair, *sum);
         w[i] = __builtin_bit_cast(uint32_t, pair);
     }
     return __builtin_bit_cast(bf16x8, w);

@@ -5,8 +5,9 @@
 // and none waits for a first load but at its start.  A wavefront works for up to 32 query heads that share keys, with the tile in LDS of its
 // own (no barriers), the next one on its way in registers and the pages of the one behind it looked up.  Weights need no
 // maximum (|y| <= cap), so what several wavefronts have of a sequence is joined by adding numerators and denominators; a
-// sequence within one share is finished there.  Weights go into the product as two BFloat16 terms, 16 bits in all: the matrix unit idles, so the
-// second term costs nothing, and the output is as far off as its own rounding.
+// sequence within one share is finished there.  Weights go into the product as two BFloat16 terms, 15 bits in all: the matrix unit idles, so the
+// second term costs nothing, and the output is as far off as its own rounding.  Both terms have the weight's sign: of opposite ones, or with a zero
+// among them, an infinite value would come out as NaN.
 //
 // What bounds it: memory.  64 texts of up to 8192 tokens, 32 heads of 128 on 8: 1.04 GB in 177 us, 5.9 TB/s (a wide read of as much memory reaches 6.9); two of
 // 131071: 174 us, 6.2.  One text of 777 tokens: 10 us, half of it the second launch.
@@ -186,13 +187,20 @@ __global__ __launch_bounds__(64, 2) void cap_decode_kernel(DecodeArgs a, KtCapPa
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(capped(s[r] * a.s.to_x, lines));
         if (j0 < now.first || j0 + kKeys > now.n_keys) keep(p, Span(now.first, now.n_keys, j0));
+        // The matrix units wait for memory here: weights go in as two BFloat16 values each, 15 bits of them at least, and are summed as they go in.
+        // Both are positive where the weight is, so that an infinite value stays one: the first is the weight cut off, the second
+        // what is left of 1 + 2^-16 times it, and never zero.
+        u32x4 cut[2];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum += p[r];
-        // The matrix units wait for memory here: weights go in as two BFloat16 values each, 16 bits of them.
-        const bf16x8 weights[2] = {pack8(p), pack8(p + 8)};
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t pair = __builtin_amdgcn_perm(__float_as_uint(p[2 * i + 1]), __float_as_uint(p[2 * i]), 0x07060302u);  // the high halves
+            sum = sum_of(__builtin_bit_cast(bf16x2, pair), sum);
+            cut[i / 4][i % 4] = pair;
+        }
+        const bf16x8 weights[2] = {__builtin_bit_cast(bf16x8, cut[0]), __builtin_bit_cast(bf16x8, cut[1])};
 #pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] -= (float)weights[r / 8][r % 8];
-        const bf16x8 rests[2] = {pack8(p), pack8(p + 8)};
+        for (int r = 0; r < 16; ++r) p[r] = __builtin_fmaf(p[r], 1.0f + 0x1p-16f, -__uint_as_float(__float_as_uint(p[r]) & 0xFFFF0000u));
+        const bf16x8 rests[2] = {pack8(p, &sum), pack8(p + 8, &sum)};
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll

@@ -439,6 +439,34 @@ def test_single_tokens_over_pages(gpu, lengths, page, heads, kv_heads, dim, wind
         _near(o[s:s + 1], want["o"], want["o_off"], f"sequence {s}")
 
 
+@pytest.mark.parametrize("window", [0, 50])
+@pytest.mark.parametrize("cap,spread", [(32.0, 2.0), (64.0, 4.0), (64.0, 0.0)])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(8, 2, 128), (40, 1, 64)])
+def test_single_tokens_that_see_infinities(gpu, heads, kv_heads, dim, cap, spread, window):
+    """A value that is infinite or NaN reaches its column of the rows that see it, as itself: weights are positive, whatever they are (all of them
+    exactly 1 where spread is 0).  In texts of one share and of many, beside ones that a window hides; as pieces of one token too."""
+    binding, _, torch = gpu
+    lengths = [1, 40, 300, 3000, 129]
+    (k, v, pages), each = _cache(torch, 48, lengths, 16, kv_heads, dim, spread=spread)
+    rng = np.random.default_rng(49)
+    for s, n in enumerate(lengths):
+        for j in {n - 1, n // 2, max(n - 45, 0), 0}:
+            for value in (np.inf, -np.inf, np.nan):
+                head, columns = rng.integers(kv_heads), rng.integers(0, dim, 3)
+                v[pages[s, j // 16].item(), j % 16, head, torch.from_numpy(columns).cuda()] = value
+                each[s][1][j, head, columns] = value
+    q64 = _grid(rng, (len(lengths), heads, dim), spread)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    options = dict(cap=cap, scale=dim ** -0.5, window=window)
+    one = torch.arange(len(lengths) + 1, dtype=torch.int32, device="cuda")
+    for what, o in (("single", binding.kcap_attention_paged(_bf16(torch, q64), k, v, pages, n, **options)),
+                    ("pieces", binding.kcap_attention_paged(_bf16(torch, q64), k, v, pages, n, one, **options))):
+        for s, (ks, vs) in enumerate(each):
+            want = kcap_oracle.attention(q64[s:s + 1], ks, vs, [0, 1], [0, len(ks)], **options)
+            assert np.isinf(want["o"]).any() and np.isnan(want["o"]).any()
+            _near(o[s:s + 1], want["o"], want["o_off"], f"{what}, sequence {s}")
+
+
 @pytest.mark.parametrize("window", [0, 45])
 @pytest.mark.parametrize("page", [8, 128])
 @pytest.mark.parametrize("heads,kv_heads,dim", [(4, 2, 128), (3, 1, 64)])
