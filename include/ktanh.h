@@ -336,7 +336,8 @@ typedef struct kcap_shape {
  *   o    device, out: BFloat16 [q_rows][heads][dim], dense; rows in no document become 0
  *   rest device, out, may be NULL: like o, what its rounding dropped, rounded: training keeps it for the gradients
  *   lse  device, out, may be NULL: Float32 [heads][q_rows], log of the sum of e^y (kcap_attention_backward reads it)
- * q, k, v 16-byte aligned, o and rest 8-byte (KT_ERR_ALIGN).  q_rows == 0 or docs == 0 returns KT_OK without a launch.
+ * q, k, v 16-byte aligned, o and rest 8-byte (KT_ERR_ALIGN).  q_rows == 0 or docs == 0 returns KT_OK without a launch;
+ * without documents the outputs stay as they are, here and in the other calls of attention (`binding` fills them).
  * KT_ERR_SHAPE: another dim, heads not a multiple of kv_heads, a cap or scale out of range, more than 2^30 rows.
  * KT_ERR_LUT: also a table whose K exceeds 1. */
 ktanh_status_t kcap_attention(const kcap_shape_t *shape, const uint16_t *q, const uint16_t *k, const uint16_t *v,

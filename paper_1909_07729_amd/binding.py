@@ -626,6 +626,14 @@ def _empty(shape, dtype, like, stream):
         return torch.empty(shape, dtype=dtype, device=like.device)
 
 
+def _of_no_document(stream, *tensors, value=0.0):
+    """Results where there are no documents, for which the library launches nothing: all rows are rows of none."""
+    with torch.cuda.stream(stream):
+        for t in tensors:
+            if t is not None:
+                t.fill_(value)
+
+
 def _dense_out(t, what, shape, dtypes):
     _check(t, dtypes, what)
     if tuple(t.shape) != tuple(shape):
@@ -664,6 +672,9 @@ def kcap_attention(q, k, v, q_offsets, k_offsets=None, *, cap, scale=None, causa
                                          out.data_ptr(), None if rest is None else rest.data_ptr(), lse.data_ptr(), _lut_arg(lut), _stream_handle(stream))
     if st != 0:
         raise KtanhError(st, _entry)
+    if docs == 0:
+        _of_no_document(stream, out, rest)
+        _of_no_document(stream, lse, value=-float("inf"))
     return out, lse
 
 
@@ -698,6 +709,8 @@ def kcap_attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets=None, 
                               dv.data_ptr(), workspace.data_ptr(), _lut_arg(lut), _stream_handle(stream))
     if st != 0:
         raise KtanhError(st, _entry)
+    if docs == 0:
+        _of_no_document(stream, dq, dk, dv)
     return dq, dk, dv
 
 
@@ -758,6 +771,8 @@ def kcap_attention_paged(q, k_cache, v_cache, pages, lengths, q_offsets=None, *,
                               None if workspace is None else workspace.data_ptr(), _lut_arg(lut), _stream_handle(stream))
     if st != 0:
         raise KtanhError(st, _entry)
+    if docs == 0:
+        _of_no_document(stream, out)
     return out
 
 

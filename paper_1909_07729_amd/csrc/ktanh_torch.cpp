@@ -531,6 +531,9 @@ const Tensor *int32_of(PyObject *o, int64_t count)
     return t != nullptr && t->dim() == 1 && t->numel() == count ? t : nullptr;
 }
 
+// Offsets of one document or more: calls without any launch nothing, and the Python code fills their results.
+bool has_documents(const Tensor &offsets) { return offsets.dim() == 1 && offsets.numel() > 1; }
+
 // A given output, or null in *t for None; false if it is not one.
 bool output_of(PyObject *o, at::ScalarType type, at::IntArrayRef sizes, const Tensor **t)
 {
@@ -605,7 +608,7 @@ PyObject *cap_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     if (nargs != 14 || !ordinary_thread()) Py_RETURN_NONE;
     const bool wide = args[13] == Py_True;
     const Tensor *q = rows_of(args[0], 3), *k = rows_of(args[1], 3), *v = rows_of(args[2], 3), *q_offsets = tensor_of(args[3], at::kInt);
-    if (q == nullptr || k == nullptr || v == nullptr || q_offsets == nullptr || q_offsets->dim() != 1 || q_offsets->numel() < 1) Py_RETURN_NONE;
+    if (q == nullptr || k == nullptr || v == nullptr || q_offsets == nullptr || !has_documents(*q_offsets)) Py_RETURN_NONE;
     const int64_t docs = q_offsets->numel() - 1;
     const Tensor *k_offsets = int32_of(args[4], docs + 1);
     CapOptions options;
@@ -654,7 +657,7 @@ bool offsets_of(PyObject *o, const Tensor &q, const Tensor **t, int64_t *docs)
     *docs = q.size(0);
     if (o == Py_None) return true;
     *t = tensor_of(o, at::kInt);
-    if (*t == nullptr || (*t)->dim() != 1 || (*t)->numel() < 1) return false;
+    if (*t == nullptr || !has_documents(**t)) return false;
     *docs = (*t)->numel() - 1;
     return true;
 }
@@ -785,7 +788,7 @@ PyObject *train_cap_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     HANDLE_TH_ERRORS
     if (nargs != 10 || !ordinary_thread()) Py_RETURN_NONE;
     const Tensor *q = rows_of(args[0], 3), *k = rows_of(args[1], 3), *v = rows_of(args[2], 3), *q_offsets = tensor_of(args[3], at::kInt);
-    if (q == nullptr || k == nullptr || v == nullptr || q_offsets == nullptr || q_offsets->dim() != 1 || q_offsets->numel() < 1) Py_RETURN_NONE;
+    if (q == nullptr || k == nullptr || v == nullptr || q_offsets == nullptr || !has_documents(*q_offsets)) Py_RETURN_NONE;
     const Tensor *k_offsets = int32_of(args[4], q_offsets->numel());
     CapOptions options;
     kcap_shape_t shape;

@@ -754,3 +754,49 @@ def test_refusals(gpu):
         binding.kcap_append(q, k, v, *good, pages, n, cos=cos, sin=cos[:3])
     empty = binding.kcap_attention(q[:0], k[:0], v[:0], torch.zeros(1, dtype=torch.int32, device="cuda"), cap=50.0)
     assert empty[0].shape == (0, 4, 64) and empty[1].shape == (4, 0)
+
+
+# ------------------------------------------------------------------------------------- no documents
+
+
+def test_rows_without_any_document(gpu):
+    """Offsets of no document at all beside tensors that have rows: all of them are rows of no document, and their results are zero."""
+    binding, autograd, torch = gpu
+    (q, k, v), _ = _inputs(torch, 50, 70, 90, 4, 2, 64)
+    none = torch.zeros(1, dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+
+    def held(shape, dtype=torch.bfloat16):
+        return torch.full(shape, 7.0, dtype=dtype, device="cuda")
+    for attend, backward in ((binding.kcap_attention, binding.kcap_attention_backward), (binding.kcap_attention64, binding.kcap_attention64_backward)):
+        for stream in (None, side):
+            side.wait_stream(torch.cuda.current_stream())
+            out, lse, rest = held(q.shape), held((4, 70), torch.float32), held(q.shape)
+            side.wait_stream(torch.cuda.current_stream())
+            o, sums = attend(q, k, v, none, cap=50.0, out=out, lse=lse, rest=rest, stream=stream)
+            torch.cuda.synchronize()
+            assert o is out and sums is lse and not o.any() and not rest.any() and (lse == -float("inf")).all()
+            grads = [held(t.shape) for t in (q, k, v)]
+            side.wait_stream(torch.cuda.current_stream())
+            got = backward(held(q.shape), q, k, v, o, lse, none, cap=50.0, dq=grads[0], dk=grads[1], dv=grads[2], rest=rest, stream=stream)
+            torch.cuda.synchronize()
+            assert all(a is b and not a.any() for a, b in zip(got, grads))
+    for intervals in (32, 64):
+        leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+        o = autograd.kcap_attention(*leaves, none, cap=50.0, intervals=intervals)
+        assert not o.any() and not any(t.any() for t in torch.autograd.grad(o, leaves, torch.ones_like(o)))
+    cache = torch.ones((4, 16, 2, 64), dtype=torch.bfloat16, device="cuda")
+    pages, lengths = torch.zeros((0, 3), dtype=torch.int32, device="cuda"), none[:0]
+    for paged in (binding.kcap_attention_paged, binding.kcap_attention64_paged):
+        for stream in (None, side):
+            out = held(q.shape)
+            side.wait_stream(torch.cuda.current_stream())
+            assert paged(q, cache, cache, pages, lengths, none, cap=50.0, out=out, stream=stream) is out
+            torch.cuda.synchronize()
+            assert not out.any()
+        assert not paged(q, cache, cache, pages, lengths, none, cap=50.0).any()
+    assert paged(q[:0], cache, cache, pages, lengths, cap=50.0).shape == (0, 4, 64)
+    cos = torch.ones((16, 32), device="cuda")
+    turned = held(q.shape)          # rows of no sequence are left as they are
+    binding.kcap_append(q, k[:70], v[:70], cache, cache, pages, lengths, none, cos=cos, sin=cos, out=turned)
+    assert (turned == 7).all() and (cache == 1).all()
