@@ -306,7 +306,10 @@ ktanh_status_t klstm_cell64_backward(const uint16_t *gates, const float *c_prev,
  * q . k and the weights are Float32; the weights are rounded to BFloat16 for the product with the values, whose
  * sum is Float32 and is divided by the sum of the rounded weights (the log-sum is that of the weights before); outputs are rounded to
  * nearest even.  Since |y| <= cap <= KCAP_MAX no maximum is
- * subtracted; the sums of e^y v must stay within Float32, which they do at any cap for values up to 1e9.  K-TanH jumps at the ends of its intervals, by up to 0.016: y by up to 0.016 cap, and two
+ * subtracted, and the sums of e^y v have to stay within Float32: a row that sees n keys may have values up to 3e38 / (n e^cap), which is
+ * 3e25 / n at a cap of 30, 6e16 / n at 50 and 5e10 / n at 64 (beyond it its output may be infinite);
+ * products below 1e-45 are lost, at the lowest scores under a cap of 64 values below 1e-17.
+ * K-TanH jumps at the ends of its intervals, by up to 0.016: y by up to 0.016 cap, and two
  * computations whose q . k differ in the last bits may differ by that there.
  *
  * Masks.  Sequences ("documents") are packed one behind the other; a query sees keys of its own document alone.  Where a

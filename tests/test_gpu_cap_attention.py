@@ -109,6 +109,30 @@ def test_caps_and_tables(gpu, cap, spread, intervals):
         _near(lse, want["lse"], want["lse_off"], "lse")
 
 
+@pytest.mark.parametrize("heads", [2, 512])
+@pytest.mark.parametrize("cap,keys", [(64.0, 3000), (64.0, 60), (50.0, 1000)])
+def test_values_up_to_what_the_sums_hold(gpu, cap, keys, heads):
+    """Scores that are all at the cap and values up to 3e38 / (keys e^cap), over documents and over pages: no sum leaves Float32."""
+    binding, _, torch = gpu
+    largest = 3e38 / (keys * np.exp(cap))
+    k64, v64 = np.full((keys, 1, 64), 8.0), np.full((keys, 1, 64), largest)
+    v64[:, :, 1::2] *= np.random.default_rng(51).uniform(-1.0, 1.0, (keys, 1, 32))
+    k, v = _bf16(torch, k64), _bf16(torch, v64)
+    v = torch.where(v.abs() > largest, v * (1 - 2.0 ** -7), v)        # rounding to BFloat16 may have gone beyond
+    v64, q64 = v.double().cpu().numpy(), np.full((2, heads, 64), 7.0)
+    options = dict(cap=cap, scale=1.0)                           # x is 56 and more
+    want = kcap_oracle.attention(q64[:, :1], k64, v64, [0, 2], [0, keys], **options)
+    want, off = (np.broadcast_to(want[n], q64.shape) for n in ("o", "o_off"))
+    assert np.isfinite(want).all()
+    q, at, at_k = _bf16(torch, q64), _offsets(torch, [2])[0], _offsets(torch, [keys])[0]
+    _near(binding.kcap_attention(q, k, v, at, at_k, **options)[0], want, off, "documents")
+    pages = -(-keys // 16)
+    k_cache, v_cache = (torch.cat([t, t.new_zeros((pages * 16 - keys, 1, 64))]).view(pages, 16, 1, 64) for t in (k, v))
+    table, n = torch.arange(pages, dtype=torch.int32, device="cuda")[None], torch.tensor([keys], dtype=torch.int32, device="cuda")
+    _near(binding.kcap_attention_paged(q, k_cache, v_cache, table, n, at, **options), want, off, "pieces")
+    _near(binding.kcap_attention_paged(q[1:], k_cache, v_cache, table, n, **options), want[1:], off[1:], "single")
+
+
 @pytest.mark.parametrize("mask", ["causal", "window", "all"])
 def test_what_is_not_seen_does_not_reach_a_row(gpu, mask):
     """NaN and infinities in keys and values: of other documents, later than the query, before its window, and in rows of no document."""
