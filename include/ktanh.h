@@ -317,7 +317,7 @@ ktanh_status_t klstm_cell64_backward(const uint16_t *gates, const float *c_prev,
  * p = i + keys - queries.  With `causal` it sees the keys up to p, with window w > 0 those from p - w + 1 on.  A query
  * that sees no key has the output 0 and the log-sum -infinity.  Keys and values that a query does not see do not
  * reach its output, infinities and NaN included; a NaN among the scores it sees makes its output NaN, and so does
- * an overflowing q . k.  An infinite value that it sees makes that place of its output infinite, two of opposite signs NaN.
+ * an overflowing q . k or q . k * (scale / cap).  An infinite value that it sees makes that place of its output infinite, two of opposite signs NaN.
  *
  * Shared heads: query head h reads key/value head h / (heads / kv_heads).
  * Offsets and lengths are read on the GPU, where values out of range are taken as the nearest in range. */
@@ -330,7 +330,7 @@ typedef struct kcap_shape {
     size_t q_row, q_head;          /* strides in elements, multiples of 8 below 2^24: tensors are   */
     size_t k_row, k_head;          /*   [rows][heads][dim] with dim contiguous                      */
     size_t v_row, v_head;
-    double scale, cap;             /* scale finite, 0 < cap <= KCAP_MAX                             */
+    double scale, cap;             /* 0 < cap <= KCAP_MAX, scale and scale / cap finite in Float32  */
     size_t window;                 /* 0: none                                                       */
     int causal;
 } kcap_shape_t;

@@ -26,7 +26,7 @@ inline ktanh_status_t read_shape(const kcap_shape_t *s, const uint16_t *q, const
     if (s->dim != 64 && s->dim != 128) return KT_ERR_SHAPE;
     if (s->heads == 0 || s->kv_heads == 0 || s->heads % s->kv_heads != 0) return KT_ERR_SHAPE;
     if (s->docs > kMost || s->q_rows > kMost || s->k_rows > kMost || s->heads > 65536) return KT_ERR_SHAPE;
-    if (!(s->cap > 0.0 && s->cap <= KCAP_MAX) || !std::isfinite(s->scale)) return KT_ERR_SHAPE;
+    if (!(s->cap > 0.0 && s->cap <= KCAP_MAX) || !std::isfinite((float)s->scale) || !std::isfinite((float)(s->scale / s->cap))) return KT_ERR_SHAPE;
     for (size_t stride : {s->q_row, s->q_head, s->k_row, s->k_head, s->v_row, s->v_head}) {
         if (stride % 8 != 0) return KT_ERR_ALIGN;
         if (stride >= (size_t)1 << 24) return KT_ERR_SHAPE;

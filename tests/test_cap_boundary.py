@@ -158,6 +158,19 @@ def test_append_refuses(binding):
     assert call(_shape(binding, dim=48), good) == 4 and call(_shape(binding, q_row=20), good) == 2
 
 
+@pytest.mark.parametrize("scale,cap", [(1.0, 1e-40), (1e300, 50.0), (-1e30, 1e-10), (1e39, 64.0)])
+def test_a_scale_over_cap_beyond_float32_is_refused(binding, scale, cap):
+    """An infinite factor gives NaN for a score of zero, and an infinite argument for one that saturates."""
+    lib = binding.load_library()
+    options = dict(scale=scale, cap=cap)
+    some = [FAKE] * 6
+    assert lib.kcap_attention(_shape(binding, **options), *some, NULL, NULL, None, NULL) == 4
+    assert lib.kcap_attention64(_shape(binding, **options), *some, NULL, NULL, None, NULL) == 4
+    assert lib.kcap_attention_backward(_shape(binding, **options), FAKE, 256, 64, *[FAKE] * 4, NULL, *[FAKE] * 7, None, NULL) == 4
+    for q_at in (NULL, FAKE):
+        assert lib.kcap_attention_paged(_shape(binding, docs=64, k_rows=0, **options), _pages(binding), *[FAKE] * 5, q_at, FAKE, FAKE, None, NULL) == 4
+
+
 def test_lines_of_k_under_sanitizers(tmp_path):
     """The packing of K-TanH's tables as lines, with ASan and UBSan: on every interval the line is Algorithm 1's value."""
     csrc = os.path.join(ROOT, "paper_1909_07729_amd", "csrc")
