@@ -33,15 +33,17 @@ def _rotated(x, cos, sin):
 
 
 class PagedCache:
-    """Keys and values of every layer in pages that sequences share; pages are handed out as sequences grow."""
+    """Keys and values of every layer in pages.  Each sequence has pages of its own for `longest` tokens, handed out at the start in a random
+    order, so that no sequence's pages are neighbours.  ``held``, counted on the host: keys that the longest sequence has at most."""
 
     def __init__(self, layers, sequences, longest, kv_heads, dim, page=16, device="cuda"):
         most = -(-longest // page)
         shape = (sequences * most, page, kv_heads, dim)
         self.k, self.v = ([torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(layers)] for _ in range(2))
-        order = torch.randperm(sequences * most, generator=torch.Generator().manual_seed(0))     # no sequence's pages are neighbours
+        order = torch.randperm(sequences * most, generator=torch.Generator().manual_seed(0))
         self.pages = order.view(sequences, most).int().to(device)
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
+        self.page, self.held = page, 0
 
 
 class LanguageModel(torch.nn.Module):
@@ -81,17 +83,23 @@ class LanguageModel(torch.nn.Module):
         return self._layers(tokens, attend)
 
     @torch.no_grad()
-    def serve(self, tokens, cache: PagedCache, offsets=None):
-        """New tokens of every sequence of the cache, one each or, with offsets, a piece of its text; grows the cache."""
+    def serve(self, tokens, cache: PagedCache, offsets=None, longest=None):
+        """New tokens of every sequence of the cache, one each or, with offsets, a piece of its text; grows the cache.  `longest`: tokens of the
+        longest piece, where the caller knows it."""
+        room = cache.pages.shape[1] * cache.page
+        if longest is None:
+            longest = 1 if offsets is None else min(tokens.shape[0], max(room - cache.held, 0))
+        held = cache.held + longest
         paged = binding.kcap_attention_paged if self.intervals == 32 else binding.kcap_attention64_paged
         new = torch.ones_like(cache.lengths) if offsets is None else offsets.diff()
         lengths = cache.lengths + new
+        pages = cache.pages[:, :-(-held // cache.page)]     # those that the longest sequence needs: the work is cut by them
 
         def attend(i, q, k, v):
-            q = binding.kcap_append(q, k, v, cache.k[i], cache.v[i], cache.pages, cache.lengths, offsets, cos=self.cos, sin=self.sin)
-            return paged(q, cache.k[i], cache.v[i], cache.pages, lengths, offsets, cap=self.cap)
+            q = binding.kcap_append(q, k, v, cache.k[i], cache.v[i], pages, cache.lengths, offsets, cos=self.cos, sin=self.sin)
+            return paged(q, cache.k[i], cache.v[i], pages, lengths, offsets, cap=self.cap)
         logits = self._layers(tokens, attend)
-        cache.lengths = lengths
+        cache.lengths, cache.held = lengths, held
         return logits
 
 
@@ -135,7 +143,7 @@ def generate(model, prompts, count, piece=24, page=16):
     for start in range(0, longest, piece):
         parts = [p[start:start + piece] for p in prompts]
         offsets = torch.tensor([0] + [len(p) for p in parts]).cumsum(0).int().cuda()
-        logits = model.serve(torch.cat(parts), cache, offsets)
+        logits = model.serve(torch.cat(parts), cache, offsets, min(piece, longest - start))
         ends = offsets[1:].long() - 1
         done = torch.tensor([len(p) > 0 for p in parts], device="cuda")
         last[done] = logits[ends[done]]
