@@ -86,10 +86,12 @@ class LanguageModel(torch.nn.Module):
     def serve(self, tokens, cache: PagedCache, offsets=None, longest=None):
         """New tokens of every sequence of the cache, one each or, with offsets, a piece of its text; grows the cache.  `longest`: tokens of the
         longest piece, where the caller knows it."""
-        room = cache.pages.shape[1] * cache.page
+        room = min(self.cos.shape[0], cache.pages.shape[1] * cache.page)
         if longest is None:
             longest = 1 if offsets is None else min(tokens.shape[0], max(room - cache.held, 0))
         held = cache.held + longest
+        if held > room:
+            raise ValueError(f"{held} tokens of a sequence are more than the model's angles or the cache's pages hold")
         paged = binding.kcap_attention_paged if self.intervals == 32 else binding.kcap_attention64_paged
         new = torch.ones_like(cache.lengths) if offsets is None else offsets.diff()
         lengths = cache.lengths + new
@@ -119,6 +121,8 @@ def documents(generator, count, vocabulary, longest):
 
 def train(model, steps, batch=16, longest=128, seed=0):
     """Mean losses of the steps."""
+    if longest > model.cos.shape[0]:
+        raise ValueError(f"the model has angles for {model.cos.shape[0]} tokens")
     generator = torch.Generator().manual_seed(seed)
     optimizer = torch.optim.Adam(model.parameters(), lr=2e-3)
     losses = []
@@ -138,6 +142,8 @@ def train(model, steps, batch=16, longest=128, seed=0):
 def generate(model, prompts, count, piece=24, page=16):
     """Greedy continuation of prompts (a list of token tensors) by `count` tokens; (tokens [prompts, count], logits of each step)."""
     sequences, longest = len(prompts), max(len(p) for p in prompts)
+    if longest + count > model.cos.shape[0]:
+        raise ValueError(f"the model has angles for {model.cos.shape[0]} tokens")
     cache = PagedCache(len(model.qkv), sequences, longest + count, model.kv_heads, model.dim, page)
     last = torch.empty((sequences, model.embedding.shape[0]), device="cuda")
     for start in range(0, longest, piece):
