@@ -1,9 +1,9 @@
 // Internal to libktanh: arguments of the capped-attention kernels and the checks that their entry points share.
 #pragma once
-#include <algorithm>
 #include <cmath>
 
 #include "ktanh_cap.h"
+#include "ktanh_cap_plan.h"
 
 namespace ktanh_cap {
 
@@ -93,32 +93,6 @@ inline ktanh_status_t read_pages(const kcap_pages_t *p, const int32_t *pages, co
     out->k_page = (uint32_t)p->k_page;
     out->v_page = (uint32_t)p->v_page;
     return KT_OK;
-}
-
-// Query heads of a group that a block has together.
-inline int heads_together(size_t group) { return group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1; }
-
-// Whether blocks hold 32 queries, their wavefronts sharing the tiles of keys, rather than 32 in each: the shorter time of the block that takes
-// longest, or of all blocks, by what they take for a tile alone, a compute unit with all that it holds, and around their tiles.  Documents may be twice as
-// long as the average.  Output, then gradients, causal, in us, wavefronts of their own rows | sharing the tiles:
-//    1024 rows,  8 heads of 128 on 8        36  63 |  15  39
-//    4096 rows,  8 heads of 128 on 8       128 245 |  65 179
-//    1500 rows, 32 heads of 128 on 8        51 130 |  45 128
-//    2048 rows, 32 heads of 128 on 8        68 218 |  72 229
-//    eight documents of 256, 32 heads on 8  17  50 |  39  82
-//    8192 rows,  5 heads of 128 on 1       249 561 | 144 459
-//    a document of 32 rows, 8 heads of 64  4.7 10.3 | 5.0 11.3
-inline bool split_tiles(const kcap_shape_t &s)
-{
-    if (s.k_rows <= 32 * s.docs) return false;  // one tile cannot be shared
-    const double docs = (double)s.docs, queries = (double)s.q_rows / docs, keys = (double)s.k_rows / docs;
-    const bool narrow = s.window > 0 && (double)s.window + 128.0 < keys;
-    const double seen = narrow ? (double)s.window + 128.0 : keys, mean = s.causal && !narrow ? 0.5 : 1.0, longest = docs > 1.0 && !narrow ? 2.0 : 1.0;
-    const double together = heads_together(s.heads / s.kv_heads);
-    const double own_blocks = std::ceil(queries * together / 128.0) * docs * (double)s.heads / together, own_tiles = seen / 32.0;
-    const double sharing_blocks = std::ceil(queries / 32.0) * docs * (double)s.heads, sharing_tiles = seen / 128.0;
-    return std::max(5.0 + 1.35 * longest * sharing_tiles, sharing_blocks / 256.0 * (0.85 * mean * sharing_tiles + 3.2)) <
-           std::max(3.0 + 1.03 * longest * own_tiles, own_blocks / 256.0 * (0.57 * mean * own_tiles + 3.5));
 }
 
 // Rows of a stretch, as a power of two: of a block whose wavefronts share tiles, or of one with as many query heads of a group together as its four

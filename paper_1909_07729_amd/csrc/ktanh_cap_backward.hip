@@ -471,48 +471,6 @@ __global__ __launch_bounds__(kThreads) void cap_join_grads_kernel(BackwardArgs a
     *reinterpret_cast<bf16x8 *>((blockIdx.y == 0 ? a.dk : a.dv) + i) = pack8(v);
 }
 
-// How the blocks over keys are cut: their rows, and into how many parts the query heads that share a key/value head are dealt, each with a
-// block and sums in Float32 of its own that another kernel adds up.
-struct KeysPlan {
-    bool split;
-    int parts;
-};
-
-// The least time of all: of the block that takes longest, or of all blocks with some of that one's at their end, by what a block takes for a tile
-// alone, and a compute unit with all that it holds, and around its tiles; and of the parts written and read.  Documents may be twice as long as
-// the average.  Gradients causal, 32 heads of 128 on 8, in us with four | two | one part | one part in blocks of 32 rows:
-//    six documents, 8192 rows in all    722 |  719 |  948 |  694
-//    64 documents of 256                552 |  438 |  341
-//    eight documents of 2048           1421 | 1303 | 1244 | 1374
-//    one of 8192                       2191 | 2187 | 2876 | 2300
-//    16 of 256                          141 |  113 |  116 |  105
-KeysPlan keys_plan(const kcap_shape_t &s)
-{
-    KeysPlan best{false, 1};
-    if (s.docs == 0 || s.kv_heads == 0 || s.heads < s.kv_heads) return best;
-    const int group = (int)(s.heads / s.kv_heads);
-    const double docs = (double)s.docs, queries = (double)s.q_rows / docs, keys = (double)s.k_rows / docs;
-    double least = 0.0;
-    for (const bool split : {false, true}) {
-        if (split && s.q_rows <= 32 * s.docs) break;  // one tile cannot be shared
-        const double rows = split ? 32.0 : 128.0, at_once = split ? 4.0 : 1.0, alone_us = split ? 2.2 : 1.8, all_us = split ? 1.15 : 1.0, around_us = split ? 22.0 : 8.0;
-        const bool narrow = s.window > 0 && (double)s.window + rows < queries;
-        const double tiles = (narrow ? (double)s.window + rows : queries) / 32.0 / at_once, mean = s.causal && !narrow ? tiles / 2.0 : tiles;
-        for (int parts = 1; parts <= group; ++parts) {
-            if (group % parts != 0) continue;
-            const double heads = group / parts, blocks = std::ceil(keys / rows) * docs * (double)s.kv_heads * parts;
-            const double longest = heads * tiles * (s.docs > 1 && !narrow ? 2.0 : 1.0) * alone_us, all = blocks * heads * mean * all_us / 256.0 + around_us * blocks / 512.0;
-            const double join = parts > 1 ? 5.0 + parts * (double)s.k_rows * (double)s.kv_heads * (double)s.dim * 16.0 / 6e6 : 0.0;
-            const double t = std::max(longest, all + longest / 4.0) + join;
-            if (least == 0.0 || t < least) {
-                least = t;
-                best = KeysPlan{split, parts};
-            }
-        }
-    }
-    return best;
-}
-
 size_t delta_bytes(const kcap_shape_t &s) { return (s.heads * s.q_rows * 4 + 127) / 128 * 128; }
 
 template <class Lut>
