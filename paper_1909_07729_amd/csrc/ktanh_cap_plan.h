@@ -42,13 +42,16 @@ struct KeysPlan {
 };
 
 // The least time of all: of the block that takes longest, or of all blocks with some of that one's at their end, by what a block takes for a tile
-// alone, and a compute unit with all that it holds, and around its tiles; and of the parts written and read.  Documents may be twice as long as
-// the average.  Gradients causal, 32 heads of 128 on 8, in us with four | two | one part | one part in blocks of 32 rows:
-//    six documents, 8192 rows in all    722 |  719 |  948 |  694
-//    64 documents of 256                552 |  438 |  341
-//    eight documents of 2048           1421 | 1303 | 1244 | 1374
-//    one of 8192                       2191 | 2187 | 2876 | 2300
-//    16 of 256                          141 |  113 |  116 |  105
+// alone, and a compute unit with all that it holds, and around its tiles; and of the parts written and read.  Documents count as 1.6 times as long
+// as the average.  Fitted to 1277 calls, documents alike in length or cut at random, 5 to 64 heads: 1.5 % above the best plan on average (alike or one
+// 1.2, cut evenly 0.8, at random 2.7), 1.4 % of them more than 20 % above.  Gradients causal, in us with four | two | one part | one part in blocks of 32 rows:
+//    six documents, 8192 rows at random, 32 heads of 128 on 8    934 |  988 | 1338 |  905
+//    64 documents of 256                                         526 |  413 |  334 |  413
+//    32 documents of 256                                         283 |  228 |  185 |  245
+//    16 documents of 256                                         140 |  114 |  121 |  111
+//    eight documents of 2048                                    1411 | 1291 | 1267 | 1341
+//    one of 8192                                                2100 | 2198 | 2700 | 2291
+//    64 documents of 256, 8 heads of 64 on 2                      74 |   67 |   77 |   53
 inline KeysPlan keys_plan(const kcap_shape_t &s)
 {
     KeysPlan best{false, 1};
@@ -58,15 +61,16 @@ inline KeysPlan keys_plan(const kcap_shape_t &s)
     double least = 0.0;
     for (const bool split : {false, true}) {
         if (split && s.q_rows <= 32 * s.docs) break;  // one tile cannot be shared
-        const double rows = split ? 32.0 : 128.0, at_once = split ? 4.0 : 1.0, alone_us = split ? 2.2 : 1.8, all_us = split ? 1.15 : 1.0, around_us = split ? 22.0 : 8.0;
+        const double rows = split ? 32.0 : 128.0, at_once = split ? 4.0 : 1.0, alone_us = split ? 2.3 : 1.8;
+        const double all_us = s.dim == 64 ? 0.9 : split ? 1.2 : 1.05, around_us = (split ? 12.0 : 6.0) * (s.dim == 64 ? 0.5 : 1.0);
         const bool narrow = s.window > 0 && (double)s.window + rows < queries;
         const double tiles = (narrow ? (double)s.window + rows : queries) / 32.0 / at_once, mean = s.causal && !narrow ? tiles / 2.0 : tiles;
         for (int parts = 1; parts <= group; ++parts) {
             if (group % parts != 0) continue;
             const double heads = group / parts, blocks = std::ceil(keys / rows) * docs * (double)s.kv_heads * parts;
-            const double longest = heads * tiles * (s.docs > 1 && !narrow ? 2.0 : 1.0) * alone_us, all = blocks * heads * mean * all_us / 256.0 + around_us * blocks / 512.0;
+            const double longest = heads * tiles * (s.docs > 1 && !narrow ? 1.6 : 1.0) * alone_us, all = blocks * heads * mean * all_us / 256.0 + around_us * blocks / 512.0;
             const double join = parts > 1 ? 5.0 + parts * (double)s.k_rows * (double)s.kv_heads * (double)s.dim * 16.0 / 6e6 : 0.0;
-            const double t = std::max(longest, all + longest / 4.0) + join;
+            const double t = std::max(longest, all + 0.3 * longest) + join;
             if (least == 0.0 || t < least) {
                 least = t;
                 best = KeysPlan{split, parts};

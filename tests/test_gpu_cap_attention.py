@@ -329,8 +329,9 @@ def test_gradients_with_many_blocks_and_with_few_are_the_same(gpu):
             assert torch.allclose(a[rows].float(), b.float(), rtol=2 ** -7, atol=2 ** -12)
 
 
-@pytest.mark.parametrize("heads,kv_heads,dim,q_rows", [(16, 8, 64, 512), (16, 1, 128, 512), (4, 2, 64, 60), (3, 1, 128, 60)])
-def test_gradients_of_keys_that_no_query_sees(gpu, heads, kv_heads, dim, q_rows):
+@pytest.mark.parametrize("heads,kv_heads,dim,q_rows,causal", [(16, 8, 64, 512, True), (16, 1, 128, 512, True), (32, 2, 128, 1024, False),
+                                                              (4, 2, 64, 60, True), (3, 1, 128, 60, True)])
+def test_gradients_of_keys_that_no_query_sees(gpu, heads, kv_heads, dim, q_rows, causal):
     """Whole blocks of keys without a query, of a document that has none and before the window of one that has few: in blocks of 128 keys,
     with the shared heads in parts (many queries) and in one block (few), their gradients are exactly zero."""
     binding, _, torch = gpu
@@ -339,7 +340,7 @@ def test_gradients_of_keys_that_no_query_sees(gpu, heads, kv_heads, dim, q_rows)
     do = _bf16(torch, np.random.default_rng(47).standard_normal((q_rows, heads, dim)))
     (q_at, _), (k_at, _) = _offsets(torch, [q_rows, 0]), _offsets(torch, [keys, keys])
     for window, seen_from in ((0, 0), (64, keys - q_rows - 63)):
-        options = dict(cap=50.0, window=window)
+        options = dict(cap=50.0, window=window, causal=causal)
         o, lse = binding.kcap_attention(q, k, v, q_at, k_at, **options)
         outs = [torch.full_like(t, 7.0) for t in (q, k, v)]
         binding.kcap_attention_backward(do, q, k, v, o, lse, q_at, k_at, dq=outs[0], dk=outs[1], dv=outs[2], **options)
