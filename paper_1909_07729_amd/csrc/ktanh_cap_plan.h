@@ -12,8 +12,8 @@ namespace ktanh_cap {
 inline int heads_together(size_t group) { return group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1; }
 
 // Whether blocks hold 32 queries, their wavefronts sharing the tiles of keys, rather than 32 in each: the shorter time of the block that takes
-// longest, or of all blocks, by what they take for a tile alone, a compute unit with all that it holds, and around their tiles.  Documents may be twice as
-// long as the average.  Output, then gradients, causal, in us, wavefronts of their own rows | sharing the tiles:
+// longest, or of all blocks, by what they take for a tile alone, a compute unit with all that it holds, and around their tiles.  Documents count as
+// 1.2 times as long as the average.  Output, then gradients, causal, in us, wavefronts of their own rows | sharing the tiles:
 //    1024 rows,  8 heads of 128 on 8        36  63 |  15  39
 //    4096 rows,  8 heads of 128 on 8       128 245 |  65 179
 //    1500 rows, 32 heads of 128 on 8        51 130 |  45 128
@@ -21,17 +21,23 @@ inline int heads_together(size_t group) { return group % 4 == 0 ? 4 : group % 2 
 //    eight documents of 256, 32 heads on 8  17  50 |  39  82
 //    8192 rows,  5 heads of 128 on 1       249 561 | 144 459
 //    a document of 32 rows, 8 heads of 64  4.7 10.3 | 5.0 11.3
+// and the output alone:
+//    four documents of 1250, 16 heads on 4      52 |  84
+//    four of 700, 16 heads of 128 on 16         33 |  41
+//    four of 700, 8 heads of 64 on 2            24 |  16
+//    20 at random, 10000 rows, 5 heads on 1     65 |  52
 inline bool split_tiles(const kcap_shape_t &s)
 {
     if (s.k_rows <= 32 * s.docs) return false;  // one tile cannot be shared
     const double docs = (double)s.docs, queries = (double)s.q_rows / docs, keys = (double)s.k_rows / docs;
     const bool narrow = s.window > 0 && (double)s.window + 128.0 < keys;
-    const double seen = narrow ? (double)s.window + 128.0 : keys, mean = s.causal && !narrow ? 0.5 : 1.0, longest = docs > 1.0 && !narrow ? 2.0 : 1.0;
+    const double seen = narrow ? (double)s.window + 128.0 : keys, mean = s.causal && !narrow ? 0.5 : 1.0, longest = docs > 1.0 && !narrow ? 1.2 : 1.0;
     const double together = heads_together(s.heads / s.kv_heads);
     const double own_blocks = std::ceil(queries * together / 128.0) * docs * (double)s.heads / together, own_tiles = seen / 32.0;
     const double sharing_blocks = std::ceil(queries / 32.0) * docs * (double)s.heads, sharing_tiles = seen / 128.0;
-    return std::max(5.0 + 1.35 * longest * sharing_tiles, sharing_blocks / 256.0 * (0.85 * mean * sharing_tiles + 3.2)) <
-           std::max(3.0 + 1.03 * longest * own_tiles, own_blocks / 256.0 * (0.57 * mean * own_tiles + 3.5));
+    const double rounds = (s.dim == 64 ? 0.6 : 1.0) / 256.0;  // of heads of 64 a compute unit holds more
+    return std::max(5.0 + 1.35 * longest * sharing_tiles, rounds * sharing_blocks * (0.85 * mean * sharing_tiles + 3.2)) <
+           std::max(3.0 + 1.03 * longest * own_tiles, rounds * own_blocks * (0.57 * mean * own_tiles + 3.5));
 }
 
 // How the blocks over keys are cut: their rows, and into how many parts the query heads that share a key/value head are dealt, each with a

@@ -54,3 +54,23 @@ def test_keys_gradients_take_near_the_least_that_was_measured(plan_of):
     for shape, (_, split, parts) in zip(KEYS, plan_of(KEYS)):
         times = KEYS[shape]
         assert times[split, parts] <= 1.2 * min(times.values()), (shape, split, parts, times)
+
+
+# us of the output by (wavefronts of their own rows, sharing the tiles)
+OUTPUTS = {
+    # alike in length
+    (4, 5000, 16, 4, 128): (52.1, 84.2), (2, 4096, 24, 8, 128): (80.4, 129.0), (20, 10000, 5, 1, 128): (26.6, 42.1), (6, 8192, 8, 1, 128): (53.0, 75.2),
+    (2, 1024, 40, 8, 128): (25.8, 34.3), (8, 2048, 16, 16, 128): (17.6, 22.2), (4, 2800, 16, 16, 128): (33.1, 40.5), (16, 4096, 8, 1, 128): (17.5, 21.3),
+    (8, 2048, 32, 8, 128): (21.0, 40.5), (16, 8192, 32, 8, 128): (75.3, 180.4), (4, 2800, 8, 2, 64): (24.3, 16.4), (4, 2800, 8, 1, 128): (30.0, 25.3),
+    # one
+    (1, 2048, 32, 8, 128): (69.2, 76.0), (1, 8192, 5, 1, 128): (249.0, 144.0), (1, 1024, 8, 8, 128): (36.0, 15.0),
+    # cut at random
+    (28, 5000, 6, 2, 64): (21.8, 16.1),
+}
+
+
+def test_outputs_take_near_the_least_that_was_measured(plan_of):
+    """Within 25 %, as 98 in 100 of the calls that the rule was fitted to."""
+    for shape, (split, _, _) in zip(OUTPUTS, plan_of(OUTPUTS)):
+        times = OUTPUTS[shape]
+        assert times[split] <= 1.25 * min(times), (shape, split, times)

@@ -293,6 +293,16 @@ def test_blocks_of_128_rows(gpu, docs, mask, kv_heads, dim):
     test_gradients(gpu, docs, mask, heads, kv_heads, dim)
 
 
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("heads,kv_heads,dim", HEADS)
+def test_shared_tiles_of_ragged_documents(gpu, mask, heads, kv_heads, dim):
+    """Few heads and long enough documents that the four wavefronts of a block share its tiles, with ones of every size around a tile among them."""
+    lengths = [65, 0, 1, 127, 700, 33, 128]
+    got, want = _grads(gpu, 52, lengths, lengths, heads, kv_heads, dim, lead=3, cap=32.0, scale=dim ** -0.5, **MASKS[mask])
+    for name, t in got.items():
+        _near(t, want[name], want[name + "_off"], name)
+
+
 @pytest.mark.parametrize("mask", ["causal", "window"])
 def test_what_is_not_seen_does_not_reach_a_row_of_many_heads(gpu, mask):
     binding, _, torch = gpu
