@@ -122,7 +122,7 @@ class _KCapAttention(torch.autograd.Function):
     def backward(ctx, dout):
         attend = binding.kcap_attention64_backward if ctx.wide else binding.kcap_attention_backward
         *tensors, q_offsets, k_offsets, rest = ctx.saved_tensors
-        if dout.stride(-1) != 1 or any(step % 8 for step in dout.stride()[:2]) or dout.data_ptr() % 16:
+        if dout.stride(-1) != 1 or any(step % 8 or step >= 1 << 24 for step in dout.stride()[:2]) or dout.data_ptr() % 16:
             dout = dout.contiguous()        # also the expanded gradient of a sum
         return (*attend(dout, *tensors, q_offsets, k_offsets, rest=rest, **ctx.options), None, None, None, None)
 

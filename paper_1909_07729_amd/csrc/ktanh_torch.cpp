@@ -762,7 +762,8 @@ struct CapAttention : public torch::autograd::Function<CapAttention> {
         for (const size_t i : {(size_t)5, (size_t)6}) checked(saved[i], kBf16, "the saved output");
         checked(saved[7], kF32, "the saved sums");
         Tensor d_o = grads[0];
-        if (d_o.stride(2) != 1 || d_o.stride(0) % 8 != 0 || d_o.stride(1) % 8 != 0 || reinterpret_cast<uintptr_t>(d_o.const_data_ptr()) % 16 != 0)
+        auto taken = [](int64_t step) { return step % 8 == 0 && step < 1 << 24; };
+        if (d_o.stride(2) != 1 || !taken(d_o.stride(0)) || !taken(d_o.stride(1)) || reinterpret_cast<uintptr_t>(d_o.const_data_ptr()) % 16 != 0)
             d_o = d_o.contiguous();  // also the expanded gradient of a sum
         kcap_shape_t shape;
         const CapOptions options{ctx->saved_data["cap"].toDouble(), ctx->saved_data["scale"].toDouble(), ctx->saved_data["causal"].toBool(),

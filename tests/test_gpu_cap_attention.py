@@ -389,6 +389,21 @@ def test_gradient_of_a_sum_and_of_shared_inputs(gpu):
     assert torch.equal(dq, want[0]) and torch.equal(dk, want[1] + want[2])
 
 
+@pytest.mark.parametrize("lut", [False, True])
+def test_gradient_with_strides_that_the_kernels_do_not_take(gpu, lut):
+    """An incoming gradient heads first, its heads 2^24 elements apart: nothing that the caller of autograd chose."""
+    binding, autograd, torch = gpu
+    (q, k, v), _ = _inputs(torch, 53, 40, 40, 2, 1, 64)
+    at, _ = _offsets(torch, [40])
+    far = torch.zeros((1 << 24) + 40 * 64, dtype=torch.bfloat16, device="cuda").as_strided((40, 2, 64), (64, 1 << 24, 1))
+    far.copy_(_bf16(torch, np.random.default_rng(54).standard_normal((40, 2, 64))))
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    o = autograd.kcap_attention(*leaves, at, cap=50.0, lut=binding.ktanh_default_lut() if lut else None)     # a caller's table takes the Python code
+    got = torch.autograd.grad(o, leaves, far, retain_graph=True)
+    for a, b in zip(got, torch.autograd.grad(o, leaves, far.contiguous())):
+        assert torch.equal(a, b)
+
+
 def test_what_rounding_dropped(gpu):
     """o and its rest together are the output to sixteen bits; with it the gradients of a peaked head are at least as near."""
     binding, _, torch = gpu
