@@ -11,8 +11,8 @@
 // P and dS are rounded to BFloat16 where they become operands: dq and dk are then off by 0.0025 of their norm, of which 0.0017 is the
 // rounding of the results themselves.  A second term would double the instructions of three of the seven products.
 //
-// What bounds it: six documents of 8192 tokens in all, 32 heads of 128 on 8, causal: dq 291 us, dk and dv 413 in blocks of 32
-// rows (380 in blocks of 128, and 46 to join four parts).  A tile of 32 x 32 takes 24 (32) matrix and 220 (235) vector instructions, in 197 (247) registers, so that two
+// What bounds it: six documents of 8192 tokens in all, 32 heads of 128 on 8, causal: dq 320 us, dk and dv 455 in blocks of 32
+// rows (medians of ten passes from an idle card; the least 290 and 409, in blocks of 128 then 380 and 46 to join four parts).  A tile of 32 x 32 takes 24 (32) matrix and 220 (235) vector instructions, in 197 (247) registers, so that two
 // wavefronts share a SIMD: its matrix unit is busy 34 (33) % of the time and its vector unit 46 (38) %, and the rest is waiting for one another and for LDS, which is
 // busy 35 (43) %.  Two tiles behind one barrier, or all operands of a tile read ahead, changed less than 2 %.
 #include "ktanh_cap_args.h"

@@ -9,8 +9,8 @@
 // second term costs nothing, and the output is as far off as its own rounding.  Both terms have the weight's sign: of opposite ones, or with a zero
 // among them, an infinite value would come out as NaN.
 //
-// What bounds it: memory.  64 texts of up to 8192 tokens, 32 heads of 128 on 8: 1.04 GB in 177 us, 5.9 TB/s (a wide read of as much memory reaches 6.9); two of
-// 131071: 174 us, 6.2.  One text of 777 tokens: 10 us, half of it the second launch.
+// What bounds it: memory.  64 texts of up to 8192 tokens, 32 heads of 128 on 8: 1.04 GB in 178 us, 5.9 TB/s (a wide read of as much memory reaches 6.9); two of
+// 131071: 175 us, 6.1.  One text of 777 tokens: 10 us, half of it the second launch.
 #include "ktanh_cap_args.h"
 
 using namespace ktanh_cap;
