@@ -301,23 +301,25 @@ ktanh_status_t klstm_cell64_backward(const uint16_t *gates, const float *c_prev,
  * Where a transformer bounds its attention scores with TanH, K-TanH takes its place.  For a query q and a key k
  * that it sees, in Float32:
  *   t = Kf(q.k * (scale / cap)),   y = cap * t,   weight = e^y / sum of e^y over the keys that q sees
- * and the output is the weighted sum of the values.  Kf is ktanh_f32 with the bits that its shift drops kept (the line
- * A x + B that Algorithm 1 follows on each interval), one fused multiply-add; scale / cap is rounded to Float32 once.
+ * and the output is the weighted sum of the values.  Kf is ktanh_f32 with the bits that its shift drops kept
+ * (the line A x + B that Algorithm 1 follows on each interval), one fused multiply-add; scale / cap is rounded
+ * to Float32 once.
  * q . k and the weights are Float32; the weights are rounded to BFloat16 for the product with the values, whose
- * sum is Float32 and is divided by the sum of the rounded weights (the log-sum is that of the weights before); outputs are rounded to
- * nearest even.  Since |y| <= cap <= KCAP_MAX no maximum is
- * subtracted, and the sums of e^y v have to stay within Float32: a row that sees n keys may have values up to 3e38 / (n e^cap), which is
- * 3e25 / n at a cap of 30, 6e16 / n at 50 and 5e10 / n at 64 (beyond it its output may be infinite);
- * products below 1e-45 are lost, at the lowest scores under a cap of 64 values below 1e-17.
+ * sum is Float32 and is divided by the sum of the rounded weights (the log-sum is that of the weights before);
+ * outputs are rounded to nearest even.  Since |y| <= cap <= KCAP_MAX no maximum is subtracted, and the sums of
+ * e^y v have to stay within Float32: a row that sees n keys may have values up to 3e38 / (n e^cap), which is
+ * 3e25 / n at a cap of 30, 6e16 / n at 50 and 5e10 / n at 64 (beyond it its output may be infinite); products
+ * below 1e-45 are lost, at the lowest scores under a cap of 64 values below 1e-17.
  * K-TanH jumps at the ends of its intervals, by up to 0.016: y by up to 0.016 cap, and two
  * computations whose q . k differ in the last bits may differ by that there.
  *
- * Masks.  Sequences ("documents") are packed one behind the other; a query sees keys of its own document alone.  Where a
- * document has fewer or more queries than keys, the last query stands at the last key: query i is at place
- * p = i + keys - queries.  With `causal` it sees the keys up to p, with window w > 0 those from p - w + 1 on.  A query
- * that sees no key has the output 0 and the log-sum -infinity.  Keys and values that a query does not see do not
- * reach its output, infinities and NaN included; a NaN among the scores it sees makes its output NaN, and so does
- * an overflowing q . k or q . k * (scale / cap).  An infinite value that it sees makes that place of its output infinite, two of opposite signs NaN.
+ * Masks.  Sequences ("documents") are packed one behind the other; a query sees keys of its own document
+ * alone.  Where a document has fewer or more queries than keys, the last query stands at the last key: query i
+ * is at place p = i + keys - queries.  With `causal` it sees the keys up to p, with window w > 0 those from p -
+ * w + 1 on.  A query that sees no key has the output 0 and the log-sum -infinity.  Keys and values that a query
+ * does not see do not reach its output, infinities and NaN included; a NaN among the scores it sees makes its
+ * output NaN, and so does an overflowing q . k or q . k * (scale / cap).  An infinite value that it sees makes
+ * that place of its output infinite, two of opposite signs NaN.
  *
  * Shared heads: query head h reads key/value head h / (heads / kv_heads).
  * Offsets and lengths are read on the GPU, where values out of range are taken as the nearest in range. */
@@ -339,9 +341,11 @@ typedef struct kcap_shape {
  *   o    device, out: BFloat16 [q_rows][heads][dim], dense; rows in no document become 0
  *   rest device, out, may be NULL: like o, what its rounding dropped, rounded: training keeps it for the gradients
  *   lse  device, out, may be NULL: Float32 [heads][q_rows], log of the sum of e^y (kcap_attention_backward reads it)
- * q, k, v 16-byte aligned, o and rest 8-byte (KT_ERR_ALIGN).  q_rows == 0 or docs == 0 returns KT_OK without a launch;
- * without documents the outputs stay as they are, here and in the other calls of attention (`binding` fills them).
- * KT_ERR_SHAPE: another dim, heads not a multiple of kv_heads, a cap or scale out of range, more than 2^30 rows.
+ * q, k, v 16-byte aligned, o and rest 8-byte (KT_ERR_ALIGN).  q_rows == 0 or docs == 0 returns KT_OK without a
+ * launch; without documents the outputs stay as they are, here and in the other calls of attention (`binding`
+ * fills them).
+ * KT_ERR_SHAPE: another dim, heads not a multiple of kv_heads, a cap or scale out of range, more than 2^30
+ * rows.
  * KT_ERR_LUT: also a table whose K exceeds 1. */
 ktanh_status_t kcap_attention(const kcap_shape_t *shape, const uint16_t *q, const uint16_t *k, const uint16_t *v,
                               const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *o, uint16_t *rest, float *lse,
@@ -352,9 +356,9 @@ ktanh_status_t kcap_attention64(const kcap_shape_t *shape, const uint16_t *q, co
 
 /* Gradients of kcap_attention from its inputs and its o and lse, with the library's derivative identity of TanH:
  *   P = e^(y - lse),  dS = P (dO.V - sum over dim of dO * O) (1 - t^2),  dq = scale dS K,  dk = scale dS^T Q,  dv = P^T dO
- * Products take BFloat16 roundings of P and dS and sum in Float32; gradients of shared heads are summed in Float32 before they are
- * rounded, in a fixed order.  Rows in no document, and queries that see no key, have the gradient 0.  A NaN or
- * infinity in a document may reach all of that document's gradients.
+ * Products take BFloat16 roundings of P and dS and sum in Float32; gradients of shared heads are summed in
+ * Float32 before they are rounded, in a fixed order.  Rows in no document, and queries that see no key, have
+ * the gradient 0.  A NaN or infinity in a document may reach all of that document's gradients.
  *   d_o        device, BFloat16 [q_rows][heads][dim] with strides do_row, do_head (multiples of 8 below 2^24), 16-byte aligned
  *   o, rest, lse  as kcap_attention gave them.  rest may be NULL: dq and dk of peaked rows are then less exact (for scores of
  *              standard deviation 6 they are 0.005 off in norm instead of 0.0027, of which 0.0017 is their own rounding)
@@ -383,8 +387,8 @@ typedef struct kcap_pages {
 } kcap_pages_t;
 
 /* The same attention over a paged cache, causal: the queries are the last tokens of their sequences, whose keys and
- * values (their own among them) are in the cache.  shape: docs = sequences, q_rows, heads, kv_heads, dim, q_row, q_head,
- * scale, cap, window; the rest is not read.
+ * values (their own among them) are in the cache.  shape: docs = sequences, q_rows, heads, kv_heads, dim,
+ * q_row, q_head, scale, cap, window; the rest is not read.
  *   pages      device, [docs][most] with rows table_row apart; a number outside the cache is taken as the nearest page
  *   lengths    device, docs: keys of each sequence
  *   q_offsets  device, docs + 1, or NULL: one query for each sequence (q_rows == docs), which is the faster form for that
@@ -402,14 +406,16 @@ ktanh_status_t kcap_attention64_paged(const kcap_shape_t *shape, const kcap_page
                                       ktanh_stream_t stream);
 
 /* New tokens into the cache: their keys rotated to their positions, their values as they are; and their
- * queries rotated.  Token i of sequence s (row q_offsets[s] + i) has the position lengths[s] + i, lengths being the keys
- * in the cache before the call.  Pairs (a, b) become (a cos - b sin, b cos + a sin) in Float32, rounded once; pair i of the first
- * 2 * angles values is (x_i, x_{i + angles}), or (x_{2i}, x_{2i+1}) where `interleaved`; what is behind them is copied.
+ * queries rotated.  Token i of sequence s (row q_offsets[s] + i) has the position lengths[s] + i, lengths being
+ * the keys in the cache before the call.  Pairs (a, b) become (a cos - b sin, b cos + a sin) in Float32,
+ * rounded once; pair i of the first 2 * angles values is (x_i, x_{i + angles}), or (x_{2i}, x_{2i+1}) where
+ * `interleaved`; what is behind them is copied.
  * shape: docs, q_rows (tokens), heads, kv_heads, dim and all strides; the rest is not read.
  *   cos, sin   device, Float32 [positions][angles], dense, 16-byte aligned; angles a multiple of 8, 2 * angles <= dim
  *   q_offsets  device, docs + 1, or NULL: one token for each sequence
  *   q_out      device, BFloat16 [q_rows][heads][dim], dense, 16-byte aligned; may be q where q is dense
- * Rows in no sequence are left as they are.  A token whose position has no page in the table, or a page number outside the cache, is not written to the cache; one whose
+ * Rows in no sequence are left as they are.  A token whose position has no page in the table, or a page number
+ * outside the cache, is not written to the cache; one whose
  * position has no angles has NaN for its query and is not written either. */
 ktanh_status_t kcap_append(const kcap_shape_t *shape, const kcap_pages_t *cache, const uint16_t *q, const uint16_t *k,
                            const uint16_t *v, uint16_t *q_out, uint16_t *k_cache, uint16_t *v_cache, const int32_t *pages,

@@ -4,19 +4,19 @@
 //
 // K is the Float32 form of Algorithm 1 (arXiv:1909.07729).  On one interval of the table it is a line,
 //   K(x) = A x + B for x > 0,   A = 2^(E - E_i - r),   B = 2^(E - 127) (1 - 2^-r + b/128),
-// which the kernels evaluate with one fused multiply-add: what the shift of Algorithm 1 drops below the
-// last place of a Float32 is kept.  128 lines are held in LDS, indexed by the three low exponent bits and the four
-// high mantissa bits of |x| clamped to [0.25 - 2^-26, 16]: the identity below 0.25, saturation from 4 on and the
-// table in between need no comparisons, and tables of 32 and of 64 intervals run the same code.
+// which the kernels evaluate with one fused multiply-add: what the shift of Algorithm 1 drops below the last
+// place of a Float32 is kept.  128 lines are held in LDS, indexed by the three low exponent bits and the four
+// high mantissa bits of |x| clamped to [0.25 - 2^-26, 16]: the identity below 0.25, saturation from 4 on and
+// the table in between need no comparisons, and tables of 32 and of 64 intervals run the same code.
 //
 // |y| <= cap, and caps are at most 64, so e^y stays within e^-64 .. e^64 and the softmax needs no running
 // maximum: the weights are summed as they are, which also lets parts of a row be joined by adding.
 //
-// Matrix products use v_mfma_f32_32x32x16_bf16.  Scores are formed so that the lane that holds a weight holds it
-// where the next product wants it: an accumulator's lane l has column l & 31 and the rows
-// (r & 3) + 8 (r >> 2) + 4 (l >> 5), r = 0..15; packed to BFloat16, registers 8 i .. 8 i + 7 are the second operand of a
-// product over 16 of those rows in the order  8 i' + 4 (l >> 5) + (j & 3),  and the first operand is read from LDS in that same
-// order by transposing reads of 4 rows x 16 columns (ds_read_b64_tr_b16).  No weight crosses lanes.
+// Matrix products use v_mfma_f32_32x32x16_bf16.  Scores are formed so that the lane that holds a weight holds
+// it where the next product wants it: an accumulator's lane l has column l & 31 and the rows (r & 3) + 8 (r >>
+// 2) + 4 (l >> 5), r = 0..15; packed to BFloat16, registers 8 i .. 8 i + 7 are the second operand of a product
+// over 16 of those rows in the order  8 i' + 4 (l >> 5) + (j & 3),  and the first operand is read from LDS in
+// that same order by transposing reads of 4 rows x 16 columns (ds_read_b64_tr_b16).  No weight crosses lanes.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -36,8 +36,9 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4_at8 __attribute__((ext_vector_type(4), aligned(8)));  // 16 bytes anywhere that eight may be
 
 constexpr int kThreads = 256, kWaves = 4;
-// A wavefront has 32 rows.  The four of a block go over the tiles of the other tensor together, with 128 rows, or the same 64 or 32 rows of two or four
-// heads that share that tensor; or (SPLIT) all four have the same 32 rows, each goes over every fourth tile on its own, and their sums are joined at the end.
+// A wavefront has 32 rows.  The four of a block go over the tiles of the other tensor together, with 128 rows,
+// or the same 64 or 32 rows of two or four heads that share that tensor; or (SPLIT) all four have the same 32
+// rows, each goes over every fourth tile on its own, and their sums are joined at the end.
 constexpr int kRows = 128;
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -62,11 +63,14 @@ __device__ __forceinline__ bf16x8 pack8(const float *v)
     return __builtin_bit_cast(bf16x8, u32x4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])});
 }
 
-__device__ __forceinline__ float sum_of(bf16x2 pair, float sum) { return __builtin_amdgcn_fdot2_f32_bf16(pair, __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false); }
+__device__ __forceinline__ float sum_of(bf16x2 pair, float sum)
+{
+    return __builtin_amdgcn_fdot2_f32_bf16(pair, __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
+}
 
-// The same, with the sum of the rounded values.  Outputs are divided by the sum of the weights as the product has them: the
-// roundings of one weight in numerator and denominator cancel (o is off by 0.0018 of its norm instead of 0.0023, 0.0017 of it the
-// rounding of o itself).
+// The same, with the sum of the rounded values.  Outputs are divided by the sum of the weights as the product
+// has them: the roundings of one weight in numerator and denominator cancel (o is off by 0.0018 of its norm
+// instead of 0.0023, 0.0017 of it the rounding of o itself).
 __device__ __forceinline__ bf16x8 pack8(const float *v, float *sum)
 {
     u32x4 w;
@@ -92,8 +96,8 @@ __device__ __forceinline__ void spread_lines(f32x2 *lines, const KtCapPack &pack
     }
 }
 
-// unit * K(x).  A NaN stays one.  Everything below 0.25 reads one line, so that lanes of small scores share an address: table reads
-// at many are what the LDS unit has least time for.
+// unit * K(x).  A NaN stays one.  Everything below 0.25 reads one line, so that lanes of small scores share an
+// address: table reads at many are what the LDS unit has least time for.
 __device__ __forceinline__ f32x2 line_of(float x, const f32x2 *lines)
 {
     const uint32_t key = __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fabsf(x), 0x1.fffffep-3f, 16.0f));
@@ -104,11 +108,12 @@ __device__ __forceinline__ float on_line(float x, f32x2 line) { return __builtin
 
 __device__ __forceinline__ float capped(float x, const f32x2 *lines) { return on_line(x, line_of(x, lines)); }
 
-// Which accumulator rows of a lane, numbered from 0 at `at`, lie in [first, last): others become zero.  In a branch of its
-// own (the statement keeps the compiler from testing every tile).
+// Which accumulator rows of a lane, numbered from 0 at `at`, lie in [first, last): others become zero.  In a
+// branch of its own (the statement keeps the compiler from testing every tile).
 struct Span {
     uint32_t from, count;
-    __device__ __forceinline__ Span(int first, int last, int at) : from((uint32_t)(at + 4 * (int)((threadIdx.x & 63) >> 5) - first)), count((uint32_t)max(last - first, 0))
+    __device__ __forceinline__ Span(int first, int last, int at)
+        : from((uint32_t)(at + 4 * (int)((threadIdx.x & 63) >> 5) - first)), count((uint32_t)max(last - first, 0))
     {
     }
     __device__ __forceinline__ bool has(int r) const { return from + (uint32_t)((r & 3) + 8 * (r >> 2)) < count; }
@@ -122,9 +127,10 @@ __device__ __forceinline__ void keep(float *p, Span span)
 }
 
 // ------------------------------------------------------------------------------------- tiles in LDS
-// Rows of D BFloat16 values, 16 bytes apart, in an order in which the two low bits of a row's number change places with the two
-// above them.  Both ways of reading then run without bank conflicts, eight rows at one 16-byte chunk (ds_read_b128) and 64 bytes of
-// four consecutive rows (transposing reads), and all reads of a lane are one address and constant offsets.
+// Rows of D BFloat16 values, 16 bytes apart, in an order in which the two low bits of a row's number change
+// places with the two above them.  Both ways of reading then run without bank conflicts, eight rows at one
+// 16-byte chunk (ds_read_b128) and 64 bytes of four consecutive rows (transposing reads), and all reads of a
+// lane are one address and constant offsets.
 template <int D> constexpr int kPitch = 2 * D + 16;
 
 template <int D>
@@ -141,7 +147,8 @@ __device__ __forceinline__ bf16x8 rows_of(const char *tile, int row0, int k)
     return *reinterpret_cast<const bf16x8 *>(tile + chunk_at<D>(lane & 31, lane >> 5) + row0 * kPitch<D> + 32 * k);
 }
 
-// Operand of columns 32 c .. 32 c + 31 of the tile over its rows row0 .. row0 + 15 in the order of a packed accumulator.
+// Operand of columns 32 c .. 32 c + 31 of the tile over its rows row0 .. row0 + 15 in the order of a packed
+// accumulator.
 template <int D>
 __device__ __forceinline__ bf16x8 columns_of(const char *tile, int row0, int c)
 {
@@ -153,9 +160,11 @@ __device__ __forceinline__ bf16x8 columns_of(const char *tile, int row0, int c)
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// 32 rows of D BFloat16 values as direct loads bring them (each instruction of a wavefront writes 1 KiB in the order of its lanes):
-// row m lies in stretch m % kStretches, m / kStretches rows into it.  The stretches start such that, again, eight rows at one
-// 16-byte chunk and 64 bytes of four consecutive rows lie in different banks, and all reads of a lane are one address and constants.
+// 32 rows of D BFloat16 values as direct loads bring them (each instruction of a wavefront writes 1 KiB in the
+// order of its lanes):
+// row m lies in stretch m % kStretches, m / kStretches rows into it.  The stretches start such that, again,
+// eight rows at one 16-byte chunk and 64 bytes of four consecutive rows lie in different banks, and all reads
+// of a lane are one address and constants.
 template <int D>
 struct Keys32 {
     static constexpr int kStretches = D / 16, kDeep = 32 / kStretches, kChunks = D / 8;
@@ -196,8 +205,8 @@ __device__ __forceinline__ void load_direct(const void *from, char *to)
 // This wavefront's loads, direct ones among them, have arrived.
 __device__ __forceinline__ void wait_for_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 
-// A tile in LDS is complete, and what was in the place of the next one has been read: behind the block's barrier where its wavefronts
-// share it, else behind this wavefront's own reads and writes.
+// A tile in LDS is complete, and what was in the place of the next one has been read: behind the block's
+// barrier where its wavefronts share it, else behind this wavefront's own reads and writes.
 template <bool SPLIT>
 __device__ __forceinline__ void tile_complete()
 {
@@ -205,15 +214,17 @@ __device__ __forceinline__ void tile_complete()
     else __syncthreads();
 }
 
-// 32 rows of D BFloat16 values to memory by whole rows, through `tile` of LDS: a wavefront's own, or (SPLIT) the block's, of which each wavefront has a
-// fourth of the columns.  quad(i) are values 8 i + 4 (lane / 32) .. + 3 of row lane & 31, from the wavefront's first column on.  Straight from the
-// accumulator each store touches 32 rows, 16 bytes of each: 16 documents of 256 tokens, 32 heads of 128, take 46 us so, and 30 this way.
+// 32 rows of D BFloat16 values to memory by whole rows, through `tile` of LDS: a wavefront's own, or (SPLIT)
+// the block's, of which each wavefront has a fourth of the columns.  quad(i) are values 8 i + 4 (lane / 32) ..
+// + 3 of row lane & 31, from the wavefront's first column on.  Straight from the accumulator each store touches
+// 32 rows, 16 bytes of each: 16 documents of 256 tokens, 32 heads of 128, take 46 us so, and 30 this way.
 // Chunks of 16 bytes change places with the low bits of their row's number against bank conflicts.
 template <int D, bool SPLIT, class Quad>
 __device__ __forceinline__ void store_rows(char *tile, uint16_t *to, long long row, int there, Quad quad)
 {
     constexpr int kChunks = D / 8, kMine = SPLIT ? kChunks / kWaves : kChunks, kLanes = SPLIT ? kThreads : 64;
-    const int lane = threadIdx.x & 63, first = SPLIT ? (int)(threadIdx.x >> 6) * kMine : 0, member = SPLIT ? (int)threadIdx.x : lane, chunk = member % kChunks;
+    const int lane = threadIdx.x & 63, first = SPLIT ? (int)(threadIdx.x >> 6) * kMine : 0;
+    const int member = SPLIT ? (int)threadIdx.x : lane, chunk = member % kChunks;
     auto complete = [] {
         if constexpr (SPLIT) __syncthreads();
         else tile_complete<true>();
@@ -253,8 +264,9 @@ __device__ __forceinline__ void store_rows_wide(char *tile, float *to, long long
     }
 }
 
-// Tiles of 32 rows of two tensors on their way to LDS, one behind the other, and of each the stretches that wavefront `wave` of LOADERS brings;
-// a row behind the last one is read as the last.  One address for all lanes and 32 bits of offset for each (strides are below 2^24).
+// Tiles of 32 rows of two tensors on their way to LDS, one behind the other, and of each the stretches that
+// wavefront `wave` of LOADERS brings; a row behind the last one is read as the last.  One address for all lanes
+// and 32 bits of offset for each (strides are below 2^24).
 template <int D, int LOADERS, int STEP = 32>
 struct Stream {
     typedef Keys32<D> Tile;
@@ -265,7 +277,8 @@ struct Stream {
     const char *a, *b;  // the next tile's first row of this wavefront
     uint32_t a_off, b_off;
 
-    __device__ __forceinline__ Stream(const uint16_t *a_rows, long long a_row, const uint16_t *b_rows, long long b_row, int last, int wave, int at)
+    __device__ __forceinline__ Stream(const uint16_t *a_rows, long long a_row, const uint16_t *b_rows, long long b_row,
+                                      int last, int wave, int at)
         : a_rows(a_rows), b_rows(b_rows), a_row(a_row), b_row(b_row), last(last), wave(wave)
     {
         const uint32_t row = Tile::row_of_lane(0), chunk = 16 * Tile::chunk_of_lane();
@@ -282,8 +295,9 @@ struct Stream {
     __device__ __forceinline__ void next(int at, char *a_tile, char *b_tile)
     {
         const bool there = at + 32 <= last + 1;
-        // Of two stretches each chooses its addresses, eight are in the code twice: with the second form for two 16384 tokens in 32 heads of 128 take
-        // 2360 us instead of 2310, with the first for eight 2048 in 8 heads 29.7 instead of 25.9.
+        // Of two stretches each chooses its addresses, eight are in the code twice: with the second form for
+        // two 16384 tokens in 32 heads of 128 take 2360 us instead of 2310, with the first for eight 2048 in 8
+        // heads 29.7 instead of 25.9.
         if constexpr (kShare <= 2) {
 #pragma unroll
             for (int n = 0; n < kShare; ++n) {
@@ -324,8 +338,8 @@ struct Stream {
 };
 
 // ------------------------------------------------------------------------------------------- blocks
-// What a block has to do: a stretch of rows, by its rank in work, for one key/value head, one of the parts that it is cut into, and
-// one of the `members` that share its keys (query heads of the group).
+// What a block has to do: a stretch of rows, by its rank in work, for one key/value head, one of the parts that
+// it is cut into, and one of the `members` that share its keys (query heads of the group).
 struct Unit {
     int kv_head, rank, part, member;
 };
@@ -336,9 +350,10 @@ __host__ __device__ __forceinline__ unsigned long long unit_blocks(unsigned long
     return (tiles * kv_heads * parts + 7) / 8 * 8 * members;
 }
 
-// Consecutive blocks go to the eight dies in turn.  The members of a unit come to one die, and share its second-level cache; where the
-// key/value heads are a multiple of eight, all units of a head do, eight heads after the other; else the heads take turns, so that in either case
-// each die has as much of the long stretches as of the short ones and of those that are empty (pieces of 500 tokens of eight sequences, 12 heads on 4:
+// Consecutive blocks go to the eight dies in turn.  The members of a unit come to one die, and share its
+// second-level cache; where the key/value heads are a multiple of eight, all units of a head do, eight heads
+// after the other; else the heads take turns, so that in either case each die has as much of the long stretches
+// as of the short ones and of those that are empty (pieces of 500 tokens of eight sequences, 12 heads on 4:
 // 268 us; with half of a head's ranks to each die 392).  False: nothing to do.
 __device__ __forceinline__ bool unit_of_block(unsigned block, unsigned tiles, int kv_heads, int parts, int members, Unit *unit)
 {
@@ -351,7 +366,8 @@ __device__ __forceinline__ bool unit_of_block(unsigned block, unsigned tiles, in
     return true;
 }
 
-// A stretch of 2^shift rows of a document.  There are at most rows >> shift and documents in sum, known without reading the offsets.
+// A stretch of 2^shift rows of a document.  There are at most rows >> shift and documents in sum, known without
+// reading the offsets.
 // Offsets outside [0, rows] are taken as the nearest in range, so that a wrong one reads nothing out of bounds.
 struct Stretch {
     int doc, begin, end, first;  // rows of the document, and the first of the stretch; first >= end: nothing to do
@@ -367,7 +383,8 @@ __device__ __forceinline__ int offset_at(const int *offsets, int d, int rows)
     return offsets == nullptr ? min(d, rows) : min(max(offsets[d], 0), rows);
 }
 
-// The last document for which `starts` (true up to some document, false behind it) holds; 0 if none.  By whole wavefronts.
+// The last document for which `starts` (true up to some document, false behind it) holds; 0 if none.  By whole
+// wavefronts.
 template <class Starts>
 __device__ __forceinline__ int last_document(int docs, Starts starts)
 {
@@ -401,13 +418,16 @@ __device__ __forceinline__ int lanes_before(int v, int bits)
     return sum;
 }
 
-// The stretch of 2^shift rows that is the rank-th in work, the most first: blocks start in this order, and the last ones to start are
-// short (in the order of the rows sixteen documents of 8192 tokens keep the chip 79 % busy, like this 94).  By whole wavefronts.
-// `others_of(d)`: rows of the other tensor that document d has; asked for together with the document's own.  Work, in units of as many rows: those rows if all are seen; if causal, the
-// number of the stretch and the rows before the document's first (`rising`: queries, over keys), or its number from the end (keys, over
-// queries).  More than 64 documents stay in the order of their rows.
+// The stretch of 2^shift rows that is the rank-th in work, the most first: blocks start in this order, and the
+// last ones to start are short (in the order of the rows sixteen documents of 8192 tokens keep the chip 79 %
+// busy, like this 94).  By whole wavefronts.
+// `others_of(d)`: rows of the other tensor that document d has; asked for together with the document's own.
+// Work, in units of as many rows: those rows if all are seen; if causal, the number of the stretch and the rows
+// before the document's first (`rising`: queries, over keys), or its number from the end (keys, over queries).
+// More than 64 documents stay in the order of their rows.
 template <class OthersOf>
-__device__ __forceinline__ Stretch stretch_of(int shift, int rank, const int *offsets, int docs, int rows, bool causal, bool rising, OthersOf others_of)
+__device__ __forceinline__ Stretch stretch_of(int shift, int rank, const int *offsets, int docs, int rows, bool causal,
+                                              bool rising, OthersOf others_of)
 {
     Stretch s;
     if (docs > 64) {
@@ -468,8 +488,8 @@ __device__ __forceinline__ Others rows_in(const int *offsets, int doc, int rows)
     return Others{begin, max(offset_at(offsets, doc + 1, rows) - begin, 0)};
 }
 
-// Rows of one head that no document covers (documents follow each other, so they lie before the first and behind the last)
-// of a dense tensor [rows][heads][D] become zero; by one block.
+// Rows of one head that no document covers (documents follow each other, so they lie before the first and
+// behind the last) of a dense tensor [rows][heads][D] become zero; by one block.
 template <int D, class Also>
 __device__ __forceinline__ void clear_rows(uint16_t *tensor, const int *offsets, int docs, int rows, int heads, int head, Also also)
 {

@@ -1,10 +1,13 @@
-// libktanh: new tokens into a paged cache, keys rotated on the way, values as they are, and the queries rotated.
+// libktanh: new tokens into a paged cache, keys rotated on the way, values as they are, and the queries
+// rotated.
 //
-// Moves each value once.  A lane takes units of 16 values of one head, two 16-byte pieces: both halves of eight rotated pairs, or
-// what is behind the rotated part.  A wavefront works for one token, so that its place (document, length, page: three loads one behind
-// the other) is looked up once, while the values are on their way.
+// Moves each value once.  A lane takes units of 16 values of one head, two 16-byte pieces: both halves of eight
+// rotated pairs, or what is behind the rotated part.  A wavefront works for one token, so that its place
+// (document, length, page: three loads one behind the other) is looked up once, while the values are on their
+// way.
 //
-// What bounds it: memory.  16384 tokens of 32 heads of 128 on 8: 411 MB in 69 us, 6.0 TB/s; 64 tokens take 5 us, a launch and two latencies.
+// What bounds it: memory.  16384 tokens of 32 heads of 128 on 8: 411 MB in 69 us, 6.0 TB/s; 64 tokens take 5
+// us, a launch and two latencies.
 #include "ktanh_cap_args.h"
 
 using namespace ktanh_cap;

@@ -26,7 +26,8 @@ inline ktanh_status_t read_shape(const kcap_shape_t *s, const uint16_t *q, const
     if (s->dim != 64 && s->dim != 128) return KT_ERR_SHAPE;
     if (s->heads == 0 || s->kv_heads == 0 || s->heads % s->kv_heads != 0) return KT_ERR_SHAPE;
     if (s->docs > kMost || s->q_rows > kMost || s->k_rows > kMost || s->heads > 65536) return KT_ERR_SHAPE;
-    if (!(s->cap > 0.0 && s->cap <= KCAP_MAX) || !std::isfinite((float)s->scale) || !std::isfinite((float)(s->scale / s->cap))) return KT_ERR_SHAPE;
+    if (!(s->cap > 0.0 && s->cap <= KCAP_MAX)) return KT_ERR_SHAPE;
+    if (!std::isfinite((float)s->scale) || !std::isfinite((float)(s->scale / s->cap))) return KT_ERR_SHAPE;
     for (size_t stride : {s->q_row, s->q_head, s->k_row, s->k_head, s->v_row, s->v_head}) {
         if (stride % 8 != 0) return KT_ERR_ALIGN;
         if (stride >= (size_t)1 << 24) return KT_ERR_SHAPE;
@@ -77,7 +78,8 @@ inline ktanh_status_t read_pages(const kcap_pages_t *p, const int32_t *pages, co
 {
     if (pages == nullptr || lengths == nullptr || k == nullptr || v == nullptr) return KT_ERR_NULL;
     if (p->page_size == 0 || (p->page_size & (p->page_size - 1)) != 0 || p->page_size > 1u << 20) return KT_ERR_SHAPE;
-    if (p->page_count == 0 || p->page_count > 0x7FFFFFFF || p->most == 0 || p->most > (1u << 30) / p->page_size || p->table_row > (size_t)1 << 40) return KT_ERR_SHAPE;
+    if (p->page_count == 0 || p->page_count > 0x7FFFFFFF || p->table_row > (size_t)1 << 40) return KT_ERR_SHAPE;
+    if (p->most == 0 || p->most > (1u << 30) / p->page_size) return KT_ERR_SHAPE;
     for (size_t stride : {p->k_page, p->k_slot, p->k_head, p->v_page, p->v_slot, p->v_head}) {
         if (stride % 8 != 0) return KT_ERR_ALIGN;
         if (stride >= (size_t)1 << 31) return KT_ERR_SHAPE;
@@ -95,21 +97,21 @@ inline ktanh_status_t read_pages(const kcap_pages_t *p, const int32_t *pages, co
     return KT_OK;
 }
 
-// Rows of a stretch, as a power of two: of a block whose wavefronts share tiles, or of one with as many query heads of a group together as its four
-// wavefronts can have.  16 documents of 8192 tokens, 32 heads of 128 on 8: 108.7 us with one head, 102.4 with four; 4 tokens each behind up to
-// 2000 of 64 sequences 109 and 70.
+// Rows of a stretch, as a power of two: of a block whose wavefronts share tiles, or of one with as many query
+// heads of a group together as its four wavefronts can have.  16 documents of 8192 tokens, 32 heads of 128 on
+// 8: 108.7 us with one head, 102.4 with four; 4 tokens each behind up to 2000 of 64 sequences 109 and 70.
 inline int rows_shift(const CapShape &s, bool split) { return split ? 5 : 7 - __builtin_ctz((unsigned)heads_together((size_t)s.group)); }
 inline unsigned long long stretches(size_t rows, size_t docs, int shift) { return (rows >> shift) + docs; }
 
-// Many queries of each sequence over the cache (ktanh_cap_forward.hip).  Where parts are above 1 the workspace holds
-// forward_sums Float32 sums and as many times dim numerators.
+// Many queries of each sequence over the cache (ktanh_cap_forward.hip).  Where parts are above 1 the workspace
+// holds forward_sums Float32 sums and as many times dim numerators.
 struct ForwardPlan {
     bool split;
     int parts;
 };
 ForwardPlan forward_plan(const kcap_shape_t &s, const kcap_pages_t &p);
 inline size_t forward_sums(size_t parts, size_t rows, size_t heads) { return (parts * rows * heads + 31) / 32 * 32; }
-ktanh_status_t launch_forward_paged(const CapShape &s, const CapPages &p, const int *q_offsets, uint16_t *o, int dim, ForwardPlan plan, float *workspace,
-                                    const KtCapPack &pack, ktanh_stream_t stream);
+ktanh_status_t launch_forward_paged(const CapShape &s, const CapPages &p, const int *q_offsets, uint16_t *o, int dim,
+                                    ForwardPlan plan, float *workspace, const KtCapPack &pack, ktanh_stream_t stream);
 
 }  // namespace ktanh_cap

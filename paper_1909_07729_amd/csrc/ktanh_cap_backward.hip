@@ -3,18 +3,22 @@
 //   P = e^(y - lse),  dP = dO V^T,  delta = rowsum(dO * O),  dS = P (dP - delta) (1 - t^2),
 //   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
 //
-// 1 - t^2 is the library's derivative identity of TanH at K-TanH's value.  Scores are formed again in two kernels, each
-// summing what it owns in registers, so that no gradient is added to by two blocks and results do not depend on their order:
+// 1 - t^2 is the library's derivative identity of TanH at K-TanH's value.  Scores are formed again in two
+// kernels, each summing what it owns in registers, so that no gradient is added to by two blocks and results do
+// not depend on their order:
 //   cap_dq_kernel    32 queries for each wavefront (or for all), over their keys; also forms delta
 //   cap_dkdv_kernel  32 keys for each wavefront (or for all) of a key/value head, over the queries of the heads that share them
 //
-// P and dS are rounded to BFloat16 where they become operands: dq and dk are then off by 0.0025 of their norm, of which 0.0017 is the
-// rounding of the results themselves.  A second term would double the instructions of three of the seven products.
+// P and dS are rounded to BFloat16 where they become operands: dq and dk are then off by 0.0025 of their norm,
+// of which 0.0017 is the rounding of the results themselves.  A second term would double the instructions of
+// three of the seven products.
 //
-// What bounds it: six documents of 8192 tokens in all, 32 heads of 128 on 8, causal: dq 320 us, dk and dv 455 in blocks of 32
-// rows (medians of ten passes from an idle card; the least 290 and 409, in blocks of 128 then 380 and 46 to join four parts).  A tile of 32 x 32 takes 24 (32) matrix and 220 (235) vector instructions, in 197 (247) registers, so that two
-// wavefronts share a SIMD: its matrix unit is busy 34 (33) % of the time and its vector unit 46 (38) %, and the rest is waiting for one another and for LDS, which is
-// busy 35 (43) %.  Two tiles behind one barrier, or all operands of a tile read ahead, changed less than 2 %.
+// What bounds it: six documents of 8192 tokens in all, 32 heads of 128 on 8, causal: dq 320 us, dk and dv 455
+// in blocks of 32 rows (medians of ten passes from an idle card; the least 290 and 409, in blocks of 128 then
+// 380 and 46 to join four parts).  A tile of 32 x 32 takes 24 (32) matrix and 220 (235) vector instructions, in
+// 197 (247) registers, so that two wavefronts share a SIMD: its matrix unit is busy 34 (33) % of the time and
+// its vector unit 46 (38) %, and the rest is waiting for one another and for LDS, which is busy 35 (43) %.  Two
+// tiles behind one barrier, or all operands of a tile read ahead, changed less than 2 %.
 #include "ktanh_cap_args.h"
 
 using namespace ktanh_cap;
@@ -36,7 +40,8 @@ struct BackwardArgs {
 
 constexpr int kTile = 32;  // rows of a tile in LDS
 
-// Of the rows that this wavefront loaded, those behind the last become zero in both tiles: what they hold is not the document's.
+// Of the rows that this wavefront loaded, those behind the last become zero in both tiles: what they hold is
+// not the document's.
 template <int D, int LOADERS>
 __device__ __forceinline__ void clear_behind(char *a_tile, char *b_tile, int wave, int there)
 {
@@ -67,12 +72,16 @@ __device__ __forceinline__ f32x4 quad(const f32x16 *acc, int i)
     return f32x4{c[4 * (i % 4)], c[4 * (i % 4) + 1], c[4 * (i % 4) + 2], c[4 * (i % 4) + 3]};
 }
 
-__device__ __forceinline__ void store4(uint16_t *to, f32x4 v) { *reinterpret_cast<u32x2 *>(to) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])}; }
+__device__ __forceinline__ void store4(uint16_t *to, f32x4 v)
+{
+    *reinterpret_cast<u32x2 *>(to) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+}
 __device__ __forceinline__ void store4(float *to, f32x4 v) { *reinterpret_cast<f32x4 *>(to) = v; }
 
-// An accumulator as the wavefront's rows (first `to`, `next` apart, `there` of them) of a dense tensor, times `by`.  SPLIT: the sum of all
-// wavefronts' in their order, a fourth of the columns by each; by all threads, and `sums` is free once more behind the next barrier.  BY_ROWS: by way of `tile`, LDS
-// that nobody reads any more but the sums' readers.
+// An accumulator as the wavefront's rows (first `to`, `next` apart, `there` of them) of a dense tensor, times
+// `by`.  SPLIT: the sum of all wavefronts' in their order, a fourth of the columns by each; by all threads, and
+// `sums` is free once more behind the next barrier.  BY_ROWS: by way of `tile`, LDS that nobody reads any more
+// but the sums' readers.
 template <int D, bool SPLIT, bool BY_ROWS, class T, class Sums>
 __device__ __forceinline__ void store_acc(T *to, long long next, int there, const f32x16 (&acc)[D / 32], float by, Sums &sums, char *tile)
 {
@@ -129,7 +138,8 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
     __shared__ __align__(16) Shared shared;
     f32x2 *lines = shared.lines;
 
-    const int together = SPLIT ? 0 : 7 - a.shift, members = a.s.group >> together;  // heads of a block, as a power of two; blocks that share keys
+    // heads of a block, as a power of two; blocks that share keys
+    const int together = SPLIT ? 0 : 7 - a.shift, members = a.s.group >> together;
     const unsigned blocks = (unsigned)unit_blocks(a.tiles, a.s.kv_heads, 1, members);
     if (blockIdx.x >= blocks) {
         clear_rows<D>(a.dq, a.q_offsets, a.s.docs, a.s.q_rows, a.s.heads, (int)(blockIdx.x - blocks), [](int) {});
@@ -196,10 +206,12 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
         wait_for_loads();
         const bool whole = j0 >= whole_from && j0 + kTile <= whole_to;
         if (j0 + kTile > n_keys) clear_behind<D, kLoaders>(k_tile, v_tile, loader, n_keys - j0);
-        // Behind this barrier the tile is complete and all are done with the one before, whose place the next one takes.
+        // Behind this barrier the tile is complete and all are done with the one before, whose place the next
+        // one takes.
         tile_complete<SPLIT>();
         if (!SPLIT && j0 + kStep < key_end) stream.next(j0 + kStep, next_k, next_v);
-        if (idle || (!whole && ((a.s.causal && j0 > place0 + 31) || (a.s.window > 0 && j0 + kTile - 1 <= place0 - a.s.window)))) return;
+        if (idle) return;
+        if (!whole && ((a.s.causal && j0 > place0 + 31) || (a.s.window > 0 && j0 + kTile - 1 <= place0 - a.s.window))) return;
         f32x16 s = f32x16{0}, dp = f32x16{0};
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) s = mfma(Keys32<D>::rows(k_tile, k), q[k], s);
@@ -248,8 +260,10 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dq_kernel(BackwardArgs a, KtC
         }
     }
     __syncthreads();
-    constexpr bool kByRows = SPLIT || D == 128;  // at 64 its registers would leave room for three wavefronts instead of four: 8192 tokens 748 us, 730 without
-    store_acc<D, SPLIT, kByRows>(a.dq + ((long long)row0 * a.s.heads + head) * D, (long long)a.s.heads * D, at.end - row0, dq, a.s.scale, shared.sums, shared.tiles[0].k[0] + (SPLIT ? 0 : wave * kBytes));
+    // At 64 its registers would leave room for three wavefronts instead of four: 8192 tokens 748 us, 730 without.
+    constexpr bool kByRows = SPLIT || D == 128;
+    store_acc<D, SPLIT, kByRows>(a.dq + ((long long)row0 * a.s.heads + head) * D, (long long)a.s.heads * D, at.end - row0, dq,
+                                 a.s.scale, shared.sums, shared.tiles[0].k[0] + (SPLIT ? 0 : wave * kBytes));
 }
 
 template <int D, bool SPLIT>
@@ -264,7 +278,8 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
     };
     struct Shared {
         f32x2 lines[128];  // first: the offset of a line is its address
-        char v[SPLIT ? 1 : kWaves][kBytes];  // the wavefronts' 32 rows of values: registers for them would leave one wavefront to a SIMD
+        // the wavefronts' 32 rows of values: registers for them would leave one wavefront to a SIMD
+        char v[SPLIT ? 1 : kWaves][kBytes];
         union {
             Tiles tiles[kTiles];
             f32x4 sums[SPLIT ? kWaves : 1][SPLIT ? D / 8 : 1][64];  // of each wavefront, at the end
@@ -310,7 +325,8 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
 #pragma unroll
         for (int n = 0; n < kShare; ++n) {
             const int g = SPLIT ? wave * kShare + n : n;
-            load_direct(v.at + min(row0 + Keys32<D>::row_of_lane(g), at.end - 1) * v.row + 8 * Keys32<D>::chunk_of_lane(), values + Keys32<D>::stretch_at(g));
+            load_direct(v.at + min(row0 + Keys32<D>::row_of_lane(g), at.end - 1) * v.row + 8 * Keys32<D>::chunk_of_lane(),
+                        values + Keys32<D>::stretch_at(g));
         }
     }
     f32x16 dk[kBlocks], dv[kBlocks];
@@ -342,7 +358,9 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
     now.query -= kTiles * kTile;
     advance(now);
     Where next = now;
-    Stream<D, kLoaders, kTiles * kTile> stream(q.at + first_query * q.row + next.head * q.head, q.row, d_o.at + first_query * d_o.row + next.head * d_o.head, d_o.row, n_queries - 1, loader, next.query);
+    Stream<D, kLoaders, kTiles * kTile> stream(q.at + first_query * q.row + next.head * q.head, q.row,
+                                               d_o.at + first_query * d_o.row + next.head * d_o.head, d_o.row,
+                                               n_queries - 1, loader, next.query);
     // Where wavefronts share a tile, one brings 16 of its 64 sums.
     const int sum_lanes = SPLIT ? 64 : 16, sum_row = SPLIT ? lane & 31 : 16 * (wave >> 1) + (lane & 15);
     const bool is_delta = SPLIT ? lane >= 32 : (wave & 1) != 0;
@@ -359,8 +377,8 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
             stream.start(next.query);
         }
     };
-    auto step = [&](int i0, const char *__restrict__ v_tile, char *__restrict__ q_tile, char *__restrict__ do_tile, float *__restrict__ sums, char *__restrict__ next_q,
-                    char *__restrict__ next_do) {
+    auto step = [&](int i0, const char *__restrict__ v_tile, char *__restrict__ q_tile, char *__restrict__ do_tile,
+                    float *__restrict__ sums, char *__restrict__ next_q, char *__restrict__ next_do) {
         wait_for_loads();
         if (i0 + kTile > n_queries) clear_behind<D, kLoaders>(q_tile, do_tile, loader, n_queries - i0);
         if (lane < sum_lanes) sums[(is_delta ? kTile : 0) + sum_row] = is_delta ? next_sum : next_sum * kLog2e;
@@ -432,7 +450,8 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
         advance(now);
     }
     const long long first_at = ((long long)row0 * a.s.kv_heads + kv_head) * D, to_next = (long long)a.s.kv_heads * D;
-    // The wavefront's rows of values are free behind its last tile.  A block that no query sees has had none, and has not waited for those rows yet.
+    // The wavefront's rows of values are free behind its last tile.  A block that no query sees has had none,
+    // and has not waited for those rows yet.
     if constexpr (SPLIT) {
         __syncthreads();
     } else {
@@ -452,7 +471,8 @@ __global__ __launch_bounds__(kThreads, 2) void cap_dkdv_kernel(BackwardArgs a, K
     }
 }
 
-// The parts of shared heads added up in their order, zero for rows of no document: 8 values of dk or dv for each thread.
+// The parts of shared heads added up in their order, zero for rows of no document: 8 values of dk or dv for
+// each thread.
 __global__ __launch_bounds__(kThreads) void cap_join_grads_kernel(BackwardArgs a, long long width)
 {
     const long long i = ((long long)blockIdx.x * kThreads + threadIdx.x) * 8, each = a.s.k_rows * width;
@@ -474,9 +494,10 @@ __global__ __launch_bounds__(kThreads) void cap_join_grads_kernel(BackwardArgs a
 size_t delta_bytes(const kcap_shape_t &s) { return (s.heads * s.q_rows * 4 + 127) / 128 * 128; }
 
 template <class Lut>
-ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t do_row, size_t do_head, const uint16_t *q, const uint16_t *k,
-                        const uint16_t *v, const uint16_t *o, const uint16_t *rest, const float *lse, const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *dq,
-                        uint16_t *dk, uint16_t *dv, void *workspace, const Lut *lut, ktanh_stream_t stream)
+ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t do_row, size_t do_head, const uint16_t *q,
+                        const uint16_t *k, const uint16_t *v, const uint16_t *o, const uint16_t *rest, const float *lse,
+                        const int32_t *q_offsets, const int32_t *k_offsets, uint16_t *dq, uint16_t *dk, uint16_t *dv,
+                        void *workspace, const Lut *lut, ktanh_stream_t stream)
 {
     if (shape == nullptr) return KT_ERR_NULL;
     if (shape->docs == 0 || (shape->q_rows == 0 && shape->k_rows == 0)) return KT_OK;
@@ -487,9 +508,12 @@ ktanh_status_t backward(const kcap_shape_t *shape, const uint16_t *d_o, size_t d
     BackwardArgs a{};
     ktanh_status_t st = read_shape(shape, q, k, v, &a.s);
     if (st != KT_OK) return st;
-    if (do_row % 8 != 0 || do_head % 8 != 0 || !aligned16(d_o) || !aligned16(o) || !aligned16(rest) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(workspace) ||
-        reinterpret_cast<uintptr_t>(lse) % 4 != 0 || reinterpret_cast<uintptr_t>(q_offsets) % 4 != 0 || reinterpret_cast<uintptr_t>(k_offsets) % 4 != 0)
-        return KT_ERR_ALIGN;
+    if (do_row % 8 != 0 || do_head % 8 != 0) return KT_ERR_ALIGN;
+    for (const void *at : {(const void *)d_o, (const void *)o, (const void *)rest, (const void *)dq, (const void *)dk, (const void *)dv,
+                           (const void *)workspace})
+        if (!aligned16(at)) return KT_ERR_ALIGN;
+    for (const void *at : {(const void *)lse, (const void *)q_offsets, (const void *)k_offsets})
+        if (reinterpret_cast<uintptr_t>(at) % 4 != 0) return KT_ERR_ALIGN;
     if (do_row >= (size_t)1 << 24 || do_head >= (size_t)1 << 24) return KT_ERR_SHAPE;
     KtCapPack pack;
     if ((st = pack_lines(lut, &pack)) != KT_OK) return st;

@@ -1,16 +1,18 @@
 // libktanh: capped attention over a paged cache, one query for each sequence.
 //
-// What it costs is reading the keys and values once.  All tiles of 32 keys of all sequences and key/value heads form one row, which is
-// cut into equal shares, one for each wavefront that the chip holds: however the lengths differ, all are done at the same time,
-// and none waits for a first load but at its start.  A wavefront works for up to 32 query heads that share keys, with the tile in LDS of its
-// own (no barriers), the next one on its way in registers and the pages of the one behind it looked up.  Weights need no
-// maximum (|y| <= cap), so what several wavefronts have of a sequence is joined by adding numerators and denominators; a
-// sequence within one share is finished there.  Weights go into the product as two BFloat16 terms, 15 bits in all: the matrix unit idles, so the
-// second term costs nothing, and the output is as far off as its own rounding.  Both terms have the weight's sign: of opposite ones, or with a zero
-// among them, an infinite value would come out as NaN.
+// What it costs is reading the keys and values once.  All tiles of 32 keys of all sequences and key/value heads
+// form one row, which is cut into equal shares, one for each wavefront that the chip holds: however the lengths
+// differ, all are done at the same time, and none waits for a first load but at its start.  A wavefront works
+// for up to 32 query heads that share keys, with the tile in LDS of its own (no barriers), the next one on its
+// way in registers and the pages of the one behind it looked up.  Weights need no maximum (|y| <= cap), so what
+// several wavefronts have of a sequence is joined by adding numerators and denominators; a sequence within one
+// share is finished there.  Weights go into the product as two BFloat16 terms, 15 bits in all: the matrix unit
+// idles, so the second term costs nothing, and the output is as far off as its own rounding.  Both terms have
+// the weight's sign: of opposite ones, or with a zero among them, an infinite value would come out as NaN.
 //
-// What bounds it: memory.  64 texts of up to 8192 tokens, 32 heads of 128 on 8: 1.04 GB in 178 us, 5.9 TB/s (a wide read of as much memory reaches 6.9); two of
-// 131071: 175 us, 6.1.  One text of 777 tokens: 10 us, half of it the second launch.
+// What bounds it: memory.  64 texts of up to 8192 tokens, 32 heads of 128 on 8: 1.04 GB in 178 us, 5.9 TB/s (a
+// wide read of as much memory reaches 6.9); two of 131071: 175 us, 6.1.  One text of 777 tokens: 10 us, half of
+// it the second launch.
 #include "ktanh_cap_args.h"
 
 using namespace ktanh_cap;
@@ -23,7 +25,8 @@ struct DecodeArgs {
     CapShape s;
     CapPages p;
     uint16_t *o;
-    // what a wavefront has of the first and of the last sequence of its share, if others have the rest: [shares][2][rows] and [..][rows][dim]
+    // what a wavefront has of the first and of the last sequence of its share, if others have the rest:
+    // [shares][2][rows] and [..][rows][dim]
     float *sums, *parts;
     int shares, rows, row_blocks, slices;
 };
@@ -130,8 +133,10 @@ __global__ __launch_bounds__(64, 2) void cap_decode_kernel(DecodeArgs a, KtCapPa
             const int row = lane / kChunks + n * (64 / kChunks), j = min(at.j0 + row, at.n_keys - 1);
             const int in_page = j & ((1 << a.p.shift) - 1), p = __shfl(page, row);
             // read once: with the hint a batch takes 200 us instead of 222
-            next_k[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(k + wide(p, a.p.k_page) + wide(in_page, (uint32_t)a.s.k.row) + 8 * (lane % kChunks)));
-            next_v[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(v + wide(p, a.p.v_page) + wide(in_page, (uint32_t)a.s.v.row) + 8 * (lane % kChunks)));
+            next_k[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(
+                k + wide(p, a.p.k_page) + wide(in_page, (uint32_t)a.s.k.row) + 8 * (lane % kChunks)));
+            next_v[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(
+                v + wide(p, a.p.v_page) + wide(in_page, (uint32_t)a.s.v.row) + 8 * (lane % kChunks)));
         }
     };
     bf16x8 q[kSteps];
@@ -187,13 +192,15 @@ __global__ __launch_bounds__(64, 2) void cap_decode_kernel(DecodeArgs a, KtCapPa
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(capped(s[r] * a.s.to_x, lines));
         if (j0 < now.first || j0 + kKeys > now.n_keys) keep(p, Span(now.first, now.n_keys, j0));
-        // The matrix units wait for memory here: weights go in as two BFloat16 values each, 15 bits of them at least, and are summed as they go in.
-        // Both are positive where the weight is, so that an infinite value stays one: the first is the weight cut off, the second
-        // what is left of 1 + 2^-16 times it, and never zero.
+        // The matrix units wait for memory here: weights go in as two BFloat16 values each, 15 bits of them at
+        // least, and are summed as they go in.
+        // Both are positive where the weight is, so that an infinite value stays one: the first is the weight
+        // cut off, the second what is left of 1 + 2^-16 times it, and never zero.
         u32x4 cut[2];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t pair = __builtin_amdgcn_perm(__float_as_uint(p[2 * i + 1]), __float_as_uint(p[2 * i]), 0x07060302u);  // the high halves
+            // the high halves of two weights
+            const uint32_t pair = __builtin_amdgcn_perm(__float_as_uint(p[2 * i + 1]), __float_as_uint(p[2 * i]), 0x07060302u);
             sum = sum_of(__builtin_bit_cast(bf16x2, pair), sum);
             cut[i / 4][i % 4] = pair;
         }
@@ -248,9 +255,11 @@ __global__ __launch_bounds__(64, 2) void cap_decode_kernel(DecodeArgs a, KtCapPa
     }
 }
 
-// The parts of a sequence and key/value head added up: four values of a row for each thread, the shares dealt to as many threads
-// as there are for them in turn, and what those have joined in their order.  Where sequences are few eight blocks take a slice of the values each:
-// two texts of 131071 tokens 174 us with slices, 188 without, 32 texts of up to 2000 37 and 33, 96 of up to 300 in 8 heads 38 and 17.
+// The parts of a sequence and key/value head added up: four values of a row for each thread, the shares dealt
+// to as many threads as there are for them in turn, and what those have joined in their order.  Where sequences
+// are few eight blocks take a slice of the values each:
+// two texts of 131071 tokens 174 us with slices, 188 without, 32 texts of up to 2000 37 and 33, 96 of up to 300
+// in 8 heads 38 and 17.
 constexpr int kJoinThreads = 256;
 
 template <int D>
@@ -258,7 +267,8 @@ __global__ __launch_bounds__(kJoinThreads) void cap_join_kernel(DecodeArgs a)
 {
     __shared__ f32x4 parts[kJoinThreads];
     __shared__ float sums[kJoinThreads];
-    const int pairs = a.s.kv_heads * a.row_blocks, slice = blockIdx.x % a.slices, seq = blockIdx.x / a.slices / pairs, pair = blockIdx.x / a.slices % pairs;
+    const int pairs = a.s.kv_heads * a.row_blocks, slice = blockIdx.x % a.slices;
+    const int seq = blockIdx.x / a.slices / pairs, pair = blockIdx.x / a.slices % pairs;
     const int head0 = pair / a.row_blocks * a.s.group + 32 * (pair % a.row_blocks), heads = min(32, a.s.group - 32 * (pair % a.row_blocks));
     const Row all(a, 0, seq);
     const int tiles = tiles_of(a, seq), from = all.before + pair * tiles;
@@ -289,8 +299,10 @@ __global__ __launch_bounds__(kJoinThreads) void cap_join_kernel(DecodeArgs a)
         u32x2{pack2(n[0] * to_mean, n[1] * to_mean), pack2(n[2] * to_mean, n[3] * to_mean)};
 }
 
-// Wavefronts: as many as the chip holds (eight to a compute unit at dim 128, twelve at 64), at most one for each tile that the table has room for.
-// 64 texts of up to 8192 tokens, with four, eight and sixteen to a compute unit 223, 177 and 185 us at dim 128, with six, twelve and eighteen 112, 101 and 103 at 64.
+// Wavefronts: as many as the chip holds (eight to a compute unit at dim 128, twelve at 64), at most one for
+// each tile that the table has room for.
+// 64 texts of up to 8192 tokens, with four, eight and sixteen to a compute unit 223, 177 and 185 us at dim 128,
+// with six, twelve and eighteen 112, 101 and 103 at 64.
 struct Shares {
     unsigned long long tiles, shares, rows, row_blocks;
     Shares(const kcap_shape_t &s, const kcap_pages_t &p)
@@ -364,7 +376,8 @@ ktanh_status_t attention_paged(const kcap_shape_t *shape, const kcap_pages_t *ca
 extern "C" size_t kcap_attention_paged_workspace(const kcap_shape_t *shape, const kcap_pages_t *cache, int single)
 {
     if (shape == nullptr || cache == nullptr || shape->docs == 0 || cache->page_size == 0 || cache->page_size > 1u << 20 ||
-        cache->most == 0 || cache->most > 1u << 30 || shape->docs > 1u << 30 || shape->heads > 65536 || shape->kv_heads > 65536 || shape->dim > 128 || shape->q_rows > 1u << 30)
+        cache->most == 0 || cache->most > 1u << 30 || shape->docs > 1u << 30 || shape->q_rows > 1u << 30 ||
+        shape->heads > 65536 || shape->kv_heads > 65536 || shape->dim > 128)
         return 0;
     if (!single) {
         const size_t parts = (size_t)forward_plan(*shape, *cache).parts;

@@ -1,16 +1,18 @@
 // libktanh: attention with scores capped through K-TanH over many queries: packed documents, and pieces of
 // prompts over a paged cache.
 //
-// A wavefront holds 32 queries in its registers, a block 128 of one document, or the same 64 or 32 of two or four heads that share keys, and
-// goes once over the keys that they see in tiles of 32, double-buffered in LDS by direct loads.  Where blocks are few (SPLIT) all
-// four wavefronts hold the same 32 queries of one head, each goes over every fourth tile with a place in LDS of its own, and the four sums are joined at the end.
+// A wavefront holds 32 queries in its registers, a block 128 of one document, or the same 64 or 32 of two or
+// four heads that share keys, and goes once over the keys that they see in tiles of 32, double-buffered in LDS
+// by direct loads.  Where blocks are few (SPLIT) all four wavefronts hold the same 32 queries of one head, each
+// goes over every fourth tile with a place in LDS of its own, and the four sums are joined at the end.
 //   S^T = K Q^T (keys x queries), p = e^(cap K(x)) in the accumulator, O^T += V^T P^T with P^T as it lies.
 //
-// What bounds it: 16384 tokens, 32 heads of 128, causal, take 2290 us, 960 TFLOP/s.  The matrix instructions alone take 1430 (1.54 PFLOP/s, what
-// the card's clock allows a large product too), reading their operands from LDS 160 more, bringing the tiles 310, the cap, the
-// exponentials and the sums, about 130 vector instructions for 16 matrix instructions, 430.  Three wavefronts share a SIMD because the tile's 32 keys
-// and the direct loads leave 160 registers enough: with 64 keys to a tile, through registers, and two wavefronts 2736; with 32 keys through
-// registers 2620.
+// What bounds it: 16384 tokens, 32 heads of 128, causal, take 2290 us, 960 TFLOP/s.  The matrix instructions
+// alone take 1430 (1.54 PFLOP/s, what the card's clock allows a large product too), reading their operands from
+// LDS 160 more, bringing the tiles 310, the cap, the exponentials and the sums, about 130 vector instructions
+// for 16 matrix instructions, 430.  Three wavefronts share a SIMD because the tile's 32 keys and the direct
+// loads leave 160 registers enough: with 64 keys to a tile, through registers, and two wavefronts 2736; with 32
+// keys through registers 2620.
 #include <type_traits>
 
 #include "ktanh_cap_args.h"
@@ -101,8 +103,8 @@ __device__ __forceinline__ void take_special(u32x4 *v)
     }
 }
 
-// Of the rows that this wavefront loaded: values behind the last key become zero, as infinities and NaN do.  Their weights are zero,
-// and the product would not be.
+// Of the rows that this wavefront loaded: values behind the last key become zero, as infinities and NaN do.
+// Their weights are zero, and the product would not be.
 template <int D, int LOADERS>
 __device__ __forceinline__ void clean_values(char *v_tile, int wave, int there)
 {
@@ -126,7 +128,8 @@ struct ForwardArgs {
     CapPages p;
     unsigned tiles;
     int shift;  // of the rows of a stretch
-    // PAGED: blocks of a stretch that share its keys, with sums [parts][q_rows][heads] and numerators [parts][q_rows][heads][dim] in Float32
+    // PAGED: blocks of a stretch that share its keys, with sums [parts][q_rows][heads] and numerators
+    // [parts][q_rows][heads][dim] in Float32
     int parts;
     float *part_sums, *part_values;
 };
@@ -153,7 +156,8 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
     __shared__ __align__(16) Shared shared;
     f32x2 *lines = shared.lines;
 
-    const int together = SPLIT ? 0 : 7 - a.shift, members = a.s.group >> together;  // heads of a block, as a power of two; blocks that share keys
+    // heads of a block, as a power of two; blocks that share keys
+    const int together = SPLIT ? 0 : 7 - a.shift, members = a.s.group >> together;
     const unsigned blocks = (unsigned)unit_blocks(a.tiles, a.s.kv_heads, a.parts, members);
     if (blockIdx.x >= blocks) {
         const int head = (int)(blockIdx.x - blocks);
@@ -222,10 +226,11 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
     if constexpr (SPLIT) __syncthreads();
     float sum, rounded_sum;  // of the weights, and of the weights as the product has them
 
-    // Tiles that every query of the block sees whole.  In the others a weight may be zero because its key is hidden, and the product
-    // with an infinite or NaN value would not be: a block whose numerators are not all finite goes over its keys once more, and
-    // then takes such values out of these tiles and adds them behind the loop where they are seen.  (Looking for them in every such tile took 4 to 7 %
-    // of the time over documents of some hundred tokens and windows.)
+    // Tiles that every query of the block sees whole.  In the others a weight may be zero because its key is
+    // hidden, and the product with an infinite or NaN value would not be: a block whose numerators are not all
+    // finite goes over its keys once more, and then takes such values out of these tiles and adds them behind
+    // the loop where they are seen.  (Looking for them in every such tile took 4 to 7 % of the time over
+    // documents of some hundred tokens and windows.)
     const int whole_from = a.s.window > 0 ? block_last - a.s.window + 1 : 0, whole_to = a.s.causal ? min(n_keys, block_first + 1) : n_keys;
     auto whole = [&](int j0) { return j0 >= whole_from && j0 + kKeys <= whole_to; };
     const int first_seen = a.s.window > 0 ? max(0, my_place - a.s.window + 1) : 0, last_seen = a.s.causal ? min(n_keys, my_place + 1) : n_keys;
@@ -252,7 +257,8 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
         wait_for_loads();
         const bool is_whole = whole(j0);
         if (careful.value && !is_whole) clean_values<D, kLoaders>(v_tile, loader, n_keys - j0);
-        // Behind this barrier the tile is complete and all are done with the one before, whose place the next one takes.
+        // Behind this barrier the tile is complete and all are done with the one before, whose place the next
+        // one takes.
         tile_complete<SPLIT>();
         if (!SPLIT && j0 + kStep < key_end) stream.next(j0 + kStep, next_k, next_v);
         if (is_whole ? !idle : !idle && !(a.s.causal && j0 > place0 + 31) && !(a.s.window > 0 && j0 + kKeys - 1 <= place0 - a.s.window))
@@ -306,13 +312,18 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
 
     sum += __shfl_xor(sum, 32);
     rounded_sum += __shfl_xor(rounded_sum, 32);
-    // Numerators 4 i .. 4 i + 3 of every 32: a wavefront's own, or (SPLIT) a fourth of all, joined in the order of the wavefronts.
+    // Numerators 4 i .. 4 i + 3 of every 32: a wavefront's own, or (SPLIT) a fourth of all, joined in the order
+    // of the wavefronts.
     constexpr int kQuads = D / 8, kMine = SPLIT ? kQuads / kWaves : kQuads;
     const int quad0 = SPLIT ? wave * kMine : 0;
     f32x4 n[kMine];
+    auto quad = [&](int i) {
+        const f32x16 &c = o[i / 4];
+        return f32x4{c[4 * (i % 4)], c[4 * (i % 4) + 1], c[4 * (i % 4) + 2], c[4 * (i % 4) + 3]};
+    };
     if constexpr (SPLIT) {
 #pragma unroll
-        for (int i = 0; i < kQuads; ++i) shared.sums[wave][i][lane] = f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+        for (int i = 0; i < kQuads; ++i) shared.sums[wave][i][lane] = quad(i);
         shared.weights[wave][lane] = lane < 32 ? rounded_sum : sum;
         __syncthreads();
 #pragma unroll
@@ -327,7 +338,7 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < kQuads; ++i) n[i] = f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+        for (int i = 0; i < kQuads; ++i) n[i] = quad(i);
     }
     const bool writes_sums = lane < 32 && (!SPLIT || wave == 0) && row < at.end;
     if (SUMS && writes_sums)
@@ -342,7 +353,8 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 2 : 3) void cap_forward_kernel(Fo
 #pragma unroll
             for (int i = 0; i < kMine; ++i) *reinterpret_cast<f32x4 *>(values + 8 * i) = n[i];
         } else {
-            store_rows_wide<D>(shared.tiles[0].k[0] + wave * kBytes, a.part_values + at_row * D, (long long)a.s.heads * D, at.end - row0, [&](int i) { return n[i]; });
+            store_rows_wide<D>(shared.tiles[0].k[0] + wave * kBytes, a.part_values + at_row * D, (long long)a.s.heads * D,
+                               at.end - row0, [&](int i) { return n[i]; });
         }
         return;
     }
@@ -391,7 +403,8 @@ __global__ __launch_bounds__(kThreads) void cap_join_parts_kernel(ForwardArgs a)
 template <bool PAGED, bool SUMS>
 ktanh_status_t launch_forward(const ForwardArgs &a, size_t dim, bool split, const KtCapPack &pack, ktanh_stream_t stream)
 {
-    const unsigned long long blocks = unit_blocks(a.tiles, a.s.kv_heads, a.parts, split ? a.s.group : a.s.group >> (7 - a.shift)) + (a.parts == 1 ? a.s.heads : 0);
+    const int members = split ? a.s.group : a.s.group >> (7 - a.shift);
+    const unsigned long long blocks = unit_blocks(a.tiles, a.s.kv_heads, a.parts, members) + (a.parts == 1 ? a.s.heads : 0);
     const unsigned long long joins = ((unsigned long long)a.s.q_rows * a.s.heads * dim / 4 + kThreads - 1) / kThreads;
     if (blocks > kMaxBlocks || (a.parts > 1 && joins > kMaxBlocks)) return KT_ERR_SHAPE;
     auto *kernel = split ? dim == 64 ? &cap_forward_kernel<64, PAGED, SUMS, true> : &cap_forward_kernel<128, PAGED, SUMS, true>
@@ -414,7 +427,8 @@ ktanh_status_t attention(const kcap_shape_t *shape, const uint16_t *q, const uin
 {
     if (shape == nullptr) return KT_ERR_NULL;
     if (shape->q_rows == 0 || shape->docs == 0) return KT_OK;
-    if (q == nullptr || q_offsets == nullptr || k_offsets == nullptr || o == nullptr || ((k == nullptr || v == nullptr) && shape->k_rows != 0)) return KT_ERR_NULL;
+    if (q == nullptr || q_offsets == nullptr || k_offsets == nullptr || o == nullptr) return KT_ERR_NULL;
+    if ((k == nullptr || v == nullptr) && shape->k_rows != 0) return KT_ERR_NULL;
     ForwardArgs a{};
     ktanh_status_t st = read_shape(shape, q, k, v, &a.s);
     if (st != KT_OK) return st;
@@ -431,16 +445,20 @@ ktanh_status_t attention(const kcap_shape_t *shape, const uint16_t *q, const uin
     const bool split = split_tiles(*shape);
     a.shift = rows_shift(a.s, split);
     a.tiles = (unsigned)stretches(shape->q_rows, shape->docs, a.shift);
-    return lse != nullptr ? launch_forward<false, true>(a, shape->dim, split, pack, stream) : launch_forward<false, false>(a, shape->dim, split, pack, stream);
+    return lse != nullptr ? launch_forward<false, true>(a, shape->dim, split, pack, stream)
+                          : launch_forward<false, false>(a, shape->dim, split, pack, stream);
 }
 
 }  // namespace
 
-// How many blocks share the keys of a stretch, and of which kind they are: the least time of all, by what a block takes for a tile and around its
-// tiles, how many a compute unit holds, and the launch that joins parts written and read at 4 TB/s.  Only the longest text is known here; texts
-// are taken to be spread evenly up to it, so that the time is that of the longest or that of all on average.
-// Four pieces of 512 tokens behind texts of up to 6000, 32 heads of 128: 253 us in one part, 261 in two, 228 in three (of 6000 each: 260, 304, 277).
-// 8 tokens behind 16384 of four sequences: 143 us in blocks of 128 rows, 96 in blocks of 32; 512 behind 512 of eight: 58 and 107.
+// How many blocks share the keys of a stretch, and of which kind they are: the least time of all, by what a
+// block takes for a tile and around its tiles, how many a compute unit holds, and the launch that joins parts
+// written and read at 4 TB/s.  Only the longest text is known here; texts are taken to be spread evenly up to
+// it, so that the time is that of the longest or that of all on average.
+// Four pieces of 512 tokens behind texts of up to 6000, 32 heads of 128: 253 us in one part, 261 in two, 228 in
+// three (of 6000 each: 260, 304, 277).
+// 8 tokens behind 16384 of four sequences: 143 us in blocks of 128 rows, 96 in blocks of 32; 512 behind 512 of
+// eight: 58 and 107.
 ktanh_cap::ForwardPlan ktanh_cap::forward_plan(const kcap_shape_t &s, const kcap_pages_t &p)
 {
     ForwardPlan best{false, 1};
@@ -452,7 +470,8 @@ ktanh_cap::ForwardPlan ktanh_cap::forward_plan(const kcap_shape_t &s, const kcap
         const size_t together = split ? 1 : (size_t)heads_together(s.heads / s.kv_heads);
         const double rows = split ? 32.0 : (double)(kRows / together), blocks = std::ceil(each / rows) * docs * (double)(s.heads / together);
         const double keys = s.window > 0 ? std::min(cached, (double)s.window + std::min(rows, each)) : cached;
-        // Microseconds of 32 keys with 128 rows, or 128 with 32, by how many blocks a compute unit holds, up to as many as it can.
+        // Microseconds of 32 keys with 128 rows, or 128 with 32, by how many blocks a compute unit holds, up to
+        // as many as it can.
         const double full_us[4] = {0.0, 1.2, 1.45, 1.85}, split_us[3] = {0.0, 1.75, 2.6};
         const double *tile_us = split ? split_us : full_us;
         const int most = split ? 2 : 3;
@@ -469,8 +488,9 @@ ktanh_cap::ForwardPlan ktanh_cap::forward_plan(const kcap_shape_t &s, const kcap
     return best;
 }
 
-ktanh_status_t ktanh_cap::launch_forward_paged(const CapShape &s, const CapPages &p, const int *q_offsets, uint16_t *o, int dim, ForwardPlan plan,
-                                               float *workspace, const KtCapPack &pack, ktanh_stream_t stream)
+ktanh_status_t ktanh_cap::launch_forward_paged(const CapShape &s, const CapPages &p, const int *q_offsets, uint16_t *o,
+                                               int dim, ForwardPlan plan, float *workspace, const KtCapPack &pack,
+                                               ktanh_stream_t stream)
 {
     ForwardArgs a{};
     a.s = s;

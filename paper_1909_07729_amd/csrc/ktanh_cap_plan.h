@@ -1,5 +1,6 @@
-// Internal to libktanh: how the work of the capped attention over documents is cut into blocks.  Host code, from what is known on the host: numbers of
-// documents, rows and heads, but not how the rows are dealt to the documents.
+// Internal to libktanh: how the work of the capped attention over documents is cut into blocks.  Host code,
+// from what is known on the host: numbers of documents, rows and heads, but not how the rows are dealt to the
+// documents.
 #pragma once
 #include <algorithm>
 #include <cmath>
@@ -11,9 +12,10 @@ namespace ktanh_cap {
 // Query heads of a group that a block has together.
 inline int heads_together(size_t group) { return group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1; }
 
-// Whether blocks hold 32 queries, their wavefronts sharing the tiles of keys, rather than 32 in each: the shorter time of the block that takes
-// longest, or of all blocks, by what they take for a tile alone, a compute unit with all that it holds, and around their tiles.  Documents count as
-// 1.2 times as long as the average.  Output, then gradients, causal, in us, wavefronts of their own rows | sharing the tiles:
+// Whether blocks hold 32 queries, their wavefronts sharing the tiles of keys, rather than 32 in each: the
+// shorter time of the block that takes longest, or of all blocks, by what they take for a tile alone, a compute
+// unit with all that it holds, and around their tiles.  Documents count as 1.2 times as long as the average.
+// Output, then gradients, causal, in us, wavefronts of their own rows | sharing the tiles:
 //    1024 rows,  8 heads of 128 on 8        36  63 |  15  39
 //    4096 rows,  8 heads of 128 on 8       128 245 |  65 179
 //    1500 rows, 32 heads of 128 on 8        51 130 |  45 128
@@ -31,7 +33,8 @@ inline bool split_tiles(const kcap_shape_t &s)
     if (s.k_rows <= 32 * s.docs) return false;  // one tile cannot be shared
     const double docs = (double)s.docs, queries = (double)s.q_rows / docs, keys = (double)s.k_rows / docs;
     const bool narrow = s.window > 0 && (double)s.window + 128.0 < keys;
-    const double seen = narrow ? (double)s.window + 128.0 : keys, mean = s.causal && !narrow ? 0.5 : 1.0, longest = docs > 1.0 && !narrow ? 1.2 : 1.0;
+    const double seen = narrow ? (double)s.window + 128.0 : keys, mean = s.causal && !narrow ? 0.5 : 1.0;
+    const double longest = docs > 1.0 && !narrow ? 1.2 : 1.0;
     const double together = heads_together(s.heads / s.kv_heads);
     const double own_blocks = std::ceil(queries * together / 128.0) * docs * (double)s.heads / together, own_tiles = seen / 32.0;
     const double sharing_blocks = std::ceil(queries / 32.0) * docs * (double)s.heads, sharing_tiles = seen / 128.0;
@@ -40,17 +43,19 @@ inline bool split_tiles(const kcap_shape_t &s)
            std::max(3.0 + 1.03 * longest * own_tiles, rounds * own_blocks * (0.57 * mean * own_tiles + 3.5));
 }
 
-// How the blocks over keys are cut: their rows, and into how many parts the query heads that share a key/value head are dealt, each with a
-// block and sums in Float32 of its own that another kernel adds up.
+// How the blocks over keys are cut: their rows, and into how many parts the query heads that share a key/value
+// head are dealt, each with a block and sums in Float32 of its own that another kernel adds up.
 struct KeysPlan {
     bool split;
     int parts;
 };
 
-// The least time of all: of the block that takes longest, or of all blocks with some of that one's at their end, by what a block takes for a tile
-// alone, and a compute unit with all that it holds, and around its tiles; and of the parts written and read.  Documents count as 1.6 times as long
-// as the average.  Fitted to 1277 calls, documents alike in length or cut at random, 5 to 64 heads: 1.5 % above the best plan on average (alike or one
-// 1.2, cut evenly 0.8, at random 2.7), 1.4 % of them more than 20 % above.  Gradients causal, in us with four | two | one part | one part in blocks of 32 rows:
+// The least time of all: of the block that takes longest, or of all blocks with some of that one's at their
+// end, by what a block takes for a tile alone, and a compute unit with all that it holds, and around its tiles;
+// and of the parts written and read.  Documents count as 1.6 times as long as the average.  Fitted to 754 calls
+// with 5 to 40 heads and held against 523 more: 1.5 % above the best plan on average (documents alike or only
+// one 1.2, of evenly spread lengths 0.8, cut at random 2.7), 1.4 % of them more than 20 % above.  Gradients
+// causal, in us with four | two | one part | one part in blocks of 32 rows:
 //    six documents, 8192 rows at random, 32 heads of 128 on 8    934 |  988 | 1338 |  905
 //    64 documents of 256                                         526 |  413 |  334 |  413
 //    32 documents of 256                                         283 |  228 |  185 |  245
@@ -74,7 +79,8 @@ inline KeysPlan keys_plan(const kcap_shape_t &s)
         for (int parts = 1; parts <= group; ++parts) {
             if (group % parts != 0) continue;
             const double heads = group / parts, blocks = std::ceil(keys / rows) * docs * (double)s.kv_heads * parts;
-            const double longest = heads * tiles * (s.docs > 1 && !narrow ? 1.6 : 1.0) * alone_us, all = blocks * heads * mean * all_us / 256.0 + around_us * blocks / 512.0;
+            const double longest = heads * tiles * (s.docs > 1 && !narrow ? 1.6 : 1.0) * alone_us;
+            const double all = blocks * heads * mean * all_us / 256.0 + around_us * blocks / 512.0;
             const double join = parts > 1 ? 5.0 + parts * (double)s.k_rows * (double)s.kv_heads * (double)s.dim * 16.0 / 6e6 : 0.0;
             const double t = std::max(longest, all + 0.3 * longest) + join;
             if (least == 0.0 || t < least) {

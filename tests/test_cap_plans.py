@@ -50,7 +50,7 @@ KEYS = {
 
 
 def test_keys_gradients_take_near_the_least_that_was_measured(plan_of):
-    """Within 20 %: the rule's own times are fitted to some 1300 calls, of which 98 in 100 are."""
+    """Within 20 %, as 98 in 100 of the 1277 calls that the rule was held against."""
     for shape, (_, split, parts) in zip(KEYS, plan_of(KEYS)):
         times = KEYS[shape]
         assert times[split, parts] <= 1.2 * min(times.values()), (shape, split, parts, times)
@@ -70,7 +70,7 @@ OUTPUTS = {
 
 
 def test_outputs_take_near_the_least_that_was_measured(plan_of):
-    """Within 25 %, as 98 in 100 of the calls that the rule was fitted to."""
+    """Within 25 %, as 99 in 100 of those calls."""
     for shape, (split, _, _) in zip(OUTPUTS, plan_of(OUTPUTS)):
         times = OUTPUTS[shape]
         assert times[split] <= 1.25 * min(times), (shape, split, times)
