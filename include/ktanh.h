@@ -297,6 +297,53 @@ ktanh_status_t klstm_cell64_backward(const uint16_t *gates, const float *c_prev,
                                      const float *dc_next, uint16_t *dgates, float *dc_prev, size_t B,
                                      size_t H, const ktanh_lut64_t *lut, ktanh_stream_t stream);
 
+/* ---- Activations that keep their input in 8 bits ------------------------------------------------------
+ * kswish and kgelu (and their 64-interval and Float32 forms) that also write what the backward pass needs in one byte a value in
+ * place of two or four, and that pass.  Each KTANH_KEEP8_GROUP consecutive values (the last ones may be fewer) share a Float32 scale;
+ * with m the largest finite magnitude among them, in Float32 operations rounded to nearest even:
+ *   scale = m / 127,   code = round(x * (127 / m));     m below 2^-120: scale 0 and codes 0
+ * A code stands for x8 = code * scale, rounded to the tensor's type; -128 stands for an infinity or a NaN, and is read as a NaN.
+ *   in, out    device, n elements each; out is that of kswish / kgelu, bit for bit, and may be in
+ *   codes      device, n bytes
+ *   scales     device, Float32, one for each group: n / KTANH_KEEP8_GROUP rounded up
+ * backward: dx is that of kswish_backward / kgelu_backward at x8, bit for bit, and y, where it is not NULL, that of kswish / kgelu
+ * at x8 (which the gradient of the weights behind the activation takes, so that the activation's output need not be kept either).
+ * dx or y may be dy, but not both.  Alignment: elements of in, out, dy, dx and y, and 4 bytes of scales (KT_ERR_ALIGN); tensors that start on
+ * 16 bytes are faster by up to a fifth.  Up to 2^34 - 256 Float32 or 2^35 - 512 BFloat16 elements (KT_ERR_SHAPE). */
+#define KTANH_KEEP8_GROUP 128
+ktanh_status_t kswish_keep8(const uint16_t *in, uint16_t *out, int8_t *codes, float *scales, size_t n, const ktanh_lut_t *lut,
+                            ktanh_stream_t stream);
+ktanh_status_t kgelu_keep8(const uint16_t *in, uint16_t *out, int8_t *codes, float *scales, size_t n, const ktanh_lut_t *lut,
+                           ktanh_stream_t stream);
+ktanh_status_t kswish64_keep8(const uint16_t *in, uint16_t *out, int8_t *codes, float *scales, size_t n, const ktanh_lut64_t *lut,
+                              ktanh_stream_t stream);
+ktanh_status_t kgelu64_keep8(const uint16_t *in, uint16_t *out, int8_t *codes, float *scales, size_t n, const ktanh_lut64_t *lut,
+                             ktanh_stream_t stream);
+ktanh_status_t kswish_f32_keep8(const float *in, float *out, int8_t *codes, float *scales, size_t n, const ktanh_lut_t *lut,
+                                ktanh_stream_t stream);
+ktanh_status_t kgelu_f32_keep8(const float *in, float *out, int8_t *codes, float *scales, size_t n, const ktanh_lut_t *lut,
+                               ktanh_stream_t stream);
+ktanh_status_t kswish64_f32_keep8(const float *in, float *out, int8_t *codes, float *scales, size_t n, const ktanh_lut64_t *lut,
+                                  ktanh_stream_t stream);
+ktanh_status_t kgelu64_f32_keep8(const float *in, float *out, int8_t *codes, float *scales, size_t n, const ktanh_lut64_t *lut,
+                                 ktanh_stream_t stream);
+ktanh_status_t kswish_keep8_backward(const uint16_t *dy, const int8_t *codes, const float *scales, uint16_t *dx, uint16_t *y, size_t n,
+                                     const ktanh_lut_t *lut, ktanh_stream_t stream);
+ktanh_status_t kgelu_keep8_backward(const uint16_t *dy, const int8_t *codes, const float *scales, uint16_t *dx, uint16_t *y, size_t n,
+                                    const ktanh_lut_t *lut, ktanh_stream_t stream);
+ktanh_status_t kswish64_keep8_backward(const uint16_t *dy, const int8_t *codes, const float *scales, uint16_t *dx, uint16_t *y, size_t n,
+                                       const ktanh_lut64_t *lut, ktanh_stream_t stream);
+ktanh_status_t kgelu64_keep8_backward(const uint16_t *dy, const int8_t *codes, const float *scales, uint16_t *dx, uint16_t *y, size_t n,
+                                      const ktanh_lut64_t *lut, ktanh_stream_t stream);
+ktanh_status_t kswish_f32_keep8_backward(const float *dy, const int8_t *codes, const float *scales, float *dx, float *y, size_t n,
+                                         const ktanh_lut_t *lut, ktanh_stream_t stream);
+ktanh_status_t kgelu_f32_keep8_backward(const float *dy, const int8_t *codes, const float *scales, float *dx, float *y, size_t n,
+                                        const ktanh_lut_t *lut, ktanh_stream_t stream);
+ktanh_status_t kswish64_f32_keep8_backward(const float *dy, const int8_t *codes, const float *scales, float *dx, float *y, size_t n,
+                                           const ktanh_lut64_t *lut, ktanh_stream_t stream);
+ktanh_status_t kgelu64_f32_keep8_backward(const float *dy, const int8_t *codes, const float *scales, float *dx, float *y, size_t n,
+                                          const ktanh_lut64_t *lut, ktanh_stream_t stream);
+
 /* ---- Attention with capped scores -------------------------------------------------------------------
  * Where a transformer bounds its attention scores with TanH, K-TanH takes its place.  For a query q and a key k
  * that it sees, in Float32:

@@ -72,6 +72,23 @@ class _FromInput(torch.autograd.Function):
         return getattr(binding, ctx.bwd_name)(dy.contiguous(), x, lut=ctx.lut), None, None
 
 
+class _Kept8(torch.autograd.Function):
+    """Swish and GELU whose input is kept in 8 bits for the backward pass."""
+
+    @staticmethod
+    def forward(ctx, x, lut, names):
+        fwd_name = names[_is_f32(x)][0]
+        y, codes, scales = getattr(binding, fwd_name + "_keep8")(x.contiguous(), lut=lut)
+        ctx.save_for_backward(codes, scales)
+        ctx.lut, ctx.bwd_name = lut, fwd_name + "_keep8_backward"
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        codes, scales = ctx.saved_tensors
+        return getattr(binding, ctx.bwd_name)(dy.contiguous(), codes, scales, lut=ctx.lut), None, None
+
+
 # (forward entry point, gradient entry point) by table width [wide] and tensor type [Float32];
 # the gradients of TanH and Sigmoid read the forward output and no table, so they serve both widths
 _TANH = {False: {False: ("ktanh_bf16", "ktanh_bf16_backward"), True: ("ktanh_f32", "ktanh_f32_backward")},
@@ -149,14 +166,27 @@ def ksigmoid(x: torch.Tensor, lut=None, intervals: int = 32) -> torch.Tensor:
     return _activation(2, _FromOutput, _SIGMOID, x, lut, intervals)
 
 
-def kswish(x: torch.Tensor, lut=None, intervals: int = 32) -> torch.Tensor:
-    """Swish through K-TanH of a BFloat16 or Float32 tensor, differentiable with respect to ``x``."""
-    return _activation(4, _FromInput, _SWISH, x, lut, intervals)
+def _from_input(code, names, x, lut, intervals, keep):
+    if keep is None:
+        return _activation(code, _FromInput, names, x, lut, intervals)
+    if keep != 8:
+        raise ValueError("keep must be None or 8")
+    wide = _is_wide(lut, intervals)
+    if x.requires_grad and torch.is_grad_enabled():
+        return _Kept8.apply(x, lut, names[wide])
+    return _activation(code, _FromInput, names, x, lut, intervals)      # nothing is kept
 
 
-def kgelu(x: torch.Tensor, lut=None, intervals: int = 32) -> torch.Tensor:
-    """GELU (tanh form) through K-TanH of a BFloat16 or Float32 tensor, differentiable with respect to ``x``."""
-    return _activation(6, _FromInput, _GELU, x, lut, intervals)
+def kswish(x: torch.Tensor, lut=None, intervals: int = 32, keep=None) -> torch.Tensor:
+    """Swish through K-TanH of a BFloat16 or Float32 tensor, differentiable with respect to ``x``.  ``keep=8``: the backward pass
+    finds ``x`` in 8 bits (``binding.kswish_keep8``)."""
+    return _from_input(4, _SWISH, x, lut, intervals, keep)
+
+
+def kgelu(x: torch.Tensor, lut=None, intervals: int = 32, keep=None) -> torch.Tensor:
+    """GELU (tanh form) through K-TanH of a BFloat16 or Float32 tensor, differentiable with respect to ``x``.  ``keep=8``: the
+    backward pass finds ``x`` in 8 bits (``binding.kgelu_keep8``)."""
+    return _from_input(6, _GELU, x, lut, intervals, keep)
 
 
 def klstm_cell(gates: torch.Tensor, c_prev: torch.Tensor, lut=None, intervals: int = 32):

@@ -52,6 +52,10 @@ SIGNATURES = {
     "kcap_attention_paged_workspace": "agt",
     "kcap_attention_paged": "agppppppppls", "kcap_attention64_paged": "agppppppppLs",
     "kcap_append": "agpppppppppppnnts",
+    "kswish_keep8": "ppppnls", "kswish_keep8_backward": "pppppnls", "kgelu_keep8": "ppppnls", "kgelu_keep8_backward": "pppppnls",
+    "kswish_f32_keep8": "ppppnls", "kswish_f32_keep8_backward": "pppppnls", "kgelu_f32_keep8": "ppppnls", "kgelu_f32_keep8_backward": "pppppnls",
+    "kswish64_keep8": "ppppnLs", "kswish64_keep8_backward": "pppppnLs", "kgelu64_keep8": "ppppnLs", "kgelu64_keep8_backward": "pppppnLs",
+    "kswish64_f32_keep8": "ppppnLs", "kswish64_f32_keep8_backward": "pppppnLs", "kgelu64_f32_keep8": "ppppnLs", "kgelu64_f32_keep8_backward": "pppppnLs",
 }
 EXPORTS = tuple(SIGNATURES)
 
@@ -575,6 +579,142 @@ def klstm_cell_backward(gates, c_prev, dh, dc_next, dgates=None, dc_prev=None, l
     if st != 0:
         raise KtanhError(st, _entry)
     return dgates, dc_prev
+
+
+# --------------------------------------------------------------------- activations that keep 8 bits
+
+KEEP8_GROUP = 128       # values that share a scale
+
+
+def _check_here(*tensors):
+    """Calls run on the current device."""
+    for t in tensors:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _like(t, like, dtypes, what, stream):
+    """A given output that is as large as `like`, or a new one."""
+    if t is None:
+        return _empty(like.shape, like.dtype, like, stream)
+    _check(t, dtypes, what)
+    if t.numel() != like.numel():
+        raise ValueError(f"{what} differs in size")
+    return t
+
+
+def _check_checkpoint(codes, scales, count):
+    _check(codes, (torch.int8,), "codes")
+    _check(scales, (torch.float32,), "scales")
+    if codes.numel() != count or scales.numel() != -(-count // KEEP8_GROUP):
+        raise ValueError("codes must have one byte for each value and scales one number for each 128")
+
+
+def _keep8(name, x, out, codes, scales, lut, stream, dtypes):
+    _check(x, dtypes, "in")
+    out = _like(out, x, dtypes, "out", stream)
+    codes = _empty(x.shape, torch.int8, x, stream) if codes is None else codes
+    scales = _empty((-(-x.numel() // KEEP8_GROUP),), torch.float32, x, stream) if scales is None else scales
+    _check_checkpoint(codes, scales, x.numel())
+    _check_here(x, out, codes, scales)
+    st = getattr(load_library(), name)(x.data_ptr(), out.data_ptr(), codes.data_ptr(), scales.data_ptr(), x.numel(), _lut_arg(lut),
+                                       _stream_handle(stream))
+    if st != 0:
+        raise KtanhError(st, name)
+    return out, codes, scales
+
+
+def _keep8_backward(name, dy, codes, scales, rebuild, dx, y, lut, stream, dtypes):
+    _check(dy, dtypes, "dy")
+    _check_checkpoint(codes, scales, dy.numel())
+    dx = _like(dx, dy, dtypes, "dx", stream)
+    y = _like(y, dy, dtypes, "y", stream) if rebuild or y is not None else None
+    _check_here(dy, codes, scales, dx, y)
+    st = getattr(load_library(), name)(dy.data_ptr(), codes.data_ptr(), scales.data_ptr(), dx.data_ptr(), None if y is None else y.data_ptr(),
+                                       dy.numel(), _lut_arg(lut), _stream_handle(stream))
+    if st != 0:
+        raise KtanhError(st, name)
+    return dx if y is None else (dx, y)
+
+
+def kswish_keep8(x, out=None, codes=None, scales=None, lut=None, stream=None):
+    """``kswish`` that also keeps its input in 8 bits: (out, codes int8 like ``x``, scales Float32 of each 128 consecutive values)."""
+    return _keep8("kswish_keep8", x, out, codes, scales, lut, stream, _BF16_VIEWS)
+
+
+def kswish_keep8_backward(dy, codes, scales, rebuild=False, dx=None, y=None, lut=None, stream=None):
+    """``kswish_backward`` at the values that the codes stand for: dx, or with ``rebuild`` (dx, ``kswish`` of those values)."""
+    return _keep8_backward("kswish_keep8_backward", dy, codes, scales, rebuild, dx, y, lut, stream, _BF16_VIEWS)
+
+
+def kgelu_keep8(x, out=None, codes=None, scales=None, lut=None, stream=None):
+    """``kgelu`` that also keeps its input in 8 bits: (out, codes int8 like ``x``, scales Float32 of each 128 consecutive values)."""
+    return _keep8("kgelu_keep8", x, out, codes, scales, lut, stream, _BF16_VIEWS)
+
+
+def kgelu_keep8_backward(dy, codes, scales, rebuild=False, dx=None, y=None, lut=None, stream=None):
+    """``kgelu_backward`` at the values that the codes stand for: dx, or with ``rebuild`` (dx, ``kgelu`` of those values)."""
+    return _keep8_backward("kgelu_keep8_backward", dy, codes, scales, rebuild, dx, y, lut, stream, _BF16_VIEWS)
+
+
+def kswish_f32_keep8(x, out=None, codes=None, scales=None, lut=None, stream=None):
+    """``kswish_keep8`` on Float32 tensors."""
+    return _keep8("kswish_f32_keep8", x, out, codes, scales, lut, stream, (torch.float32,))
+
+
+def kswish_f32_keep8_backward(dy, codes, scales, rebuild=False, dx=None, y=None, lut=None, stream=None):
+    """``kswish_keep8_backward`` on Float32 tensors."""
+    return _keep8_backward("kswish_f32_keep8_backward", dy, codes, scales, rebuild, dx, y, lut, stream, (torch.float32,))
+
+
+def kgelu_f32_keep8(x, out=None, codes=None, scales=None, lut=None, stream=None):
+    """``kgelu_keep8`` on Float32 tensors."""
+    return _keep8("kgelu_f32_keep8", x, out, codes, scales, lut, stream, (torch.float32,))
+
+
+def kgelu_f32_keep8_backward(dy, codes, scales, rebuild=False, dx=None, y=None, lut=None, stream=None):
+    """``kgelu_keep8_backward`` on Float32 tensors."""
+    return _keep8_backward("kgelu_f32_keep8_backward", dy, codes, scales, rebuild, dx, y, lut, stream, (torch.float32,))
+
+
+def kswish64_keep8(x, out=None, codes=None, scales=None, lut=None, stream=None):
+    """``kswish_keep8`` with a 64-interval table (``KtanhLut64``; None = the fitted one)."""
+    return _keep8("kswish64_keep8", x, out, codes, scales, lut, stream, _BF16_VIEWS)
+
+
+def kswish64_keep8_backward(dy, codes, scales, rebuild=False, dx=None, y=None, lut=None, stream=None):
+    """``kswish_keep8_backward`` with a 64-interval table (``KtanhLut64``; None = the fitted one)."""
+    return _keep8_backward("kswish64_keep8_backward", dy, codes, scales, rebuild, dx, y, lut, stream, _BF16_VIEWS)
+
+
+def kgelu64_keep8(x, out=None, codes=None, scales=None, lut=None, stream=None):
+    """``kgelu_keep8`` with a 64-interval table (``KtanhLut64``; None = the fitted one)."""
+    return _keep8("kgelu64_keep8", x, out, codes, scales, lut, stream, _BF16_VIEWS)
+
+
+def kgelu64_keep8_backward(dy, codes, scales, rebuild=False, dx=None, y=None, lut=None, stream=None):
+    """``kgelu_keep8_backward`` with a 64-interval table (``KtanhLut64``; None = the fitted one)."""
+    return _keep8_backward("kgelu64_keep8_backward", dy, codes, scales, rebuild, dx, y, lut, stream, _BF16_VIEWS)
+
+
+def kswish64_f32_keep8(x, out=None, codes=None, scales=None, lut=None, stream=None):
+    """``kswish_keep8`` with a 64-interval table (``KtanhLut64``; None = the fitted one) on Float32 tensors."""
+    return _keep8("kswish64_f32_keep8", x, out, codes, scales, lut, stream, (torch.float32,))
+
+
+def kswish64_f32_keep8_backward(dy, codes, scales, rebuild=False, dx=None, y=None, lut=None, stream=None):
+    """``kswish_keep8_backward`` with a 64-interval table (``KtanhLut64``; None = the fitted one) on Float32 tensors."""
+    return _keep8_backward("kswish64_f32_keep8_backward", dy, codes, scales, rebuild, dx, y, lut, stream, (torch.float32,))
+
+
+def kgelu64_f32_keep8(x, out=None, codes=None, scales=None, lut=None, stream=None):
+    """``kgelu_keep8`` with a 64-interval table (``KtanhLut64``; None = the fitted one) on Float32 tensors."""
+    return _keep8("kgelu64_f32_keep8", x, out, codes, scales, lut, stream, (torch.float32,))
+
+
+def kgelu64_f32_keep8_backward(dy, codes, scales, rebuild=False, dx=None, y=None, lut=None, stream=None):
+    """``kgelu_keep8_backward`` with a 64-interval table (``KtanhLut64``; None = the fitted one) on Float32 tensors."""
+    return _keep8_backward("kgelu64_f32_keep8_backward", dy, codes, scales, rebuild, dx, y, lut, stream, (torch.float32,))
 
 
 # ------------------------------------------------------------------------- attention with capped scores

@@ -1,0 +1,358 @@
+// libktanh: Swish and GELU that keep their input in 8 bits for the backward pass, and that pass.
+//
+// What the backward pass of Swish and GELU needs is the forward input.  Kept as it is it costs 2 or 4 bytes a value from the forward to
+// the backward pass; here it costs one, and 4 bytes for each 128 consecutive values (a group): with m the largest finite magnitude of
+// the group
+//   scale = m / 127,   code = round(x * (127 / m)),   and what the code stands for is code * scale, rounded to the tensor's type.
+// The gradient is that of kswish_backward and kgelu_backward at the values that the codes stand for, operation for operation.  The code -128 stands
+// for an infinity or a NaN, whose gradient is a NaN in those calls too (Swish and GELU multiply it by a slope of zero); it is left out
+// of m, so that its neighbours keep their values.
+#include "ktanh_slopes.h"
+#include "ktanh_stream_impl.h"
+
+#include <type_traits>
+
+using namespace ktanh_device;
+
+namespace {
+
+constexpr unsigned kGroup = KTANH_KEEP8_GROUP;
+constexpr float kTiny = 0x1p-120f;  // below it 127 / m leaves Float32: such a group is taken as zeros
+
+// A lane has one 128-bit vector of values and as many codes, a wavefront 512 (BFloat16) or 256 (Float32) values, which are whole groups
+// of 16 or 32 lanes: the largest magnitude is found with cross-lane moves, and no group is shared between wavefronts.
+template <class ELEM> constexpr unsigned kPerLane = 16 / sizeof(ELEM);
+template <class ELEM> constexpr unsigned kGroupLanes = kGroup / kPerLane<ELEM>;
+
+template <class ELEM> struct CodeVec { typedef u32x2 type; };
+template <> struct CodeVec<uint32_t> { typedef uint32_t type; };
+
+// ------------------------------------------------------------------------------------ accesses
+// `count` (of kPerLane) elements from p, zeros behind them.  A whole vector comes with one access, also from an address that is only
+// aligned to its elements; only the last lane with values of a launch has fewer.
+template <bool ALIGNED, class ELEM>
+__device__ __forceinline__ uint4 load_values(const ELEM *p, unsigned count)
+{
+    if (count == kPerLane<ELEM>) return load_vec<ALIGNED, false>(reinterpret_cast<const char *>(p));
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    for (unsigned i = 0; i < kPerLane<ELEM>; ++i)
+        if (i < count) w[i * sizeof(ELEM) / 4] |= (uint32_t)p[i] << (8 * (i * sizeof(ELEM) % 4));
+    return uint4{w[0], w[1], w[2], w[3]};
+}
+
+template <bool ALIGNED, bool KEEP, class ELEM>
+__device__ __forceinline__ void store_values(ELEM *p, uint4 v, unsigned count)
+{
+    if (count == kPerLane<ELEM>) {
+        if constexpr (ALIGNED) store_stream<KEEP>(reinterpret_cast<uint4 *>(p), v);
+        else *reinterpret_cast<u32x4_anywhere *>(p) = u32x4{v.x, v.y, v.z, v.w};
+        return;
+    }
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    for (unsigned i = 0; i < kPerLane<ELEM>; ++i)
+        if (i < count) p[i] = (ELEM)(w[i * sizeof(ELEM) / 4] >> (8 * (i * sizeof(ELEM) % 4)));
+}
+
+typedef u32x2 u32x2_anywhere __attribute__((aligned(1)));
+typedef uint32_t u32_anywhere __attribute__((aligned(1)));
+
+// Codes, one byte each: two words a lane (BFloat16) or one.
+template <bool ALIGNED, class ELEM>
+__device__ __forceinline__ uint2 load_codes(const int8_t *p, unsigned count)
+{
+    if (count == kPerLane<ELEM>) {
+        if constexpr (sizeof(ELEM) == 2) {
+            u32x2 t;
+            if constexpr (ALIGNED) t = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p));
+            else t = *reinterpret_cast<const u32x2_anywhere *>(p);
+            return uint2{t.x, t.y};
+        } else {
+            if constexpr (ALIGNED) return uint2{__builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(p)), 0u};
+            else return uint2{*reinterpret_cast<const u32_anywhere *>(p), 0u};
+        }
+    }
+    uint32_t w[2] = {0u, 0u};
+    for (unsigned i = 0; i < kPerLane<ELEM>; ++i)
+        if (i < count) w[i / 4] |= (uint32_t)(uint8_t)p[i] << (8 * (i % 4));
+    return uint2{w[0], w[1]};
+}
+
+template <bool ALIGNED, class ELEM>
+__device__ __forceinline__ void store_codes(int8_t *p, uint2 c, unsigned count)
+{
+    if (count == kPerLane<ELEM>) {
+        if constexpr (sizeof(ELEM) == 2) {
+            if constexpr (ALIGNED) __builtin_nontemporal_store(u32x2{c.x, c.y}, reinterpret_cast<u32x2 *>(p));
+            else *reinterpret_cast<u32x2_anywhere *>(p) = u32x2{c.x, c.y};
+        } else {
+            if constexpr (ALIGNED) __builtin_nontemporal_store(c.x, reinterpret_cast<uint32_t *>(p));
+            else *reinterpret_cast<u32_anywhere *>(p) = c.x;
+        }
+        return;
+    }
+    const uint32_t w[2] = {c.x, c.y};
+    for (unsigned i = 0; i < kPerLane<ELEM>; ++i)
+        if (i < count) p[i] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
+}
+
+// ------------------------------------------------------------------------------------ codes
+// The vector's values in Float32.
+template <class ELEM>
+__device__ __forceinline__ void widen(uint4 v, float (&x)[kPerLane<ELEM>])
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (unsigned i = 0; i < 4; ++i) {
+        if constexpr (sizeof(ELEM) == 2) {
+            x[2 * i] = widen_lo(w[i]);
+            x[2 * i + 1] = widen_hi(w[i]);
+        } else {
+            x[i] = __uint_as_float(w[i]);
+        }
+    }
+}
+
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// The largest of a group's lanes, in all of them: four moves within a row of 16 lanes, and one to the other row for groups of 32.
+template <unsigned LANES>
+__device__ __forceinline__ uint32_t largest_of_group(uint32_t m)
+{
+    m = larger(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x128, 0xF, 0xF, false));  // row_ror:8
+    m = larger(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x124, 0xF, 0xF, false));
+    m = larger(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x122, 0xF, 0xF, false));
+    m = larger(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x121, 0xF, 0xF, false));
+    if constexpr (LANES == 32) m = larger(m, (uint32_t)__builtin_amdgcn_ds_swizzle((int)m, 0x401F));  // lane ^ 16
+    return m;
+}
+
+// The bits of the largest finite magnitude of a lane's values, as a Float32.  Magnitudes order like their bits.
+template <class ELEM>
+__device__ __forceinline__ uint32_t largest_of_lane(uint4 v, bool &odd)
+{
+    if constexpr (sizeof(ELEM) == 2) {
+        const uint32_t a = v.x & kMag2, b = v.y & kMag2, c = v.z & kMag2, d = v.w & kMag2;
+        const uint32_t m2 = max_pair(max_pair(a, b), max_pair(c, d));
+        const uint32_t m = larger(m2 & 0xFFFFu, m2 >> 16);
+        odd = m >= 0x7F80u;
+        return m << 16;
+    } else {
+        const uint32_t m = larger(larger(v.x & 0x7FFFFFFFu, v.y & 0x7FFFFFFFu), larger(v.z & 0x7FFFFFFFu, v.w & 0x7FFFFFFFu));
+        odd = m >= 0x7F800000u;
+        return m;
+    }
+}
+
+// The codes of a lane's vector, and its group's scale.
+template <class ELEM>
+__device__ __forceinline__ uint2 codes_of(uint4 v, float &scale)
+{
+    constexpr unsigned N = kPerLane<ELEM>;
+    float x[N];
+    widen<ELEM>(v, x);
+    bool odd;
+    uint32_t m = largest_of_lane<ELEM>(v, odd);
+    const bool any_odd = __any(odd);  // the wavefront has an infinity or a NaN
+    if (any_odd) {
+        m = 0;
+#pragma unroll
+        for (unsigned i = 0; i < N; ++i) {
+            const uint32_t mag = __float_as_uint(x[i]) & 0x7FFFFFFFu;
+            m = larger(m, mag < 0x7F800000u ? mag : 0u);
+        }
+    }
+    const float top = __uint_as_float(largest_of_group<kGroupLanes<ELEM>>(m));
+    const float inverse = top < kTiny ? 0.f : 127.0f / top;
+    scale = top < kTiny ? 0.f : top / 127.0f;
+    // x * inverse is at most 127 (1 + 2^-23); 1.5 * 2^23 added to it rounds it to an integer, to nearest even, whose two's complement
+    // is in the sum's low bits
+    uint32_t q[N];
+#pragma unroll
+    for (unsigned i = 0; i < N; ++i) q[i] = __float_as_uint(x[i] * inverse + 12582912.0f);
+    if (any_odd) {
+#pragma unroll
+        for (unsigned i = 0; i < N; ++i)
+            if ((__float_as_uint(x[i]) & 0x7FFFFFFFu) >= 0x7F800000u) q[i] = 0x80u;
+    }
+    auto four = [](uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+        return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u), 0x05040100u);
+    };
+    uint2 out{four(q[0], q[1], q[2], q[3]), 0u};
+    if constexpr (N == 8) out.y = four(q[4], q[5], q[6], q[7]);
+    return out;
+}
+
+// What four codes stand for, in Float32.
+__device__ __forceinline__ void values_of(uint32_t codes, float scale, float (&x)[4])
+{
+#pragma unroll
+    for (unsigned i = 0; i < 4; ++i) x[i] = (float)(int8_t)(codes >> (8 * i)) * scale;
+    // bytes equal to 0x80 leave a zero byte here; the lowest such byte is found exactly, and that is all that is asked
+    const uint32_t d = codes ^ 0x80808080u;
+    const bool odd = ((d - 0x01010101u) & ~d & 0x80808080u) != 0;
+    if (__any(odd)) {
+#pragma unroll
+        for (unsigned i = 0; i < 4; ++i)
+            if ((uint8_t)(codes >> (8 * i)) == 0x80u) x[i] = __builtin_nanf("");
+    }
+}
+
+// ------------------------------------------------------------------------------------ forward
+template <class ELEM, int OP, bool WIDE, bool ALIGNED, bool KEEP>
+__global__ __launch_bounds__(kBlock) void keep8_kernel(const ELEM *in, ELEM *out, int8_t *codes, float *scales, unsigned long long n,
+                                                       KtLutPack pack)
+{
+    constexpr unsigned N = kPerLane<ELEM>;
+    const LaneTable tab(pack);
+    const unsigned long long at = ((unsigned long long)blockIdx.x * kBlock + threadIdx.x) * N;
+    const unsigned count = at >= n ? 0u : n - at < N ? (unsigned)(n - at) : N;
+    uint4 v = uint4{0u, 0u, 0u, 0u};
+    if (count != 0) v = load_values<ALIGNED>(in + at, count);
+    float scale;
+    const uint2 c = codes_of<ELEM>(v, scale);
+    if (count != 0) {
+        store_codes<ALIGNED, ELEM>(codes + at, c, count);
+        if (threadIdx.x % kGroupLanes<ELEM> == 0) scales[at / kGroup] = scale;
+    }
+    if constexpr (sizeof(ELEM) == 2) v = apply_vec_bf16<OP, WIDE>(v, tab);
+    else v = apply_vec_f32<OP, WIDE>(v, tab);
+    if (count != 0) store_values<ALIGNED, KEEP>(out + at, v, count);
+}
+
+// ------------------------------------------------------------------------------------ backward
+// The activation itself from x and the K value that slope_of takes: x s, and (x / 2)(1 + t), which rounds like x (0.5 + 0.5 t).
+template <int GRAD>
+__device__ __forceinline__ float value_of(float x, float k)
+{
+    if constexpr (GRAD == GRAD_SWISH) return x * k;
+    else return x * __builtin_fmaf(0.5f, k, 0.5f);
+}
+
+template <class ELEM, int GRAD, bool WIDE, bool ALIGNED, bool KEEP, bool REBUILD>
+__global__ __launch_bounds__(kBlock) void keep8_backward_kernel(const ELEM *dy, const int8_t *codes, const float *scales, ELEM *dx,
+                                                                unsigned long long n, ELEM *y, KtLutPack pack)
+{
+    constexpr unsigned N = kPerLane<ELEM>;
+    const LaneTable tab(pack);
+    const unsigned long long at = ((unsigned long long)blockIdx.x * kBlock + threadIdx.x) * N;
+    const unsigned count = at >= n ? 0u : n - at < N ? (unsigned)(n - at) : N;
+    uint2 c{0u, 0u};
+    uint4 d = uint4{0u, 0u, 0u, 0u};
+    float scale = 0.f;
+    if (count != 0) {
+        c = load_codes<ALIGNED, ELEM>(codes + at, count);
+        scale = scales[at / kGroup];
+        d = load_values<ALIGNED>(dy + at, count);
+    }
+    float x[N];
+    values_of(c.x, scale, reinterpret_cast<float(&)[4]>(x[0]));
+    if constexpr (N == 8) values_of(c.y, scale, reinterpret_cast<float(&)[4]>(x[4]));
+    const uint32_t dw[4] = {d.x, d.y, d.z, d.w};
+    uint32_t gw[4], yw[4];
+#pragma unroll
+    for (unsigned i = 0; i < 4; ++i) {
+        float k[2] = {0.f, 0.f};
+        if constexpr (sizeof(ELEM) == 2) {
+            const uint32_t w = narrow_pair(x[2 * i], x[2 * i + 1]);
+            const Slopes s = slopes_of_word<ELEM, GRAD, WIDE>(w, tab, k);
+            gw[i] = grad_word<ELEM>(dw[i], s);
+            yw[i] = narrow_pair(value_of<GRAD>(widen_lo(w), k[0]), value_of<GRAD>(widen_hi(w), k[1]));
+        } else {
+            const Slopes s = slopes_of_word<ELEM, GRAD, WIDE>(__float_as_uint(x[i]), tab, k);
+            gw[i] = grad_word<ELEM>(dw[i], s);
+            yw[i] = __float_as_uint(value_of<GRAD>(x[i], k[0]));
+        }
+    }
+    if (count != 0) {
+        store_values<ALIGNED, KEEP>(dx + at, uint4{gw[0], gw[1], gw[2], gw[3]}, count);
+        if constexpr (REBUILD) store_values<ALIGNED, KEEP>(y + at, uint4{yw[0], yw[1], yw[2], yw[3]}, count);
+    }
+}
+
+// ------------------------------------------------------------------------------------ host side
+// Bits of the addresses that are below the width of the accesses.
+template <class ELEM>
+bool on_the_grid(const void *a, const void *b, const void *c, const void *codes)
+{
+    const uintptr_t values = reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c);
+    return values % 16 == 0 && reinterpret_cast<uintptr_t>(codes) % kPerLane<ELEM> == 0;
+}
+
+template <class ELEM>
+ktanh_status_t check_call(const void *a, const void *b, const void *c, const void *codes, const void *scales, size_t n, unsigned *tiles)
+{
+    if (a == nullptr || b == nullptr || codes == nullptr || scales == nullptr) return KT_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c)) % sizeof(ELEM) != 0 ||
+        reinterpret_cast<uintptr_t>(scales) % 4 != 0)
+        return KT_ERR_ALIGN;
+    constexpr unsigned long long kTile = kBlock * kPerLane<ELEM>;
+    if (n > kMaxTiles * kTile) return KT_ERR_SHAPE;
+    *tiles = (unsigned)((n + kTile - 1) / kTile);
+    return KT_OK;
+}
+
+template <class ELEM, int OP, class Lut>
+ktanh_status_t launch_keep8(const void *in, void *out, int8_t *codes, float *scales, size_t n, const Lut *lut, ktanh_stream_t stream)
+{
+    constexpr bool WIDE = is_wide(static_cast<const Lut *>(nullptr));
+    if (n == 0) return KT_OK;
+    unsigned tiles;
+    ktanh_status_t st = check_call<ELEM>(in, out, nullptr, codes, scales, n, &tiles);
+    if (st != KT_OK) return st;
+    KtLutPack pack;
+    st = pack_for(lut, sizeof(ELEM) == 4, &pack);
+    if (st != KT_OK) return st;
+    auto launch = [&](auto kernel) {
+        return launch_checked(kernel, tiles, kBlock, stream, static_cast<const ELEM *>(in), static_cast<ELEM *>(out), codes, scales,
+                              (unsigned long long)n, pack);
+    };
+    if (!on_the_grid<ELEM>(in, out, nullptr, codes)) return launch(keep8_kernel<ELEM, OP, WIDE, false, true>);
+    return stays_cached(n * sizeof(ELEM)) ? launch(keep8_kernel<ELEM, OP, WIDE, true, true>) : launch(keep8_kernel<ELEM, OP, WIDE, true, false>);
+}
+
+template <class ELEM, int GRAD, class Lut>
+ktanh_status_t launch_keep8_backward(const void *dy, const int8_t *codes, const float *scales, void *dx, void *y, size_t n, const Lut *lut,
+                                     ktanh_stream_t stream)
+{
+    constexpr bool WIDE = is_wide(static_cast<const Lut *>(nullptr));
+    if (n == 0) return KT_OK;
+    unsigned tiles;
+    ktanh_status_t st = check_call<ELEM>(dy, dx, y, codes, scales, n, &tiles);
+    if (st != KT_OK) return st;
+    KtLutPack pack;
+    st = pack_for(lut, sizeof(ELEM) == 4, &pack);
+    if (st != KT_OK) return st;
+    auto launch = [&](auto kernel) {
+        return launch_checked(kernel, tiles, kBlock, stream, static_cast<const ELEM *>(dy), codes, scales, static_cast<ELEM *>(dx),
+                              (unsigned long long)n, static_cast<ELEM *>(y), pack);
+    };
+    auto with = [&](auto aligned, auto kept) {
+        constexpr bool ALIGNED = decltype(aligned)::value, KEEP = decltype(kept)::value;
+        return y != nullptr ? launch(keep8_backward_kernel<ELEM, GRAD, WIDE, ALIGNED, KEEP, true>)
+                            : launch(keep8_backward_kernel<ELEM, GRAD, WIDE, ALIGNED, KEEP, false>);
+    };
+    if (!on_the_grid<ELEM>(dy, dx, y, codes)) return with(std::false_type(), std::true_type());
+    return stays_cached(n * sizeof(ELEM)) ? with(std::true_type(), std::true_type()) : with(std::true_type(), std::false_type());
+}
+
+}  // namespace
+
+#define KEEP8(name, ELEM, CTYPE, OP, GRAD, LUT)                                                                                  \
+    extern "C" ktanh_status_t name##_keep8(const CTYPE *in, CTYPE *out, int8_t *codes, float *scales, size_t n, const LUT *lut,  \
+                                           ktanh_stream_t stream)                                                                \
+    {                                                                                                                            \
+        return launch_keep8<ELEM, OP>(in, out, codes, scales, n, lut, stream);                                                   \
+    }                                                                                                                            \
+    extern "C" ktanh_status_t name##_keep8_backward(const CTYPE *dy, const int8_t *codes, const float *scales, CTYPE *dx,        \
+                                                    CTYPE *y, size_t n, const LUT *lut, ktanh_stream_t stream)                   \
+    {                                                                                                                            \
+        return launch_keep8_backward<ELEM, GRAD>(dy, codes, scales, dx, y, n, lut, stream);                                      \
+    }
+KEEP8(kswish, uint16_t, uint16_t, OP_SWISH, GRAD_SWISH, ktanh_lut_t)
+KEEP8(kgelu, uint16_t, uint16_t, OP_GELU, GRAD_GELU, ktanh_lut_t)
+KEEP8(kswish_f32, uint32_t, float, OP_SWISH, GRAD_SWISH, ktanh_lut_t)
+KEEP8(kgelu_f32, uint32_t, float, OP_GELU, GRAD_GELU, ktanh_lut_t)
+KEEP8(kswish64, uint16_t, uint16_t, OP_SWISH, GRAD_SWISH, ktanh_lut64_t)
+KEEP8(kgelu64, uint16_t, uint16_t, OP_GELU, GRAD_GELU, ktanh_lut64_t)
+KEEP8(kswish64_f32, uint32_t, float, OP_SWISH, GRAD_SWISH, ktanh_lut64_t)
+KEEP8(kgelu64_f32, uint32_t, float, OP_GELU, GRAD_GELU, ktanh_lut64_t)
