@@ -344,6 +344,55 @@ ktanh_status_t kswish64_f32_keep8_backward(const float *dy, const int8_t *codes,
 ktanh_status_t kgelu64_f32_keep8_backward(const float *dy, const int8_t *codes, const float *scales, float *dx, float *y, size_t n,
                                           const ktanh_lut64_t *lut, ktanh_stream_t stream);
 
+/* ---- Products in 8-bit integers --------------------------------------------------------------------------
+ * For serving: weights in one byte each with a Float32 scale for each output channel, and rows (tokens) that are brought to 8 bits when they
+ * arrive, each with a scale of its own, behind an activation or none.
+ *
+ * kq8_rows: rows of values to integers.  y is x, or kswish(x) / kgelu(x) as those calls round it (kq8_rows64: their 64-interval forms; x
+ * Float32: their Float32 forms).  With m the largest |y| of the row, in Float32 operations rounded to nearest even:
+ *   scale = m / 127,   code = round(y * (127 / m));     m below 2^-120: scale 0 and codes 0
+ * A row with an infinity or a NaN has the scale NaN and codes 0, and so NaN in all its products.  Weights are brought to 8 bits with
+ * the same call, their rows being the output channels.
+ *
+ * kq8_product: out[t][o] = (float(sum over i of codes[t][i] * w[o][i]) * scales[t]) * w_scale[o] + bias[o], the sum exact, the rest Float32,
+ * one rounding per operation, and one more for BFloat16 outputs.
+ *
+ * kq8_linear: kq8_rows and kq8_product in one call, with the same results. */
+enum { KQ8_NONE = 0, KQ8_SWISH = 1, KQ8_GELU = 2 };
+
+typedef struct kq8_shape {
+    size_t rows, inner, outer;     /* x [rows][inner], w [outer][inner], out [rows][outer]; rows and outer up to 2^30 */
+    size_t x_row, w_row, out_row;  /* strides of the rows, in elements; elements of a row are neighbours              */
+    int x_f32, out_f32;            /* Float32, else BFloat16                                                          */
+    int activation;                /* of kq8_rows and kq8_linear                                                      */
+} kq8_shape_t;
+
+/*   x          device, elements of x aligned (KT_ERR_ALIGN; no more is required, multiples of 16 bytes are faster)
+ *   codes      device, out: [rows][inner] bytes with rows codes_row apart
+ *   scales     device, out: Float32 [rows]
+ * shape: rows, inner, x_row, x_f32, activation; the rest is not read. */
+ktanh_status_t kq8_rows(const kq8_shape_t *shape, const void *x, int8_t *codes, size_t codes_row, float *scales, const ktanh_lut_t *lut,
+                        ktanh_stream_t stream);
+ktanh_status_t kq8_rows64(const kq8_shape_t *shape, const void *x, int8_t *codes, size_t codes_row, float *scales, const ktanh_lut64_t *lut,
+                          ktanh_stream_t stream);
+
+/*   codes      device, [rows][inner] with rows x_row apart, any values (-128 too)
+ *   w          device, [outer][inner] with rows w_row apart, any values.  Rows of codes and of weights that start on multiples of 16 bytes
+ *              are faster; bytes between the rows are never used
+ *   scales     device, Float32 [rows]         w_scale, bias   device, Float32 [outer]; bias may be NULL
+ *   out        device, out: [rows][outer] BFloat16 or Float32 with rows out_row apart
+ * inner up to 131071 (KT_ERR_SHAPE).  inner == 0 gives sums of zero; rows == 0 or outer == 0 returns KT_OK without a launch. */
+ktanh_status_t kq8_product(const kq8_shape_t *shape, const int8_t *codes, const float *scales, const int8_t *w, const float *w_scale,
+                           const float *bias, void *out, ktanh_stream_t stream);
+
+/*   workspace  device, 16-byte aligned, kq8_linear_workspace bytes; what it holds before does not matter, and calls that may run at once
+ *              need one each */
+size_t kq8_linear_workspace(const kq8_shape_t *shape);
+ktanh_status_t kq8_linear(const kq8_shape_t *shape, const void *x, const int8_t *w, const float *w_scale, const float *bias, void *out,
+                          void *workspace, const ktanh_lut_t *lut, ktanh_stream_t stream);
+ktanh_status_t kq8_linear64(const kq8_shape_t *shape, const void *x, const int8_t *w, const float *w_scale, const float *bias, void *out,
+                            void *workspace, const ktanh_lut64_t *lut, ktanh_stream_t stream);
+
 /* ---- Attention with capped scores -------------------------------------------------------------------
  * Where a transformer bounds its attention scores with TanH, K-TanH takes its place.  For a query q and a key k
  * that it sees, in Float32:

@@ -27,7 +27,7 @@ INTERVALS = 32
 
 # Every function include/ktanh.h declares, with the kinds of its parameters:
 #   p = device tensor pointer, n = size_t, l = table pointer (32 intervals), L = table pointer (64),
-#   a = kcap_shape_t pointer, g = kcap_pages_t pointer, t = int, s = stream, i = int status.  The ctypes prototypes below are built from these strings and nothing else.
+#   a = kcap_shape_t pointer, g = kcap_pages_t pointer, q = kq8_shape_t pointer, t = int, s = stream, i = int status.  The ctypes prototypes below are built from these strings and nothing else.
 SIGNATURES = {
     "ktanh_status_string": "i", "ktanh_default_lut": "", "ktanh_lut_validate": "l",
     "ktanh_lut64_validate": "L", "ktanh_fit_lut": "l", "ktanh_fit_lut64": "L", "ktanh_fit_lut_bmin0": "l",
@@ -52,6 +52,8 @@ SIGNATURES = {
     "kcap_attention_paged_workspace": "agt",
     "kcap_attention_paged": "agppppppppls", "kcap_attention64_paged": "agppppppppLs",
     "kcap_append": "agpppppppppppnnts",
+    "kq8_rows": "qppnpls", "kq8_rows64": "qppnpLs", "kq8_product": "qpppppps", "kq8_linear_workspace": "q",
+    "kq8_linear": "qppppppls", "kq8_linear64": "qppppppLs",
     "kswish_keep8": "ppppnls", "kswish_keep8_backward": "pppppnls", "kgelu_keep8": "ppppnls", "kgelu_keep8_backward": "pppppnls",
     "kswish_f32_keep8": "ppppnls", "kswish_f32_keep8_backward": "pppppnls", "kgelu_f32_keep8": "ppppnls", "kgelu_f32_keep8_backward": "pppppnls",
     "kswish64_keep8": "ppppnLs", "kswish64_keep8_backward": "pppppnLs", "kgelu64_keep8": "ppppnLs", "kgelu64_keep8_backward": "pppppnLs",
@@ -115,6 +117,13 @@ class KcapPages(ctypes.Structure):
                 ("page_size", "page_count", "most", "table_row", "k_page", "k_slot", "k_head", "v_page", "v_slot", "v_head")]
 
 
+class Kq8Shape(ctypes.Structure):
+    """Mirror of ``kq8_shape_t``."""
+
+    _fields_ = [(name, ctypes.c_size_t) for name in ("rows", "inner", "outer", "x_row", "w_row", "out_row")]
+    _fields_ += [(name, ctypes.c_int) for name in ("x_f32", "out_f32", "activation")]
+
+
 class KtanhError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -157,14 +166,15 @@ def load_library() -> ctypes.CDLL:
         lib = ctypes.CDLL(LIB_PATH)
         kinds = {"p": ctypes.c_void_p, "n": ctypes.c_size_t, "s": ctypes.c_void_p, "i": ctypes.c_int,
                  "l": ctypes.POINTER(KtanhLut), "L": ctypes.POINTER(KtanhLut64),
-                 "a": ctypes.POINTER(KcapShape), "g": ctypes.POINTER(KcapPages), "t": ctypes.c_int}
+                 "a": ctypes.POINTER(KcapShape), "g": ctypes.POINTER(KcapPages), "q": ctypes.POINTER(Kq8Shape), "t": ctypes.c_int}
         for name, params in SIGNATURES.items():
             fn = getattr(lib, name)
             fn.argtypes = [kinds[k] for k in params]
             fn.restype = ctypes.c_int
         lib.ktanh_status_string.restype = ctypes.c_char_p
         lib.ktanh_default_lut.restype = ctypes.POINTER(KtanhLut)
-        lib.kcap_attention_paged_workspace.restype = lib.kcap_attention_backward_workspace.restype = ctypes.c_size_t
+        for name in ("kcap_attention_paged_workspace", "kcap_attention_backward_workspace", "kq8_linear_workspace"):
+            getattr(lib, name).restype = ctypes.c_size_t
         _load_host()
         _lib = lib
     return _lib
@@ -715,6 +725,131 @@ def kgelu64_f32_keep8(x, out=None, codes=None, scales=None, lut=None, stream=Non
 def kgelu64_f32_keep8_backward(dy, codes, scales, rebuild=False, dx=None, y=None, lut=None, stream=None):
     """``kgelu_keep8_backward`` with a 64-interval table (``KtanhLut64``; None = the fitted one) on Float32 tensors."""
     return _keep8_backward("kgelu64_f32_keep8_backward", dy, codes, scales, rebuild, dx, y, lut, stream, (torch.float32,))
+
+
+# -------------------------------------------------------------------------- products in 8-bit integers
+
+_ACTIVATIONS = {None: 0, "swish": 1, "gelu": 2}
+
+
+def _check_matrix(t, dtypes, what):
+    """[rows, columns] with the columns of a row contiguous; any other stride."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor (device memory)")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{what} has dtype {t.dtype}, expected one of {dtypes}")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or t.stride(0) < 0:
+        raise ValueError(f"{what} must be [rows, columns], contiguous in its last dimension")
+
+
+def _check_vector(t, what, count):
+    _check(t, (torch.float32,), what)
+    if tuple(t.shape) != (count,):
+        raise ValueError(f"{what} must be of shape {(count,)}")
+
+
+def _activation_code(activation):
+    if activation not in _ACTIVATIONS:
+        raise ValueError("activation must be None, 'swish' or 'gelu'")
+    return _ACTIVATIONS[activation]
+
+
+_Q8_TYPES = (torch.bfloat16, torch.float32)
+
+
+def kq8_rows(x, activation=None, codes=None, scales=None, lut=None, stream=None, _entry="kq8_rows"):
+    """Rows in 8-bit integers: x [rows, columns] BFloat16 or Float32, any row stride, or ``kswish`` / ``kgelu`` of it, as (codes int8 [rows,
+    columns], scales Float32 [rows]); a code stands for code * scale of its row.  Weights are brought to 8 bits with it as well, their rows
+    being the output channels.  Rows of codes that are allocated here start at multiples of 16 bytes.
+    """
+    _check_matrix(x, _Q8_TYPES, "x")
+    rows, columns = x.shape
+    if codes is None:
+        codes = _empty((rows, -(-columns // 16) * 16), torch.int8, x, stream)[:, :columns]
+    if scales is None:
+        scales = _empty((rows,), torch.float32, x, stream)
+    _check_matrix(codes, (torch.int8,), "codes")
+    _check_vector(scales, "scales", rows)
+    if codes.shape != x.shape:
+        raise ValueError("codes and x differ in shape")
+    if rows > 1 and codes.stride(0) < columns:
+        raise ValueError("rows of codes overlap")
+    _check_here(x, codes, scales)
+    shape = Kq8Shape(rows, columns, 0, _step(x, 0), 0, 0, x.dtype == torch.float32, 0, _activation_code(activation))
+    st = getattr(load_library(), _entry)(shape, x.data_ptr(), codes.data_ptr(), _step(codes, 0), scales.data_ptr(), _lut_arg(lut), _stream_handle(stream))
+    if st != 0:
+        raise KtanhError(st, _entry)
+    return codes, scales
+
+
+def kq8_rows64(x, activation=None, **options):
+    """``kq8_rows`` with a 64-interval table (``KtanhLut64``; None = the fitted one) in the activation."""
+    return kq8_rows(x, activation, **options, _entry="kq8_rows64")
+
+
+def _q8_weights(weight, weight_scales, bias, rows, inner, out, out_dtype, like, stream):
+    """The checked output of a product, and the number of channels."""
+    _check_matrix(weight, (torch.int8,), "weight")
+    outer = weight.shape[0]
+    if weight.shape[1] != inner:
+        raise ValueError("the rows and the weights differ in their inner size")
+    _check_vector(weight_scales, "weight_scales", outer)
+    if bias is not None:
+        _check_vector(bias, "bias", outer)
+    if out is None:
+        if out_dtype not in _Q8_TYPES:
+            raise TypeError(f"out_dtype must be one of {_Q8_TYPES}")
+        return _empty((rows, outer), out_dtype, like, stream), outer
+    _check_matrix(out, _Q8_TYPES, "out")
+    if tuple(out.shape) != (rows, outer):
+        raise ValueError(f"out must be of shape {(rows, outer)}")
+    if rows > 1 and out.stride(0) < outer:
+        raise ValueError("rows of out overlap")
+    return out, outer
+
+
+def _pointer(t):
+    return None if t is None else t.data_ptr()
+
+
+def kq8_product(codes, scales, weight, weight_scales, bias=None, *, out_dtype=torch.bfloat16, out=None, stream=None):
+    """(codes @ weight.T) * scales * weight_scales + bias: codes int8 [rows, inner] with scales Float32 [rows], weight int8 [outer, inner] with
+    scales Float32 [outer], bias Float32 [outer] or None, any row strides; the sums are exact.  Returns out [rows, outer], BFloat16 or
+    Float32 (``out``'s own type where it is given)."""
+    _check_matrix(codes, (torch.int8,), "codes")
+    rows, inner = codes.shape
+    _check_vector(scales, "scales", rows)
+    out, outer = _q8_weights(weight, weight_scales, bias, rows, inner, out, out_dtype, codes, stream)
+    _check_here(codes, scales, weight, weight_scales, bias, out)
+    shape = Kq8Shape(rows, inner, outer, _step(codes, 0), _step(weight, 0), _step(out, 0), 0, out.dtype == torch.float32, 0)
+    st = load_library().kq8_product(shape, codes.data_ptr(), scales.data_ptr(), weight.data_ptr(), weight_scales.data_ptr(), _pointer(bias),
+                                    out.data_ptr(), _stream_handle(stream))
+    if st != 0:
+        raise KtanhError(st, "kq8_product")
+    return out
+
+
+def kq8_linear(x, weight, weight_scales, bias=None, *, activation=None, out_dtype=torch.bfloat16, out=None, lut=None, stream=None,
+               _entry="kq8_linear"):
+    """``kq8_product`` of ``kq8_rows(x, activation)``, in one call: x [rows, inner] BFloat16 or Float32, any row stride."""
+    _check_matrix(x, _Q8_TYPES, "x")
+    rows, inner = x.shape
+    out, outer = _q8_weights(weight, weight_scales, bias, rows, inner, out, out_dtype, x, stream)
+    _check_here(x, weight, weight_scales, bias, out)
+    shape = Kq8Shape(rows, inner, outer, _step(x, 0), _step(weight, 0), _step(out, 0), x.dtype == torch.float32, out.dtype == torch.float32,
+                     _activation_code(activation))
+    lib = load_library()
+    workspace = _empty((lib.kq8_linear_workspace(shape),), torch.uint8, x, stream)
+    st = getattr(lib, _entry)(shape, x.data_ptr(), weight.data_ptr(), weight_scales.data_ptr(), _pointer(bias), out.data_ptr(), _pointer(workspace),
+                              _lut_arg(lut), _stream_handle(stream))
+    if st != 0:
+        raise KtanhError(st, _entry)
+    return out
+
+
+def kq8_linear64(x, weight, weight_scales, bias=None, **options):
+    """``kq8_linear`` with a 64-interval table (``KtanhLut64``; None = the fitted one) in the activation."""
+    return kq8_linear(x, weight, weight_scales, bias, **options, _entry="kq8_linear64")
 
 
 # ------------------------------------------------------------------------- attention with capped scores

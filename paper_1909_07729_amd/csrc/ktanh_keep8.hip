@@ -7,6 +7,7 @@
 // The gradient is that of kswish_backward and kgelu_backward at the values that the codes stand for, operation for operation.  The code -128 stands
 // for an infinity or a NaN, whose gradient is a NaN in those calls too (Swish and GELU multiply it by a slope of zero); it is left out
 // of m, so that its neighbours keep their values.
+#include "ktanh_codes.h"
 #include "ktanh_slopes.h"
 #include "ktanh_stream_impl.h"
 
@@ -17,103 +18,12 @@ using namespace ktanh_device;
 namespace {
 
 constexpr unsigned kGroup = KTANH_KEEP8_GROUP;
-constexpr float kTiny = 0x1p-120f;  // below it 127 / m leaves Float32: such a group is taken as zeros
 
 // A lane has one 128-bit vector of values and as many codes, a wavefront 512 (BFloat16) or 256 (Float32) values, which are whole groups
 // of 16 or 32 lanes: the largest magnitude is found with cross-lane moves, and no group is shared between wavefronts.
-template <class ELEM> constexpr unsigned kPerLane = 16 / sizeof(ELEM);
 template <class ELEM> constexpr unsigned kGroupLanes = kGroup / kPerLane<ELEM>;
 
-template <class ELEM> struct CodeVec { typedef u32x2 type; };
-template <> struct CodeVec<uint32_t> { typedef uint32_t type; };
-
-// ------------------------------------------------------------------------------------ accesses
-// `count` (of kPerLane) elements from p, zeros behind them.  A whole vector comes with one access, also from an address that is only
-// aligned to its elements; only the last lane with values of a launch has fewer.
-template <bool ALIGNED, class ELEM>
-__device__ __forceinline__ uint4 load_values(const ELEM *p, unsigned count)
-{
-    if (count == kPerLane<ELEM>) return load_vec<ALIGNED, false>(reinterpret_cast<const char *>(p));
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-    for (unsigned i = 0; i < kPerLane<ELEM>; ++i)
-        if (i < count) w[i * sizeof(ELEM) / 4] |= (uint32_t)p[i] << (8 * (i * sizeof(ELEM) % 4));
-    return uint4{w[0], w[1], w[2], w[3]};
-}
-
-template <bool ALIGNED, bool KEEP, class ELEM>
-__device__ __forceinline__ void store_values(ELEM *p, uint4 v, unsigned count)
-{
-    if (count == kPerLane<ELEM>) {
-        if constexpr (ALIGNED) store_stream<KEEP>(reinterpret_cast<uint4 *>(p), v);
-        else *reinterpret_cast<u32x4_anywhere *>(p) = u32x4{v.x, v.y, v.z, v.w};
-        return;
-    }
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    for (unsigned i = 0; i < kPerLane<ELEM>; ++i)
-        if (i < count) p[i] = (ELEM)(w[i * sizeof(ELEM) / 4] >> (8 * (i * sizeof(ELEM) % 4)));
-}
-
-typedef u32x2 u32x2_anywhere __attribute__((aligned(1)));
-typedef uint32_t u32_anywhere __attribute__((aligned(1)));
-
-// Codes, one byte each: two words a lane (BFloat16) or one.
-template <bool ALIGNED, class ELEM>
-__device__ __forceinline__ uint2 load_codes(const int8_t *p, unsigned count)
-{
-    if (count == kPerLane<ELEM>) {
-        if constexpr (sizeof(ELEM) == 2) {
-            u32x2 t;
-            if constexpr (ALIGNED) t = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p));
-            else t = *reinterpret_cast<const u32x2_anywhere *>(p);
-            return uint2{t.x, t.y};
-        } else {
-            if constexpr (ALIGNED) return uint2{__builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(p)), 0u};
-            else return uint2{*reinterpret_cast<const u32_anywhere *>(p), 0u};
-        }
-    }
-    uint32_t w[2] = {0u, 0u};
-    for (unsigned i = 0; i < kPerLane<ELEM>; ++i)
-        if (i < count) w[i / 4] |= (uint32_t)(uint8_t)p[i] << (8 * (i % 4));
-    return uint2{w[0], w[1]};
-}
-
-template <bool ALIGNED, class ELEM>
-__device__ __forceinline__ void store_codes(int8_t *p, uint2 c, unsigned count)
-{
-    if (count == kPerLane<ELEM>) {
-        if constexpr (sizeof(ELEM) == 2) {
-            if constexpr (ALIGNED) __builtin_nontemporal_store(u32x2{c.x, c.y}, reinterpret_cast<u32x2 *>(p));
-            else *reinterpret_cast<u32x2_anywhere *>(p) = u32x2{c.x, c.y};
-        } else {
-            if constexpr (ALIGNED) __builtin_nontemporal_store(c.x, reinterpret_cast<uint32_t *>(p));
-            else *reinterpret_cast<u32_anywhere *>(p) = c.x;
-        }
-        return;
-    }
-    const uint32_t w[2] = {c.x, c.y};
-    for (unsigned i = 0; i < kPerLane<ELEM>; ++i)
-        if (i < count) p[i] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
-}
-
 // ------------------------------------------------------------------------------------ codes
-// The vector's values in Float32.
-template <class ELEM>
-__device__ __forceinline__ void widen(uint4 v, float (&x)[kPerLane<ELEM>])
-{
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (unsigned i = 0; i < 4; ++i) {
-        if constexpr (sizeof(ELEM) == 2) {
-            x[2 * i] = widen_lo(w[i]);
-            x[2 * i + 1] = widen_hi(w[i]);
-        } else {
-            x[i] = __uint_as_float(w[i]);
-        }
-    }
-}
-
-__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
-
 // The largest of a group's lanes, in all of them: four moves within a row of 16 lanes, and one to the other row for groups of 32.
 template <unsigned LANES>
 __device__ __forceinline__ uint32_t largest_of_group(uint32_t m)
@@ -124,23 +34,6 @@ __device__ __forceinline__ uint32_t largest_of_group(uint32_t m)
     m = larger(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x121, 0xF, 0xF, false));
     if constexpr (LANES == 32) m = larger(m, (uint32_t)__builtin_amdgcn_ds_swizzle((int)m, 0x401F));  // lane ^ 16
     return m;
-}
-
-// The bits of the largest finite magnitude of a lane's values, as a Float32.  Magnitudes order like their bits.
-template <class ELEM>
-__device__ __forceinline__ uint32_t largest_of_lane(uint4 v, bool &odd)
-{
-    if constexpr (sizeof(ELEM) == 2) {
-        const uint32_t a = v.x & kMag2, b = v.y & kMag2, c = v.z & kMag2, d = v.w & kMag2;
-        const uint32_t m2 = max_pair(max_pair(a, b), max_pair(c, d));
-        const uint32_t m = larger(m2 & 0xFFFFu, m2 >> 16);
-        odd = m >= 0x7F80u;
-        return m << 16;
-    } else {
-        const uint32_t m = larger(larger(v.x & 0x7FFFFFFFu, v.y & 0x7FFFFFFFu), larger(v.z & 0x7FFFFFFFu, v.w & 0x7FFFFFFFu));
-        odd = m >= 0x7F800000u;
-        return m;
-    }
 }
 
 // The codes of a lane's vector, and its group's scale.
@@ -162,23 +55,18 @@ __device__ __forceinline__ uint2 codes_of(uint4 v, float &scale)
         }
     }
     const float top = __uint_as_float(largest_of_group<kGroupLanes<ELEM>>(m));
-    const float inverse = top < kTiny ? 0.f : 127.0f / top;
-    scale = top < kTiny ? 0.f : top / 127.0f;
-    // x * inverse is at most 127 (1 + 2^-23); 1.5 * 2^23 added to it rounds it to an integer, to nearest even, whose two's complement
-    // is in the sum's low bits
+    const float inverse = inverse_of(top);
+    scale = scale_of(top);
     uint32_t q[N];
 #pragma unroll
-    for (unsigned i = 0; i < N; ++i) q[i] = __float_as_uint(x[i] * inverse + 12582912.0f);
+    for (unsigned i = 0; i < N; ++i) q[i] = rounded_code(x[i], inverse);
     if (any_odd) {
 #pragma unroll
         for (unsigned i = 0; i < N; ++i)
             if ((__float_as_uint(x[i]) & 0x7FFFFFFFu) >= 0x7F800000u) q[i] = 0x80u;
     }
-    auto four = [](uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-        return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u), 0x05040100u);
-    };
-    uint2 out{four(q[0], q[1], q[2], q[3]), 0u};
-    if constexpr (N == 8) out.y = four(q[4], q[5], q[6], q[7]);
+    uint2 out{four_codes(q[0], q[1], q[2], q[3]), 0u};
+    if constexpr (N == 8) out.y = four_codes(q[4], q[5], q[6], q[7]);
     return out;
 }
 
