@@ -518,6 +518,40 @@ ktanh_status_t kcap_append(const kcap_shape_t *shape, const kcap_pages_t *cache,
                            const int32_t *lengths, const int32_t *q_offsets, const float *cos, const float *sin,
                            size_t positions, size_t angles, int interleaved, ktanh_stream_t stream);
 
+/* ---- The next token -----------------------------------------------------------------------------------------
+ * One token of each row of logits, from a uniform number that the caller gives.  z are the logits in Float32, with cap > 0
+ * z = cap * Kf(z / cap) (Float32, one rounding per operation, Kf being ktanh_f32); -infinity stays -infinity, which masks a token.  Tokens are
+ * ranked by z, the lowest index first among equal ones, with weights w = exp((z - max z) / temperature), G(r) being the sum of the first r:
+ *   top_k  keeps the first top_k tokens (0, or more than there are: all)
+ *   top_p  of these the fewest first ones with G(r) >= top_p * G(top_k), one at least
+ *   min_p  of these those with w >= min_p
+ * and of the n that are left the token is the first with G(r) > uniform * G(n).  A temperature of 0 or below takes the first token by rank.
+ * Weights and their sums are held in 64 bits, in an order that does not change from call to call; tokens with a weight below e^-51 of the
+ * first's do not count.
+ * A row with a NaN, or with nothing but masked tokens, has the token -1.  With a logit of +infinity only such tokens have a weight. */
+#define KSAMPLE_MOST 1048575
+
+typedef struct ksample_shape {
+    size_t rows, vocabulary;       /* logits [rows][vocabulary], 1 to KSAMPLE_MOST tokens, up to 2^30 rows  */
+    size_t row;                    /* stride of the rows, in elements                                       */
+    int f32;                       /* Float32, else BFloat16                                                */
+    double cap;                    /* 0: none                                                               */
+    double temperature;            /* settings of all rows, Float32 numbers, where the pointer of the rows' */
+    double top_p, min_p;           /*   own is NULL; temperature 0 to 3e38, top_p and min_p 0 to 1          */
+    size_t top_k;
+} ksample_shape_t;
+
+/*   logits     device, elements aligned (KT_ERR_ALIGN)
+ *   uniform    device, Float32 [rows], in [0, 1); values outside, here and in the rows' own settings, are taken as the nearest inside
+ *              (1: the last of the kept tokens), and NaNs as 0 (top_p: 1)
+ *   temperature, top_p, min_p   device, Float32 [rows], or NULL         top_k   device, int32 [rows], or NULL
+ *   tokens     device, out: int64 [rows]
+ * KT_ERR_SHAPE: sizes or settings out of range, a cap below 1e-30.  `lut` is read where cap > 0. */
+ktanh_status_t ksample(const ksample_shape_t *shape, const void *logits, const float *uniform, const float *temperature, const int32_t *top_k,
+                       const float *top_p, const float *min_p, int64_t *tokens, const ktanh_lut_t *lut, ktanh_stream_t stream);
+ktanh_status_t ksample64(const ksample_shape_t *shape, const void *logits, const float *uniform, const float *temperature, const int32_t *top_k,
+                         const float *top_p, const float *min_p, int64_t *tokens, const ktanh_lut64_t *lut, ktanh_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

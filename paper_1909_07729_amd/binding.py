@@ -27,7 +27,7 @@ INTERVALS = 32
 
 # Every function include/ktanh.h declares, with the kinds of its parameters:
 #   p = device tensor pointer, n = size_t, l = table pointer (32 intervals), L = table pointer (64),
-#   a = kcap_shape_t pointer, g = kcap_pages_t pointer, q = kq8_shape_t pointer, t = int, s = stream, i = int status.  The ctypes prototypes below are built from these strings and nothing else.
+#   a = kcap_shape_t pointer, g = kcap_pages_t pointer, q = kq8_shape_t pointer, m = ksample_shape_t pointer, t = int, s = stream, i = int status.  The ctypes prototypes below are built from these strings and nothing else.
 SIGNATURES = {
     "ktanh_status_string": "i", "ktanh_default_lut": "", "ktanh_lut_validate": "l",
     "ktanh_lut64_validate": "L", "ktanh_fit_lut": "l", "ktanh_fit_lut64": "L", "ktanh_fit_lut_bmin0": "l",
@@ -54,6 +54,7 @@ SIGNATURES = {
     "kcap_append": "agpppppppppppnnts",
     "kq8_rows": "qppnpls", "kq8_rows64": "qppnpLs", "kq8_product": "qpppppps", "kq8_linear_workspace": "q",
     "kq8_linear": "qppppppls", "kq8_linear64": "qppppppLs",
+    "ksample": "mpppppppls", "ksample64": "mpppppppLs",
     "kswish_keep8": "ppppnls", "kswish_keep8_backward": "pppppnls", "kgelu_keep8": "ppppnls", "kgelu_keep8_backward": "pppppnls",
     "kswish_f32_keep8": "ppppnls", "kswish_f32_keep8_backward": "pppppnls", "kgelu_f32_keep8": "ppppnls", "kgelu_f32_keep8_backward": "pppppnls",
     "kswish64_keep8": "ppppnLs", "kswish64_keep8_backward": "pppppnLs", "kgelu64_keep8": "ppppnLs", "kgelu64_keep8_backward": "pppppnLs",
@@ -124,6 +125,13 @@ class Kq8Shape(ctypes.Structure):
     _fields_ += [(name, ctypes.c_int) for name in ("x_f32", "out_f32", "activation")]
 
 
+class KsampleShape(ctypes.Structure):
+    """Mirror of ``ksample_shape_t``."""
+
+    _fields_ = [("rows", ctypes.c_size_t), ("vocabulary", ctypes.c_size_t), ("row", ctypes.c_size_t), ("f32", ctypes.c_int)]
+    _fields_ += [(name, ctypes.c_double) for name in ("cap", "temperature", "top_p", "min_p")] + [("top_k", ctypes.c_size_t)]
+
+
 class KtanhError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -166,7 +174,7 @@ def load_library() -> ctypes.CDLL:
         lib = ctypes.CDLL(LIB_PATH)
         kinds = {"p": ctypes.c_void_p, "n": ctypes.c_size_t, "s": ctypes.c_void_p, "i": ctypes.c_int,
                  "l": ctypes.POINTER(KtanhLut), "L": ctypes.POINTER(KtanhLut64),
-                 "a": ctypes.POINTER(KcapShape), "g": ctypes.POINTER(KcapPages), "q": ctypes.POINTER(Kq8Shape), "t": ctypes.c_int}
+                 "a": ctypes.POINTER(KcapShape), "g": ctypes.POINTER(KcapPages), "q": ctypes.POINTER(Kq8Shape), "m": ctypes.POINTER(KsampleShape), "t": ctypes.c_int}
         for name, params in SIGNATURES.items():
             fn = getattr(lib, name)
             fn.argtypes = [kinds[k] for k in params]
@@ -850,6 +858,51 @@ def kq8_linear(x, weight, weight_scales, bias=None, *, activation=None, out_dtyp
 def kq8_linear64(x, weight, weight_scales, bias=None, **options):
     """``kq8_linear`` with a 64-interval table (``KtanhLut64``; None = the fitted one) in the activation."""
     return kq8_linear(x, weight, weight_scales, bias, **options, _entry="kq8_linear64")
+
+
+# ---------------------------------------------------------------------------------------- the next token
+
+
+def _setting(value, what, rows, dtype):
+    """A setting of all rows as a number, or one of each row as a tensor: (number, tensor or None)."""
+    if not torch.is_tensor(value):
+        return value, None
+    _check(value, (dtype,), what)
+    if tuple(value.shape) != (rows,):
+        raise ValueError(f"{what} must be a number or of shape {(rows,)}")
+    return 0, value
+
+
+def ksample(logits, uniform, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, cap=0.0, out=None, lut=None, stream=None, _entry="ksample"):
+    """One token of each row: logits [rows, vocabulary] BFloat16 or Float32, any row stride; uniform Float32 [rows] in [0, 1).
+
+    Tokens are ranked by logit, the lowest index first among equals.  ``top_k`` keeps the first (0: all), ``top_p`` of these the fewest whose weight
+    is that share, ``min_p`` those whose weight is at least that share of the first's; the token is the first whose weight and its
+    predecessors' exceed ``uniform`` of all that are kept.  A temperature of 0 takes the first.  Settings are numbers, or tensors [rows] (Float32;
+    int32 for top_k).  ``cap`` > 0 caps the logits through K-TanH before all else, cap * K(z / cap); -infinity masks a token.
+    Returns int64 [rows]; -1 for a row with a NaN or without a token that is not masked.
+    """
+    _check_matrix(logits, _Q8_TYPES, "logits")
+    rows, vocabulary = logits.shape
+    _check_vector(uniform, "uniform", rows)
+    (temperature, temperatures), (top_k, top_ks), (top_p, top_ps), (min_p, min_ps) = (
+        _setting(v, what, rows, dtype) for v, what, dtype in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
+                                                             (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)))
+    if top_k < 0:
+        raise ValueError("top_k must not be negative")
+    out = _empty((rows,), torch.int64, logits, stream) if out is None else _dense_out(out, "out", (rows,), (torch.int64,))
+    _check_here(logits, uniform, temperatures, top_ks, top_ps, min_ps, out)
+    shape = KsampleShape(rows, vocabulary, _step(logits, 0), logits.dtype == torch.float32, cap, temperature, top_p, min_p, top_k)
+    st = getattr(load_library(), _entry)(shape, logits.data_ptr(), uniform.data_ptr(), *map(_pointer, (temperatures, top_ks, top_ps, min_ps)), out.data_ptr(),
+                                         _lut_arg(lut), _stream_handle(stream))
+    if st != 0:
+        raise KtanhError(st, _entry)
+    return out
+
+
+def ksample64(logits, uniform, **options):
+    """``ksample`` with a 64-interval table (``KtanhLut64``; None = the fitted one) in the cap."""
+    return ksample(logits, uniform, **options, _entry="ksample64")
 
 
 # ------------------------------------------------------------------------- attention with capped scores
