@@ -16,7 +16,6 @@ namespace {
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef i32x4 i32x4_anywhere __attribute__((aligned(1)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 
 struct Operands {
     const int8_t *x, *w;
@@ -45,42 +44,265 @@ __device__ __forceinline__ i32x4 load16(const int8_t *p, int count)
     return v;
 }
 
-// The result at (t, o .. o + 3), as far as it is inside.
-template <bool F32, bool WHOLE>
-__device__ __forceinline__ void store_scaled(const Operands &a, unsigned t, unsigned o, const int (&sum)[4])
+// Results leave by rows, 16 bytes of a lane's at once, to any address of an element's alignment.
+template <bool F32> struct Result;
+template <> struct Result<false> {
+    typedef uint16_t type;
+    typedef u32x4 anywhere __attribute__((aligned(2)));
+    static constexpr unsigned kEach = 8;    // of a 16-byte chunk
+};
+template <> struct Result<true> {
+    typedef float type;
+    typedef u32x4 anywhere __attribute__((aligned(4)));
+    static constexpr unsigned kEach = 4;
+};
+
+template <bool F32>
+__device__ __forceinline__ void store_chunk(const Operands &a, unsigned t, unsigned o, u32x4 v)
 {
+    typedef typename Result<F32>::type T;
     if (t >= a.rows || o >= a.outer) return;
-    const float row = a.x_scale[t];
-    float y[4];
+    T *to = static_cast<T *>(a.out) + t * a.out_row + o;
+    if (o + Result<F32>::kEach <= a.outer) {
+        *reinterpret_cast<typename Result<F32>::anywhere *>(to) = v;
+        return;
+    }
+    const T *from = reinterpret_cast<const T *>(&v);
+    for (unsigned i = 0; i < Result<F32>::kEach - 1; ++i)
+        if (o + i < a.outer) to[i] = from[i];
+}
+
+// Scales, or biases, of channels o .. o + 3; past the last channel the last one's.
+__device__ __forceinline__ f32x4 four_of(const float *p, unsigned o, unsigned outer)
+{
+    typedef f32x4 anywhere __attribute__((aligned(4)));
+    if (o + 4 <= outer) return *reinterpret_cast<const anywhere *>(p + o);
+    auto at = [&](unsigned i) { return p[i < outer ? i : outer - 1]; };
+    return f32x4{at(o), at(o + 1), at(o + 2), at(o + 3)};
+}
+
+__device__ __forceinline__ f32x4 scaled(i32x4 sum, float row, f32x4 channel, f32x4 bias, bool biased)
+{
+    f32x4 y;
 #pragma unroll
     for (unsigned i = 0; i < 4; ++i) {
-        const unsigned at = WHOLE || o + i < a.outer ? o + i : o;
-        y[i] = ((float)sum[i] * row) * a.w_scale[at];
-        if (a.bias != nullptr) y[i] = y[i] + a.bias[at];
+        y[i] = ((float)sum[i] * row) * channel[i];
+        if (biased) y[i] = y[i] + bias[i];
     }
-    const unsigned long long at = t * a.out_row + o;
-    if constexpr (F32) {
-        float *to = static_cast<float *>(a.out) + at;
-        if constexpr (WHOLE) *reinterpret_cast<f32x4 *>(to) = f32x4{y[0], y[1], y[2], y[3]};
-        else
-            for (unsigned i = 0; i < 4; ++i)
-                if (o + i < a.outer) to[i] = y[i];
-    } else {
-        uint16_t *to = static_cast<uint16_t *>(a.out) + at;
-        const uint32_t lo = narrow_pair(y[0], y[1]), hi = narrow_pair(y[2], y[3]);
-        if constexpr (WHOLE) *reinterpret_cast<u32x2 *>(to) = u32x2{lo, hi};
-        else {
-            const uint32_t w[2] = {lo, hi};
-            for (unsigned i = 0; i < 4; ++i)
-                if (o + i < a.outer) to[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
+    return y;
+}
+
+// Four neighbouring results into LDS.
+template <bool F32>
+__device__ __forceinline__ void put_four(char *to, f32x4 y)
+{
+    if constexpr (F32) *reinterpret_cast<f32x4 *>(to) = y;
+    else *reinterpret_cast<u32x2 *>(to) = u32x2{narrow_pair(y[0], y[1]), narrow_pair(y[2], y[3])};
+}
+
+// ------------------------------------------------------------------------------------ tiles
+// Products of many rows.  A block of four wavefronts has TO output channels and TT rows, each wavefront a quarter of it (two by two).  Tiles of 128
+// integers of the inner dimension come into LDS by direct loads, in two places; operands are read a step of 32 integers ahead of the products
+// that take them, and the next tile but one is asked for between the last products of a tile, when its place has been read.
+//
+// Rows of a tile are 128 bytes, half of the width of LDS.  Chunks of 16 bytes change places with bits 1 to 3 of their row's number, so that sixteen
+// neighbouring rows at one chunk, which are read at once, lie in different banks.
+typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
+constexpr unsigned kDeep = 128;     // integers of a tile
+
+__device__ __forceinline__ void load_direct(const int8_t *from, char *to)
+{
+    typedef const __attribute__((address_space(1))) void *global;
+    typedef __attribute__((address_space(3))) void *local;
+    __builtin_amdgcn_global_load_lds((global)from, (local)to, 16, 0, 0);
+}
+
+// R rows of an operand, of which `there` are inside (the rest is read as the last), brought to LDS by the block.
+template <unsigned R>
+struct Side {
+    const int8_t *base;         // the tile's first row
+    unsigned offset[R / 32];    // of this lane's chunks
+    static constexpr unsigned kLoads = R / 32;
+
+    // The chunk that a lane brings to place lane % 8 of row 8 i + lane / 8.
+    __device__ __forceinline__ static unsigned chunk_of(unsigned i) { return threadIdx.x % 8 ^ (4 * i + threadIdx.x % 64 / 16) % 8; }
+
+    __device__ __forceinline__ Side(const int8_t *rows, unsigned long long row, unsigned first, unsigned last)
+    {
+        const unsigned lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        base = rows + first * row;
+#pragma unroll
+        for (unsigned i = 0; i < kLoads; ++i) {
+            const unsigned at = wave * (R / 4) + i * 8 + lane / 8, most = last - first;
+            offset[i] = (at < most ? at : most) * (unsigned)row + chunk_of(i) * 16;
         }
+    }
+    __device__ __forceinline__ void load(unsigned i, unsigned k, char *tile) const
+    {
+        load_direct(base + k + offset[i], tile + (__builtin_amdgcn_readfirstlane(threadIdx.x / 64) * (R / 4) + i * 8) * kDeep);
+    }
+    // The end of the rows, fewer than kDeep integers, zeros behind them.
+    __device__ __forceinline__ void load_end(unsigned k, unsigned inner, char *tile) const
+    {
+        const unsigned lane = threadIdx.x % 64;
+#pragma unroll
+        for (unsigned i = 0; i < kLoads; ++i)
+            *reinterpret_cast<i32x4 *>(tile + (threadIdx.x / 64 * (R / 4) + i * 8) * kDeep + lane * 16) =
+                load16<true>(base + k + offset[i], (int)(inner - k) - (int)(chunk_of(i) * 16));
+    }
+};
+
+// Which tile a block takes.  Blocks go to the eight XCDs in turn, each with an L2 of its own: each XCD gets a run of tiles, and a run goes through four tiles
+// of rows at a time, so that the blocks that an XCD works on at once share rows and channels.
+struct Corner {
+    unsigned over, across;
+};
+__device__ __forceinline__ Corner corner_of(unsigned block, unsigned over, unsigned across)
+{
+    constexpr unsigned kRows = 4;
+    const unsigned each = over * across / 8, id = block < 8 * each ? block % 8 * each + block / 8 : block;
+    const unsigned group = id / (kRows * over), in = id % (kRows * over), rows = across - group * kRows < kRows ? across - group * kRows : kRows;
+    return Corner{in / rows, group * kRows + in % rows};
+}
+
+template <unsigned TO, unsigned TT, bool F32>
+__global__ __launch_bounds__(256, TO * TT > 128 * 128 ? 1 : 2) void q8_tile_kernel(Operands a, unsigned over, unsigned across)
+{
+    constexpr unsigned OI = TO / 64, TI = TT / 64, kPlace = (TO + TT) * kDeep;
+    __shared__ __align__(16) char lds[2 * kPlace];
+    const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const Corner at = corner_of(blockIdx.x, over, across);
+    const unsigned o0 = at.over * TO, t0 = at.across * TT;
+    const Side<TO> w(a.w, a.w_row, o0, a.outer - 1);
+    const Side<TT> x(a.x, a.x_row, t0, a.rows - 1);
+    constexpr unsigned kLoads = w.kLoads + x.kLoads;
+    auto load = [&](unsigned n, unsigned k, char *place) {
+        if (n < w.kLoads) w.load(n, k, place);
+        else x.load(n - w.kLoads, k, place + TO * kDeep);
+    };
+    i32x16 sum[OI][TI];
+#pragma unroll
+    for (unsigned i = 0; i < OI; ++i)
+#pragma unroll
+        for (unsigned j = 0; j < TI; ++j) sum[i][j] = i32x16{0};
+    // operands of 32 integers: a lane has 16 of one row
+    const unsigned w_at = (wave / 2 * (TO / 2) + lane % 32) * kDeep, x_at = TO * kDeep + (wave % 2 * (TT / 2) + lane % 32) * kDeep;
+    i32x4 wf[2][OI], xf[2][TI];
+    auto read = [&](const char *place, unsigned step) {
+        const unsigned chunk = ((2 * step + lane / 32) ^ lane / 2 % 8) * 16;
+#pragma unroll
+        for (unsigned i = 0; i < OI; ++i) wf[step % 2][i] = *reinterpret_cast<const i32x4 *>(place + w_at + chunk + i * 32 * kDeep);
+#pragma unroll
+        for (unsigned j = 0; j < TI; ++j) xf[step % 2][j] = *reinterpret_cast<const i32x4 *>(place + x_at + chunk + j * 32 * kDeep);
+    };
+    auto multiply = [&](unsigned step, auto between) {
+#pragma unroll
+        for (unsigned i = 0; i < OI; ++i)
+#pragma unroll
+            for (unsigned j = 0; j < TI; ++j) {
+                sum[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[step % 2][i], xf[step % 2][j], sum[i][j], 0, 0, 0);
+                between(i * TI + j);
+            }
+    };
+    auto nothing = [](unsigned) {};
+    const unsigned tiles = a.inner / kDeep;
+    // Without a branch: past the last tiles the last one is asked for again, into a place that nobody reads, and what is read ahead is not used.
+    auto step = [&](unsigned tile, char *__restrict__ here, const char *__restrict__ next) {
+#pragma unroll
+        for (unsigned s = 0; s < 3; ++s) {
+            read(here, s + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(s, nothing);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // the next tile is complete, and this one has been read by all
+        __builtin_amdgcn_s_waitcnt(0x0070);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        read(next, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        const unsigned k = (tile + 2 < tiles ? tile + 2 : tiles - 1) * kDeep;
+        multiply(3, [&](unsigned n) {
+            constexpr unsigned kEach = (kLoads + OI * TI - 1) / (OI * TI);
+#pragma unroll
+            for (unsigned e = 0; e < kEach; ++e)
+                if (n * kEach + e < kLoads) load(n * kEach + e, k, here);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    if (tiles != 0) {
+        char *here = lds, *next = lds + kPlace;
+#pragma unroll
+        for (unsigned n = 0; n < kLoads; ++n) load(n, 0, here);
+        const unsigned k = tiles > 1 ? kDeep : 0;
+#pragma unroll
+        for (unsigned n = 0; n < kLoads; ++n) load(n, k, next);
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+        __syncthreads();
+        read(here, 0);
+        for (unsigned tile = 0; tile < tiles; ++tile) {
+            step(tile, here, next);
+            char *const other = here;
+            here = next;
+            next = other;
+        }
+        __builtin_amdgcn_s_waitcnt(0x0070);
+    }
+    char *const first = lds;
+    if (a.inner % kDeep != 0) {
+        __syncthreads();
+        w.load_end(tiles * kDeep, a.inner, first);
+        x.load_end(tiles * kDeep, a.inner, first + TO * kDeep);
+        __syncthreads();
+#pragma unroll
+        for (unsigned s = 0; s < 4; ++s) {
+            read(first, s);
+            multiply(s, nothing);
+        }
+    }
+    // A lane has, of 32 channels and 32 rows, four times 4 neighbouring channels of one row.  The results of 32 rows go through a wavefront's own
+    // place in LDS, and leave by whole rows of its channels: straight from the registers each store would touch 32 rows, 16 bytes of each.
+    __syncthreads();
+    constexpr unsigned kSize = F32 ? 4 : 2, kRow = TO / 2 * kSize, kPitch = kRow + 16, kChunks = kRow / 16;
+    static_assert(4 * 32 * kPitch <= sizeof(lds), "four wavefronts' results");
+    char *const mine = lds + wave * 32 * kPitch;
+    const unsigned o1 = o0 + wave / 2 * (TO / 2), t1 = t0 + wave % 2 * (TT / 2);
+    const bool biased = a.bias != nullptr;
+    f32x4 channel[OI][4], bias[OI][4];
+#pragma unroll
+    for (unsigned i = 0; i < OI; ++i)
+#pragma unroll
+        for (unsigned q = 0; q < 4; ++q) {
+            const unsigned o = o1 + i * 32 + q * 8 + lane / 32 * 4;
+            channel[i][q] = four_of(a.w_scale, o, a.outer);
+            bias[i][q] = biased ? four_of(a.bias, o, a.outer) : f32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+    for (unsigned j = 0; j < TI; ++j) {
+        const unsigned t = t1 + j * 32 + lane % 32;
+        const float row = a.x_scale[t < a.rows ? t : a.rows - 1];
+#pragma unroll
+        for (unsigned i = 0; i < OI; ++i)
+#pragma unroll
+            for (unsigned q = 0; q < 4; ++q) {
+                const i32x4 four = {sum[i][j][4 * q], sum[i][j][4 * q + 1], sum[i][j][4 * q + 2], sum[i][j][4 * q + 3]};
+                put_four<F32>(mine + lane % 32 * kPitch + (i * 32 + q * 8 + lane / 32 * 4) * kSize, scaled(four, row, channel[i][q], bias[i][q], biased));
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+#pragma unroll
+        for (unsigned n = 0; n < 32 * kChunks / 64; ++n) {
+            const unsigned at = (n * 64 + lane) / kChunks, chunk = (n * 64 + lane) % kChunks;
+            store_chunk<F32>(a, t1 + j * 32 + at, o1 + chunk * Result<F32>::kEach, *reinterpret_cast<const u32x4 *>(mine + at * kPitch + chunk * 16));
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
     }
 }
 
+// ------------------------------------------------------------------------------------ a shared inner dimension
 // A block has OT output channels and TT rows, and its W wavefronts share the inner dimension in steps of 64 integers: wavefront s takes the steps
 // s, s + W, ..., so that the block reads whole cache lines.  Operands go from memory to the matrix cores' registers; the wavefronts' sums
 // meet in LDS.
-template <unsigned OT, unsigned TT, unsigned W, bool F32, bool ALIGNED, bool WHOLE>
+template <unsigned OT, unsigned TT, unsigned W, bool F32, bool ALIGNED>
 __global__ __launch_bounds__(64 * W) void q8_shared_inner_kernel(Operands a)
 {
     constexpr unsigned OI = OT / 16, TI = TT / 16;
@@ -142,13 +364,23 @@ __global__ __launch_bounds__(64 * W) void q8_shared_inner_kernel(Operands a)
         for (unsigned j = 0; j < TI; ++j)
             *reinterpret_cast<i32x4 *>(&part[wave][16 * j + lane % 16][16 * i + lane / 16 * 4]) = sum[i][j];
     __syncthreads();
-    for (unsigned e = threadIdx.x; e < TT * OT / 4; e += 64 * W) {
-        const unsigned t = e / (OT / 4), o = e % (OT / 4) * 4;
-        i32x4 v = *reinterpret_cast<const i32x4 *>(&part[0][t][o]);
+    constexpr unsigned E = Result<F32>::kEach;
+    for (unsigned e = threadIdx.x; e < TT * OT / E; e += 64 * W) {
+        const unsigned t = e / (OT / E), o = e % (OT / E) * E;
+        if (t0 + t >= a.rows || o0 + o >= a.outer) continue;
+        const float row = a.x_scale[t0 + t];
+        u32x4 out;
 #pragma unroll
-        for (unsigned i = 1; i < W; ++i) v += *reinterpret_cast<const i32x4 *>(&part[i][t][o]);
-        const int four[4] = {v.x, v.y, v.z, v.w};
-        store_scaled<F32, WHOLE>(a, t0 + t, o0 + o, four);
+        for (unsigned h = 0; h < E / 4; ++h) {
+            i32x4 v = *reinterpret_cast<const i32x4 *>(&part[0][t][o + 4 * h]);
+#pragma unroll
+            for (unsigned i = 1; i < W; ++i) v += *reinterpret_cast<const i32x4 *>(&part[i][t][o + 4 * h]);
+            const unsigned c = o0 + o + 4 * h;
+            const bool biased = a.bias != nullptr;
+            const f32x4 y = scaled(v, row, four_of(a.w_scale, c, a.outer), biased ? four_of(a.bias, c, a.outer) : f32x4{0, 0, 0, 0}, biased);
+            put_four<F32>(reinterpret_cast<char *>(&out) + 8 * h, y);
+        }
+        store_chunk<F32>(a, t0 + t, o0 + o, out);
     }
 }
 
@@ -174,8 +406,6 @@ ktanh_status_t launch_product(const kq8_shape_t &s, const int8_t *x, size_t x_ro
     a.outer = (unsigned)s.outer;
     a.inner = (unsigned)s.inner;
     const bool aligned = !off(x, 16) && a.x_row % 16 == 0 && !off(w, 16) && a.w_row % 16 == 0;
-    // four neighbouring results are stored at once
-    const bool whole = s.outer % 4 == 0 && a.out_row % 4 == 0 && !off(out, s.out_f32 ? 16 : 8);
     auto launch = [&](auto kernel, unsigned threads, unsigned ot, unsigned tt) {
         const size_t over = (s.outer + ot - 1) / ot, across = (s.rows + tt - 1) / tt;
         if (over * threads >= (1ull << 32) || across > 65535) return KT_ERR_SHAPE;
@@ -183,14 +413,20 @@ ktanh_status_t launch_product(const kq8_shape_t &s, const int8_t *x, size_t x_ro
         return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)over, (unsigned)across), dim3(threads), args, 0,
                                static_cast<hipStream_t>(stream)) == hipSuccess ? KT_OK : KT_ERR_HIP;
     };
-    auto sized = [&](auto f32, auto on_grid, auto fours) {
-        constexpr bool F = decltype(f32)::value, A = decltype(on_grid)::value, H = decltype(fours)::value;
-        if (s.rows <= 16) return launch(q8_shared_inner_kernel<16, 16, 8, F, A, H>, 512, 16, 16);
-        if (s.rows <= 32) return launch(q8_shared_inner_kernel<32, 32, 4, F, A, H>, 256, 32, 32);
-        return launch(q8_shared_inner_kernel<64, 64, 4, F, A, H>, 256, 64, 64);
+    auto sized = [&](auto f32, auto on_grid) {
+        constexpr bool F = decltype(f32)::value, A = decltype(on_grid)::value;
+        if constexpr (A) {
+            // a tile's offsets are 32-bit
+            if (s.rows >= 128 && a.x_row < 1u << 23 && a.w_row < 1u << 23) {
+                const unsigned over = (a.outer + 255) / 256, across = (a.rows + 255) / 256;
+                return launch_checked(q8_tile_kernel<256, 256, F>, over * across, 256, stream, a, over, across);
+            }
+        }
+        if (s.rows <= 16) return launch(q8_shared_inner_kernel<16, 16, 8, F, A>, 512, 16, 16);
+        if (s.rows <= 32) return launch(q8_shared_inner_kernel<32, 32, 4, F, A>, 256, 32, 32);
+        return launch(q8_shared_inner_kernel<64, 64, 4, F, A>, 256, 64, 64);
     };
-    auto stored = [&](auto f32, auto on_grid) { return whole ? sized(f32, on_grid, std::true_type()) : sized(f32, on_grid, std::false_type()); };
-    auto typed = [&](auto f32) { return aligned ? stored(f32, std::true_type()) : stored(f32, std::false_type()); };
+    auto typed = [&](auto f32) { return aligned ? sized(f32, std::true_type()) : sized(f32, std::false_type()); };
     return s.out_f32 ? typed(std::true_type()) : typed(std::false_type());
 }
 
