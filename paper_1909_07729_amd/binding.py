@@ -26,7 +26,7 @@ HOST_PATH = os.path.join(_HERE, "_ktanh_torch.so")
 INTERVALS = 32
 
 # Every function include/ktanh.h declares, with the kinds of its parameters:
-#   p = device tensor pointer, n = size_t, l = table pointer (32 intervals), L = table pointer (64),
+#   p = device tensor pointer, b = the same where a call's tensors are not all of a size (codes and scales beside values), n = size_t, l = table pointer (32 intervals), L = table pointer (64),
 #   a = kcap_shape_t pointer, g = kcap_pages_t pointer, q = kq8_shape_t pointer, m = ksample_shape_t pointer, t = int, s = stream, i = int status.  The ctypes prototypes below are built from these strings and nothing else.
 SIGNATURES = {
     "ktanh_status_string": "i", "ktanh_default_lut": "", "ktanh_lut_validate": "l",
@@ -55,10 +55,10 @@ SIGNATURES = {
     "kq8_rows": "qppnpls", "kq8_rows64": "qppnpLs", "kq8_product": "qpppppps", "kq8_linear_workspace": "q",
     "kq8_linear": "qppppppls", "kq8_linear64": "qppppppLs",
     "ksample": "mpppppppls", "ksample64": "mpppppppLs",
-    "kswish_keep8": "ppppnls", "kswish_keep8_backward": "pppppnls", "kgelu_keep8": "ppppnls", "kgelu_keep8_backward": "pppppnls",
-    "kswish_f32_keep8": "ppppnls", "kswish_f32_keep8_backward": "pppppnls", "kgelu_f32_keep8": "ppppnls", "kgelu_f32_keep8_backward": "pppppnls",
-    "kswish64_keep8": "ppppnLs", "kswish64_keep8_backward": "pppppnLs", "kgelu64_keep8": "ppppnLs", "kgelu64_keep8_backward": "pppppnLs",
-    "kswish64_f32_keep8": "ppppnLs", "kswish64_f32_keep8_backward": "pppppnLs", "kgelu64_f32_keep8": "ppppnLs", "kgelu64_f32_keep8_backward": "pppppnLs",
+    "kswish_keep8": "bbbbnls", "kswish_keep8_backward": "bbbbbnls", "kgelu_keep8": "bbbbnls", "kgelu_keep8_backward": "bbbbbnls",
+    "kswish_f32_keep8": "bbbbnls", "kswish_f32_keep8_backward": "bbbbbnls", "kgelu_f32_keep8": "bbbbnls", "kgelu_f32_keep8_backward": "bbbbbnls",
+    "kswish64_keep8": "bbbbnLs", "kswish64_keep8_backward": "bbbbbnLs", "kgelu64_keep8": "bbbbnLs", "kgelu64_keep8_backward": "bbbbbnLs",
+    "kswish64_f32_keep8": "bbbbnLs", "kswish64_f32_keep8_backward": "bbbbbnLs", "kgelu64_f32_keep8": "bbbbnLs", "kgelu64_f32_keep8_backward": "bbbbbnLs",
 }
 EXPORTS = tuple(SIGNATURES)
 
@@ -172,7 +172,7 @@ def load_library() -> ctypes.CDLL:
             raise FileNotFoundError(
                 f"{LIB_PATH} is not built; run `python -c 'import __graft_entry__ as g; g.build()'`")
         lib = ctypes.CDLL(LIB_PATH)
-        kinds = {"p": ctypes.c_void_p, "n": ctypes.c_size_t, "s": ctypes.c_void_p, "i": ctypes.c_int,
+        kinds = {"p": ctypes.c_void_p, "b": ctypes.c_void_p, "n": ctypes.c_size_t, "s": ctypes.c_void_p, "i": ctypes.c_int,
                  "l": ctypes.POINTER(KtanhLut), "L": ctypes.POINTER(KtanhLut64),
                  "a": ctypes.POINTER(KcapShape), "g": ctypes.POINTER(KcapPages), "q": ctypes.POINTER(Kq8Shape), "m": ctypes.POINTER(KsampleShape), "t": ctypes.c_int}
         for name, params in SIGNATURES.items():
@@ -628,7 +628,16 @@ def _check_checkpoint(codes, scales, count):
         raise ValueError("codes must have one byte for each value and scales one number for each 128")
 
 
+# by 4 * {0 Swish, 1 GELU} + 2 * {0 BFloat16, 1 Float32} + {0: 32, 1: 64 intervals}, as in csrc/ktanh_torch.cpp
+_KEEP8_INDEX = {f"k{a}{w}{t}_keep8": 4 * i + 2 * j + k for i, a in enumerate(("swish", "gelu")) for j, t in enumerate(("", "_f32"))
+                for k, w in enumerate(("", "64"))}
+
+
 def _keep8(name, x, out, codes, scales, lut, stream, dtypes):
+    if stream is None and _host is not None and out is None and codes is None and scales is None:
+        done = _host.keep8(_KEEP8_INDEX[name], x, lut)
+        if done is not None:
+            return done
     _check(x, dtypes, "in")
     out = _like(out, x, dtypes, "out", stream)
     codes = _empty(x.shape, torch.int8, x, stream) if codes is None else codes
@@ -643,6 +652,10 @@ def _keep8(name, x, out, codes, scales, lut, stream, dtypes):
 
 
 def _keep8_backward(name, dy, codes, scales, rebuild, dx, y, lut, stream, dtypes):
+    if stream is None and _host is not None and dx is None and y is None:
+        done = _host.keep8_backward(_KEEP8_INDEX[name[:-len("_backward")]], dy, codes, scales, rebuild is True, lut)
+        if done is not None:
+            return done
     _check(dy, dtypes, "dy")
     _check_checkpoint(codes, scales, dy.numel())
     dx = _like(dx, dy, dtypes, "dx", stream)
@@ -824,6 +837,10 @@ def kq8_product(codes, scales, weight, weight_scales, bias=None, *, out_dtype=to
     """(codes @ weight.T) * scales * weight_scales + bias: codes int8 [rows, inner] with scales Float32 [rows], weight int8 [outer, inner] with
     scales Float32 [outer], bias Float32 [outer] or None, any row strides; the sums are exact.  Returns out [rows, outer], BFloat16 or
     Float32 (``out``'s own type where it is given)."""
+    if stream is None and _host is not None:
+        done = _host.q8_product(codes, scales, weight, weight_scales, bias, out_dtype, out)
+        if done is not None:
+            return done
     _check_matrix(codes, (torch.int8,), "codes")
     rows, inner = codes.shape
     _check_vector(scales, "scales", rows)
@@ -840,6 +857,10 @@ def kq8_product(codes, scales, weight, weight_scales, bias=None, *, out_dtype=to
 def kq8_linear(x, weight, weight_scales, bias=None, *, activation=None, out_dtype=torch.bfloat16, out=None, lut=None, stream=None,
                _entry="kq8_linear"):
     """``kq8_product`` of ``kq8_rows(x, activation)``, in one call: x [rows, inner] BFloat16 or Float32, any row stride."""
+    if stream is None and _host is not None:
+        done = _host.q8_linear(x, weight, weight_scales, bias, out_dtype, out, activation, lut, _entry == "kq8_linear64")
+        if done is not None:
+            return done
     _check_matrix(x, _Q8_TYPES, "x")
     rows, inner = x.shape
     out, outer = _q8_weights(weight, weight_scales, bias, rows, inner, out, out_dtype, x, stream)
@@ -882,12 +903,18 @@ def ksample(logits, uniform, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, 
     int32 for top_k).  ``cap`` > 0 caps the logits through K-TanH before all else, cap * K(z / cap); -infinity masks a token.
     Returns int64 [rows]; -1 for a row with a NaN or without a token that is not masked.
     """
+    if stream is None and _host is not None:
+        done = _host.sample(logits, uniform, temperature, top_k, top_p, min_p, cap, out, lut, _entry == "ksample64")
+        if done is not None:
+            return done
     _check_matrix(logits, _Q8_TYPES, "logits")
     rows, vocabulary = logits.shape
     _check_vector(uniform, "uniform", rows)
     (temperature, temperatures), (top_k, top_ks), (top_p, top_ps), (min_p, min_ps) = (
         _setting(v, what, rows, dtype) for v, what, dtype in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
                                                              (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)))
+    if not isinstance(top_k, int):
+        raise TypeError("top_k must be a whole number or a tensor")
     if top_k < 0:
         raise ValueError("top_k must not be negative")
     out = _empty((rows,), torch.int64, logits, stream) if out is None else _dense_out(out, "out", (rows,), (torch.int64,))

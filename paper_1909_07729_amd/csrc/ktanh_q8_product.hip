@@ -333,29 +333,42 @@ __global__ __launch_bounds__(64 * W) void q8_shared_inner_kernel(Operands a)
 #pragma unroll
             for (unsigned j = 0; j < TI; ++j) sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[i], xf[j], sum[i][j], 0, 0, 0);
     };
-    const unsigned whole = a.inner / 64;
-    constexpr unsigned U = OI + TI > 4 ? 2 : 8;
-    unsigned s = wave;
-    for (; s + (U - 1) * W < whole; s += U * W) {
-        i32x4 wf[U][OI], xf[U][TI];
+    // Whole groups of U steps, the next group's operands on their way during the products of one; past the last the last is asked for again.
+    constexpr unsigned U = OI + TI > 4 ? 2 : OI + TI > 2 ? 4 : 8;
+    const unsigned whole = a.inner / 64, mine = whole > wave ? (whole - wave + W - 1) / W : 0, groups = mine / U;
+    i32x4 wf[2][U][OI], xf[2][U][TI];
+    auto load = [&](unsigned to, unsigned group) {
+        const unsigned at = (wave + (group < groups ? group : groups - 1) * U * W) * 64;
 #pragma unroll
         for (unsigned u = 0; u < U; ++u) {
 #pragma unroll
-            for (unsigned i = 0; i < OI; ++i) wf[u][i] = load16<ALIGNED>(w[i] + (s + u * W) * 64ull);
+            for (unsigned i = 0; i < OI; ++i) wf[to][u][i] = load16<ALIGNED>(w[i] + at + u * W * 64);
 #pragma unroll
-            for (unsigned i = 0; i < TI; ++i) xf[u][i] = load16<ALIGNED>(x[i] + (s + u * W) * 64ull);
+            for (unsigned i = 0; i < TI; ++i) xf[to][u][i] = load16<ALIGNED>(x[i] + at + u * W * 64);
         }
+    };
+    if (groups != 0) {
+        load(0, 0);
+        for (unsigned g = 0; g < groups; g += 2) {
+            load(1, g + 1);
 #pragma unroll
-        for (unsigned u = 0; u < U; ++u) multiply(wf[u], xf[u]);
+            for (unsigned u = 0; u < U; ++u) multiply(wf[0][u], xf[0][u]);
+            load(0, g + 2);
+            if (g + 1 < groups) {
+#pragma unroll
+                for (unsigned u = 0; u < U; ++u) multiply(wf[1][u], xf[1][u]);
+            }
+        }
     }
+    unsigned s = wave + groups * U * W;
     for (; s * 64 < a.inner; s += W) {
         const int there = (int)a.inner - (int)(s * 64 + k);
-        i32x4 wf[OI], xf[TI];
+        i32x4 w1[OI], x1[TI];
 #pragma unroll
-        for (unsigned i = 0; i < OI; ++i) wf[i] = load16<ALIGNED>(w[i] + s * 64ull, there);
+        for (unsigned i = 0; i < OI; ++i) w1[i] = load16<ALIGNED>(w[i] + s * 64, there);
 #pragma unroll
-        for (unsigned i = 0; i < TI; ++i) xf[i] = load16<ALIGNED>(x[i] + s * 64ull, there);
-        multiply(wf, xf);
+        for (unsigned i = 0; i < TI; ++i) x1[i] = load16<ALIGNED>(x[i] + s * 64, there);
+        multiply(w1, x1);
     }
     // a lane has 4 neighbouring channels of a row
 #pragma unroll

@@ -11,6 +11,7 @@
 // by the caller, tracing, dispatch and function modes, functional transforms, forward-mode gradients.  So
 // what is refused is refused there, with the messages of old, and nothing is decided here that a mode or a
 // transform would have to see.
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -806,6 +807,325 @@ PyObject *train_cap_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
+// ------------------------------------------------------------------- activations that keep 8 bits
+typedef ktanh_status_t (*Keep8)(const void *, void *, int8_t *, float *, size_t, const void *lut, ktanh_stream_t);
+typedef ktanh_status_t (*Keep8Backward)(const void *, const int8_t *, const float *, void *, void *, size_t, const void *lut, ktanh_stream_t);
+
+template <auto F> struct Keep8Of;
+template <class T, class L, ktanh_status_t (*F)(const T *, T *, int8_t *, float *, size_t, const L *, ktanh_stream_t)>
+struct Keep8Of<F> {
+    static constexpr Table table = TableKind<L>::value;
+    static ktanh_status_t call(const void *x, void *y, int8_t *codes, float *scales, size_t n, const void *lut, ktanh_stream_t s)
+    {
+        return F(static_cast<const T *>(x), static_cast<T *>(y), codes, scales, n, static_cast<const L *>(lut), s);
+    }
+};
+template <auto F> struct Keep8BackwardOf;
+template <class T, class L, ktanh_status_t (*F)(const T *, const int8_t *, const float *, T *, T *, size_t, const L *, ktanh_stream_t)>
+struct Keep8BackwardOf<F> {
+    static ktanh_status_t call(const void *dy, const int8_t *codes, const float *scales, void *dx, void *y, size_t n, const void *lut, ktanh_stream_t s)
+    {
+        return F(static_cast<const T *>(dy), codes, scales, static_cast<T *>(dx), static_cast<T *>(y), n, static_cast<const L *>(lut), s);
+    }
+};
+
+struct Keep8Entry {
+    const char *name, *backward_name;
+    Keep8 call;
+    Keep8Backward backward_call;
+    Table table;
+    at::ScalarType type;
+};
+#define KEEP8(fn, type) {#fn "_keep8", #fn "_keep8_backward", Keep8Of<&fn##_keep8>::call, Keep8BackwardOf<&fn##_keep8_backward>::call, Keep8Of<&fn##_keep8>::table, type}
+// by 4 * {0 Swish, 1 GELU} + 2 * {0 BFloat16, 1 Float32} + {0: 32, 1: 64 intervals}
+const Keep8Entry kKeep8[] = {
+    KEEP8(kswish, kBf16), KEEP8(kswish64, kBf16), KEEP8(kswish_f32, kF32), KEEP8(kswish64_f32, kF32),
+    KEEP8(kgelu, kBf16), KEEP8(kgelu64, kBf16), KEEP8(kgelu_f32, kF32), KEEP8(kgelu64_f32, kF32),
+};
+
+struct Kept {
+    Tensor y, codes, scales;
+};
+int64_t groups_of(int64_t count) { return (count + KTANH_KEEP8_GROUP - 1) / KTANH_KEEP8_GROUP; }
+
+Kept run_keep8(const Keep8Entry &entry, const Tensor &x, const void *lut)
+{
+    Kept k{at::empty_like(x), at::empty(x.sizes(), x.options().dtype(at::kChar)), at::empty({groups_of(x.numel())}, x.options().dtype(kF32))};
+    check_status(entry.call(x.const_data_ptr(), k.y.mutable_data_ptr(), static_cast<int8_t *>(k.codes.mutable_data_ptr()),
+                            static_cast<float *>(k.scales.mutable_data_ptr()), (size_t)x.numel(), lut, current_stream()), entry.name);
+    return k;
+}
+
+Tensor run_keep8_backward(const Keep8Entry &entry, const Tensor &dy, const Tensor &codes, const Tensor &scales, const Tensor &y, const void *lut)
+{
+    const Tensor dx = at::empty_like(dy);
+    check_status(entry.backward_call(dy.const_data_ptr(), static_cast<const int8_t *>(codes.const_data_ptr()), static_cast<const float *>(scales.const_data_ptr()),
+                                     dx.mutable_data_ptr(), y.defined() ? y.mutable_data_ptr() : nullptr, (size_t)dy.numel(), lut, current_stream()),
+                 entry.backward_name);
+    return dx;
+}
+
+const Keep8Entry *keep8_entry(PyObject *index)
+{
+    const long i = PyLong_AsLong(index);
+    return i < 0 || i >= (long)std::size(kKeep8) ? nullptr : &kKeep8[i];
+}
+
+// keep8(index, x, lut) -> (y, codes, scales), or None
+PyObject *keep8_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    const Keep8Entry *entry = nargs == 3 ? keep8_entry(args[0]) : nullptr;
+    if (entry == nullptr || !ordinary_thread()) Py_RETURN_NONE;
+    const Tensor *x = tensor_of(args[1], entry->type);
+    const TableArgument lut(args[2], entry->table);
+    if (x == nullptr || !lut.good()) Py_RETURN_NONE;
+    Kept k;
+    {
+        pybind11::gil_scoped_release no_gil;
+        k = run_keep8(*entry, *x, lut.pointer());
+    }
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(k.y)), THPVariable_Wrap(std::move(k.codes)), THPVariable_Wrap(std::move(k.scales)));
+    END_HANDLE_TH_ERRORS
+}
+
+// keep8_backward(index, dy, codes, scales, rebuild, lut) -> dx or (dx, y), or None
+PyObject *keep8_backward_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    const Keep8Entry *entry = nargs == 6 ? keep8_entry(args[0]) : nullptr;
+    if (entry == nullptr || !ordinary_thread()) Py_RETURN_NONE;
+    const Tensor *dy = tensor_of(args[1], entry->type), *codes = tensor_of(args[2], at::kChar), *scales = tensor_of(args[3], kF32);
+    const TableArgument lut(args[5], entry->table);
+    if (dy == nullptr || codes == nullptr || scales == nullptr || codes->numel() != dy->numel() || scales->numel() != groups_of(dy->numel()) || !lut.good())
+        Py_RETURN_NONE;
+    const bool rebuild = args[4] == Py_True;
+    Tensor dx, y;
+    {
+        pybind11::gil_scoped_release no_gil;
+        if (rebuild) y = at::empty_like(*dy);
+        dx = run_keep8_backward(*entry, *dy, *codes, *scales, y, lut.pointer());
+    }
+    if (!rebuild) return THPVariable_Wrap(std::move(dx));
+    return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(dx)), THPVariable_Wrap(std::move(y)));
+    END_HANDLE_TH_ERRORS
+}
+
+struct KeptActivation : public torch::autograd::Function<KeptActivation> {
+    static Tensor forward(AutogradContext *ctx, const Tensor &x, int64_t index)
+    {
+        const Kept k = run_keep8(kKeep8[index], x, nullptr);
+        ctx->save_for_backward({k.codes, k.scales});
+        ctx->saved_data["index"] = index;
+        return k.y;
+    }
+    static variable_list backward(AutogradContext *ctx, const variable_list &grads)
+    {
+        const variable_list saved = ctx->get_saved_variables();
+        const Keep8Entry &entry = kKeep8[ctx->saved_data["index"].toInt()];
+        const Tensor dy = grads[0].contiguous();
+        checked(dy, entry.type, "dy");
+        const Tensor &codes = checked(saved[0], at::kChar, "the saved codes"), &scales = checked(saved[1], kF32, "the saved scales");
+        TORCH_CHECK_VALUE(codes.numel() == dy.numel() && scales.numel() == groups_of(dy.numel()), "dy and the saved tensors differ in size");
+        return {run_keep8_backward(entry, dy, codes, scales, Tensor(), nullptr), Tensor()};
+    }
+};
+
+// train_keep8(index of the BFloat16 entry, x), x asking for a gradient -> y, or None
+PyObject *train_keep8_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (nargs != 2 || !ordinary_thread()) Py_RETURN_NONE;
+    long index = PyLong_AsLong(args[0]);
+    if (index < 0 || index + 2 >= (long)std::size(kKeep8)) Py_RETURN_NONE;
+    const Tensor *x = tensor_of(args[1], kBf16);
+    if (x == nullptr) {
+        x = tensor_of(args[1], kF32);
+        index += 2;
+    }
+    if (x == nullptr || !differentiable(*x) || !at::GradMode::is_enabled() || !x->requires_grad()) Py_RETURN_NONE;
+    Tensor y;
+    {
+        pybind11::gil_scoped_release no_gil;
+        y = KeptActivation::apply(*x, (int64_t)index);
+    }
+    return THPVariable_Wrap(std::move(y));
+    END_HANDLE_TH_ERRORS
+}
+
+// ------------------------------------------------------------------------ products in 8-bit integers
+// A matrix behind a Python object, its columns neighbours in memory.
+const Tensor *matrix_of(PyObject *o, at::ScalarType type)
+{
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const Tensor &t = THPVariable_Unpack(o);
+    if (!t.defined() || !ordinary_strided(t, type) || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1) || t.stride(0) < 0) return nullptr;
+    return &t;
+}
+const Tensor *matrix_of_values(PyObject *o)
+{
+    const Tensor *t = matrix_of(o, kBf16);
+    return t != nullptr ? t : matrix_of(o, kF32);
+}
+const Tensor *vector_of(PyObject *o, at::ScalarType type, int64_t count)
+{
+    const Tensor *t = tensor_of(o, type);
+    return t != nullptr && t->dim() == 1 && t->numel() == count ? t : nullptr;
+}
+
+const float *floats(const Tensor &t) { return static_cast<const float *>(t.const_data_ptr()); }
+const int8_t *bytes(const Tensor &t) { return static_cast<const int8_t *>(t.const_data_ptr()); }
+
+bool activation_of(PyObject *o, int *activation)
+{
+    if (o == Py_None) *activation = KQ8_NONE;
+    else if (!PyUnicode_CheckExact(o)) return false;
+    else if (PyUnicode_CompareWithASCIIString(o, "swish") == 0) *activation = KQ8_SWISH;
+    else if (PyUnicode_CompareWithASCIIString(o, "gelu") == 0) *activation = KQ8_GELU;
+    else return false;
+    return true;
+}
+
+// weight, weight_scales, bias (or None), out_dtype, out (or None) of a product
+struct Q8Weights {
+    const Tensor *weight, *scales, *bias = nullptr, *given = nullptr;
+    at::ScalarType type = kBf16;
+
+    bool take(PyObject *const *args, int64_t rows, int64_t inner)
+    {
+        weight = matrix_of(args[0], at::kChar);
+        if (weight == nullptr || weight->size(1) != inner) return false;
+        const int64_t outer = weight->size(0);
+        scales = vector_of(args[1], kF32, outer);
+        if (scales == nullptr) return false;
+        if (args[2] != Py_None && (bias = vector_of(args[2], kF32, outer)) == nullptr) return false;
+        if (args[4] != Py_None) {
+            given = matrix_of_values(args[4]);
+            if (given == nullptr || given->size(0) != rows || given->size(1) != outer || (rows > 1 && given->stride(0) < outer)) return false;
+            type = given->scalar_type();
+            return true;
+        }
+        if (!THPDtype_Check(args[3])) return false;
+        type = reinterpret_cast<THPDtype *>(args[3])->scalar_type;
+        return type == kBf16 || type == kF32;
+    }
+    Tensor out(const Tensor &like, int64_t rows) const { return given != nullptr ? *given : at::empty({rows, weight->size(0)}, like.options().dtype(type)); }
+    kq8_shape_t shape(const Tensor &x, const Tensor &out, int activation) const
+    {
+        return kq8_shape_t{(size_t)x.size(0), (size_t)x.size(1), (size_t)weight->size(0), step(x, 0), step(*weight, 0), step(out, 0),
+                           x.scalar_type() == kF32, type == kF32, activation};
+    }
+};
+
+Tensor workspace_of(size_t size, const Tensor &like)
+{
+    return size != 0 ? at::empty({(int64_t)size}, like.options().dtype(at::kByte)) : Tensor();
+}
+
+// q8_linear(x, weight, weight_scales, bias, out_dtype, out, activation, lut, wide) -> out, or None
+PyObject *q8_linear_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (nargs != 9 || !ordinary_thread()) Py_RETURN_NONE;
+    const bool wide = args[8] == Py_True;
+    const Tensor *x = matrix_of_values(args[0]);
+    Q8Weights w;
+    int activation;
+    if (x == nullptr || !w.take(args + 1, x->size(0), x->size(1)) || !activation_of(args[6], &activation)) Py_RETURN_NONE;
+    const TableArgument lut(args[7], wide ? TABLE64 : TABLE32);
+    if (!lut.good()) Py_RETURN_NONE;
+    Tensor made;
+    {
+        pybind11::gil_scoped_release no_gil;
+        made = w.out(*x, x->size(0));
+        const kq8_shape_t shape = w.shape(*x, made, activation);
+        const Tensor workspace = workspace_of(kq8_linear_workspace(&shape), *x);
+        void *work = workspace.defined() ? workspace.mutable_data_ptr() : nullptr;
+        const float *bias = w.bias != nullptr ? floats(*w.bias) : nullptr;
+        check_status(wide ? kq8_linear64(&shape, x->const_data_ptr(), bytes(*w.weight), floats(*w.scales), bias, made.mutable_data_ptr(), work,
+                                         static_cast<const ktanh_lut64_t *>(lut.pointer()), current_stream())
+                          : kq8_linear(&shape, x->const_data_ptr(), bytes(*w.weight), floats(*w.scales), bias, made.mutable_data_ptr(), work,
+                                       static_cast<const ktanh_lut_t *>(lut.pointer()), current_stream()),
+                     wide ? "kq8_linear64" : "kq8_linear");
+    }
+    return THPVariable_Wrap(std::move(made));
+    END_HANDLE_TH_ERRORS
+}
+
+// q8_product(codes, scales, weight, weight_scales, bias, out_dtype, out) -> out, or None
+PyObject *q8_product_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (nargs != 7 || !ordinary_thread()) Py_RETURN_NONE;
+    const Tensor *codes = matrix_of(args[0], at::kChar);
+    if (codes == nullptr) Py_RETURN_NONE;
+    const Tensor *scales = vector_of(args[1], kF32, codes->size(0));
+    Q8Weights w;
+    if (scales == nullptr || !w.take(args + 2, codes->size(0), codes->size(1))) Py_RETURN_NONE;
+    Tensor made;
+    {
+        pybind11::gil_scoped_release no_gil;
+        made = w.out(*codes, codes->size(0));
+        const kq8_shape_t shape = w.shape(*codes, made, KQ8_NONE);
+        check_status(kq8_product(&shape, bytes(*codes), floats(*scales), bytes(*w.weight), floats(*w.scales), w.bias != nullptr ? floats(*w.bias) : nullptr,
+                                 made.mutable_data_ptr(), current_stream()),
+                     "kq8_product");
+    }
+    return THPVariable_Wrap(std::move(made));
+    END_HANDLE_TH_ERRORS
+}
+
+// ------------------------------------------------------------------------------------- the next token
+// A setting: a number into *number, or a tensor of one for each row into *own.
+bool setting_of(PyObject *o, at::ScalarType type, int64_t rows, double *number, const Tensor **own)
+{
+    *own = nullptr;
+    if (number_of(o, number)) return true;
+    *number = 0.0;
+    *own = vector_of(o, type, rows);
+    return *own != nullptr;
+}
+
+// sample(logits, uniform, temperature, top_k, top_p, min_p, cap, out, lut, wide) -> tokens, or None
+PyObject *sample_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (nargs != 10 || !ordinary_thread()) Py_RETURN_NONE;
+    const bool wide = args[9] == Py_True;
+    const Tensor *logits = matrix_of_values(args[0]);
+    if (logits == nullptr) Py_RETURN_NONE;
+    const int64_t rows = logits->size(0);
+    const Tensor *uniform = vector_of(args[1], kF32, rows), *temperature, *top_k, *top_p, *min_p, *given;
+    ksample_shape_t s;
+    double first;
+    if (uniform == nullptr || !setting_of(args[2], kF32, rows, &s.temperature, &temperature) || PyFloat_CheckExact(args[3]) ||
+        !setting_of(args[3], at::kInt, rows, &first, &top_k) || !(first >= 0.0 && first < 1e9) || !setting_of(args[4], kF32, rows, &s.top_p, &top_p) ||
+        !setting_of(args[5], kF32, rows, &s.min_p, &min_p) || !number_of(args[6], &s.cap) || !output_of(args[7], at::kLong, {rows}, &given))
+        Py_RETURN_NONE;
+    const TableArgument lut(args[8], wide ? TABLE64 : TABLE32);
+    if (!lut.good()) Py_RETURN_NONE;
+    s.rows = (size_t)rows;
+    s.vocabulary = (size_t)logits->size(1);
+    s.row = step(*logits, 0);
+    s.f32 = logits->scalar_type() == kF32;
+    s.top_k = (size_t)first;
+    Tensor made;
+    {
+        pybind11::gil_scoped_release no_gil;
+        made = given != nullptr ? *given : at::empty({rows}, logits->options().dtype(at::kLong));
+        auto own = [](const Tensor *t) { return t != nullptr ? floats(*t) : nullptr; };
+        const int32_t *ks = top_k != nullptr ? ints(*top_k) : nullptr;
+        auto *tokens = static_cast<int64_t *>(made.mutable_data_ptr());
+        check_status(wide ? ksample64(&s, logits->const_data_ptr(), floats(*uniform), own(temperature), ks, own(top_p), own(min_p), tokens,
+                                      static_cast<const ktanh_lut64_t *>(lut.pointer()), current_stream())
+                          : ksample(&s, logits->const_data_ptr(), floats(*uniform), own(temperature), ks, own(top_p), own(min_p), tokens,
+                                    static_cast<const ktanh_lut_t *>(lut.pointer()), current_stream()),
+                     wide ? "ksample64" : "ksample");
+    }
+    return THPVariable_Wrap(std::move(made));
+    END_HANDLE_TH_ERRORS
+}
+
 // ------------------------------------------------------------------------------------------ module
 // setup(KtanhLut, KtanhLut64, KtanhError): the classes of binding.py
 PyObject *setup_call(PyObject *, PyObject *args)
@@ -833,6 +1153,12 @@ PyMethodDef kMethods[] = {
     {"cap_attention_paged", as_method(cap_paged_call), METH_FASTCALL, nullptr},
     {"cap_append", as_method(cap_append_call), METH_FASTCALL, nullptr},
     {"train_cap_attention", as_method(train_cap_call), METH_FASTCALL, nullptr},
+    {"keep8", as_method(keep8_call), METH_FASTCALL, nullptr},
+    {"keep8_backward", as_method(keep8_backward_call), METH_FASTCALL, nullptr},
+    {"train_keep8", as_method(train_keep8_call), METH_FASTCALL, nullptr},
+    {"q8_linear", as_method(q8_linear_call), METH_FASTCALL, nullptr},
+    {"q8_product", as_method(q8_product_call), METH_FASTCALL, nullptr},
+    {"sample", as_method(sample_call), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyMethodDef g_unary_defs[std::size(kUnary)], g_binary_defs[std::size(kBinary)];

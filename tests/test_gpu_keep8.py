@@ -243,3 +243,37 @@ def test_graphs_and_streams(gpu):
         for got, w in ((y, want), (codes, c), (scales, s), (dx, d), (back, b)):
             assert torch.equal(got, w)
     assert torch.autograd.grad(eager, x, dy)[0].shape == x.shape
+
+
+def test_both_host_paths_give_the_same(gpu, monkeypatch):
+    """Ordinary calls go through C++ where it is built, others through Python."""
+    torch, binding = gpu
+    from paper_1909_07729_amd import autograd
+    assert binding._host is not None
+    torch.manual_seed(0)
+    for name in NAMES:
+        f32 = name.endswith("_f32")
+        x = torch.randn(3, 700, device="cuda").to(torch.float32 if f32 else torch.bfloat16)
+        table = binding.ktanh_fit_lut64() if "64" in name else binding.ktanh_fit_lut_bmin0()
+        results = []
+        for host in (binding._host, None):
+            monkeypatch.setattr(binding, "_host", host)
+            leaf = x.clone().requires_grad_()
+            y = getattr(autograd, name.split("64")[0].split("_f32")[0])(leaf, intervals=64 if "64" in name else 32, keep=8)
+            made = []
+            for lut in (None, table):
+                kept = getattr(binding, name + "_keep8")(x, lut=lut)
+                made += [*kept, getattr(binding, name + "_keep8_backward")(x, *kept[1:], lut=lut),
+                         *getattr(binding, name + "_keep8_backward")(x, *kept[1:], rebuild=True, lut=lut)]
+            results.append([y, *torch.autograd.grad(y, leaf, x), *made])
+            monkeypatch.undo()
+        for a, b in zip(*results):
+            assert a.dtype == b.dtype and a.shape == b.shape and torch.equal(a, b), name
+    with pytest.raises(binding.KtanhError):
+        bad = binding.ktanh_default_lut()
+        bad.r[5] = 9
+        binding.kgelu_keep8(x.bfloat16(), lut=bad)
+    with pytest.raises(TypeError):
+        binding.kgelu_keep8(x.double())
+    with pytest.raises(ValueError):
+        binding.kgelu_keep8_backward(x.bfloat16(), *binding.kgelu_keep8(x[:1].bfloat16())[1:])

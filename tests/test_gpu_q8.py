@@ -239,3 +239,41 @@ def test_graphs_streams_and_repeated_calls(gpu):
     two = both(x, stream=side)
     side.synchronize()
     assert torch.equal(one, want) and torch.equal(two, want)
+
+
+def test_both_host_paths_give_the_same(gpu, monkeypatch):
+    """Ordinary calls go through C++ where it is built, others through Python."""
+    torch, binding = gpu
+    assert binding._host is not None
+    x = _x(torch, 5, 100, torch.bfloat16, 1, apart=3)
+    weight, weight_scales = binding.kq8_rows(_x(torch, 70, 100, torch.bfloat16, 2))
+    codes, scales = binding.kq8_rows(x)
+    bias, table = _scales(torch, 70, 3), binding.ktanh_fit_lut_bmin0()
+    wide = torch.empty((5, 90), dtype=torch.float32, device="cuda")
+    results = []
+    for host in (binding._host, None):
+        monkeypatch.setattr(binding, "_host", host)
+        made = [binding.kq8_linear(v, weight, weight_scales, b, activation=act, out_dtype=dtype)
+                for v in (x, x.float()) for b in (None, bias) for act in (None, "gelu", "swish") for dtype in (torch.bfloat16, torch.float32)]
+        made += [binding.kq8_linear64(x, weight, weight_scales, activation="gelu"), binding.kq8_linear(x, weight, weight_scales, activation="gelu", lut=table),
+                 binding.kq8_product(codes, scales, weight, weight_scales, bias), binding.kq8_product(codes, scales, weight, weight_scales, out_dtype=torch.float32),
+                 binding.kq8_linear(x, weight, weight_scales, out=wide[:, :70]).clone(), binding.kq8_product(codes, scales, weight, weight_scales, out=wide[:, 20:]).clone()]
+        results.append(made)
+        monkeypatch.undo()
+    for a, b in zip(*results):
+        assert a.dtype == b.dtype and a.shape == b.shape and torch.equal(a, b)
+
+
+def test_refused_calls(gpu):
+    torch, binding = gpu
+    x, w, one = torch.ones((4, 64), device="cuda"), torch.ones((8, 64), dtype=torch.int8, device="cuda"), torch.ones(8, device="cuda")
+    for call, error in ((lambda: binding.kq8_linear(x, w[:, :32], one), ValueError), (lambda: binding.kq8_linear(x, w, one[:4]), ValueError),
+                        (lambda: binding.kq8_linear(x, w.short(), one), TypeError), (lambda: binding.kq8_linear(x.half(), w, one), TypeError),
+                        (lambda: binding.kq8_linear(x, w, one, out_dtype=torch.float16), TypeError), (lambda: binding.kq8_linear(x, w, one, one.double()), TypeError),
+                        (lambda: binding.kq8_linear(x, w, one, activation="relu"), ValueError), (lambda: binding.kq8_linear(x.t(), w[:, :4], one), ValueError),
+                        (lambda: binding.kq8_linear(x, w, one, out=torch.empty((4, 9), device="cuda")), ValueError),
+                        (lambda: binding.kq8_linear(x, w, one, out=torch.empty(8, device="cuda").expand(4, 8)), ValueError),
+                        (lambda: binding.kq8_rows(x[0]), ValueError), (lambda: binding.kq8_rows(x, codes=w), ValueError),
+                        (lambda: binding.kq8_rows(x, codes=w[:1].expand(4, 64)), ValueError), (lambda: binding.kq8_product(w, one[:2], w, one), ValueError)):
+        with pytest.raises(error):
+            call()

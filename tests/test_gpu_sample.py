@@ -211,3 +211,28 @@ def test_graphs_streams_and_outputs(gpu):
     side.synchronize()
     assert torch.equal(one, want[1])
     assert binding.ksample(logits[:0], u[:0]).shape == (0,)
+
+
+def test_both_host_paths_give_the_same_and_refuse(gpu, monkeypatch):
+    """Ordinary calls go through C++ where it is built, others through Python."""
+    torch, binding = gpu
+    assert binding._host is not None
+    logits, u = _logits(torch, 6, 5000, "bfloat16", 9)[:, 3:], _uniform(torch, 6, 9)
+    each = {"temperature": torch.full((6,), 0.7, device="cuda"), "top_k": torch.full((6,), 30, dtype=torch.int32, device="cuda"),
+            "top_p": torch.full((6,), 0.9, device="cuda"), "min_p": torch.full((6,), 0.01, device="cuda")}
+    results = []
+    for host in (binding._host, None):
+        monkeypatch.setattr(binding, "_host", host)
+        results.append([binding.ksample(logits, u), binding.ksample(logits.float(), u, temperature=0.7, top_k=30, top_p=0.9, min_p=0.01),
+                        binding.ksample(logits, u, **each), binding.ksample64(logits, u, cap=30, top_p=1), binding.ksample(logits, u, top_k=10 ** 12)])
+        for bad, error in ((dict(temperature=-1.0), binding.KtanhError), (dict(top_p=1.5), binding.KtanhError), (dict(cap=-3.0), binding.KtanhError),
+                           (dict(top_k=-1), ValueError), (dict(top_k=2.5), TypeError), (dict(temperature=each["temperature"][:3]), ValueError),
+                           (dict(top_k=each["top_p"]), TypeError), (dict(out=torch.empty(6, device="cuda")), TypeError)):
+            with pytest.raises(error):
+                binding.ksample(logits, u, **bad)
+        monkeypatch.undo()
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and torch.equal(results[0][1], results[0][2])
+    with pytest.raises(ValueError):
+        binding.ksample(logits, u[:5])
+    with pytest.raises(binding.KtanhError):
+        binding.ksample(logits[:, :0], u)
