@@ -532,8 +532,8 @@ ktanh_status_t kcap_append(const kcap_shape_t *shape, const kcap_pages_t *cache,
 #define KSAMPLE_MOST 1048575
 
 typedef struct ksample_shape {
-    size_t rows, vocabulary;       /* logits [rows][vocabulary], 1 to KSAMPLE_MOST tokens, up to 2^30 rows  */
-    size_t row;                    /* stride of the rows, in elements                                       */
+    size_t rows, vocabulary;       /* logits [rows][vocabulary], 1 to KSAMPLE_MOST tokens; rows times chunks  */
+    size_t row;                    /* stride of the rows, in elements      (of 32768) below 2^22             */
     int f32;                       /* Float32, else BFloat16                                                */
     double cap;                    /* 0: none                                                               */
     double temperature;            /* settings of all rows, Float32 numbers, where the pointer of the rows' */
@@ -546,11 +546,14 @@ typedef struct ksample_shape {
  *              (1: the last of the kept tokens), and NaNs as 0 (top_p: 1)
  *   temperature, top_p, min_p   device, Float32 [rows], or NULL         top_k   device, int32 [rows], or NULL
  *   tokens     device, out: int64 [rows]
+ *   workspace  device, 16-byte aligned, ksample_workspace bytes; unused and may be NULL where that is 0 (up to 32768 tokens).  What it holds
+ *              before does not matter; calls that may run at once need one each
  * KT_ERR_SHAPE: sizes or settings out of range, a cap below 1e-30.  `lut` is read where cap > 0. */
+size_t ksample_workspace(const ksample_shape_t *shape);
 ktanh_status_t ksample(const ksample_shape_t *shape, const void *logits, const float *uniform, const float *temperature, const int32_t *top_k,
-                       const float *top_p, const float *min_p, int64_t *tokens, const ktanh_lut_t *lut, ktanh_stream_t stream);
+                       const float *top_p, const float *min_p, int64_t *tokens, void *workspace, const ktanh_lut_t *lut, ktanh_stream_t stream);
 ktanh_status_t ksample64(const ksample_shape_t *shape, const void *logits, const float *uniform, const float *temperature, const int32_t *top_k,
-                         const float *top_p, const float *min_p, int64_t *tokens, const ktanh_lut64_t *lut, ktanh_stream_t stream);
+                         const float *top_p, const float *min_p, int64_t *tokens, void *workspace, const ktanh_lut64_t *lut, ktanh_stream_t stream);
 
 #ifdef __cplusplus
 }

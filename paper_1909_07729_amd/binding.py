@@ -54,7 +54,7 @@ SIGNATURES = {
     "kcap_append": "agpppppppppppnnts",
     "kq8_rows": "qppnpls", "kq8_rows64": "qppnpLs", "kq8_product": "qpppppps", "kq8_linear_workspace": "q",
     "kq8_linear": "qppppppls", "kq8_linear64": "qppppppLs",
-    "ksample": "mpppppppls", "ksample64": "mpppppppLs",
+    "ksample_workspace": "m", "ksample": "mppppppppls", "ksample64": "mppppppppLs",
     "kswish_keep8": "bbbbnls", "kswish_keep8_backward": "bbbbbnls", "kgelu_keep8": "bbbbnls", "kgelu_keep8_backward": "bbbbbnls",
     "kswish_f32_keep8": "bbbbnls", "kswish_f32_keep8_backward": "bbbbbnls", "kgelu_f32_keep8": "bbbbnls", "kgelu_f32_keep8_backward": "bbbbbnls",
     "kswish64_keep8": "bbbbnLs", "kswish64_keep8_backward": "bbbbbnLs", "kgelu64_keep8": "bbbbnLs", "kgelu64_keep8_backward": "bbbbbnLs",
@@ -181,7 +181,7 @@ def load_library() -> ctypes.CDLL:
             fn.restype = ctypes.c_int
         lib.ktanh_status_string.restype = ctypes.c_char_p
         lib.ktanh_default_lut.restype = ctypes.POINTER(KtanhLut)
-        for name in ("kcap_attention_paged_workspace", "kcap_attention_backward_workspace", "kq8_linear_workspace"):
+        for name in ("kcap_attention_paged_workspace", "kcap_attention_backward_workspace", "kq8_linear_workspace", "ksample_workspace"):
             getattr(lib, name).restype = ctypes.c_size_t
         _load_host()
         _lib = lib
@@ -920,8 +920,11 @@ def ksample(logits, uniform, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, 
     out = _empty((rows,), torch.int64, logits, stream) if out is None else _dense_out(out, "out", (rows,), (torch.int64,))
     _check_here(logits, uniform, temperatures, top_ks, top_ps, min_ps, out)
     shape = KsampleShape(rows, vocabulary, _step(logits, 0), logits.dtype == torch.float32, cap, temperature, top_p, min_p, top_k)
-    st = getattr(load_library(), _entry)(shape, logits.data_ptr(), uniform.data_ptr(), *map(_pointer, (temperatures, top_ks, top_ps, min_ps)), out.data_ptr(),
-                                         _lut_arg(lut), _stream_handle(stream))
+    lib = load_library()
+    size = lib.ksample_workspace(shape)
+    workspace = _empty((size,), torch.uint8, logits, stream) if size else None
+    st = getattr(lib, _entry)(shape, logits.data_ptr(), uniform.data_ptr(), *map(_pointer, (temperatures, top_ks, top_ps, min_ps)), out.data_ptr(),
+                              _pointer(workspace), _lut_arg(lut), _stream_handle(stream))
     if st != 0:
         raise KtanhError(st, _entry)
     return out

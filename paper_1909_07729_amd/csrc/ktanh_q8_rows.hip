@@ -1,6 +1,6 @@
 // libktanh: rows of values, or of an activation's outputs, in 8-bit integers with a scale for each row.
 //
-// One pass: a row is held in registers between the search for its largest magnitude and its rounding (rows beyond 65536 BFloat16 or 32768
+// One pass: a row is held in registers between the search for its largest magnitude and its rounding (rows beyond 32768 BFloat16 or 16384
 // Float32 values are read twice).  Bound by memory: 3 bytes a BFloat16 value.
 #include "ktanh_codes.h"
 #include "ktanh_q8.h"
@@ -115,7 +115,7 @@ ktanh_status_t launch_rows(const kq8_shape_t &s, const void *x, int8_t *codes, s
         if (vectors <= 512) return launch(q8_rows_kernel<ELEM, ACT, WIDE, ALIGNED, 256, 2>, 256);
         if (vectors <= 1024) return launch(q8_rows_kernel<ELEM, ACT, WIDE, ALIGNED, 256, 4>, 256);
         if (vectors <= 2048) return launch(q8_rows_kernel<ELEM, ACT, WIDE, ALIGNED, 256, 8>, 256);
-        if (vectors <= 8192) return launch(q8_rows_kernel<ELEM, ACT, WIDE, ALIGNED, 1024, 8>, 1024);
+        if (vectors <= 4096) return launch(q8_rows_kernel<ELEM, ACT, WIDE, ALIGNED, 1024, 4>, 1024);
         return launch(q8_rows_kernel<ELEM, ACT, WIDE, ALIGNED, 1024, 0>, 1024);
     };
     return aligned ? of(std::true_type()) : of(std::false_type());

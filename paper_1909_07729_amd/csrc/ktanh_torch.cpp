@@ -1116,9 +1116,11 @@ PyObject *sample_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         auto own = [](const Tensor *t) { return t != nullptr ? floats(*t) : nullptr; };
         const int32_t *ks = top_k != nullptr ? ints(*top_k) : nullptr;
         auto *tokens = static_cast<int64_t *>(made.mutable_data_ptr());
-        check_status(wide ? ksample64(&s, logits->const_data_ptr(), floats(*uniform), own(temperature), ks, own(top_p), own(min_p), tokens,
+        const Tensor workspace = workspace_of(ksample_workspace(&s), *logits);
+        void *work = workspace.defined() ? workspace.mutable_data_ptr() : nullptr;
+        check_status(wide ? ksample64(&s, logits->const_data_ptr(), floats(*uniform), own(temperature), ks, own(top_p), own(min_p), tokens, work,
                                       static_cast<const ktanh_lut64_t *>(lut.pointer()), current_stream())
-                          : ksample(&s, logits->const_data_ptr(), floats(*uniform), own(temperature), ks, own(top_p), own(min_p), tokens,
+                          : ksample(&s, logits->const_data_ptr(), floats(*uniform), own(temperature), ks, own(top_p), own(min_p), tokens, work,
                                     static_cast<const ktanh_lut_t *>(lut.pointer()), current_stream()),
                      wide ? "ksample64" : "ksample");
     }

@@ -87,7 +87,7 @@ def test_settings_of_each_row(gpu, dtype, rows, vocabulary):
     assert got.tolist() == [_token(z[r], un[r], **{n: v[r].item() for n, v in values.items()}) for r in range(rows)]
 
 
-@pytest.mark.parametrize("vocabulary", [3000, 30000])
+@pytest.mark.parametrize("vocabulary", [3000, 30000, 70000])
 def test_ties_flat_rows_and_outliers(gpu, vocabulary):
     """Rows that crowd one bin: equal logits, two values, a flat row under one outlier, differences at the last bit."""
     torch, binding = gpu
