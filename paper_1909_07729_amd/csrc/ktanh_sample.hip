@@ -10,8 +10,10 @@
 // Within a bin weights are summed as integers, multiples of 2^-32 of the power of two above: such sums do not depend on the order in which
 // lanes add to them.  Sums over bins and over sorted tokens are doubles in a fixed order.
 //
-// A block holds up to 32768 logits in registers.  Rows of no more take one launch, and are read once.  Longer ones are cut into chunks of that size
-// and take four: the chunks' largest logits, their bins, their tokens of the bins that hold answers, and one block for the answers.
+// A block holds up to 32768 logits in registers.  Rows of no more take one launch, and are read once.  Longer ones are cut into chunks and take
+// four: the chunks' largest logits, their bins, their tokens of the bins that hold answers, and one block for the answers.
+// Sums over the bins and over the listed tokens are formed once, with barriers; questions are then searches that every wavefront makes for
+// itself, with none.
 #include "ktanh_codes.h"
 #include "ktanh_stream_impl.h"
 
@@ -24,19 +26,18 @@ namespace {
 
 constexpr unsigned kThreads = 1024, kBins = kThreads;   // a bin for each lane of a block
 constexpr unsigned kListed = 2048;                      // tokens that a block sorts
-constexpr unsigned kChunk = 32 * kThreads;
+constexpr unsigned kRanked = 512;                       // of these, how many by counting
+constexpr unsigned kMost = 32, kFew = 8;                // logits of a lane
 constexpr unsigned kSteps = 7;                          // log2 of the finest bins to a factor of two
 constexpr double kFar = 73.5;                           // KSAMPLE_MOST 2^-kFar < 2^-53: what lies beyond does not reach a sum of doubles
 constexpr double kLog2e = 1.4426950408889634;
-constexpr uint32_t kNan = 0xFFFFFFFFu, kNothing = 0x007FFFFFu;   // keys of a NaN and of -infinity
 
 typedef unsigned long long u64;
 
-// Float32 values in their order as integers; one zero, and NaNs above all.
+// Float32 values in their order as integers, with one zero.
 __device__ __forceinline__ uint32_t key_of(float z)
 {
     const uint32_t u = __float_as_uint(z + 0.0f);
-    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return kNan;
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float value_of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
@@ -55,8 +56,9 @@ struct SampleArgs {
     float cap;
     long long *tokens;
     // of rows in chunks: by row and chunk, and by row
-    u64 *best, *bins, *list;
-    uint32_t *low, *by_min, *listed;
+    u64 *bins, *list;
+    float4 *ends;       // the largest logit, the smallest, whether there is a NaN, the index of the largest
+    uint32_t *by_min, *listed;
 };
 
 // A value that all lanes have alike, in scalar registers: the vector ones hold the logits.
@@ -108,19 +110,24 @@ __device__ __forceinline__ uint4 load_logits(const ELEM *from, unsigned at, unsi
     if (count != 0) v = load_values<false, true>(from + at, count);
     return v;
 }
-template <class ELEM, bool CAP, bool WIDE>
-__device__ __forceinline__ void logits_of(uint4 v, unsigned at, unsigned end, float cap, const LaneTable &tab, float (&z)[kPerLane<ELEM>])
+// What is behind the row is like masked tokens, which the cap leaves masked.  The table reads need all lanes.
+template <bool CAP, bool WIDE>
+__device__ __forceinline__ float logit_of(float z, bool inside, float cap, const LaneTable &tab)
 {
-    widen<ELEM>(v, z);
-#pragma unroll
-    for (unsigned i = 0; i < kPerLane<ELEM>; ++i) {
-        if constexpr (CAP) {    // the table reads need all lanes
-            const float t = __uint_as_float(ktanh_f32_one<WIDE>(__float_as_uint(z[i] / cap), tab));
-            z[i] = z[i] == -INFINITY ? z[i] : cap * t;      // a masked token stays masked
-        }
-        if (at + i >= end) z[i] = -INFINITY;                // what is behind the row is like masked tokens
+    if constexpr (CAP) {
+        const float t = __uint_as_float(ktanh_f32_one<WIDE>(__float_as_uint(z / cap), tab));
+        z = z == -INFINITY ? z : cap * t;
     }
+    return inside ? z : -INFINITY;
 }
+
+// Which logits can be among the first: (top - z) * by < limit, in Float32 operations, which keep the order of logits.  by == 0: all.
+struct Near {
+    float top, by, limit;
+    __device__ __forceinline__ bool all() const { return by == 0.f; }
+    __device__ __forceinline__ bool operator()(float z) const { return (top - z) * by < limit; }
+};
+constexpr Near kAll{0.f, 0.f, 1.f};
 
 // Logits of `first` .. `end` - 1 in a block's registers, E to a lane.
 template <class ELEM, bool CAP, bool WIDE, unsigned E>
@@ -136,13 +143,23 @@ struct Held {
         for (unsigned v = 0; v < E / N; ++v) raw[v] = load_logits(from, place(v), end);
 #pragma unroll
         for (unsigned v = 0; v < E / N; ++v) {
-            logits_of<ELEM, CAP, WIDE>(raw[v], place(v), end, cap, tab, z[v]);
+            widen<ELEM>(raw[v], z[v]);
+#pragma unroll
+            for (unsigned i = 0; i < N; ++i) z[v][i] = logit_of<CAP, WIDE>(z[v][i], place(v) + i < end, cap, tab);
             if constexpr (CAP) {    // one vector at a time: all at once do not fit the registers
 #pragma unroll
                 for (unsigned i = 0; i < N; ++i) asm volatile("" : "+v"(z[v][i]));
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
+    }
+    // The others are masked from here on.
+    __device__ __forceinline__ void keep(const Near &near)
+    {
+#pragma unroll
+        for (unsigned v = 0; v < E / N; ++v)
+#pragma unroll
+            for (unsigned i = 0; i < N; ++i) z[v][i] = near(z[v][i]) ? z[v][i] : -INFINITY;
     }
     __device__ __forceinline__ unsigned place(unsigned v) const { return first + (v * kThreads + threadIdx.x) * N; }
     // f(z, index) for each, by every lane of a block.  What f makes of a logit is made again in the next pass, and not kept.
@@ -151,35 +168,38 @@ struct Held {
     {
 #pragma unroll
         for (unsigned v = 0; v < E / N; ++v) {
+            unsigned at = place(v);
+            asm volatile("" : "+v"(at));
 #pragma unroll
             for (unsigned i = 0; i < N; ++i) asm volatile("" : "+v"(z[v][i]));
 #pragma unroll
             for (unsigned i = 0; i < N; ++i) {
-                f(z[v][i], place(v) + i);
+                f(z[v][i], at + i);
                 if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
 };
 
-// The same from memory, each time.
+// The same from memory, each time: for the few rows whose answers are not where the sums of bins say.
 template <class ELEM, bool CAP, bool WIDE>
 struct Read {
     const ELEM *from;
     unsigned end;
     float cap;
     const LaneTable &tab;
+    Near near;
 
     template <class F>
     __device__ __forceinline__ void each(F f) const
     {
-        constexpr unsigned N = kPerLane<ELEM>;
-        for (unsigned base = 0; base < end; base += kThreads * N) {
-            const unsigned at = base + threadIdx.x * N;
-            float z[N];
-            logits_of<ELEM, CAP, WIDE>(load_logits(from, at, end), at, end, cap, tab, z);
-#pragma unroll
-            for (unsigned i = 0; i < N; ++i) f(z[i], at + i);
+#pragma unroll 1
+        for (unsigned base = 0; base < end; base += kThreads) {
+            const unsigned at = base + threadIdx.x;
+            uint32_t u = at < end ? (uint32_t)from[at] : 0u;
+            if constexpr (sizeof(ELEM) == 2) u <<= 16;
+            const float z = logit_of<CAP, WIDE>(__uint_as_float(u), at < end, cap, tab);
+            f(near.all() || near(z) ? z : -INFINITY, at);
         }
     }
 };
@@ -190,63 +210,116 @@ struct Mass {
     double mass;
 };
 __device__ __forceinline__ Mass operator+(Mass a, Mass b) { return Mass{a.count + b.count, a.mass + b.mass}; }
+__device__ __forceinline__ Mass uniform(Mass m) { return Mass{uniform(m.count), uniform(m.mass)}; }
+
+constexpr unsigned kWaves = kThreads / 64;
 
 struct Shared {
-    Mass part[kThreads / 64];
-    u64 best[kThreads / 64];
-    uint32_t low[kThreads / 64];
+    Mass part[kWaves];
+    float top[kWaves], low[kWaves];
+    uint32_t strange[kWaves], first[kWaves];
+    unsigned from[4], to[4];        // bins that the plan lists
     double power[1u << kSteps];     // 2^(-j / 128)
     u64 bins[kBins];                // count << 48 | mass
-    Mass own[kBins], upto[kBins];   // of each bin, and of all up to it: a lane's own, which its registers have no room for
+    uint32_t count[kBins];          // of all bins up to each
+    double mass[kBins];
     uint32_t flags[kBins / 32];     // bins whose tokens are listed
     uint32_t starts[kBins];         // of the flagged bins in the list
     u64 list[kListed];
-    uint32_t listed, found;
-    Mass before, at;
+    double list_mass[kListed];      // of all listed tokens up to each
+    uint32_t ranks[kRanked];
+    uint32_t listed, by_min;
     u64 low_place, high_place;
+    // a question that is not answered by the list
+    uint32_t asked;
+    unsigned asked_bin;
+    uint32_t asked_count, asked_above;
+    double asked_mass;
+    Mass asked_before, asked_with;
 };
 
-// Sums over the first lanes of a wavefront.
-template <unsigned LANES>
+// Moves between the lanes of a wavefront; lanes that none moves to get 0.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, true); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ Mass moved(Mass m)
+{
+    const u64 v = (u64)__double_as_longlong(m.mass);
+    const u64 to = (u64)moved<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)v);
+    return Mass{moved<CTRL, ROWS>(m.count), __longlong_as_double((long long)to)};
+}
+// Sums of a wavefront's lanes up to and with each: within rows of 16 lanes, then from row to row.
 __device__ __forceinline__ Mass scanned(Mass v)
 {
-    const unsigned lane = threadIdx.x % LANES;
-#pragma unroll
-    for (unsigned by = 1; by < LANES; by *= 2) {
-        const Mass other{(uint32_t)__shfl_up((int)v.count, by), __shfl_up(v.mass, by)};
-        if (lane >= by) v = v + other;
-    }
-    return v;
+    v = v + moved<0x111, 0xF>(v);   // row_shr
+    v = v + moved<0x112, 0xF>(v);
+    v = v + moved<0x114, 0xF>(v);
+    v = v + moved<0x118, 0xF>(v);
+    v = v + moved<0x142, 0xA>(v);   // row_bcast:15
+    return v + moved<0x143, 0xC>(v);
 }
 
-// Sum of the lanes up to and with this one; `total` is that of all.
-__device__ __forceinline__ Mass sum_up_to(Mass v, Shared &sh, Mass &total)
+// Sum of the block's lanes up to and with this one.
+__device__ __forceinline__ Mass sum_up_to(Mass v, Shared &sh)
 {
-    constexpr unsigned kWaves = kThreads / 64;
     const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const Mass run = scanned<64>(v);
+    const Mass run = scanned(v);
     __syncthreads();        // the last use of part
     if (lane == 63) sh.part[wave] = run;
     __syncthreads();
-    const Mass parts = scanned<kWaves>(sh.part[lane % kWaves]);
-    total = Mass{(uint32_t)__shfl((int)parts.count, kWaves - 1), __shfl(parts.mass, kWaves - 1)};
-    const Mass first{(uint32_t)__shfl((int)parts.count, (int)wave - 1), __shfl(parts.mass, (int)wave - 1)};
-    return wave != 0 ? first + run : run;
+    const Mass parts = scanned(lane < kWaves ? sh.part[lane] : Mass{0, 0.0});
+    const Mass before{(uint32_t)__shfl((int)parts.count, (int)wave - 1), __shfl(parts.mass, (int)wave - 1)};
+    return wave != 0 ? before + run : run;
 }
 
-// Sorts sh.list[0 .. n), n <= kListed; what is behind it up to a power of two is overwritten.
+// The first of n (at most 64 * 64) for which `holds`, n if for none: a search by a wavefront whose lanes look at 64 places at once.  `holds` stays true once
+// it is.
+template <class F>
+__device__ __forceinline__ unsigned first_where(unsigned n, F holds)
+{
+    const unsigned lane = threadIdx.x % 64, step = (n + 63) / 64;
+    auto at = [&](unsigned i) { return i < n && holds(i); };
+    const unsigned end = (lane + 1) * step - 1;
+    const u64 ends = __ballot(end < n ? holds(end) : lane * step < n && holds(n - 1));
+    if (ends == 0) return n;
+    const unsigned first = (unsigned)__builtin_ctzll(ends) * step;
+    const u64 inside = __ballot(lane < step && at(first + lane));
+    return inside == 0 ? n - 1 : first + (unsigned)__builtin_ctzll(inside);
+}
+
+// Sorts sh.list[0 .. n), n <= kListed; what is behind it up to a power of two is overwritten.  Few by counting for each how many are below it, shared
+// out among all lanes (64 tokens: 4 comparisons a lane); many by a bitonic network.
 __device__ __forceinline__ void sort_list(Shared &sh, unsigned n)
 {
-    unsigned size = 64;
-    while (size < n) size *= 2;
+    __syncthreads();
+    if (n <= kRanked) {
+        unsigned lg = 6;
+        while ((1u << lg) < n) ++lg;
+        const unsigned i = threadIdx.x & ((1u << lg) - 1), slice = threadIdx.x >> lg, slices = kThreads >> lg;
+        if (threadIdx.x < kRanked) sh.ranks[threadIdx.x] = 0;
+        const u64 mine = i < n ? sh.list[i] : 0;
+        __syncthreads();
+        uint32_t below = 0;
+        for (unsigned j = slice; j < n; j += slices) below += sh.list[j] < mine;
+        if (i < n && below != 0) atomicAdd(&sh.ranks[i], below);
+        __syncthreads();
+        if (threadIdx.x < n) sh.list[sh.ranks[i]] = mine;
+        __syncthreads();
+        return;
+    }
+    unsigned lg = 10;
+    while ((1u << lg) < n) ++lg;
+    const unsigned size = 1u << lg;
     for (unsigned i = n + threadIdx.x; i < size; i += kThreads) sh.list[i] = ~0ull;
-    for (unsigned k = 2; k <= size; k *= 2)
-        for (unsigned j = k / 2; j > 0; j /= 2) {
-            __syncthreads();
-            const unsigned a = (threadIdx.x / j) * 2 * j + threadIdx.x % j, b = a + j;
+    for (unsigned lk = 1; lk <= lg; ++lk)
+        for (unsigned lj = lk; lj-- > 0;) {
+            // up to a distance of 64 a wavefront stays within its own 128 places
+            if (lk == 1 || lj > 6 || (lj == 6 && lk > 7)) __syncthreads();
+            else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const unsigned a = (threadIdx.x >> lj) << (lj + 1) | (threadIdx.x & ((1u << lj) - 1)), b = a | 1u << lj;
             if (b < size) {
                 const u64 x = sh.list[a], y = sh.list[b];
-                if ((x > y) == ((a & k) == 0)) {
+                if ((x > y) == ((a >> lk & 1u) == 0)) {
                     sh.list[a] = y;
                     sh.list[b] = x;
                 }
@@ -255,55 +328,98 @@ __device__ __forceinline__ void sort_list(Shared &sh, unsigned n)
     __syncthreads();
 }
 
-// The first token by rank of a source, and the smallest logit that is not masked, as its key.
-template <class SOURCE>
-__device__ __forceinline__ void ends_of(SOURCE &source, Shared &sh, u64 &best, uint32_t &low)
+// What a source's logits tell before any weight: the largest, the smallest that is not masked (infinity if all are), and whether there is a NaN.
+struct Ends {
+    float top, low;
+    bool strange;
+    __device__ __forceinline__ void meet(float t, float l, bool s)
+    {
+        top = t > top ? t : top;
+        low = l < low ? l : low;
+        strange = strange || s;
+    }
+    // A row without a token to choose from.
+    __device__ __forceinline__ bool empty() const { return strange || top == -INFINITY; }
+};
+constexpr Ends kNoEnds{-INFINITY, INFINITY, false};
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void meet_moved(Ends &e)     // lanes that none moves to meet themselves
 {
-    best = ~0ull;
-    low = kNan;
-    source.each([&](float z, unsigned i) {
-        const uint32_t k = key_of(z);
-        const u64 p = place_of(k, i);
-        best = p < best ? p : best;
-        if (k > kNothing) low = k < low ? k : low;
-    });
-    auto meet = [&](int lanes) {
-        for (int step = 1; step < lanes; step *= 2) {
-            const u64 p = __shfl_xor(best, step);
-            const uint32_t k = (uint32_t)__shfl_xor((int)low, step);
-            best = p < best ? p : best;
-            low = k < low ? k : low;
-        }
+    auto other = [](float v) {
+        const int u = (int)__float_as_uint(v);
+        return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(u, u, CTRL, ROWS, 0xF, false));
     };
-    meet(64);
+    e.meet(other(e.top), other(e.low), false);
+}
+// Of all lanes of a wavefront, in all of them.
+__device__ __forceinline__ Ends met(Ends e)
+{
+    meet_moved<0x111, 0xF>(e);
+    meet_moved<0x112, 0xF>(e);
+    meet_moved<0x114, 0xF>(e);
+    meet_moved<0x118, 0xF>(e);
+    meet_moved<0x142, 0xA>(e);
+    meet_moved<0x143, 0xC>(e);
+    auto last = [](float v) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63)); };
+    return Ends{last(e.top), last(e.low), __any(e.strange) != 0};
+}
+
+template <class SOURCE>
+__device__ __forceinline__ Ends ends_of(SOURCE &source, Shared &sh)
+{
+    Ends e = kNoEnds;
+    source.each([&](float z, unsigned) { e.meet(z, z == -INFINITY ? INFINITY : z, z != z); });
+    e = met(e);
     if (threadIdx.x % 64 == 0) {
-        sh.best[threadIdx.x / 64] = best;
-        sh.low[threadIdx.x / 64] = low;
+        sh.top[threadIdx.x / 64] = e.top;
+        sh.low[threadIdx.x / 64] = e.low;
+        sh.strange[threadIdx.x / 64] = e.strange;
     }
     __syncthreads();
-    best = sh.best[threadIdx.x % (kThreads / 64)];
-    low = sh.low[threadIdx.x % (kThreads / 64)];
-    meet(kThreads / 64);
+    const unsigned part = threadIdx.x % kWaves;
+    return met(Ends{sh.top[part], sh.low[part], sh.strange[part] != 0});
+}
+
+// The lowest index of a logit equal to `top`, or what is above all indices.
+template <class SOURCE>
+__device__ __forceinline__ uint32_t first_of(SOURCE &source, float top, Shared &sh)
+{
+    uint32_t first = ~0u;
+    source.each([&](float z, unsigned i) {
+        if (z == top && i < first) first = i;
+    });
+    for (int step = 1; step < 64; step *= 2) {
+        const uint32_t other = (uint32_t)__shfl_xor((int)first, step);
+        first = other < first ? other : first;
+    }
+    if (threadIdx.x % 64 == 0) sh.first[threadIdx.x / 64] = first;
+    __syncthreads();
+    first = sh.first[0];
+    for (unsigned i = 1; i < kWaves; ++i) first = sh.first[i] < first ? sh.first[i] : first;
+    return first;
 }
 
 // ------------------------------------------------------------------------------------ weights and bins
 // Depth: how far a logit is below the largest, as the power of two that its weight is below 1.
 struct Weights {
     float top;
+    bool infinite;      // the largest logit is: only its like have a weight
     double scale;
     unsigned shift;     // kSteps less the log2 of the bins to a factor of two
 
-    __device__ __forceinline__ Weights(uint32_t top_key, uint32_t low_key, double scale) : top(uniform(value_of_key(top_key))), scale(scale)
+    __device__ __forceinline__ Weights(const Ends &e, double scale) : top(e.top), infinite(e.top == INFINITY), scale(scale)
     {
-        const double down = ((double)top - (double)value_of_key(low_key)) * scale, range = down < kFar ? down : kFar;
+        const double down = ((double)e.top - (double)e.low) * scale, range = down < kFar ? down : kFar;
         unsigned by = 0;    // kBins = 8 << kSteps
         while (by < 4 && range > (double)(7u << by)) ++by;
         shift = uniform(by);
     }
+    // Not below kFar, or a NaN: no weight.
     __device__ __forceinline__ double depth_of(float z) const
     {
-        const double d = z == top ? 0.0 : ((double)top - (double)z) * scale;
-        return d < kFar ? d : (double)INFINITY;     // also a NaN, of -infinity at an infinite temperature
+        if (infinite) return z == top ? 0.0 : (double)INFINITY;
+        return ((double)top - (double)z) * scale;
     }
     // A depth below kFar in steps of 2^-kSteps, and the weight as a part of the power of two above it: 2^-(steps % 128 / 128) 2^-r, |r| <= 2^-8, by a table and
     // four terms of the exponential series (the fifth is below 2e-15).
@@ -335,9 +451,16 @@ struct Weights {
 
 constexpr u64 kOneToken = 1ull << 48, kMassBits = kOneToken - 1;
 
+// By the bits of j: 2^(-1/128), 2^(-1/64) and so on.
 __device__ __forceinline__ void fill_powers(Shared &sh)
 {
-    if (threadIdx.x < 1u << kSteps) sh.power[threadIdx.x] = exp2(-(double)threadIdx.x / (1u << kSteps));
+    constexpr double kPowers[kSteps] = {0.99459942348363317565, 0.98922801319397548413, 0.97857206208770013453, 0.95760328069857364694,
+                                        0.91700404320467123174, 0.84089641525371454303, 0.70710678118654752440};
+    if (threadIdx.x >= 1u << kSteps) return;
+    double v = 1.0;
+#pragma unroll
+    for (unsigned i = 0; i < kSteps; ++i) v *= threadIdx.x >> i & 1u ? kPowers[i] : 1.0;
+    sh.power[threadIdx.x] = v;
 }
 
 // A token's count and mass for its bin.
@@ -346,11 +469,34 @@ __device__ __forceinline__ u64 packed(double part)
     return ((u64)__double_as_longlong(__builtin_fma(part, 0x1p32, 0x1p52)) & 0xFFFFFFFFFFFFFull) | kOneToken;     // part <= 1.003
 }
 
-// Bins of a source of at most kChunk logits into sh.bins; how many tokens min-p keeps.
+// Where top-k leaves few tokens, the ones that may be among them: by counts alone, which cost less than weights.
 template <class SOURCE>
-__device__ __forceinline__ uint32_t fill_bins(SOURCE &source, const Weights &w, double reach, Shared &sh)
+__device__ __forceinline__ Near nearest(SOURCE &source, const Ends &e, uint32_t k, Shared &sh)
+{
+    const float width = e.top - e.low;
+    if (!(width > 0.f && width < 3e38f)) return kAll;     // all alike, or an infinity
+    const float by = (float)(kBins - 1) / width;
+    sh.count[threadIdx.x] = 0;
+    __syncthreads();
+    source.each([&](float z, unsigned) {
+        const float d = (e.top - z) * by;
+        if (d < (float)kBins) atomicAdd(&sh.count[(unsigned)d], 1u);
+    });
+    __syncthreads();
+    const uint32_t upto = sum_up_to(Mass{sh.count[threadIdx.x], 0.0}, sh).count;
+    __syncthreads();
+    sh.count[threadIdx.x] = upto;
+    __syncthreads();
+    const unsigned last = first_where(kBins, [&](unsigned i) { return sh.count[i] >= k; });
+    return Near{e.top, by, (float)(last + 1)};      // bins 0 .. last; all if the tokens are fewer than k
+}
+
+// Bins of a source of at most 32768 logits into sh.bins, and how many tokens min-p keeps into sh.by_min.
+template <class SOURCE>
+__device__ __forceinline__ void fill_bins(SOURCE &source, const Weights &w, double reach, Shared &sh)
 {
     sh.bins[threadIdx.x] = 0;
+    if (threadIdx.x == 0) sh.by_min = 0;
     fill_powers(sh);
     __syncthreads();
     uint32_t kept = 0;
@@ -362,18 +508,19 @@ __device__ __forceinline__ uint32_t fill_bins(SOURCE &source, const Weights &w, 
         atomicAdd(&sh.bins[w.bin_of(steps)], packed(part));
         kept += depth <= reach;
     });
-    Mass total;
-    sum_up_to(Mass{kept, 0.0}, sh, total);
-    return uniform(total.count);
+    const Mass all = scanned(Mass{kept, 0.0});
+    if (threadIdx.x % 64 == 63) atomicAdd(&sh.by_min, all.count);
+    __syncthreads();
 }
 
-// Tokens of the flagged bins into sh.list, unsorted.
+// Tokens of the flagged bins, all of whose logits are between `low` and `high`, into sh.list, unsorted.
 template <class SOURCE>
-__device__ __forceinline__ void list_flagged(SOURCE &source, const Weights &w, Shared &sh)
+__device__ __forceinline__ void list_flagged(SOURCE &source, const Weights &w, float low, float high, Shared &sh)
 {
     if (threadIdx.x == 0) sh.listed = 0;
     __syncthreads();
     source.each([&](float z, unsigned i) {
+        if (!(z >= low && z <= high)) return;
         const double depth = w.depth_of(z);
         if (!(depth < kFar)) return;
         const unsigned b = w.bin_of(w.steps_of(depth));
@@ -390,7 +537,7 @@ struct Question {
     uint32_t count;
     double mass;
     bool above;     // more than the mass, not as much
-    __device__ __forceinline__ bool reached(Mass m) const { return m.count >= count || (above ? m.mass > mass : m.mass >= mass); }
+    __device__ __forceinline__ bool reached(uint32_t c, double m) const { return c >= count || (above ? m > mass : m >= mass); }
 };
 
 struct Bin {
@@ -403,113 +550,120 @@ struct Questions {
     const Settings &s;
     Shared &sh;
     Mass total;
+    uint32_t by_min;
+    float low_logit, high_logit;    // of the tokens that the plan lists
 
-    __device__ __forceinline__ Questions(const Weights &w, const Settings &s, Shared &sh, uint32_t count, u64 mass) : w(w), s(s), sh(sh)
+    __device__ __forceinline__ Questions(const Weights &w, const Settings &s, Shared &sh, uint32_t by_min) : w(w), s(s), sh(sh), by_min(by_min) {}
+
+    // Sums of the bins, of which a lane has one.
+    __device__ __forceinline__ void add_up(uint32_t count, u64 mass)
     {
-        const Mass own{count, (double)mass * w.unit_of(threadIdx.x)};
-        sh.own[threadIdx.x] = own;
-        sh.upto[threadIdx.x] = sum_up_to(own, sh, total);
-        total = Mass{uniform(total.count), uniform(total.mass)};
+        const Mass upto = sum_up_to(Mass{count, (double)mass * w.unit_of(threadIdx.x)}, sh);
+        sh.count[threadIdx.x] = upto.count;
+        sh.mass[threadIdx.x] = upto.mass;
+        __syncthreads();
+        total = uniform(Mass{sh.count[kBins - 1], sh.mass[kBins - 1]});
     }
 
-    // The first bin with tokens at whose end `q` is reached, or the last with tokens.
-    __device__ __forceinline__ Bin find(const Question &q, Mass own, Mass upto, uint32_t last)
+    // The first of bins with tokens, by their sums, at whose end `q` is reached.  The last such bin is if no other.
+    __device__ __forceinline__ Bin find(Question q, const uint32_t *count, const double *mass) const
     {
-        __syncthreads();
-        if (threadIdx.x == 0) sh.found = kBins;
-        __syncthreads();
-        if (own.count != 0 && (upto.count == last || q.reached(upto))) atomicMin(&sh.found, threadIdx.x);
-        __syncthreads();
-        const unsigned at = sh.found;
-        if (threadIdx.x == at) {
-            sh.before = Mass{upto.count - own.count, upto.mass - own.mass};
-            sh.at = upto;
-        }
-        __syncthreads();
-        return Bin{uniform(at), {uniform(sh.before.count), uniform(sh.before.mass)}, {uniform(sh.at.count), uniform(sh.at.mass)}};
+        const uint32_t all = count[kBins - 1];
+        if (q.count > all) q.count = all;
+        unsigned at = first_where(kBins, [&](unsigned i) { return q.reached(count[i], mass[i]); });
+        if (count[at] == (at != 0 ? count[at - 1] : 0u))    // an empty one, where sums differ by a rounding
+            at = first_where(kBins, [&](unsigned i) { return count[i] > count[at]; });
+        const Mass before = at != 0 ? Mass{count[at - 1], mass[at - 1]} : Mass{0, 0.0};
+        return Bin{uniform(at), uniform(before), uniform(Mass{count[at], mass[at]})};
     }
-    __device__ __forceinline__ Bin find(const Question &q) { return find(q, sh.own[threadIdx.x], sh.upto[threadIdx.x], total.count); }
+    __device__ __forceinline__ Bin find(const Question &q) const { return find(q, sh.count, sh.mass); }
 
     __device__ __forceinline__ bool flagged(unsigned bin) const { return (sh.flags[bin / 32] >> (bin % 32) & 1u) != 0; }
 
-    // Flags bins lo .. hi, and says where each flagged bin starts in the list; how many tokens are flagged.
-    __device__ __forceinline__ uint32_t flag(unsigned lo, unsigned hi, bool more)
+    // Flags this lane's bin or not, and says where each flagged bin starts in the list.
+    __device__ __forceinline__ void flag(bool mine)
     {
-        const bool mine = (threadIdx.x >= lo && threadIdx.x <= hi) || (more && flagged(threadIdx.x));
         const u64 wave = __ballot(mine);
-        __syncthreads();
         if (threadIdx.x % 32 == 0) sh.flags[threadIdx.x / 32] = (uint32_t)(wave >> (threadIdx.x % 64));
-        Mass all;
-        const uint32_t count = mine ? sh.own[threadIdx.x].count : 0u;
-        const Mass end = sum_up_to(Mass{count, 0.0}, sh, all);
-        sh.starts[threadIdx.x] = end.count - count;
+        const uint32_t count = mine ? sh.count[threadIdx.x] - (threadIdx.x != 0 ? sh.count[threadIdx.x - 1] : 0u) : 0u;
+        sh.starts[threadIdx.x] = sum_up_to(Mass{count, 0.0}, sh).count - count;
         __syncthreads();
-        return uniform(all.count);
     }
 
-    // Flags the bins that, as far as the bins tell, hold the answers: all up to the last of them where these are few tokens.
-    __device__ __forceinline__ void plan(uint32_t by_min)
+    // Flags the bins that hold the answers as far as the sums of bins tell: what one question leaves open between the ends of its bin is carried to the
+    // next, from `low` to `high`.  The first wavefront's work.
+    __device__ __forceinline__ void plan()
     {
-        uint32_t listed = flag(1, 0, false);
-        Mass low = total, high = total;     // what is kept, at the least and at the most
-        auto add = [&](const Bin &b) {
-            if (b.with.count <= kListed) {
-                flag(0, b.at, false);
-                return true;
-            }
-            const uint32_t tokens = b.with.count - b.before.count;
-            if (!flagged(b.at) && listed + tokens <= kListed) listed = flag(b.at, b.at, true);
-            if (b.before.count < low.count) low = b.before;
-            if (b.with.count < high.count) high = b.with;
-            return false;
-        };
-        if (s.top_k < total.count && add(find(Question{s.top_k, (double)INFINITY, false}))) return;
-        if (s.top_p < 1.0) {
-            const double most = s.top_p * high.mass, least = s.top_p * low.mass;
-            if (add(find(Question{high.count, most, false}))) return;
-            if (least < most && add(find(Question{high.count, least, false}))) return;
+        if (threadIdx.x < 64) {
+            uint32_t listed = 0;
+            Mass low = total, high = total;
+            unsigned asked = 0;
+            auto add = [&](const Question &least, const Question &most) {
+                const Bin to = find(most), from = least.count == most.count && least.mass == most.mass ? to : find(least);
+                low = from.before;
+                high = to.with;
+                const uint32_t tokens = high.count - low.count;
+                const bool fits = listed + tokens <= kListed;
+                if (fits) listed += tokens;
+                if (threadIdx.x == 0) {
+                    sh.from[asked] = fits ? from.at : kBins;
+                    sh.to[asked] = to.at;
+                }
+                ++asked;
+            };
+            constexpr double kAny = (double)INFINITY;
+            auto some = [](uint32_t count) { return count != 0 ? count : 1u; };
+            if (s.top_k < total.count) add(Question{s.top_k, kAny, false}, Question{s.top_k, kAny, false});
+            if (s.top_p < 1.0) add(Question{some(low.count), s.top_p * low.mass, false}, Question{high.count, s.top_p * high.mass, false});
+            if (by_min < high.count) add(Question{by_min < low.count ? by_min : some(low.count), kAny, false}, Question{by_min, kAny, false});
+            add(Question{some(low.count), s.u * low.mass, true}, Question{high.count, s.u * high.mass, true});
+            for (; asked < 4; ++asked)
+                if (threadIdx.x == 0) sh.from[asked] = kBins;
         }
-        if (by_min < high.count && add(find(Question{by_min, (double)INFINITY, false}))) return;
-        const Bin first = find(Question{high.count, s.u * low.mass, true}), last = find(Question{high.count, s.u * high.mass, true});
-        if (last.with.count <= kListed) {
-            flag(0, last.at, false);
-            return;
+        __syncthreads();
+        bool mine = false;
+        unsigned first = kBins, last = 0;
+        for (unsigned i = 0; i < 4; ++i) {
+            const unsigned from = sh.from[i], to = sh.to[i];
+            mine = mine || (threadIdx.x >= from && threadIdx.x <= to);
+            if (from >= kBins) continue;
+            first = from < first ? from : first;
+            last = to > last ? to : last;
         }
-        if (listed + last.with.count - first.before.count <= kListed) flag(first.at, last.at, true);
+        flag(mine);
+        // logits of bins `first` to `last`, and of one more on either side
+        const double step = 1.0 / ((double)(1u << (kSteps - w.shift)) * w.scale);
+        high_logit = (float)((double)w.top - ((double)first - 1.0) * step);
+        low_logit = last < kBins - 2 ? (float)((double)w.top - ((double)last + 2.0) * step) : -INFINITY;
+        if (w.infinite || !(step < 1e30)) {
+            high_logit = INFINITY;
+            low_logit = -INFINITY;
+        }
+        high_logit = uniform(high_logit);
+        low_logit = uniform(low_logit);
     }
 
-    // Of n listed tokens from `start` on, before which `before` ranks: the first with which `q` is reached (the last if it never is), and what is
-    // kept with it.
-    __device__ __forceinline__ unsigned find_listed(const Question &q, unsigned start, unsigned n, Mass before, Mass &kept)
+    // Sorts n listed tokens and sums their weights.
+    __device__ __forceinline__ void finish_list(unsigned n)
     {
+        sort_list(sh, n);
         const unsigned i = threadIdx.x * 2;
-        auto weight = [&](unsigned at) { return at < n ? w.weight_of(value_of_key(~(uint32_t)(sh.list[start + at] >> 32)), sh.power) : 0.0; };
+        auto weight = [&](unsigned at) { return at < n ? w.weight_of(value_of_key(~(uint32_t)(sh.list[at] >> 32)), sh.power) : 0.0; };
         const double w0 = weight(i), w1 = weight(i + 1);
-        Mass all;
-        const Mass m1 = before + sum_up_to(Mass{(i < n ? 1u : 0u) + (i + 1 < n ? 1u : 0u), w0 + w1}, sh, all);
-        const Mass m0{m1.count - (i + 1 < n ? 1u : 0u), m1.mass - w1};
+        const double upto = sum_up_to(Mass{0, w0 + w1}, sh).mass;
+        sh.list_mass[i] = upto - w1;
+        sh.list_mass[i + 1] = upto;
         __syncthreads();
-        if (threadIdx.x == 0) sh.found = n - 1;
-        __syncthreads();
-        if (i < n && q.reached(m0)) atomicMin(&sh.found, i);
-        else if (i + 1 < n && q.reached(m1)) atomicMin(&sh.found, i + 1);
-        __syncthreads();
-        const unsigned at = sh.found;
-        if (i == at) sh.at = m0;
-        else if (i + 1 == at) sh.at = m1;
-        __syncthreads();
-        kept = Mass{uniform(sh.at.count), uniform(sh.at.mass)};
-        return start + at;
     }
 
-    // Lists the tokens of a bin of more than kListed that are near the answer: bins of places inside it, until they are few.
+    // Lists the tokens of a bin of more than kListed that are near the answer: bins of places inside it, until they are few.  `before` moves up to them.
     template <class SOURCE>
-    __device__ __forceinline__ unsigned narrow(const SOURCE &source, const Question &q, unsigned bin, Mass &before)
+    __device__ __forceinline__ unsigned narrow(SOURCE &source, const Question &q, unsigned bin, Mass &before)
     {
         auto each = [&](auto f) {
             source.each([&](float z, unsigned i) {
                 const double depth = w.depth_of(z);
-                if (depth < kFar && w.bin_of(w.steps_of(depth)) == bin) f(z, depth, place_of(key_of(z), i));
+                if (depth < kFar && w.bin_of(w.steps_of(depth)) == bin) f(depth, place_of(key_of(z), i));
             });
         };
         __syncthreads();
@@ -518,20 +672,21 @@ struct Questions {
             sh.high_place = 0;
         }
         __syncthreads();
-        each([&](float, double, u64 p) {
+        each([&](double, u64 p) {
             atomicMin(&sh.low_place, p);
             atomicMax(&sh.high_place, p);
         });
         __syncthreads();
         u64 first = sh.low_place, last = sh.high_place;
+        uint32_t *const count = reinterpret_cast<uint32_t *>(sh.list);      // sums of the bins of places
+        double *const mass = sh.list_mass;
         for (;;) {
-            // counts and masses apart: a bin may hold more tokens than a chunk
             const u64 step = (last - first) / kBins + 1;
             __syncthreads();
-            sh.bins[threadIdx.x] = 0;
+            sh.bins[threadIdx.x] = 0;       // counts and masses apart: a bin may hold more tokens than a chunk
             sh.starts[threadIdx.x] = 0;
             __syncthreads();
-            each([&](float, double depth, u64 p) {
+            each([&](double depth, u64 p) {
                 if (p < first || p > last) return;
                 unsigned steps;
                 const unsigned b = (unsigned)((p - first) / step);
@@ -539,82 +694,112 @@ struct Questions {
                 atomicAdd(&sh.starts[b], 1u);
             });
             __syncthreads();
-            const Mass mine{sh.starts[threadIdx.x], (double)sh.bins[threadIdx.x] * w.unit_of(bin)};
-            Mass all;
-            const Mass end = before + sum_up_to(mine, sh, all);
-            const Bin b = find(q, mine, end, before.count + all.count);
-            before = b.before;
+            const Mass upto = before + sum_up_to(Mass{sh.starts[threadIdx.x], (double)sh.bins[threadIdx.x] * w.unit_of(bin)}, sh);
+            count[threadIdx.x] = upto.count - before.count;
+            mass[threadIdx.x] = upto.mass;
+            __syncthreads();
+            Question here = q;
+            here.count = q.count > before.count ? q.count - before.count : 1u;
+            const Bin b = find(here, count, mass);
+            if (b.at != 0) before = Mass{before.count + b.before.count, b.before.mass};
             first += b.at * step;
             if (last - first >= step) last = first + step - 1;
             if (b.with.count - b.before.count <= kListed) break;    // a step of 1 holds one token
         }
+        __syncthreads();
         if (threadIdx.x == 0) sh.listed = 0;
         __syncthreads();
-        each([&](float, double, u64 p) {
+        each([&](double, u64 p) {
             if (p < first || p > last) return;
             const unsigned at = atomicAdd(&sh.listed, 1u);
             if (at < kListed) sh.list[at] = p;
         });
         __syncthreads();
-        sort_list(sh, sh.listed);
-        return sh.listed;
+        return uniform(sh.listed);
     }
 
-    // The answer: its index in the list, and what is kept with it.
-    template <class SOURCE>
-    __device__ __forceinline__ unsigned ask(const SOURCE &source, const Question &q, Mass &kept)
+    // Top-k, top-p, min-p, the choice; whether it is asked at all.
+    __device__ __forceinline__ bool question(unsigned turn, const Mass &kept, Question &q) const
     {
-        const Bin b = find(q);
-        Mass before = b.before;
-        unsigned start = 0, n = b.with.count - b.before.count;
-        if (flagged(b.at)) {
-            start = sh.starts[b.at];
-        } else if (n <= kListed) {
-            flag(b.at, b.at, false);
-            list_flagged(source, w, sh);
-            sort_list(sh, n);
-        } else {
-            n = narrow(source, q, b.at, before);
-            flag(1, 0, false);
+        q = Question{kept.count, (double)INFINITY, turn == 3};
+        if (turn == 0) {
+            q.count = s.top_k;
+            return s.top_k < kept.count;
         }
-        return find_listed(q, start, n, before, kept);
+        if (turn == 1) {
+            q.mass = s.top_p * kept.mass;
+            return s.top_p < 1.0;
+        }
+        if (turn == 2) {
+            q.count = by_min;
+            return by_min < kept.count;
+        }
+        q.mass = s.u * kept.mass;
+        return true;
     }
 
-    // The token, where the tokens of the flagged bins are listed and sorted.
+    // The token (in the first wavefront, which asks the questions), where the tokens of the flagged bins are listed and sorted.  All lanes list others
+    // where a question needs them.
     template <class SOURCE>
-    __device__ __forceinline__ long long choose(const SOURCE &source, uint32_t by_min)
+    __device__ __forceinline__ long long choose(SOURCE &source)
     {
-        Mass kept = total;
-        unsigned at = 0;
-#pragma unroll 1
-        for (unsigned turn = 0; turn < 4; ++turn) {     // top-k, top-p, min-p, the choice
-            Question q{kept.count, (double)INFINITY, turn == 3};
-            bool needed = true;
-            if (turn == 0) {
-                needed = s.top_k < kept.count;
-                q.count = s.top_k;
-            } else if (turn == 1) {
-                needed = s.top_p < 1.0;
-                q.mass = s.top_p * kept.mass;
-            } else if (turn == 2) {
-                needed = by_min < kept.count;
-                q.count = by_min;
-            } else {
-                q.mass = s.u * kept.mass;
+        Mass kept = total, before{0, 0.0};
+        unsigned turn = 0, at = 0, n = 0;
+        bool relisted = false;      // for the question that is asked next, n tokens behind `before`
+        for (;;) {
+            if (threadIdx.x < 64) {
+                bool open = false;
+                for (; turn < 4 && !open; ) {
+                    Question q;
+                    if (question(turn, kept, q)) {
+                        unsigned start = 0;
+                        if (!relisted) {
+                            const Bin b = find(q);
+                            before = b.before;
+                            n = b.with.count - b.before.count;
+                            open = !flagged(b.at);
+                            if (!open) {
+                                start = uniform(sh.starts[b.at]);
+                            } else if (threadIdx.x == 0) {
+                                sh.asked_bin = b.at;
+                                sh.asked_count = q.count;
+                                sh.asked_above = q.above;
+                                sh.asked_mass = q.mass;
+                                sh.asked_before = b.before;
+                                sh.asked_with = b.with;
+                            }
+                        }
+                        if (!open) {
+                            const double base = before.mass - (start != 0 ? sh.list_mass[start - 1] : 0.0);
+                            const unsigned i = first_where(n, [&](unsigned i) { return q.reached(before.count + i + 1, base + sh.list_mass[start + i]); });
+                            at = uniform(start + (i < n ? i : n - 1));
+                            kept = uniform(Mass{before.count + at - start + 1, base + sh.list_mass[at]});
+                            relisted = false;
+                        }
+                    }
+                    if (!open) ++turn;
+                }
+                if (threadIdx.x == 0) sh.asked = open;
             }
-            if (needed) at = ask(source, q, kept);
+            __syncthreads();
+            if (uniform(sh.asked) == 0) break;
+            const unsigned bin = uniform(sh.asked_bin);
+            before = uniform(sh.asked_before);
+            n = uniform(sh.asked_with.count) - before.count;
+            __syncthreads();
+            if (n <= kListed) {
+                flag(threadIdx.x == bin);
+                list_flagged(source, w, -INFINITY, INFINITY, sh);
+            } else {
+                n = narrow(source, Question{uniform(sh.asked_count), uniform(sh.asked_mass), sh.asked_above != 0}, bin, before);
+                flag(false);
+            }
+            finish_list(n);
+            relisted = true;
         }
         return (long long)(uint32_t)sh.list[at];
     }
 };
-
-// A row's token where it takes no weights: none in a row with a NaN or without tokens, or the first by rank.
-__device__ __forceinline__ bool is_simple(u64 best, const Settings &s, long long &token)
-{
-    const uint32_t key = ~(uint32_t)(best >> 32);
-    token = key == kNan || key <= kNothing ? -1 : (long long)(uint32_t)best;
-    return token < 0 || s.greedy;
-}
 
 // ------------------------------------------------------------------------------------ kernels
 // A row to a block.
@@ -625,120 +810,117 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, KtLutPac
     const LaneTable tab(pack);
     const Settings s = settings_of(a, blockIdx.x);
     Held<ELEM, CAP, WIDE, E> held(static_cast<const ELEM *>(a.logits) + blockIdx.x * a.row, 0, a.vocabulary, a.cap, tab);
-    u64 best;
-    uint32_t low;
-    ends_of(held, sh, best, low);
-    long long token;
-    if (!is_simple(best, s, token)) {
-        const Weights w(~(uint32_t)(best >> 32), low, s.scale);
-        const uint32_t by_min = fill_bins(held, w, s.reach, sh);
-        const u64 mine = sh.bins[threadIdx.x];
-        Questions questions(w, s, sh, (uint32_t)(mine >> 48), mine & kMassBits);
-        questions.plan(by_min);
-        list_flagged(held, w, sh);
-        sort_list(sh, sh.listed);
-        // another list than the plan's, if one is needed, comes from memory: the registers are the questions'
-        const Read<ELEM, CAP, WIDE> read{static_cast<const ELEM *>(a.logits) + blockIdx.x * a.row, a.vocabulary, a.cap, tab};
-        token = questions.choose(read, by_min);
+    const Ends e = ends_of(held, sh);
+    long long token = -1;
+    if (!e.empty()) {
+        if (s.greedy) {
+            token = first_of(held, e.top, sh);
+        } else {
+            const Weights w(e, s.scale);
+            Near near = kAll;
+            if (s.top_k <= kListed && s.top_k < a.vocabulary) near = nearest(held, e, s.top_k, sh);
+            if (!near.all()) held.keep(near);
+            fill_bins(held, w, s.reach, sh);
+            Questions questions(w, s, sh, uniform(sh.by_min));
+            questions.add_up((uint32_t)(sh.bins[threadIdx.x] >> 48), sh.bins[threadIdx.x] & kMassBits);
+            questions.plan();
+            list_flagged(held, w, questions.low_logit, questions.high_logit, sh);
+            questions.finish_list(uniform(sh.listed));
+            // another list than the plan's, if one is needed, comes from memory: the registers are the questions'
+            Read<ELEM, CAP, WIDE> read{static_cast<const ELEM *>(a.logits) + blockIdx.x * a.row, a.vocabulary, a.cap, tab, near};
+            token = questions.choose(read);
+        }
     }
     if (threadIdx.x == 0) a.tokens[blockIdx.x] = token;
 }
 
-// Rows in chunks.  Blocks have a chunk each but for the last launch.
+// Rows in chunks of E logits a lane.  Blocks have a chunk each but for the last launch.
 struct Where {
     unsigned row, first, end;
 };
+template <unsigned E>
 __device__ __forceinline__ Where chunk_of(const SampleArgs &a)
 {
+    constexpr unsigned kChunk = E * kThreads;
     const unsigned row = blockIdx.x / a.chunks, first = blockIdx.x % a.chunks * kChunk;
     return Where{row, first, a.vocabulary - first < kChunk ? a.vocabulary : first + kChunk};
 }
 
 // The row's ends from those of its chunks.
-__device__ __forceinline__ void row_ends(const SampleArgs &a, unsigned row, u64 &best, uint32_t &low)
+__device__ __forceinline__ Ends row_ends(const SampleArgs &a, unsigned row)
 {
-    best = ~0ull;
-    low = kNan;
+    Ends e = kNoEnds;
     for (unsigned c = 0; c < a.chunks; ++c) {
-        const u64 p = a.best[row * (u64)a.chunks + c];
-        const uint32_t k = a.low[row * (u64)a.chunks + c];
-        best = p < best ? p : best;
-        low = k < low ? k : low;
+        const float4 v = a.ends[row * (u64)a.chunks + c];
+        e.meet(v.x, v.y, v.z != 0.f);
     }
+    return e;
 }
 
-// This lane's bin of the row.
-__device__ __forceinline__ Questions row_questions(const SampleArgs &a, unsigned row, const Weights &w, const Settings &s, Shared &sh, uint32_t &by_min)
+// The row's bins added up from those of its chunks, and the plan.
+__device__ __forceinline__ void add_up_row(const SampleArgs &a, unsigned row, Questions &questions)
 {
-    uint32_t count = 0;
+    uint32_t count = 0, by_min = 0;
     u64 mass = 0;
-    by_min = 0;
     for (unsigned c = 0; c < a.chunks; ++c) {
         const u64 at = row * (u64)a.chunks + c, v = a.bins[at * kBins + threadIdx.x];
         count += (uint32_t)(v >> 48);
         mass += v & kMassBits;
         by_min += a.by_min[at];
     }
-    return Questions(w, s, sh, count, mass);
+    questions.by_min = by_min;
+    questions.add_up(count, mass);
+    questions.plan();
 }
 
-template <class ELEM, bool CAP, bool WIDE>
+template <class ELEM, bool CAP, bool WIDE, unsigned E>
 __global__ __launch_bounds__(kThreads) void sample_ends_kernel(SampleArgs a, KtLutPack pack)
 {
     __shared__ Shared sh;
     const LaneTable tab(pack);
-    const Where at = chunk_of(a);
-    Held<ELEM, CAP, WIDE, 32> held(static_cast<const ELEM *>(a.logits) + at.row * a.row, at.first, at.end, a.cap, tab);
-    u64 best;
-    uint32_t low;
-    ends_of(held, sh, best, low);
+    const Where at = chunk_of<E>(a);
+    Held<ELEM, CAP, WIDE, E> held(static_cast<const ELEM *>(a.logits) + at.row * a.row, at.first, at.end, a.cap, tab);
+    const Ends e = ends_of(held, sh);
+    const uint32_t first = settings_of(a, at.row).greedy ? first_of(held, e.top, sh) : 0u;
     if (threadIdx.x == 0) {
-        a.best[blockIdx.x] = best;
-        a.low[blockIdx.x] = low;
+        a.ends[blockIdx.x] = float4{e.top, e.low, e.strange ? 1.f : 0.f, __uint_as_float(first)};
         if (at.first == 0) a.listed[at.row] = 0;
     }
 }
 
-template <class ELEM, bool CAP, bool WIDE>
+template <class ELEM, bool CAP, bool WIDE, unsigned E>
 __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a, KtLutPack pack)
 {
     __shared__ Shared sh;
     const LaneTable tab(pack);
-    const Where at = chunk_of(a);
+    const Where at = chunk_of<E>(a);
     const Settings s = settings_of(a, at.row);
-    u64 best;
-    uint32_t low;
-    row_ends(a, at.row, best, low);
-    long long token;
-    if (is_simple(best, s, token)) return;
-    Held<ELEM, CAP, WIDE, 32> held(static_cast<const ELEM *>(a.logits) + at.row * a.row, at.first, at.end, a.cap, tab);
-    const uint32_t by_min = fill_bins(held, Weights(~(uint32_t)(best >> 32), low, s.scale), s.reach, sh);
+    const Ends e = row_ends(a, at.row);
+    if (e.empty() || s.greedy) return;
+    Held<ELEM, CAP, WIDE, E> held(static_cast<const ELEM *>(a.logits) + at.row * a.row, at.first, at.end, a.cap, tab);
+    fill_bins(held, Weights(e, s.scale), s.reach, sh);
     a.bins[blockIdx.x * (u64)kBins + threadIdx.x] = sh.bins[threadIdx.x];
-    if (threadIdx.x == 0) a.by_min[blockIdx.x] = by_min;
+    if (threadIdx.x == 0) a.by_min[blockIdx.x] = sh.by_min;
 }
 
-template <class ELEM, bool CAP, bool WIDE>
+template <class ELEM, bool CAP, bool WIDE, unsigned E>
 __global__ __launch_bounds__(kThreads) void sample_list_kernel(SampleArgs a, KtLutPack pack)
 {
     __shared__ Shared sh;
     const LaneTable tab(pack);
-    const Where at = chunk_of(a);
+    const Where at = chunk_of<E>(a);
     const Settings s = settings_of(a, at.row);
-    u64 best;
-    uint32_t low;
-    row_ends(a, at.row, best, low);
-    long long token;
-    if (is_simple(best, s, token)) return;
-    const Weights w(~(uint32_t)(best >> 32), low, s.scale);
-    uint32_t by_min;
-    Questions questions = row_questions(a, at.row, w, s, sh, by_min);
-    questions.plan(by_min);
-    Held<ELEM, CAP, WIDE, 32> held(static_cast<const ELEM *>(a.logits) + at.row * a.row, at.first, at.end, a.cap, tab);
-    list_flagged(held, w, sh);
+    const Ends e = row_ends(a, at.row);
+    if (e.empty() || s.greedy) return;
+    const Weights w(e, s.scale);
+    Questions questions(w, s, sh, 0);
+    add_up_row(a, at.row, questions);
+    Held<ELEM, CAP, WIDE, E> held(static_cast<const ELEM *>(a.logits) + at.row * a.row, at.first, at.end, a.cap, tab);
+    list_flagged(held, w, questions.low_logit, questions.high_logit, sh);
     const unsigned n = sh.listed;       // at most kListed: the plan's
-    if (threadIdx.x == 0) sh.found = atomicAdd(&a.listed[at.row], n);
+    if (threadIdx.x == 0) sh.by_min = atomicAdd(&a.listed[at.row], n);
     __syncthreads();
-    const unsigned start = sh.found;
+    const unsigned start = sh.by_min;
     for (unsigned i = threadIdx.x; i < n; i += kThreads)
         if (start + i < kListed) a.list[at.row * (u64)kListed + start + i] = sh.list[i];
 }
@@ -750,21 +932,25 @@ __global__ __launch_bounds__(kThreads) void sample_answer_kernel(SampleArgs a, K
     const LaneTable tab(pack);
     const unsigned row = blockIdx.x;
     const Settings s = settings_of(a, row);
-    u64 best;
-    uint32_t low;
-    row_ends(a, row, best, low);
-    long long token;
-    if (!is_simple(best, s, token)) {
-        const Weights w(~(uint32_t)(best >> 32), low, s.scale);
-        fill_powers(sh);
-        uint32_t by_min;
-        Questions questions = row_questions(a, row, w, s, sh, by_min);
-        questions.plan(by_min);
-        const unsigned n = a.listed[row];
-        for (unsigned i = threadIdx.x; i < n && i < kListed; i += kThreads) sh.list[i] = a.list[row * (u64)kListed + i];
-        sort_list(sh, n < kListed ? n : kListed);
-        const Read<ELEM, CAP, WIDE> read{static_cast<const ELEM *>(a.logits) + row * a.row, a.vocabulary, a.cap, tab};
-        token = questions.choose(read, by_min);
+    const Ends e = row_ends(a, row);
+    long long token = -1;
+    if (!e.empty()) {
+        if (s.greedy) {
+            for (unsigned c = a.chunks; c-- > 0;) {     // the first chunk with the largest logit
+                const float4 v = a.ends[row * (u64)a.chunks + c];
+                if (v.x == e.top) token = (long long)__float_as_uint(v.w);
+            }
+        } else {
+            const Weights w(e, s.scale);
+            fill_powers(sh);
+            Questions questions(w, s, sh, 0);
+            add_up_row(a, row, questions);
+            const unsigned listed = a.listed[row], n = listed < kListed ? listed : kListed;
+            for (unsigned i = threadIdx.x; i < n; i += kThreads) sh.list[i] = a.list[row * (u64)kListed + i];
+            questions.finish_list(n);
+            Read<ELEM, CAP, WIDE> read{static_cast<const ELEM *>(a.logits) + row * a.row, a.vocabulary, a.cap, tab, kAll};
+            token = questions.choose(read);
+        }
     }
     if (threadIdx.x == 0) a.tokens[row] = token;
 }
@@ -782,7 +968,18 @@ ktanh_status_t check_shape(const ksample_shape_t *s)
     return KT_OK;
 }
 
-size_t chunks_of(size_t vocabulary) { return (vocabulary + kChunk - 1) / kChunk; }
+// Logits of a lane, and chunks of a row.
+struct Cut {
+    unsigned each;
+    size_t chunks;
+};
+Cut cut_of(size_t rows, size_t vocabulary)
+{
+    auto chunks = [&](unsigned each) { return (vocabulary + each * kThreads - 1) / (each * kThreads); };
+    if (vocabulary <= kFew * kThreads) return Cut{kFew, 1};
+    if (vocabulary <= kMost * kThreads) return Cut{kMost, 1};
+    return rows * chunks(kMost) >= 192 ? Cut{kMost, chunks(kMost)} : Cut{kFew, chunks(kFew)};
+}
 
 template <class Lut>
 ktanh_status_t sample_entry(const ksample_shape_t *s, const void *logits, const float *uniform, const float *temperature, const int32_t *top_k,
@@ -804,7 +1001,8 @@ ktanh_status_t sample_entry(const ksample_shape_t *s, const void *logits, const 
     a.logits = logits;
     a.row = s->rows > 1 ? s->row : 0;
     a.vocabulary = (unsigned)s->vocabulary;
-    a.chunks = (unsigned)chunks_of(s->vocabulary);
+    const Cut cut = cut_of(s->rows, s->vocabulary);
+    a.chunks = (unsigned)cut.chunks;
     a.uniform = uniform;
     a.temperature = temperature;
     a.top_k = top_k;
@@ -816,16 +1014,16 @@ ktanh_status_t sample_entry(const ksample_shape_t *s, const void *logits, const 
     a.one_min_p = (float)s->min_p;
     a.cap = (float)s->cap;
     a.tokens = reinterpret_cast<long long *>(tokens);
-    a.best = a.bins = a.list = nullptr;
-    a.low = a.by_min = a.listed = nullptr;
+    a.bins = a.list = nullptr;
+    a.ends = nullptr;
+    a.by_min = a.listed = nullptr;
     const size_t rows = s->rows, blocks = rows * a.chunks;
     if (a.chunks > 1) {
         if (workspace == nullptr) return KT_ERR_NULL;
         a.bins = static_cast<u64 *>(workspace);
         a.list = a.bins + blocks * kBins;
-        a.best = a.list + rows * kListed;
-        a.low = reinterpret_cast<uint32_t *>(a.best + blocks);
-        a.by_min = a.low + blocks;
+        a.ends = reinterpret_cast<float4 *>(a.list + rows * kListed);
+        a.by_min = reinterpret_cast<uint32_t *>(a.ends + blocks);
         a.listed = a.by_min + blocks;
     }
     if (blocks * kThreads >= (size_t)1 << 32) return KT_ERR_SHAPE;
@@ -833,12 +1031,15 @@ ktanh_status_t sample_entry(const ksample_shape_t *s, const void *logits, const 
     auto of = [&](auto elem, auto capped) {
         typedef decltype(elem) ELEM;
         constexpr bool CAP = decltype(capped)::value, W = CAP && WIDE;
-        if (s->vocabulary <= 8 * kThreads) return launch(sample_kernel<ELEM, CAP, W, 8>, rows);
-        if (a.chunks == 1) return launch(sample_kernel<ELEM, CAP, W, 32>, rows);
-        ktanh_status_t done = launch(sample_ends_kernel<ELEM, CAP, W>, blocks);
-        if (done == KT_OK) done = launch(sample_bins_kernel<ELEM, CAP, W>, blocks);
-        if (done == KT_OK) done = launch(sample_list_kernel<ELEM, CAP, W>, blocks);
-        return done == KT_OK ? launch(sample_answer_kernel<ELEM, CAP, W>, rows) : done;
+        if (a.chunks == 1) return cut.each == kFew ? launch(sample_kernel<ELEM, CAP, W, kFew>, rows) : launch(sample_kernel<ELEM, CAP, W, kMost>, rows);
+        auto chunked = [&](auto each) {
+            constexpr unsigned E = decltype(each)::value;
+            ktanh_status_t done = launch(sample_ends_kernel<ELEM, CAP, W, E>, blocks);
+            if (done == KT_OK) done = launch(sample_bins_kernel<ELEM, CAP, W, E>, blocks);
+            if (done == KT_OK) done = launch(sample_list_kernel<ELEM, CAP, W, E>, blocks);
+            return done == KT_OK ? launch(sample_answer_kernel<ELEM, CAP, W>, rows) : done;
+        };
+        return cut.each == kFew ? chunked(std::integral_constant<unsigned, kFew>()) : chunked(std::integral_constant<unsigned, kMost>());
     };
     if (s->f32) return s->cap > 0.0 ? of(uint32_t(), std::true_type()) : of(uint32_t(), std::false_type());
     return s->cap > 0.0 ? of(uint16_t(), std::true_type()) : of(uint16_t(), std::false_type());
@@ -849,8 +1050,8 @@ ktanh_status_t sample_entry(const ksample_shape_t *s, const void *logits, const 
 extern "C" size_t ksample_workspace(const ksample_shape_t *shape)
 {
     if (check_shape(shape) != KT_OK) return 0;
-    const size_t chunks = chunks_of(shape->vocabulary), blocks = shape->rows * chunks;
-    return chunks == 1 ? 0 : blocks * (kBins * sizeof(u64) + sizeof(u64) + 2 * sizeof(uint32_t)) + shape->rows * (kListed * sizeof(u64) + sizeof(uint32_t));
+    const size_t chunks = cut_of(shape->rows, shape->vocabulary).chunks, blocks = shape->rows * chunks;
+    return chunks == 1 ? 0 : blocks * (kBins * sizeof(u64) + sizeof(float4) + sizeof(uint32_t)) + shape->rows * (kListed * sizeof(u64) + sizeof(uint32_t));
 }
 extern "C" ktanh_status_t ksample(const ksample_shape_t *shape, const void *logits, const float *uniform, const float *temperature, const int32_t *top_k,
                                   const float *top_p, const float *min_p, int64_t *tokens, void *workspace, const ktanh_lut_t *lut, ktanh_stream_t stream)
