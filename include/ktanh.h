@@ -381,12 +381,13 @@ ktanh_status_t kq8_rows64(const kq8_shape_t *shape, const void *x, int8_t *codes
  *              are faster; bytes between the rows are never used
  *   scales     device, Float32 [rows]         w_scale, bias   device, Float32 [outer]; bias may be NULL
  *   out        device, out: [rows][outer] BFloat16 or Float32 with rows out_row apart
+ *   workspace  device, 16-byte aligned, kq8_product_workspace bytes (kq8_linear_workspace for kq8_linear), may be NULL where that is 0; what it
+ *              holds before does not matter, and calls that may run at once need one each
  * inner up to 131071 (KT_ERR_SHAPE).  inner == 0 gives sums of zero; rows == 0 or outer == 0 returns KT_OK without a launch. */
+size_t kq8_product_workspace(const kq8_shape_t *shape);
 ktanh_status_t kq8_product(const kq8_shape_t *shape, const int8_t *codes, const float *scales, const int8_t *w, const float *w_scale,
-                           const float *bias, void *out, ktanh_stream_t stream);
+                           const float *bias, void *out, void *workspace, ktanh_stream_t stream);
 
-/*   workspace  device, 16-byte aligned, kq8_linear_workspace bytes; what it holds before does not matter, and calls that may run at once
- *              need one each */
 size_t kq8_linear_workspace(const kq8_shape_t *shape);
 ktanh_status_t kq8_linear(const kq8_shape_t *shape, const void *x, const int8_t *w, const float *w_scale, const float *bias, void *out,
                           void *workspace, const ktanh_lut_t *lut, ktanh_stream_t stream);

@@ -52,7 +52,7 @@ SIGNATURES = {
     "kcap_attention_paged_workspace": "agt",
     "kcap_attention_paged": "agppppppppls", "kcap_attention64_paged": "agppppppppLs",
     "kcap_append": "agpppppppppppnnts",
-    "kq8_rows": "qppnpls", "kq8_rows64": "qppnpLs", "kq8_product": "qpppppps", "kq8_linear_workspace": "q",
+    "kq8_rows": "qppnpls", "kq8_rows64": "qppnpLs", "kq8_product_workspace": "q", "kq8_product": "qppppppps", "kq8_linear_workspace": "q",
     "kq8_linear": "qppppppls", "kq8_linear64": "qppppppLs",
     "ksample_workspace": "m", "ksample": "mppppppppls", "ksample64": "mppppppppLs",
     "kswish_keep8": "bbbbnls", "kswish_keep8_backward": "bbbbbnls", "kgelu_keep8": "bbbbnls", "kgelu_keep8_backward": "bbbbbnls",
@@ -181,7 +181,7 @@ def load_library() -> ctypes.CDLL:
             fn.restype = ctypes.c_int
         lib.ktanh_status_string.restype = ctypes.c_char_p
         lib.ktanh_default_lut.restype = ctypes.POINTER(KtanhLut)
-        for name in ("kcap_attention_paged_workspace", "kcap_attention_backward_workspace", "kq8_linear_workspace", "ksample_workspace"):
+        for name in ("kcap_attention_paged_workspace", "kcap_attention_backward_workspace", "kq8_product_workspace", "kq8_linear_workspace", "ksample_workspace"):
             getattr(lib, name).restype = ctypes.c_size_t
         _load_host()
         _lib = lib
@@ -847,8 +847,11 @@ def kq8_product(codes, scales, weight, weight_scales, bias=None, *, out_dtype=to
     out, outer = _q8_weights(weight, weight_scales, bias, rows, inner, out, out_dtype, codes, stream)
     _check_here(codes, scales, weight, weight_scales, bias, out)
     shape = Kq8Shape(rows, inner, outer, _step(codes, 0), _step(weight, 0), _step(out, 0), 0, out.dtype == torch.float32, 0)
-    st = load_library().kq8_product(shape, codes.data_ptr(), scales.data_ptr(), weight.data_ptr(), weight_scales.data_ptr(), _pointer(bias),
-                                    out.data_ptr(), _stream_handle(stream))
+    lib = load_library()
+    size = lib.kq8_product_workspace(shape)
+    workspace = _empty((size,), torch.uint8, codes, stream) if size else None
+    st = lib.kq8_product(shape, codes.data_ptr(), scales.data_ptr(), weight.data_ptr(), weight_scales.data_ptr(), _pointer(bias), out.data_ptr(),
+                         _pointer(workspace), _stream_handle(stream))
     if st != 0:
         raise KtanhError(st, "kq8_product")
     return out

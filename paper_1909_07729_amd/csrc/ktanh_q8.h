@@ -30,7 +30,69 @@ inline ktanh_status_t check_product(const kq8_shape_t *s)
     return KT_OK;
 }
 
-// Codes of a call that makes its own: rows of a multiple of 16 bytes, then the scales.
+// Which blocks a product is cut into.  Tiles through LDS (channels by rows), of which `parts` blocks share the inner dimension and leave sums that a second
+// launch joins; or blocks of 16 by 16 whose wavefronts share it (SHARED), for few results and short rows.
+//
+// The plan is the one that takes least by a model of what steps, rounds of blocks, memory and launches cost.  Its numbers are measured, us of calls on
+// weights out of the cache, by the model's choice | the others:
+//     1 x 4096 x 4096   SHARED 5.9 | 64x64 10.7                  256 x 4096 x 4096    64x64 12.8 | 128x64 18.5, 128x128 31.6
+//    16 x 16384 x 4096  64x64 in 4 parts 22.4 | 1 part 35.6      512 x 16384 x 1024   128x64 in 4 parts 23.6 | 1 part 54.2
+//    64 x 1024 x 1024   SHARED 3.4 | 64x64 5.1                  1024 x 4096 x 4096    128x64 32.5 | 128x128 35.2, 256x256 62.0
+//    64 x 4096 x 16384  64x64 19.4 | 128x64 23.3, SHARED 74.6   2048 x 4096 x 4096    128x128 42.9 | 256x256 63.7, 128x64 59.9
+//   128 x 4096 x 4096   64x64 10.9 | 128x64 14.0, SHARED 35.5   2048 x 4096 x 6144    256x256 65.5 | 128x128 73.6
+//   128 x 1024 x 512    SHARED 3.4 | 64x64 5.1                  8192 x 16384 x 4096   256x256 481 | 128x128 536
+enum Kind { T256, T128, T128_64, T64, SHARED };
+struct Tile {
+    unsigned over, across;      // output channels, rows
+    double alone, together;     // us of a step of 128 integers of a block by itself on a CU, and of each of two
+};
+constexpr Tile kTiles[] = {{256, 256, 1.85, 1.9}, {128, 128, 0.94, 0.59}, {128, 64, 0.35, 0.33}, {64, 64, 0.22, 0.216}, {16, 16, 0, 0}};
+
+struct Plan {
+    Kind kind;
+    unsigned parts;
+};
+
+inline double us_of(Kind kind, unsigned parts, size_t rows, size_t inner, size_t outer)
+{
+    const Tile &t = kTiles[kind];
+    const double blocks = (double)((outer + t.over - 1) / t.over) * (double)((rows + t.across - 1) / t.across) * parts;
+    const double rounds = blocks <= 256 ? 1 : (double)(size_t)((blocks + 255) / 256), pairs = (double)(size_t)(rounds / 2);
+    double us;
+    if (kind == SHARED) us = rounds * (0.5 + 0.48 * (double)((inner + 511) / 512));
+    else us = (double)((inner + 128 * parts - 1) / (128 * parts)) * (pairs * 2 * t.together + (rounds - pairs * 2) * t.alone);
+    // memory at 5 TB/s, less where not every CU has a block
+    const double memory = ((double)rows + (double)outer) * (double)inner / 5e6 * (blocks < 256 ? 1 + (256 - blocks) / 512 : 1);
+    if (us < memory) us = memory;
+    us += kind == SHARED ? 2.5 : 3.5;
+    if (parts > 1) us += 2.5 + (double)parts * (double)rows * (double)outer * 8 / 4e6;
+    return us;
+}
+
+inline Plan plan_of(size_t rows, size_t inner, size_t outer)
+{
+    Plan best{SHARED, 1};
+    double least = us_of(SHARED, 1, rows, inner, outer);
+    for (int kind = T256; kind < SHARED; ++kind)
+        for (unsigned parts = 1; parts <= 8; parts *= 2) {
+            if (parts > 1 && (kind == T256 || inner / 128 < 4 * parts)) break;      // four tiles for each at least
+            const double us = us_of((Kind)kind, parts, rows, inner, outer);
+            if (us < least) {
+                least = us;
+                best = Plan{(Kind)kind, parts};
+            }
+        }
+    return best;
+}
+
+// A call's workspace: codes that it makes itself (rows of a multiple of 16 bytes, then the scales), and the sums of parts.
 inline size_t padded(size_t inner) { return (inner + 15) / 16 * 16; }
+inline size_t rows_bytes(const kq8_shape_t &s) { return (s.rows * (padded(s.inner) + sizeof(float)) + 15) / 16 * 16; }
+inline size_t sums_bytes(const kq8_shape_t &s)
+{
+    if (s.rows == 0 || s.outer == 0) return 0;
+    const unsigned parts = plan_of(s.rows, s.inner, s.outer).parts;
+    return parts > 1 ? s.rows * s.outer * sizeof(int32_t) * parts : 0;
+}
 
 }  // namespace ktanh_q8

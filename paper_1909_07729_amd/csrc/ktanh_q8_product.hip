@@ -44,31 +44,33 @@ __device__ __forceinline__ i32x4 load16(const int8_t *p, int count)
     return v;
 }
 
+// What leaves a block: results, or (SUMS) the sums of its part of the inner dimension, as the bits of Float32.
+enum Out { BF16 = 0, F32 = 1, SUMS = 2 };
+
 // Results leave by rows, 16 bytes of a lane's at once, to any address of an element's alignment.
-template <bool F32> struct Result;
-template <> struct Result<false> {
-    typedef uint16_t type;
-    typedef u32x4 anywhere __attribute__((aligned(2)));
-    static constexpr unsigned kEach = 8;    // of a 16-byte chunk
-};
-template <> struct Result<true> {
+template <Out OUT> struct Result {
     typedef float type;
     typedef u32x4 anywhere __attribute__((aligned(4)));
-    static constexpr unsigned kEach = 4;
+    static constexpr unsigned kEach = 4;    // of a 16-byte chunk
+};
+template <> struct Result<BF16> {
+    typedef uint16_t type;
+    typedef u32x4 anywhere __attribute__((aligned(2)));
+    static constexpr unsigned kEach = 8;
 };
 
-template <bool F32>
+template <Out OUT>
 __device__ __forceinline__ void store_chunk(const Operands &a, unsigned t, unsigned o, u32x4 v)
 {
-    typedef typename Result<F32>::type T;
+    typedef typename Result<OUT>::type T;
     if (t >= a.rows || o >= a.outer) return;
     T *to = static_cast<T *>(a.out) + t * a.out_row + o;
-    if (o + Result<F32>::kEach <= a.outer) {
-        *reinterpret_cast<typename Result<F32>::anywhere *>(to) = v;
+    if (o + Result<OUT>::kEach <= a.outer) {
+        *reinterpret_cast<typename Result<OUT>::anywhere *>(to) = v;
         return;
     }
     const T *from = reinterpret_cast<const T *>(&v);
-    for (unsigned i = 0; i < Result<F32>::kEach - 1; ++i)
+    for (unsigned i = 0; i < Result<OUT>::kEach - 1; ++i)
         if (o + i < a.outer) to[i] = from[i];
 }
 
@@ -93,10 +95,10 @@ __device__ __forceinline__ f32x4 scaled(i32x4 sum, float row, f32x4 channel, f32
 }
 
 // Four neighbouring results into LDS.
-template <bool F32>
+template <Out OUT>
 __device__ __forceinline__ void put_four(char *to, f32x4 y)
 {
-    if constexpr (F32) *reinterpret_cast<f32x4 *>(to) = y;
+    if constexpr (OUT != BF16) *reinterpret_cast<f32x4 *>(to) = y;
     else *reinterpret_cast<u32x2 *>(to) = u32x2{narrow_pair(y[0], y[1]), narrow_pair(y[2], y[3])};
 }
 
@@ -110,11 +112,20 @@ __device__ __forceinline__ void put_four(char *to, f32x4 y)
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 constexpr unsigned kDeep = 128;     // integers of a tile
 
-__device__ __forceinline__ void load_direct(const int8_t *from, char *to)
+// 16 bytes of each lane from `base` + its offset to LDS, at `to` + 16 * lane, with no register between.  As an instruction, because the compiler
+// would wait for all such loads before any read of LDS that it cannot tell apart from them; wait_for_tiles counts them instead.  (Nothing else in these
+// kernels uses M0.)
+__device__ __forceinline__ void load_direct(const int8_t *base, unsigned offset, char *to)
 {
-    typedef const __attribute__((address_space(1))) void *global;
-    typedef __attribute__((address_space(3))) void *local;
-    __builtin_amdgcn_global_load_lds((global)from, (local)to, 16, 0, 0);
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)to;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(__builtin_amdgcn_readfirstlane(at)), "v"(offset), "s"(base) : "memory");
+}
+// All but the last LOADS of this wavefront's loads have arrived, and its reads of LDS are done.
+template <unsigned LOADS>
+__device__ __forceinline__ void wait_for_tiles()
+{
+    static_assert(LOADS < 64, "six bits");
+    __builtin_amdgcn_s_waitcnt((LOADS & 15) | 7 << 4 | (LOADS >> 4) << 14);
 }
 
 // R rows of an operand, of which `there` are inside (the rest is read as the last), brought to LDS by the block.
@@ -139,7 +150,7 @@ struct Side {
     }
     __device__ __forceinline__ void load(unsigned i, unsigned k, char *tile) const
     {
-        load_direct(base + k + offset[i], tile + (__builtin_amdgcn_readfirstlane(threadIdx.x / 64) * (R / 4) + i * 8) * kDeep);
+        load_direct(base + k, offset[i], tile + (__builtin_amdgcn_readfirstlane(threadIdx.x / 64) * (R / 4) + i * 8) * kDeep);
     }
     // The end of the rows, fewer than kDeep integers, zeros behind them.
     __device__ __forceinline__ void load_end(unsigned k, unsigned inner, char *tile) const
@@ -165,13 +176,14 @@ __device__ __forceinline__ Corner corner_of(unsigned block, unsigned over, unsig
     return Corner{in / rows, group * kRows + in % rows};
 }
 
-template <unsigned TO, unsigned TT, bool F32>
-__global__ __launch_bounds__(256, TO * TT > 128 * 128 ? 1 : 2) void q8_tile_kernel(Operands a, unsigned over, unsigned across)
+template <unsigned TO, unsigned TT, unsigned PLACES, Out OUT>
+__global__ __launch_bounds__(256, TO * TT > 128 * 128 ? 1 : 2) void q8_tile_kernel(Operands a, unsigned over, unsigned across, unsigned parts)
 {
     constexpr unsigned OI = TO / 64, TI = TT / 64, kPlace = (TO + TT) * kDeep;
-    __shared__ __align__(16) char lds[2 * kPlace];
+    __shared__ __align__(16) char lds[PLACES * kPlace];
     const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const Corner at = corner_of(blockIdx.x, over, across);
+    const unsigned part = blockIdx.x / (over * across);
+    const Corner at = corner_of(blockIdx.x - part * (over * across), over, across);
     const unsigned o0 = at.over * TO, t0 = at.across * TT;
     const Side<TO> w(a.w, a.w_row, o0, a.outer - 1);
     const Side<TT> x(a.x, a.x_row, t0, a.rows - 1);
@@ -205,9 +217,12 @@ __global__ __launch_bounds__(256, TO * TT > 128 * 128 ? 1 : 2) void q8_tile_kern
             }
     };
     auto nothing = [](unsigned) {};
-    const unsigned tiles = a.inner / kDeep;
+    // this block's tiles of the inner dimension; the last part has what is left of a tile as well
+    const unsigned all = a.inner / kDeep, from = (unsigned)((unsigned long long)all * part / parts),
+                   tiles = (unsigned)((unsigned long long)all * (part + 1) / parts) - from;
     // Without a branch: past the last tiles the last one is asked for again, into a place that nobody reads, and what is read ahead is not used.
-    auto step = [&](unsigned tile, char *__restrict__ here, const char *__restrict__ next) {
+    auto tile_at = [&](unsigned tile) { return (from + (tile < tiles ? tile : tiles - 1)) * kDeep; };
+    auto step = [&](unsigned tile, char *here, const char *next) {
 #pragma unroll
         for (unsigned s = 0; s < 3; ++s) {
             read(here, s + 1);
@@ -216,12 +231,12 @@ __global__ __launch_bounds__(256, TO * TT > 128 * 128 ? 1 : 2) void q8_tile_kern
             __builtin_amdgcn_sched_barrier(0);
         }
         // the next tile is complete, and this one has been read by all
-        __builtin_amdgcn_s_waitcnt(0x0070);
+        wait_for_tiles<kLoads * (PLACES - 2)>();
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         read(next, 0);
         __builtin_amdgcn_sched_barrier(0);
-        const unsigned k = (tile + 2 < tiles ? tile + 2 : tiles - 1) * kDeep;
+        const unsigned k = tile_at(tile + PLACES);
         multiply(3, [&](unsigned n) {
             constexpr unsigned kEach = (kLoads + OI * TI - 1) / (OI * TI);
 #pragma unroll
@@ -231,28 +246,26 @@ __global__ __launch_bounds__(256, TO * TT > 128 * 128 ? 1 : 2) void q8_tile_kern
         });
     };
     if (tiles != 0) {
-        char *here = lds, *next = lds + kPlace;
 #pragma unroll
-        for (unsigned n = 0; n < kLoads; ++n) load(n, 0, here);
-        const unsigned k = tiles > 1 ? kDeep : 0;
+        for (unsigned p = 0; p < PLACES; ++p)
 #pragma unroll
-        for (unsigned n = 0; n < kLoads; ++n) load(n, k, next);
-        __builtin_amdgcn_s_waitcnt(0x0F70);
+            for (unsigned n = 0; n < kLoads; ++n) load(n, tile_at(p), lds + p * kPlace);
+        wait_for_tiles<kLoads * (PLACES - 1)>();
         __syncthreads();
-        read(here, 0);
+        read(lds, 0);
+        unsigned here = 0;
         for (unsigned tile = 0; tile < tiles; ++tile) {
-            step(tile, here, next);
-            char *const other = here;
+            const unsigned next = here + 1 < PLACES ? here + 1 : 0;
+            step(tile, lds + here * kPlace, lds + next * kPlace);
             here = next;
-            next = other;
         }
-        __builtin_amdgcn_s_waitcnt(0x0070);
+        wait_for_tiles<0>();
     }
     char *const first = lds;
-    if (a.inner % kDeep != 0) {
+    if (part + 1 == parts && a.inner % kDeep != 0) {
         __syncthreads();
-        w.load_end(tiles * kDeep, a.inner, first);
-        x.load_end(tiles * kDeep, a.inner, first + TO * kDeep);
+        w.load_end(all * kDeep, a.inner, first);
+        x.load_end(all * kDeep, a.inner, first + TO * kDeep);
         __syncthreads();
 #pragma unroll
         for (unsigned s = 0; s < 4; ++s) {
@@ -263,16 +276,18 @@ __global__ __launch_bounds__(256, TO * TT > 128 * 128 ? 1 : 2) void q8_tile_kern
     // A lane has, of 32 channels and 32 rows, four times 4 neighbouring channels of one row.  The results of 32 rows go through a wavefront's own
     // place in LDS, and leave by whole rows of its channels: straight from the registers each store would touch 32 rows, 16 bytes of each.
     __syncthreads();
-    constexpr unsigned kSize = F32 ? 4 : 2, kRow = TO / 2 * kSize, kPitch = kRow + 16, kChunks = kRow / 16;
-    static_assert(4 * 32 * kPitch <= sizeof(lds), "four wavefronts' results");
+    constexpr unsigned kSize = OUT == BF16 ? 2 : 4, kRow = TO / 2 * kSize, kPitch = kRow + 16, kChunks = kRow / 16;
+    static_assert(4 * 32 * kPitch <= PLACES * kPlace, "four wavefronts' results");
     char *const mine = lds + wave * 32 * kPitch;
     const unsigned o1 = o0 + wave / 2 * (TO / 2), t1 = t0 + wave % 2 * (TT / 2);
     const bool biased = a.bias != nullptr;
+    if constexpr (OUT == SUMS) a.out = static_cast<float *>(a.out) + (unsigned long long)part * a.rows * a.outer;
     f32x4 channel[OI][4], bias[OI][4];
 #pragma unroll
     for (unsigned i = 0; i < OI; ++i)
 #pragma unroll
         for (unsigned q = 0; q < 4; ++q) {
+            if constexpr (OUT == SUMS) continue;
             const unsigned o = o1 + i * 32 + q * 8 + lane / 32 * 4;
             channel[i][q] = four_of(a.w_scale, o, a.outer);
             bias[i][q] = biased ? four_of(a.bias, o, a.outer) : f32x4{0, 0, 0, 0};
@@ -280,19 +295,22 @@ __global__ __launch_bounds__(256, TO * TT > 128 * 128 ? 1 : 2) void q8_tile_kern
 #pragma unroll
     for (unsigned j = 0; j < TI; ++j) {
         const unsigned t = t1 + j * 32 + lane % 32;
-        const float row = a.x_scale[t < a.rows ? t : a.rows - 1];
+        const float row = OUT == SUMS ? 0.f : a.x_scale[t < a.rows ? t : a.rows - 1];
 #pragma unroll
         for (unsigned i = 0; i < OI; ++i)
 #pragma unroll
             for (unsigned q = 0; q < 4; ++q) {
                 const i32x4 four = {sum[i][j][4 * q], sum[i][j][4 * q + 1], sum[i][j][4 * q + 2], sum[i][j][4 * q + 3]};
-                put_four<F32>(mine + lane % 32 * kPitch + (i * 32 + q * 8 + lane / 32 * 4) * kSize, scaled(four, row, channel[i][q], bias[i][q], biased));
+                f32x4 y;
+                if constexpr (OUT == SUMS) y = __builtin_bit_cast(f32x4, four);
+                else y = scaled(four, row, channel[i][q], bias[i][q], biased);
+                put_four<OUT>(mine + lane % 32 * kPitch + (i * 32 + q * 8 + lane / 32 * 4) * kSize, y);
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
 #pragma unroll
         for (unsigned n = 0; n < 32 * kChunks / 64; ++n) {
             const unsigned at = (n * 64 + lane) / kChunks, chunk = (n * 64 + lane) % kChunks;
-            store_chunk<F32>(a, t1 + j * 32 + at, o1 + chunk * Result<F32>::kEach, *reinterpret_cast<const u32x4 *>(mine + at * kPitch + chunk * 16));
+            store_chunk<OUT>(a, t1 + j * 32 + at, o1 + chunk * Result<OUT>::kEach, *reinterpret_cast<const u32x4 *>(mine + at * kPitch + chunk * 16));
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
     }
@@ -302,7 +320,7 @@ __global__ __launch_bounds__(256, TO * TT > 128 * 128 ? 1 : 2) void q8_tile_kern
 // A block has OT output channels and TT rows, and its W wavefronts share the inner dimension in steps of 64 integers: wavefront s takes the steps
 // s, s + W, ..., so that the block reads whole cache lines.  Operands go from memory to the matrix cores' registers; the wavefronts' sums
 // meet in LDS.
-template <unsigned OT, unsigned TT, unsigned W, bool F32, bool ALIGNED>
+template <unsigned OT, unsigned TT, unsigned W, Out OUT, bool ALIGNED>
 __global__ __launch_bounds__(64 * W) void q8_shared_inner_kernel(Operands a)
 {
     constexpr unsigned OI = OT / 16, TI = TT / 16;
@@ -333,12 +351,13 @@ __global__ __launch_bounds__(64 * W) void q8_shared_inner_kernel(Operands a)
 #pragma unroll
             for (unsigned j = 0; j < TI; ++j) sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[i], xf[j], sum[i][j], 0, 0, 0);
     };
-    // Whole groups of U steps, the next group's operands on their way during the products of one; past the last the last is asked for again.
+    // Whole groups of U steps, the next group's operands on their way during the products of one.
     constexpr unsigned U = OI + TI > 4 ? 2 : OI + TI > 2 ? 4 : 8;
     const unsigned whole = a.inner / 64, mine = whole > wave ? (whole - wave + W - 1) / W : 0, groups = mine / U;
     i32x4 wf[2][U][OI], xf[2][U][TI];
     auto load = [&](unsigned to, unsigned group) {
-        const unsigned at = (wave + (group < groups ? group : groups - 1) * U * W) * 64;
+        if (group >= groups) return;
+        const unsigned at = (wave + group * U * W) * 64;
 #pragma unroll
         for (unsigned u = 0; u < U; ++u) {
 #pragma unroll
@@ -347,17 +366,15 @@ __global__ __launch_bounds__(64 * W) void q8_shared_inner_kernel(Operands a)
             for (unsigned i = 0; i < TI; ++i) xf[to][u][i] = load16<ALIGNED>(x[i] + at + u * W * 64);
         }
     };
-    if (groups != 0) {
-        load(0, 0);
-        for (unsigned g = 0; g < groups; g += 2) {
-            load(1, g + 1);
+    load(0, 0);
+    for (unsigned g = 0; g < groups; g += 2) {
+        load(1, g + 1);
 #pragma unroll
-            for (unsigned u = 0; u < U; ++u) multiply(wf[0][u], xf[0][u]);
-            load(0, g + 2);
-            if (g + 1 < groups) {
+        for (unsigned u = 0; u < U; ++u) multiply(wf[0][u], xf[0][u]);
+        load(0, g + 2);
+        if (g + 1 < groups) {
 #pragma unroll
-                for (unsigned u = 0; u < U; ++u) multiply(wf[1][u], xf[1][u]);
-            }
+            for (unsigned u = 0; u < U; ++u) multiply(wf[1][u], xf[1][u]);
         }
     }
     unsigned s = wave + groups * U * W;
@@ -377,7 +394,7 @@ __global__ __launch_bounds__(64 * W) void q8_shared_inner_kernel(Operands a)
         for (unsigned j = 0; j < TI; ++j)
             *reinterpret_cast<i32x4 *>(&part[wave][16 * j + lane % 16][16 * i + lane / 16 * 4]) = sum[i][j];
     __syncthreads();
-    constexpr unsigned E = Result<F32>::kEach;
+    constexpr unsigned E = Result<OUT>::kEach;
     for (unsigned e = threadIdx.x; e < TT * OT / E; e += 64 * W) {
         const unsigned t = e / (OT / E), o = e % (OT / E) * E;
         if (t0 + t >= a.rows || o0 + o >= a.outer) continue;
@@ -391,10 +408,45 @@ __global__ __launch_bounds__(64 * W) void q8_shared_inner_kernel(Operands a)
             const unsigned c = o0 + o + 4 * h;
             const bool biased = a.bias != nullptr;
             const f32x4 y = scaled(v, row, four_of(a.w_scale, c, a.outer), biased ? four_of(a.bias, c, a.outer) : f32x4{0, 0, 0, 0}, biased);
-            put_four<F32>(reinterpret_cast<char *>(&out) + 8 * h, y);
+            put_four<OUT>(reinterpret_cast<char *>(&out) + 8 * h, y);
         }
-        store_chunk<F32>(a, t0 + t, o0 + o, out);
+        store_chunk<OUT>(a, t0 + t, o0 + o, out);
     }
+}
+
+// ------------------------------------------------------------------------------------ parts joined
+// The sums of the parts of the inner dimension added up, scaled and stored; a chunk of 16 bytes to a lane.
+template <Out OUT>
+__global__ __launch_bounds__(256) void q8_join_kernel(Operands a, const int *sums, unsigned parts)
+{
+    constexpr unsigned E = Result<OUT>::kEach;
+    const unsigned across = (a.outer + E - 1) / E;
+    const unsigned long long id = blockIdx.x * 256ull + threadIdx.x;
+    if (id >= (unsigned long long)across * a.rows) return;
+    const unsigned t = (unsigned)(id / across), o = (unsigned)(id % across) * E;
+    const unsigned long long each = (unsigned long long)a.rows * a.outer;
+    typedef i32x4 anywhere __attribute__((aligned(4)));
+    const float row = a.x_scale[t];
+    const bool biased = a.bias != nullptr;
+    u32x4 out;
+#pragma unroll
+    for (unsigned h = 0; h < E / 4; ++h) {
+        const unsigned c = o + 4 * h;
+        if (c >= a.outer) break;
+        i32x4 v = {0, 0, 0, 0};
+        for (unsigned p = 0; p < parts; ++p) {
+            const int *from = sums + p * each + t * (unsigned long long)a.outer + c;
+            if (c + 4 <= a.outer) {
+                v += *reinterpret_cast<const anywhere *>(from);
+            } else {
+                for (unsigned i = 0; i < 3; ++i)
+                    if (c + i < a.outer) v[i] += from[i];
+            }
+        }
+        put_four<OUT>(reinterpret_cast<char *>(&out) + 8 * h,
+                      scaled(v, row, four_of(a.w_scale, c, a.outer), biased ? four_of(a.bias, c, a.outer) : f32x4{0, 0, 0, 0}, biased));
+    }
+    store_chunk<OUT>(a, t, o, out);
 }
 
 }  // namespace
@@ -403,7 +455,7 @@ namespace ktanh_q8 {
 
 // Arguments have been checked.
 ktanh_status_t launch_product(const kq8_shape_t &s, const int8_t *x, size_t x_row, const float *x_scale, const int8_t *w, const float *w_scale,
-                              const float *bias, void *out, ktanh_stream_t stream)
+                              const float *bias, void *out, void *workspace, ktanh_stream_t stream)
 {
     Operands a;
     a.x = x;
@@ -426,21 +478,46 @@ ktanh_status_t launch_product(const kq8_shape_t &s, const int8_t *x, size_t x_ro
         return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)over, (unsigned)across), dim3(threads), args, 0,
                                static_cast<hipStream_t>(stream)) == hipSuccess ? KT_OK : KT_ERR_HIP;
     };
-    auto sized = [&](auto f32, auto on_grid) {
-        constexpr bool F = decltype(f32)::value, A = decltype(on_grid)::value;
-        if constexpr (A) {
-            // a tile's offsets are 32-bit
-            if (s.rows >= 128 && a.x_row < 1u << 23 && a.w_row < 1u << 23) {
-                const unsigned over = (a.outer + 255) / 256, across = (a.rows + 255) / 256;
-                return launch_checked(q8_tile_kernel<256, 256, F>, over * across, 256, stream, a, over, across);
+    const Plan plan = plan_of(s.rows, s.inner, s.outer);
+    // a tile's offsets are 32-bit
+    if (aligned && plan.kind != SHARED && a.x_row < 1u << 23 && a.w_row < 1u << 23) {
+        auto tiled = [&](auto out) {
+            constexpr Out O = decltype(out)::value;
+            auto launch = [&](auto kernel) {
+                const Tile t = kTiles[plan.kind];
+                const unsigned over = (a.outer + t.over - 1) / t.over, across = (a.rows + t.across - 1) / t.across;
+                return launch_checked(kernel, over * across * plan.parts, 256, stream, a, over, across, plan.parts);
+            };
+            if constexpr (O != SUMS) {
+                if (plan.kind == T256) return launch(q8_tile_kernel<256, 256, 2, O>);
             }
-        }
-        if (s.rows <= 16) return launch(q8_shared_inner_kernel<16, 16, 8, F, A>, 512, 16, 16);
-        if (s.rows <= 32) return launch(q8_shared_inner_kernel<32, 32, 4, F, A>, 256, 32, 32);
-        return launch(q8_shared_inner_kernel<64, 64, 4, F, A>, 256, 64, 64);
+            switch (plan.kind) {
+            case T128: return launch(q8_tile_kernel<128, 128, 2, O>);
+            case T128_64: return launch(q8_tile_kernel<128, 64, 3, O>);
+            default: return launch(q8_tile_kernel<64, 64, 4, O>);
+            }
+        };
+        if (plan.parts == 1) return s.out_f32 ? tiled(std::integral_constant<Out, F32>()) : tiled(std::integral_constant<Out, BF16>());
+        Operands last = a;
+        a.out = workspace;
+        a.out_row = a.outer;
+        const ktanh_status_t st = tiled(std::integral_constant<Out, SUMS>());
+        if (st != KT_OK) return st;
+        auto join = [&](auto kernel, unsigned each) {
+            const unsigned long long chunks = (unsigned long long)((a.outer + each - 1) / each) * a.rows;
+            return launch_checked(kernel, (unsigned)((chunks + 255) / 256), 256, stream, last, static_cast<const int *>(workspace), plan.parts);
+        };
+        return s.out_f32 ? join(q8_join_kernel<F32>, 4) : join(q8_join_kernel<BF16>, 8);
+    }
+    auto sized = [&](auto out_type, auto on_grid) {
+        constexpr Out O = decltype(out_type)::value;
+        constexpr bool A = decltype(on_grid)::value;
+        // rows off the 16-byte grid: larger blocks from two of the small ones on each CU on (300 x 300 x 300 6.3 us against 10.5, 2000 x 200 x 5000 258 against 41)
+        if (plan.kind == SHARED || s.rows <= 32 || ((s.rows + 15) / 16) * ((s.outer + 15) / 16) <= 512) return launch(q8_shared_inner_kernel<16, 16, 8, O, A>, 512, 16, 16);
+        return launch(q8_shared_inner_kernel<64, 64, 4, O, A>, 256, 64, 64);
     };
-    auto typed = [&](auto f32) { return aligned ? sized(f32, std::true_type()) : sized(f32, std::false_type()); };
-    return s.out_f32 ? typed(std::true_type()) : typed(std::false_type());
+    auto typed = [&](auto out_type) { return aligned ? sized(out_type, std::true_type()) : sized(out_type, std::false_type()); };
+    return s.out_f32 ? typed(std::integral_constant<Out, F32>()) : typed(std::integral_constant<Out, BF16>());
 }
 
 }  // namespace ktanh_q8
@@ -473,13 +550,14 @@ ktanh_status_t linear_entry(const kq8_shape_t *s, const void *x, const int8_t *w
     if constexpr (is_wide(static_cast<const Lut *>(nullptr))) st = kq8_rows64(s, x, codes, row, scales, lut, stream);
     else st = kq8_rows(s, x, codes, row, scales, lut, stream);
     if (st != KT_OK) return st;
-    return launch_product(*s, codes, row, scales, w, w_scale, bias, out, stream);
+    void *const sums = codes + rows_bytes(*s);
+    return launch_product(*s, codes, row, scales, w, w_scale, bias, out, sums, stream);
 }
 
 }  // namespace
 
 extern "C" ktanh_status_t kq8_product(const kq8_shape_t *shape, const int8_t *codes, const float *scales, const int8_t *w, const float *w_scale,
-                                      const float *bias, void *out, ktanh_stream_t stream)
+                                      const float *bias, void *out, void *workspace, ktanh_stream_t stream)
 {
     ktanh_status_t st = check_product(shape);
     if (st != KT_OK) return st;
@@ -487,14 +565,17 @@ extern "C" ktanh_status_t kq8_product(const kq8_shape_t *shape, const int8_t *co
     if (scales == nullptr || (shape->inner != 0 && codes == nullptr)) return KT_ERR_NULL;
     st = check_weights(shape, w, w_scale, bias, out);
     if (st != KT_OK) return st;
-    if (off(scales, 4)) return KT_ERR_ALIGN;
-    return launch_product(*shape, codes, shape->x_row, scales, w, w_scale, bias, out, stream);
+    if (off(scales, 4) || off(workspace, 16)) return KT_ERR_ALIGN;
+    if (workspace == nullptr && sums_bytes(*shape) != 0) return KT_ERR_NULL;
+    return launch_product(*shape, codes, shape->x_row, scales, w, w_scale, bias, out, workspace, stream);
 }
+
+extern "C" size_t kq8_product_workspace(const kq8_shape_t *shape) { return check_product(shape) != KT_OK ? 0 : sums_bytes(*shape); }
 
 extern "C" size_t kq8_linear_workspace(const kq8_shape_t *shape)
 {
     if (check_rows(shape) != KT_OK || check_product(shape) != KT_OK) return 0;
-    return shape->rows * (padded(shape->inner) + sizeof(float));
+    return rows_bytes(*shape) + sums_bytes(*shape);
 }
 
 extern "C" ktanh_status_t kq8_linear(const kq8_shape_t *shape, const void *x, const int8_t *w, const float *w_scale, const float *bias, void *out,

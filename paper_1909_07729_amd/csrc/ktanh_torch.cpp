@@ -1067,8 +1067,9 @@ PyObject *q8_product_call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         pybind11::gil_scoped_release no_gil;
         made = w.out(*codes, codes->size(0));
         const kq8_shape_t shape = w.shape(*codes, made, KQ8_NONE);
+        const Tensor workspace = workspace_of(kq8_product_workspace(&shape), *codes);
         check_status(kq8_product(&shape, bytes(*codes), floats(*scales), bytes(*w.weight), floats(*w.scales), w.bias != nullptr ? floats(*w.bias) : nullptr,
-                                 made.mutable_data_ptr(), current_stream()),
+                                 made.mutable_data_ptr(), workspace.defined() ? workspace.mutable_data_ptr() : nullptr, current_stream()),
                      "kq8_product");
     }
     return THPVariable_Wrap(std::move(made));

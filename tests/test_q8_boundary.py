@@ -60,8 +60,8 @@ def test_rows_refuse(binding):
 def test_products_refuse(binding):
     lib = binding.load_library()
 
-    def product(shape, codes=FAKE, scales=FAKE, w=FAKE, w_scale=FAKE, bias=NULL, out=FAKE):
-        return lib.kq8_product(shape, codes, scales, w, w_scale, bias, out, NULL)
+    def product(shape, codes=FAKE, scales=FAKE, w=FAKE, w_scale=FAKE, bias=NULL, out=FAKE, workspace=FAKE):
+        return lib.kq8_product(shape, codes, scales, w, w_scale, bias, out, workspace, NULL)
 
     def linear(shape, x=FAKE, w=FAKE, w_scale=FAKE, bias=NULL, out=FAKE, workspace=FAKE, lut=None):
         return lib.kq8_linear(shape, x, w, w_scale, bias, out, workspace, lut, NULL)
@@ -80,7 +80,9 @@ def test_products_refuse(binding):
         half = ctypes.c_void_p(0x1002)
         assert call(_shape(binding), w_scale=half) == 2 and call(_shape(binding), bias=half) == 2
         assert call(_shape(binding), out=ODD) == 2 and call(_shape(binding, out_f32=1), out=half) == 2
-    assert product(_shape(binding), scales=ctypes.c_void_p(0x1002)) == 2
+    assert product(_shape(binding), scales=ctypes.c_void_p(0x1002)) == 2 and product(_shape(binding), workspace=ctypes.c_void_p(0x1008)) == 2
+    parts = _shape(binding, rows=64, inner=16384, outer=1024, x_row=16384, w_row=16384, out_row=1024)
+    assert lib.kq8_product_workspace(parts) > 0 and product(parts, workspace=NULL) == 1
     assert linear(_shape(binding), x=ODD) == 2 and linear(_shape(binding), workspace=ctypes.c_void_p(0x1008)) == 2
     assert linear(_shape(binding, activation=7)) == 4
     table = binding.ktanh_default_lut()
@@ -92,6 +94,9 @@ def test_workspace(binding):
     lib = binding.load_library()
     assert lib.kq8_linear_workspace(_shape(binding)) == 8 * (64 + 4)
     assert lib.kq8_linear_workspace(_shape(binding, inner=65)) == 8 * (80 + 4)
+    few = _shape(binding, rows=64, inner=16384, outer=1024, x_row=16384, w_row=16384, out_row=1024)
+    assert lib.kq8_linear_workspace(few) == 64 * (16384 + 4) + lib.kq8_product_workspace(few)
+    assert lib.kq8_product_workspace(few) % (64 * 1024 * 4) == 0 and lib.kq8_product_workspace(_shape(binding)) == 0
     assert lib.kq8_linear_workspace(_shape(binding, rows=0)) == 0 and lib.kq8_linear_workspace(_shape(binding, inner=131072)) == 0
 
 
