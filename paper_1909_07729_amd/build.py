@@ -13,7 +13,7 @@ LIB_PATH = os.path.join(_HERE, "libktanh.so")
 SOURCES = ["ktanh_stream.hip", "ktanh_lstm.hip", "ktanh_lstm_chunks.hip", "ktanh_lstm_ring.hip",
            "ktanh_backward.hip", "ktanh_cap_forward.hip", "ktanh_cap_backward.hip", "ktanh_cap_decode.hip",
            "ktanh_cap_append.hip", "ktanh_keep8.hip", "ktanh_q8_rows.hip",
-           "ktanh_q8_product.hip", "ktanh_sample.hip", "ktanh_lut.cpp", "ktanh_fit.cpp"]
+           "ktanh_q8_product.hip", "ktanh_q8_few.hip", "ktanh_sample.hip", "ktanh_lut.cpp", "ktanh_fit.cpp"]
 # measurement yardsticks (include/ktanh_probe.h): a library of their own, loaded only by the benchmark
 PROBE_LIB_PATH = os.path.join(_HERE, "libktanh_probe.so")
 PROBE_SOURCES = ["ktanh_probe.hip", "ktanh_lut.cpp", "ktanh_fit.cpp"]

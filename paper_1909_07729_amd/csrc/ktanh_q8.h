@@ -95,4 +95,8 @@ inline size_t sums_bytes(const kq8_shape_t &s)
     return parts > 1 ? s.rows * s.outer * sizeof(int32_t) * parts : 0;
 }
 
+// Few short rows and their product in one launch, where that is the faster way (*done), with either table.
+ktanh_status_t launch_few(const kq8_shape_t &s, const void *x, const int8_t *w, const float *w_scale, const float *bias, void *out, const ktanh_lut_t *lut,
+                          const ktanh_lut64_t *lut64, bool wide, ktanh_stream_t stream, bool *done);
+
 }  // namespace ktanh_q8

@@ -5,102 +5,13 @@
 // The sums are exact (32-bit integers); the scaling is Float32, one rounding per operation.
 #include <type_traits>
 
-#include "ktanh_device.h"
 #include "ktanh_q8.h"
+#include "ktanh_q8_device.h"
 
 using namespace ktanh_device;
 using namespace ktanh_q8;
 
 namespace {
-
-typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-typedef i32x4 i32x4_anywhere __attribute__((aligned(1)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-struct Operands {
-    const int8_t *x, *w;
-    unsigned long long x_row, w_row;
-    const float *x_scale, *w_scale, *bias;
-    void *out;
-    unsigned long long out_row;
-    unsigned rows, outer, inner;
-};
-
-// 16 integers from p, of which the first `count` are there (the rest zeros): at the end of a row.
-template <bool ALIGNED>
-__device__ __forceinline__ i32x4 load16(const int8_t *p)
-{
-    if constexpr (ALIGNED) return *reinterpret_cast<const i32x4 *>(p);
-    else return *reinterpret_cast<const i32x4_anywhere *>(p);
-}
-template <bool ALIGNED>
-__device__ __forceinline__ i32x4 load16(const int8_t *p, int count)
-{
-    if (count >= 16) return load16<ALIGNED>(p);
-    i32x4 v = {0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (i < count) v[i / 4] |= (int)(uint8_t)p[i] << (8 * (i % 4));
-    return v;
-}
-
-// What leaves a block: results, or (SUMS) the sums of its part of the inner dimension, as the bits of Float32.
-enum Out { BF16 = 0, F32 = 1, SUMS = 2 };
-
-// Results leave by rows, 16 bytes of a lane's at once, to any address of an element's alignment.
-template <Out OUT> struct Result {
-    typedef float type;
-    typedef u32x4 anywhere __attribute__((aligned(4)));
-    static constexpr unsigned kEach = 4;    // of a 16-byte chunk
-};
-template <> struct Result<BF16> {
-    typedef uint16_t type;
-    typedef u32x4 anywhere __attribute__((aligned(2)));
-    static constexpr unsigned kEach = 8;
-};
-
-template <Out OUT>
-__device__ __forceinline__ void store_chunk(const Operands &a, unsigned t, unsigned o, u32x4 v)
-{
-    typedef typename Result<OUT>::type T;
-    if (t >= a.rows || o >= a.outer) return;
-    T *to = static_cast<T *>(a.out) + t * a.out_row + o;
-    if (o + Result<OUT>::kEach <= a.outer) {
-        *reinterpret_cast<typename Result<OUT>::anywhere *>(to) = v;
-        return;
-    }
-    const T *from = reinterpret_cast<const T *>(&v);
-    for (unsigned i = 0; i < Result<OUT>::kEach - 1; ++i)
-        if (o + i < a.outer) to[i] = from[i];
-}
-
-// Scales, or biases, of channels o .. o + 3; past the last channel the last one's.
-__device__ __forceinline__ f32x4 four_of(const float *p, unsigned o, unsigned outer)
-{
-    typedef f32x4 anywhere __attribute__((aligned(4)));
-    if (o + 4 <= outer) return *reinterpret_cast<const anywhere *>(p + o);
-    auto at = [&](unsigned i) { return p[i < outer ? i : outer - 1]; };
-    return f32x4{at(o), at(o + 1), at(o + 2), at(o + 3)};
-}
-
-__device__ __forceinline__ f32x4 scaled(i32x4 sum, float row, f32x4 channel, f32x4 bias, bool biased)
-{
-    f32x4 y;
-#pragma unroll
-    for (unsigned i = 0; i < 4; ++i) {
-        y[i] = ((float)sum[i] * row) * channel[i];
-        if (biased) y[i] = y[i] + bias[i];
-    }
-    return y;
-}
-
-// Four neighbouring results into LDS.
-template <Out OUT>
-__device__ __forceinline__ void put_four(char *to, f32x4 y)
-{
-    if constexpr (OUT != BF16) *reinterpret_cast<f32x4 *>(to) = y;
-    else *reinterpret_cast<u32x2 *>(to) = u32x2{narrow_pair(y[0], y[1]), narrow_pair(y[2], y[3])};
-}
 
 // ------------------------------------------------------------------------------------ tiles
 // Products of many rows.  A block of four wavefronts has TO output channels and TT rows, each wavefront a quarter of it (two by two).  Tiles of 128
@@ -394,24 +305,7 @@ __global__ __launch_bounds__(64 * W) void q8_shared_inner_kernel(Operands a)
         for (unsigned j = 0; j < TI; ++j)
             *reinterpret_cast<i32x4 *>(&part[wave][16 * j + lane % 16][16 * i + lane / 16 * 4]) = sum[i][j];
     __syncthreads();
-    constexpr unsigned E = Result<OUT>::kEach;
-    for (unsigned e = threadIdx.x; e < TT * OT / E; e += 64 * W) {
-        const unsigned t = e / (OT / E), o = e % (OT / E) * E;
-        if (t0 + t >= a.rows || o0 + o >= a.outer) continue;
-        const float row = a.x_scale[t0 + t];
-        u32x4 out;
-#pragma unroll
-        for (unsigned h = 0; h < E / 4; ++h) {
-            i32x4 v = *reinterpret_cast<const i32x4 *>(&part[0][t][o + 4 * h]);
-#pragma unroll
-            for (unsigned i = 1; i < W; ++i) v += *reinterpret_cast<const i32x4 *>(&part[i][t][o + 4 * h]);
-            const unsigned c = o0 + o + 4 * h;
-            const bool biased = a.bias != nullptr;
-            const f32x4 y = scaled(v, row, four_of(a.w_scale, c, a.outer), biased ? four_of(a.bias, c, a.outer) : f32x4{0, 0, 0, 0}, biased);
-            put_four<OUT>(reinterpret_cast<char *>(&out) + 8 * h, y);
-        }
-        store_chunk<OUT>(a, t0 + t, o0 + o, out);
-    }
+    store_joined<OT, TT, W, OUT>(a, o0, t0, part);
 }
 
 // ------------------------------------------------------------------------------------ parts joined
@@ -532,6 +426,18 @@ ktanh_status_t check_weights(const kq8_shape_t *s, const int8_t *w, const float 
     return KT_OK;
 }
 
+// Few short rows go to integers within the product's launch (ktanh_q8_few.hip).
+ktanh_status_t launch_few(const kq8_shape_t &s, const void *x, const int8_t *w, const float *w_scale, const float *bias, void *out, const ktanh_lut_t *lut,
+                          ktanh_stream_t stream, bool *done)
+{
+    return ktanh_q8::launch_few(s, x, w, w_scale, bias, out, lut, nullptr, false, stream, done);
+}
+ktanh_status_t launch_few(const kq8_shape_t &s, const void *x, const int8_t *w, const float *w_scale, const float *bias, void *out, const ktanh_lut64_t *lut,
+                          ktanh_stream_t stream, bool *done)
+{
+    return ktanh_q8::launch_few(s, x, w, w_scale, bias, out, nullptr, lut, true, stream, done);
+}
+
 template <class Lut>
 ktanh_status_t linear_entry(const kq8_shape_t *s, const void *x, const int8_t *w, const float *w_scale, const float *bias, void *out, void *workspace,
                             const Lut *lut, ktanh_stream_t stream)
@@ -544,6 +450,9 @@ ktanh_status_t linear_entry(const kq8_shape_t *s, const void *x, const int8_t *w
     st = check_weights(s, w, w_scale, bias, out);
     if (st != KT_OK) return st;
     if (off(x, s->x_f32 ? 4 : 2) || off(workspace, 16)) return KT_ERR_ALIGN;
+    bool done = false;
+    st = launch_few(*s, x, w, w_scale, bias, out, lut, stream, &done);
+    if (done) return st;
     int8_t *codes = static_cast<int8_t *>(workspace);
     const size_t row = padded(s->inner);
     float *scales = reinterpret_cast<float *>(codes + s->rows * row);
