@@ -39,14 +39,14 @@ inline ktanh_status_t check_product(const kq8_shape_t *s)
 //    16 x 16384 x 4096  64x64 in 4 parts 22.4 | 1 part 35.6      512 x 16384 x 1024   128x64 in 4 parts 23.6 | 1 part 54.2
 //    64 x 1024 x 1024   SHARED 3.4 | 64x64 5.1                  1024 x 4096 x 4096    128x64 32.5 | 128x128 35.2, 256x256 62.0
 //    64 x 4096 x 16384  64x64 19.4 | 128x64 23.3, SHARED 74.6   2048 x 4096 x 4096    128x128 42.9 | 256x256 63.7, 128x64 59.9
-//   128 x 4096 x 4096   64x64 10.9 | 128x64 14.0, SHARED 35.5   2048 x 4096 x 6144    256x256 65.5 | 128x128 73.6
+//   128 x 4096 x 4096   64x64 10.9 | 128x64 14.0, SHARED 35.5   2048 x 4096 x 6144    192x256 54.2 | 256x256 65.5, 128x128 73.6
 //   128 x 1024 x 512    SHARED 3.4 | 64x64 5.1                  8192 x 16384 x 4096   256x256 481 | 128x128 536
-enum Kind { T256, T128, T128_64, T64, SHARED };
+enum Kind { T256, T192, T128, T128_64, T64, SHARED };
 struct Tile {
     unsigned over, across;      // output channels, rows
     double alone, together;     // us of a step of 128 integers of a block by itself on a CU, and of each of two
 };
-constexpr Tile kTiles[] = {{256, 256, 1.85, 1.9}, {128, 128, 0.94, 0.59}, {128, 64, 0.35, 0.33}, {64, 64, 0.22, 0.216}, {16, 16, 0, 0}};
+constexpr Tile kTiles[] = {{256, 256, 1.85, 1.9}, {192, 256, 1.45, 1.48}, {128, 128, 0.94, 0.59}, {128, 64, 0.35, 0.33}, {64, 64, 0.22, 0.216}, {16, 16, 0, 0}};
 
 struct Plan {
     Kind kind;
@@ -75,7 +75,7 @@ inline Plan plan_of(size_t rows, size_t inner, size_t outer)
     double least = us_of(SHARED, 1, rows, inner, outer);
     for (int kind = T256; kind < SHARED; ++kind)
         for (unsigned parts = 1; parts <= 8; parts *= 2) {
-            if (parts > 1 && (kind == T256 || inner / 128 < 4 * parts)) break;      // four tiles for each at least
+            if (parts > 1 && (kind <= T192 || inner / 128 < 4 * parts)) break;      // four tiles for each at least
             const double us = us_of((Kind)kind, parts, rows, inner, outer);
             if (us < least) {
                 least = us;

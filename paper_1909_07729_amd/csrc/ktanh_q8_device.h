@@ -19,22 +19,33 @@ struct Operands {
     unsigned rows, outer, inner;
 };
 
-// 16 integers from p, of which the first `count` are there (the rest zeros): at the end of a row.
+// 16 integers from p.
 template <bool ALIGNED>
 __device__ __forceinline__ i32x4 load16(const int8_t *p)
 {
     if constexpr (ALIGNED) return *reinterpret_cast<const i32x4 *>(p);
     else return *reinterpret_cast<const i32x4_anywhere *>(p);
 }
+// The same of a row of `inner` integers, `count` of which are from p on (any number; zeros behind them).  The row's last integers come with one load that ends
+// where the row does, and are moved to their place.
 template <bool ALIGNED>
-__device__ __forceinline__ i32x4 load16(const int8_t *p, int count)
+__device__ __forceinline__ i32x4 load16(const int8_t *p, int count, unsigned inner)
 {
     if (count >= 16) return load16<ALIGNED>(p);
     i32x4 v = {0, 0, 0, 0};
+    if (count <= 0) return v;
+    if (inner < 16) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (i < count) v[i / 4] |= (int)(uint8_t)p[i] << (8 * (i % 4));
-    return v;
+        for (int i = 0; i < 16; ++i)
+            if (i < count) v[i / 4] |= (int)(uint8_t)p[i] << (8 * (i % 4));
+        return v;
+    }
+    const unsigned by = 16 - inner % 16;    // bytes that come too early: alike in all lanes
+    v = load16<false>(p - by);
+    if (by & 8) v = i32x4{v[2], v[3], 0, 0};
+    if (by & 4) v = i32x4{v[1], v[2], v[3], 0};
+    auto moved = [&](int high, int low) { return (int)__builtin_amdgcn_alignbyte((uint32_t)high, (uint32_t)low, by & 3); };
+    return i32x4{moved(v[1], v[0]), moved(v[2], v[1]), moved(v[3], v[2]), moved(0, v[3])};
 }
 
 // What leaves a block: results, or (SUMS) the sums of its part of the inner dimension, as the bits of Float32.

@@ -70,7 +70,7 @@ struct Side {
 #pragma unroll
         for (unsigned i = 0; i < kLoads; ++i)
             *reinterpret_cast<i32x4 *>(tile + (threadIdx.x / 64 * (R / 4) + i * 8) * kDeep + lane * 16) =
-                load16<true>(base + k + offset[i], (int)(inner - k) - (int)(chunk_of(i) * 16));
+                load16<true>(base + k + offset[i], (int)(inner - k) - (int)(chunk_of(i) * 16), inner);
     }
 };
 
@@ -293,9 +293,9 @@ __global__ __launch_bounds__(64 * W) void q8_shared_inner_kernel(Operands a)
         const int there = (int)a.inner - (int)(s * 64 + k);
         i32x4 w1[OI], x1[TI];
 #pragma unroll
-        for (unsigned i = 0; i < OI; ++i) w1[i] = load16<ALIGNED>(w[i] + s * 64, there);
+        for (unsigned i = 0; i < OI; ++i) w1[i] = load16<ALIGNED>(w[i] + s * 64, there, a.inner);
 #pragma unroll
-        for (unsigned i = 0; i < TI; ++i) x1[i] = load16<ALIGNED>(x[i] + s * 64, there);
+        for (unsigned i = 0; i < TI; ++i) x1[i] = load16<ALIGNED>(x[i] + s * 64, there, a.inner);
         multiply(w1, x1);
     }
     // a lane has 4 neighbouring channels of a row
@@ -384,6 +384,7 @@ ktanh_status_t launch_product(const kq8_shape_t &s, const int8_t *x, size_t x_ro
             };
             if constexpr (O != SUMS) {
                 if (plan.kind == T256) return launch(q8_tile_kernel<256, 256, 2, O>);
+                if (plan.kind == T192) return launch(q8_tile_kernel<192, 256, 2, O>);
             }
             switch (plan.kind) {
             case T128: return launch(q8_tile_kernel<128, 128, 2, O>);

@@ -1,7 +1,8 @@
 // libktanh: rows of values, or of an activation's outputs, in 8-bit integers with a scale for each row.
 //
 // One pass: a row is held in registers between the search for its largest magnitude and its rounding (rows beyond 32768 BFloat16 or 16384
-// Float32 values are read twice).  Bound by memory: 3 bytes a BFloat16 value.
+// Float32 values are read twice).  Bound by memory: 3 bytes a BFloat16 value; 8192 rows of 16384 take 72 us (5.6 TB/s), behind GELU 85.  A block to a
+// row, of as many lanes as keep it in 8 vectors each: what a lane holds it needs again, and its rounding waits for the whole row's largest.
 #include "ktanh_codes.h"
 #include "ktanh_q8.h"
 #include "ktanh_stream_impl.h"
@@ -53,18 +54,24 @@ __global__ __launch_bounds__(THREADS) void q8_rows_kernel(const ELEM *x, unsigne
         const unsigned count = count_at(at);
         uint4 v = uint4{0u, 0u, 0u, 0u};
         if (count != 0) v = load_values<ALIGNED, true>(from + at, count);
-        return activated<ELEM, ACT, WIDE>(v, tab);
+        return v;
     };
     bool odd;
     uint32_t m = 0;
     uint4 v[R == 0 ? 1 : R];
     if constexpr (R == 0) {
-        for (unsigned at = 0; at < cols; at += THREADS * N) m = larger(m, largest_of_lane<ELEM>(load(at + threadIdx.x * N), odd));
+        for (unsigned at = 0; at < cols; at += THREADS * N)
+            m = larger(m, largest_of_lane<ELEM>(activated<ELEM, ACT, WIDE>(load(at + threadIdx.x * N), tab), odd));
     } else {
 #pragma unroll
         for (unsigned r = 0; r < R; ++r) v[r] = load((r * THREADS + threadIdx.x) * N);
 #pragma unroll
-        for (unsigned r = 0; r < R; ++r) m = larger(m, largest_of_lane<ELEM>(v[r], odd));
+        for (unsigned r = 0; r < R; ++r) {
+            v[r] = activated<ELEM, ACT, WIDE>(v[r], tab);
+            m = larger(m, largest_of_lane<ELEM>(v[r], odd));
+            // one after the other: all at once take 193 registers a lane where these take 64 (8192 rows of 16384 behind GELU 152 us against 85)
+            if constexpr (ACT != KQ8_NONE) __builtin_amdgcn_sched_barrier(0);
+        }
     }
     m = largest_of_block<THREADS>(m, part);
     const bool finite = m < kInf;
@@ -83,7 +90,7 @@ __global__ __launch_bounds__(THREADS) void q8_rows_kernel(const ELEM *x, unsigne
     };
     if constexpr (R == 0) {
         for (unsigned at = 0; at < cols; at += THREADS * N) {
-            const uint4 w = load(at + threadIdx.x * N);
+            const uint4 w = activated<ELEM, ACT, WIDE>(load(at + threadIdx.x * N), tab);
             store(at + threadIdx.x * N, w);
         }
     } else {
@@ -111,6 +118,8 @@ ktanh_status_t launch_rows(const kq8_shape_t &s, const void *x, int8_t *codes, s
         constexpr bool ALIGNED = decltype(on_grid)::value;
         const size_t vectors = (s.inner + N - 1) / N;
         if (vectors <= 64) return launch(q8_rows_kernel<ELEM, ACT, WIDE, ALIGNED, 64, 1>, 64);
+        // 8192 rows of 1024: 6.7 us, behind GELU 8.9; with the next blocks 8.1 and 12.9
+        if (vectors <= 128) return launch(q8_rows_kernel<ELEM, ACT, WIDE, ALIGNED, 128, 1>, 128);
         if (vectors <= 256) return launch(q8_rows_kernel<ELEM, ACT, WIDE, ALIGNED, 256, 1>, 256);
         if (vectors <= 512) return launch(q8_rows_kernel<ELEM, ACT, WIDE, ALIGNED, 256, 2>, 256);
         if (vectors <= 1024) return launch(q8_rows_kernel<ELEM, ACT, WIDE, ALIGNED, 256, 4>, 256);
