@@ -11,7 +11,7 @@
 // lanes add to them.  Sums over bins and over sorted tokens are doubles in a fixed order.
 //
 // A block holds up to 32768 logits in registers.  Rows of no more take one launch, and are read once.  Longer ones are cut into chunks and take
-// four: the chunks' largest logits, their bins, their tokens of the bins that hold answers, and one block for the answers.
+// three: the chunks' largest logits, their bins, and their tokens of the bins that hold answers, among which the row's last block chooses.
 // Sums over the bins and over the listed tokens are formed once, with barriers; questions are then searches that every wavefront makes for
 // itself, with none.
 #include "ktanh_codes.h"
@@ -57,8 +57,8 @@ struct SampleArgs {
     long long *tokens;
     // of rows in chunks: by row and chunk, and by row
     u64 *bins, *list;
-    float4 *ends;       // the largest logit, the smallest, whether there is a NaN, the index of the largest
-    uint32_t *by_min, *listed;
+    float4 *ends;       // the largest logit, the smallest, the largest magnitude (the bits of a NaN if there is one), the index of the largest
+    uint32_t *by_min, *listed, *arrived;
 };
 
 // A value that all lanes have alike, in scalar registers: the vector ones hold the logits.
@@ -129,23 +129,35 @@ struct Near {
 };
 constexpr Near kAll{0.f, 0.f, 1.f};
 
-// Logits of `first` .. `end` - 1 in a block's registers, E to a lane.
+// Logits of `first` .. `end` - 1 for a block, E to a lane, asked for.
+template <class ELEM, unsigned E>
+struct OnTheWay {
+    static constexpr unsigned N = kPerLane<ELEM>;
+    uint4 v[E / N];
+    unsigned first, end;
+
+    OnTheWay() = default;
+    __device__ __forceinline__ OnTheWay(const ELEM *from, unsigned first, unsigned end) : first(first), end(end)
+    {
+#pragma unroll
+        for (unsigned i = 0; i < E / N; ++i) v[i] = load_logits(from, first + (i * kThreads + threadIdx.x) * N, end);
+    }
+};
+
+// The same in a block's registers.
 template <class ELEM, bool CAP, bool WIDE, unsigned E>
 struct Held {
     static constexpr unsigned N = kPerLane<ELEM>;
     float z[E / N][N];
     unsigned first;
 
-    __device__ __forceinline__ Held(const ELEM *from, unsigned first, unsigned end, float cap, const LaneTable &tab) : first(first)
+    __device__ __forceinline__ Held(const OnTheWay<ELEM, E> &raw, float cap, const LaneTable &tab) : first(raw.first)
     {
-        uint4 raw[E / N];
-#pragma unroll
-        for (unsigned v = 0; v < E / N; ++v) raw[v] = load_logits(from, place(v), end);
 #pragma unroll
         for (unsigned v = 0; v < E / N; ++v) {
-            widen<ELEM>(raw[v], z[v]);
+            widen<ELEM>(raw.v[v], z[v]);
 #pragma unroll
-            for (unsigned i = 0; i < N; ++i) z[v][i] = logit_of<CAP, WIDE>(z[v][i], place(v) + i < end, cap, tab);
+            for (unsigned i = 0; i < N; ++i) z[v][i] = logit_of<CAP, WIDE>(z[v][i], place(v) + i < raw.end, cap, tab);
             if constexpr (CAP) {    // one vector at a time: all at once do not fit the registers
 #pragma unroll
                 for (unsigned i = 0; i < N; ++i) asm volatile("" : "+v"(z[v][i]));
@@ -217,9 +229,9 @@ constexpr unsigned kWaves = kThreads / 64;
 struct Shared {
     Mass part[kWaves];
     float top[kWaves], low[kWaves];
-    uint32_t strange[kWaves], first[kWaves];
+    uint32_t widest[kWaves], first[kWaves];
     unsigned from[4], to[4];        // bins that the plan lists
-    double power[1u << kSteps];     // 2^(-j / 128)
+    double power[1u << kSteps];     // 2^(32 - j / 128)
     u64 bins[kBins];                // count << 48 | mass
     uint32_t count[kBins];          // of all bins up to each
     double mass[kBins];
@@ -283,6 +295,7 @@ __device__ __forceinline__ unsigned first_where(unsigned n, F holds)
     const u64 ends = __ballot(end < n ? holds(end) : lane * step < n && holds(n - 1));
     if (ends == 0) return n;
     const unsigned first = (unsigned)__builtin_ctzll(ends) * step;
+    if (n <= 64) return first;
     const u64 inside = __ballot(lane < step && at(first + lane));
     return inside == 0 ? n - 1 : first + (unsigned)__builtin_ctzll(inside);
 }
@@ -331,26 +344,25 @@ __device__ __forceinline__ void sort_list(Shared &sh, unsigned n)
 // What a source's logits tell before any weight: the largest, the smallest that is not masked (infinity if all are), and whether there is a NaN.
 struct Ends {
     float top, low;
-    bool strange;
-    __device__ __forceinline__ void meet(float t, float l, bool s)
+    uint32_t widest;    // magnitude, as bits
+    __device__ __forceinline__ void meet(float t, float l, uint32_t m)
     {
-        top = t > top ? t : top;
-        low = l < low ? l : low;
-        strange = strange || s;
+        top = __builtin_fmaxf(top, t);
+        low = __builtin_fminf(low, l);
+        widest = m > widest ? m : widest;
     }
+    __device__ __forceinline__ bool strange() const { return widest > 0x7F800000u; }
     // A row without a token to choose from.
-    __device__ __forceinline__ bool empty() const { return strange || top == -INFINITY; }
+    __device__ __forceinline__ bool empty() const { return strange() || top == -INFINITY; }
 };
-constexpr Ends kNoEnds{-INFINITY, INFINITY, false};
+constexpr Ends kNoEnds{-INFINITY, INFINITY, 0};
 
 template <int CTRL, int ROWS>
 __device__ __forceinline__ void meet_moved(Ends &e)     // lanes that none moves to meet themselves
 {
-    auto other = [](float v) {
-        const int u = (int)__float_as_uint(v);
-        return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(u, u, CTRL, ROWS, 0xF, false));
-    };
-    e.meet(other(e.top), other(e.low), false);
+    auto bits = [](uint32_t u) { return (uint32_t)__builtin_amdgcn_update_dpp((int)u, (int)u, CTRL, ROWS, 0xF, false); };
+    auto other = [&](float v) { return __uint_as_float(bits(__float_as_uint(v))); };
+    e.meet(other(e.top), other(e.low), bits(e.widest));
 }
 // Of all lanes of a wavefront, in all of them.
 __device__ __forceinline__ Ends met(Ends e)
@@ -361,24 +373,24 @@ __device__ __forceinline__ Ends met(Ends e)
     meet_moved<0x118, 0xF>(e);
     meet_moved<0x142, 0xA>(e);
     meet_moved<0x143, 0xC>(e);
-    auto last = [](float v) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63)); };
-    return Ends{last(e.top), last(e.low), __any(e.strange) != 0};
+    auto last = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); };
+    return Ends{__uint_as_float(last(__float_as_uint(e.top))), __uint_as_float(last(__float_as_uint(e.low))), last(e.widest)};
 }
 
 template <class SOURCE>
 __device__ __forceinline__ Ends ends_of(SOURCE &source, Shared &sh)
 {
     Ends e = kNoEnds;
-    source.each([&](float z, unsigned) { e.meet(z, z == -INFINITY ? INFINITY : z, z != z); });
+    source.each([&](float z, unsigned) { e.meet(z, z == -INFINITY ? INFINITY : z, __float_as_uint(z) & 0x7FFFFFFFu); });
     e = met(e);
     if (threadIdx.x % 64 == 0) {
         sh.top[threadIdx.x / 64] = e.top;
         sh.low[threadIdx.x / 64] = e.low;
-        sh.strange[threadIdx.x / 64] = e.strange;
+        sh.widest[threadIdx.x / 64] = e.widest;
     }
     __syncthreads();
     const unsigned part = threadIdx.x % kWaves;
-    return met(Ends{sh.top[part], sh.low[part], sh.strange[part] != 0});
+    return met(Ends{sh.top[part], sh.low[part], sh.widest[part]});
 }
 
 // The lowest index of a logit equal to `top`, or what is above all indices.
@@ -407,6 +419,9 @@ struct Weights {
     bool infinite;      // the largest logit is: only its like have a weight
     double scale;
     unsigned shift;     // kSteps less the log2 of the bins to a factor of two
+    // In scalar registers: as literals they would be moved to vector ones for every logit.
+    double magic = 0x1.8p45;        // its last place is 2^-kSteps
+    double series[4] = {-0.69314718055994530942, 0.24022650695910071233, -0.05550410866482157995, 0.00961812910762847716};
 
     __device__ __forceinline__ Weights(const Ends &e, double scale) : top(e.top), infinite(e.top == INFINITY), scale(scale)
     {
@@ -414,6 +429,7 @@ struct Weights {
         unsigned by = 0;    // kBins = 8 << kSteps
         while (by < 4 && range > (double)(7u << by)) ++by;
         shift = uniform(by);
+        asm volatile("" : "+s"(magic), "+s"(series[0]), "+s"(series[1]), "+s"(series[2]), "+s"(series[3]));
     }
     // Not below kFar, or a NaN: no weight.
     __device__ __forceinline__ double depth_of(float z) const
@@ -421,58 +437,57 @@ struct Weights {
         if (infinite) return z == top ? 0.0 : (double)INFINITY;
         return ((double)top - (double)z) * scale;
     }
-    // A depth below kFar in steps of 2^-kSteps, and the weight as a part of the power of two above it: 2^-(steps % 128 / 128) 2^-r, |r| <= 2^-8, by a table and
-    // four terms of the exponential series (the fifth is below 2e-15).
-    __device__ __forceinline__ double part_of(double depth, const double *power, unsigned &steps) const
+    // A depth below kFar in steps of 2^-kSteps, and the weight in 2^-32 of the power of two above it, as the product of 2^(32 - steps % 128 / 128) from a table and
+    // 2^-r, |r| <= 2^-8, by four terms of its series (the fifth is below 2e-15).
+    __device__ __forceinline__ double part_of(double depth, unsigned &steps) const
     {
-        constexpr double kMagic = 0x1.8p45;     // its last place is 2^-kSteps
-        const double y = depth + kMagic, r = (depth - (y - kMagic)) * -0.6931471805599453;
+        const double y = depth + magic, r = depth - (y - magic);
         steps = (unsigned)__double_as_longlong(y);
-        const double series = __builtin_fma(__builtin_fma(__builtin_fma(__builtin_fma(r, 1.0 / 24, 1.0 / 6), r, 0.5), r, 1.0), r, 1.0);
-        return power[steps & 127u] * series;
+        return __builtin_fma(__builtin_fma(__builtin_fma(__builtin_fma(r, series[3], series[2]), r, series[1]), r, series[0]), r, 1.0);
     }
     __device__ __forceinline__ double weight_of(float z, const double *power) const
     {
         const double depth = depth_of(z);
         if (!(depth < kFar)) return 0.0;
         unsigned steps;
-        const double part = part_of(depth, power, steps);
-        return ldexp(part, -(int)(steps >> kSteps));
+        const double part = part_of(depth, steps);
+        return ldexp(power[steps & 127u] * part, -32 - (int)(steps >> kSteps));
     }
     __device__ __forceinline__ unsigned bin_of(unsigned steps) const
     {
         const unsigned b = steps >> shift;
         return b < kBins - 1 ? b : kBins - 1;
     }
-    __device__ __forceinline__ unsigned steps_of(double depth) const { return (unsigned)__double_as_longlong(depth + 0x1.8p45); }
+    __device__ __forceinline__ unsigned steps_of(double depth) const { return (unsigned)__double_as_longlong(depth + magic); }
     // The power of two that a bin's mass is held in.
     __device__ __forceinline__ double unit_of(unsigned bin) const { return ldexp(1.0, -32 - (int)(bin >> (kSteps - shift))); }
 };
 
 constexpr u64 kOneToken = 1ull << 48, kMassBits = kOneToken - 1;
 
-// By the bits of j: 2^(-1/128), 2^(-1/64) and so on.
+// 2^(32 - j / 128), by the bits of j: 2^(-1/128), 2^(-1/64) and so on.
 __device__ __forceinline__ void fill_powers(Shared &sh)
 {
     constexpr double kPowers[kSteps] = {0.99459942348363317565, 0.98922801319397548413, 0.97857206208770013453, 0.95760328069857364694,
                                         0.91700404320467123174, 0.84089641525371454303, 0.70710678118654752440};
     if (threadIdx.x >= 1u << kSteps) return;
-    double v = 1.0;
+    double v = 0x1p32;
 #pragma unroll
     for (unsigned i = 0; i < kSteps; ++i) v *= threadIdx.x >> i & 1u ? kPowers[i] : 1.0;
     sh.power[threadIdx.x] = v;
 }
 
 // A token's count and mass for its bin.
-__device__ __forceinline__ u64 packed(double part)
+__device__ __forceinline__ u64 packed(double power, double part)
 {
-    return ((u64)__double_as_longlong(__builtin_fma(part, 0x1p32, 0x1p52)) & 0xFFFFFFFFFFFFFull) | kOneToken;     // part <= 1.003
+    return ((u64)__double_as_longlong(__builtin_fma(power, part, 0x1p52)) & 0xFFFFFFFFFFFFFull) | kOneToken;      // at most 1.003 2^32
 }
 
-// Where top-k leaves few tokens, the ones that may be among them: by counts alone, which cost less than weights.
+// Where top-k leaves few tokens, the ones that may be among them, and how many they are: by counts alone, which cost less than weights.
 template <class SOURCE>
-__device__ __forceinline__ Near nearest(SOURCE &source, const Ends &e, uint32_t k, Shared &sh)
+__device__ __forceinline__ Near nearest(SOURCE &source, const Ends &e, uint32_t k, uint32_t &tokens, Shared &sh)
 {
+    tokens = ~0u;
     const float width = e.top - e.low;
     if (!(width > 0.f && width < 3e38f)) return kAll;     // all alike, or an infinity
     const float by = (float)(kBins - 1) / width;
@@ -488,7 +503,8 @@ __device__ __forceinline__ Near nearest(SOURCE &source, const Ends &e, uint32_t 
     sh.count[threadIdx.x] = upto;
     __syncthreads();
     const unsigned last = first_where(kBins, [&](unsigned i) { return sh.count[i] >= k; });
-    return Near{e.top, by, (float)(last + 1)};      // bins 0 .. last; all if the tokens are fewer than k
+    tokens = uniform(sh.count[last < kBins ? last : kBins - 1]);
+    return uniform(Near{e.top, by, (float)(last + 1)});      // bins 0 .. last; all if the tokens are fewer than k
 }
 
 // Bins of a source of at most 32768 logits into sh.bins, and how many tokens min-p keeps into sh.by_min.
@@ -504,8 +520,8 @@ __device__ __forceinline__ void fill_bins(SOURCE &source, const Weights &w, doub
         const double depth = w.depth_of(z);
         if (!(depth < kFar)) return;
         unsigned steps;
-        const double part = w.part_of(depth, sh.power, steps);
-        atomicAdd(&sh.bins[w.bin_of(steps)], packed(part));
+        const double part = w.part_of(depth, steps);
+        atomicAdd(&sh.bins[w.bin_of(steps)], packed(sh.power[steps & 127u], part));
         kept += depth <= reach;
     });
     const Mass all = scanned(Mass{kept, 0.0});
@@ -529,6 +545,47 @@ __device__ __forceinline__ void list_flagged(SOURCE &source, const Weights &w, f
         if (at < kListed) sh.list[at] = place_of(key_of(z), i);
     });
     __syncthreads();
+}
+
+// The near tokens, at most kListed, into sh.list, unsorted.
+template <class SOURCE>
+__device__ __forceinline__ void list_near(SOURCE &source, const Weights &w, const Near &near, Shared &sh)
+{
+    if (threadIdx.x == 0) sh.listed = 0;
+    __syncthreads();
+    source.each([&](float z, unsigned i) {
+        if (!near(z) || !(w.depth_of(z) < kFar)) return;
+        sh.list[atomicAdd(&sh.listed, 1u)] = place_of(key_of(z), i);
+    });
+    __syncthreads();
+}
+
+// Sorts n listed tokens and sums their weights.
+__device__ __forceinline__ void finish_list(const Weights &w, unsigned n, Shared &sh)
+{
+    sort_list(sh, n);
+    const unsigned i = threadIdx.x * 2;
+    auto weight = [&](unsigned at) { return at < n ? w.weight_of(value_of_key(~(uint32_t)(sh.list[at] >> 32)), sh.power) : 0.0; };
+    const double w0 = weight(i), w1 = weight(i + 1);
+    const double upto = sum_up_to(Mass{0, w0 + w1}, sh).mass;
+    sh.list_mass[i] = upto - w1;
+    sh.list_mass[i + 1] = upto;
+    __syncthreads();
+}
+
+// The token where all that can be chosen are listed and sorted, n of them: no bins are needed.  The first wavefront's work.
+__device__ __forceinline__ long long choose_listed(const Weights &w, const Settings &s, unsigned n, const Shared &sh)
+{
+    if (s.top_k < n) n = s.top_k;
+    if (s.top_p < 1.0) {
+        const double most = s.top_p * sh.list_mass[n - 1];
+        const unsigned i = uniform(first_where(n, [&](unsigned i) { return sh.list_mass[i] >= most; }));
+        n = i < n ? i + 1 : n;
+    }
+    if (s.reach < kFar) n = uniform(first_where(n, [&](unsigned i) { return w.depth_of(value_of_key(~(uint32_t)(sh.list[i] >> 32))) > s.reach; }));
+    const double most = s.u * sh.list_mass[n - 1];
+    const unsigned i = uniform(first_where(n, [&](unsigned i) { return sh.list_mass[i] > most; }));
+    return (long long)(uint32_t)sh.list[i < n ? i : n - 1];
 }
 
 // ------------------------------------------------------------------------------------ questions
@@ -643,19 +700,6 @@ struct Questions {
         low_logit = uniform(low_logit);
     }
 
-    // Sorts n listed tokens and sums their weights.
-    __device__ __forceinline__ void finish_list(unsigned n)
-    {
-        sort_list(sh, n);
-        const unsigned i = threadIdx.x * 2;
-        auto weight = [&](unsigned at) { return at < n ? w.weight_of(value_of_key(~(uint32_t)(sh.list[at] >> 32)), sh.power) : 0.0; };
-        const double w0 = weight(i), w1 = weight(i + 1);
-        const double upto = sum_up_to(Mass{0, w0 + w1}, sh).mass;
-        sh.list_mass[i] = upto - w1;
-        sh.list_mass[i + 1] = upto;
-        __syncthreads();
-    }
-
     // Lists the tokens of a bin of more than kListed that are near the answer: bins of places inside it, until they are few.  `before` moves up to them.
     template <class SOURCE>
     __device__ __forceinline__ unsigned narrow(SOURCE &source, const Question &q, unsigned bin, Mass &before)
@@ -690,7 +734,8 @@ struct Questions {
                 if (p < first || p > last) return;
                 unsigned steps;
                 const unsigned b = (unsigned)((p - first) / step);
-                atomicAdd(&sh.bins[b], packed(w.part_of(depth, sh.power, steps)) & kMassBits);
+                const double part = w.part_of(depth, steps);
+                atomicAdd(&sh.bins[b], packed(sh.power[steps & 127u], part) & kMassBits);
                 atomicAdd(&sh.starts[b], 1u);
             });
             __syncthreads();
@@ -794,7 +839,7 @@ struct Questions {
                 n = narrow(source, Question{uniform(sh.asked_count), uniform(sh.asked_mass), sh.asked_above != 0}, bin, before);
                 flag(false);
             }
-            finish_list(n);
+            finish_list(w, n, sh);
             relisted = true;
         }
         return (long long)(uint32_t)sh.list[at];
@@ -808,8 +853,9 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, KtLutPac
 {
     __shared__ Shared sh;
     const LaneTable tab(pack);
+    const OnTheWay<ELEM, E> raw(static_cast<const ELEM *>(a.logits) + blockIdx.x * a.row, 0, a.vocabulary);
     const Settings s = settings_of(a, blockIdx.x);
-    Held<ELEM, CAP, WIDE, E> held(static_cast<const ELEM *>(a.logits) + blockIdx.x * a.row, 0, a.vocabulary, a.cap, tab);
+    Held<ELEM, CAP, WIDE, E> held(raw, a.cap, tab);
     const Ends e = ends_of(held, sh);
     long long token = -1;
     if (!e.empty()) {
@@ -818,17 +864,27 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, KtLutPac
         } else {
             const Weights w(e, s.scale);
             Near near = kAll;
-            if (s.top_k <= kListed && s.top_k < a.vocabulary) near = nearest(held, e, s.top_k, sh);
-            if (!near.all()) held.keep(near);
-            fill_bins(held, w, s.reach, sh);
-            Questions questions(w, s, sh, uniform(sh.by_min));
-            questions.add_up((uint32_t)(sh.bins[threadIdx.x] >> 48), sh.bins[threadIdx.x] & kMassBits);
-            questions.plan();
-            list_flagged(held, w, questions.low_logit, questions.high_logit, sh);
-            questions.finish_list(uniform(sh.listed));
+            uint32_t tokens = ~0u;
+            if (s.top_k <= kListed && s.top_k < a.vocabulary) near = nearest(held, e, s.top_k, tokens, sh);
+            const bool few = tokens <= kRanked;
+            Questions questions(w, s, sh, 0);
+            if (few) {
+                fill_powers(sh);
+                list_near(held, w, near, sh);
+            } else {
+                if (!near.all()) held.keep(near);
+                fill_bins(held, w, s.reach, sh);
+                questions.by_min = uniform(sh.by_min);
+                questions.add_up((uint32_t)(sh.bins[threadIdx.x] >> 48), sh.bins[threadIdx.x] & kMassBits);
+                questions.plan();
+                list_flagged(held, w, questions.low_logit, questions.high_logit, sh);
+            }
+            const unsigned n = uniform(sh.listed);
+            finish_list(w, n, sh);
             // another list than the plan's, if one is needed, comes from memory: the registers are the questions'
             Read<ELEM, CAP, WIDE> read{static_cast<const ELEM *>(a.logits) + blockIdx.x * a.row, a.vocabulary, a.cap, tab, near};
-            token = questions.choose(read);
+            if (!few) token = questions.choose(read);
+            else if (threadIdx.x < 64) token = choose_listed(w, s, n, sh);
         }
     }
     if (threadIdx.x == 0) a.tokens[blockIdx.x] = token;
@@ -850,9 +906,10 @@ __device__ __forceinline__ Where chunk_of(const SampleArgs &a)
 __device__ __forceinline__ Ends row_ends(const SampleArgs &a, unsigned row)
 {
     Ends e = kNoEnds;
+#pragma unroll 4
     for (unsigned c = 0; c < a.chunks; ++c) {
         const float4 v = a.ends[row * (u64)a.chunks + c];
-        e.meet(v.x, v.y, v.z != 0.f);
+        e.meet(v.x, v.y, __float_as_uint(v.z));
     }
     return e;
 }
@@ -862,6 +919,7 @@ __device__ __forceinline__ void add_up_row(const SampleArgs &a, unsigned row, Qu
 {
     uint32_t count = 0, by_min = 0;
     u64 mass = 0;
+#pragma unroll 4
     for (unsigned c = 0; c < a.chunks; ++c) {
         const u64 at = row * (u64)a.chunks + c, v = a.bins[at * kBins + threadIdx.x];
         count += (uint32_t)(v >> 48);
@@ -879,80 +937,85 @@ __global__ __launch_bounds__(kThreads) void sample_ends_kernel(SampleArgs a, KtL
     __shared__ Shared sh;
     const LaneTable tab(pack);
     const Where at = chunk_of<E>(a);
-    Held<ELEM, CAP, WIDE, E> held(static_cast<const ELEM *>(a.logits) + at.row * a.row, at.first, at.end, a.cap, tab);
+    const OnTheWay<ELEM, E> raw(static_cast<const ELEM *>(a.logits) + at.row * a.row, at.first, at.end);
+    Held<ELEM, CAP, WIDE, E> held(raw, a.cap, tab);
     const Ends e = ends_of(held, sh);
     const uint32_t first = settings_of(a, at.row).greedy ? first_of(held, e.top, sh) : 0u;
     if (threadIdx.x == 0) {
-        a.ends[blockIdx.x] = float4{e.top, e.low, e.strange ? 1.f : 0.f, __uint_as_float(first)};
-        if (at.first == 0) a.listed[at.row] = 0;
+        a.ends[blockIdx.x] = float4{e.top, e.low, __uint_as_float(e.widest), __uint_as_float(first)};
+        if (at.first == 0) a.listed[at.row] = a.arrived[at.row] = 0;
     }
 }
 
 template <class ELEM, bool CAP, bool WIDE, unsigned E>
-__global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a, KtLutPack pack)
+__global__ __launch_bounds__(kThreads, 8) void sample_bins_kernel(SampleArgs a, KtLutPack pack)
 {
     __shared__ Shared sh;
     const LaneTable tab(pack);
     const Where at = chunk_of<E>(a);
+    const OnTheWay<ELEM, E> raw(static_cast<const ELEM *>(a.logits) + at.row * a.row, at.first, at.end);
     const Settings s = settings_of(a, at.row);
     const Ends e = row_ends(a, at.row);
     if (e.empty() || s.greedy) return;
-    Held<ELEM, CAP, WIDE, E> held(static_cast<const ELEM *>(a.logits) + at.row * a.row, at.first, at.end, a.cap, tab);
+    Held<ELEM, CAP, WIDE, E> held(raw, a.cap, tab);
     fill_bins(held, Weights(e, s.scale), s.reach, sh);
     a.bins[blockIdx.x * (u64)kBins + threadIdx.x] = sh.bins[threadIdx.x];
     if (threadIdx.x == 0) a.by_min[blockIdx.x] = sh.by_min;
 }
 
+// The chunks' tokens of the bins that hold answers; the block that is the row's last to have listed its own has them all, and answers.  None waits for
+// another.
 template <class ELEM, bool CAP, bool WIDE, unsigned E>
-__global__ __launch_bounds__(kThreads) void sample_list_kernel(SampleArgs a, KtLutPack pack)
+__global__ __launch_bounds__(kThreads, 8) void sample_answer_kernel(SampleArgs a, KtLutPack pack)
 {
     __shared__ Shared sh;
     const LaneTable tab(pack);
     const Where at = chunk_of<E>(a);
+    const ELEM *const from = static_cast<const ELEM *>(a.logits) + at.row * a.row;
+    // asked for before all else, where the registers are enough for that and for two blocks on a CU
+    constexpr bool kEarly = sizeof(ELEM) * E <= 64;
+    OnTheWay<ELEM, E> raw;
+    if constexpr (kEarly) raw = OnTheWay<ELEM, E>(from, at.first, at.end);
     const Settings s = settings_of(a, at.row);
     const Ends e = row_ends(a, at.row);
-    if (e.empty() || s.greedy) return;
+    if (e.empty() || s.greedy) {
+        if (at.first != 0 || threadIdx.x != 0) return;
+        long long token = -1;
+        for (unsigned c = a.chunks; c-- > 0 && !e.empty();) {   // the first chunk with the largest logit
+            const float4 v = a.ends[at.row * (u64)a.chunks + c];
+            if (v.x == e.top) token = (long long)__float_as_uint(v.w);
+        }
+        a.tokens[at.row] = token;
+        return;
+    }
     const Weights w(e, s.scale);
+    fill_powers(sh);
     Questions questions(w, s, sh, 0);
     add_up_row(a, at.row, questions);
-    Held<ELEM, CAP, WIDE, E> held(static_cast<const ELEM *>(a.logits) + at.row * a.row, at.first, at.end, a.cap, tab);
-    list_flagged(held, w, questions.low_logit, questions.high_logit, sh);
-    const unsigned n = sh.listed;       // at most kListed: the plan's
-    if (threadIdx.x == 0) sh.by_min = atomicAdd(&a.listed[at.row], n);
-    __syncthreads();
-    const unsigned start = sh.by_min;
-    for (unsigned i = threadIdx.x; i < n; i += kThreads)
-        if (start + i < kListed) a.list[at.row * (u64)kListed + start + i] = sh.list[i];
-}
-
-template <class ELEM, bool CAP, bool WIDE>
-__global__ __launch_bounds__(kThreads) void sample_answer_kernel(SampleArgs a, KtLutPack pack)
-{
-    __shared__ Shared sh;
-    const LaneTable tab(pack);
-    const unsigned row = blockIdx.x;
-    const Settings s = settings_of(a, row);
-    const Ends e = row_ends(a, row);
-    long long token = -1;
-    if (!e.empty()) {
-        if (s.greedy) {
-            for (unsigned c = a.chunks; c-- > 0;) {     // the first chunk with the largest logit
-                const float4 v = a.ends[row * (u64)a.chunks + c];
-                if (v.x == e.top) token = (long long)__float_as_uint(v.w);
-            }
-        } else {
-            const Weights w(e, s.scale);
-            fill_powers(sh);
-            Questions questions(w, s, sh, 0);
-            add_up_row(a, row, questions);
-            const unsigned listed = a.listed[row], n = listed < kListed ? listed : kListed;
-            for (unsigned i = threadIdx.x; i < n; i += kThreads) sh.list[i] = a.list[row * (u64)kListed + i];
-            questions.finish_list(n);
-            Read<ELEM, CAP, WIDE> read{static_cast<const ELEM *>(a.logits) + row * a.row, a.vocabulary, a.cap, tab, kAll};
-            token = questions.choose(read);
-        }
+    {
+        if constexpr (!kEarly) raw = OnTheWay<ELEM, E>(from, at.first, at.end);
+        Held<ELEM, CAP, WIDE, E> held(raw, a.cap, tab);
+        list_flagged(held, w, questions.low_logit, questions.high_logit, sh);
     }
-    if (threadIdx.x == 0) a.tokens[row] = token;
+    const unsigned mine = uniform(sh.listed);       // at most kListed: the plan's
+    if (threadIdx.x == 0) sh.asked_bin = atomicAdd(&a.listed[at.row], mine);
+    __syncthreads();
+    u64 *const list = a.list + at.row * (u64)kListed;
+    for (unsigned i = threadIdx.x; i < mine; i += kThreads)
+        if (sh.asked_bin + i < kListed) __hip_atomic_store(&list[sh.asked_bin + i], sh.list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // These stores go to where all dies see them, and are there before the block counts as arrived.  A fence of the whole GPU would write every L2 back, each
+    // wavefront's once more: 64 rows of 131072 took 145 us with them.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) sh.asked = atomicAdd(&a.arrived[at.row], 1u) + 1 == a.chunks;
+    __syncthreads();
+    if (uniform(sh.asked) == 0) return;
+    const unsigned listed = uniform(__hip_atomic_load(&a.listed[at.row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)), n = listed < kListed ? listed : kListed;
+    for (unsigned i = threadIdx.x; i < n; i += kThreads) sh.list[i] = __hip_atomic_load(&list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    finish_list(w, n, sh);
+    Read<ELEM, CAP, WIDE> read{from, a.vocabulary, a.cap, tab, kAll};
+    const long long token = questions.choose(read);
+    if (threadIdx.x == 0) a.tokens[at.row] = token;
 }
 
 // ------------------------------------------------------------------------------------ host side
@@ -978,7 +1041,8 @@ Cut cut_of(size_t rows, size_t vocabulary)
     auto chunks = [&](unsigned each) { return (vocabulary + each * kThreads - 1) / (each * kThreads); };
     if (vocabulary <= kFew * kThreads) return Cut{kFew, 1};
     if (vocabulary <= kMost * kThreads) return Cut{kMost, 1};
-    return rows * chunks(kMost) >= 192 ? Cut{kMost, chunks(kMost)} : Cut{kFew, chunks(kFew)};
+    // chunks of 8192 where each has a CU (32 rows of 50000: 27 us, 33 with chunks of 32768), of 32768 beyond (32 rows of 131072: 37 us against 51)
+    return rows * chunks(kFew) <= 256 ? Cut{kFew, chunks(kFew)} : Cut{kMost, chunks(kMost)};
 }
 
 template <class Lut>
@@ -1016,7 +1080,7 @@ ktanh_status_t sample_entry(const ksample_shape_t *s, const void *logits, const 
     a.tokens = reinterpret_cast<long long *>(tokens);
     a.bins = a.list = nullptr;
     a.ends = nullptr;
-    a.by_min = a.listed = nullptr;
+    a.by_min = a.listed = a.arrived = nullptr;
     const size_t rows = s->rows, blocks = rows * a.chunks;
     if (a.chunks > 1) {
         if (workspace == nullptr) return KT_ERR_NULL;
@@ -1025,6 +1089,7 @@ ktanh_status_t sample_entry(const ksample_shape_t *s, const void *logits, const 
         a.ends = reinterpret_cast<float4 *>(a.list + rows * kListed);
         a.by_min = reinterpret_cast<uint32_t *>(a.ends + blocks);
         a.listed = a.by_min + blocks;
+        a.arrived = a.listed + rows;
     }
     if (blocks * kThreads >= (size_t)1 << 32) return KT_ERR_SHAPE;
     auto launch = [&](auto kernel, size_t n) { return launch_checked(kernel, (unsigned)n, kThreads, stream, a, pack); };
@@ -1036,8 +1101,7 @@ ktanh_status_t sample_entry(const ksample_shape_t *s, const void *logits, const 
             constexpr unsigned E = decltype(each)::value;
             ktanh_status_t done = launch(sample_ends_kernel<ELEM, CAP, W, E>, blocks);
             if (done == KT_OK) done = launch(sample_bins_kernel<ELEM, CAP, W, E>, blocks);
-            if (done == KT_OK) done = launch(sample_list_kernel<ELEM, CAP, W, E>, blocks);
-            return done == KT_OK ? launch(sample_answer_kernel<ELEM, CAP, W>, rows) : done;
+            return done == KT_OK ? launch(sample_answer_kernel<ELEM, CAP, W, E>, blocks) : done;
         };
         return cut.each == kFew ? chunked(std::integral_constant<unsigned, kFew>()) : chunked(std::integral_constant<unsigned, kMost>());
     };
@@ -1051,7 +1115,7 @@ extern "C" size_t ksample_workspace(const ksample_shape_t *shape)
 {
     if (check_shape(shape) != KT_OK) return 0;
     const size_t chunks = cut_of(shape->rows, shape->vocabulary).chunks, blocks = shape->rows * chunks;
-    return chunks == 1 ? 0 : blocks * (kBins * sizeof(u64) + sizeof(float4) + sizeof(uint32_t)) + shape->rows * (kListed * sizeof(u64) + sizeof(uint32_t));
+    return chunks == 1 ? 0 : blocks * (kBins * sizeof(u64) + sizeof(float4) + sizeof(uint32_t)) + shape->rows * (kListed * sizeof(u64) + 2 * sizeof(uint32_t));
 }
 extern "C" ktanh_status_t ksample(const ksample_shape_t *shape, const void *logits, const float *uniform, const float *temperature, const int32_t *top_k,
                                   const float *top_p, const float *min_p, int64_t *tokens, void *workspace, const ktanh_lut_t *lut, ktanh_stream_t stream)
