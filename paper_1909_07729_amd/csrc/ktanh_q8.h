@@ -35,34 +35,44 @@ inline ktanh_status_t check_product(const kq8_shape_t *s)
 //
 // The plan is the one that takes least by a model of what steps, rounds of blocks, memory and launches cost.  Its numbers are measured, us of calls on
 // weights out of the cache, by the model's choice | the others:
-//     1 x 4096 x 4096   SHARED 5.9 | 64x64 10.7                  256 x 4096 x 4096    64x64 12.8 | 128x64 18.5, 128x128 31.6
-//    16 x 16384 x 4096  64x64 in 4 parts 22.4 | 1 part 35.6      512 x 16384 x 1024   128x64 in 4 parts 23.6 | 1 part 54.2
-//    64 x 1024 x 1024   SHARED 3.4 | 64x64 5.1                  1024 x 4096 x 4096    128x64 32.5 | 128x128 35.2, 256x256 62.0
-//    64 x 4096 x 16384  64x64 19.4 | 128x64 23.3, SHARED 74.6   2048 x 4096 x 4096    128x128 42.9 | 256x256 63.7, 128x64 59.9
-//   128 x 4096 x 4096   64x64 10.9 | 128x64 14.0, SHARED 35.5   2048 x 4096 x 6144    192x256 54.2 | 256x256 65.5, 128x128 73.6
+//     1 x 4096 x 4096   SHARED 5.9 | 64x64 10.7                  128 x 4096 x 16384   128x64 23.7 | 64x64 26.9, 128x128 27.9, SHARED 139
+//    16 x 16384 x 4096  SHARED 23.3 | 64x64 in 4 parts 22.4,     256 x 4096 x 4096    64x64 11.8 | 128x64 14.3, 128x128 19.3
+//                       in one 35.5                              512 x 4096 x 4096    128x64 17.2 | 64x64 18.0, 128x128 21.5
+//    24 x 2048 x 50000  128x32 23.8 | 128x64 24.9, 64x64 26.5    512 x 16384 x 1024   128x64 in 4 parts 23.6 | in one 54.2
+//    64 x 1024 x 1024   SHARED 3.4 | 64x64 5.1                  1024 x 4096 x 4096    128x128 25.3 | 128x64 31.3, 256x256 61.4
+//    64 x 4096 x 16384  64x64 19.2 | 128x64 22.9, SHARED 74.5   2048 x 4096 x 4096    128x128 41.1 | 192x256 52.9, 128x64 57.1
+//   128 x 4096 x 4096   64x64 11.1 | 128x64 14.0, SHARED 35.5   2048 x 4096 x 6144    192x256 54.2 | 256x256 65.5, 128x128 73.6
 //   128 x 1024 x 512    SHARED 3.4 | 64x64 5.1                  8192 x 16384 x 4096   256x256 481 | 128x128 536
-enum Kind { T256, T192, T128, T128_64, T64, SHARED };
+enum Kind { T256, T192, T128, T128_64, T64, T128_32, SHARED };
 struct Tile {
     unsigned over, across;      // output channels, rows
     double alone, together;     // us of a step of 128 integers of a block by itself on a CU, and of each of two
 };
-constexpr Tile kTiles[] = {{256, 256, 1.85, 1.9}, {192, 256, 1.45, 1.48}, {128, 128, 0.94, 0.59}, {128, 64, 0.35, 0.33}, {64, 64, 0.22, 0.216}, {16, 16, 0, 0}};
+constexpr Tile kTiles[] = {{256, 256, 1.85, 1.9}, {192, 256, 1.45, 1.48}, {128, 128, 0.94, 0.59}, {128, 64, 0.35, 0.41}, {64, 64, 0.22, 0.216}, {128, 32, 0.22, 0.216}, {16, 16, 0, 0}};
+constexpr double kRoomy = 0.71;     // of a T128 block with three places, where every block has a CU of its own
 
 struct Plan {
     Kind kind;
     unsigned parts;
 };
 
+inline double blocks_of(Kind kind, size_t rows, size_t outer, unsigned parts)
+{
+    const Tile &t = kTiles[kind];
+    return (double)((outer + t.over - 1) / t.over) * (double)((rows + t.across - 1) / t.across) * parts;
+}
+
 inline double us_of(Kind kind, unsigned parts, size_t rows, size_t inner, size_t outer)
 {
     const Tile &t = kTiles[kind];
-    const double blocks = (double)((outer + t.over - 1) / t.over) * (double)((rows + t.across - 1) / t.across) * parts;
+    const double blocks = blocks_of(kind, rows, outer, parts);
     const double rounds = blocks <= 256 ? 1 : (double)(size_t)((blocks + 255) / 256), pairs = (double)(size_t)(rounds / 2);
     double us;
     if (kind == SHARED) us = rounds * (0.5 + 0.48 * (double)((inner + 511) / 512));
-    else us = (double)((inner + 128 * parts - 1) / (128 * parts)) * (pairs * 2 * t.together + (rounds - pairs * 2) * t.alone);
-    // memory at 5 TB/s, less where not every CU has a block
-    const double memory = ((double)rows + (double)outer) * (double)inner / 5e6 * (blocks < 256 ? 1 + (256 - blocks) / 512 : 1);
+    else us = (double)((inner + 128 * parts - 1) / (128 * parts)) * (pairs * 2 * t.together + (rounds - pairs * 2) * (kind == T128 && blocks <= 256 ? kRoomy : t.alone));
+    // memory at 5 TB/s, less where not every CU has a block or tiles are read past the last row
+    double memory = ((double)rows + (double)outer) * (double)inner / 5e6 * (blocks < 256 ? 1 + (256 - blocks) / 512 : 1);
+    memory *= 1.2 - 0.2 * (double)rows / (double)((rows + t.across - 1) / t.across * t.across);
     if (us < memory) us = memory;
     us += kind == SHARED ? 2.5 : 3.5;
     if (parts > 1) us += 2.5 + (double)parts * (double)rows * (double)outer * 8 / 4e6;

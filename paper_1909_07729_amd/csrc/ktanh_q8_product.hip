@@ -47,7 +47,7 @@ struct Side {
     static constexpr unsigned kLoads = R / 32;
 
     // The chunk that a lane brings to place lane % 8 of row 8 i + lane / 8.
-    __device__ __forceinline__ static unsigned chunk_of(unsigned i) { return threadIdx.x % 8 ^ (4 * i + threadIdx.x % 64 / 16) % 8; }
+    __device__ __forceinline__ static unsigned chunk_of(unsigned i) { return threadIdx.x % 8 ^ (threadIdx.x / 64 * (R / 8) + 4 * i + threadIdx.x % 64 / 16) % 8; }
 
     __device__ __forceinline__ Side(const int8_t *rows, unsigned long long row, unsigned first, unsigned last)
     {
@@ -88,9 +88,10 @@ __device__ __forceinline__ Corner corner_of(unsigned block, unsigned over, unsig
 }
 
 template <unsigned TO, unsigned TT, unsigned PLACES, Out OUT>
-__global__ __launch_bounds__(256, TO * TT > 128 * 128 ? 1 : 2) void q8_tile_kernel(Operands a, unsigned over, unsigned across, unsigned parts)
+__global__ __launch_bounds__(256, PLACES * (TO + TT) * kDeep > 81920 ? 1 : 2) void q8_tile_kernel(Operands a, unsigned over, unsigned across, unsigned parts)
 {
-    constexpr unsigned OI = TO / 64, TI = TT / 64, kPlace = (TO + TT) * kDeep;
+    constexpr unsigned WT = TT < 64 ? 1 : 2, WO = 4 / WT;       // wavefronts side by side along the rows, and along the channels
+    constexpr unsigned OI = TO / WO / 32, TI = TT / WT / 32, kPlace = (TO + TT) * kDeep;
     __shared__ __align__(16) char lds[PLACES * kPlace];
     const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const unsigned part = blockIdx.x / (over * across);
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(256, TO * TT > 128 * 128 ? 1 : 2) void q8_tile_kern
 #pragma unroll
         for (unsigned j = 0; j < TI; ++j) sum[i][j] = i32x16{0};
     // operands of 32 integers: a lane has 16 of one row
-    const unsigned w_at = (wave / 2 * (TO / 2) + lane % 32) * kDeep, x_at = TO * kDeep + (wave % 2 * (TT / 2) + lane % 32) * kDeep;
+    const unsigned w_at = (wave / WT * (TO / WO) + lane % 32) * kDeep, x_at = TO * kDeep + (wave % WT * (TT / WT) + lane % 32) * kDeep;
     i32x4 wf[2][OI], xf[2][TI];
     auto read = [&](const char *place, unsigned step) {
         const unsigned chunk = ((2 * step + lane / 32) ^ lane / 2 % 8) * 16;
@@ -187,10 +188,10 @@ __global__ __launch_bounds__(256, TO * TT > 128 * 128 ? 1 : 2) void q8_tile_kern
     // A lane has, of 32 channels and 32 rows, four times 4 neighbouring channels of one row.  The results of 32 rows go through a wavefront's own
     // place in LDS, and leave by whole rows of its channels: straight from the registers each store would touch 32 rows, 16 bytes of each.
     __syncthreads();
-    constexpr unsigned kSize = OUT == BF16 ? 2 : 4, kRow = TO / 2 * kSize, kPitch = kRow + 16, kChunks = kRow / 16;
+    constexpr unsigned kSize = OUT == BF16 ? 2 : 4, kRow = TO / WO * kSize, kPitch = kRow + 16, kChunks = kRow / 16;
     static_assert(4 * 32 * kPitch <= PLACES * kPlace, "four wavefronts' results");
     char *const mine = lds + wave * 32 * kPitch;
-    const unsigned o1 = o0 + wave / 2 * (TO / 2), t1 = t0 + wave % 2 * (TT / 2);
+    const unsigned o1 = o0 + wave / WT * (TO / WO), t1 = t0 + wave % WT * (TT / WT);
     const bool biased = a.bias != nullptr;
     if constexpr (OUT == SUMS) a.out = static_cast<float *>(a.out) + (unsigned long long)part * a.rows * a.outer;
     f32x4 channel[OI][4], bias[OI][4];
@@ -387,8 +388,10 @@ ktanh_status_t launch_product(const kq8_shape_t &s, const int8_t *x, size_t x_ro
                 if (plan.kind == T192) return launch(q8_tile_kernel<192, 256, 2, O>);
             }
             switch (plan.kind) {
-            case T128: return launch(q8_tile_kernel<128, 128, 2, O>);
+            // a third place where a CU has no second block anyway: 1024 x 4096 x 4096 26.3 us, 34.8 with two
+            case T128: return blocks_of(T128, s.rows, s.outer, plan.parts) <= 256 ? launch(q8_tile_kernel<128, 128, 3, O>) : launch(q8_tile_kernel<128, 128, 2, O>);
             case T128_64: return launch(q8_tile_kernel<128, 64, 3, O>);
+            case T128_32: return launch(q8_tile_kernel<128, 32, 3, O>);
             default: return launch(q8_tile_kernel<64, 64, 4, O>);
             }
         };

@@ -129,6 +129,24 @@ def test_products(gpu, rows, inner, outer, dtype):
     assert torch.equal(out.cpu(), _want(torch, codes, scales, weight, weight_scales, bias, out.dtype))
 
 
+# Every kind of tile with ends of rows, channels and inner dimension that fill none, in one part and in several (tests/test_q8_plans.py holds the plans to these).
+TILES = [(8190, 1040, 8190), (2040, 520, 6130), (2040, 1160, 4090), (1000, 656, 4000), (770, 1040, 2000), (900, 8200, 900), (24, 528, 50000), (30, 300, 30000),
+         (500, 16400, 1000), (100, 16400, 500), (1000, 131071, 70)]
+
+
+@pytest.mark.parametrize("rows, inner, outer", TILES)
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_products_in_tiles(gpu, rows, inner, outer, dtype):
+    torch, binding = gpu
+    pad = -inner % 16
+    codes, weight = _codes(torch, rows, inner, 1, pad), _codes(torch, outer, inner, 2, pad)
+    scales, weight_scales = _scales(torch, rows, 3), _scales(torch, outer, 4)
+    room = torch.full((rows + 1, outer + 3), 7.0, dtype=getattr(torch, dtype), device="cuda")
+    out = binding.kq8_product(codes, scales, weight, weight_scales, out=room[:rows, :outer])
+    assert torch.equal(out.cpu(), _want(torch, codes, scales, weight, weight_scales, None, out.dtype))
+    assert (room[rows] == 7).all() and (room[:, outer:] == 7).all()
+
+
 @pytest.mark.parametrize("rows, inner, outer", [(1, 1000, 100), (16, 129, 70), (40, 333, 200), (130, 1000, 131), (300, 777, 301)])
 @pytest.mark.parametrize("layout", range(6))
 def test_products_with_strides(gpu, rows, inner, outer, layout):
