@@ -26,14 +26,17 @@ __device__ __forceinline__ i32x4 load16(const int8_t *p)
     if constexpr (ALIGNED) return *reinterpret_cast<const i32x4 *>(p);
     else return *reinterpret_cast<const i32x4_anywhere *>(p);
 }
-// The same of a row of `inner` integers, `count` of which are from p on (any number; zeros behind them).  The row's last integers come with one load that ends
-// where the row does, and are moved to their place.
-template <bool ALIGNED>
-__device__ __forceinline__ i32x4 load16(const int8_t *p, int count, unsigned inner)
+// The same of a row of `inner` integers, `count` of which are from p on (any number; zeros behind them), in two steps, so that the first can be far ahead of
+// the second.  The row's last integers come with one load that ends where the row does, and are then moved to their place.
+__device__ __forceinline__ i32x4 ask16(const int8_t *p, int count, unsigned inner)
 {
-    if (count >= 16) return load16<ALIGNED>(p);
     i32x4 v = {0, 0, 0, 0};
-    if (count <= 0) return v;
+    if (count > 0 && inner >= 16) v = load16<false>(count >= 16 ? p : p - (16 - inner % 16));
+    return v;
+}
+__device__ __forceinline__ i32x4 take16(i32x4 v, const int8_t *p, int count, unsigned inner)
+{
+    if (count <= 0 || count >= 16) return v;
     if (inner < 16) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -41,12 +44,12 @@ __device__ __forceinline__ i32x4 load16(const int8_t *p, int count, unsigned inn
         return v;
     }
     const unsigned by = 16 - inner % 16;    // bytes that come too early: alike in all lanes
-    v = load16<false>(p - by);
     if (by & 8) v = i32x4{v[2], v[3], 0, 0};
     if (by & 4) v = i32x4{v[1], v[2], v[3], 0};
     auto moved = [&](int high, int low) { return (int)__builtin_amdgcn_alignbyte((uint32_t)high, (uint32_t)low, by & 3); };
     return i32x4{moved(v[1], v[0]), moved(v[2], v[1]), moved(v[3], v[2]), moved(0, v[3])};
 }
+__device__ __forceinline__ i32x4 load16(const int8_t *p, int count, unsigned inner) { return take16(ask16(p, count, inner), p, count, inner); }
 
 // What leaves a block: results, or (SUMS) the sums of its part of the inner dimension, as the bits of Float32.
 enum Out { BF16 = 0, F32 = 1, SUMS = 2 };

@@ -95,7 +95,7 @@ __global__ __launch_bounds__(64 * kWaves) void q8_few_kernel(Operands a, const E
         for (unsigned u = 0; u < kSteps; ++u)
             if (first + kSteps + u < mine) wf[u] = load16<true>(w + (wave + (first + kSteps + u) * kWaves) * 64);
     }
-    if (steps % kWaves == wave && a.inner % 64 != 0) multiply(load16<true>(w + steps * 64, (int)a.inner - (int)(steps * 64 + k), a.inner), steps);
+    if (steps % kWaves == wave && a.inner % 64 != 0) multiply(load16(w + steps * 64, (int)a.inner - (int)(steps * 64 + k), a.inner), steps);
     *reinterpret_cast<i32x4 *>(&part[wave][lane % 16][lane / 16 * 4]) = sum;
     __syncthreads();
     a.x_scale = scales;
