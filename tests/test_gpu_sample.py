@@ -87,6 +87,55 @@ def test_settings_of_each_row(gpu, dtype, rows, vocabulary):
     assert got.tolist() == [_token(z[r], un[r], **{n: v[r].item() for n, v in values.items()}) for r in range(rows)]
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows, vocabulary", [(61, 40001), (60, 65536), (33, 70003), (259, 33000)])
+def test_many_long_rows(gpu, dtype, rows, vocabulary):
+    """Chunks of 32768 logits, the last of a row full, short or of one vector; greedy rows, empty ones and others in one call, twice with the same workspace."""
+    torch, binding = gpu
+    rng = np.random.default_rng(vocabulary)
+    logits, u = _logits(torch, rows, vocabulary, dtype, rows), _uniform(torch, rows, 1)
+    logits[3] = -float("inf")
+    logits[4, -1] = float("nan")
+    logits[5, :-1] = -float("inf")
+    logits[6, : vocabulary // 2] = -float("inf")
+    values = {"temperature": rng.choice([0.0, 0.5, 1.0, 8.0], rows).astype(np.float32), "top_k": rng.choice([0, 0, 1, 40, 5000], rows).astype(np.int32),
+              "top_p": rng.choice([1.0, 0.9, 0.5], rows).astype(np.float32), "min_p": rng.choice([0.0, 0.0, 0.02], rows).astype(np.float32)}
+    settings = {n: torch.from_numpy(v).cuda() for n, v in values.items()}
+    z, un = logits.float().cpu().numpy(), u.cpu().numpy()
+    want = [_token(z[r], un[r], **{n: v[r].item() for n, v in values.items()}) for r in range(rows)]
+    assert want[3] == want[4] == -1 and want[5] == vocabulary - 1
+    graph, out = torch.cuda.CUDAGraph(), torch.empty(rows, dtype=torch.int64, device="cuda")
+    binding.ksample(logits, u, out=out, **settings)
+    assert out.tolist() == want
+    with torch.cuda.graph(graph):
+        binding.ksample(logits, u, out=out, **settings)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        assert out.tolist() == want
+
+
+@pytest.mark.parametrize("vocabulary", [100, 1500, 9000, 32768])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+def test_few_tokens_of_top_k(gpu, oracle, vocabulary, cap):
+    """What top-k leaves with others near it: ties over its end, masked tokens, rows with fewer tokens than it asks for, every other setting behind it."""
+    torch, binding = gpu
+    logits = _logits(torch, 7, vocabulary, "float32", vocabulary)
+    logits[1] = logits[1].round()
+    logits[2, torch.arange(vocabulary, device="cuda") % 3 != 0] = -float("inf")
+    logits[3, 10:] = -float("inf")
+    logits[4] = logits[4] * 1e-4 + 5
+    logits[5] = 0
+    logits[5, : vocabulary // 4] = -700.0               # of no weight
+    z = logits.cpu().numpy() if cap == 0 else _capped(oracle, logits.cpu().numpy(), cap, False)
+    for i, settings in enumerate([dict(top_k=2), dict(top_k=30), dict(top_k=60, top_p=0.8), dict(top_k=40, min_p=0.3), dict(top_k=500, temperature=4.0, top_p=0.97, min_p=0.01),
+                                  dict(top_k=513), dict(top_k=99, temperature=0.02), dict(top_k=20, top_p=0.0), dict(top_k=45, min_p=1.0)]):
+        u = _uniform(torch, 7, i)
+        un = u.cpu().numpy()
+        got = binding.ksample(logits, u, cap=cap, **settings).tolist()
+        assert got == [_token(z[r], un[r], **settings) for r in range(7)], settings
+
+
 @pytest.mark.parametrize("vocabulary", [3000, 30000, 70000])
 def test_ties_flat_rows_and_outliers(gpu, vocabulary):
     """Rows that crowd one bin: equal logits, two values, a flat row under one outlier, differences at the last bit."""
