@@ -14,9 +14,13 @@ using namespace ktanh_q8;
 namespace {
 
 // ------------------------------------------------------------------------------------ tiles
-// Products of many rows.  A block of four wavefronts has TO output channels and TT rows, each wavefront a quarter of it (two by two).  Tiles of 128
-// integers of the inner dimension come into LDS by direct loads, in two places; operands are read a step of 32 integers ahead of the products
-// that take them, and the next tile but one is asked for between the last products of a tile, when its place has been read.
+// Products of many rows.  A block of four wavefronts has TO output channels and TT rows, each wavefront a quarter of it (two by two, or four along the
+// channels where the rows are 32).  Tiles of 128 integers of the inner dimension come into LDS by direct loads, into a ring of PLACES; operands are read a step
+// of 32 integers ahead of the products that take them, and the place of a tile is filled again between its last products, when it has been read.
+//
+// What bounds it: with many rows the matrix cores and the clock under them (8192 x 16384 x 4096 477 us, 2300 TOP/s, 58 % of the cycles at 1.75 GHz; its
+// operands pass LDS, 1 KB for 64 products at 256 by 256, where 128 by 128 needs twice that); with few rows the weights' way from memory (64 x 4096 x 16384 13.4 us from
+// the last-level cache, 5.2 TB/s, 19 from memory; 24 x 2048 x 50000 21 us, 5.0 TB/s).
 //
 // Rows of a tile are 128 bytes, half of the width of LDS.  Chunks of 16 bytes change places with bits 1 to 3 of their row's number, so that sixteen
 // neighbouring rows at one chunk, which are read at once, lie in different banks.
@@ -262,7 +266,7 @@ __global__ __launch_bounds__(256, PLACES * (TO + TT) * kDeep > 81920 ? 1 : 2) vo
 // ------------------------------------------------------------------------------------ a shared inner dimension
 // A block has OT output channels and TT rows, and its W wavefronts share the inner dimension in steps of 64 integers: wavefront s takes the steps
 // s, s + W, ..., so that the block reads whole cache lines.  Operands go from memory to the matrix cores' registers; the wavefronts' sums
-// meet in LDS.
+// meet in LDS.  Bound by latency and the weights' way from memory: 1 x 4096 x 4096 takes 5.5 us from the last-level cache (3.1 TB/s, launch included), 64 x 1024 x 1024 3.4.
 template <unsigned OT, unsigned TT, unsigned W, Out OUT, bool ALIGNED>
 __global__ __launch_bounds__(64 * W) void q8_shared_inner_kernel(Operands a)
 {
@@ -341,7 +345,8 @@ __global__ __launch_bounds__(64 * W) void q8_shared_inner_kernel(Operands a)
 }
 
 // ------------------------------------------------------------------------------------ parts joined
-// The sums of the parts of the inner dimension added up, scaled and stored; a chunk of 16 bytes to a lane.
+// The sums of the parts of the inner dimension added up, scaled and stored; a chunk of 16 bytes to a lane.  Bound by memory and its launch: 4 parts of
+// 512 x 1024 take 3 us.
 template <Out OUT>
 __global__ __launch_bounds__(256) void q8_join_kernel(Operands a, const int *sums, unsigned parts)
 {

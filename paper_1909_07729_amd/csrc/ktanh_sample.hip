@@ -13,7 +13,11 @@
 // A block holds up to 32768 logits in registers.  Rows of no more take one launch, and are read once.  Longer ones are cut into chunks and take
 // three: the chunks' largest logits, their bins, and their tokens of the bins that hold answers, among which the row's last block chooses.
 // Sums over the bins and over the listed tokens are formed once, with barriers; questions are then searches that every wavefront makes for
-// itself, with none.
+// itself, with none.  Where top-k leaves few tokens they are all listed, and nothing else is needed.
+//
+// What bounds it: in a row of its own the steps' latencies, one behind the other (one row of 32000: top-k 50 and top-p 0.95 in 12.3 us, top-p alone in 21.6, greedy in
+// 6.5); in many the vector instructions, 20 a logit for its cap alone (64 rows of 131072: 41 us uncapped, 57 capped: ends 13.6, bins 18.2, answers 28.4).  The
+// logits themselves, 17 or 34 MB, are 3 to 5 us of each pass.
 #include "ktanh_codes.h"
 #include "ktanh_stream_impl.h"
 
