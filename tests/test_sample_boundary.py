@@ -62,7 +62,7 @@ def test_entry_points_refuse(binding):
 def test_workspace(binding):
     size = binding.load_library().ksample_workspace
     assert size(_shape(binding, vocabulary=32768)) == 0 and size(_shape(binding, rows=0, vocabulary=40000)) == 0
-    assert size(_shape(binding, vocabulary=32769)) == 4 * 5 * (1024 * 8 + 20) + 4 * (2048 * 8 + 4)
+    assert size(_shape(binding, vocabulary=32769)) == 4 * 5 * (1024 * 8 + 20) + 4 * (2048 * 8 + 8)
 
 
 def test_binding_refuses(binding):
