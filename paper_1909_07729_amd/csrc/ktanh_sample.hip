@@ -15,7 +15,7 @@
 // Sums over the bins and over the listed tokens are formed once, with barriers; questions are then searches that every wavefront makes for
 // itself, with none.  Where top-k leaves few tokens they are all listed, and nothing else is needed.
 //
-// What bounds it: in a row of its own the steps' latencies, one behind the other (one row of 32000: top-k 50 and top-p 0.95 in 12.3 us, top-p alone in 21.6, greedy in
+// What bounds it: in a row of its own the steps' latencies, one behind the other (one row of 32000: top-k 50 and top-p 0.95 in 10.9 us, top-p alone in 21.6, greedy in
 // 6.5); in many the vector instructions, 20 a logit for its cap alone (64 rows of 131072: 41 us uncapped, 57 capped: ends 13.6, bins 18.2, answers 28.4).  The
 // logits themselves, 17 or 34 MB, are 3 to 5 us of each pass.
 #include "ktanh_codes.h"
@@ -382,10 +382,11 @@ __device__ __forceinline__ Ends met(Ends e)
 }
 
 template <class SOURCE>
-__device__ __forceinline__ Ends ends_of(SOURCE &source, Shared &sh)
+__device__ __forceinline__ Ends ends_of(SOURCE &source, float &lane_top, Shared &sh)
 {
     Ends e = kNoEnds;
     source.each([&](float z, unsigned) { e.meet(z, z == -INFINITY ? INFINITY : z, __float_as_uint(z) & 0x7FFFFFFFu); });
+    lane_top = e.top;
     e = met(e);
     if (threadIdx.x % 64 == 0) {
         sh.top[threadIdx.x / 64] = e.top;
@@ -487,6 +488,13 @@ __device__ __forceinline__ u64 packed(double power, double part)
     return ((u64)__double_as_longlong(__builtin_fma(power, part, 0x1p52)) & 0xFFFFFFFFFFFFFull) | kOneToken;      // at most 1.003 2^32
 }
 
+// The largest logits of lanes as a source: the k-th largest of them is no larger than the k-th largest of all.
+struct Tops {
+    float z;
+    template <class F>
+    __device__ __forceinline__ void each(F f) const { f(z, 0u); }
+};
+
 // Where top-k leaves few tokens, the ones that may be among them, and how many they are: by counts alone, which cost less than weights.
 template <class SOURCE>
 __device__ __forceinline__ Near nearest(SOURCE &source, const Ends &e, uint32_t k, uint32_t &tokens, Shared &sh)
@@ -551,7 +559,7 @@ __device__ __forceinline__ void list_flagged(SOURCE &source, const Weights &w, f
     __syncthreads();
 }
 
-// The near tokens, at most kListed, into sh.list, unsorted.
+// The near tokens into sh.list, unsorted, as far as they are at most kListed; sh.listed: how many they are.
 template <class SOURCE>
 __device__ __forceinline__ void list_near(SOURCE &source, const Weights &w, const Near &near, Shared &sh)
 {
@@ -559,7 +567,8 @@ __device__ __forceinline__ void list_near(SOURCE &source, const Weights &w, cons
     __syncthreads();
     source.each([&](float z, unsigned i) {
         if (!near(z) || !(w.depth_of(z) < kFar)) return;
-        sh.list[atomicAdd(&sh.listed, 1u)] = place_of(key_of(z), i);
+        const unsigned at = atomicAdd(&sh.listed, 1u);
+        if (at < kListed) sh.list[at] = place_of(key_of(z), i);
     });
     __syncthreads();
 }
@@ -860,22 +869,35 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, KtLutPac
     const OnTheWay<ELEM, E> raw(static_cast<const ELEM *>(a.logits) + blockIdx.x * a.row, 0, a.vocabulary);
     const Settings s = settings_of(a, blockIdx.x);
     Held<ELEM, CAP, WIDE, E> held(raw, a.cap, tab);
-    const Ends e = ends_of(held, sh);
+    float lane_top;
+    const Ends e = ends_of(held, lane_top, sh);
     long long token = -1;
     if (!e.empty()) {
         if (s.greedy) {
             token = first_of(held, e.top, sh);
         } else {
             const Weights w(e, s.scale);
+            fill_powers(sh);
             Near near = kAll;
+            bool few = false;
             uint32_t tokens = ~0u;
-            if (s.top_k <= kListed && s.top_k < a.vocabulary) near = nearest(held, e, s.top_k, tokens, sh);
-            const bool few = tokens <= kRanked;
+            if (E == kMost && s.top_k <= kRanked / 2) {
+                // counting the lanes' largest alone, which mostly leaves little more than is asked for (one row of 32000: 50 in 11.0 us, 200 in 15.6; with all
+                // logits counted 12.8 and 16.5; rows that have fewer logits than lanes would be counted twice)
+                Tops tops{lane_top};
+                near = nearest(tops, e, s.top_k, tokens, sh);
+                if (!near.all()) {
+                    list_near(held, w, near, sh);
+                    few = uniform(sh.listed) <= kRanked;
+                }
+            }
+            if (!few && s.top_k <= kListed && s.top_k < a.vocabulary) {
+                near = nearest(held, e, s.top_k, tokens, sh);
+                few = tokens <= kRanked;
+                if (few) list_near(held, w, near, sh);
+            }
             Questions questions(w, s, sh, 0);
-            if (few) {
-                fill_powers(sh);
-                list_near(held, w, near, sh);
-            } else {
+            if (!few) {
                 if (!near.all()) held.keep(near);
                 fill_bins(held, w, s.reach, sh);
                 questions.by_min = uniform(sh.by_min);
@@ -943,7 +965,8 @@ __global__ __launch_bounds__(kThreads) void sample_ends_kernel(SampleArgs a, KtL
     const Where at = chunk_of<E>(a);
     const OnTheWay<ELEM, E> raw(static_cast<const ELEM *>(a.logits) + at.row * a.row, at.first, at.end);
     Held<ELEM, CAP, WIDE, E> held(raw, a.cap, tab);
-    const Ends e = ends_of(held, sh);
+    float lane_top;
+    const Ends e = ends_of(held, lane_top, sh);
     const uint32_t first = settings_of(a, at.row).greedy ? first_of(held, e.top, sh) : 0u;
     if (threadIdx.x == 0) {
         a.ends[blockIdx.x] = float4{e.top, e.low, __uint_as_float(e.widest), __uint_as_float(first)};
