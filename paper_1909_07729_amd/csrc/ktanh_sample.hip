@@ -169,14 +169,6 @@ struct Held {
             }
         }
     }
-    // The others are masked from here on.
-    __device__ __forceinline__ void keep(const Near &near)
-    {
-#pragma unroll
-        for (unsigned v = 0; v < E / N; ++v)
-#pragma unroll
-            for (unsigned i = 0; i < N; ++i) z[v][i] = near(z[v][i]) ? z[v][i] : -INFINITY;
-    }
     __device__ __forceinline__ unsigned place(unsigned v) const { return first + (v * kThreads + threadIdx.x) * N; }
     // f(z, index) for each, by every lane of a block.  What f makes of a logit is made again in the next pass, and not kept.
     template <class F>
@@ -204,7 +196,6 @@ struct Read {
     unsigned end;
     float cap;
     const LaneTable &tab;
-    Near near;
 
     template <class F>
     __device__ __forceinline__ void each(F f) const
@@ -215,7 +206,7 @@ struct Read {
             uint32_t u = at < end ? (uint32_t)from[at] : 0u;
             if constexpr (sizeof(ELEM) == 2) u <<= 16;
             const float z = logit_of<CAP, WIDE>(__uint_as_float(u), at < end, cap, tab);
-            f(near.all() || near(z) ? z : -INFINITY, at);
+            f(z, at);
         }
     }
 };
@@ -495,7 +486,8 @@ struct Tops {
     __device__ __forceinline__ void each(F f) const { f(z, 0u); }
 };
 
-// Where top-k leaves few tokens, the ones that may be among them, and how many they are: by counts alone, which cost less than weights.
+// Which tokens may be among the first k, and how many these are: by counts alone, which cost less than weights where they are few (one row of 32000: 50
+// in 12.8 us, 20.3 by weights; 1000 in 28.1, by weights 24.3).
 template <class SOURCE>
 __device__ __forceinline__ Near nearest(SOURCE &source, const Ends &e, uint32_t k, uint32_t &tokens, Shared &sh)
 {
@@ -878,27 +870,28 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, KtLutPac
         } else {
             const Weights w(e, s.scale);
             fill_powers(sh);
-            Near near = kAll;
+            // Where all that top-k leaves, with what is near its last, are at most kRanked tokens, they are listed, and nothing else is needed.
             bool few = false;
-            uint32_t tokens = ~0u;
-            if (E == kMost && s.top_k <= kRanked / 2) {
-                // counting the lanes' largest alone, which mostly leaves little more than is asked for (one row of 32000: 50 in 11.0 us, 200 in 15.6; with all
-                // logits counted 12.8 and 16.5; rows that have fewer logits than lanes would be counted twice)
-                Tops tops{lane_top};
-                near = nearest(tops, e, s.top_k, tokens, sh);
-                if (!near.all()) {
-                    list_near(held, w, near, sh);
-                    few = uniform(sh.listed) <= kRanked;
+            if (s.top_k <= kRanked / 2 && s.top_k < a.vocabulary) {
+                uint32_t tokens;
+                if (E == kMost) {
+                    // counting the lanes' largest alone mostly leaves little more than is asked for (one row of 32000: 50 in 11.0 us, 200 in 15.3; with all
+                    // logits counted 12.8 and 16.5; rows with few logits for each lane would be counted twice)
+                    Tops tops{lane_top};
+                    const Near near = nearest(tops, e, s.top_k, tokens, sh);
+                    if (!near.all()) {
+                        list_near(held, w, near, sh);
+                        few = uniform(sh.listed) <= kRanked;
+                    }
                 }
-            }
-            if (!few && s.top_k <= kListed && s.top_k < a.vocabulary) {
-                near = nearest(held, e, s.top_k, tokens, sh);
-                few = tokens <= kRanked;
-                if (few) list_near(held, w, near, sh);
+                if (!few) {
+                    const Near near = nearest(held, e, s.top_k, tokens, sh);
+                    few = tokens <= kRanked;
+                    if (few) list_near(held, w, near, sh);
+                }
             }
             Questions questions(w, s, sh, 0);
             if (!few) {
-                if (!near.all()) held.keep(near);
                 fill_bins(held, w, s.reach, sh);
                 questions.by_min = uniform(sh.by_min);
                 questions.add_up((uint32_t)(sh.bins[threadIdx.x] >> 48), sh.bins[threadIdx.x] & kMassBits);
@@ -908,7 +901,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a, KtLutPac
             const unsigned n = uniform(sh.listed);
             finish_list(w, n, sh);
             // another list than the plan's, if one is needed, comes from memory: the registers are the questions'
-            Read<ELEM, CAP, WIDE> read{static_cast<const ELEM *>(a.logits) + blockIdx.x * a.row, a.vocabulary, a.cap, tab, near};
+            Read<ELEM, CAP, WIDE> read{static_cast<const ELEM *>(a.logits) + blockIdx.x * a.row, a.vocabulary, a.cap, tab};
             if (!few) token = questions.choose(read);
             else if (threadIdx.x < 64) token = choose_listed(w, s, n, sh);
         }
@@ -1040,7 +1033,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_answer_kernel(SampleArgs a
     const unsigned listed = uniform(__hip_atomic_load(&a.listed[at.row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)), n = listed < kListed ? listed : kListed;
     for (unsigned i = threadIdx.x; i < n; i += kThreads) sh.list[i] = __hip_atomic_load(&list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     finish_list(w, n, sh);
-    Read<ELEM, CAP, WIDE> read{from, a.vocabulary, a.cap, tab, kAll};
+    Read<ELEM, CAP, WIDE> read{from, a.vocabulary, a.cap, tab};
     const long long token = questions.choose(read);
     if (threadIdx.x == 0) a.tokens[at.row] = token;
 }
