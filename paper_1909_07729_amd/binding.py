@@ -660,6 +660,8 @@ def _keep8_backward(name, dy, codes, scales, rebuild, dx, y, lut, stream, dtypes
     _check_checkpoint(codes, scales, dy.numel())
     dx = _like(dx, dy, dtypes, "dx", stream)
     y = _like(y, dy, dtypes, "y", stream) if rebuild or y is not None else None
+    if y is not None and y.numel() != 0 and y.data_ptr() == dx.data_ptr():
+        raise ValueError("dx and y are the same memory")
     _check_here(dy, codes, scales, dx, y)
     st = getattr(load_library(), name)(dy.data_ptr(), codes.data_ptr(), scales.data_ptr(), dx.data_ptr(), None if y is None else y.data_ptr(),
                                        dy.numel(), _lut_arg(lut), _stream_handle(stream))

@@ -277,3 +277,19 @@ def test_both_host_paths_give_the_same(gpu, monkeypatch):
         binding.kgelu_keep8(x.double())
     with pytest.raises(ValueError):
         binding.kgelu_keep8_backward(x.bfloat16(), *binding.kgelu_keep8(x[:1].bfloat16())[1:])
+
+
+def test_one_output_for_both_is_refused(gpu):
+    torch, binding = gpu[:2]
+    x = torch.randn(1000, device="cuda").bfloat16()
+    _, codes, scales = binding.kgelu_keep8(x)
+    with pytest.raises(ValueError):
+        binding.kgelu_keep8_backward(x, codes, scales, dx=x, y=x)
+    with pytest.raises(ValueError):
+        both = torch.empty_like(x)
+        binding.kgelu_keep8_backward(x, codes, scales, dx=both, y=both)
+    dx, y = binding.kgelu_keep8_backward(x, codes, scales, rebuild=True)
+    dy = x.clone()
+    assert all(torch.equal(a, b) for a, b in zip(binding.kgelu_keep8_backward(dy, codes, scales, dx=dy, y=torch.empty_like(x)), (dx, y)))
+    dy = x.clone()
+    assert all(torch.equal(a, b) for a, b in zip(binding.kgelu_keep8_backward(dy, codes, scales, dx=torch.empty_like(x), y=dy), (dx, y)))
