@@ -493,7 +493,7 @@ __device__ __forceinline__ Near nearest(SOURCE &source, const Ends &e, uint32_t 
 {
     tokens = ~0u;
     const float width = e.top - e.low;
-    if (!(width > 0.f && width < 3e38f)) return kAll;     // all alike, or an infinity
+    if (!(width > 0x1p-110f && width < 3e38f)) return kAll;     // all alike, too near each other for a quotient in Float32, or an infinity
     const float by = (float)(kBins - 1) / width;
     sh.count[threadIdx.x] = 0;
     __syncthreads();
