@@ -35,6 +35,7 @@ constexpr unsigned kMost = 32, kFew = 8;                // logits of a lane
 constexpr unsigned kSteps = 7;                          // log2 of the finest bins to a factor of two
 constexpr double kFar = 73.5;                           // KSAMPLE_MOST 2^-kFar < 2^-53: what lies beyond does not reach a sum of doubles
 constexpr double kLog2e = 1.4426950408889634;
+constexpr float kHottest = 3e38f;                       // the highest temperature
 
 typedef unsigned long long u64;
 
@@ -91,7 +92,8 @@ __device__ __forceinline__ float in_unit(float v, float otherwise) { return v >=
 __device__ __forceinline__ Settings settings_of(const SampleArgs &a, unsigned row)
 {
     Settings s;
-    const float t = a.temperature != nullptr ? a.temperature[row] : a.one_temperature;
+    float t = a.temperature != nullptr ? a.temperature[row] : a.one_temperature;
+    t = t > kHottest ? kHottest : t;
     const int32_t k = a.top_k != nullptr ? a.top_k[row] : (int32_t)a.one_top_k;
     s.top_k = k <= 0 || (uint32_t)k > a.vocabulary ? a.vocabulary : (uint32_t)k;
     s.greedy = !(t > 0.f) || s.top_k == 1;

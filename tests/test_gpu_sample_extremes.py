@@ -49,3 +49,17 @@ def test_capped_rows_of_tiny_spread(gpu, oracle, vocabulary):
     for top_k in (2, 50, 256):
         got = binding.ksample(logits, u, cap=30.0, top_k=top_k).tolist()
         assert got == [_token(z[r], un[r], top_k=top_k) for r in range(len(z))]
+
+
+@pytest.mark.parametrize("vocabulary", [2, 300, 9000, 40000])
+def test_temperatures_beyond_the_highest(gpu, vocabulary):
+    """Rows' own temperatures above 3e38 are 3e38, at which logits of that size still differ: weights of 1 and e^-2."""
+    torch, binding = gpu
+    rng = np.random.default_rng(vocabulary)
+    z = np.where(rng.random((6, vocabulary)) < 0.5, np.float32(3e38), np.float32(-3e38)).astype(np.float32)
+    z[:, 0], z[:, -1] = 3e38, -3e38
+    temperature = np.array([3e38, np.inf, 3.1e38, np.finfo(np.float32).max, np.inf, np.inf], np.float32)
+    u = np.array([0.7, 0.7, 0.8, 0.9, 0.3, 0.95], np.float32)
+    got = binding.ksample(torch.from_numpy(z).cuda(), torch.from_numpy(u).cuda(), temperature=torch.from_numpy(temperature).cuda()).tolist()
+    assert got == [_token(z[r], u[r], temperature=3e38) for r in range(6)]
+    assert vocabulary > 2 or got[:2] == [0, 0]
