@@ -357,7 +357,10 @@ ktanh_status_t kgelu64_f32_keep8_backward(const float *dy, const int8_t *codes, 
  * kq8_product: out[t][o] = (float(sum over i of codes[t][i] * w[o][i]) * scales[t]) * w_scale[o] + bias[o], the sum exact, the rest Float32,
  * one rounding per operation, and one more for BFloat16 outputs.
  *
- * kq8_linear: kq8_rows and kq8_product in one call, with the same results. */
+ * kq8_linear: kq8_rows and kq8_product in one call, with the same results.
+ *
+ * Blocks read while others write: what a call writes shares no memory with what it reads, `out == x` included (KT_ERR_SHAPE).  Rows of one
+ * stride may lie beside each other in one buffer. */
 enum { KQ8_NONE = 0, KQ8_SWISH = 1, KQ8_GELU = 2 };
 
 typedef struct kq8_shape {

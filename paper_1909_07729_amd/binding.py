@@ -783,7 +783,7 @@ _Q8_TYPES = (torch.bfloat16, torch.float32)
 def kq8_rows(x, activation=None, codes=None, scales=None, lut=None, stream=None, _entry="kq8_rows"):
     """Rows in 8-bit integers: x [rows, columns] BFloat16 or Float32, any row stride, or ``kswish`` / ``kgelu`` of it, as (codes int8 [rows,
     columns], scales Float32 [rows]); a code stands for code * scale of its row.  Weights are brought to 8 bits with it as well, their rows
-    being the output channels.  Rows of codes that are allocated here start at multiples of 16 bytes.
+    being the output channels.  Rows of codes that are allocated here start at multiples of 16 bytes.  Given outputs share no memory with x.
     """
     _check_matrix(x, _Q8_TYPES, "x")
     rows, columns = x.shape
@@ -838,7 +838,7 @@ def _pointer(t):
 def kq8_product(codes, scales, weight, weight_scales, bias=None, *, out_dtype=torch.bfloat16, out=None, stream=None):
     """(codes @ weight.T) * scales * weight_scales + bias: codes int8 [rows, inner] with scales Float32 [rows], weight int8 [outer, inner] with
     scales Float32 [outer], bias Float32 [outer] or None, any row strides; the sums are exact.  Returns out [rows, outer], BFloat16 or
-    Float32 (``out``'s own type where it is given)."""
+    Float32 (``out``'s own type where it is given; it shares no memory with the operands)."""
     if stream is None and _host is not None:
         done = _host.q8_product(codes, scales, weight, weight_scales, bias, out_dtype, out)
         if done is not None:
@@ -861,7 +861,7 @@ def kq8_product(codes, scales, weight, weight_scales, bias=None, *, out_dtype=to
 
 def kq8_linear(x, weight, weight_scales, bias=None, *, activation=None, out_dtype=torch.bfloat16, out=None, lut=None, stream=None,
                _entry="kq8_linear"):
-    """``kq8_product`` of ``kq8_rows(x, activation)``, in one call: x [rows, inner] BFloat16 or Float32, any row stride."""
+    """``kq8_product`` of ``kq8_rows(x, activation)``, in one call: x [rows, inner] BFloat16 or Float32, any row stride; not ``out``."""
     if stream is None and _host is not None:
         done = _host.q8_linear(x, weight, weight_scales, bias, out_dtype, out, activation, lut, _entry == "kq8_linear64")
         if done is not None:

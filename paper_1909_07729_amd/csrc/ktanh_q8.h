@@ -13,6 +13,32 @@ constexpr size_t kMostStride = (size_t)1 << 40;
 inline bool off(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 inline size_t stride(size_t rows, size_t step) { return rows > 1 ? step : 0; }     // that of a single row means nothing
 
+// Memory that a call reads or writes: rows of `bytes`, `step` bytes apart.
+struct Memory {
+    const void *at;
+    size_t rows, bytes, step;
+};
+inline Memory vector(const void *p, size_t bytes) { return Memory{p, 1, bytes, 0}; }
+inline Memory matrix(const void *p, size_t rows, size_t row, size_t step, size_t size)
+{
+    return step == 0 || rows == 1 ? vector(p, row * size) : Memory{p, rows, row * size, step * size};
+}
+
+// Whether no byte is in both.  Where their spans cross, of those that are known to be apart by their columns: rows of one stride (or a single row), each
+// beside the other's.  Blocks of a launch read while others write, so that no shared byte would be safe.
+inline bool apart(const Memory &a, const Memory &b)
+{
+    if (a.at == nullptr || b.at == nullptr || a.rows == 0 || b.rows == 0 || a.bytes == 0 || b.bytes == 0) return true;
+    typedef unsigned __int128 wide;
+    const wide a0 = reinterpret_cast<uintptr_t>(a.at), b0 = reinterpret_cast<uintptr_t>(b.at);
+    if (a0 + (wide)(a.rows - 1) * a.step + a.bytes <= b0 || b0 + (wide)(b.rows - 1) * b.step + b.bytes <= a0) return true;
+    if (a.rows == 1 && b.rows == 1) return false;
+    const size_t step = a.rows == 1 ? b.step : a.step;
+    if (b.rows != 1 && b.step != step) return false;
+    const size_t ahead = (size_t)((b0 % step + step - a0 % step) % step);       // of a row of b behind the nearest start of one of a's
+    return ahead >= a.bytes && ahead + b.bytes <= step;
+}
+
 inline ktanh_status_t check_rows(const kq8_shape_t *s)
 {
     if (s == nullptr) return KT_ERR_NULL;

@@ -466,6 +466,17 @@ ktanh_status_t check_weights(const kq8_shape_t *s, const int8_t *w, const float 
     return KT_OK;
 }
 
+// Whether a product's results share no memory with what it reads: x of x_size bytes an element, weights, scales, bias.
+bool out_apart(const kq8_shape_t &s, const void *x, size_t x_size, const float *scales, const int8_t *w, const float *w_scale, const float *bias, const void *out)
+{
+    const Memory to = matrix(out, s.rows, s.outer, stride(s.rows, s.out_row), s.out_f32 ? 4 : 2);
+    return apart(to, matrix(x, s.rows, s.inner, stride(s.rows, s.x_row), x_size)) && apart(to, matrix(w, s.outer, s.inner, stride(s.outer, s.w_row), 1)) &&
+           apart(to, vector(scales, s.rows * sizeof(float))) && apart(to, vector(w_scale, s.outer * sizeof(float))) && apart(to, vector(bias, s.outer * sizeof(float)));
+}
+
+ktanh_status_t check_table(const ktanh_lut_t *lut) { return lut == nullptr ? KT_OK : ktanh_lut_validate(lut); }
+ktanh_status_t check_table(const ktanh_lut64_t *lut) { return lut == nullptr ? KT_OK : ktanh_lut64_validate(lut); }
+
 // Few short rows go to integers within the product's launch (ktanh_q8_few.hip).
 ktanh_status_t launch_few(const kq8_shape_t &s, const void *x, const int8_t *w, const float *w_scale, const float *bias, void *out, const ktanh_lut_t *lut,
                           ktanh_stream_t stream, bool *done)
@@ -490,6 +501,10 @@ ktanh_status_t linear_entry(const kq8_shape_t *s, const void *x, const int8_t *w
     st = check_weights(s, w, w_scale, bias, out);
     if (st != KT_OK) return st;
     if (off(x, s->x_f32 ? 4 : 2) || off(workspace, 16)) return KT_ERR_ALIGN;
+    if (!out_apart(*s, x, s->x_f32 ? 4 : 2, nullptr, w, w_scale, bias, out)) {
+        st = s->activation == KQ8_NONE ? KT_OK : check_table(lut);
+        return st != KT_OK ? st : KT_ERR_SHAPE;
+    }
     bool done = false;
     st = launch_few(*s, x, w, w_scale, bias, out, lut, stream, &done);
     if (done) return st;
@@ -516,6 +531,7 @@ extern "C" ktanh_status_t kq8_product(const kq8_shape_t *shape, const int8_t *co
     if (st != KT_OK) return st;
     if (off(scales, 4) || off(workspace, 16)) return KT_ERR_ALIGN;
     if (workspace == nullptr && sums_bytes(*shape) != 0) return KT_ERR_NULL;
+    if (!out_apart(*shape, codes, 1, scales, w, w_scale, bias, out)) return KT_ERR_SHAPE;
     return launch_product(*shape, codes, shape->x_row, scales, w, w_scale, bias, out, workspace, stream);
 }
 

@@ -109,6 +109,9 @@ ktanh_status_t launch_rows(const kq8_shape_t &s, const void *x, int8_t *codes, s
     if (st != KT_OK) return st;
     const size_t x_row = stride(s.rows, s.x_row);
     codes_row = stride(s.rows, codes_row);
+    const Memory in = matrix(x, s.rows, s.inner, x_row, sizeof(ELEM)), out = matrix(codes, s.rows, s.inner, codes_row, 1),
+                 scaling = vector(scales, s.rows * sizeof(float));
+    if (!apart(in, out) || !apart(in, scaling) || !apart(out, scaling)) return KT_ERR_SHAPE;
     const bool aligned = !off(x, 16) && x_row % N == 0 && !off(codes, N) && codes_row % N == 0;
     auto launch = [&](auto kernel, unsigned threads) {
         return launch_checked(kernel, (unsigned)s.rows, threads, stream, static_cast<const ELEM *>(x), (unsigned long long)x_row, (unsigned)s.inner, codes,
