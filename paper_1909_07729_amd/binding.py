@@ -653,7 +653,7 @@ def _keep8(name, x, out, codes, scales, lut, stream, dtypes):
 
 def _keep8_backward(name, dy, codes, scales, rebuild, dx, y, lut, stream, dtypes):
     if stream is None and _host is not None and dx is None and y is None:
-        done = _host.keep8_backward(_KEEP8_INDEX[name[:-len("_backward")]], dy, codes, scales, rebuild is True, lut)
+        done = _host.keep8_backward(_KEEP8_INDEX[name[:-len("_backward")]], dy, codes, scales, bool(rebuild), lut)
         if done is not None:
             return done
     _check(dy, dtypes, "dy")
