@@ -308,7 +308,7 @@ ktanh_status_t klstm_cell64_backward(const uint16_t *gates, const float *c_prev,
  *   scales     device, Float32, one for each group: n / KTANH_KEEP8_GROUP rounded up
  * backward: dx is that of kswish_backward / kgelu_backward at x8, bit for bit, and y, where it is not NULL, that of kswish / kgelu
  * at x8 (which the gradient of the weights behind the activation takes, so that the activation's output need not be kept either).
- * dx or y may be dy, but not both.  Alignment: elements of in, out, dy, dx and y, and 4 bytes of scales (KT_ERR_ALIGN); tensors that start on
+ * dx or y may be dy; y == dx is refused (KT_ERR_SHAPE).  Alignment: elements of in, out, dy, dx and y, and 4 bytes of scales (KT_ERR_ALIGN); tensors that start on
  * 16 bytes are faster by up to a fifth.  Up to 2^34 - 256 Float32 or 2^35 - 512 BFloat16 elements (KT_ERR_SHAPE). */
 #define KTANH_KEEP8_GROUP 128
 ktanh_status_t kswish_keep8(const uint16_t *in, uint16_t *out, int8_t *codes, float *scales, size_t n, const ktanh_lut_t *lut,

@@ -214,6 +214,7 @@ ktanh_status_t launch_keep8_backward(const void *dy, const int8_t *codes, const 
     KtLutPack pack;
     st = pack_for(lut, sizeof(ELEM) == 4, &pack);
     if (st != KT_OK) return st;
+    if (y == dx) return KT_ERR_SHAPE;
     auto launch = [&](auto kernel) {
         return launch_checked(kernel, tiles, kBlock, stream, static_cast<const ELEM *>(dy), codes, scales, static_cast<ELEM *>(dx),
                               (unsigned long long)n, static_cast<ELEM *>(y), pack);
