@@ -302,6 +302,7 @@ ktanh_status_t klstm_cell64_backward(const uint16_t *gates, const float *c_prev,
  * place of two or four, and that pass.  Each KTANH_KEEP8_GROUP consecutive values (the last ones may be fewer) share a Float32 scale;
  * with m the largest finite magnitude among them, in Float32 operations rounded to nearest even:
  *   scale = m / 127,   code = round(x * (127 / m));     m below 2^-120: scale 0 and codes 0
+ * (Float32 tensors: scales of at most 0x1.020406p121, the largest whose 127-fold is finite.)
  * A code stands for x8 = code * scale, rounded to the tensor's type; -128 stands for an infinity or a NaN, and is read as a NaN.
  *   in, out    device, n elements each; out is that of kswish / kgelu, bit for bit, and may be in
  *   codes      device, n bytes

@@ -40,6 +40,10 @@ __device__ __forceinline__ uint32_t largest_of_group(uint32_t m)
     return m;
 }
 
+// 127 times it is the last Float32 but one: a group with the last, which stands for masked places, would have a scale whose 127-fold is infinite, and so NaNs
+// for gradients.
+constexpr float kMostScale = 0x1.020406p121f;
+
 // The codes of a lane's vector, and its group's scale.
 template <class ELEM>
 __device__ __forceinline__ uint2 codes_of(uint4 v, float &scale)
@@ -61,6 +65,7 @@ __device__ __forceinline__ uint2 codes_of(uint4 v, float &scale)
     const float top = __uint_as_float(largest_of_group<kGroupLanes<ELEM>>(m));
     const float inverse = inverse_of(top);
     scale = scale_of(top);
+    if constexpr (sizeof(ELEM) == 4) scale = __builtin_fminf(scale, kMostScale);
     uint32_t q[N];
 #pragma unroll
     for (unsigned i = 0; i < N; ++i) q[i] = rounded_code(x[i], inverse);
