@@ -9,6 +9,7 @@ namespace ktanh_q8 {
 constexpr size_t kMostRows = (size_t)1 << 30;       // rows, and output channels
 constexpr size_t kMostInner = 131071;               // 128 * 128 * 131071 < 2^31: every sum of products fits 32 bits
 constexpr size_t kMostStride = (size_t)1 << 40;
+constexpr size_t kMostLanes = ((size_t)1 << 32) - 1;    // of a launch
 
 inline bool off(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 inline size_t stride(size_t rows, size_t step) { return rows > 1 ? step : 0; }     // that of a single row means nothing

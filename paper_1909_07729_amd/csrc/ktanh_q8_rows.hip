@@ -113,9 +113,17 @@ ktanh_status_t launch_rows(const kq8_shape_t &s, const void *x, int8_t *codes, s
                  scaling = vector(scales, s.rows * sizeof(float));
     if (!apart(in, out) || !apart(in, scaling) || !apart(out, scaling)) return KT_ERR_SHAPE;
     const bool aligned = !off(x, 16) && x_row % N == 0 && !off(codes, N) && codes_row % N == 0;
+    // a launch has fewer than 2^32 lanes
     auto launch = [&](auto kernel, unsigned threads) {
-        return launch_checked(kernel, (unsigned)s.rows, threads, stream, static_cast<const ELEM *>(x), (unsigned long long)x_row, (unsigned)s.inner, codes,
-                              (unsigned long long)codes_row, scales, pack);
+        const size_t most = kMostLanes / threads;
+        for (size_t first = 0; first < s.rows; first += most) {
+            const size_t rows = s.rows - first < most ? s.rows - first : most;
+            const ktanh_status_t done =
+                launch_checked(kernel, (unsigned)rows, threads, stream, static_cast<const ELEM *>(x) + first * x_row, (unsigned long long)x_row, (unsigned)s.inner,
+                               codes + first * codes_row, (unsigned long long)codes_row, scales + first, pack);
+            if (done != KT_OK) return done;
+        }
+        return KT_OK;
     };
     auto of = [&](auto on_grid) {
         constexpr bool ALIGNED = decltype(on_grid)::value;
