@@ -122,6 +122,29 @@ inline Plan plan_of(size_t rows, size_t inner, size_t outer)
     return best;
 }
 
+// The kernel that a product takes: tiles; or, where operands are off the 16-byte grid or a tile's offsets would leave 32 bits, blocks of 16 by 16 or of 64 by 64 whose
+// wavefronts share the inner dimension.  Large ones from two of the small ones on each CU on (300 x 300 x 300 6.3 us against 10.5, 2000 x 200 x 5000 258 against 41).
+enum Way { TILES, SHARED16, SHARED64 };
+inline Way way_of(const Plan &plan, size_t rows, size_t outer, bool aligned, size_t x_row, size_t w_row)
+{
+    if (aligned && plan.kind != SHARED && x_row < (size_t)1 << 23 && w_row < (size_t)1 << 23) return TILES;
+    return plan.kind == SHARED || rows <= 32 || ((rows + 15) / 16) * ((outer + 15) / 16) <= 512 ? SHARED16 : SHARED64;
+}
+
+// Rows and channels of one launch: fewer than 2^32 lanes, and where the grid has two dimensions at most 65535 blocks of rows.
+struct Piece {
+    size_t rows, outer;
+};
+inline Piece piece_of(Way way, const Plan &plan, size_t rows, size_t outer)
+{
+    const size_t over = way == TILES ? kTiles[plan.kind].over : way == SHARED16 ? 16 : 64, across = way == TILES ? kTiles[plan.kind].across : over;
+    const size_t most = kMostLanes / (way == SHARED16 ? 512 : 256) / (way == TILES ? plan.parts : 1);
+    size_t channels = (outer + over - 1) / over;
+    if (channels > most) channels = most;
+    const size_t row_blocks = way == TILES ? most / channels : 65535;
+    return Piece{rows < row_blocks * across ? rows : row_blocks * across, outer < channels * over ? outer : channels * over};
+}
+
 // A call's workspace: codes that it makes itself (rows of a multiple of 16 bytes, then the scales), and the sums of parts.
 inline size_t padded(size_t inner) { return (inner + 15) / 16 * 16; }
 inline size_t rows_bytes(const kq8_shape_t &s) { return (s.rows * (padded(s.inner) + sizeof(float)) + 15) / 16 * 16; }

@@ -384,40 +384,16 @@ __global__ __launch_bounds__(256) void q8_join_kernel(Operands a, const int *sum
 
 namespace ktanh_q8 {
 
-// Arguments have been checked.
-ktanh_status_t launch_product(const kq8_shape_t &s, const int8_t *x, size_t x_row, const float *x_scale, const int8_t *w, const float *w_scale,
-                              const float *bias, void *out, void *workspace, ktanh_stream_t stream)
+// One launch's rows and channels, with a second launch for the sums of parts.
+static ktanh_status_t launch_piece(const Operands &a, const Plan &plan, Way way, bool aligned, bool roomy, bool out_f32, void *workspace, ktanh_stream_t stream)
 {
-    Operands a;
-    a.x = x;
-    a.w = w;
-    a.x_row = stride(s.rows, x_row);
-    a.w_row = stride(s.outer, s.w_row);
-    a.x_scale = x_scale;
-    a.w_scale = w_scale;
-    a.bias = bias;
-    a.out = out;
-    a.out_row = stride(s.rows, s.out_row);
-    a.rows = (unsigned)s.rows;
-    a.outer = (unsigned)s.outer;
-    a.inner = (unsigned)s.inner;
-    const bool aligned = !off(x, 16) && a.x_row % 16 == 0 && !off(w, 16) && a.w_row % 16 == 0;
-    auto launch = [&](auto kernel, unsigned threads, unsigned ot, unsigned tt) {
-        const size_t over = (s.outer + ot - 1) / ot, across = (s.rows + tt - 1) / tt;
-        if (over * threads >= (1ull << 32) || across > 65535) return KT_ERR_SHAPE;
-        void *args[] = {&a};
-        return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)over, (unsigned)across), dim3(threads), args, 0,
-                               static_cast<hipStream_t>(stream)) == hipSuccess ? KT_OK : KT_ERR_HIP;
-    };
-    const Plan plan = plan_of(s.rows, s.inner, s.outer);
-    // a tile's offsets are 32-bit
-    if (aligned && plan.kind != SHARED && a.x_row < 1u << 23 && a.w_row < 1u << 23) {
-        auto tiled = [&](auto out) {
+    if (way == TILES) {
+        auto tiled = [&](const Operands &to, auto out) {
             constexpr Out O = decltype(out)::value;
             auto launch = [&](auto kernel) {
                 const Tile t = kTiles[plan.kind];
-                const unsigned over = (a.outer + t.over - 1) / t.over, across = (a.rows + t.across - 1) / t.across;
-                return launch_checked(kernel, over * across * plan.parts, 256, stream, a, over, across, plan.parts);
+                const unsigned over = (to.outer + t.over - 1) / t.over, across = (to.rows + t.across - 1) / t.across;
+                return launch_checked(kernel, over * across * plan.parts, 256, stream, to, over, across, plan.parts);
             };
             if constexpr (O != SUMS) {
                 if (plan.kind == T256) return launch(q8_tile_kernel<256, 256, 2, O>);
@@ -425,33 +401,67 @@ ktanh_status_t launch_product(const kq8_shape_t &s, const int8_t *x, size_t x_ro
             }
             switch (plan.kind) {
             // a third place where a CU has no second block anyway: 1024 x 4096 x 4096 26.3 us, 34.8 with two
-            case T128: return blocks_of(T128, s.rows, s.outer, plan.parts) <= 256 ? launch(q8_tile_kernel<128, 128, 3, O>) : launch(q8_tile_kernel<128, 128, 2, O>);
+            case T128: return roomy ? launch(q8_tile_kernel<128, 128, 3, O>) : launch(q8_tile_kernel<128, 128, 2, O>);
             case T128_64: return launch(q8_tile_kernel<128, 64, 3, O>);
             case T128_32: return launch(q8_tile_kernel<128, 32, 3, O>);
             default: return launch(q8_tile_kernel<64, 64, 4, O>);
             }
         };
-        if (plan.parts == 1) return s.out_f32 ? tiled(std::integral_constant<Out, F32>()) : tiled(std::integral_constant<Out, BF16>());
-        Operands last = a;
-        a.out = workspace;
-        a.out_row = a.outer;
-        const ktanh_status_t st = tiled(std::integral_constant<Out, SUMS>());
+        if (plan.parts == 1) return out_f32 ? tiled(a, std::integral_constant<Out, F32>()) : tiled(a, std::integral_constant<Out, BF16>());
+        Operands sums = a;
+        sums.out = workspace;
+        sums.out_row = a.outer;
+        const ktanh_status_t st = tiled(sums, std::integral_constant<Out, SUMS>());
         if (st != KT_OK) return st;
         auto join = [&](auto kernel, unsigned each) {
             const unsigned long long chunks = (unsigned long long)((a.outer + each - 1) / each) * a.rows;
-            return launch_checked(kernel, (unsigned)((chunks + 255) / 256), 256, stream, last, static_cast<const int *>(workspace), plan.parts);
+            return launch_checked(kernel, (unsigned)((chunks + 255) / 256), 256, stream, a, static_cast<const int *>(workspace), plan.parts);
         };
-        return s.out_f32 ? join(q8_join_kernel<F32>, 4) : join(q8_join_kernel<BF16>, 8);
+        return out_f32 ? join(q8_join_kernel<F32>, 4) : join(q8_join_kernel<BF16>, 8);
     }
+    auto launch = [&](auto kernel, unsigned threads, unsigned each) {
+        Operands to = a;
+        void *args[] = {&to};
+        return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((a.outer + each - 1) / each, (a.rows + each - 1) / each), dim3(threads), args, 0,
+                               static_cast<hipStream_t>(stream)) == hipSuccess ? KT_OK : KT_ERR_HIP;
+    };
     auto sized = [&](auto out_type, auto on_grid) {
         constexpr Out O = decltype(out_type)::value;
         constexpr bool A = decltype(on_grid)::value;
-        // rows off the 16-byte grid: larger blocks from two of the small ones on each CU on (300 x 300 x 300 6.3 us against 10.5, 2000 x 200 x 5000 258 against 41)
-        if (plan.kind == SHARED || s.rows <= 32 || ((s.rows + 15) / 16) * ((s.outer + 15) / 16) <= 512) return launch(q8_shared_inner_kernel<16, 16, 8, O, A>, 512, 16, 16);
-        return launch(q8_shared_inner_kernel<64, 64, 4, O, A>, 256, 64, 64);
+        return way == SHARED16 ? launch(q8_shared_inner_kernel<16, 16, 8, O, A>, 512, 16) : launch(q8_shared_inner_kernel<64, 64, 4, O, A>, 256, 64);
     };
     auto typed = [&](auto out_type) { return aligned ? sized(out_type, std::true_type()) : sized(out_type, std::false_type()); };
-    return s.out_f32 ? typed(std::integral_constant<Out, F32>()) : typed(std::integral_constant<Out, BF16>());
+    return out_f32 ? typed(std::integral_constant<Out, F32>()) : typed(std::integral_constant<Out, BF16>());
+}
+
+// Arguments have been checked.
+ktanh_status_t launch_product(const kq8_shape_t &s, const int8_t *x, size_t x_row, const float *x_scale, const int8_t *w, const float *w_scale,
+                              const float *bias, void *out, void *workspace, ktanh_stream_t stream)
+{
+    Operands a;
+    a.x_row = stride(s.rows, x_row);
+    a.w_row = stride(s.outer, s.w_row);
+    a.out_row = stride(s.rows, s.out_row);
+    a.inner = (unsigned)s.inner;
+    const bool aligned = !off(x, 16) && a.x_row % 16 == 0 && !off(w, 16) && a.w_row % 16 == 0;
+    const Plan plan = plan_of(s.rows, s.inner, s.outer);
+    const Way way = way_of(plan, s.rows, s.outer, aligned, a.x_row, a.w_row);
+    const bool roomy = blocks_of(T128, s.rows, s.outer, plan.parts) <= 256;
+    const Piece piece = piece_of(way, plan, s.rows, s.outer);
+    for (size_t t = 0; t < s.rows; t += piece.rows)
+        for (size_t o = 0; o < s.outer; o += piece.outer) {
+            a.rows = (unsigned)(s.rows - t < piece.rows ? s.rows - t : piece.rows);
+            a.outer = (unsigned)(s.outer - o < piece.outer ? s.outer - o : piece.outer);
+            a.x = x + t * a.x_row;
+            a.x_scale = x_scale + t;
+            a.w = w + o * a.w_row;
+            a.w_scale = w_scale + o;
+            a.bias = bias != nullptr ? bias + o : nullptr;
+            a.out = static_cast<char *>(out) + (t * a.out_row + o) * (s.out_f32 ? sizeof(float) : sizeof(uint16_t));
+            const ktanh_status_t st = launch_piece(a, plan, way, aligned, roomy, s.out_f32 != 0, workspace, stream);
+            if (st != KT_OK) return st;
+        }
+    return KT_OK;
 }
 
 }  // namespace ktanh_q8

@@ -34,3 +34,45 @@ def test_rows(gpu, rows, inner):
         else:
             want = binding.kq8_rows(x[:1], "gelu")
             assert (codes[at:end] == want[0]).all() and (scales[at:end] == want[1]).all()
+
+
+# rows, inner, outer, whether on the 16-byte grid: tests/test_q8_ways.py holds these to more than one launch
+PRODUCTS = [(5000000, 17, 1, 0), (4200000, 17, 70, 0), (1, 17, (1 << 27) + 100, 0), (1 << 30, 16, 1, 1)]
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("rows, inner, outer, aligned", PRODUCTS)
+def test_products(gpu, rows, inner, outer, aligned, dtype):
+    """Against the definition, a part of the results at a time: exact sums, Float32 operations."""
+    torch, binding = gpu
+    gen = torch.Generator("cuda").manual_seed(2)
+
+    def operand(count):     # many channels, or very many rows, are the same memory
+        same = count > 1 << 24
+        room = torch.randint(-128, 128, (16 + (1 if same else count) * inner,), generator=gen, dtype=torch.int8, device="cuda")
+        t = room[0 if aligned else 1:][:(1 if same else count) * inner].view(-1, inner)
+        return t.expand(count, -1) if same else t
+    codes, weight = operand(rows), operand(outer)
+    scales, weight_scales, bias = (torch.rand(n, generator=gen, device="cuda") + 0.5 for n in (rows, outer, outer))
+    out = torch.full((rows, outer), 7.0, dtype=getattr(torch, dtype), device="cuda")
+    binding.kq8_product(codes, scales, weight, weight_scales, bias, out=out)
+    part = max(1, (1 << 24) // max(1, min(outer, 1 << 20)))
+    channels = 1 << 24
+    for t in range(0, rows, part):
+        for o in range(0, outer, channels):
+            rows_here, channels_here = slice(t, min(t + part, rows)), slice(o, min(o + channels, outer))
+            sums = codes[rows_here].float() @ weight[channels_here].float().t()         # below 2^24: exact in Float32
+            want = sums * scales[rows_here, None] * weight_scales[channels_here] + bias[channels_here]
+            assert torch.equal(out[rows_here, channels_here], want.to(out.dtype)), (t, o)
+
+
+def test_linear(gpu):
+    torch, binding = gpu
+    rows, inner, outer = (1 << 26) + 5, 4, 2
+    gen = torch.Generator("cuda").manual_seed(3)
+    x = torch.randn((rows, inner), generator=gen, device="cuda").bfloat16()
+    weight = torch.randint(-128, 128, (outer, inner), generator=gen, dtype=torch.int8, device="cuda")
+    weight_scales = torch.rand(outer, generator=gen, device="cuda")
+    out = binding.kq8_linear(x, weight, weight_scales, activation="swish")
+    for t in range(0, rows, 1 << 22):
+        assert torch.equal(out[t:t + (1 << 22)], binding.kq8_linear(x[t:t + (1 << 22)], weight, weight_scales, activation="swish"))
