@@ -45,3 +45,16 @@ def test_the_tests_of_many_rows_and_channels_take_several_launches(ways):
     from test_gpu_q8_many import PRODUCTS
     for (rows, inner, outer, aligned), (way, *_, piece_rows, piece_outer) in zip(PRODUCTS, ways([(*p, 17 - p[3], 17 - p[3]) for p in PRODUCTS]), strict=True):
         assert (way == TILES) == bool(aligned) and (piece_rows < rows or piece_outer < outer)
+
+
+def test_the_tests_off_the_grid_reach_the_blocks_of_64(ways):
+    from test_gpu_q8_off_grid import FAR, OFF_GRID
+
+    def on_grid(inner, apart, start):
+        return start % 16 == 0 and (inner + apart) % 16 == 0
+    calls = [(r, i, o, int(on_grid(i, xa, xs) and on_grid(i, wa, ws)), i + xa, i + wa) for r, i, o, xa, xs, wa, ws in OFF_GRID]
+    assert not any(c[3] for c in calls)
+    far = [(r, i, o, 1, x, w) for r, i, o, x, w in FAR]
+    assert all(x % 16 == w % 16 == 0 for *_, x, w in FAR)
+    assert all(way == SHARED64 for way, *_ in ways(calls + far))
+    assert ways([(600, 1001, 1000, 0, 1008, 1001)])[0][0] == SHARED64
