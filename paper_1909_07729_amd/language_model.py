@@ -201,12 +201,13 @@ def generate(model, prompts, count, piece=24, page=16, weights=None, sample=None
         ends = offsets[1:].long() - 1
         done = torch.tensor([len(p) > 0 for p in parts], device="cuda")
         last[done] = logits[ends[done]]
+    sampled = binding.ksample if model.intervals == 32 else binding.ksample64
     tokens, seen = [], [last.clone()]
     for _ in range(count):
         if sample is None:
             tokens.append(seen[-1].argmax(-1))
         else:
-            tokens.append(binding.ksample(seen[-1], torch.rand(sequences, generator=generator, device="cuda"), **sample))
+            tokens.append(sampled(seen[-1], torch.rand(sequences, generator=generator, device="cuda"), **sample))
         seen.append(model.serve(tokens[-1], cache, weights=weights))
     return torch.stack(tokens, 1), torch.stack(seen[:-1], 1)
 
