@@ -209,7 +209,10 @@ def generate(model, prompts, count, piece=24, page=16, weights=None, sample=None
         else:
             tokens.append(sampled(seen[-1], torch.rand(sequences, generator=generator, device="cuda"), **sample))
         seen.append(model.serve(tokens[-1], cache, weights=weights))
-    return torch.stack(tokens, 1), torch.stack(seen[:-1], 1)
+    tokens = torch.stack(tokens, 1)
+    if sample is not None and (tokens < 0).any():       # which the embedding takes as its last
+        raise ValueError("a step's logits hold a NaN: no token was chosen")
+    return tokens, torch.stack(seen[:-1], 1)
 
 
 def main(argv=None):

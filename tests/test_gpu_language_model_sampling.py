@@ -23,3 +23,15 @@ def test_the_cap_goes_through_the_models_table(lm, monkeypatch, intervals):
     numbers = torch.Generator("cuda").manual_seed(4)
     for i in range(7):
         assert torch.equal(made[:, i], mine(logits[:, i], torch.rand(6, generator=numbers, device="cuda"), **sample))
+
+
+@pytest.mark.parametrize("weights", [False, True])
+def test_logits_without_a_token(lm, weights):
+    """``ksample`` answers -1, which an embedding would take as its last token."""
+    torch, module = lm
+    torch.manual_seed(1)
+    model, prompts = module.LanguageModel(), _prompts(torch, module, 3)
+    with torch.no_grad():
+        model.head[5, 7] = float("nan")
+    with pytest.raises(ValueError):
+        module.generate(model, prompts, 4, sample={"temperature": 0.9, "top_k": 20}, weights=module.Weights8(model) if weights else None)
