@@ -59,6 +59,7 @@ class _ActivatedLinear(torch.autograd.Function):
         return F.linear(y, weight)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dz):
         codes, scales, weight = ctx.saved_tensors
         backward = binding.kgelu64_keep8_backward if ctx.wide else binding.kgelu_keep8_backward
