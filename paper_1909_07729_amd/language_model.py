@@ -191,6 +191,8 @@ def generate(model, prompts, count, piece=24, page=16, weights=None, sample=None
     """Continuation of prompts (a list of token tensors) by `count` tokens; (tokens [prompts, count], logits of each step).  Greedy, or with `sample`,
     the settings of ``binding.ksample``, from uniform numbers of `generator` (on the GPU).  `weights`: as for ``serve``."""
     sequences, longest = len(prompts), max(len(p) for p in prompts)
+    if any(len(p) == 0 for p in prompts):
+        raise ValueError("a prompt without tokens has no logits to continue from")
     if longest + count > model.cos.shape[0]:
         raise ValueError(f"the model has angles for {model.cos.shape[0]} tokens")
     cache = PagedCache(len(model.qkv), sequences, longest + count, model.kv_heads, model.dim, page)
