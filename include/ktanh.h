@@ -530,9 +530,10 @@ ktanh_status_t kcap_append(const kcap_shape_t *shape, const kcap_pages_t *cache,
  *   top_k  keeps the first top_k tokens (0, or more than there are: all)
  *   top_p  of these the fewest first ones with G(r) >= top_p * G(top_k), one at least
  *   min_p  of these those with w >= min_p
- * and of the n that are left the token is the first with G(r) > uniform * G(n).  A temperature of 0 or below takes the first token by rank.
- * Weights and their sums are held in 64 bits, in an order that does not change from call to call; tokens with a weight below e^-51 of the
- * first's do not count.
+ * and of the n that are left the token is the first with G(r) > uniform * G(n).  A temperature of 0 takes the first token by rank.
+ * Weights are formed in 64 bits.  Those of a bin (at most a factor of two) are added up as multiples of 2^-32 of the power of two above them, bins and
+ * ranked tokens in 64 bits, so that a number within about 2^-32 of a border may fall to either side, the same in each call; tokens with a
+ * weight below e^-51 of the first's do not count.
  * A row with a NaN, or with nothing but masked tokens, has the token -1.  With a logit of +infinity only such tokens have a weight. */
 #define KSAMPLE_MOST 1048575
 
@@ -548,12 +549,12 @@ typedef struct ksample_shape {
 
 /*   logits     device, elements aligned (KT_ERR_ALIGN)
  *   uniform    device, Float32 [rows], in [0, 1); values outside, here and in the rows' own settings, are taken as the nearest inside
- *              (1: the last of the kept tokens), and NaNs as 0 (top_p: 1)
+ *              (1: the last of the kept tokens; a temperature below 0: 0), and NaNs as 0 (top_p: 1)
  *   temperature, top_p, min_p   device, Float32 [rows], or NULL         top_k   device, int32 [rows], or NULL
  *   tokens     device, out: int64 [rows]
  *   workspace  device, 16-byte aligned, ksample_workspace bytes; unused and may be NULL where that is 0 (up to 32768 tokens).  What it holds
  *              before does not matter; calls that may run at once need one each
- * KT_ERR_SHAPE: sizes or settings out of range, a cap below 1e-30.  `lut` is read where cap > 0. */
+ * KT_ERR_SHAPE: sizes or settings of all rows out of range (a negative temperature among them), a cap below 1e-30.  `lut` is read where cap > 0. */
 size_t ksample_workspace(const ksample_shape_t *shape);
 ktanh_status_t ksample(const ksample_shape_t *shape, const void *logits, const float *uniform, const float *temperature, const int32_t *top_k,
                        const float *top_p, const float *min_p, int64_t *tokens, void *workspace, const ktanh_lut_t *lut, ktanh_stream_t stream);

@@ -3,7 +3,8 @@
 // What the backward pass of Swish and GELU needs is the forward input.  Kept as it is it costs 2 or 4 bytes a value from the forward to
 // the backward pass; here it costs one, and 4 bytes for each 128 consecutive values (a group): with m the largest finite magnitude of
 // the group
-//   scale = m / 127,   code = round(x * (127 / m)),   and what the code stands for is code * scale, rounded to the tensor's type.
+//   scale = m / 127,   code = round(x * (127 / m)),   and what the code stands for is code * scale, rounded to the tensor's type
+// (the scale is held below where that is infinite).
 // The gradient is that of kswish_backward and kgelu_backward at the values that the codes stand for, operation for operation.  The code -128 stands
 // for an infinity or a NaN, whose gradient is a NaN in those calls too (Swish and GELU multiply it by a slope of zero); it is left out
 // of m, so that its neighbours keep their values.

@@ -70,6 +70,9 @@ inline ktanh_status_t check_product(const kq8_shape_t *s)
 //    64 x 4096 x 16384  64x64 19.2 | 128x64 22.9, SHARED 74.5   2048 x 4096 x 4096    128x128 41.1 | 192x256 52.9, 128x64 57.1
 //   128 x 4096 x 4096   64x64 11.1 | 128x64 14.0, SHARED 35.5   2048 x 4096 x 6144    192x256 54.2 | 256x256 65.5, 128x128 73.6
 //   128 x 1024 x 512    SHARED 3.4 | 64x64 5.1                  8192 x 16384 x 4096   256x256 481 | 128x128 536
+// What the model leaves out is the end of rows that fill no tile, with its two barriers and four steps that nothing hides: 777 x 1001 x 2003 takes 11.2 us where it says 6.3.
+// Between 128 and 1024 rows its choices are 1.7 to 2.6 times what memory and the matrix cores need: a block of four wavefronts to a CU is one to a SIMD, and nothing runs
+// while it waits for LDS and for its tile.
 enum Kind { T256, T192, T128, T128_64, T64, T128_32, SHARED };
 struct Tile {
     unsigned over, across;      // output channels, rows

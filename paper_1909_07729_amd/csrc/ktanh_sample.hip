@@ -1025,8 +1025,9 @@ __global__ __launch_bounds__(kThreads, 8) void sample_answer_kernel(SampleArgs a
     u64 *const list = a.list + at.row * (u64)kListed;
     for (unsigned i = threadIdx.x; i < mine; i += kThreads)
         if (sh.asked_bin + i < kListed) __hip_atomic_store(&list[sh.asked_bin + i], sh.list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    // These stores go to where all dies see them, and are there before the block counts as arrived.  A fence of the whole GPU would write every L2 back, each
-    // wavefront's once more: 64 rows of 131072 took 145 us with them.
+    // These stores go to where all dies see them, and are there before the block counts as arrived: on gfx950 agent-scope stores and
+    // loads carry sc1, with which they do not stop at the L2 of their die, and vmcnt counts a store until it is done.  The order rests on that and on the barrier, not on
+    // release and acquire: a fence of the whole GPU would write every L2 back, each wavefront's once more (64 rows of 131072 took 145 us with them).
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (threadIdx.x == 0) sh.asked = atomicAdd(&a.arrived[at.row], 1u) + 1 == a.chunks;

@@ -189,7 +189,8 @@ def train(model, steps, batch=16, longest=128, seed=0):
 @torch.no_grad()
 def generate(model, prompts, count, piece=24, page=16, weights=None, sample=None, generator=None):
     """Continuation of prompts (a list of token tensors) by `count` tokens; (tokens [prompts, count], logits of each step).  Greedy, or with `sample`,
-    the settings of ``binding.ksample``, from uniform numbers of `generator` (on the GPU).  `weights`: as for ``serve``."""
+    the settings of ``binding.ksample`` (``ksample64`` for a model with 64 intervals), from uniform numbers of `generator` (on the GPU).  `weights`: as for
+    ``serve``.  A step whose logits hold a NaN raises ValueError."""
     sequences, longest = len(prompts), max(len(p) for p in prompts)
     if any(len(p) == 0 for p in prompts):
         raise ValueError("a prompt without tokens has no logits to continue from")
